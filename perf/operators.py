@@ -86,8 +86,8 @@ def draw(rng):
     elif op == "reorder":
         beams, dtype = _log_int(rng, 2, 32), rng.choice(["bf16", "f32"])
         heads, width, tokens = rng.randint(1, 12), rng.choice([33, 64, 80, 96, 128, 250]), _log_int(rng, 1, 2048)
-        tensors = max(1, min(rng.randint(1, 32), 250_000_000 // (beams * heads * width * tokens)))
-        batch = _log_int(rng, 1, max(1, min(64, 500_000_000 // (tensors * beams * heads * width * tokens * 4))))
+        tensors = max(1, min(rng.randint(1, 32), 160_000_000 // (beams * heads * width * tokens)))
+        batch = _log_int(rng, 1, max(1, min(64, 300_000_000 // (tensors * beams * heads * width * tokens * 4))))
         case = _reorder("", batch, beams, rng.choice([beams, beams, rng.randint(1, beams)]), tensors, heads, tokens, width,
                         dtype, rng.choice([True, False]))
     elif op == "plan":
@@ -101,7 +101,7 @@ def draw(rng):
         case = _plan("", batch, beams, block, min(1 << 20, int(most * rng.uniform(0.9, 2.0)) + 64), width, held, append, fork)
     else:
         pairs, tensors, size = _log_int(rng, 1, 1500), rng.randint(1, 24), 16 * _log_int(rng, 4, 4096)
-        tensors = max(1, min(tensors, 3_000_000_000 // (size * (2 * pairs + 40))))
+        tensors = max(1, min(tensors, 1_500_000_000 // (size * (2 * pairs + 40))))
         case = _copy("", pairs, rng.choice([0.1, 0.5, 0.9]), tensors, 2 * pairs + rng.randint(1, 40), size,
                      rng.choice(["bf16", "f32"]))
     return {k: v for k, v in case.items() if k != "name"}
