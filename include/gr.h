@@ -48,6 +48,10 @@ extern "C" {
                                        selects was solved; gr_verify refuses such a block (token -1)       */
 #define GR_CHECK_FAILED          7  /* bounds-checked build of the library only: a kernel skipped an access
                                        outside an array's extent while it worked on this instance          */
+#define GR_NO_BLOCKS             8  /* gr_block_plan: the pool has too few free blocks for the row         */
+#define GR_ROW_FULL              9  /* gr_block_plan: more tokens than the row's table or the slot map hold */
+#define GR_BAD_ROW              10  /* gr_block_plan: a negative count, a length beyond the table, a parent outside
+                                       the group, or a block id outside the pool                            */
 
 /* host-side argument errors (return values) */
 #define GR_E_INVALID   (-1)  /* a size, temperature or option is out of range */
@@ -59,6 +63,8 @@ extern "C" {
 /* capacities */
 #define GR_MAX_SUPPORT 128   /* largest draft support for which the convex programs are solved */
 #define GR_MAX_DRAFTS  32    /* largest n                                                     */
+#define GR_MAX_BEAMS   32    /* largest number of hypotheses in a group                       */
+#define GR_MAX_SELECT  128   /* most continuations gr_beam_select returns for a group         */
 
 /*
  * Solver options (host struct, read during the call).  NULL selects the defaults.
@@ -291,6 +297,127 @@ int gr_read_rule(const void* params, int batch, int kcap, int* ids, int* block, 
  */
 int gr_read_slice(const void* params, const int* draft_tokens, int batch, int n, int* U, double* pi,
                   double* rho, int* status, void* stream);
+
+/*
+ * ------------------------------------------------------------------------------------------------
+ * Around the decoding step: beam search's selection (the other rule that turns logit rows into emitted
+ * tokens), and what a serving loop does with the outcome of either rule -- hypotheses, drafted or searched,
+ * go on from a parent's state, in dense states (gr_reorder_states) or in a paged cache (gr_block_plan,
+ * gr_copy_blocks).  (The paper has no counterpart.)  Conventions as above.
+ * ------------------------------------------------------------------------------------------------
+ *
+ * gr_beam_select -- the best continuations of every group of `beams` hypotheses.
+ *
+ * Of group b, hypothesis w and token v, with x = logits[b, w, v]:
+ *   total = scores[b, w] + x / temperature - log sum_v' exp(x' / temperature),
+ *   key   = total / L^length_penalty,  L = max(1, lengths[b, w] + 1)   (key = total without `lengths`);
+ * a finished hypothesis (done[b, w] != 0) has the one continuation `eos`, with total = scores[b, w] and
+ * L = max(1, lengths[b, w]); its logits are not read.  The `select` largest keys are returned in descending
+ * order; equal keys: the smaller w first, then the larger logit, then the smaller v.  Keys are compared as
+ * 64-bit values; where two hypotheses' continuations come so close that the streaming pass's sums may not tell
+ * them apart, their rows' sums are taken again in 64 bits.
+ *   logits   [batch, beams, V], dtype GR_F32 or GR_BF16: row (b, w) begins (b * beams + w) * ld elements after
+ *            the base pointer (aligned to the element), ld >= V.  -infinity masks a token: it is never returned, and
+ *            a row may be masked as a whole.  NaN or +infinity in a row that is read: GR_BAD_LOGITS.
+ *   scores   [batch, beams] float.  -infinity: there is no such hypothesis, its logits are not read.
+ *            NaN or +infinity: GR_BAD_LOGITS.
+ *   lengths  [batch, beams] int or NULL; |length_penalty| <= 32 (0 without lengths).
+ *   done     [batch, beams] bytes or NULL (no hypothesis is finished).  With `done`, eos must be a token id;
+ *            without, eos may be -1 (no token finishes a hypothesis).
+ *   1 <= beams <= GR_MAX_BEAMS, 1 <= select <= GR_MAX_SELECT, V <= 2^21, temperature > 0.
+ *   workspace   gr_beam_workspace_bytes() bytes, 16-byte aligned.
+ *   out_token, out_parent [batch, select] int; out_score [batch, select] float (total); out_length [batch,
+ *            select] int (L) or NULL; out_done [batch, select] bytes: the parent was finished or the token is
+ *            eos.  Places that no continuation is left for: token -1, parent -1, score -infinity, length 0,
+ *            done 0; all places of a group with GR_BAD_LOGITS.  None of them may be an input of the same call.
+ *   status   out [batch] GR_OK or GR_BAD_LOGITS.
+ */
+size_t gr_beam_workspace_bytes(int V, int beams, int select, int batch);
+int gr_beam_select(const void* logits, int dtype, int V, long long ld, int beams, int batch, float temperature,
+                   const float* scores, const int* lengths, const unsigned char* done, int eos,
+                   float length_penalty, int select, void* workspace, int* out_token, int* out_parent,
+                   float* out_score, int* out_length, unsigned char* out_done, int* status, void* stream);
+
+/*
+ * gr_reorder_states -- state j of group b becomes a copy of state parents[b, j] of that group, in `count`
+ * tensors of one layout (the layers' caches, recurrent states, drafted hidden states).
+ *
+ * A state is `parts` pieces (heads, say) of part_bytes bytes.  Piece p of state w of group b begins
+ * b * src_group + w * src_beam + p * src_part bytes after src[i], and likewise for dst[i].
+ *   src, dst   HOST arrays of `count` device pointers.  dst[i] == src[i] with equal strides reorders in place (any
+ *              mapping, cycles and repeated parents included); otherwise the memory of dst[i] must not overlap that of
+ *              any src.  The same dst twice (or two that begin less than part_bytes apart) is GR_E_INVALID, and so
+ *              are strides that make the pieces of a dst overlap.  Within src, groups, states and pieces may coincide
+ *              (stride 0), unless it is reordered in place.
+ *   parents    [batch, beams_out] int.  -1, or any number outside 0 .. beams_in - 1: that state is left as it was.
+ *   lengths    [batch, beams_in] int or NULL.  With it a piece is a run of tokens of token_bytes bytes each and only the
+ *              first lengths[b, parent] tokens of each piece are copied (clamped to what the piece holds); the
+ *              rest of dst stays as it was.  token_bytes must divide part_bytes.
+ *   1 <= beams_in, beams_out <= GR_MAX_BEAMS; in place beams_out <= beams_in.
+ * No workspace.  Any alignment works; pointers, strides and part_bytes that are multiples of 16 are fastest.
+ */
+typedef struct gr_state_layout {
+    int       batch, beams_in, beams_out, parts;
+    long long src_group, src_beam, src_part;
+    long long dst_group, dst_beam, dst_part;
+    long long part_bytes;
+    long long token_bytes;
+} gr_state_layout;
+int gr_reorder_states(const void* const* src, void* const* dst, int count, const gr_state_layout* layout,
+                      const int* parents, const int* lengths, void* stream);
+
+/*
+ * gr_block_plan -- block tables and slots of a paged cache for the next step, built on the device.
+ *
+ * A pool of num_blocks blocks of block_size tokens serves `rows` rows, each with a table of `width` block ids and
+ * a number of tokens: token t of row r lies in block table[r, t / block_size] at t % block_size.  Blocks may be
+ * shared between rows; refs[i] counts the rows that hold block i (0: free).  Rows form groups of `beams`.
+ * Per row r of a group, in one call:
+ *   1. it goes on from row parents[r] of its group (NULL: from itself; -1: from nothing, it holds no tokens then),
+ *      of which it keeps base = min(lengths[parent], keep[r]) tokens (keep NULL: all of them), and the blocks
+ *      they lie in; what it held otherwise is released.  Parents are read before any row changes.
+ *   2. append[r] tokens are added.  Where the first of them lands in a partly filled block that another row
+ *      holds too, the row gets a block of its own for it and the pair (copy_src, copy_dst) is listed, to be
+ *      copied (gr_copy_blocks) before the new tokens are written.  If every holder of the block is about to write to it,
+ *      the one with the most tokens in it (the lowest row of several) keeps it and only the others copy.
+ *   3. new blocks are the free ones with the smallest ids, taken in the order of the rows (the copy's first), those that
+ *      were released in this call among them.
+ * Rows that cannot be served keep their `base` tokens and blocks and get no new ones; status says why:
+ *   GR_ROW_FULL   more tokens than width * block_size, or more appended tokens up to and with this row than max_tokens;
+ *   GR_NO_BLOCKS  the row needs blocks, and up to and with it (counting all rows that are not GR_ROW_FULL or GR_BAD_ROW)
+ *                 more are needed than are free;
+ *   GR_BAD_ROW    append[r] < 0 (taken as 0), lengths[parent] outside 0 .. width * block_size (clamped), a parent outside
+ *                 -1 .. beams - 1 (taken as -1), or a held block id that the call reads and that is outside the pool.
+ *   keep[r] < 0 counts as 0.
+ *   table     in/out [rows, width] int.  Entries that a row no longer holds become -1.  (Start with -1 everywhere.)
+ *   lengths   in/out [rows] int;  refs in/out [num_blocks] int.   (Start with 0.)
+ *   slots     out [max_tokens] long long: slot (block * block_size + offset) of every appended token, row after row;
+ *             -1 for the tokens of rows that were not served and behind the last one.
+ *   positions out [max_tokens] int: index of the token within its row, -1 where slots is.
+ *   offsets   out [rows + 1] int: row r's tokens are offsets[r] .. offsets[r + 1] - 1 (by append as given, cut at max_tokens).
+ *   copy_src, copy_dst  out [rows] int, -1 where nothing is copied.
+ *   status    out [rows].
+ *   workspace gr_block_workspace_bytes() bytes, 16-byte aligned.
+ *   rows a multiple of beams, 1 <= beams <= GR_MAX_BEAMS (beams only matters with parents), rows <= 2^20,
+ *   rows * width < 2^31, num_blocks <= 2^26, width * block_size < 2^31.  The arrays must not overlap one another.
+ */
+size_t gr_block_workspace_bytes(int rows, int num_blocks);
+int gr_block_plan(int* table, int rows, int width, int beams, int block_size, int* lengths, int* refs, int num_blocks,
+                  const int* parents, const int* keep, const int* append, int max_tokens, void* workspace,
+                  long long* slots, int* positions, int* offsets, int* copy_src, int* copy_dst, int* status,
+                  void* stream);
+
+/*
+ * gr_copy_blocks -- block copy_dst[i] of every cache becomes a copy of block copy_src[i], for the listed pairs.
+ *   caches      HOST array of `count` device pointers; block k of a cache begins k * block_stride bytes after it and
+ *               is block_bytes long (block_stride >= block_bytes).  The same cache twice (or two that begin less than
+ *               block_bytes apart) is GR_E_INVALID.
+ *   copy_src, copy_dst  [pairs] int, as gr_block_plan writes them: a pair with an index outside 0 .. num_blocks - 1 (-1:
+ *               nothing to copy) is skipped.  Blocks that are copied to must be distinct and none may be copied from.
+ * No workspace.  Any alignment works; multiples of 16 are fastest.
+ */
+int gr_copy_blocks(void* const* caches, int count, int num_blocks, long long block_stride, long long block_bytes,
+                   const int* copy_src, const int* copy_dst, int pairs, void* stream);
 
 /* Text for a GR_* / GR_E_* code (host pointer to a static string). */
 const char* gr_strerror(int code);

@@ -20,6 +20,8 @@ GR_OK, GR_NOT_CONVERGED, GR_SUPPORT_TOO_LARGE, GR_BAD_LOGITS, GR_DRAFT_OUT_OF_SU
 GR_MAX_SUPPORT, GR_MAX_DRAFTS = 128, 32
 GR_STATIC_MAX_BATCH = 256
 GR_PARTIAL_RULE = 6
+GR_NO_BLOCKS, GR_ROW_FULL, GR_BAD_ROW = 8, 9, 10
+GR_MAX_BEAMS, GR_MAX_SELECT = 32, 128
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_HERE, "libgr_b200.so")
@@ -37,6 +39,13 @@ class Options(C.Structure):
     def __init__(self, tol: float = 3e-7, max_iters: int = 40, quad_step: float = 0.4, scan_done_event=None,
                  force_robust: int = 0, tau: float = 0.0):
         super().__init__(tol, max_iters, quad_step, scan_done_event, force_robust, tau)
+
+
+class StateLayout(C.Structure):
+    """gr_state_layout: where the pieces of a state lie, in bytes."""
+    _fields_ = ([(n, C.c_int) for n in ("batch", "beams_in", "beams_out", "parts")]
+                + [(n, C.c_longlong) for n in ("src_group", "src_beam", "src_part", "dst_group", "dst_beam", "dst_part",
+                                               "part_bytes", "token_bytes")])
 
 
 def library_path() -> str:
@@ -74,6 +83,22 @@ def load_library():
     lib.gr_read_rule.argtypes = [vp, C.c_int, C.c_int, ip, ip, dp, dp, dp, dp, vp]
     lib.gr_read_slice.restype = C.c_int
     lib.gr_read_slice.argtypes = [vp, ip, C.c_int, C.c_int, ip, dp, dp, ip, vp]
+    lib.gr_beam_workspace_bytes.restype = C.c_size_t
+    lib.gr_beam_workspace_bytes.argtypes = [C.c_int] * 4
+    lib.gr_beam_select.restype = C.c_int
+    lib.gr_beam_select.argtypes = [vp, C.c_int, C.c_int, C.c_longlong, C.c_int, C.c_int, C.c_float, fp, ip, vp, C.c_int,
+                                   C.c_float, C.c_int, vp, ip, ip, fp, ip, vp, ip, vp]
+    lib.gr_reorder_states.restype = C.c_int
+    lib.gr_reorder_states.argtypes = [C.POINTER(C.c_void_p), C.POINTER(C.c_void_p), C.c_int, C.POINTER(StateLayout), ip,
+                                      ip, vp]
+    lib.gr_block_workspace_bytes.restype = C.c_size_t
+    lib.gr_block_workspace_bytes.argtypes = [C.c_int] * 2
+    lib.gr_block_plan.restype = C.c_int
+    lib.gr_block_plan.argtypes = [ip, C.c_int, C.c_int, C.c_int, C.c_int, ip, ip, C.c_int, ip, ip, ip, C.c_int, vp, vp, ip,
+                                  ip, ip, ip, ip, vp]
+    lib.gr_copy_blocks.restype = C.c_int
+    lib.gr_copy_blocks.argtypes = [C.POINTER(C.c_void_p), C.c_int, C.c_int, C.c_longlong, C.c_longlong, ip, ip, C.c_int,
+                                   vp]
     lib.gr_strerror.restype = C.c_char_p
     lib.gr_strerror.argtypes = [C.c_int]
     _lib = lib
@@ -142,6 +167,46 @@ def gr_read_rule(params: int, batch: int, kcap: int, ids: int, block: int, w: in
 def gr_read_slice(params: int, draft_tokens: int, batch: int, n: int, U: int, pi: int, rho: int, status: int,
                   stream: int) -> int:
     return int(load_library().gr_read_slice(params, draft_tokens, batch, n, U, pi, rho, status, stream))
+
+
+def gr_beam_workspace_bytes(V: int, beams: int, select: int, batch: int) -> int:
+    return int(load_library().gr_beam_workspace_bytes(V, beams, select, batch))
+
+
+def gr_beam_select(logits: int, dtype: int, V: int, ld: int, beams: int, batch: int, temperature: float, scores: int,
+                   lengths: int, done: int, eos: int, length_penalty: float, select: int, workspace: int, out_token: int,
+                   out_parent: int, out_score: int, out_length: int, out_done: int, status: int, stream: int) -> int:
+    return int(load_library().gr_beam_select(logits, dtype, V, ld, beams, batch, temperature, scores, lengths, done, eos,
+                                             length_penalty, select, workspace, out_token, out_parent, out_score,
+                                             out_length, out_done, status, stream))
+
+
+def gr_reorder_states(src, dst, layout: Optional[StateLayout], parents: int, lengths: int, stream: int) -> int:
+    """src, dst: sequences of device addresses."""
+    n = len(src)
+    return int(load_library().gr_reorder_states((C.c_void_p * n)(*src), (C.c_void_p * n)(*dst), n,
+                                                C.byref(layout) if layout is not None else None, parents, lengths,
+                                                stream))
+
+
+def gr_block_workspace_bytes(rows: int, num_blocks: int) -> int:
+    return int(load_library().gr_block_workspace_bytes(rows, num_blocks))
+
+
+def gr_block_plan(table: int, rows: int, width: int, beams: int, block_size: int, lengths: int, refs: int,
+                  num_blocks: int, parents: int, keep: int, append: int, max_tokens: int, workspace: int, slots: int,
+                  positions: int, offsets: int, copy_src: int, copy_dst: int, status: int, stream: int) -> int:
+    return int(load_library().gr_block_plan(table, rows, width, beams, block_size, lengths, refs, num_blocks, parents,
+                                            keep, append, max_tokens, workspace, slots, positions, offsets, copy_src,
+                                            copy_dst, status, stream))
+
+
+def gr_copy_blocks(caches, num_blocks: int, block_stride: int, block_bytes: int, copy_src: int, copy_dst: int,
+                   pairs: int, stream: int) -> int:
+    """caches: a sequence of device addresses."""
+    n = len(caches)
+    return int(load_library().gr_copy_blocks((C.c_void_p * n)(*caches), n, num_blocks, block_stride, block_bytes,
+                                             copy_src, copy_dst, pairs, stream))
 
 
 # ---------------------------------------------------------------- torch tensors
@@ -385,3 +450,269 @@ def solve_verify_host(q_logits: torch.Tensor, p_logits: torch.Tensor, draft_toke
     out = torch.cat([t.view(torch.uint8) for t in (v.token, sv.alpha_star, v.status, v.accepted)]).cpu()
     token, alpha, status = (out[4 * B * i:4 * B * (i + 1)] for i in range(3))
     return token.view(torch.int32), out[12 * B:], alpha.view(torch.float32), status.view(torch.int32)
+
+
+# ---------------------------------------------------------------- around the decoding step
+
+def _need(t, what: str, dtype, shape=None, device=None, optional: bool = False):
+    """The address of a contiguous CUDA tensor of this type, shape and device (0 for None where that is allowed)."""
+    if t is None and optional:
+        return 0
+    kinds = dtype if isinstance(dtype, tuple) else (dtype,)
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.is_contiguous()) or t.dtype not in kinds:
+        raise GrError(f"{what}: expected a contiguous CUDA tensor of {' or '.join(str(k) for k in kinds)}")
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise GrError(f"{what}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
+    if device is not None and t.device != device:
+        raise GrError(f"{what}: on {t.device}, the other tensors on {device}")
+    return t.data_ptr()
+
+
+class _on:
+    """The tensors' device made current for the call; gives that device's current stream."""
+
+    def __init__(self, device):
+        self._guard = torch.cuda.device(device)
+
+    def __enter__(self) -> int:
+        self._guard.__enter__()
+        return _stream()
+
+    def __exit__(self, *exc):
+        return self._guard.__exit__(*exc)
+
+
+@dataclasses.dataclass
+class Beams:
+    """Result of beam_select: the best continuations of each group, best first (token and parent -1: none left)."""
+    token: torch.Tensor      # [B, select] int32
+    parent: torch.Tensor     # [B, select] int32
+    score: torch.Tensor      # [B, select] float32
+    length: torch.Tensor     # [B, select] int32 (zeros unless lengths were given)
+    done: torch.Tensor       # [B, select] bool
+    status: torch.Tensor     # [B] int32
+    workspace: torch.Tensor  # uint8, scratch
+
+
+def beam_select(logits: torch.Tensor, scores: torch.Tensor, select: Optional[int] = None, temperature: float = 1.0,
+                lengths: Optional[torch.Tensor] = None, done: Optional[torch.Tensor] = None, eos: int = -1,
+                length_penalty: float = 0.0, out: Optional[Beams] = None) -> Beams:
+    """gr_beam_select on torch CUDA tensors: logits [B, beams, V] float32 or bfloat16 (rows at any one distance, elements
+    next to one another), scores [B, beams] float32, lengths [B, beams] int32, done [B, beams] bool or uint8.  `select`
+    defaults to the number of beams.  `out`: a result of an earlier call of the same shape, written again (it must not
+    be read from by this call: scores, lengths and done are other tensors)."""
+    if not (isinstance(logits, torch.Tensor) and logits.is_cuda and logits.dim() == 3):
+        raise GrError("logits must be a [B, beams, V] CUDA tensor")
+    B, W, V = logits.shape
+    dev, code = logits.device, _dtype_code(logits)
+    ld = logits.stride(1) if W > 1 else logits.stride(0) if B > 1 else V
+    if B * W * V > 0 and ((V > 1 and logits.stride(2) != 1) or (B > 1 and W > 1 and logits.stride(0) != W * ld) or ld < V):
+        raise GrError("logits: the rows must be apart by one distance, their elements next to one another")
+    ld = max(int(ld), V)
+    K = W if select is None else int(select)
+    a_scores = _need(scores, "scores", torch.float32, (B, W), dev)
+    a_lengths = _need(lengths, "lengths", torch.int32, (B, W), dev, optional=True)
+    a_done = _need(done, "done", (torch.bool, torch.uint8), (B, W), dev, optional=True)
+    wbytes = gr_beam_workspace_bytes(V, W, K, B)
+    if wbytes == 0:
+        raise GrError("invalid shape")
+    if out is None or out.token.shape != (B, K) or out.token.device != dev or out.workspace.numel() < wbytes:
+        out = Beams(torch.empty(B, K, dtype=torch.int32, device=dev), torch.empty(B, K, dtype=torch.int32, device=dev),
+                    torch.empty(B, K, dtype=torch.float32, device=dev), torch.zeros(B, K, dtype=torch.int32, device=dev),
+                    torch.empty(B, K, dtype=torch.bool, device=dev), torch.empty(B, dtype=torch.int32, device=dev),
+                    torch.empty(wbytes, dtype=torch.uint8, device=dev))
+    for name, t, kept in (("scores", scores, out.score), ("lengths", lengths, out.length), ("done", done, out.done)):
+        if t is not None and t.numel() and t.data_ptr() == kept.data_ptr():
+            raise GrError(f"{name} is a tensor of `out`, which this call writes")
+    with _on(dev) as stream:
+        rc = gr_beam_select(logits.data_ptr(), code, V, ld, W, B, temperature, a_scores, a_lengths, a_done, int(eos),
+                            length_penalty, K, out.workspace.data_ptr(), out.token.data_ptr(), out.parent.data_ptr(),
+                            out.score.data_ptr(), out.length.data_ptr() if lengths is not None else 0,
+                            out.done.data_ptr(), out.status.data_ptr(), stream)
+    _check(rc, "gr_beam_select")
+    return out
+
+
+def _state_layout(x: torch.Tensor, token_dim: Optional[int]):
+    """(parts, bytes between parts, bytes of a part, bytes of a token) of the states in x [B, beams, ...]."""
+    e = x.element_size()
+    shape, stride = list(x.shape), list(x.stride())
+    at = 2 if token_dim is None else token_dim
+    part = 1
+    for d in range(x.dim() - 1, at - 1, -1):
+        if shape[d] > 1 and stride[d] != part:
+            raise GrError("states: the dimensions from the tokens on must lie next to one another")
+        part *= shape[d]
+    parts, step = 1, 0
+    for d in range(at - 1, 1, -1):
+        if shape[d] == 1:
+            continue
+        if parts > 1 and stride[d] != step * parts:
+            raise GrError("states: the dimensions before the tokens must have one distance between their pieces")
+        step = stride[d] if parts == 1 else step
+        parts *= shape[d]
+    tokens = 1 if token_dim is None else shape[token_dim]
+    return parts, step * e, part * e, part // tokens * e if tokens else e
+
+
+def _bytes_of(t: torch.Tensor):
+    """[first, last) byte of the memory that a tensor's elements span."""
+    if t.numel() == 0:
+        return t.data_ptr(), t.data_ptr()
+    span = sum((n - 1) * s for n, s in zip(t.shape, t.stride()))
+    return t.data_ptr(), t.data_ptr() + (span + 1) * t.element_size()
+
+
+def reorder_states(states, parents: torch.Tensor, lengths: Optional[torch.Tensor] = None,
+                   token_dim: Optional[int] = None, out=None):
+    """gr_reorder_states on torch CUDA tensors: `states` is a list of tensors [B, beams, ...] (of any types and layouts),
+    parents [B, chosen] int32.  In place, with chosen <= beams, unless `out` (a list of tensors [B, chosen, ...]) is
+    given, which must not share memory with the states.  With lengths [B, beams] int32 the dimension `token_dim` of the
+    states counts tokens, of which each parent's first lengths[b, parent] are copied.  Returns `out` or `states`."""
+    states = list(states)
+    to = states if out is None else list(out)
+    if len(to) != len(states):
+        raise GrError("out: one tensor for each of the states")
+    if not states:
+        return to
+    if not isinstance(parents, torch.Tensor) or parents.dim() != 2:
+        raise GrError("parents must be a [B, chosen] CUDA tensor of torch.int32")
+    B, chosen = parents.shape
+    dev = parents.device
+    a_parents = _need(parents, "parents", torch.int32)
+    if (lengths is None) != (token_dim is None):
+        raise GrError("lengths and token_dim go together")
+    groups = {}
+    W = None
+    for x, y in zip(states, to):
+        if not (isinstance(x, torch.Tensor) and x.is_cuda and x.dim() >= 2 and x.device == dev and x.shape[0] == B):
+            raise GrError("states must be CUDA tensors [B, beams, ...] on the device of parents")
+        if W is None:
+            W = x.shape[1]
+        if x.shape[1] != W:
+            raise GrError("states: one number of beams")
+        if y is not x and not (isinstance(y, torch.Tensor) and y.device == dev and y.dtype == x.dtype
+                               and y.shape == (B, chosen) + tuple(x.shape[2:])):
+            raise GrError("out must hold tensors [B, chosen, ...] like the states")
+        if token_dim is not None and not 2 <= token_dim < x.dim():
+            raise GrError("token_dim must be a dimension behind the beams")
+        parts, part_step, part, token = _state_layout(x, token_dim)
+        parts_y, part_step_y, _, _ = (parts, part_step, part, token) if y is x else _state_layout(y, token_dim)
+        e = x.element_size()
+        key = (parts, x.stride(0) * e, x.stride(1) * e, part_step, y.stride(0) * e, y.stride(1) * e, part_step_y, part,
+               token)
+        groups.setdefault(key, []).append((x, y))
+    if out is not None:
+        spans = [_bytes_of(x) for x in states]
+        for y in to:
+            lo, hi = _bytes_of(y)
+            if any(lo < b and a < hi for a, b in spans):
+                raise GrError("out shares memory with the states")
+    first = [y.data_ptr() for y in to if y.numel()]
+    if len(set(first)) < len(first):
+        raise GrError("the same tensor twice")
+    a_lengths = _need(lengths, "lengths", torch.int32, (B, W), dev, optional=True)
+    with _on(dev) as stream:
+        for key, pairs in groups.items():
+            parts, sg, sb, sp, dg, db, dp, part, token = key
+            if B * parts * part == 0 or chosen == 0:
+                continue
+            layout = StateLayout(B, W, chosen, parts, sg if B > 1 else 0, sb if W > 1 else 0, sp, dg if B > 1 else 0,
+                                 db if (W if out is None else chosen) > 1 else 0, dp, part, token)
+            rc = gr_reorder_states([x.data_ptr() for x, _ in pairs], [y.data_ptr() for _, y in pairs], layout, a_parents,
+                                   a_lengths, stream)
+            _check(rc, "gr_reorder_states")
+    return to
+
+
+@dataclasses.dataclass
+class BlockTables:
+    """Block tables of a paged cache: row r's token t lies in block table[r, t // block_size] at t % block_size; refs[i]
+    rows hold block i.  Rows come in groups of `beams`."""
+    table: torch.Tensor      # [rows, width] int32, -1 where no block is held
+    lengths: torch.Tensor    # [rows] int32 tokens
+    refs: torch.Tensor       # [num_blocks] int32
+    block_size: int
+    beams: int = 1
+
+    @staticmethod
+    def empty(rows: int, width: int, num_blocks: int, block_size: int, beams: int = 1, device="cuda") -> "BlockTables":
+        return BlockTables(torch.full((rows, width), -1, dtype=torch.int32, device=device),
+                           torch.zeros(rows, dtype=torch.int32, device=device),
+                           torch.zeros(num_blocks, dtype=torch.int32, device=device), block_size, beams)
+
+
+@dataclasses.dataclass
+class BlockPlan:
+    """Result of block_plan: where the appended tokens go, and which blocks are to be copied before they are written."""
+    slots: torch.Tensor      # [max_tokens] int64, -1 behind the last token
+    positions: torch.Tensor  # [max_tokens] int32
+    offsets: torch.Tensor    # [rows + 1] int32
+    copy_src: torch.Tensor   # [rows] int32, -1: nothing to copy
+    copy_dst: torch.Tensor   # [rows] int32
+    status: torch.Tensor     # [rows] int32
+    workspace: torch.Tensor  # uint8, scratch
+
+
+def block_plan(tables: BlockTables, append: torch.Tensor, max_tokens: int, keep: Optional[torch.Tensor] = None,
+               parents: Optional[torch.Tensor] = None, out: Optional[BlockPlan] = None) -> BlockPlan:
+    """gr_block_plan on torch CUDA tensors: `tables` is updated in place; append, keep [rows] int32, parents [rows] or
+    [rows / beams, beams] int32 (row numbers within the group, as beam_select returns them)."""
+    if not isinstance(tables.table, torch.Tensor) or tables.table.dim() != 2:
+        raise GrError("table must be a [rows, width] CUDA tensor of torch.int32")
+    R, width = tables.table.shape
+    dev, i32 = tables.table.device, torch.int32
+    a_table = _need(tables.table, "table", i32)
+    a_lengths = _need(tables.lengths, "lengths", i32, (R,), dev)
+    N = int(tables.refs.numel())
+    a_refs = _need(tables.refs, "refs", i32, (N,), dev)
+    a_append = _need(append, "append", i32, (R,), dev)
+    a_keep = _need(keep, "keep", i32, (R,), dev, optional=True)
+    a_parents = _need(parents, "parents", i32, None, dev, optional=True)
+    if parents is not None and tuple(parents.shape) != (R,):
+        if tables.beams < 1 or tuple(parents.shape) != (R // tables.beams, tables.beams):
+            raise GrError("parents must be [rows] or [rows / beams, beams]")
+    wbytes = gr_block_workspace_bytes(R, N)
+    if wbytes == 0 or max_tokens < 0:
+        raise GrError("invalid shape")
+    if (out is None or out.slots.shape[0] != max_tokens or out.offsets.shape[0] != R + 1 or out.slots.device != dev
+            or out.workspace.numel() < wbytes):
+        out = BlockPlan(torch.empty(max_tokens, dtype=torch.int64, device=dev),
+                        torch.empty(max_tokens, dtype=i32, device=dev), torch.empty(R + 1, dtype=i32, device=dev),
+                        torch.empty(R, dtype=i32, device=dev), torch.empty(R, dtype=i32, device=dev),
+                        torch.empty(R, dtype=i32, device=dev), torch.empty(wbytes, dtype=torch.uint8, device=dev))
+    with _on(dev) as stream:
+        rc = gr_block_plan(a_table, R, width, tables.beams, tables.block_size, a_lengths, a_refs, N, a_parents, a_keep,
+                           a_append, max_tokens, out.workspace.data_ptr(), out.slots.data_ptr(), out.positions.data_ptr(),
+                           out.offsets.data_ptr(), out.copy_src.data_ptr(), out.copy_dst.data_ptr(),
+                           out.status.data_ptr(), stream)
+    _check(rc, "gr_block_plan")
+    return out
+
+
+def copy_blocks(caches, copy_src: torch.Tensor, copy_dst: torch.Tensor) -> None:
+    """gr_copy_blocks on torch CUDA tensors: `caches` is a list of tensors [num_blocks, ...] whose blocks are contiguous,
+    copy_src and copy_dst [pairs] int32 as block_plan returns them."""
+    caches = list(caches)
+    if not caches:
+        return
+    if not isinstance(copy_src, torch.Tensor) or copy_src.dim() != 1:
+        raise GrError("copy_src must be a [pairs] CUDA tensor of torch.int32")
+    dev = copy_src.device
+    a_src = _need(copy_src, "copy_src", torch.int32)
+    a_dst = _need(copy_dst, "copy_dst", torch.int32, copy_src.shape, dev)
+    groups = {}
+    for x in caches:
+        if not (isinstance(x, torch.Tensor) and x.is_cuda and x.device == dev and x.dim() >= 1):
+            raise GrError("caches must be CUDA tensors [num_blocks, ...] on the device of copy_src")
+        if x.numel() == 0:
+            continue
+        per = x.numel() // x.shape[0]
+        if not x[0].is_contiguous() or (x.shape[0] > 1 and x.stride(0) < per):
+            raise GrError("caches: a block's elements must lie next to one another, and the blocks apart")
+        e = x.element_size()
+        groups.setdefault((x.shape[0], (x.stride(0) if x.shape[0] > 1 else per) * e, per * e), []).append(x.data_ptr())
+    with _on(dev) as stream:
+        for (blocks, stride, size), at in groups.items():
+            rc = gr_copy_blocks(at, blocks, stride, size, a_src, a_dst, int(copy_src.shape[0]), stream)
+            _check(rc, "gr_copy_blocks")

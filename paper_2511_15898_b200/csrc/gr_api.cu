@@ -259,6 +259,9 @@ const char* gr_strerror(int code)
         case GR_STALE_PARAMS: return "params block was not written by gr_solve";
         case GR_PARTIAL_RULE: return "rule solved only for the drafts given to gr_solve_verify";
         case GR_CHECK_FAILED: return "bounds-checked build: an out-of-range access was skipped";
+        case GR_NO_BLOCKS: return "too few free blocks in the pool for the row";
+        case GR_ROW_FULL: return "more tokens than the row's block table or the slot map holds";
+        case GR_BAD_ROW: return "negative count, parent outside the group or block id outside the pool";
         case GR_E_INVALID: return "invalid size, temperature or option";
         case GR_E_NULL: return "required pointer is NULL";
         case GR_E_ALIGN: return "pointer is not 16-byte aligned";

@@ -1,0 +1,604 @@
+// gr_beam_select: the best continuations of groups of hypotheses.
+//
+// Two kernels.  The first streams the logit rows once, every row in one or several parts of a CTA each: a part leaves its
+// `select` largest logits in descending order and the sum of its exponentials.  The second, a CTA per group, puts the sums
+// together, turns the listed logits into scores and ranks them.
+//
+// The sum.  With s = log2(e) / T split into two fp32 numbers (s_hi + s_lo, both positive) an element contributes
+// 2^(x s - R), R the whole number above x s of the largest element met so far by the thread: two FMAs and one ex2 an element,
+// no systematic error from the rounding of s (which alone costs 4e-7 of a log-sum over 10^5 ids), exact factors between sums of
+// different R, fp32 sums over one batch of vectors, fp64 from there on.  An element that is -infinity gives 0; NaN and
+// +infinity make the sum NaN, as does a maximum whose product with s overflows: such rows' sums are taken again in fp64 by the
+// second kernel, which tells the two apart.
+//
+// The order.  Within a row it is that of the logits.  Between rows scores are compared in fp64; the streamed sums are good to
+// about 1e-8 (kNear is far above that), and where two continuations lie closer than kNear the rows' sums are taken again in
+// fp64, so that the order is that of the 64-bit scores.
+#include <limits.h>
+#include <math.h>
+#include "gr_host.h"
+#include "gr_scan.cuh"
+
+namespace gr {
+
+constexpr int kBeamThreads = 256;
+constexpr int kBeamWarps = kBeamThreads / 32;
+constexpr int kBeamMaxParts = 16;
+constexpr int kBeamMaxLists = 256;             // rows of a group times parts
+constexpr int kBeamMaxListed = 4096;           // entries of a group's lists
+static_assert(GR_MAX_BEAMS * GR_MAX_SELECT <= kBeamMaxListed && GR_MAX_SELECT <= kMaxSupport, "lists");
+constexpr double kNear = 1e-6;
+constexpr float kLargestRef = 16777216.f;
+
+// what a part leaves: this, then its keys (ckey) in descending order
+struct __align__(16) BeamPart {
+    double sum;              // of 2^(x s - ref)
+    float ref;
+    int count;               // keys that follow
+    int state;               // kPartSkipped, kPartCheck
+    int pad;
+};
+constexpr int kPartSkipped = 1, kPartCheck = 2;
+static_assert(sizeof(BeamPart) == 32, "workspace layout");
+
+struct BeamArgs {
+    const void* logits; const float* scores; const int* lengths; const unsigned char* done;
+    long long ld;
+    int V, beams, select, keep, parts, eos;        // keep: keys per part
+    float s_hi, s_lo;
+    double temp, penalty;
+    char* ws;
+    int* out_token; int* out_parent; float* out_score; int* out_length; unsigned char* out_done; int* status;
+};
+
+__host__ __device__ inline int beam_stride(int keep) { return (int)sizeof(BeamPart) + 8 * ((keep + 1) & ~1); }
+
+using BeamSm = ScanShared<kBeamThreads, 1280, 2048, 1>;
+
+// v 2^k, k a whole number at or below 0 (what falls below 2^-1000 of v is dropped); a NaN stays one
+__device__ __forceinline__ double times_pow2(double v, float k)
+{
+    if (!(k > -1000.f)) return v != v || k != k ? __longlong_as_double(0x7ff8000000000000ll) : 0.0;
+    return v * __hiloint2double((1023 + (int)k) << 20, 0);
+}
+
+// ---------------------------------------------------------------- streaming
+
+// Cuts the `listed` keys to those above `least`, in place (at most GR_MAX_SELECT of them: one for each thread).
+template <class SS>
+__device__ __forceinline__ void keep_keys(SS& sh, int listed, unsigned long long least)
+{
+    const unsigned long long k = (int)threadIdx.x < listed ? sh.keys[threadIdx.x] : 0ull;
+    if (threadIdx.x == 0) sh.kept = 0;
+    __syncthreads();
+    if (k > least) sh.keys[atomicAdd(&sh.kept, 1)] = k;
+    __syncthreads();
+}
+
+template <typename T, int U>
+__global__ void __launch_bounds__(kBeamThreads, 4)
+beam_stream_kernel(const __grid_constant__ BeamArgs A)
+{
+    using VT = VecTraits<T>;
+    constexpr int N = VT::N, S = kChunk / (32 * N), NB = S / U;
+    static_assert(S % U == 0, "a chunk is a whole number of batches");
+    __shared__ BeamSm sh;
+    __shared__ float s_ref[kBeamWarps];
+    __shared__ double s_sum[kBeamWarps];
+    pdl_wait();
+    GR_CHECK_FLAG_DECL;
+    GR_CHECK_FLAG_INIT;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const long long row = blockIdx.x / A.parts;
+    const int part = blockIdx.x % A.parts;
+    BeamPart* rec = reinterpret_cast<BeamPart*>(A.ws + (size_t)blockIdx.x * beam_stride(A.keep));
+    GR_PTR(unsigned long long) rec_keys = GR_MKPTR(unsigned long long, reinterpret_cast<unsigned long long*>(rec + 1), A.keep, GR_CHECK_FLAG);
+    if (A.scores[row] == -INFINITY || (A.done && A.done[row])) {
+        if (tid == 0) { BeamPart p = {0.0, -INFINITY, 0, kPartSkipped, 0}; *rec = p; }
+        return;
+    }
+    const int V = A.V, K = A.keep;
+    const T* x = (const T*)A.logits + row * A.ld;
+    const int head = row_head(x, 0, V, (int)sizeof(T));
+    const int nch = num_chunks(V, head);
+    // this part's chunks: first + warp, + stride, ...
+    const int first = part * kBeamWarps, stride = A.parts * kBeamWarps;
+    const bool use_tau = V > BeamSm::kCap;             // (else every element may be listed)
+    const int vec_end = head + ((V - head) / N) * N, tail = V - vec_end;
+    if (tid == 0) { sh.cnt = 0; sh.tau = -3.402823466e38f; sh.reset_checks(); }
+    __syncthreads();
+
+    float g0 = -INFINITY, ref = -INFINITY;             // this thread's largest logit; the whole number above its product with s
+    double acc = 0.0;
+    const unsigned long long hi2 = f_pack(A.s_hi, A.s_hi), lo2 = f_pack(A.s_lo, A.s_lo);
+    const int rounds = first < nch ? (nch - first + stride - 1) / stride : 0;
+    // a new largest element: what has been added up moves to its reference
+    auto raise = [&](float m) {
+        g0 = m;
+        const float r = ceilf(m * A.s_hi);
+        if (acc != 0.0) acc = times_pow2(acc, ref - r);
+        ref = r;
+    };
+    auto scalar = [&](int i, float tau) {
+        const float v = load_logit<T>(x, i);
+        if (v > g0) raise(v);
+        const float y = fmaf(v, A.s_lo, fmaf(v, A.s_hi, ref == -INFINITY ? 0.f : -ref));
+        acc += (double)ex2(y);
+        if (v >= tau) push_vector(sh, VT::alone(v), i);
+    };
+    int r = 0, upto = use_tau ? 1 : rounds;
+#pragma unroll 1
+    while (true) {
+#pragma unroll 1
+        for (; r < min(upto, rounds); r++) {
+            const int c = first + r * stride + warp;
+            const bool cvalid = c < nch;
+            const bool whole = cvalid && head + (c + 1) * kChunk <= vec_end;
+#pragma unroll 1
+            for (int nb = 0; nb < NB; nb++) {
+                const int base = head + c * kChunk + (nb * U * 32 + lane) * N;
+                const bool sample = use_tau && r == 0 && nb == 0;
+                const float tau = sample ? INFINITY : *((volatile float*)&sh.tau);
+                ulonglong2 v[U];
+                auto batch = [&](auto all) {
+                    auto in = [&](int i0) { return decltype(all)::value || i0 + N <= vec_end; };
+#pragma unroll
+                    for (int u = 0; u < U; u++) {
+                        const int i0 = base + u * 32 * N;
+                        v[u].x = VT::kNone; v[u].y = VT::kNone;
+                        bool ok = in(i0);
+#ifdef GR_CHECK
+                        if (ok && (i0 < 0 || i0 + N > V || ((size_t)(x + i0) & 15))) { *GR_CHECK_FLAG = 1; ok = false; }
+#endif
+                        if (ok) v[u] = ldg_stream(x + i0);
+                    }
+                    if (nb == 0) {
+                        if (c == 0 && lane < head) scalar(lane, tau);
+                        if (c == nch - 1 && lane < tail) scalar(vec_end + lane, tau);
+                    }
+                    float each[U];
+                    each[0] = VT::largest(v[0]);
+                    float most = each[0];
+#pragma unroll
+                    for (int u = 1; u < U; u++) { each[u] = VT::largest(v[u]); most = fmaxf(most, each[u]); }
+                    if (most > g0) raise(most);
+                    // (an element that is -infinity gives 0 whatever the reference, as long as that is finite)
+                    const float down = ref == -INFINITY ? 0.f : -ref;
+                    const unsigned long long down2 = f_pack(down, down);
+                    unsigned long long sum2 = 0ull;
+#pragma unroll
+                    for (int u = 0; u < U; u++) {
+#pragma unroll
+                        for (int i = 0; i < VT::kPairs; i++) {
+                            const unsigned long long w = VT::pair(v[u], i);
+                            const unsigned long long y = fma2(w, lo2, fma2(w, hi2, down2));
+                            sum2 = add2(sum2, f_pack(ex2(f_lo(y)), ex2(f_hi(y))));
+                        }
+                    }
+                    acc += (double)f_lo(sum2) + (double)f_hi(sum2);
+#pragma unroll
+                    for (int u = 0; u < U; u++) if (each[u] >= tau) push_vector(sh, v[u], base + u * 32 * N);
+                };
+                if (whole) batch(std::true_type());
+                else if (cvalid) batch(std::false_type());
+                if (sample) {
+                    // the first batch had no threshold: it gives one, and is tested now
+                    refine_tau(sh, g0, K);
+                    if (cvalid) {
+                        const float t1 = *((volatile float*)&sh.tau);
+#pragma unroll
+                        for (int u = 0; u < U; u++) {
+                            if ((whole || base + u * 32 * N + N <= vec_end) && VT::largest(v[u]) >= t1) push_vector(sh, v[u], base + u * 32 * N);
+                        }
+                        auto late = [&](int i) {
+                            const float w = load_logit<T>(x, i);
+                            if (w >= t1) push_vector(sh, VT::alone(w), i);
+                        };
+                        if (c == 0 && lane < head) late(lane);
+                        if (c == nch - 1 && lane < tail) late(vec_end + lane);
+                    }
+                }
+            }
+        }
+        if (r >= rounds) break;
+        // a better threshold whenever the part read has grown fourfold, and a shorter list where it would not hold what is to come
+        const int listed = refine_tau(sh, g0, K);
+        const int more = (K + K * K / kBeamThreads) * min(3 * r, rounds - r);
+        if (listed <= BeamSm::kList && 5 * more > 4 * (BeamSm::kList - listed) * r) keep_listed<T>(sh, listed);
+        upto *= 4;
+    }
+    // ---- the part's sum
+    {
+        float top = ref;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+        // (a thread that met NaN or +infinity holds NaN; one that met nothing, or -infinity only, 0)
+        double part_sum = acc;
+        if (acc != 0.0 && ref != top) part_sum = times_pow2(acc, ref - top);
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) part_sum += __shfl_xor_sync(0xffffffffu, part_sum, o);
+        if (lane == 0) { s_ref[warp] = top; s_sum[warp] = part_sum; }
+    }
+    __syncthreads();
+    // ---- candidates: a last threshold from the list itself, then keys of those that pass it
+    int M = sh.cnt;
+    bool over = M > BeamSm::kList;
+    if (!over) {
+        constexpr int kPer = (BeamSm::kList + kBeamThreads - 1) / kBeamThreads;
+        // (the keys take the list's place: what a thread lists is in its registers before)
+        ulonglong2 vv[kPer];
+        int id[kPer];
+        float own = -INFINITY;
+#pragma unroll
+        for (int u = 0; u < kPer; u++) {
+            const int e = tid + u * kBeamThreads;
+            vv[u].x = VT::kNone; vv[u].y = VT::kNone; id[u] = 0;
+            if (e < M) { vv[u] = GR_ARRAY_AS(ulonglong2, sh.keys, e); id[u] = GR_ARRAY_AS(int, sh.keys, 4 * BeamSm::kList + e); }
+            own = fmaxf(own, VT::largest(vv[u]));
+        }
+        if (M > K) refine_tau(sh, own, K);
+        const float tau = sh.tau;
+        if (tid == 0) sh.kept = 0;
+        __syncthreads();
+        if (own >= tau) {
+#pragma unroll
+            for (int u = 0; u < kPer; u++) {
+                if (VT::largest(vv[u]) < tau) continue;
+#pragma unroll
+                for (int i = 0; i < N; i++) {
+                    const float w = VT::element(vv[u], i);
+                    if (w >= tau && w > -INFINITY) {
+                        const int slot = atomicAdd(&sh.kept, 1);
+                        if (slot < BeamSm::kCap) sh.keys[slot] = ckey(w, id[u] + i);
+                    }
+                }
+            }
+        }
+        __syncthreads();
+        M = sh.kept;
+        over = M > BeamSm::kCap;
+    }
+    if (over) {
+        __syncthreads();
+        exact_select_slow<T>(sh, x, V, head, nch, first, stride, K);
+        // (masked tokens come last in that order; they are not continuations)
+        const unsigned long long masked = ((unsigned long long)fkey(-INFINITY) << 32) | 0xffffffffull;
+        const int listed = min(sh.cnt, K);
+        M = __syncthreads_count(tid < listed && sh.keys[min(tid, K - 1)] > masked);
+        if (M < listed) keep_keys(sh, listed, masked);
+    }
+    const int nsel = min(K, M);
+    rank_select(sh, M, nsel, [&](int rank, unsigned long long key) { rec_keys[rank] = key; });
+    if (tid == 0) {
+        float top = s_ref[0];
+        for (int w = 1; w < kBeamWarps; w++) top = fmaxf(top, s_ref[w]);
+        double sum = 0.0;
+        for (int w = 0; w < kBeamWarps; w++) {
+            if (s_sum[w] != 0.0) sum += s_ref[w] == top ? s_sum[w] : times_pow2(s_sum[w], s_ref[w] - top);
+        }
+        BeamPart p = {sum, top, nsel, sh.checks() | GR_CHECK_VALUE ? kPartCheck : 0, 0};
+        *rec = p;
+    }
+}
+
+// ---------------------------------------------------------------- the group's choice
+
+struct BeamGroup {
+    double lse[GR_MAX_BEAMS], scale[GR_MAX_BEAMS], score[GR_MAX_BEAMS];
+    double red[kBeamWarps];
+    int length[GR_MAX_BEAMS];
+    unsigned char kind[GR_MAX_BEAMS], again[GR_MAX_BEAMS], exact[GR_MAX_BEAMS];
+    int bad, check, count, redo;
+    double least, slack;     // slack: kNear as a difference of keys
+    double best_key[GR_MAX_SELECT + 1];
+    int best_at[GR_MAX_SELECT + 1];
+};
+constexpr int kRowNone = 0, kRowDone = 1, kRowLive = 2;
+
+// log sum exp(x / T) of a row in fp64, the same for every thread; -infinity for a row that is masked as a whole; `bad` set for
+// one with a NaN or +infinity.  (Every thread takes the elements of its index modulo the CTA's size, so that equal rows give
+// equal sums wherever they lie.)
+template <typename T>
+__device__ __noinline__ double row_lse(const T* x, int V, double temp, double* red, int* bad)
+{
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    float m = -INFINITY;
+    int wrong = 0;
+    for (int i = tid; i < V; i += kBeamThreads) {
+        const float v = load_logit<T>(x, i);
+        if (!(v < INFINITY)) wrong = 1;
+        m = fmaxf(m, v);
+    }
+    wrong = __syncthreads_or(wrong);
+    if (wrong) { if (tid == 0) *bad = 1; return 0.0; }
+    m = warp_max(m);
+    if (lane == 0) red[warp] = (double)m;
+    __syncthreads();
+    double top = red[0];
+    for (int w = 1; w < kBeamWarps; w++) top = fmax(top, red[w]);
+    __syncthreads();
+    if (top == -INFINITY) return -INFINITY;
+    double sum = 0.0;
+    for (int i = tid; i < V; i += kBeamThreads) {
+        const double v = (double)load_logit<T>(x, i);
+        if (v > -INFINITY) sum += exp_neg((top - v) / temp);
+    }
+#pragma unroll 1
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    if (lane == 0) red[warp] = sum;
+    __syncthreads();
+    double all = 0.0;
+    for (int w = 0; w < kBeamWarps; w++) all += red[w];
+    __syncthreads();
+    return top / temp + m_log(all);
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kBeamThreads)
+beam_choose_kernel(const __grid_constant__ BeamArgs A)
+{
+    extern __shared__ __align__(16) unsigned char s_dyn[];
+    __shared__ BeamGroup g;
+    pdl_wait();
+    GR_CHECK_FLAG_DECL;
+    GR_CHECK_FLAG_INIT;
+    const int tid = threadIdx.x;
+    const long long b = blockIdx.x;
+    const int W = A.beams, P = A.parts, K = A.select, keep = A.keep, lists = W * P, most = lists * keep;
+    // lists in shared memory: the keys as scores, the logits and tokens, the survivors
+    GR_PTR(double) key = GR_MKPTR(double, reinterpret_cast<double*>(s_dyn), most, GR_CHECK_FLAG);
+    GR_PTR(unsigned long long) raw = GR_MKPTR(unsigned long long, reinterpret_cast<unsigned long long*>(s_dyn) + most, most, GR_CHECK_FLAG);
+    GR_PTR(int) live = GR_MKPTR(int, reinterpret_cast<int*>(s_dyn + 16 * (size_t)most), most, GR_CHECK_FLAG);
+    GR_PTR(int) count = GR_MKPTR(int, reinterpret_cast<int*>(s_dyn + 16 * (size_t)most) + most, lists, GR_CHECK_FLAG);
+    const char* recs = A.ws + (size_t)b * lists * beam_stride(keep);
+    if (tid == 0) { g.bad = 0; g.check = 0; g.redo = 0; }
+    __syncthreads();
+    // ---- rows
+    static_assert(GR_MAX_BEAMS <= 32, "a lane of the first warp for each row");
+    if (tid < W) {
+        const int w = tid;
+        const float s = A.scores[b * W + w];
+        const int n = A.lengths ? A.lengths[b * W + w] : 0;
+        const bool fin = A.done && A.done[b * W + w];
+        if (!(s < INFINITY)) g.bad = 1;
+        g.score[w] = (double)s;
+        g.kind[w] = s == -INFINITY ? kRowNone : fin ? kRowDone : kRowLive;
+        g.length[w] = max(1, fin ? n : (n < INT_MAX ? n + 1 : n));
+        g.scale[w] = A.penalty != 0.0 ? pow((double)g.length[w], A.penalty) : 1.0;
+        g.again[w] = 0; g.exact[w] = 0;
+        double lse = 0.0;
+        if (g.kind[w] == kRowLive) {
+            float top = -INFINITY;
+            for (int p = 0; p < P; p++) top = fmaxf(top, reinterpret_cast<const BeamPart*>(recs + (size_t)(w * P + p) * beam_stride(keep))->ref);
+            double sum = 0.0;
+            int listed = 0;
+            for (int p = 0; p < P; p++) {
+                const BeamPart* r = reinterpret_cast<const BeamPart*>(recs + (size_t)(w * P + p) * beam_stride(keep));
+                if (r->sum != 0.0) sum += r->ref == top ? r->sum : times_pow2(r->sum, r->ref - top);
+                if (r->state & kPartCheck) g.check = 1;
+                listed += r->count;
+            }
+            lse = ((double)top + log2(sum)) * 0.69314718055994530942;
+            // NaN, an infinity, or logits so large that R, an fp32 number, is not the whole number above their product with s
+            // to within a few units: in fp64.  (Not where every token is masked: nothing depends on that sum.)
+            if (!(fabsf(top) <= kLargestRef) || !(sum < INFINITY)) g.again[w] = listed > 0 || sum != 0.0;
+        }
+        g.lse[w] = lse;
+        if (g.again[w]) g.redo = 1;
+    }
+    if (tid < 32) {
+        double least = tid < W ? g.scale[tid] : INFINITY;
+#pragma unroll 1
+        for (int o = 16; o > 0; o >>= 1) least = fmin(least, __shfl_xor_sync(0xffffffffu, least, o));
+        if (tid == 0) g.slack = kNear / least;
+    }
+    for (int l = tid; l < lists; l += kBeamThreads) count[l] = reinterpret_cast<const BeamPart*>(recs + (size_t)l * beam_stride(keep))->count;
+    __syncthreads();
+    for (int e = tid; e < most; e += kBeamThreads) {
+        const int l = e / keep, i = e % keep;
+        unsigned long long k = 0ull;
+        if (i < count[l]) k = reinterpret_cast<const unsigned long long*>(recs + (size_t)l * beam_stride(keep) + sizeof(BeamPart))[i];
+        raw[e] = k;
+    }
+    __syncthreads();
+    // a finished hypothesis has one continuation, in its first part's list
+    for (int w = tid; w < W; w += kBeamThreads) {
+        if (g.kind[w] == kRowDone) { count[w * P] = 1; raw[w * P * keep] = ckey(0.f, A.eos); }
+    }
+    __syncthreads();
+    auto total_of = [&](int e) {
+        const int w = e / keep / P;
+        return g.kind[w] == kRowDone ? g.score[w] : g.score[w] + ((double)fkey_inv((unsigned)(raw[e] >> 32)) / A.temp - g.lse[w]);
+    };
+    int M = 0;
+#pragma unroll 1
+    while (true) {
+        // ---- sums that are to be taken again
+        if (g.redo) {
+#pragma unroll 1
+            for (int w = 0; w < W; w++) {
+                if (!g.again[w]) continue;
+                const double lse = row_lse<T>((const T*)A.logits + (b * W + w) * A.ld, A.V, A.temp, g.red, &g.bad);
+                __syncthreads();
+                if (tid == 0) { g.lse[w] = lse; g.again[w] = 0; g.exact[w] = 1; }
+                __syncthreads();
+            }
+        }
+        if (g.bad) break;
+        __syncthreads();
+        if (tid == 0) { g.count = 0; g.redo = 0; g.least = -INFINITY; }
+        // ---- scores, and a bound below the select-th: of the q-th entries of the lists the ceil(K / q)-th largest, q the
+        // smallest power of two that leaves at most half of the lists above it
+        for (int e = tid; e < most; e += kBeamThreads) {
+            const int l = e / keep, i = e % keep;
+            key[e] = i < count[l] ? total_of(e) / g.scale[l / P] : -INFINITY;
+        }
+        int q = 1;
+        while (q < keep && 2 * ((K + q - 1) / q) > lists) q *= 2;
+        q = min(q, keep);
+        const int place = (K + q - 1) / q;
+        __syncthreads();
+        if (place <= lists) {
+            for (int l = tid; l < lists; l += kBeamThreads) {
+                const double mine = key[l * keep + q - 1];
+                int rank = 0;
+                for (int o = 0; o < lists; o++) {
+                    const double k = key[o * keep + q - 1];
+                    rank += k > mine || (k == mine && o < l) ? 1 : 0;
+                }
+                if (rank == place - 1) g.least = mine;
+            }
+        }
+        __syncthreads();
+        // (those within kNear below the bound too: they may have to be told from the last ones)
+        const double least = g.least - g.slack;
+        for (int e = tid; e < most; e += kBeamThreads) {
+            if (e % keep < count[e / keep] && !(key[e] < least)) live[atomicAdd(&g.count, 1)] = e;
+        }
+        __syncthreads();
+        M = g.count;
+        // ---- ranks: larger key, then the row before, then the place in the row (by logit, then by token)
+        for (int a = tid; a < M; a += kBeamThreads) {
+            const int e = live[a], w = e / keep / P;
+            const double mine = key[e];
+            const unsigned long long mine_raw = raw[e];
+            int rank = 0;
+#pragma unroll 4
+            for (int o = 0; o < M; o++) {
+                const int f = live[o], v = f / keep / P;
+                const double k = key[f];
+                const bool ahead = v == w ? raw[f] > mine_raw : (k > mine || (k == mine && v < w));
+                rank += ahead ? 1 : 0;
+            }
+            if (rank <= K) { g.best_key[rank] = mine; g.best_at[rank] = e; }
+        }
+        __syncthreads();
+        // ---- continuations of different rows that lie too close for the streamed sums
+        auto close = [&](int e, int f, double apart) {
+            const int w = e / keep / P, v = f / keep / P;
+            if (w == v || fabs(apart) > g.slack) return;
+            if (g.kind[w] == kRowLive && !g.exact[w]) { g.again[w] = 1; g.redo = 1; }
+            if (g.kind[v] == kRowLive && !g.exact[v]) { g.again[v] = 1; g.redo = 1; }
+        };
+        for (int i = tid; i + 1 < min(M, K + 1); i += kBeamThreads) close(g.best_at[i], g.best_at[i + 1], g.best_key[i] - g.best_key[i + 1]);
+        if (M > K) {
+            const double last = g.best_key[K - 1];
+            for (int a = tid; a < M; a += kBeamThreads) close(live[a], g.best_at[K - 1], key[live[a]] - last);
+        }
+        __syncthreads();
+        if (!g.redo) break;
+    }
+    // ---- results
+    const bool bad = g.bad != 0;
+    for (int i = tid; i < K; i += kBeamThreads) {
+        const size_t at = (size_t)b * K + i;
+        int token = -1, parent = -1, length = 0;
+        float score = -INFINITY;
+        unsigned char fin = 0;
+        if (!bad && i < M) {
+            const int e = g.best_at[i];
+            parent = e / keep / P;
+            token = (int)(0xffffffffu - (unsigned)raw[e]);
+            score = (float)total_of(e);
+            length = g.length[parent];
+            fin = g.kind[parent] == kRowDone || token == A.eos;
+        }
+        A.out_token[at] = token; A.out_parent[at] = parent; A.out_score[at] = score; A.out_done[at] = fin;
+        if (A.out_length) A.out_length[at] = length;
+    }
+    if (tid == 0) {
+        A.status[b] = bad ? GR_BAD_LOGITS : g.check ? GR_CHECK_FAILED : GR_OK;
+#ifdef GR_CHECK
+        if (GR_CHECK_VALUE) A.status[b] = GR_CHECK_FAILED;
+#endif
+    }
+}
+
+// parts of a row: as many as there are CTAs of one wave for, each with a chunk per warp at least
+static int beam_parts(int V, int rows, int beams, int keep)
+{
+    const int chunks = (V + kChunk - 1) / kChunk;
+    int most = (chunks + kBeamWarps - 1) / kBeamWarps;
+    if (most > kBeamMaxParts) most = kBeamMaxParts;
+    int parts = (4 * kSms) / (rows > 0 ? rows : 1);
+    if (parts > most) parts = most;
+    if (parts > kBeamMaxLists / beams) parts = kBeamMaxLists / beams;
+    if (parts > kBeamMaxListed / (beams * keep)) parts = kBeamMaxListed / (beams * keep);
+    return parts < 1 ? 1 : parts;
+}
+
+static bool beam_shape_ok(int V, int beams, int select, int batch)
+{
+    return V >= 1 && V <= (1 << 21) && beams >= 1 && beams <= GR_MAX_BEAMS && select >= 1 && select <= GR_MAX_SELECT
+        && batch >= 0 && (long long)batch * beams <= (1 << 26);
+}
+
+template <typename T>
+static int launch_beam(const BeamArgs& A, int batch, cudaStream_t st)
+{
+    const int most = A.beams * A.parts * A.keep;
+    const int smem = 20 * most + 4 * A.beams * A.parts;
+    static bool raised[kMaxDevices] = {false};
+    if (smem > 40 * 1024) {
+        int dev = -1;
+        if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) { cudaGetLastError(); return GR_E_LAUNCH; }
+        if (!raised[dev]) {
+            if (cudaFuncSetAttribute(beam_choose_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, 20 * kBeamMaxListed + 4 * kBeamMaxLists) != cudaSuccess) {
+                cudaGetLastError();
+                return GR_E_LAUNCH;
+            }
+            raised[dev] = true;
+        }
+    }
+    constexpr int U = 4;
+    launch_pdl(beam_stream_kernel<T, U>, batch * A.beams * A.parts, kBeamThreads, 0, st, A);
+    launch_pdl(beam_choose_kernel<T>, batch, kBeamThreads, smem, st, A);
+    return GR_OK;
+}
+
+}  // namespace gr
+
+extern "C" {
+
+size_t gr_beam_workspace_bytes(int V, int beams, int select, int batch)
+{
+    if (!gr::beam_shape_ok(V, beams, select, batch)) return 0;
+    const int keep = select < V ? select : V, rows = (batch > 0 ? batch : 1) * beams;
+    return (size_t)rows * gr::beam_parts(V, rows, beams, keep) * gr::beam_stride(keep);
+}
+
+int gr_beam_select(const void* logits, int dtype, int V, long long ld, int beams, int batch, float temperature,
+                   const float* scores, const int* lengths, const unsigned char* done, int eos,
+                   float length_penalty, int select, void* workspace, int* out_token, int* out_parent,
+                   float* out_score, int* out_length, unsigned char* out_done, int* status, void* stream)
+{
+    if (!gr::beam_shape_ok(V, beams, select, batch)) return GR_E_INVALID;
+    if (dtype != GR_F32 && dtype != GR_BF16) return GR_E_INVALID;
+    if (!(temperature > 0.f) || !isfinite(temperature) || !(fabsf(length_penalty) <= 32.f)) return GR_E_INVALID;
+    if (ld < V || ld > (1ll << 32)) return GR_E_INVALID;
+    if (eos < -1 || eos >= V || (done && eos < 0) || (!lengths && length_penalty != 0.f)) return GR_E_INVALID;
+    if (batch == 0) return GR_OK;
+    if (!logits || !scores || !workspace || !out_token || !out_parent || !out_score || !out_done || !status) return GR_E_NULL;
+    if (((uintptr_t)logits & (dtype == GR_F32 ? 3 : 1)) || ((uintptr_t)workspace & 15)) return GR_E_ALIGN;
+    gr::BeamArgs A;
+    A.logits = logits; A.scores = scores; A.lengths = lengths; A.done = done; A.ld = ld; A.V = V; A.beams = beams;
+    A.select = select; A.keep = select < V ? select : V; A.eos = eos;
+    A.parts = gr::beam_parts(V, batch * beams, beams, A.keep);
+    A.temp = (double)temperature; A.penalty = (double)length_penalty;
+    // log2(e) / T in two parts, both positive: a logit of -infinity times either is -infinity, never NaN
+    const double s = 1.4426950408889634074 / A.temp;
+    A.s_hi = nextafterf((float)s, 0.f);
+    if ((double)A.s_hi >= s) A.s_hi = nextafterf(A.s_hi, 0.f);
+    A.s_lo = (float)(s - (double)A.s_hi);
+    A.ws = (char*)workspace;
+    A.out_token = out_token; A.out_parent = out_parent; A.out_score = out_score; A.out_length = out_length;
+    A.out_done = out_done; A.status = status;
+    gr::NvtxRange whole("gr_beam_select");
+    const int rc = dtype == GR_F32 ? gr::launch_beam<float>(A, batch, (cudaStream_t)stream)
+                                   : gr::launch_beam<__nv_bfloat16>(A, batch, (cudaStream_t)stream);
+    if (rc != GR_OK) return rc;
+    if (cudaPeekAtLastError() != cudaSuccess) { cudaGetLastError(); return GR_E_LAUNCH; }
+    return GR_OK;
+}
+
+}  // extern "C"

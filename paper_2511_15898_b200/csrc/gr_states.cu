@@ -1,0 +1,291 @@
+// What models keep per hypothesis follows the hypotheses: gr_reorder_states (dense states, in place or into other
+// tensors) and gr_copy_blocks (blocks of a paged cache that two rows shared until one of them writes).
+#include <algorithm>
+#include <memory>
+#include <new>
+#include "gr_host.h"
+
+namespace gr {
+
+constexpr int kStatesPerLaunch = 128;      // pointers that travel as kernel arguments
+constexpr int kCopyThreads = 256;
+
+struct ReorderArgs {
+    const char* src[kStatesPerLaunch];
+    char* dst[kStatesPerLaunch];
+    gr_state_layout at;
+    int count, in_place;
+    long long chunks;                      // column chunks of a piece
+};
+
+// the first n bytes of a vector
+__device__ __forceinline__ void store_bytes(char* to, const uint4& v, int n)
+{
+    const unsigned w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 16; i++) if (i < n) to[i] = (char)(w[i / 4] >> (8 * (i % 4)));
+}
+__device__ __forceinline__ void store_bytes(char* to, const uint2& v, int n)
+{
+#pragma unroll
+    for (int i = 0; i < 8; i++) if (i < n) to[i] = (char)((i < 4 ? v.x : v.y) >> (8 * (i % 4)));
+}
+__device__ __forceinline__ void store_bytes(char* to, unsigned v, int n)
+{
+#pragma unroll
+    for (int i = 0; i < 4; i++) if (i < n) to[i] = (char)(v >> (8 * i));
+}
+
+// One thread owns a column of kVec bytes of every state of a group: it reads, for each state that changes, the parent's
+// column, all of them before it writes the first.  So a group reorders in place whatever the mapping (no second buffer, no
+// order among the copies), a parent of several states is read from memory once (the other reads meet it in the first-level
+// cache), and states that stay are not touched.
+template <int W, typename Vec, int C>
+__global__ void __launch_bounds__(kCopyThreads)
+reorder_kernel(const __grid_constant__ ReorderArgs A, const int* __restrict__ parents, const int* __restrict__ lengths)
+{
+    constexpr int kVec = (int)sizeof(Vec), kStep = kCopyThreads * kVec;
+    pdl_wait();
+    const gr_state_layout& L = A.at;
+    const long long units = A.chunks * L.parts * L.batch * A.count;
+#pragma unroll 1
+    for (long long u = blockIdx.x; u < units; u += gridDim.x) {
+        const long long chunk = u % A.chunks;
+        long long rest = u / A.chunks;
+        const int part = (int)(rest % L.parts);
+        rest /= L.parts;
+        const int b = (int)(rest % L.batch), s = (int)(rest / L.batch);
+        const char* src = A.src[s] + b * L.src_group + part * L.src_part;
+        char* dst = A.dst[s] + b * L.dst_group + part * L.dst_part;
+        const long long first = chunk * C * kStep + threadIdx.x * kVec;
+        Vec v[C][W];
+        int left[W];                       // bytes that are copied from this thread's first column on (0: none, or the state stays)
+#pragma unroll
+        for (int j = 0; j < W; j++) {
+            left[j] = 0;
+            if (j < L.beams_out) {
+                const int p = __ldg(parents + (size_t)b * L.beams_out + j);
+                if (p >= 0 && p < L.beams_in && !(A.in_place && p == j)) {
+                    long long used = L.part_bytes;
+                    if (lengths) used = min(used, max(0, __ldg(lengths + (size_t)b * L.beams_in + p)) * L.token_bytes);
+                    left[j] = (int)min(max(used - first, 0ll), 1ll << 30);
+                    const char* from = src + p * L.src_beam + first;
+#pragma unroll
+                    for (int c = 0; c < C; c++) {
+                        // (a vector that holds the last used byte is read whole: pieces are a multiple of kVec long)
+                        if (c * kStep < left[j]) v[c][j] = *reinterpret_cast<const Vec*>(from + c * kStep);
+                    }
+                }
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < W; j++) {
+            char* to = dst + j * L.dst_beam + first;
+#pragma unroll
+            for (int c = 0; c < C; c++) {
+                const int more = left[j] - c * kStep;
+                if (more >= kVec) *reinterpret_cast<Vec*>(to + c * kStep) = v[c][j];
+                else if (more > 0) store_bytes(to + c * kStep, v[c][j], more);
+            }
+        }
+    }
+}
+
+struct CopyArgs {
+    char* cache[kStatesPerLaunch];
+    const int* src; const int* dst;
+    long long stride, bytes;
+    int count, num_blocks, pairs;
+};
+
+// Each CTA takes a segment of the pair list, keeps the pairs that copy something (in their order, which is then the same in
+// all CTAs of the segment), and takes its share of (pair, cache, chunk).
+template <typename Vec>
+__global__ void __launch_bounds__(kCopyThreads)
+copy_blocks_kernel(const __grid_constant__ CopyArgs A)
+{
+    constexpr int kVec = (int)sizeof(Vec), C = 4, kStep = kCopyThreads * kVec;
+    __shared__ int s_src[kCopyThreads], s_dst[kCopyThreads], s_warp[kCopyThreads / 32];
+    pdl_wait();
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int i = blockIdx.y * kCopyThreads + tid;
+    int from = -1, to = -1;
+    if (i < A.pairs) { from = A.src[i]; to = A.dst[i]; }
+    const bool copies = from >= 0 && from < A.num_blocks && to >= 0 && to < A.num_blocks && from != to;
+    const unsigned mask = __ballot_sync(0xffffffffu, copies);
+    if (lane == 0) s_warp[warp] = __popc(mask);
+    __syncthreads();
+    int at = __popc(mask & ((1u << lane) - 1u)), n = 0;
+    for (int w = 0; w < kCopyThreads / 32; w++) { if (w < warp) at += s_warp[w]; n += s_warp[w]; }
+    if (copies) { s_src[at] = from; s_dst[at] = to; }
+    __syncthreads();
+    const long long chunks = (A.bytes + (long long)C * kStep - 1) / ((long long)C * kStep);
+    const long long units = chunks * A.count * n;
+#pragma unroll 1
+    for (long long u = blockIdx.x; u < units; u += gridDim.x) {
+        const long long first = (u % chunks) * C * kStep + tid * kVec;
+        const long long rest = u / chunks;
+        const int s = (int)(rest % A.count), k = (int)(rest / A.count);
+        const char* in = A.cache[s] + s_src[k] * A.stride + first;
+        char* out = A.cache[s] + s_dst[k] * A.stride + first;
+        Vec v[C];
+#pragma unroll
+        for (int c = 0; c < C; c++) if (first + c * kStep < A.bytes) v[c] = *reinterpret_cast<const Vec*>(in + c * kStep);
+#pragma unroll
+        for (int c = 0; c < C; c++) if (first + c * kStep < A.bytes) *reinterpret_cast<Vec*>(out + c * kStep) = v[c];
+    }
+}
+
+// largest power of two up to 16 that divides everything or-ed into `bits`
+static int vec_of(unsigned long long bits) {
+    int v = 16;
+    while (bits & (unsigned long long)(v - 1)) v >>= 1;
+    return v;
+}
+
+constexpr long long kMaxBytes = 1ll << 46;        // beyond any device's memory: keeps the sums of strides in range
+
+// Whether size[i] pieces at stride[i] apart, i = 0 .. 2, of `bytes` bytes each, lie clear of one another (by nesting: each
+// stride spans all that lies within it) and within the address range; with `apart` false only the latter.
+static bool laid_out(long long bytes, const long long* stride, const int* size, bool apart)
+{
+    int order[3] = {0, 1, 2};
+    std::sort(order, order + 3, [&](int a, int b) { return stride[a] < stride[b]; });
+    if (bytes > kMaxBytes) return false;
+    __int128 span = bytes;
+    for (int i : order) {
+        if (size[i] <= 1) continue;
+        if (apart && stride[i] < span) return false;
+        span += (__int128)stride[i] * (size[i] - 1);
+        if (span > kMaxBytes) return false;
+    }
+    return true;
+}
+
+// GR_OK where the pointers lie at least `bytes` apart
+static int check_apart(const void* const* p, int count, long long bytes)
+{
+    std::unique_ptr<uintptr_t[]> at(new (std::nothrow) uintptr_t[count]);
+    if (!at) return GR_E_TOO_LARGE;
+    for (int i = 0; i < count; i++) at[i] = (uintptr_t)p[i];
+    std::sort(at.get(), at.get() + count);
+    for (int i = 1; i < count; i++) if (at[i] - at[i - 1] < (uintptr_t)bytes) return GR_E_INVALID;
+    return GR_OK;
+}
+
+template <int W>
+static void launch_reorder(const ReorderArgs& A, int vec, const int* parents, const int* lengths, cudaStream_t st)
+{
+    ReorderArgs B = A;
+    const gr_state_layout& L = A.at;
+    auto go = [&](auto kernel, int bytes, int columns) {
+        const long long per = (long long)bytes * columns * kCopyThreads;
+        B.chunks = (L.part_bytes + per - 1) / per;
+        const long long units = B.chunks * L.parts * L.batch * A.count;
+        const int grid = (int)std::min<long long>(units, 1 << 20);
+        launch_pdl(kernel, grid, kCopyThreads, 0, st, B, parents, lengths);
+    };
+    // (narrow columns: several of them per thread, so that as many bytes are in flight)
+    constexpr int N4 = W <= 8 ? 4 : 2;
+    switch (vec) {
+        case 16: go(reorder_kernel<W, uint4, 1>, 16, 1); break;
+        case 8: go(reorder_kernel<W, uint2, 2>, 8, 2); break;
+        case 4: go(reorder_kernel<W, unsigned, N4>, 4, N4); break;
+        case 2: go(reorder_kernel<W, unsigned short, N4>, 2, N4); break;
+        default: go(reorder_kernel<W, unsigned char, N4>, 1, N4); break;
+    }
+}
+
+}  // namespace gr
+
+extern "C" {
+
+int gr_reorder_states(const void* const* src, void* const* dst, int count, const gr_state_layout* layout,
+                      const int* parents, const int* lengths, void* stream)
+{
+    if (!layout) return GR_E_NULL;
+    const gr_state_layout L = *layout;
+    if (count < 0 || L.batch < 0 || L.parts < 0 || L.part_bytes < 0) return GR_E_INVALID;
+    if (L.beams_in < 1 || L.beams_in > GR_MAX_BEAMS || L.beams_out < 1 || L.beams_out > GR_MAX_BEAMS) return GR_E_INVALID;
+    if (L.src_group < 0 || L.src_beam < 0 || L.src_part < 0 || L.dst_group < 0 || L.dst_beam < 0 || L.dst_part < 0) return GR_E_INVALID;
+    if (lengths && (L.token_bytes < 1 || L.part_bytes % L.token_bytes)) return GR_E_INVALID;
+    if (count == 0 || L.batch == 0 || L.parts == 0 || L.part_bytes == 0) return GR_OK;
+    if (!src || !dst || !parents) return GR_E_NULL;
+    for (int i = 0; i < count; i++) if (!src[i] || !dst[i]) return GR_E_NULL;
+    const bool in_place = src[0] == dst[0];
+    for (int i = 1; i < count; i++) if ((src[i] == dst[i]) != in_place) return GR_E_INVALID;
+    if (in_place && (L.beams_out > L.beams_in || L.src_group != L.dst_group || L.src_beam != L.dst_beam || L.src_part != L.dst_part))
+        return GR_E_INVALID;
+    const long long to[3] = {L.dst_group, L.dst_beam, L.dst_part}, from[3] = {L.src_group, L.src_beam, L.src_part};
+    const int to_size[3] = {L.batch, in_place ? L.beams_in : L.beams_out, L.parts}, from_size[3] = {L.batch, L.beams_in, L.parts};
+    if (!gr::laid_out(L.part_bytes, to, to_size, true) || !gr::laid_out(L.part_bytes, from, from_size, false)) return GR_E_INVALID;
+    const int apart = gr::check_apart(dst, count, L.part_bytes);
+    if (apart != GR_OK) return apart;
+    unsigned long long bits = (unsigned long long)L.part_bytes;
+    if (L.batch > 1) bits |= (unsigned long long)(L.src_group | L.dst_group);
+    if (L.beams_in > 1) bits |= (unsigned long long)L.src_beam;
+    if (L.beams_out > 1) bits |= (unsigned long long)L.dst_beam;
+    if (L.parts > 1) bits |= (unsigned long long)(L.src_part | L.dst_part);
+    for (int i = 0; i < count; i++) bits |= (unsigned long long)(uintptr_t)src[i] | (unsigned long long)(uintptr_t)dst[i];
+    const int vec = gr::vec_of(bits);
+    cudaStream_t st = (cudaStream_t)stream;
+    gr::NvtxRange whole("gr_reorder_states");
+    for (int lo = 0; lo < count; lo += gr::kStatesPerLaunch) {
+        gr::ReorderArgs A;
+        A.at = L; A.in_place = in_place; A.chunks = 0;
+        A.count = std::min(count - lo, gr::kStatesPerLaunch);
+        for (int i = 0; i < A.count; i++) { A.src[i] = (const char*)src[lo + i]; A.dst[i] = (char*)dst[lo + i]; }
+        if (L.beams_out <= 4) gr::launch_reorder<4>(A, vec, parents, lengths, st);
+        else if (L.beams_out <= 8) gr::launch_reorder<8>(A, vec, parents, lengths, st);
+        else if (L.beams_out <= 16) gr::launch_reorder<16>(A, vec, parents, lengths, st);
+        else gr::launch_reorder<32>(A, vec, parents, lengths, st);
+    }
+    if (cudaPeekAtLastError() != cudaSuccess) { cudaGetLastError(); return GR_E_LAUNCH; }
+    return GR_OK;
+}
+
+int gr_copy_blocks(void* const* caches, int count, int num_blocks, long long block_stride, long long block_bytes,
+                   const int* copy_src, const int* copy_dst, int pairs, void* stream)
+{
+    if (count < 0 || num_blocks < 0 || pairs < 0 || block_bytes < 0 || block_stride < block_bytes) return GR_E_INVALID;
+    if (num_blocks > 0 && block_stride > gr::kMaxBytes / num_blocks) return GR_E_INVALID;
+    if (count == 0 || num_blocks == 0 || pairs == 0 || block_bytes == 0) return GR_OK;
+    if (!caches || !copy_src || !copy_dst) return GR_E_NULL;
+    for (int i = 0; i < count; i++) if (!caches[i]) return GR_E_NULL;
+    const int apart = gr::check_apart(caches, count, block_bytes);
+    if (apart != GR_OK) return apart;
+    unsigned long long bits = (unsigned long long)(block_stride | block_bytes);
+    for (int i = 0; i < count; i++) bits |= (unsigned long long)(uintptr_t)caches[i];
+    const int vec = gr::vec_of(bits);
+    const int segments = (int)(((long long)pairs + gr::kCopyThreads - 1) / gr::kCopyThreads);
+    if (segments > 65535) return GR_E_TOO_LARGE;
+    cudaStream_t st = (cudaStream_t)stream;
+    gr::NvtxRange whole("gr_copy_blocks");
+    for (int lo = 0; lo < count; lo += gr::kStatesPerLaunch) {
+        gr::CopyArgs A;
+        A.src = copy_src; A.dst = copy_dst; A.stride = block_stride; A.bytes = block_bytes;
+        A.num_blocks = num_blocks; A.pairs = pairs;
+        A.count = std::min(count - lo, gr::kStatesPerLaunch);
+        for (int i = 0; i < A.count; i++) A.cache[i] = (char*)caches[lo + i];
+        const dim3 grid(std::max(1, 8 * gr::kSms / segments), segments);
+        auto go = [&](auto kernel) {
+            cudaLaunchConfig_t cfg = {};
+            cudaLaunchAttribute at = {};
+            at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+            at.val.programmaticStreamSerializationAllowed = 1;
+            cfg.gridDim = grid; cfg.blockDim = dim3(gr::kCopyThreads); cfg.stream = st; cfg.attrs = &at; cfg.numAttrs = 1;
+            cudaLaunchKernelEx(&cfg, kernel, A);
+        };
+        switch (vec) {
+            case 16: go(gr::copy_blocks_kernel<uint4>); break;
+            case 8: go(gr::copy_blocks_kernel<uint2>); break;
+            case 4: go(gr::copy_blocks_kernel<unsigned>); break;
+            case 2: go(gr::copy_blocks_kernel<unsigned short>); break;
+            default: go(gr::copy_blocks_kernel<unsigned char>); break;
+        }
+    }
+    if (cudaPeekAtLastError() != cudaSuccess) { cudaGetLastError(); return GR_E_LAUNCH; }
+    return GR_OK;
+}
+
+}  // extern "C"
