@@ -8,6 +8,7 @@ the compiled library or without a CUDA device these functions raise.
 """
 from __future__ import annotations
 
+import array
 import ctypes as C
 import dataclasses
 import os
@@ -89,16 +90,14 @@ def load_library():
     lib.gr_beam_select.argtypes = [vp, C.c_int, C.c_int, C.c_longlong, C.c_int, C.c_int, C.c_float, fp, ip, vp, C.c_int,
                                    C.c_float, C.c_int, vp, ip, ip, fp, ip, vp, ip, vp]
     lib.gr_reorder_states.restype = C.c_int
-    lib.gr_reorder_states.argtypes = [C.POINTER(C.c_void_p), C.POINTER(C.c_void_p), C.c_int, C.POINTER(StateLayout), ip,
-                                      ip, vp]
+    lib.gr_reorder_states.argtypes = [vp, vp, C.c_int, C.POINTER(StateLayout), ip, ip, vp]
     lib.gr_block_workspace_bytes.restype = C.c_size_t
     lib.gr_block_workspace_bytes.argtypes = [C.c_int] * 2
     lib.gr_block_plan.restype = C.c_int
     lib.gr_block_plan.argtypes = [ip, C.c_int, C.c_int, C.c_int, C.c_int, ip, ip, C.c_int, ip, ip, ip, C.c_int, vp, vp, ip,
                                   ip, ip, ip, ip, vp]
     lib.gr_copy_blocks.restype = C.c_int
-    lib.gr_copy_blocks.argtypes = [C.POINTER(C.c_void_p), C.c_int, C.c_int, C.c_longlong, C.c_longlong, ip, ip, C.c_int,
-                                   vp]
+    lib.gr_copy_blocks.argtypes = [vp, C.c_int, C.c_int, C.c_longlong, C.c_longlong, ip, ip, C.c_int, vp]
     lib.gr_strerror.restype = C.c_char_p
     lib.gr_strerror.argtypes = [C.c_int]
     _lib = lib
@@ -183,10 +182,11 @@ def gr_beam_select(logits: int, dtype: int, V: int, ld: int, beams: int, batch: 
 
 def gr_reorder_states(src, dst, layout: Optional[StateLayout], parents: int, lengths: int, stream: int) -> int:
     """src, dst: sequences of device addresses."""
-    n = len(src)
-    return int(load_library().gr_reorder_states((C.c_void_p * n)(*src), (C.c_void_p * n)(*dst), n,
-                                                C.byref(layout) if layout is not None else None, parents, lengths,
-                                                stream))
+    if len(src) != len(dst):
+        raise GrError("src and dst: one address each for every state")
+    a, b = array.array("Q", src), array.array("Q", dst)
+    return load_library().gr_reorder_states(a.buffer_info()[0], b.buffer_info()[0], len(a),
+                                            C.byref(layout) if layout is not None else None, parents, lengths, stream)
 
 
 def gr_block_workspace_bytes(rows: int, num_blocks: int) -> int:
@@ -204,9 +204,9 @@ def gr_block_plan(table: int, rows: int, width: int, beams: int, block_size: int
 def gr_copy_blocks(caches, num_blocks: int, block_stride: int, block_bytes: int, copy_src: int, copy_dst: int,
                    pairs: int, stream: int) -> int:
     """caches: a sequence of device addresses."""
-    n = len(caches)
-    return int(load_library().gr_copy_blocks((C.c_void_p * n)(*caches), n, num_blocks, block_stride, block_bytes,
-                                             copy_src, copy_dst, pairs, stream))
+    a = array.array("Q", caches)
+    return load_library().gr_copy_blocks(a.buffer_info()[0], len(a), num_blocks, block_stride, block_bytes, copy_src,
+                                         copy_dst, pairs, stream)
 
 
 # ---------------------------------------------------------------- torch tensors
@@ -458,28 +458,23 @@ def _need(t, what: str, dtype, shape=None, device=None, optional: bool = False):
     """The address of a contiguous CUDA tensor of this type, shape and device (0 for None where that is allowed)."""
     if t is None and optional:
         return 0
-    kinds = dtype if isinstance(dtype, tuple) else (dtype,)
-    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.is_contiguous()) or t.dtype not in kinds:
-        raise GrError(f"{what}: expected a contiguous CUDA tensor of {' or '.join(str(k) for k in kinds)}")
-    if shape is not None and tuple(t.shape) != tuple(shape):
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.is_contiguous()) or t.dtype is not dtype:
+        raise GrError(f"{what}: expected a contiguous CUDA tensor of {dtype}")
+    if shape is not None and t.shape != shape:
         raise GrError(f"{what}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
     if device is not None and t.device != device:
         raise GrError(f"{what}: on {t.device}, the other tensors on {device}")
     return t.data_ptr()
 
 
-class _on:
-    """The tensors' device made current for the call; gives that device's current stream."""
-
-    def __init__(self, device):
-        self._guard = torch.cuda.device(device)
-
-    def __enter__(self) -> int:
-        self._guard.__enter__()
-        return _stream()
-
-    def __exit__(self, *exc):
-        return self._guard.__exit__(*exc)
+def _call(dev: torch.device, what: str, function, *args):
+    """A C entry point with the tensors' device current and that device's current stream."""
+    if torch.cuda.current_device() == dev.index:
+        rc = function(*args, _stream())
+    else:
+        with torch.cuda.device(dev):
+            rc = function(*args, _stream())
+    _check(rc, what)
 
 
 @dataclasses.dataclass
@@ -492,6 +487,7 @@ class Beams:
     done: torch.Tensor       # [B, select] bool
     status: torch.Tensor     # [B] int32
     workspace: torch.Tensor  # uint8, scratch
+    shape: tuple             # (B, beams, V, select)
 
 
 def beam_select(logits: torch.Tensor, scores: torch.Tensor, select: Optional[int] = None, temperature: float = 1.0,
@@ -505,31 +501,30 @@ def beam_select(logits: torch.Tensor, scores: torch.Tensor, select: Optional[int
         raise GrError("logits must be a [B, beams, V] CUDA tensor")
     B, W, V = logits.shape
     dev, code = logits.device, _dtype_code(logits)
-    ld = logits.stride(1) if W > 1 else logits.stride(0) if B > 1 else V
-    if B * W * V > 0 and ((V > 1 and logits.stride(2) != 1) or (B > 1 and W > 1 and logits.stride(0) != W * ld) or ld < V):
+    step = logits.stride()
+    ld = step[1] if W > 1 else step[0] if B > 1 else V
+    if ((V > 1 and step[2] != 1) or (B > 1 and W > 1 and step[0] != W * ld) or ld < V) and logits.numel() > 0:
         raise GrError("logits: the rows must be apart by one distance, their elements next to one another")
-    ld = max(int(ld), V)
     K = W if select is None else int(select)
-    a_scores = _need(scores, "scores", torch.float32, (B, W), dev)
-    a_lengths = _need(lengths, "lengths", torch.int32, (B, W), dev, optional=True)
-    a_done = _need(done, "done", (torch.bool, torch.uint8), (B, W), dev, optional=True)
-    wbytes = gr_beam_workspace_bytes(V, W, K, B)
-    if wbytes == 0:
-        raise GrError("invalid shape")
-    if out is None or out.token.shape != (B, K) or out.token.device != dev or out.workspace.numel() < wbytes:
+    rows = (B, W)
+    a_scores = _need(scores, "scores", torch.float32, rows, dev)
+    a_lengths = _need(lengths, "lengths", torch.int32, rows, dev, optional=True)
+    kind = torch.uint8 if done is not None and done.dtype is torch.uint8 else torch.bool
+    a_done = _need(done, "done", kind, rows, dev, optional=True)
+    if out is None or out.shape != (B, W, V, K) or out.token.device != dev:
+        wbytes = gr_beam_workspace_bytes(V, W, K, B)
+        if wbytes == 0:
+            raise GrError("invalid shape")
         out = Beams(torch.empty(B, K, dtype=torch.int32, device=dev), torch.empty(B, K, dtype=torch.int32, device=dev),
                     torch.empty(B, K, dtype=torch.float32, device=dev), torch.zeros(B, K, dtype=torch.int32, device=dev),
                     torch.empty(B, K, dtype=torch.bool, device=dev), torch.empty(B, dtype=torch.int32, device=dev),
-                    torch.empty(wbytes, dtype=torch.uint8, device=dev))
-    for name, t, kept in (("scores", scores, out.score), ("lengths", lengths, out.length), ("done", done, out.done)):
-        if t is not None and t.numel() and t.data_ptr() == kept.data_ptr():
-            raise GrError(f"{name} is a tensor of `out`, which this call writes")
-    with _on(dev) as stream:
-        rc = gr_beam_select(logits.data_ptr(), code, V, ld, W, B, temperature, a_scores, a_lengths, a_done, int(eos),
-                            length_penalty, K, out.workspace.data_ptr(), out.token.data_ptr(), out.parent.data_ptr(),
-                            out.score.data_ptr(), out.length.data_ptr() if lengths is not None else 0,
-                            out.done.data_ptr(), out.status.data_ptr(), stream)
-    _check(rc, "gr_beam_select")
+                    torch.empty(wbytes, dtype=torch.uint8, device=dev), (B, W, V, K))
+    a_score, a_length, a_fin = out.score.data_ptr(), out.length.data_ptr(), out.done.data_ptr()
+    if B > 0 and (a_scores == a_score or a_lengths == a_length or a_done == a_fin):
+        raise GrError("scores, lengths or done is a tensor of `out`, which this call writes")
+    _call(dev, "gr_beam_select", load_library().gr_beam_select, logits.data_ptr(), code, V, max(ld, V), W, B, temperature,
+          a_scores, a_lengths, a_done, eos, length_penalty, K, out.workspace.data_ptr(), out.token.data_ptr(),
+          out.parent.data_ptr(), a_score, a_length if lengths is not None else 0, a_fin, out.status.data_ptr())
     return out
 
 
@@ -555,12 +550,9 @@ def _state_layout(x: torch.Tensor, token_dim: Optional[int]):
     return parts, step * e, part * e, part // tokens * e if tokens else e
 
 
-def _bytes_of(t: torch.Tensor):
-    """[first, last) byte of the memory that a tensor's elements span."""
-    if t.numel() == 0:
-        return t.data_ptr(), t.data_ptr()
-    span = sum((n - 1) * s for n, s in zip(t.shape, t.stride()))
-    return t.data_ptr(), t.data_ptr() + (span + 1) * t.element_size()
+def _span(t: torch.Tensor) -> int:
+    """Bytes from a tensor's first element to behind its last one."""
+    return (sum((n - 1) * s for n, s in zip(t.shape, t.stride())) + 1) * t.element_size() if t.numel() else 0
 
 
 def reorder_states(states, parents: torch.Tensor, lengths: Optional[torch.Tensor] = None,
@@ -577,51 +569,51 @@ def reorder_states(states, parents: torch.Tensor, lengths: Optional[torch.Tensor
         return to
     if not isinstance(parents, torch.Tensor) or parents.dim() != 2:
         raise GrError("parents must be a [B, chosen] CUDA tensor of torch.int32")
+    a_parents = _need(parents, "parents", torch.int32)
     B, chosen = parents.shape
     dev = parents.device
-    a_parents = _need(parents, "parents", torch.int32)
     if (lengths is None) != (token_dim is None):
         raise GrError("lengths and token_dim go together")
-    groups = {}
-    W = None
-    for x, y in zip(states, to):
-        if not (isinstance(x, torch.Tensor) and x.is_cuda and x.dim() >= 2 and x.device == dev and x.shape[0] == B):
-            raise GrError("states must be CUDA tensors [B, beams, ...] on the device of parents")
-        if W is None:
-            W = x.shape[1]
-        if x.shape[1] != W:
-            raise GrError("states: one number of beams")
-        if y is not x and not (isinstance(y, torch.Tensor) and y.device == dev and y.dtype == x.dtype
-                               and y.shape == (B, chosen) + tuple(x.shape[2:])):
-            raise GrError("out must hold tensors [B, chosen, ...] like the states")
-        if token_dim is not None and not 2 <= token_dim < x.dim():
-            raise GrError("token_dim must be a dimension behind the beams")
-        parts, part_step, part, token = _state_layout(x, token_dim)
-        parts_y, part_step_y, _, _ = (parts, part_step, part, token) if y is x else _state_layout(y, token_dim)
-        e = x.element_size()
-        key = (parts, x.stride(0) * e, x.stride(1) * e, part_step, y.stride(0) * e, y.stride(1) * e, part_step_y, part,
-               token)
-        groups.setdefault(key, []).append((x, y))
-    if out is not None:
-        spans = [_bytes_of(x) for x in states]
-        for y in to:
-            lo, hi = _bytes_of(y)
-            if any(lo < b and a < hi for a, b in spans):
-                raise GrError("out shares memory with the states")
-    first = [y.data_ptr() for y in to if y.numel()]
-    if len(set(first)) < len(first):
-        raise GrError("the same tensor twice")
+    W = states[0].shape[1] if isinstance(states[0], torch.Tensor) and states[0].dim() >= 2 else 0
     a_lengths = _need(lengths, "lengths", torch.int32, (B, W), dev, optional=True)
-    with _on(dev) as stream:
-        for key, pairs in groups.items():
-            parts, sg, sb, sp, dg, db, dp, part, token = key
-            if B * parts * part == 0 or chosen == 0:
-                continue
-            layout = StateLayout(B, W, chosen, parts, sg if B > 1 else 0, sb if W > 1 else 0, sp, dg if B > 1 else 0,
-                                 db if (W if out is None else chosen) > 1 else 0, dp, part, token)
-            rc = gr_reorder_states([x.data_ptr() for x, _ in pairs], [y.data_ptr() for _, y in pairs], layout, a_parents,
-                                   a_lengths, stream)
-            _check(rc, "gr_reorder_states")
+    # runs of tensors of one layout: (layout, states, outs, bytes that a state and an out span)
+    runs = []
+    shape = step = kind = shape_y = step_y = None
+    for x, y in zip(states, to):
+        if not isinstance(x, torch.Tensor) or x.device != dev:
+            raise GrError("states must be CUDA tensors [B, beams, ...] on the device of parents")
+        if x.shape != shape or x.stride() != step or x.dtype is not kind or (y is not x and y.stride() != step_y):
+            shape, step, kind = x.shape, x.stride(), x.dtype
+            if x.dim() < 2 or shape[0] != B or shape[1] != W:
+                raise GrError("states must be [B, beams, ...], of one number of beams")
+            if token_dim is not None and not 2 <= token_dim < x.dim():
+                raise GrError("token_dim must be a dimension behind the beams")
+            parts, part_step, part, token = _state_layout(x, token_dim)
+            part_step_y = part_step if y is x else _state_layout(y, token_dim)[1]
+            step_y = y.stride()
+            shape_y = shape if out is None else (B, chosen) + tuple(shape[2:])
+            e = x.element_size()
+            layout = StateLayout(B, W, chosen, parts, step[0] * e if B > 1 else 0, step[1] * e if W > 1 else 0, part_step,
+                                 step_y[0] * e if B > 1 else 0,
+                                 step_y[1] * e if (W if out is None else chosen) > 1 else 0, part_step_y, part, token)
+            runs.append((layout, [], [], _span(x), _span(y)))
+        if y is not x and (not isinstance(y, torch.Tensor) or y.shape != shape_y or y.dtype is not kind or y.device != dev):
+            raise GrError("out must hold tensors [B, chosen, ...] like the states")
+        runs[-1][1].append(x.data_ptr())
+        if out is not None:
+            runs[-1][2].append(y.data_ptr())
+    if out is not None:
+        if (min(min(r[2]) for r in runs) < max(max(r[1]) + r[3] for r in runs)
+                and min(min(r[1]) for r in runs) < max(max(r[2]) + r[4] for r in runs)
+                and any(p < q + n and q < p + m for _, _, at, _, m in runs for p in at for _, of, _, n, _ in runs for q in of)):
+            raise GrError("out shares memory with the states")
+    if len(runs) > 1:
+        first = [p for r in runs if r[3] for p in (r[1] if out is None else r[2])]
+        if len(set(first)) < len(first):
+            raise GrError("the same tensor twice")
+    for layout, at, at_y, _, _ in runs:
+        if chosen > 0 and layout.part_bytes > 0:
+            _call(dev, "gr_reorder_states", gr_reorder_states, at, at if out is None else at_y, layout, a_parents, a_lengths)
     return to
 
 
@@ -652,6 +644,7 @@ class BlockPlan:
     copy_dst: torch.Tensor   # [rows] int32
     status: torch.Tensor     # [rows] int32
     workspace: torch.Tensor  # uint8, scratch
+    shape: tuple             # (rows, num_blocks, max_tokens)
 
 
 def block_plan(tables: BlockTables, append: torch.Tensor, max_tokens: int, keep: Optional[torch.Tensor] = None,
@@ -669,24 +662,22 @@ def block_plan(tables: BlockTables, append: torch.Tensor, max_tokens: int, keep:
     a_append = _need(append, "append", i32, (R,), dev)
     a_keep = _need(keep, "keep", i32, (R,), dev, optional=True)
     a_parents = _need(parents, "parents", i32, None, dev, optional=True)
-    if parents is not None and tuple(parents.shape) != (R,):
-        if tables.beams < 1 or tuple(parents.shape) != (R // tables.beams, tables.beams):
+    if parents is not None and parents.shape != (R,):
+        if tables.beams < 1 or parents.shape != (R // tables.beams, tables.beams):
             raise GrError("parents must be [rows] or [rows / beams, beams]")
-    wbytes = gr_block_workspace_bytes(R, N)
-    if wbytes == 0 or max_tokens < 0:
-        raise GrError("invalid shape")
-    if (out is None or out.slots.shape[0] != max_tokens or out.offsets.shape[0] != R + 1 or out.slots.device != dev
-            or out.workspace.numel() < wbytes):
+    if out is None or out.shape != (R, N, max_tokens) or out.slots.device != dev:
+        wbytes = gr_block_workspace_bytes(R, N)
+        if wbytes == 0 or max_tokens < 0:
+            raise GrError("invalid shape")
         out = BlockPlan(torch.empty(max_tokens, dtype=torch.int64, device=dev),
                         torch.empty(max_tokens, dtype=i32, device=dev), torch.empty(R + 1, dtype=i32, device=dev),
                         torch.empty(R, dtype=i32, device=dev), torch.empty(R, dtype=i32, device=dev),
-                        torch.empty(R, dtype=i32, device=dev), torch.empty(wbytes, dtype=torch.uint8, device=dev))
-    with _on(dev) as stream:
-        rc = gr_block_plan(a_table, R, width, tables.beams, tables.block_size, a_lengths, a_refs, N, a_parents, a_keep,
-                           a_append, max_tokens, out.workspace.data_ptr(), out.slots.data_ptr(), out.positions.data_ptr(),
-                           out.offsets.data_ptr(), out.copy_src.data_ptr(), out.copy_dst.data_ptr(),
-                           out.status.data_ptr(), stream)
-    _check(rc, "gr_block_plan")
+                        torch.empty(R, dtype=i32, device=dev), torch.empty(wbytes, dtype=torch.uint8, device=dev),
+                        (R, N, max_tokens))
+    _call(dev, "gr_block_plan", load_library().gr_block_plan, a_table, R, width, tables.beams, tables.block_size,
+          a_lengths, a_refs, N, a_parents, a_keep, a_append, max_tokens, out.workspace.data_ptr(), out.slots.data_ptr(),
+          out.positions.data_ptr(), out.offsets.data_ptr(), out.copy_src.data_ptr(), out.copy_dst.data_ptr(),
+          out.status.data_ptr())
     return out
 
 
@@ -701,18 +692,27 @@ def copy_blocks(caches, copy_src: torch.Tensor, copy_dst: torch.Tensor) -> None:
     dev = copy_src.device
     a_src = _need(copy_src, "copy_src", torch.int32)
     a_dst = _need(copy_dst, "copy_dst", torch.int32, copy_src.shape, dev)
-    groups = {}
+    # runs of caches of one layout: (blocks, bytes from one to the next, bytes, addresses)
+    runs = []
+    shape = step = kind = None
     for x in caches:
-        if not (isinstance(x, torch.Tensor) and x.is_cuda and x.device == dev and x.dim() >= 1):
+        if not isinstance(x, torch.Tensor) or x.device != dev:
             raise GrError("caches must be CUDA tensors [num_blocks, ...] on the device of copy_src")
-        if x.numel() == 0:
-            continue
-        per = x.numel() // x.shape[0]
-        if not x[0].is_contiguous() or (x.shape[0] > 1 and x.stride(0) < per):
-            raise GrError("caches: a block's elements must lie next to one another, and the blocks apart")
-        e = x.element_size()
-        groups.setdefault((x.shape[0], (x.stride(0) if x.shape[0] > 1 else per) * e, per * e), []).append(x.data_ptr())
-    with _on(dev) as stream:
-        for (blocks, stride, size), at in groups.items():
-            rc = gr_copy_blocks(at, blocks, stride, size, a_src, a_dst, int(copy_src.shape[0]), stream)
-            _check(rc, "gr_copy_blocks")
+        if x.shape != shape or x.stride() != step or x.dtype is not kind:
+            shape, step, kind = x.shape, x.stride(), x.dtype
+            if x.dim() < 1:
+                raise GrError("caches must be [num_blocks, ...]")
+            per = x.numel() // shape[0] if shape[0] else 0
+            if per and (not x[0].is_contiguous() or (shape[0] > 1 and step[0] < per)):
+                raise GrError("caches: a block's elements must lie next to one another, and the blocks apart")
+            e = x.element_size()
+            runs.append((shape[0], (step[0] if shape[0] > 1 else per) * e, per * e, []))
+        if per:
+            runs[-1][3].append(x.data_ptr())
+    if len(runs) > 1:
+        first = [p for r in runs for p in r[3]]
+        if len(set(first)) < len(first):
+            raise GrError("the same cache twice")
+    for blocks, stride, size, at in runs:
+        if at:
+            _call(dev, "gr_copy_blocks", gr_copy_blocks, at, blocks, stride, size, a_src, a_dst, copy_src.shape[0])
