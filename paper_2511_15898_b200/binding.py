@@ -467,14 +467,20 @@ def _need(t, what: str, dtype, shape=None, device=None, optional: bool = False):
     return t.data_ptr()
 
 
+# (the handle alone: the public call makes a Stream object around it, 3 us)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+    lambda index: int(torch.cuda.current_stream(index).cuda_stream))
+
+
 def _call(dev: torch.device, what: str, function, *args):
     """A C entry point with the tensors' device current and that device's current stream."""
     if torch.cuda.current_device() == dev.index:
-        rc = function(*args, _stream())
+        rc = function(*args, _raw_stream(dev.index))
     else:
         with torch.cuda.device(dev):
-            rc = function(*args, _stream())
-    _check(rc, what)
+            rc = function(*args, _raw_stream(dev.index))
+    if rc != 0:
+        _check(rc, what)
 
 
 @dataclasses.dataclass
@@ -596,7 +602,7 @@ def reorder_states(states, parents: torch.Tensor, lengths: Optional[torch.Tensor
             layout = StateLayout(B, W, chosen, parts, step[0] * e if B > 1 else 0, step[1] * e if W > 1 else 0, part_step,
                                  step_y[0] * e if B > 1 else 0,
                                  step_y[1] * e if (W if out is None else chosen) > 1 else 0, part_step_y, part, token)
-            runs.append((layout, [], [], _span(x), _span(y)))
+            runs.append((layout, [], [], _span(x) if out is not None else 0, _span(y) if out is not None else 0))
         if y is not x and (not isinstance(y, torch.Tensor) or y.shape != shape_y or y.dtype is not kind or y.device != dev):
             raise GrError("out must hold tensors [B, chosen, ...] like the states")
         runs[-1][1].append(x.data_ptr())
@@ -608,7 +614,7 @@ def reorder_states(states, parents: torch.Tensor, lengths: Optional[torch.Tensor
                 and any(p < q + n and q < p + m for _, _, at, _, m in runs for p in at for _, of, _, n, _ in runs for q in of)):
             raise GrError("out shares memory with the states")
     if len(runs) > 1:
-        first = [p for r in runs if r[3] for p in (r[1] if out is None else r[2])]
+        first = [p for r in runs if r[0].part_bytes for p in (r[1] if out is None else r[2])]
         if len(set(first)) < len(first):
             raise GrError("the same tensor twice")
     for layout, at, at_y, _, _ in runs:
