@@ -387,7 +387,8 @@ int gr_reorder_states(const void* const* src, void* const* dst, int count, const
  *   GR_NO_BLOCKS  the row needs blocks, and up to and with it (counting all rows that are not GR_ROW_FULL or GR_BAD_ROW)
  *                 more are needed than are free;
  *   GR_BAD_ROW    append[r] < 0 (taken as 0), lengths[parent] outside 0 .. width * block_size (clamped), a parent outside
- *                 -1 .. beams - 1 (taken as -1), or a held block id that the call reads and that is outside the pool.
+ *                 -1 .. beams - 1 (taken as -1), or a held block id outside the pool, where the call meets one: it looks at
+ *                 all blocks of a row that goes on from another, and at the partly filled one that is to be written to.
  *   keep[r] < 0 counts as 0.
  *   table     in/out [rows, width] int.  Entries that a row no longer holds become -1.  (Start with -1 everywhere.)
  *   lengths   in/out [rows] int;  refs in/out [num_blocks] int.   (Start with 0.)

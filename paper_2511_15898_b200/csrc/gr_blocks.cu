@@ -1,16 +1,23 @@
-// gr_block_plan: block tables, reference counts and slots of a paged cache for the next step, in one launch of one cluster.
+// gr_block_plan: block tables, reference counts and slots of a paged cache for the next step.
 //
 // Rows and blocks depend on one another through sums only: how many rows hold a block, how many of the holders are about to
-// write to it, how many blocks the rows before need, how many of the blocks before are free.  The phases between those
-// sums are separated by cluster barriers, so that a step is one launch instead of a chain of them; what a phase hands to the
-// next lies in the workspace.
+// write to it, how many blocks the rows before need, how many of the blocks before are free.  One cluster of CTAs goes through
+// the phases between those sums, separated by cluster barriers, instead of a chain of launches.  Around it two kernels for all
+// SMs, where there is work for them: tables that follow parents (before), and slot maps of many tokens (after).
+#include <limits.h>
+#include <algorithm>
 #include "gr_host.h"
 
 namespace gr {
 
-constexpr int kPlanThreads = 1024;
+constexpr int kPlanThreads = 512;
+constexpr int kPlanNear = 1024;            // rows that every CTA holds in shared memory
 constexpr int kPlanWarps = kPlanThreads / 32;
 constexpr int kPlanCluster = 8;
+constexpr int kSlotThreads = 256;
+constexpr int kForkThreads = 256;
+constexpr int kForkSplits = 16;
+constexpr int kSlotsAlone = 32768;          // slot maps beyond this are written by a kernel of their own
 
 // a row between the phases
 struct __align__(16) PlanRow {
@@ -20,9 +27,9 @@ struct __align__(16) PlanRow {
     int need, copies;         // blocks needed, one of them for a copy
     int status;
     int parent;               // row of the table it goes on from, or -1
-    int bad;                  // a held id outside the pool was met
     int first_token;          // number of its first token
     int start;                // number of its first new block among all needed
+    int pad;
 };
 static_assert(sizeof(PlanRow) == 48, "workspace layout");
 
@@ -34,10 +41,13 @@ struct PlanArgs {
     unsigned long long* best; int* writers;     // per block: the writer with the most tokens in it; number of writers
     int* fresh;                                  // the free blocks with the smallest ids, as many as are needed
     int* part;                                   // free blocks by CTA
+    unsigned char* bad;                          // per part of a group's columns and row: a held id outside the pool was met
     int rows, width, beams, block, num_blocks, max_tokens;
+    int wide, split;                             // refs, slots and positions lie on 16 bytes; slots by a kernel of their own
+    int splits;                                  // parts of a group's columns
 };
 
-__host__ __device__ inline int div_up(int a, int b) { return (int)(((long long)a + b - 1) / b); }
+__host__ __device__ inline int div_up(int a, int b) { return a / b + (a % b != 0 ? 1 : 0); }
 
 // Exclusive sum over the CTA's threads, in their order; the total in `total`.  (s_part: one entry per warp and one more.)
 __device__ __forceinline__ long long cta_scan(long long v, GR_PTR(long long) s_part, long long& total)
@@ -59,7 +69,7 @@ __device__ __forceinline__ long long cta_scan(long long v, GR_PTR(long long) s_p
             const long long y = __shfl_up_sync(0xffffffffu, z, o);
             if (lane >= o) z += y;
         }
-        s_part[lane] = z - w;
+        if (lane < kPlanWarps) s_part[lane] = z - w;
         if (lane == 31) s_part[kPlanWarps] = z;
     }
     __syncthreads();
@@ -70,213 +80,373 @@ __device__ __forceinline__ long long cta_scan(long long v, GR_PTR(long long) s_p
 // a count of block b, where there is such a block
 __device__ __forceinline__ void count_add(int* counts, int n, int b, int v) { if (b >= 0 && b < n) atomicAdd(counts + b, v); }
 
-__device__ __forceinline__ void plan_barrier() {
-    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+// which of the blocks i .. i + 3 are free, as bits
+__device__ __forceinline__ unsigned free_of(GR_PTR(int) refs, long long i, int n, bool wide)
+{
+    unsigned m = 0;
+#ifndef GR_CHECK
+    if (wide && i + 4 <= n) {
+        const int4 v = *reinterpret_cast<const int4*>(refs + i);
+        return (v.x == 0 ? 1u : 0u) | (v.y == 0 ? 2u : 0u) | (v.z == 0 ? 4u : 0u) | (v.w == 0 ? 8u : 0u);
+    }
+#endif
+    for (int k = 0; k < 4; k++) if (i + k < n && refs[i + k] == 0) m |= 1u << k;
+    return m;
 }
 
-// W: room for a group's entries of a column
+__device__ __forceinline__ void plan_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void plan_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+__device__ __forceinline__ void plan_barrier() { plan_arrive(); plan_wait(); }
+
+__host__ __device__ inline int plan_hash_size(int rows) { int n = 32; while (n < 2 * rows) n *= 2; return n; }
+
+// place of block b in the table of shared blocks, which it enters if it is not there (there is room for every row's)
+__device__ __forceinline__ int plan_find(GR_PTR(int) h_block, int size, int b)
+{
+    int at = (int)(((unsigned)b * 2654435761u) >> 7) & (size - 1);
+    for (int k = 0; k < size; k++, at = (at + 1) & (size - 1)) {
+        const int was = atomicCAS(&h_block[at], -1, b);
+        if (was == -1 || was == b) return at;
+    }
+    return 0;
+}
+
+// What row r keeps: its numbers that depend on no other row's.
+struct PlanKeep { int status, parent, base, before, kept; };
+__device__ __forceinline__ PlanKeep plan_keep(const PlanArgs& A, int r)
+{
+    const long long most = (long long)A.width * A.block;
+    const long long own = A.lengths[r];
+    const int keep = A.keep ? max(0, A.keep[r]) : INT_MAX;
+    PlanKeep k;
+    k.status = GR_OK;
+    k.parent = r;
+    long long len = own;
+    if (A.parents) {
+        const int p = A.parents[r];
+        if (p < -1 || p >= A.beams) k.status = GR_BAD_ROW;
+        k.parent = p >= 0 && p < A.beams ? r / A.beams * A.beams + p : -1;
+        len = k.parent >= 0 ? A.lengths[k.parent] : 0;
+    }
+    if (len < 0 || len > most) { k.status = GR_BAD_ROW; len = min(max(len, 0ll), most); }
+    k.base = min((int)len, keep);
+    k.before = div_up((int)min(max(own, 0ll), most), A.block);
+    k.kept = div_up(k.base, A.block);
+    return k;
+}
+
+// The tables follow the parents and the counts follow the tables: a group per CTA, or part of its columns.  A lane owns a
+// column of the group's tables and reads all of its entries before it writes one.
 template <int W>
+__global__ void __launch_bounds__(kForkThreads)
+fork_kernel(const __grid_constant__ PlanArgs A)
+{
+    __shared__ PlanKeep s_row[W];
+    __shared__ int s_bad[W], s_any;
+    pdl_wait();
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, G = A.beams, N = A.num_blocks;
+    const int r0 = blockIdx.x * G;
+    if (tid == 0) s_any = 0;
+    __syncthreads();
+    if (tid < G) {
+        const PlanKeep k = plan_keep(A, r0 + tid);
+        s_row[tid] = k;
+        s_bad[tid] = 0;
+        // (the columns that there is anything to do in: of a row that goes on from itself, those it releases)
+        const int upto = k.parent == r0 + tid ? (k.before > k.kept ? k.before : 0) : max(k.before, k.kept);
+        atomicMax(&s_any, upto);
+    }
+    __syncthreads();
+    const int upto = s_any;
+#pragma unroll 1
+    for (int c = ((int)blockIdx.y * (kForkThreads / 32) + warp) * 32 + lane; c < upto; c += (int)gridDim.y * kForkThreads) {
+        int now[W], was[W];
+#pragma unroll
+        for (int j = 0; j < W; j++) {
+            now[j] = was[j] = -1;
+            if (j < G && c < s_row[j].kept) now[j] = A.table[(long long)s_row[j].parent * A.width + c];
+            if (j < G && c < s_row[j].before) was[j] = A.table[(long long)(r0 + j) * A.width + c];
+        }
+#pragma unroll
+        for (int j = 0; j < W; j++) {
+            if (j >= G) break;
+            const bool held = c < s_row[j].before, holds = c < s_row[j].kept;
+            if (holds && (now[j] < 0 || now[j] >= N)) s_bad[j] = 1;
+            if (held ? was[j] == now[j] : !holds) continue;
+            if (held) count_add(A.refs, N, was[j], -1);
+            if (holds) count_add(A.refs, N, now[j], 1);
+            A.table[(long long)(r0 + j) * A.width + c] = now[j];
+        }
+    }
+    __syncthreads();
+    if (tid < G) A.bad[(size_t)blockIdx.y * A.rows + r0 + tid] = (unsigned char)s_bad[tid];
+}
+
+// a writer of a shared block that is about to be written to: by its tokens in the block, then the lowest row
+__device__ __forceinline__ unsigned long long writer_rank(int tokens, int r) { return ((unsigned long long)tokens << 32) | (0xffffffffu - (unsigned)r); }
+
+// Slots of the appended tokens, K neighbouring ones per thread (four where there are many: one search for the row, one store of
+// each kind for them).
+// `first(r)`: number of row r's first token; `at(r)`: the row.
+template <int K, class First, class Row>
+__device__ __forceinline__ void write_slots(const PlanArgs& A, GR_PTR(int) fresh, int total, long long thread, long long threads, First first, Row at)
+{
+    const int bs = A.block, R = A.rows;
+    for (long long i0 = K * thread; i0 < A.max_tokens; i0 += K * threads) {
+        long long slot[K];
+        int position[K];
+        int r = 0, next = 0, block = 0, within = 0;          // tokens up to `next` are row r's
+        bool entered = false;                                // block and within are the last token's
+        PlanRow q = {};
+#pragma unroll
+        for (int k = 0; k < K; k++) {
+            const int i = (int)i0 + k;
+            slot[k] = -1; position[k] = -1;
+            if (i0 + k >= total) continue;
+            if (i >= next) {
+                // the last row that begins at or before token i (rows without tokens begin where the next one does)
+                int lo = r, hi = R - 1;
+                while (lo < hi) {
+                    const int mid = (lo + hi + 1) >> 1;
+                    if (first(mid) <= i) lo = mid; else hi = mid - 1;
+                }
+                r = lo; entered = false;
+                next = r + 1 < R ? first(r + 1) : total;
+                q = at(r);
+            }
+            const int t = i - q.first_token;
+            if (t >= q.ask) continue;
+            position[k] = q.base + t;
+            if (entered && within + 1 < bs) within++;
+            else {
+                const int c = position[k] / bs;
+                within = position[k] - c * bs;
+                if (c >= q.kept) block = fresh[q.start + q.copies + c - q.kept];
+                else block = q.copies ? fresh[q.start] : q.last;
+                entered = true;
+            }
+            slot[k] = (long long)block * bs + within;
+        }
+        if (K == 4 && A.wide && i0 + K <= A.max_tokens) {
+            *reinterpret_cast<longlong2*>(A.slots + i0) = make_longlong2(slot[0], slot[K / 4]);
+            *reinterpret_cast<longlong2*>(A.slots + i0 + 2) = make_longlong2(slot[K / 2], slot[K - 1]);
+            *reinterpret_cast<int4*>(A.positions + i0) = make_int4(position[0], position[K / 4], position[K / 2], position[K - 1]);
+        } else {
+#pragma unroll
+            for (int k = 0; k < K; k++) if (i0 + k < A.max_tokens) { A.slots[i0 + k] = slot[k]; A.positions[i0 + k] = position[k]; }
+        }
+    }
+}
+
+// kNear: up to kPlanNear rows.  Every CTA then works all rows out for itself, in its shared memory, and the CTAs wait for one
+// another only where tables and counts have changed and where free blocks are numbered.  With more rows each CTA has a share of
+// them and the others' in the workspace.
+template <bool kNear>
 __global__ void __launch_bounds__(kPlanThreads)
 plan_kernel(const __grid_constant__ PlanArgs A)
 {
+    extern __shared__ __align__(16) unsigned char s_dyn[];
     __shared__ long long s_part_raw[kPlanWarps + 1];
     pdl_wait();
     GR_CHECK_FLAG_DECL;
     GR_CHECK_FLAG_INIT;
-    GR_PTR(long long) s_part = GR_MKPTR(long long, s_part_raw, kPlanWarps + 1, GR_CHECK_FLAG);
-    GR_PTR(int) table = GR_MKPTR(int, A.table, (long long)A.rows * A.width, GR_CHECK_FLAG);
-    GR_PTR(int) lengths = GR_MKPTR(int, A.lengths, A.rows, GR_CHECK_FLAG);
-    GR_PTR(int) refs = GR_MKPTR(int, A.refs, A.num_blocks, GR_CHECK_FLAG);
-    GR_PTR(PlanRow) row = GR_MKPTR(PlanRow, A.row, A.rows, GR_CHECK_FLAG);
-    GR_PTR(unsigned long long) best = GR_MKPTR(unsigned long long, A.best, A.num_blocks, GR_CHECK_FLAG);
-    GR_PTR(int) writers = GR_MKPTR(int, A.writers, A.num_blocks, GR_CHECK_FLAG);
-    GR_PTR(int) fresh = GR_MKPTR(int, A.fresh, A.num_blocks, GR_CHECK_FLAG);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int ctas = gridDim.x, me = blockIdx.x;
     const int R = A.rows, bs = A.block, N = A.num_blocks;
-    const int G = A.parents ? A.beams : 1;        // (without parents a row's table depends on its own alone)
     const long long most = (long long)A.width * bs;
+    GR_PTR(long long) s_part = GR_MKPTR(long long, s_part_raw, kPlanWarps + 1, GR_CHECK_FLAG);
+    GR_PTR(int) table = GR_MKPTR(int, A.table, (long long)A.rows * A.width, GR_CHECK_FLAG);
+    GR_PTR(int) refs = GR_MKPTR(int, A.refs, A.num_blocks, GR_CHECK_FLAG);
+    GR_PTR(PlanRow) row = GR_MKPTR(PlanRow, kNear ? reinterpret_cast<PlanRow*>(s_dyn) : A.row, A.rows, GR_CHECK_FLAG);
+    GR_PTR(unsigned long long) best = GR_MKPTR(unsigned long long, A.best, A.num_blocks, GR_CHECK_FLAG);
+    GR_PTR(int) writers = GR_MKPTR(int, A.writers, A.num_blocks, GR_CHECK_FLAG);
+    GR_PTR(int) fresh = GR_MKPTR(int, A.fresh, A.num_blocks, GR_CHECK_FLAG);
+    // near: the shared blocks that are written to, by open addressing (hash_size a power of two, twice the rows at least)
+    const int hash_size = kNear ? plan_hash_size(R) : 1;
+    GR_PTR(unsigned long long) h_best = GR_MKPTR(unsigned long long, reinterpret_cast<unsigned long long*>(s_dyn + sizeof(PlanRow) * (kNear ? R : 0)), hash_size, GR_CHECK_FLAG);
+    GR_PTR(int) h_block = GR_MKPTR(int, reinterpret_cast<int*>(s_dyn + sizeof(PlanRow) * (kNear ? R : 0) + 8 * (size_t)hash_size), hash_size, GR_CHECK_FLAG);
+    GR_PTR(int) h_count = GR_MKPTR(int, reinterpret_cast<int*>(s_dyn + sizeof(PlanRow) * (kNear ? R : 0) + 12 * (size_t)hash_size), hash_size, GR_CHECK_FLAG);
+    // far: this CTA's rows are me, me + ctas, ...; near: all
+    auto mine = [&](int r) { return kNear || r % ctas == me; };
 
     // ---- A: what each row keeps and asks for.  Every CTA sums the rows' tokens for itself; a thread has neighbouring rows.
+    const int per = div_up(R, kPlanThreads), lo = min(R, tid * per), hi = min(R, lo + per);
+    long long total;
     {
-        const int per = div_up(R, kPlanThreads), lo = min(R, tid * per), hi = min(R, lo + per);
-        long long sum = 0, total;
+        if (kNear) for (int i = tid; i < hash_size; i += kPlanThreads) { h_best[i] = 0ull; h_block[i] = -1; h_count[i] = 0; }
+        long long sum = 0;
         for (int r = lo; r < hi; r++) sum += max(0, A.append[r]);
+        // (a thread with one row: its loads do not wait for the sum)
+        const bool ahead = kNear && per == 1;
+        PlanKeep k;
+        if (ahead && lo < hi) k = plan_keep(A, lo);
         long long at = cta_scan(sum, s_part, total);
         for (int r = lo; r < hi; r++) {
             const int want = A.append[r];
             const long long from = at;
             at += max(0, want);
-            if (r % ctas != me) continue;
+            if (!mine(r)) continue;
+            if (!ahead) k = plan_keep(A, r);
             PlanRow q;
-            q.status = want < 0 ? GR_BAD_ROW : GR_OK;
-            q.parent = r;
-            if (A.parents) {
-                const int p = A.parents[r];
-                if (p < -1 || p >= A.beams) q.status = GR_BAD_ROW;
-                q.parent = p >= 0 && p < A.beams ? r / A.beams * A.beams + p : -1;
-            }
-            long long len = q.parent >= 0 ? lengths[q.parent] : 0;
-            if (len < 0 || len > most) { q.status = GR_BAD_ROW; len = min(max(len, 0ll), most); }
-            q.base = (int)len;
-            if (A.keep) q.base = min(q.base, max(0, A.keep[r]));
-            q.before = div_up((int)min(max((long long)lengths[r], 0ll), most), bs);
-            q.kept = div_up(q.base, bs);
+            q.status = want < 0 ? GR_BAD_ROW : k.status;
+            q.parent = k.parent; q.base = k.base; q.before = k.before; q.kept = k.kept;
             q.ask = max(0, want);
             if (q.status == GR_OK && ((long long)q.base + q.ask > most || at > A.max_tokens)) q.status = GR_ROW_FULL;
             if (q.status != GR_OK) q.ask = 0;
             q.first_token = (int)min(from, (long long)A.max_tokens);
-            q.last = -1; q.need = 0; q.copies = 0; q.bad = 0; q.start = 0;
-            if (q.ask > 0 && q.base % bs != 0) {
-                const int b = table[(long long)q.parent * A.width + q.base / bs];
-                if (b >= 0 && b < N) { q.last = b; best[b] = 0ull; writers[b] = 0; }
-            }
+            q.last = -1; q.need = 0; q.copies = 0; q.start = 0; q.pad = 0;
             row[r] = q;
-            A.offsets[r] = q.first_token;
+            if (r % ctas == me) A.offsets[r] = q.first_token;
         }
         if (me == 0 && tid == 0) A.offsets[R] = (int)min(total, (long long)A.max_tokens);
     }
-    plan_barrier();
+    if (kNear) __syncthreads(); else plan_barrier();
 
-    // ---- B: the tables follow the parents, the counts follow the tables; who writes to which block.
-    // A lane owns a column of its group's tables and reads all the entries it needs before it writes one.
-    {
-        const int segs = div_up(A.width, 32);
-        const long long units = (long long)(R / G) * segs;
-#pragma unroll 1
-        for (long long u = (long long)me * kPlanWarps + warp; u < units; u += (long long)ctas * kPlanWarps) {
-            const int r0 = (int)(u / segs) * G, c = (int)(u % segs) * 32 + lane;
-            if (c >= A.width) continue;
-            int now[W];
-#pragma unroll
-            for (int j = 0; j < W; j++) {
-                now[j] = -1;
-                if (j < G && c < row[r0 + j].kept) now[j] = table[(long long)row[r0 + j].parent * A.width + c];
-            }
-#pragma unroll
-            for (int j = 0; j < W; j++) {
-                if (j >= G) break;
-                const bool held = c < row[r0 + j].before, holds = c < row[r0 + j].kept;
-                if (holds && (now[j] < 0 || now[j] >= N)) row[r0 + j].bad = 1;
-                if (!held && !holds) continue;
-                const long long at = (long long)(r0 + j) * A.width + c;
-                const int old = held ? table[at] : -1;
-                if (held && old == now[j]) continue;
-                if (held) count_add(A.refs, N, old, -1);
-                if (holds) count_add(A.refs, N, now[j], 1);
-                table[at] = now[j];
+    // ---- B: without parents a row only releases what it does not keep, mostly nothing (a warp per row)
+    if (!A.parents) {
+        for (int r = me + ctas * warp; r < R; r += ctas * kPlanWarps) {
+            const int before = row[r].before;
+            for (int c = row[r].kept + lane; c < before; c += 32) {
+                const long long at = (long long)r * A.width + c;
+                count_add(A.refs, N, table[at], -1);
+                table[at] = -1;
             }
         }
-        for (int r = me * kPlanThreads + tid; r < R; r += ctas * kPlanThreads) {
-            const int b = row[r].last;
-            if (b < 0) continue;
-            count_add(A.writers, N, b, 1);
-            atomicMax(A.best + b, ((unsigned long long)(row[r].base % bs) << 32) | (0xffffffffu - (unsigned)r));
-        }
+        plan_barrier();
     }
-    plan_barrier();
 
-    // ---- C: what each row needs; how many blocks are free
-    for (int r = me * kPlanThreads + tid; r < R; r += ctas * kPlanThreads) {
-        PlanRow q = row[r];
-        if (q.bad) q.status = GR_BAD_ROW;
-        // (a writer without a valid last block has met an id outside the pool)
-        if (q.status == GR_OK && q.ask > 0) {
-            if (q.last >= 0 && refs[q.last] > 1) {
-                const bool keeps = writers[q.last] == refs[q.last] && (unsigned)best[q.last] == 0xffffffffu - (unsigned)r;
-                q.copies = keeps ? 0 : 1;
-            }
-            q.need = q.copies + div_up(q.base + q.ask, bs) - q.kept;
-        } else q.ask = 0;
-        row[r] = q;
-    }
+    // ---- C: who writes to a shared block, what each row needs; how many blocks are free
     const int share = (div_up(N, ctas * kPlanThreads) + 3) & ~3;
     const long long b0 = ((long long)me * kPlanThreads + tid) * share;
     int free_here = 0;
-    for (int i = 0; i < share; i++) if (b0 + i < N && refs[b0 + i] == 0) free_here++;
+    for (int i = 0; i < share; i += 4) free_here += __popc(free_of(refs, b0 + i, N, A.wide));
+    for (int r = lo; r < hi; r++) {
+        if (!mine(r)) continue;
+        PlanRow q = row[r];
+        if (A.parents) for (int y = 0; y < A.splits; y++) if (A.bad[(size_t)y * R + r]) q.status = GR_BAD_ROW;
+        if (q.status == GR_OK && q.ask > 0 && q.base % bs != 0) {
+            const int b = table[(long long)r * A.width + q.base / bs];
+            if (b < 0 || b >= N) q.status = GR_BAD_ROW;
+            else {
+                q.last = b;
+                q.need = refs[b];                            // (for now: the block's holders)
+                if (!kNear && q.need > 1) { best[b] = 0ull; writers[b] = 0; }
+            }
+        }
+        if (q.status != GR_OK) q.ask = 0;
+        row[r] = q;
+        if (kNear && q.need > 1) {
+            const int at = plan_find(h_block, hash_size, q.last);
+            atomicAdd(&h_count[at], 1);
+            atomicMax(&h_best[at], writer_rank(q.base % bs, r));
+        }
+    }
     long long cta_free;
-    const long long free_before = cta_scan(free_here, s_part, cta_free);
+    const long long free_before = cta_scan(free_here, s_part, cta_free);     // (a barrier too)
     if (tid == 0) A.part[me] = (int)cta_free;
-    plan_barrier();
-
+    if (!kNear) {
+        plan_barrier();
+        for (int r = lo; r < hi; r++) {
+            if (!mine(r) || row[r].need <= 1) continue;
+            count_add(A.writers, N, row[r].last, 1);
+            atomicMax(A.best + row[r].last, writer_rank(row[r].base % bs, r));
+        }
+        plan_barrier();
+    }
+    long long sum = 0;
+    for (int r = lo; r < hi; r++) {
+        if (!mine(r)) continue;
+        PlanRow q = row[r];
+        if (q.need > 1) {
+            // (every holder writes, and this one has the most tokens in the block: it keeps it)
+            const int at = kNear ? plan_find(h_block, hash_size, q.last) : q.last;
+            const int writing = kNear ? h_count[at] : writers[at];
+            const unsigned long long first = kNear ? h_best[at] : best[at];
+            q.copies = writing == q.need && (unsigned)first == 0xffffffffu - (unsigned)r ? 0 : 1;
+        }
+        q.need = q.ask > 0 ? q.copies + div_up(q.base + q.ask, bs) - q.kept : 0;
+        sum += q.need;
+        row[r] = q;
+    }
     // ---- D: the rows' places among the needed blocks; the free blocks by number
+    long long needed, place = 0;
+    if (kNear) place = cta_scan(sum, s_part, needed);
+    plan_barrier();
+    if (!kNear) {
+        sum = 0;
+        for (int r = lo; r < hi; r++) sum += row[r].need;
+        place = cta_scan(sum, s_part, needed);
+    }
     long long avail = 0, ahead = 0;
     for (int i = 0; i < ctas; i++) { const int f = A.part[i]; if (i < me) ahead += f; avail += f; }
-    long long needed;
-    {
-        const int per = div_up(R, kPlanThreads), lo = min(R, tid * per), hi = min(R, lo + per);
-        long long sum = 0;
-        for (int r = lo; r < hi; r++) sum += row[r].need;
-        long long at = cta_scan(sum, s_part, needed);
-        for (int r = lo; r < hi; r++) {
-            const int n = row[r].need;
-            const long long from = at;
-            at += n;
-            if (r % ctas != me) continue;
-            if (n > 0 && at > avail) { row[r].status = GR_NO_BLOCKS; row[r].ask = 0; row[r].copies = 0; row[r].start = 0; }
-            else row[r].start = (int)from;
-        }
+    for (int r = lo; r < hi; r++) {
+        const int n = row[r].need;
+        const long long from = place;
+        place += n;
+        if (!mine(r)) continue;
+        if (n > 0 && place > avail) { row[r].status = GR_NO_BLOCKS; row[r].ask = 0; row[r].copies = 0; row[r].start = 0; }
+        else row[r].start = (int)from;
     }
     {
         long long k = ahead + free_before;
         const long long upto = min(needed, avail);
-        for (int i = 0; i < share && k < upto; i++)
-            if (b0 + i < N && refs[b0 + i] == 0) fresh[k++] = (int)(b0 + i);
+        for (int i = 0; i < share && free_here > 0 && k < upto; i += 4) {
+            for (unsigned m = free_of(refs, b0 + i, N, A.wide); m && k < upto; m &= m - 1) fresh[k++] = (int)(b0 + i) + __ffs(m) - 1;
+        }
     }
     plan_barrier();
 
-    // ---- E: rows take their blocks (a warp per row); tokens get their slots
-    for (int r = me * kPlanWarps + warp; r < R; r += ctas * kPlanWarps) {
+    // ---- E: rows take their blocks, a warp for each; tokens get their slots
+    for (int r = me + ctas * warp; r < R; r += ctas * kPlanWarps) {
         const PlanRow q = row[r];
+        const long long line = (long long)r * A.width;
         const int after = div_up(q.base + q.ask, bs);
-        const long long mine = (long long)r * A.width;
+        for (int c = q.kept + lane; c < after; c += 32) {
+            const int b = fresh[q.start + q.copies + c - q.kept];
+            table[line + c] = b;
+            refs[b] = 1;
+        }
         if (lane == 0) {
-            int from = -1, to = -1;
+            int src = -1, dst = -1;
             if (q.copies) {
-                from = q.last; to = fresh[q.start];
-                count_add(A.refs, N, from, -1);
-                refs[to] = 1;
-                table[mine + q.base / bs] = to;
+                src = q.last; dst = fresh[q.start];
+                count_add(A.refs, N, src, -1);
+                refs[dst] = 1;
+                table[line + q.base / bs] = dst;
             }
-            A.copy_src[r] = from; A.copy_dst[r] = to;
-            lengths[r] = q.base + q.ask;
+            A.copy_src[r] = src; A.copy_dst[r] = dst;
+            A.lengths[r] = q.base + q.ask;
             A.status[r] = q.status;
 #ifdef GR_CHECK
             if (GR_CHECK_VALUE) A.status[r] = GR_CHECK_FAILED;
 #endif
-        }
-        for (int c = q.kept + lane; c < after; c += 32) {
-            const int b = fresh[q.start + q.copies + c - q.kept];
-            table[mine + c] = b;
-            refs[b] = 1;
+            if (kNear && A.split) A.row[r] = q;
         }
     }
-    const int total = A.offsets[R];
-    for (int i = me * kPlanThreads + tid; i < A.max_tokens; i += ctas * kPlanThreads) {
-        long long slot = -1;
-        int position = -1;
-        if (i < total) {
-            // the last row that begins at or before token i (rows without tokens begin where the next one does)
-            int lo = 0, hi = R - 1;
-            while (lo < hi) {
-                const int mid = (lo + hi + 1) >> 1;
-                if (row[mid].first_token <= i) lo = mid; else hi = mid - 1;
-            }
-            const PlanRow q = row[lo];
-            const int k = i - q.first_token;
-            if (k < q.ask) {
-                position = q.base + k;
-                const int c = position / bs;
-                int b;
-                if (c >= q.kept) b = fresh[q.start + q.copies + c - q.kept];
-                else b = q.copies ? fresh[q.start] : q.last;
-                slot = (long long)b * bs + position % bs;
-            }
-        }
-        A.slots[i] = slot;
-        A.positions[i] = position;
+    if (!A.split) {
+        const int end = (int)min(total, (long long)A.max_tokens);
+        const long long thread = (long long)me + (long long)ctas * tid, threads = (long long)ctas * kPlanThreads;
+        auto first = [&](int r) { return row[r].first_token; };
+        auto at = [&](int r) { return (PlanRow)row[r]; };
+        if (A.max_tokens <= 2 * threads) write_slots<1>(A, fresh, end, thread, threads, first, at);
+        else write_slots<4>(A, fresh, end, thread, threads, first, at);
     }
+}
+
+// the slots of many tokens, by all SMs
+__global__ void __launch_bounds__(kSlotThreads)
+slots_kernel(const __grid_constant__ PlanArgs A)
+{
+    __shared__ int s_first[kPlanNear];
+    pdl_wait();
+    const bool near = A.rows <= kPlanNear;
+    if (near) {
+        for (int r = threadIdx.x; r < A.rows; r += kSlotThreads) s_first[r] = A.row[r].first_token;
+        __syncthreads();
+    }
+    GR_PTR(int) fresh = GR_MKPTR(int, A.fresh, A.num_blocks, nullptr);
+    write_slots<4>(A, fresh, A.offsets[A.rows], (long long)blockIdx.x * kSlotThreads + threadIdx.x, (long long)gridDim.x * kSlotThreads,
+                [&](int r) { return near ? s_first[r] : A.row[r].first_token; }, [&](int r) { return A.row[r]; });
 }
 
 static size_t plan_layout(int rows, int num_blocks, char* ws, PlanArgs* A)
@@ -288,8 +458,50 @@ static size_t plan_layout(int rows, int num_blocks, char* ws, PlanArgs* A)
     char* writers = take(4 * (size_t)num_blocks);
     char* fresh = take(4 * (size_t)num_blocks);
     char* part = take(4 * (size_t)kPlanCluster);
+    char* bad = take((size_t)kForkSplits * (size_t)rows);
+    if (A) A->bad = (unsigned char*)bad;
     if (A) { A->row = (PlanRow*)row; A->best = (unsigned long long*)best; A->writers = (int*)writers; A->fresh = (int*)fresh; A->part = (int*)part; }
     return at;
+}
+
+template <bool kNear>
+static int launch_plan(const PlanArgs& A, cudaStream_t st)
+{
+    // (near: the rows and the table of shared blocks)
+    const int smem = kNear ? (int)sizeof(PlanRow) * A.rows + 16 * plan_hash_size(A.rows) : 0;
+    if (smem > 40 * 1024) {
+        constexpr int kMost = (int)sizeof(PlanRow) * kPlanNear + 16 * 2 * kPlanNear;
+        static bool raised[kMaxDevices] = {false};
+        int dev = -1;
+        if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) { cudaGetLastError(); return GR_E_LAUNCH; }
+        if (!raised[dev]) {
+            if (cudaFuncSetAttribute(plan_kernel<kNear>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost) != cudaSuccess) {
+                cudaGetLastError();
+                return GR_E_LAUNCH;
+            }
+            raised[dev] = true;
+        }
+    }
+    launch_pdl_cluster(kPlanCluster, plan_kernel<kNear>, kPlanCluster, kPlanThreads, smem, st, A);
+    return GR_OK;
+}
+
+static void launch_fork(const PlanArgs& A, cudaStream_t st)
+{
+    const int groups = A.rows / A.beams;
+    if (groups == 0) return;
+    auto go = [&](auto kernel) {
+        cudaLaunchConfig_t cfg = {};
+        cudaLaunchAttribute at = {};
+        at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        at.val.programmaticStreamSerializationAllowed = 1;
+        cfg.gridDim = dim3(groups, A.splits); cfg.blockDim = dim3(kForkThreads); cfg.stream = st; cfg.attrs = &at; cfg.numAttrs = 1;
+        cudaLaunchKernelEx(&cfg, kernel, A);
+    };
+    if (A.beams <= 4) go(fork_kernel<4>);
+    else if (A.beams <= 8) go(fork_kernel<8>);
+    else if (A.beams <= 16) go(fork_kernel<16>);
+    else go(fork_kernel<32>);
 }
 
 static bool plan_shape_ok(int rows, int num_blocks) { return rows >= 0 && rows <= (1 << 20) && num_blocks >= 0 && num_blocks <= (1 << 26); }
@@ -323,16 +535,20 @@ int gr_block_plan(int* table, int rows, int width, int beams, int block_size, in
     A.slots = slots; A.positions = positions; A.offsets = offsets; A.copy_src = copy_src; A.copy_dst = copy_dst;
     A.status = status; A.rows = rows; A.width = width; A.beams = beams; A.block = block_size;
     A.num_blocks = num_blocks; A.max_tokens = max_tokens;
+    A.wide = (((uintptr_t)refs | (uintptr_t)slots | (uintptr_t)positions) & 15) == 0;
     cudaStream_t st = (cudaStream_t)stream;
     gr::NvtxRange whole("gr_block_plan");
-    const int ctas = gr::kPlanCluster;
-    auto go = [&](auto kernel) { gr::launch_pdl_cluster(ctas, kernel, ctas, gr::kPlanThreads, 0, st, A); };
-    const int group = parents ? beams : 1;
-    if (group == 1) go(gr::plan_kernel<1>);
-    else if (group <= 4) go(gr::plan_kernel<4>);
-    else if (group <= 8) go(gr::plan_kernel<8>);
-    else if (group <= 16) go(gr::plan_kernel<16>);
-    else go(gr::plan_kernel<32>);
+    A.split = max_tokens > gr::kSlotsAlone;
+    A.splits = 0;
+    if (parents && rows > 0) {
+        // (few groups: several CTAs to the columns of one)
+        const int segs = gr::div_up(width, gr::kForkThreads), room = 2 * gr::kSms / (rows / beams);
+        A.splits = std::max(1, std::min(std::min(segs, room), gr::kForkSplits));
+        gr::launch_fork(A, st);
+    }
+    const int rc = rows <= gr::kPlanNear ? gr::launch_plan<true>(A, st) : gr::launch_plan<false>(A, st);
+    if (rc != GR_OK) return rc;
+    if (A.split) gr::launch_pdl(gr::slots_kernel, (int)std::min<long long>(4 * gr::kSms, ((long long)max_tokens + 4 * gr::kSlotThreads - 1) / (4 * gr::kSlotThreads)), gr::kSlotThreads, 0, st, A);
     if (cudaPeekAtLastError() != cudaSuccess) { cudaGetLastError(); return GR_E_LAUNCH; }
     return GR_OK;
 }
