@@ -5,9 +5,10 @@
 // together, turns the listed logits into scores and ranks them.
 //
 // The sum.  With s = log2(e) / T split into two fp32 numbers (s_hi + s_lo, both positive) an element contributes
-// 2^(x s - R), R the whole number above x s of the largest element met so far by the thread: two FMAs and one ex2 an element,
-// no systematic error from the rounding of s (which alone costs 4e-7 of a log-sum over 10^5 ids), exact factors between sums of
-// different R, fp32 sums over one batch of vectors, fp64 from there on.  An element that is -infinity gives 0; NaN and
+// 2^(x s - R), R a whole number near x s of the largest element met by the thread: two FMAs and one ex2 an element, no
+// systematic error from the rounding of s (which alone costs 4e-7 of a log-sum over 10^5 ids), exact factors between sums of
+// different R, fp32 sums over one batch of vectors, fp64 from there on.  R follows the maximum only when that is kRise above it:
+// followed at once, nearly every batch of a warp held a lane with a new maximum, and half of the instructions were its factors.  An element that is -infinity gives 0; NaN and
 // +infinity make the sum NaN, as does a maximum whose product with s overflows: such rows' sums are taken again in fp64 by the
 // second kernel, which tells the two apart.
 //
@@ -29,6 +30,7 @@ constexpr int kBeamMaxListed = 4096;           // entries of a group's lists
 static_assert(GR_MAX_BEAMS * GR_MAX_SELECT <= kBeamMaxListed && GR_MAX_SELECT <= kMaxSupport, "lists");
 constexpr double kNear = 1e-6;
 constexpr float kLargestRef = 16777216.f;
+constexpr float kRise = 24.f;                  // (2^24 times what a batch adds up is far from fp32's range)
 
 // what a part leaves: this, then its keys (ckey) in descending order
 struct __align__(16) BeamPart {
@@ -108,20 +110,23 @@ beam_stream_kernel(const __grid_constant__ BeamArgs A)
     if (tid == 0) { sh.cnt = 0; sh.tau = -3.402823466e38f; sh.reset_checks(); }
     __syncthreads();
 
-    float g0 = -INFINITY, ref = -INFINITY;             // this thread's largest logit; the whole number above its product with s
+    float g0 = -INFINITY, ref = -INFINITY;             // this thread's largest logit; the whole number near its product with s
     double acc = 0.0;
     const unsigned long long hi2 = f_pack(A.s_hi, A.s_hi), lo2 = f_pack(A.s_lo, A.s_lo);
     const int rounds = first < nch ? (nch - first + stride - 1) / stride : 0;
-    // a new largest element: what has been added up moves to its reference
+    // a larger element: what has been added up moves to its reference where that is far above
     auto raise = [&](float m) {
-        g0 = m;
-        const float r = ceilf(m * A.s_hi);
-        if (acc != 0.0) acc = times_pow2(acc, ref - r);
-        ref = r;
+        g0 = fmaxf(g0, m);
+        const float at = m * A.s_hi;
+        if (at > ref + kRise) {
+            const float r = ceilf(at);
+            if (acc != 0.0) acc = times_pow2(acc, ref - r);
+            ref = r;
+        }
     };
     auto scalar = [&](int i, float tau) {
         const float v = load_logit<T>(x, i);
-        if (v > g0) raise(v);
+        raise(v);
         const float y = fmaf(v, A.s_lo, fmaf(v, A.s_hi, ref == -INFINITY ? 0.f : -ref));
         acc += (double)ex2(y);
         if (v >= tau) push_vector(sh, VT::alone(v), i);
@@ -161,7 +166,7 @@ beam_stream_kernel(const __grid_constant__ BeamArgs A)
                     float most = each[0];
 #pragma unroll
                     for (int u = 1; u < U; u++) { each[u] = VT::largest(v[u]); most = fmaxf(most, each[u]); }
-                    if (most > g0) raise(most);
+                    raise(most);
                     // (an element that is -infinity gives 0 whatever the reference, as long as that is finite)
                     const float down = ref == -INFINITY ? 0.f : -ref;
                     const unsigned long long down2 = f_pack(down, down);
