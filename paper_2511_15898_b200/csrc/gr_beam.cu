@@ -5,10 +5,10 @@
 // together, turns the listed logits into scores and ranks them.
 //
 // The sum.  With s = log2(e) / T split into two fp32 numbers (s_hi + s_lo, both positive) an element contributes
-// 2^(x s - R), R a whole number near x s of the largest element met by the thread: two FMAs and one ex2 an element, no
+// 2^(x s - R), R a whole number near x s of the largest element met: two FMAs and one ex2 an element, no
 // systematic error from the rounding of s (which alone costs 4e-7 of a log-sum over 10^5 ids), exact factors between sums of
-// different R, fp32 sums over one batch of vectors, fp64 from there on.  R follows the maximum only when that is kRise above it:
-// followed at once, nearly every batch of a warp held a lane with a new maximum, and half of the instructions were its factors.  An element that is -infinity gives 0; NaN and
+// different R, fp32 sums over one batch of vectors, fp64 from there on.  R is one for a warp and follows the maximum only where
+// that is kRise above it (more would cost accuracy: the products' rounding grows with the distance from R).  An element that is -infinity gives 0; NaN and
 // +infinity make the sum NaN, as does a maximum whose product with s overflows: such rows' sums are taken again in fp64 by the
 // second kernel, which tells the two apart.
 //
@@ -28,9 +28,9 @@ constexpr int kBeamMaxParts = 16;
 constexpr int kBeamMaxLists = 256;             // rows of a group times parts
 constexpr int kBeamMaxListed = 4096;           // entries of a group's lists
 static_assert(GR_MAX_BEAMS * GR_MAX_SELECT <= kBeamMaxListed && GR_MAX_SELECT <= kMaxSupport, "lists");
-constexpr double kNear = 1e-6;
+constexpr double kNear = 6e-7;
 constexpr float kLargestRef = 16777216.f;
-constexpr float kRise = 24.f;                  // (2^24 times what a batch adds up is far from fp32's range)
+constexpr float kRise = 1.f;
 
 // what a part leaves: this, then its keys (ckey) in descending order
 struct __align__(16) BeamPart {
@@ -110,27 +110,10 @@ beam_stream_kernel(const __grid_constant__ BeamArgs A)
     if (tid == 0) { sh.cnt = 0; sh.tau = -3.402823466e38f; sh.reset_checks(); }
     __syncthreads();
 
-    float g0 = -INFINITY, ref = -INFINITY;             // this thread's largest logit; the whole number near its product with s
+    float g0 = -INFINITY, ref = -INFINITY;             // this thread's largest logit; the warp's whole number near the products with s
     double acc = 0.0;
     const unsigned long long hi2 = f_pack(A.s_hi, A.s_hi), lo2 = f_pack(A.s_lo, A.s_lo);
     const int rounds = first < nch ? (nch - first + stride - 1) / stride : 0;
-    // a larger element: what has been added up moves to its reference where that is far above
-    auto raise = [&](float m) {
-        g0 = fmaxf(g0, m);
-        const float at = m * A.s_hi;
-        if (at > ref + kRise) {
-            const float r = ceilf(at);
-            if (acc != 0.0) acc = times_pow2(acc, ref - r);
-            ref = r;
-        }
-    };
-    auto scalar = [&](int i, float tau) {
-        const float v = load_logit<T>(x, i);
-        raise(v);
-        const float y = fmaf(v, A.s_lo, fmaf(v, A.s_hi, ref == -INFINITY ? 0.f : -ref));
-        acc += (double)ex2(y);
-        if (v >= tau) push_vector(sh, VT::alone(v), i);
-    };
     int r = 0, upto = use_tau ? 1 : rounds;
 #pragma unroll 1
     while (true) {
@@ -157,16 +140,24 @@ beam_stream_kernel(const __grid_constant__ BeamArgs A)
 #endif
                         if (ok) v[u] = ldg_stream(x + i0);
                     }
+                    // (the elements before the first and behind the last vector)
+                    float e0 = -INFINITY, e1 = -INFINITY;
                     if (nb == 0) {
-                        if (c == 0 && lane < head) scalar(lane, tau);
-                        if (c == nch - 1 && lane < tail) scalar(vec_end + lane, tau);
+                        if (c == 0 && lane < head) e0 = load_logit<T>(x, lane);
+                        if (c == nch - 1 && lane < tail) e1 = load_logit<T>(x, vec_end + lane);
                     }
                     float each[U];
-                    each[0] = VT::largest(v[0]);
-                    float most = each[0];
+                    float most = fmaxf(e0, e1);
 #pragma unroll
-                    for (int u = 1; u < U; u++) { each[u] = VT::largest(v[u]); most = fmaxf(most, each[u]); }
-                    raise(most);
+                    for (int u = 0; u < U; u++) { each[u] = VT::largest(v[u]); most = fmaxf(most, each[u]); }
+                    g0 = fmaxf(g0, most);
+                    // the reference follows the maximum of the warp, where that is kRise above it; what has been added up moves
+                    // there by an exact factor
+                    if (__any_sync(0xffffffffu, most * A.s_hi > ref + kRise)) {
+                        const float to = ceilf(warp_max(most) * A.s_hi);
+                        if (acc != 0.0) acc = times_pow2(acc, ref - to);
+                        ref = to;
+                    }
                     // (an element that is -infinity gives 0 whatever the reference, as long as that is finite)
                     const float down = ref == -INFINITY ? 0.f : -ref;
                     const unsigned long long down2 = f_pack(down, down);
@@ -180,7 +171,13 @@ beam_stream_kernel(const __grid_constant__ BeamArgs A)
                             sum2 = add2(sum2, f_pack(ex2(f_lo(y)), ex2(f_hi(y))));
                         }
                     }
-                    acc += (double)f_lo(sum2) + (double)f_hi(sum2);
+                    float sum = f_lo(sum2) + f_hi(sum2);
+                    if (nb == 0 && (c == 0 || c == nch - 1)) {
+                        sum += ex2(fmaf(e0, A.s_lo, fmaf(e0, A.s_hi, down))) + ex2(fmaf(e1, A.s_lo, fmaf(e1, A.s_hi, down)));
+                        if (e0 >= tau) push_vector(sh, VT::alone(e0), lane);
+                        if (e1 >= tau) push_vector(sh, VT::alone(e1), vec_end + lane);
+                    }
+                    acc += (double)sum;
 #pragma unroll
                     for (int u = 0; u < U; u++) if (each[u] >= tau) push_vector(sh, v[u], base + u * 32 * N);
                 };
@@ -214,15 +211,10 @@ beam_stream_kernel(const __grid_constant__ BeamArgs A)
     }
     // ---- the part's sum
     {
-        float top = ref;
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
         // (a thread that met NaN or +infinity holds NaN; one that met nothing, or -infinity only, 0)
-        double part_sum = acc;
-        if (acc != 0.0 && ref != top) part_sum = times_pow2(acc, ref - top);
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) part_sum += __shfl_xor_sync(0xffffffffu, part_sum, o);
-        if (lane == 0) { s_ref[warp] = top; s_sum[warp] = part_sum; }
+        for (int o = 16; o > 0; o >>= 1) acc += __shfl_xor_sync(0xffffffffu, acc, o);
+        if (lane == 0) { s_ref[warp] = ref; s_sum[warp] = acc; }
     }
     __syncthreads();
     // ---- candidates: a last threshold from the list itself, then keys of those that pass it
@@ -289,44 +281,68 @@ beam_stream_kernel(const __grid_constant__ BeamArgs A)
 // ---------------------------------------------------------------- the group's choice
 
 struct BeamGroup {
-    double lse[GR_MAX_BEAMS], scale[GR_MAX_BEAMS], score[GR_MAX_BEAMS];
-    double red[kBeamWarps];
+    double lse[GR_MAX_BEAMS], inv_scale[GR_MAX_BEAMS], score[GR_MAX_BEAMS];
+    double red[kBeamWarps], table[64];
+    double part_sum[kBeamMaxLists];
+    float part_ref[kBeamMaxLists];
+    int count[kBeamMaxLists];
     int length[GR_MAX_BEAMS];
-    unsigned char kind[GR_MAX_BEAMS], again[GR_MAX_BEAMS], exact[GR_MAX_BEAMS];
-    int bad, check, count, redo;
-    double least, slack;     // slack: kNear as a difference of keys
+    unsigned char row[kBeamMaxLists];          // a list's row
+    unsigned char kind[GR_MAX_BEAMS];
+    unsigned char again[GR_MAX_BEAMS];         // the row's sum is to be taken again (2: it was of no use)
+    unsigned char exact[GR_MAX_BEAMS];         // ... and has been
+    int bad, check, survivors, redo;
+    double least, slack;                       // slack: kNear as a difference of keys
     double best_key[GR_MAX_SELECT + 1];
     int best_at[GR_MAX_SELECT + 1];
 };
 constexpr int kRowNone = 0, kRowDone = 1, kRowLive = 2;
 
 // log sum exp(x / T) of a row in fp64, the same for every thread; -infinity for a row that is masked as a whole; `bad` set for
-// one with a NaN or +infinity.  (Every thread takes the elements of its index modulo the CTA's size, so that equal rows give
-// equal sums wherever they lie.)
+// one with a NaN or +infinity.  `top`: its largest logit where that is known (then there is no NaN in it), else NaN.  (Every
+// thread takes the elements of its index modulo the CTA's size, so that equal rows give equal sums wherever they lie.)
+// exp(-d) = 2^-n 2^(j / 64) exp(-r) by a table and five terms, |r| <= ln 2 / 128: a row of 152064 in 16 us, for 35 by exp_neg.
 template <typename T>
-__device__ __noinline__ double row_lse(const T* x, int V, double temp, double* red, int* bad)
+__device__ __noinline__ double row_lse(const T* x, int V, double temp, float known, const double* table, double* red, int* bad)
 {
+    constexpr int kAhead = 8;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    float m = -INFINITY;
-    int wrong = 0;
-    for (int i = tid; i < V; i += kBeamThreads) {
-        const float v = load_logit<T>(x, i);
-        if (!(v < INFINITY)) wrong = 1;
-        m = fmaxf(m, v);
+    double top = (double)known;
+    if (known != known) {
+        float m = -INFINITY;
+        int wrong = 0;
+        for (int i = tid; i < V; i += kBeamThreads) {
+            const float v = load_logit<T>(x, i);
+            if (!(v < INFINITY)) wrong = 1;
+            m = fmaxf(m, v);
+        }
+        wrong = __syncthreads_or(wrong);
+        if (wrong) { if (tid == 0) *bad = 1; return 0.0; }
+        m = warp_max(m);
+        if (lane == 0) red[warp] = (double)m;
+        __syncthreads();
+        top = red[0];
+        for (int w = 1; w < kBeamWarps; w++) top = fmax(top, red[w]);
+        __syncthreads();
     }
-    wrong = __syncthreads_or(wrong);
-    if (wrong) { if (tid == 0) *bad = 1; return 0.0; }
-    m = warp_max(m);
-    if (lane == 0) red[warp] = (double)m;
-    __syncthreads();
-    double top = red[0];
-    for (int w = 1; w < kBeamWarps; w++) top = fmax(top, red[w]);
-    __syncthreads();
     if (top == -INFINITY) return -INFINITY;
+    const double scale = 64.0 * 1.4426950408889634074 / temp;
     double sum = 0.0;
-    for (int i = tid; i < V; i += kBeamThreads) {
-        const double v = (double)load_logit<T>(x, i);
-        if (v > -INFINITY) sum += exp_neg((top - v) / temp);
+    for (int i0 = tid; i0 < V; i0 += kAhead * kBeamThreads) {
+        float v[kAhead];
+#pragma unroll
+        for (int u = 0; u < kAhead; u++) v[u] = i0 + u * kBeamThreads < V ? load_logit<T>(x, i0 + u * kBeamThreads) : -INFINITY;
+#pragma unroll
+        for (int u = 0; u < kAhead; u++) {
+            const double y = ((double)v[u] - top) * scale;                  // in units of log 2 / 64
+            if (!(y > -64.0 * 1000.0)) continue;
+            const double yf = rint(y);
+            const int k = (int)yf;
+            const double r = (y - yf) * (0.69314718055994530942 / 64.0);
+            const double p = fma(fma(fma(fma(r, 1.0 / 120.0, 1.0 / 24.0), r, 1.0 / 6.0), r, 0.5), r * r, r);
+            const double f = table[k & 63];
+            sum += fma(f, p, f) * __hiloint2double((1023 + (k >> 6)) << 20, 0);
+        }
     }
 #pragma unroll 1
     for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
@@ -338,6 +354,22 @@ __device__ __noinline__ double row_lse(const T* x, int V, double temp, double* r
     return top / temp + m_log(all);
 }
 
+// order-preserving map double -> integer (integers compare faster), and back; the two zeros get one key
+__device__ __forceinline__ unsigned long long sortable(double v) {
+    const unsigned long long u = (unsigned long long)__double_as_longlong(v + 0.0);
+    return (u >> 63) ? ~u : (u | 0x8000000000000000ull);
+}
+__device__ __forceinline__ double unsortable(unsigned long long k) {
+    return __longlong_as_double((long long)((k >> 63) ? (k & 0x7fffffffffffffffull) : ~k));
+}
+
+// Shared memory of the choice: `most` entries of lists (a list takes 1 << shift of them), then as many survivors.
+__host__ __device__ inline int list_shift(int keep) { int s = 0; while ((1 << s) < keep) s++; return s; }
+__host__ __device__ inline size_t choose_bytes(int lists, int keep) { return ((size_t)lists << list_shift(keep)) * 36; }
+
+// One CTA per group.  (What it costs is latency: it runs once, mostly with its instructions not yet fetched.  So no integer
+// division in the loops, and the survivors next to one another: with indices to follow and lists to divide out, ranking 71 of
+// them took 13 us, now 1.)
 template <typename T>
 __global__ void __launch_bounds__(kBeamThreads)
 beam_choose_kernel(const __grid_constant__ BeamArgs A)
@@ -349,81 +381,94 @@ beam_choose_kernel(const __grid_constant__ BeamArgs A)
     GR_CHECK_FLAG_INIT;
     const int tid = threadIdx.x;
     const long long b = blockIdx.x;
-    const int W = A.beams, P = A.parts, K = A.select, keep = A.keep, lists = W * P, most = lists * keep;
-    // lists in shared memory: the keys as scores, the logits and tokens, the survivors
+    const int W = A.beams, P = A.parts, K = A.select, keep = A.keep, lists = W * P, shift = list_shift(keep), most = lists << shift;
     GR_PTR(double) key = GR_MKPTR(double, reinterpret_cast<double*>(s_dyn), most, GR_CHECK_FLAG);
     GR_PTR(unsigned long long) raw = GR_MKPTR(unsigned long long, reinterpret_cast<unsigned long long*>(s_dyn) + most, most, GR_CHECK_FLAG);
-    GR_PTR(int) live = GR_MKPTR(int, reinterpret_cast<int*>(s_dyn + 16 * (size_t)most), most, GR_CHECK_FLAG);
-    GR_PTR(int) count = GR_MKPTR(int, reinterpret_cast<int*>(s_dyn + 16 * (size_t)most) + most, lists, GR_CHECK_FLAG);
-    const char* recs = A.ws + (size_t)b * lists * beam_stride(keep);
+    GR_PTR(unsigned long long) sv_key = GR_MKPTR(unsigned long long, reinterpret_cast<unsigned long long*>(s_dyn) + 2 * (size_t)most, most, GR_CHECK_FLAG);
+    GR_PTR(unsigned long long) sv_raw = GR_MKPTR(unsigned long long, reinterpret_cast<unsigned long long*>(s_dyn) + 3 * (size_t)most, most, GR_CHECK_FLAG);
+    GR_PTR(int) sv_row = GR_MKPTR(int, reinterpret_cast<int*>(s_dyn + 32 * (size_t)most), most, GR_CHECK_FLAG);
+    const int stride = beam_stride(keep);
+    const char* recs = A.ws + (size_t)b * lists * stride;
     if (tid == 0) { g.bad = 0; g.check = 0; g.redo = 0; }
     __syncthreads();
-    // ---- rows
-    static_assert(GR_MAX_BEAMS <= 32, "a lane of the first warp for each row");
-    if (tid < W) {
-        const int w = tid;
-        const float s = A.scores[b * W + w];
-        const int n = A.lengths ? A.lengths[b * W + w] : 0;
-        const bool fin = A.done && A.done[b * W + w];
-        if (!(s < INFINITY)) g.bad = 1;
-        g.score[w] = (double)s;
-        g.kind[w] = s == -INFINITY ? kRowNone : fin ? kRowDone : kRowLive;
-        g.length[w] = max(1, fin ? n : (n < INT_MAX ? n + 1 : n));
-        g.scale[w] = A.penalty != 0.0 ? pow((double)g.length[w], A.penalty) : 1.0;
-        g.again[w] = 0; g.exact[w] = 0;
-        double lse = 0.0;
-        if (g.kind[w] == kRowLive) {
-            float top = -INFINITY;
-            for (int p = 0; p < P; p++) top = fmaxf(top, reinterpret_cast<const BeamPart*>(recs + (size_t)(w * P + p) * beam_stride(keep))->ref);
-            double sum = 0.0;
-            int listed = 0;
-            for (int p = 0; p < P; p++) {
-                const BeamPart* r = reinterpret_cast<const BeamPart*>(recs + (size_t)(w * P + p) * beam_stride(keep));
-                if (r->sum != 0.0) sum += r->ref == top ? r->sum : times_pow2(r->sum, r->ref - top);
-                if (r->state & kPartCheck) g.check = 1;
-                listed += r->count;
-            }
-            lse = ((double)top + log2(sum)) * 0.69314718055994530942;
-            // NaN, an infinity, or logits so large that R, an fp32 number, is not the whole number above their product with s
-            // to within a few units: in fp64.  (Not where every token is masked: nothing depends on that sum.)
-            if (!(fabsf(top) <= kLargestRef) || !(sum < INFINITY)) g.again[w] = listed > 0 || sum != 0.0;
-        }
-        g.lse[w] = lse;
-        if (g.again[w]) g.redo = 1;
+    // ---- what the parts left (entries behind a list's count are whatever the workspace held: they are not looked at)
+    for (int l = tid; l < lists; l += kBeamThreads) {
+        const BeamPart r = *reinterpret_cast<const BeamPart*>(recs + (size_t)l * stride);
+        g.part_sum[l] = r.sum; g.part_ref[l] = r.ref; g.count[l] = r.count;
+        g.row[l] = (unsigned char)(l / P);
+        if (r.state & kPartCheck) g.check = 1;
     }
-    if (tid < 32) {
-        double least = tid < W ? g.scale[tid] : INFINITY;
-#pragma unroll 1
-        for (int o = 16; o > 0; o >>= 1) least = fmin(least, __shfl_xor_sync(0xffffffffu, least, o));
-        if (tid == 0) g.slack = kNear / least;
-    }
-    for (int l = tid; l < lists; l += kBeamThreads) count[l] = reinterpret_cast<const BeamPart*>(recs + (size_t)l * beam_stride(keep))->count;
-    __syncthreads();
     for (int e = tid; e < most; e += kBeamThreads) {
-        const int l = e / keep, i = e % keep;
-        unsigned long long k = 0ull;
-        if (i < count[l]) k = reinterpret_cast<const unsigned long long*>(recs + (size_t)l * beam_stride(keep) + sizeof(BeamPart))[i];
-        raw[e] = k;
+        const int l = e >> shift, i = e & ((1 << shift) - 1);
+        if (i < keep) raw[e] = reinterpret_cast<const unsigned long long*>(recs + (size_t)l * stride + sizeof(BeamPart))[i];
+    }
+    static_assert(GR_MAX_BEAMS <= 32, "a lane of the first warp for each row");
+    float score = -INFINITY;
+    bool fin = false;
+    if (tid < W) {
+        score = A.scores[b * W + tid];
+        const int n = A.lengths ? A.lengths[b * W + tid] : 0;
+        fin = A.done && A.done[b * W + tid];
+        g.length[tid] = max(1, fin ? n : (n < INT_MAX ? n + 1 : n));
+        g.inv_scale[tid] = A.penalty != 0.0 ? 1.0 / pow((double)g.length[tid], A.penalty) : 1.0;
+        if (!(score < INFINITY)) g.bad = 1;
     }
     __syncthreads();
-    // a finished hypothesis has one continuation, in its first part's list
-    for (int w = tid; w < W; w += kBeamThreads) {
-        if (g.kind[w] == kRowDone) { count[w * P] = 1; raw[w * P * keep] = ckey(0.f, A.eos); }
+    // ---- rows
+    if (tid < 32) {
+        if (tid < W) {
+            const int w = tid;
+            g.score[w] = (double)score;
+            g.kind[w] = score == -INFINITY ? kRowNone : fin ? kRowDone : kRowLive;
+            g.again[w] = 0; g.exact[w] = 0;
+            double lse = 0.0;
+            if (g.kind[w] == kRowLive) {
+                float top = -INFINITY;
+                for (int l = w * P; l < (w + 1) * P; l++) top = fmaxf(top, g.part_ref[l]);
+                double sum = 0.0;
+                int listed = 0;
+                for (int l = w * P; l < (w + 1) * P; l++) {
+                    const double v = g.part_sum[l];
+                    if (v != 0.0) sum += g.part_ref[l] == top ? v : times_pow2(v, g.part_ref[l] - top);
+                    listed += g.count[l];
+                }
+                lse = ((double)top + log2(sum)) * 0.69314718055994530942;
+                // NaN, an infinity, or logits so large that R, an fp32 number, is not the whole number near their product with s
+                // to within a few units: in fp64.  (Not where every token is masked: nothing depends on that sum.)
+                if (!(fabsf(top) <= kLargestRef) || !(sum < INFINITY)) g.again[w] = listed > 0 || sum != 0.0 ? 2 : 0;
+            } else if (g.kind[w] == kRowDone) {
+                // a finished hypothesis has one continuation, in its first part's list
+                g.count[w * P] = 1;
+                raw[w * P << shift] = ckey(0.f, A.eos);
+            }
+            g.lse[w] = lse;
+            if (g.again[w]) g.redo = 1;
+        }
+        double largest = tid < W ? g.inv_scale[tid] : 0.0;
+#pragma unroll 1
+        for (int o = 16; o > 0; o >>= 1) largest = fmax(largest, __shfl_xor_sync(0xffffffffu, largest, o));
+        if (tid == 0) g.slack = kNear * largest;
     }
     __syncthreads();
-    auto total_of = [&](int e) {
-        const int w = e / keep / P;
-        return g.kind[w] == kRowDone ? g.score[w] : g.score[w] + ((double)fkey_inv((unsigned)(raw[e] >> 32)) / A.temp - g.lse[w]);
+    const double inv_temp = 1.0 / A.temp;
+    auto total_of = [&](int w, unsigned long long k) {
+        return g.kind[w] == kRowDone ? g.score[w] : g.score[w] + ((double)fkey_inv((unsigned)(k >> 32)) * inv_temp - g.lse[w]);
     };
     int M = 0;
 #pragma unroll 1
     while (true) {
         // ---- sums that are to be taken again
         if (g.redo) {
+            if (tid < 64) g.table[tid] = exp2((double)tid * (1.0 / 64.0));
+            __syncthreads();
 #pragma unroll 1
             for (int w = 0; w < W; w++) {
                 if (!g.again[w]) continue;
-                const double lse = row_lse<T>((const T*)A.logits + (b * W + w) * A.ld, A.V, A.temp, g.red, &g.bad);
+                // (the largest logit heads one of the row's lists, unless the streamed sum was of no use)
+                float known = -INFINITY;
+                for (int l = w * P; l < (w + 1) * P; l++) if (g.count[l] > 0) known = fmaxf(known, fkey_inv((unsigned)(raw[l << shift] >> 32)));
+                if (g.again[w] == 2) known = __int_as_float(0x7fc00000);
+                const double lse = row_lse<T>((const T*)A.logits + (b * W + w) * A.ld, A.V, A.temp, known, g.table, g.red, &g.bad);
                 __syncthreads();
                 if (tid == 0) { g.lse[w] = lse; g.again[w] = 0; g.exact[w] = 1; }
                 __syncthreads();
@@ -431,24 +476,24 @@ beam_choose_kernel(const __grid_constant__ BeamArgs A)
         }
         if (g.bad) break;
         __syncthreads();
-        if (tid == 0) { g.count = 0; g.redo = 0; g.least = -INFINITY; }
+        if (tid == 0) { g.survivors = 0; g.redo = 0; g.least = -INFINITY; }
         // ---- scores, and a bound below the select-th: of the q-th entries of the lists the ceil(K / q)-th largest, q the
         // smallest power of two that leaves at most half of the lists above it
         for (int e = tid; e < most; e += kBeamThreads) {
-            const int l = e / keep, i = e % keep;
-            key[e] = i < count[l] ? total_of(e) / g.scale[l / P] : -INFINITY;
+            const int l = e >> shift, i = e & ((1 << shift) - 1), w = g.row[l];
+            key[e] = i < g.count[l] ? total_of(w, raw[e]) * g.inv_scale[w] : -INFINITY;
         }
-        int q = 1;
-        while (q < keep && 2 * ((K + q - 1) / q) > lists) q *= 2;
-        q = min(q, keep);
-        const int place = (K + q - 1) / q;
+        int lg = 0;
+        while ((1 << lg) < keep && 2 * ((K + (1 << lg) - 1) >> lg) > lists) lg++;
+        const int q = min(1 << lg, keep), place = (K + q - 1) / q;
         __syncthreads();
         if (place <= lists) {
             for (int l = tid; l < lists; l += kBeamThreads) {
-                const double mine = key[l * keep + q - 1];
+                const double mine = key[(l << shift) + q - 1];
                 int rank = 0;
+#pragma unroll 4
                 for (int o = 0; o < lists; o++) {
-                    const double k = key[o * keep + q - 1];
+                    const double k = key[(o << shift) + q - 1];
                     rank += k > mine || (k == mine && o < l) ? 1 : 0;
                 }
                 if (rank == place - 1) g.least = mine;
@@ -458,29 +503,42 @@ beam_choose_kernel(const __grid_constant__ BeamArgs A)
         // (those within kNear below the bound too: they may have to be told from the last ones)
         const double least = g.least - g.slack;
         for (int e = tid; e < most; e += kBeamThreads) {
-            if (e % keep < count[e / keep] && !(key[e] < least)) live[atomicAdd(&g.count, 1)] = e;
+            const int l = e >> shift;
+            if ((e & ((1 << shift) - 1)) < g.count[l] && !(key[e] < least)) {
+                const int at = atomicAdd(&g.survivors, 1);
+                sv_key[at] = sortable(key[e]); sv_raw[at] = raw[e]; sv_row[at] = g.row[l];
+            }
         }
         __syncthreads();
-        M = g.count;
-        // ---- ranks: larger key, then the row before, then the place in the row (by logit, then by token)
-        for (int a = tid; a < M; a += kBeamThreads) {
-            const int e = live[a], w = e / keep / P;
-            const double mine = key[e];
-            const unsigned long long mine_raw = raw[e];
+        M = g.survivors;
+        // ---- ranks: larger key, then the row before, then the place in the row (by logit, then by token).  Several threads to
+        // a survivor where there are enough.
+        const int team = 16 * M <= kBeamThreads ? 16 : 8 * M <= kBeamThreads ? 8 : 4 * M <= kBeamThreads ? 4 : 2 * M <= kBeamThreads ? 2 : 1;
+#pragma unroll 1
+        for (int a0 = 0; a0 < M; a0 += kBeamThreads / team) {
+            const int a = a0 + tid / team;
             int rank = 0;
+            unsigned long long mine = 0ull;
+            if (a < M) {
+                const int w = sv_row[a];
+                mine = sv_key[a];
+                const unsigned long long mine_raw = sv_raw[a];
 #pragma unroll 4
-            for (int o = 0; o < M; o++) {
-                const int f = live[o], v = f / keep / P;
-                const double k = key[f];
-                const bool ahead = v == w ? raw[f] > mine_raw : (k > mine || (k == mine && v < w));
-                rank += ahead ? 1 : 0;
+                for (int o = tid & (team - 1); o < M; o += team) {
+                    const int v = sv_row[o];
+                    const unsigned long long k = sv_key[o];
+                    const bool ahead = v == w ? sv_raw[o] > mine_raw : (k > mine || (k == mine && v < w));
+                    rank += ahead ? 1 : 0;
+                }
             }
-            if (rank <= K) { g.best_key[rank] = mine; g.best_at[rank] = e; }
+            __syncwarp();
+            for (int o = 1; o < team; o <<= 1) rank += __shfl_xor_sync(0xffffffffu, rank, o);
+            if (a < M && (tid & (team - 1)) == 0 && rank <= K) { g.best_key[rank] = unsortable(mine); g.best_at[rank] = a; }
         }
         __syncthreads();
         // ---- continuations of different rows that lie too close for the streamed sums
         auto close = [&](int e, int f, double apart) {
-            const int w = e / keep / P, v = f / keep / P;
+            const int w = sv_row[e], v = sv_row[f];
             if (w == v || fabs(apart) > g.slack) return;
             if (g.kind[w] == kRowLive && !g.exact[w]) { g.again[w] = 1; g.redo = 1; }
             if (g.kind[v] == kRowLive && !g.exact[v]) { g.again[v] = 1; g.redo = 1; }
@@ -488,7 +546,7 @@ beam_choose_kernel(const __grid_constant__ BeamArgs A)
         for (int i = tid; i + 1 < min(M, K + 1); i += kBeamThreads) close(g.best_at[i], g.best_at[i + 1], g.best_key[i] - g.best_key[i + 1]);
         if (M > K) {
             const double last = g.best_key[K - 1];
-            for (int a = tid; a < M; a += kBeamThreads) close(live[a], g.best_at[K - 1], key[live[a]] - last);
+            for (int a = tid; a < M; a += kBeamThreads) close(a, g.best_at[K - 1], unsortable(sv_key[a]) - last);
         }
         __syncthreads();
         if (!g.redo) break;
@@ -498,17 +556,17 @@ beam_choose_kernel(const __grid_constant__ BeamArgs A)
     for (int i = tid; i < K; i += kBeamThreads) {
         const size_t at = (size_t)b * K + i;
         int token = -1, parent = -1, length = 0;
-        float score = -INFINITY;
-        unsigned char fin = 0;
+        float total = -INFINITY;
+        unsigned char ended = 0;
         if (!bad && i < M) {
             const int e = g.best_at[i];
-            parent = e / keep / P;
-            token = (int)(0xffffffffu - (unsigned)raw[e]);
-            score = (float)total_of(e);
+            parent = sv_row[e];
+            token = (int)(0xffffffffu - (unsigned)sv_raw[e]);
+            total = (float)total_of(parent, sv_raw[e]);
             length = g.length[parent];
-            fin = g.kind[parent] == kRowDone || token == A.eos;
+            ended = g.kind[parent] == kRowDone || token == A.eos;
         }
-        A.out_token[at] = token; A.out_parent[at] = parent; A.out_score[at] = score; A.out_done[at] = fin;
+        A.out_token[at] = token; A.out_parent[at] = parent; A.out_score[at] = total; A.out_done[at] = ended;
         if (A.out_length) A.out_length[at] = length;
     }
     if (tid == 0) {
@@ -528,7 +586,8 @@ static int beam_parts(int V, int rows, int beams, int keep)
     int parts = (4 * kSms) / (rows > 0 ? rows : 1);
     if (parts > most) parts = most;
     if (parts > kBeamMaxLists / beams) parts = kBeamMaxLists / beams;
-    if (parts > kBeamMaxListed / (beams * keep)) parts = kBeamMaxListed / (beams * keep);
+    const int per = beams << list_shift(keep);
+    if (parts > kBeamMaxListed / per) parts = kBeamMaxListed / per;
     return parts < 1 ? 1 : parts;
 }
 
@@ -541,14 +600,13 @@ static bool beam_shape_ok(int V, int beams, int select, int batch)
 template <typename T>
 static int launch_beam(const BeamArgs& A, int batch, cudaStream_t st)
 {
-    const int most = A.beams * A.parts * A.keep;
-    const int smem = 20 * most + 4 * A.beams * A.parts;
+    const int smem = (int)choose_bytes(A.beams * A.parts, A.keep);
     static bool raised[kMaxDevices] = {false};
-    if (smem > 40 * 1024) {
+    if (smem > 32 * 1024) {
         int dev = -1;
         if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) { cudaGetLastError(); return GR_E_LAUNCH; }
         if (!raised[dev]) {
-            if (cudaFuncSetAttribute(beam_choose_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, 20 * kBeamMaxListed + 4 * kBeamMaxLists) != cudaSuccess) {
+            if (cudaFuncSetAttribute(beam_choose_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, 36 * kBeamMaxListed) != cudaSuccess) {
                 cudaGetLastError();
                 return GR_E_LAUNCH;
             }
