@@ -12,9 +12,11 @@
 // +infinity make the sum NaN, as does a maximum whose product with s overflows: such rows' sums are taken again in fp64 by the
 // second kernel, which tells the two apart.
 //
-// The order.  Within a row it is that of the logits.  Between rows scores are compared in fp64; the streamed sums are good to
-// about 1e-8 (kNear is far above that), and where two continuations lie closer than kNear the rows' sums are taken again in
-// fp64, so that the order is that of the 64-bit scores.
+// The order.  Within a row it is that of the logits.  Between rows scores are compared in fp64.  Two rows' streamed sums are off
+// from one another by up to 1.2e-7 + 7e-7 p in the logarithm, p the larger probability of a first token of the two (measured on 100 kinds of
+// rows: ex2 and the products round each element by a part in 10^7 and more, which a sum of many averages out); where two
+// continuations lie closer than kNear + kNearPeak p the rows' sums are taken again in fp64, so that the order is that of the
+// 64-bit scores.
 #include <limits.h>
 #include <math.h>
 #include "gr_host.h"
@@ -28,7 +30,7 @@ constexpr int kBeamMaxParts = 16;
 constexpr int kBeamMaxLists = 256;             // rows of a group times parts
 constexpr int kBeamMaxListed = 4096;           // entries of a group's lists
 static_assert(GR_MAX_BEAMS * GR_MAX_SELECT <= kBeamMaxListed && GR_MAX_SELECT <= kMaxSupport, "lists");
-constexpr double kNear = 6e-7;
+constexpr double kNear = 2e-7, kNearPeak = 1e-6;
 constexpr float kLargestRef = 16777216.f;
 constexpr float kRise = 1.f;
 
@@ -292,7 +294,8 @@ struct BeamGroup {
     unsigned char again[GR_MAX_BEAMS];         // the row's sum is to be taken again (2: it was of no use)
     unsigned char exact[GR_MAX_BEAMS];         // ... and has been
     int bad, check, survivors, redo;
-    double least, slack;                       // slack: kNear as a difference of keys
+    float peak[GR_MAX_BEAMS];                  // probability of the row's first token
+    double least, slack;                       // slack: the largest distance of keys at which sums are taken again
     double best_key[GR_MAX_SELECT + 1];
     int best_at[GR_MAX_SELECT + 1];
 };
@@ -305,7 +308,7 @@ constexpr int kRowNone = 0, kRowDone = 1, kRowLive = 2;
 template <typename T>
 __device__ __noinline__ double row_lse(const T* x, int V, double temp, float known, const double* table, double* red, int* bad)
 {
-    constexpr int kAhead = 8;
+    constexpr int kAhead = 16;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     double top = (double)known;
     if (known != known) {
@@ -326,24 +329,38 @@ __device__ __noinline__ double row_lse(const T* x, int V, double temp, float kno
         __syncthreads();
     }
     if (top == -INFINITY) return -INFINITY;
-    const double scale = 64.0 * 1.4426950408889634074 / temp;
-    double sum = 0.0;
+    // (kAhead elements at a time, without a branch between them: an element is a chain of twelve dependent operations.  Whole
+    // numbers by the sum with 1.5 2^52, whose low word they are: conversions have a sixteenth of the multiplications' rate.)
+    const double scale = 64.0 * 1.4426950408889634074 / temp, magic = 6755399441055744.0, unit = 0.69314718055994530942 / 64.0;
+    const double c1 = unit, c2 = unit * c1 / 2.0, c3 = unit * c2 / 3.0, c4 = unit * c3 / 4.0, c5 = unit * c4 / 5.0;
+    const float lowest = (float)fmax(top - 690.0 * temp, -3.4028234663852886e38);   // exp(-690): nothing beside the largest
+    double sum0 = 0.0, sum1 = 0.0;
+    float next[kAhead];
+#pragma unroll
+    for (int u = 0; u < kAhead; u++) next[u] = tid + u * kBeamThreads < V ? load_logit<T>(x, tid + u * kBeamThreads) : -INFINITY;
+#pragma unroll 1
     for (int i0 = tid; i0 < V; i0 += kAhead * kBeamThreads) {
         float v[kAhead];
 #pragma unroll
-        for (int u = 0; u < kAhead; u++) v[u] = i0 + u * kBeamThreads < V ? load_logit<T>(x, i0 + u * kBeamThreads) : -INFINITY;
+        for (int u = 0; u < kAhead; u++) {
+            const int i = i0 + (kAhead + u) * kBeamThreads;
+            v[u] = next[u];
+            next[u] = i < V ? load_logit<T>(x, i) : -INFINITY;
+        }
 #pragma unroll
         for (int u = 0; u < kAhead; u++) {
-            const double y = ((double)v[u] - top) * scale;                  // in units of log 2 / 64
-            if (!(y > -64.0 * 1000.0)) continue;
-            const double yf = rint(y);
-            const int k = (int)yf;
-            const double r = (y - yf) * (0.69314718055994530942 / 64.0);
-            const double p = fma(fma(fma(fma(r, 1.0 / 120.0, 1.0 / 24.0), r, 1.0 / 6.0), r, 0.5), r * r, r);
-            const double f = table[k & 63];
-            sum += fma(f, p, f) * __hiloint2double((1023 + (k >> 6)) << 20, 0);
+            const double y = ((double)fmaxf(v[u], lowest) - top) * scale;   // in units of log 2 / 64
+            const double whole = fmax(y, -64000.0) + magic;
+            const int k = __double2loint(whole);
+            const double z = y - (whole - magic);
+            const double p = z * fma(z, fma(z, fma(z, fma(z, c5, c4), c3), c2), c1);
+            const double t = table[k & 63];
+            const double f = __hiloint2double(__double2hiint(t) + ((k >> 6) << 20), __double2loint(t));
+            const double e = k > -64000 ? fma(f, p, f) : 0.0;
+            if (u & 1) sum1 += e; else sum0 += e;
         }
     }
+    double sum = sum0 + sum1;
 #pragma unroll 1
     for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
     if (lane == 0) red[warp] = sum;
@@ -415,12 +432,13 @@ beam_choose_kernel(const __grid_constant__ BeamArgs A)
     }
     __syncthreads();
     // ---- rows
+    const double inv_temp = 1.0 / A.temp;
     if (tid < 32) {
         if (tid < W) {
             const int w = tid;
             g.score[w] = (double)score;
             g.kind[w] = score == -INFINITY ? kRowNone : fin ? kRowDone : kRowLive;
-            g.again[w] = 0; g.exact[w] = 0;
+            g.again[w] = 0; g.exact[w] = 0; g.peak[w] = 0.f;
             double lse = 0.0;
             if (g.kind[w] == kRowLive) {
                 float top = -INFINITY;
@@ -435,6 +453,9 @@ beam_choose_kernel(const __grid_constant__ BeamArgs A)
                 lse = ((double)top + log2(sum)) * 0.69314718055994530942;
                 // NaN, an infinity, or logits so large that R, an fp32 number, is not the whole number near their product with s
                 // to within a few units: in fp64.  (Not where every token is masked: nothing depends on that sum.)
+                float first = -INFINITY;
+                for (int l = w * P; l < (w + 1) * P; l++) if (g.count[l] > 0) first = fmaxf(first, fkey_inv((unsigned)(raw[l << shift] >> 32)));
+                g.peak[w] = fminf(1.f, __expf((float)((double)first * inv_temp - lse)));
                 if (!(fabsf(top) <= kLargestRef) || !(sum < INFINITY)) g.again[w] = listed > 0 || sum != 0.0 ? 2 : 0;
             } else if (g.kind[w] == kRowDone) {
                 // a finished hypothesis has one continuation, in its first part's list
@@ -444,13 +465,12 @@ beam_choose_kernel(const __grid_constant__ BeamArgs A)
             g.lse[w] = lse;
             if (g.again[w]) g.redo = 1;
         }
-        double largest = tid < W ? g.inv_scale[tid] : 0.0;
+        double largest = tid < W ? g.inv_scale[tid] * (kNear + kNearPeak * (double)g.peak[tid]) : 0.0;
 #pragma unroll 1
         for (int o = 16; o > 0; o >>= 1) largest = fmax(largest, __shfl_xor_sync(0xffffffffu, largest, o));
-        if (tid == 0) g.slack = kNear * largest;
+        if (tid == 0) g.slack = largest;
     }
     __syncthreads();
-    const double inv_temp = 1.0 / A.temp;
     auto total_of = [&](int w, unsigned long long k) {
         return g.kind[w] == kRowDone ? g.score[w] : g.score[w] + ((double)fkey_inv((unsigned)(k >> 32)) * inv_temp - g.lse[w]);
     };
@@ -539,7 +559,9 @@ beam_choose_kernel(const __grid_constant__ BeamArgs A)
         // ---- continuations of different rows that lie too close for the streamed sums
         auto close = [&](int e, int f, double apart) {
             const int w = sv_row[e], v = sv_row[f];
-            if (w == v || fabs(apart) > g.slack) return;
+            if (w == v) return;
+            const double near_w = g.inv_scale[w] * (kNear + kNearPeak * (double)g.peak[w]), near_v = g.inv_scale[v] * (kNear + kNearPeak * (double)g.peak[v]);
+            if (fabs(apart) > fmax(near_w, near_v)) return;
             if (g.kind[w] == kRowLive && !g.exact[w]) { g.again[w] = 1; g.redo = 1; }
             if (g.kind[v] == kRowLive && !g.exact[v]) { g.again[v] = 1; g.redo = 1; }
         };
