@@ -116,6 +116,33 @@ beam_stream_kernel(const __grid_constant__ BeamArgs A)
     double acc = 0.0;
     const unsigned long long hi2 = f_pack(A.s_hi, A.s_hi), lo2 = f_pack(A.s_lo, A.s_lo);
     const int rounds = first < nch ? (nch - first + stride - 1) / stride : 0;
+    // the reference follows the maximum of the warp, where that is kRise above it (a logit above `limit`); what has been added up
+    // moves there by an exact factor
+    float limit = -INFINITY;
+    auto raise = [&](float m) {
+        const float to = ceilf(warp_max(m) * A.s_hi);
+        if (acc != 0.0) acc = times_pow2(acc, ref - to);
+        ref = to;
+        limit = (to + kRise) / A.s_hi;
+    };
+    // the elements before the first and behind the last vector of the row, by the warps that the first and last chunk fall to
+    float e0 = -INFINITY, e1 = -INFINITY;
+    auto push_edges = [&](float tau) {
+        if (e0 >= tau) push_vector(sh, VT::alone(e0), lane);
+        if (e1 >= tau) push_vector(sh, VT::alone(e1), vec_end + lane);
+    };
+    {
+        const bool has_first = first + warp == 0 && head > 0, has_last = (nch - 1) % stride == first + warp && tail > 0;
+        if (has_first && lane < head) e0 = load_logit<T>(x, lane);
+        if (has_last && lane < tail) e1 = load_logit<T>(x, vec_end + lane);
+        if (has_first || has_last) {
+            g0 = fmaxf(e0, e1);
+            raise(g0);
+            const float down = ref == -INFINITY ? 0.f : -ref;
+            acc = (double)ex2(fmaf(e0, A.s_lo, fmaf(e0, A.s_hi, down))) + (double)ex2(fmaf(e1, A.s_lo, fmaf(e1, A.s_hi, down)));
+        }
+        if (!use_tau) push_edges(-3.402823466e38f);
+    }
     int r = 0, upto = use_tau ? 1 : rounds;
 #pragma unroll 1
     while (true) {
@@ -142,24 +169,13 @@ beam_stream_kernel(const __grid_constant__ BeamArgs A)
 #endif
                         if (ok) v[u] = ldg_stream(x + i0);
                     }
-                    // (the elements before the first and behind the last vector)
-                    float e0 = -INFINITY, e1 = -INFINITY;
-                    if (nb == 0) {
-                        if (c == 0 && lane < head) e0 = load_logit<T>(x, lane);
-                        if (c == nch - 1 && lane < tail) e1 = load_logit<T>(x, vec_end + lane);
-                    }
                     float each[U];
-                    float most = fmaxf(e0, e1);
+                    each[0] = VT::largest(v[0]);
+                    float most = each[0];
 #pragma unroll
-                    for (int u = 0; u < U; u++) { each[u] = VT::largest(v[u]); most = fmaxf(most, each[u]); }
+                    for (int u = 1; u < U; u++) { each[u] = VT::largest(v[u]); most = fmaxf(most, each[u]); }
                     g0 = fmaxf(g0, most);
-                    // the reference follows the maximum of the warp, where that is kRise above it; what has been added up moves
-                    // there by an exact factor
-                    if (__any_sync(0xffffffffu, most * A.s_hi > ref + kRise)) {
-                        const float to = ceilf(warp_max(most) * A.s_hi);
-                        if (acc != 0.0) acc = times_pow2(acc, ref - to);
-                        ref = to;
-                    }
+                    if (__any_sync(0xffffffffu, most > limit)) raise(most);
                     // (an element that is -infinity gives 0 whatever the reference, as long as that is finite)
                     const float down = ref == -INFINITY ? 0.f : -ref;
                     const unsigned long long down2 = f_pack(down, down);
@@ -173,33 +189,24 @@ beam_stream_kernel(const __grid_constant__ BeamArgs A)
                             sum2 = add2(sum2, f_pack(ex2(f_lo(y)), ex2(f_hi(y))));
                         }
                     }
-                    float sum = f_lo(sum2) + f_hi(sum2);
-                    if (nb == 0 && (c == 0 || c == nch - 1)) {
-                        sum += ex2(fmaf(e0, A.s_lo, fmaf(e0, A.s_hi, down))) + ex2(fmaf(e1, A.s_lo, fmaf(e1, A.s_hi, down)));
-                        if (e0 >= tau) push_vector(sh, VT::alone(e0), lane);
-                        if (e1 >= tau) push_vector(sh, VT::alone(e1), vec_end + lane);
-                    }
-                    acc += (double)sum;
+                    acc += (double)(f_lo(sum2) + f_hi(sum2));
+                    if (most >= tau) {
 #pragma unroll
-                    for (int u = 0; u < U; u++) if (each[u] >= tau) push_vector(sh, v[u], base + u * 32 * N);
+                        for (int u = 0; u < U; u++) if (each[u] >= tau) push_vector(sh, v[u], base + u * 32 * N);
+                    }
                 };
                 if (whole) batch(std::true_type());
                 else if (cvalid) batch(std::false_type());
                 if (sample) {
                     // the first batch had no threshold: it gives one, and is tested now
                     refine_tau(sh, g0, K);
+                    const float t1 = *((volatile float*)&sh.tau);
+                    push_edges(t1);
                     if (cvalid) {
-                        const float t1 = *((volatile float*)&sh.tau);
 #pragma unroll
                         for (int u = 0; u < U; u++) {
                             if ((whole || base + u * 32 * N + N <= vec_end) && VT::largest(v[u]) >= t1) push_vector(sh, v[u], base + u * 32 * N);
                         }
-                        auto late = [&](int i) {
-                            const float w = load_logit<T>(x, i);
-                            if (w >= t1) push_vector(sh, VT::alone(w), i);
-                        };
-                        if (c == 0 && lane < head) late(lane);
-                        if (c == nch - 1 && lane < tail) late(vec_end + lane);
                     }
                 }
             }
