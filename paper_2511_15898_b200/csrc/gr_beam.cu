@@ -143,7 +143,7 @@ beam_stream_kernel(const __grid_constant__ BeamArgs A)
         }
         if (!use_tau) push_edges(-3.402823466e38f);
     }
-    int r = 0, upto = use_tau ? 1 : rounds;
+    int r = 0, upto = use_tau ? 4 : rounds;                 // rounds up to the next threshold
 #pragma unroll 1
     while (true) {
 #pragma unroll 1
@@ -212,11 +212,13 @@ beam_stream_kernel(const __grid_constant__ BeamArgs A)
             }
         }
         if (r >= rounds) break;
-        // a better threshold whenever the part read has grown fourfold, and a shorter list where it would not hold what is to come
+        upto *= 4;
+        // a better threshold whenever the part read has grown fourfold, unless less is to come than has been read; and a shorter
+        // list where it would not hold what is to come
+        if (rounds < 2 * r && 5 * (K + K * K / kBeamThreads) * (rounds - r) < 2 * BeamSm::kList * r) { upto = rounds; continue; }
         const int listed = refine_tau(sh, g0, K);
         const int more = (K + K * K / kBeamThreads) * min(3 * r, rounds - r);
         if (listed <= BeamSm::kList && 5 * more > 4 * (BeamSm::kList - listed) * r) keep_listed<T>(sh, listed);
-        upto *= 4;
     }
     // ---- the part's sum
     {
