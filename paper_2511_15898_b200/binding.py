@@ -16,6 +16,12 @@ from typing import Optional, Tuple
 
 import torch
 
+try:
+    from ._tensors import alike as _alike      # (built beside the library; without it lists are looked at one by one)
+except ImportError:
+    def _alike(tensors):
+        return None
+
 GR_F32, GR_BF16 = 0, 1
 GR_OK, GR_NOT_CONVERGED, GR_SUPPORT_TOO_LARGE, GR_BAD_LOGITS, GR_DRAFT_OUT_OF_SUPPORT, GR_STALE_PARAMS = range(6)
 GR_MAX_SUPPORT, GR_MAX_DRAFTS = 128, 32
@@ -181,12 +187,13 @@ def gr_beam_select(logits: int, dtype: int, V: int, ld: int, beams: int, batch: 
 
 
 def gr_reorder_states(src, dst, layout: Optional[StateLayout], parents: int, lengths: int, stream: int) -> int:
-    """src, dst: sequences of device addresses."""
+    """src, dst: sequences of device addresses (or bytes that hold them, 64 bits each)."""
     if len(src) != len(dst):
         raise GrError("src and dst: one address each for every state")
-    a, b = array.array("Q", src), array.array("Q", dst)
-    return load_library().gr_reorder_states(a.buffer_info()[0], b.buffer_info()[0], len(a),
-                                            C.byref(layout) if layout is not None else None, parents, lengths, stream)
+    a = src if isinstance(src, bytes) else array.array("Q", src).tobytes()
+    b = dst if isinstance(dst, bytes) else array.array("Q", dst).tobytes()
+    return load_library().gr_reorder_states(a, b, len(a) // 8, C.byref(layout) if layout is not None else None, parents,
+                                            lengths, stream)
 
 
 def gr_block_workspace_bytes(rows: int, num_blocks: int) -> int:
@@ -203,10 +210,10 @@ def gr_block_plan(table: int, rows: int, width: int, beams: int, block_size: int
 
 def gr_copy_blocks(caches, num_blocks: int, block_stride: int, block_bytes: int, copy_src: int, copy_dst: int,
                    pairs: int, stream: int) -> int:
-    """caches: a sequence of device addresses."""
-    a = array.array("Q", caches)
-    return load_library().gr_copy_blocks(a.buffer_info()[0], len(a), num_blocks, block_stride, block_bytes, copy_src,
-                                         copy_dst, pairs, stream)
+    """caches: a sequence of device addresses (or bytes that hold them, 64 bits each)."""
+    a = caches if isinstance(caches, bytes) else array.array("Q", caches).tobytes()
+    return load_library().gr_copy_blocks(a, len(a) // 8, num_blocks, block_stride, block_bytes, copy_src, copy_dst, pairs,
+                                         stream)
 
 
 # ---------------------------------------------------------------- torch tensors
@@ -580,33 +587,48 @@ def reorder_states(states, parents: torch.Tensor, lengths: Optional[torch.Tensor
     dev = parents.device
     if (lengths is None) != (token_dim is None):
         raise GrError("lengths and token_dim go together")
-    W = states[0].shape[1] if isinstance(states[0], torch.Tensor) and states[0].dim() >= 2 else 0
+    if not isinstance(states[0], torch.Tensor) or states[0].dim() < 2:
+        raise GrError("states must be CUDA tensors [B, beams, ...] on the device of parents")
+    W = states[0].shape[1]
     a_lengths = _need(lengths, "lengths", torch.int32, (B, W), dev, optional=True)
-    # runs of tensors of one layout: (layout, states, outs, bytes that a state and an out span)
+    # runs of tensors of one layout: (layout, addresses of states and outs, bytes that a state and an out span)
     runs = []
-    shape = step = kind = shape_y = step_y = None
-    for x, y in zip(states, to):
-        if not isinstance(x, torch.Tensor) or x.device != dev:
+
+    def layout_of(x, y):
+        shape, step, step_y = x.shape, x.stride(), y.stride()
+        if x.device != dev or not x.is_cuda:
             raise GrError("states must be CUDA tensors [B, beams, ...] on the device of parents")
-        if x.shape != shape or x.stride() != step or x.dtype is not kind or (y is not x and y.stride() != step_y):
-            shape, step, kind = x.shape, x.stride(), x.dtype
-            if x.dim() < 2 or shape[0] != B or shape[1] != W:
-                raise GrError("states must be [B, beams, ...], of one number of beams")
-            if token_dim is not None and not 2 <= token_dim < x.dim():
-                raise GrError("token_dim must be a dimension behind the beams")
-            parts, part_step, part, token = _state_layout(x, token_dim)
-            part_step_y = part_step if y is x else _state_layout(y, token_dim)[1]
-            step_y = y.stride()
-            shape_y = shape if out is None else (B, chosen) + tuple(shape[2:])
-            e = x.element_size()
-            layout = StateLayout(B, W, chosen, parts, step[0] * e if B > 1 else 0, step[1] * e if W > 1 else 0, part_step,
-                                 step_y[0] * e if B > 1 else 0,
-                                 step_y[1] * e if (W if out is None else chosen) > 1 else 0, part_step_y, part, token)
-            runs.append((layout, [], [], _span(x) if out is not None else 0, _span(y) if out is not None else 0))
-        if y is not x and (not isinstance(y, torch.Tensor) or y.shape != shape_y or y.dtype is not kind or y.device != dev):
+        if x.dim() < 2 or shape[0] != B or shape[1] != W:
+            raise GrError("states must be [B, beams, ...], of one number of beams")
+        if token_dim is not None and not 2 <= token_dim < x.dim():
+            raise GrError("token_dim must be a dimension behind the beams")
+        if y is not x and (y.shape != (B, chosen) + tuple(shape[2:]) or y.dtype is not x.dtype or y.device != dev):
             raise GrError("out must hold tensors [B, chosen, ...] like the states")
-        runs[-1][1].append(x.data_ptr())
-        if out is not None:
+        parts, part_step, part, token = _state_layout(x, token_dim)
+        part_step_y = part_step if y is x else _state_layout(y, token_dim)[1]
+        e = x.element_size()
+        return StateLayout(B, W, chosen, parts, step[0] * e if B > 1 else 0, step[1] * e if W > 1 else 0, part_step,
+                           step_y[0] * e if B > 1 else 0, step_y[1] * e if (W if out is None else chosen) > 1 else 0,
+                           part_step_y, part, token)
+
+    at = _alike(states)
+    at_y = at if out is None or at is None else _alike(to)
+    if at_y is not None:
+        layout = layout_of(states[0], to[0])
+        if out is None:
+            runs.append((layout, at, at, 0, 0))
+        else:
+            runs.append((layout, array.array("Q", at), array.array("Q", at_y), _span(states[0]), _span(to[0])))
+    else:
+        last = None
+        for x, y in zip(states, to):
+            if not isinstance(x, torch.Tensor) or not isinstance(y, torch.Tensor):
+                raise GrError("states must be CUDA tensors [B, beams, ...] on the device of parents")
+            kind = (x.shape, x.stride(), x.dtype, x.device, y.shape, y.stride(), y.dtype, y.device)
+            if kind != last:
+                last = kind
+                runs.append((layout_of(x, y), [], [], _span(x), _span(y)))
+            runs[-1][1].append(x.data_ptr())
             runs[-1][2].append(y.data_ptr())
     if out is not None:
         if (min(min(r[2]) for r in runs) < max(max(r[1]) + r[3] for r in runs)
@@ -619,7 +641,7 @@ def reorder_states(states, parents: torch.Tensor, lengths: Optional[torch.Tensor
             raise GrError("the same tensor twice")
     for layout, at, at_y, _, _ in runs:
         if chosen > 0 and layout.part_bytes > 0:
-            _call(dev, "gr_reorder_states", gr_reorder_states, at, at if out is None else at_y, layout, a_parents, a_lengths)
+            _call(dev, "gr_reorder_states", gr_reorder_states, at, at_y, layout, a_parents, a_lengths)
     return to
 
 
@@ -700,25 +722,34 @@ def copy_blocks(caches, copy_src: torch.Tensor, copy_dst: torch.Tensor) -> None:
     a_dst = _need(copy_dst, "copy_dst", torch.int32, copy_src.shape, dev)
     # runs of caches of one layout: (blocks, bytes from one to the next, bytes, addresses)
     runs = []
-    shape = step = kind = None
-    for x in caches:
-        if not isinstance(x, torch.Tensor) or x.device != dev:
+
+    def layout_of(x):
+        if x.device != dev or x.dim() < 1:
             raise GrError("caches must be CUDA tensors [num_blocks, ...] on the device of copy_src")
-        if x.shape != shape or x.stride() != step or x.dtype is not kind:
-            shape, step, kind = x.shape, x.stride(), x.dtype
-            if x.dim() < 1:
-                raise GrError("caches must be [num_blocks, ...]")
-            per = x.numel() // shape[0] if shape[0] else 0
-            if per and (not x[0].is_contiguous() or (shape[0] > 1 and step[0] < per)):
-                raise GrError("caches: a block's elements must lie next to one another, and the blocks apart")
-            e = x.element_size()
-            runs.append((shape[0], (step[0] if shape[0] > 1 else per) * e, per * e, []))
-        if per:
+        shape, step = x.shape, x.stride()
+        per = x.numel() // shape[0] if shape[0] else 0
+        if per and (not x[0].is_contiguous() or (shape[0] > 1 and step[0] < per)):
+            raise GrError("caches: a block's elements must lie next to one another, and the blocks apart")
+        e = x.element_size()
+        return shape[0], (step[0] if shape[0] > 1 else per) * e, per * e
+
+    at = _alike(caches)
+    if at is not None:
+        runs.append(layout_of(caches[0]) + (at,))
+    else:
+        last = None
+        for x in caches:
+            if not isinstance(x, torch.Tensor):
+                raise GrError("caches must be CUDA tensors [num_blocks, ...] on the device of copy_src")
+            kind = (x.shape, x.stride(), x.dtype, x.device)
+            if kind != last:
+                last = kind
+                runs.append(layout_of(x) + ([],))
             runs[-1][3].append(x.data_ptr())
     if len(runs) > 1:
-        first = [p for r in runs for p in r[3]]
+        first = [p for r in runs if r[2] for p in r[3]]
         if len(set(first)) < len(first):
             raise GrError("the same cache twice")
     for blocks, stride, size, at in runs:
-        if at:
+        if size > 0:
             _call(dev, "gr_copy_blocks", gr_copy_blocks, at, blocks, stride, size, a_src, a_dst, copy_src.shape[0])

@@ -18,6 +18,26 @@ HEADERS = [os.path.join(CSRC, "gr_common.cuh"), os.path.join(CSRC, "gr_prep.cuh"
            os.path.join(ROOT, "include", "gr.h")]
 
 
+# the binding's view of lists of tensors: a Python module on torch's headers
+TENSORS_SOURCE = os.path.join(CSRC, "gr_tensors.cpp")
+TENSORS = os.path.join(HERE, "_tensors.so")
+
+
+def _build_tensors(force: bool = False):
+    """The started compilation of the module, or None where it is up to date."""
+    import sysconfig
+
+    import torch
+    from torch.utils.cpp_extension import include_paths
+    if not force and os.path.exists(TENSORS) and os.path.getmtime(TENSORS) > os.path.getmtime(TENSORS_SOURCE):
+        return None
+    lib = os.path.join(os.path.dirname(torch.__file__), "lib")
+    cmd = (["g++", "-O2", "-std=c++17", "-shared", "-fPIC", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}"]
+           + [a for p in include_paths() + [sysconfig.get_paths()["include"]] for a in ("-isystem", p)]
+           + [TENSORS_SOURCE, "-L" + lib, "-ltorch_python", "-ltorch_cpu", "-lc10", "-Wl,-rpath," + lib, "-o", TENSORS])
+    return subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+
+
 def _nvcc() -> str:
     for cand in (os.environ.get("NVCC"), "/usr/local/cuda/bin/nvcc", "nvcc"):
         if cand and (os.path.sep not in cand or os.path.exists(cand)):
@@ -28,6 +48,8 @@ def _nvcc() -> str:
 def needs_build(check: bool = False) -> bool:
     lib = LIB_CHECK if check else LIB
     if not os.path.exists(lib):
+        return True
+    if not check and (not os.path.exists(TENSORS) or os.path.getmtime(TENSORS) < os.path.getmtime(TENSORS_SOURCE)):
         return True
     t = os.path.getmtime(lib)
     deps = [os.path.join(CSRC, s) for s in SOURCES] + HEADERS
@@ -62,6 +84,10 @@ def build_library(force: bool = False, verbose: bool = False, check: bool = Fals
         if not fresh:
             jobs.append((s, subprocess.Popen([_nvcc()] + flags + ["-c", src, "-o", obj], stdout=subprocess.PIPE,
                                              stderr=subprocess.STDOUT, text=True)))
+    if not check:
+        proc = _build_tensors(force)
+        if proc is not None:
+            jobs.append((os.path.basename(TENSORS_SOURCE), proc))
     failed = []
     for s, proc in jobs:
         out, _ = proc.communicate()

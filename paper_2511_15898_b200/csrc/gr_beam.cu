@@ -57,7 +57,7 @@ struct BeamArgs {
 
 __host__ __device__ inline int beam_stride(int keep) { return (int)sizeof(BeamPart) + 8 * ((keep + 1) & ~1); }
 
-using BeamSm = ScanShared<kBeamThreads, 1280, 2048, 1>;
+using BeamSm = ScanShared<kBeamThreads, 1024, 2048, 1>;
 
 // v 2^k, k a whole number at or below 0 (what falls below 2^-1000 of v is dropped); a NaN stays one
 __device__ __forceinline__ double times_pow2(double v, float k)
