@@ -14,8 +14,7 @@ struct ReorderArgs {
     const char* src[kStatesPerLaunch];
     char* dst[kStatesPerLaunch];
     gr_state_layout at;
-    int count, in_place;
-    long long chunks;                      // column chunks of a piece
+    int in_place;
 };
 
 // the first n bytes of a vector
@@ -40,54 +39,61 @@ __device__ __forceinline__ void store_bytes(char* to, unsigned v, int n)
 // column, all of them before it writes the first.  So a group reorders in place whatever the mapping (no second buffer, no
 // order among the copies), a parent of several states is read from memory once (the other reads meet it in the first-level
 // cache), and states that stay are not touched.
+// A CTA takes C * kCopyThreads neighbouring columns of one piece; what is copied from where is worked out once for it, in
+// shared memory (by every thread for itself, the chain of look-ups for 16 states cost as much as the copies).
 template <int W, typename Vec, int C>
 __global__ void __launch_bounds__(kCopyThreads)
 reorder_kernel(const __grid_constant__ ReorderArgs A, const int* __restrict__ parents, const int* __restrict__ lengths)
 {
     constexpr int kVec = (int)sizeof(Vec), kStep = kCopyThreads * kVec;
+    __shared__ const char* s_from[W];
+    __shared__ int s_left[W];                  // bytes that are copied from the CTA's first column on (0: none, or the state stays)
     pdl_wait();
     const gr_state_layout& L = A.at;
-    const long long units = A.chunks * L.parts * L.batch * A.count;
+    const int tid = threadIdx.x, pieces = L.parts * L.batch;
+    const long long start = (long long)blockIdx.x * C * kStep;
 #pragma unroll 1
-    for (long long u = blockIdx.x; u < units; u += gridDim.x) {
-        const long long chunk = u % A.chunks;
-        long long rest = u / A.chunks;
-        const int part = (int)(rest % L.parts);
-        rest /= L.parts;
-        const int b = (int)(rest % L.batch), s = (int)(rest / L.batch);
-        const char* src = A.src[s] + b * L.src_group + part * L.src_part;
-        char* dst = A.dst[s] + b * L.dst_group + part * L.dst_part;
-        const long long first = chunk * C * kStep + threadIdx.x * kVec;
-        Vec v[C][W];
-        int left[W];                       // bytes that are copied from this thread's first column on (0: none, or the state stays)
-#pragma unroll
-        for (int j = 0; j < W; j++) {
-            left[j] = 0;
-            if (j < L.beams_out) {
-                const int p = __ldg(parents + (size_t)b * L.beams_out + j);
-                if (p >= 0 && p < L.beams_in && !(A.in_place && p == j)) {
+    for (int piece = blockIdx.y; piece < pieces; piece += gridDim.y) {
+        const int b = piece / L.parts, part = piece - b * L.parts, s = blockIdx.z;
+        bool any = false;
+        if (tid < W) {
+            int left = 0;
+            const char* from = nullptr;
+            if (tid < L.beams_out) {
+                const int p = __ldg(parents + (size_t)b * L.beams_out + tid);
+                if (p >= 0 && p < L.beams_in && !(A.in_place && p == tid)) {
                     long long used = L.part_bytes;
                     if (lengths) used = min(used, max(0, __ldg(lengths + (size_t)b * L.beams_in + p)) * L.token_bytes);
-                    left[j] = (int)min(max(used - first, 0ll), 1ll << 30);
-                    const char* from = src + p * L.src_beam + first;
+                    left = (int)min(max(used - start, 0ll), 1ll << 30);
+                    from = A.src[s] + b * L.src_group + p * L.src_beam + part * L.src_part + start;
+                }
+            }
+            s_left[tid] = left; s_from[tid] = from;
+            any = left > 0;
+        }
+        if (__syncthreads_or(any)) {
+            char* dst = A.dst[s] + b * L.dst_group + part * L.dst_part + start + tid * kVec;
+            Vec v[C][W];
 #pragma unroll
-                    for (int c = 0; c < C; c++) {
-                        // (a vector that holds the last used byte is read whole: pieces are a multiple of kVec long)
-                        if (c * kStep < left[j]) v[c][j] = *reinterpret_cast<const Vec*>(from + c * kStep);
-                    }
+            for (int j = 0; j < W; j++) {
+#pragma unroll
+                for (int c = 0; c < C; c++) {
+                    // (a vector that holds the last used byte is read whole: pieces are a multiple of kVec long)
+                    if (tid * kVec + c * kStep < s_left[j]) v[c][j] = *reinterpret_cast<const Vec*>(s_from[j] + tid * kVec + c * kStep);
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < W; j++) {
+#pragma unroll
+                for (int c = 0; c < C; c++) {
+                    const int more = s_left[j] - tid * kVec - c * kStep;
+                    char* to = dst + j * L.dst_beam + c * kStep;
+                    if (more >= kVec) *reinterpret_cast<Vec*>(to) = v[c][j];
+                    else if (more > 0) store_bytes(to, v[c][j], more);
                 }
             }
         }
-#pragma unroll
-        for (int j = 0; j < W; j++) {
-            char* to = dst + j * L.dst_beam + first;
-#pragma unroll
-            for (int c = 0; c < C; c++) {
-                const int more = left[j] - c * kStep;
-                if (more >= kVec) *reinterpret_cast<Vec*>(to + c * kStep) = v[c][j];
-                else if (more > 0) store_bytes(to + c * kStep, v[c][j], more);
-            }
-        }
+        if (piece + (int)gridDim.y < pieces) __syncthreads();
     }
 }
 
@@ -174,21 +180,23 @@ static int check_apart(const void* const* p, int count, long long bytes)
 }
 
 template <int W>
-static void launch_reorder(const ReorderArgs& A, int vec, const int* parents, const int* lengths, cudaStream_t st)
+static void launch_reorder(const ReorderArgs& A, int count, int vec, const int* parents, const int* lengths, cudaStream_t st)
 {
-    ReorderArgs B = A;
     const gr_state_layout& L = A.at;
     auto go = [&](auto kernel, int bytes, int columns) {
         const long long per = (long long)bytes * columns * kCopyThreads;
-        B.chunks = (L.part_bytes + per - 1) / per;
-        const long long units = B.chunks * L.parts * L.batch * A.count;
-        const int grid = (int)std::min<long long>(units, 1 << 20);
-        launch_pdl(kernel, grid, kCopyThreads, 0, st, B, parents, lengths);
+        cudaLaunchConfig_t cfg = {};
+        cudaLaunchAttribute at = {};
+        at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        at.val.programmaticStreamSerializationAllowed = 1;
+        cfg.gridDim = dim3((unsigned)((L.part_bytes + per - 1) / per), (unsigned)std::min(L.parts * L.batch, 65535), (unsigned)count);
+        cfg.blockDim = dim3(kCopyThreads); cfg.stream = st; cfg.attrs = &at; cfg.numAttrs = 1;
+        cudaLaunchKernelEx(&cfg, kernel, A, parents, lengths);
     };
     // (narrow columns: several of them per thread, so that as many bytes are in flight)
-    constexpr int N4 = W <= 8 ? 4 : 2;
+    constexpr int N4 = W <= 4 ? 8 : W <= 8 ? 4 : 2, kWide = 2;
     switch (vec) {
-        case 16: go(reorder_kernel<W, uint4, 1>, 16, 1); break;
+        case 16: go(reorder_kernel<W, uint4, W <= 4 ? kWide : 1>, 16, W <= 4 ? kWide : 1); break;
         case 8: go(reorder_kernel<W, uint2, 2>, 8, 2); break;
         case 4: go(reorder_kernel<W, unsigned, N4>, 4, N4); break;
         case 2: go(reorder_kernel<W, unsigned short, N4>, 2, N4); break;
@@ -208,6 +216,7 @@ int gr_reorder_states(const void* const* src, void* const* dst, int count, const
     if (count < 0 || L.batch < 0 || L.parts < 0 || L.part_bytes < 0) return GR_E_INVALID;
     if (L.beams_in < 1 || L.beams_in > GR_MAX_BEAMS || L.beams_out < 1 || L.beams_out > GR_MAX_BEAMS) return GR_E_INVALID;
     if (L.src_group < 0 || L.src_beam < 0 || L.src_part < 0 || L.dst_group < 0 || L.dst_beam < 0 || L.dst_part < 0) return GR_E_INVALID;
+    if ((long long)L.batch * L.parts >= (1ll << 31)) return GR_E_INVALID;
     if (lengths && (L.token_bytes < 1 || L.part_bytes % L.token_bytes)) return GR_E_INVALID;
     if (count == 0 || L.batch == 0 || L.parts == 0 || L.part_bytes == 0) return GR_OK;
     if (!src || !dst || !parents) return GR_E_NULL;
@@ -232,13 +241,13 @@ int gr_reorder_states(const void* const* src, void* const* dst, int count, const
     gr::NvtxRange whole("gr_reorder_states");
     for (int lo = 0; lo < count; lo += gr::kStatesPerLaunch) {
         gr::ReorderArgs A;
-        A.at = L; A.in_place = in_place; A.chunks = 0;
-        A.count = std::min(count - lo, gr::kStatesPerLaunch);
-        for (int i = 0; i < A.count; i++) { A.src[i] = (const char*)src[lo + i]; A.dst[i] = (char*)dst[lo + i]; }
-        if (L.beams_out <= 4) gr::launch_reorder<4>(A, vec, parents, lengths, st);
-        else if (L.beams_out <= 8) gr::launch_reorder<8>(A, vec, parents, lengths, st);
-        else if (L.beams_out <= 16) gr::launch_reorder<16>(A, vec, parents, lengths, st);
-        else gr::launch_reorder<32>(A, vec, parents, lengths, st);
+        A.at = L; A.in_place = in_place;
+        const int n = std::min(count - lo, gr::kStatesPerLaunch);
+        for (int i = 0; i < n; i++) { A.src[i] = (const char*)src[lo + i]; A.dst[i] = (char*)dst[lo + i]; }
+        if (L.beams_out <= 4) gr::launch_reorder<4>(A, n, vec, parents, lengths, st);
+        else if (L.beams_out <= 8) gr::launch_reorder<8>(A, n, vec, parents, lengths, st);
+        else if (L.beams_out <= 16) gr::launch_reorder<16>(A, n, vec, parents, lengths, st);
+        else gr::launch_reorder<32>(A, n, vec, parents, lengths, st);
     }
     if (cudaPeekAtLastError() != cudaSuccess) { cudaGetLastError(); return GR_E_LAUNCH; }
     return GR_OK;
