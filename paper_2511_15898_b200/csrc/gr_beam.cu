@@ -79,8 +79,8 @@ __device__ __forceinline__ void keep_keys(SS& sh, int listed, unsigned long long
     __syncthreads();
 }
 
-template <typename T, int U>
-__global__ void __launch_bounds__(kBeamThreads, 4)
+template <typename T, int U, int CTAS>
+__global__ void __launch_bounds__(kBeamThreads, CTAS)
 beam_stream_kernel(const __grid_constant__ BeamArgs A)
 {
     using VT = VecTraits<T>;
@@ -244,7 +244,8 @@ beam_stream_kernel(const __grid_constant__ BeamArgs A)
             if (e < M) { vv[u] = GR_ARRAY_AS(ulonglong2, sh.keys, e); id[u] = GR_ARRAY_AS(int, sh.keys, 4 * BeamSm::kList + e); }
             own = fmaxf(own, VT::largest(vv[u]));
         }
-        if (M > K) refine_tau(sh, own, K);
+        // (a short list is ranked as it is, in less time than a threshold takes)
+        if (M > kRankAll) refine_tau(sh, own, K);
         const float tau = sh.tau;
         if (tid == 0) sh.kept = 0;
         __syncthreads();
@@ -644,8 +645,10 @@ static int launch_beam(const BeamArgs& A, int batch, cudaStream_t st)
             raised[dev] = true;
         }
     }
-    constexpr int U = 4;
-    launch_pdl(beam_stream_kernel<T, U>, batch * A.beams * A.parts, kBeamThreads, 0, st, A);
+    // Few CTAs: a whole chunk per warp in flight, so that a short part needs one trip to memory and one threshold.
+    const int ctas = batch * A.beams * A.parts;
+    if (ctas <= 2 * kSms) launch_pdl(beam_stream_kernel<T, kChunk / (32 * VecTraits<T>::N), 2>, ctas, kBeamThreads, 0, st, A);
+    else launch_pdl(beam_stream_kernel<T, 4, 4>, ctas, kBeamThreads, 0, st, A);
     launch_pdl(beam_choose_kernel<T>, batch, kBeamThreads, smem, st, A);
     return GR_OK;
 }
