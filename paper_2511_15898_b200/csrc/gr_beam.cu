@@ -305,7 +305,8 @@ struct BeamGroup {
     unsigned char exact[GR_MAX_BEAMS];         // ... and has been
     int bad, check, survivors, redo;
     float peak[GR_MAX_BEAMS];                  // probability of the row's first token
-    double least, slack;                       // slack: the largest distance of keys at which sums are taken again
+    unsigned long long least;                  // a bound below the last key that is taken (as an integer that orders like it)
+    double slack;                              // the largest distance of keys at which sums are taken again
     double best_key[GR_MAX_SELECT + 1];
     int best_at[GR_MAX_SELECT + 1];
 };
@@ -411,8 +412,8 @@ beam_choose_kernel(const __grid_constant__ BeamArgs A)
     const int W = A.beams, P = A.parts, K = A.select, keep = A.keep, lists = W * P, shift = list_shift(keep), most = lists << shift;
     GR_PTR(double) key = GR_MKPTR(double, reinterpret_cast<double*>(s_dyn), most, GR_CHECK_FLAG);
     GR_PTR(unsigned long long) raw = GR_MKPTR(unsigned long long, reinterpret_cast<unsigned long long*>(s_dyn) + most, most, GR_CHECK_FLAG);
-    GR_PTR(unsigned long long) sv_key = GR_MKPTR(unsigned long long, reinterpret_cast<unsigned long long*>(s_dyn) + 2 * (size_t)most, most, GR_CHECK_FLAG);
-    GR_PTR(unsigned long long) sv_raw = GR_MKPTR(unsigned long long, reinterpret_cast<unsigned long long*>(s_dyn) + 3 * (size_t)most, most, GR_CHECK_FLAG);
+    // (survivors: the key as an integer that orders like it, and the logit and token)
+    GR_PTR(ulonglong2) sv = GR_MKPTR(ulonglong2, reinterpret_cast<ulonglong2*>(s_dyn) + most, most, GR_CHECK_FLAG);
     GR_PTR(int) sv_row = GR_MKPTR(int, reinterpret_cast<int*>(s_dyn + 32 * (size_t)most), most, GR_CHECK_FLAG);
     const int stride = beam_stride(keep);
     const char* recs = A.ws + (size_t)b * lists * stride;
@@ -506,37 +507,40 @@ beam_choose_kernel(const __grid_constant__ BeamArgs A)
         }
         if (g.bad) break;
         __syncthreads();
-        if (tid == 0) { g.survivors = 0; g.redo = 0; g.least = -INFINITY; }
+        if (tid == 0) { g.survivors = 0; g.redo = 0; g.least = sortable(-INFINITY); }
         // ---- scores, and a bound below the select-th: of the q-th entries of the lists the ceil(K / q)-th largest, q the
         // smallest power of two that leaves at most half of the lists above it
         for (int e = tid; e < most; e += kBeamThreads) {
             const int l = e >> shift, i = e & ((1 << shift) - 1), w = g.row[l];
             key[e] = i < g.count[l] ? total_of(w, raw[e]) * g.inv_scale[w] : -INFINITY;
         }
-        int lg = 0;
-        while ((1 << lg) < keep && 2 * ((K + (1 << lg) - 1) >> lg) > lists) lg++;
-        const int q = min(1 << lg, keep), place = (K + q - 1) / q;
+        // (few lists: every power of two, and the largest of the bounds)
+        int lg0 = 0;
+        while ((1 << lg0) < keep && 2 * ((K + (1 << lg0) - 1) >> lg0) > lists) lg0++;
+        const int lg1 = lists <= 64 ? shift : lg0;
+        if (lists <= 64) lg0 = 0;
         __syncthreads();
-        if (place <= lists) {
-            for (int l = tid; l < lists; l += kBeamThreads) {
-                const double mine = key[(l << shift) + q - 1];
-                int rank = 0;
+        for (int t = tid; t < lists * (lg1 - lg0 + 1); t += kBeamThreads) {
+            const int level = t / lists, l = t - level * lists;
+            const int q = min(1 << (lg0 + level), keep), place = (K + q - 1) / q;
+            if (place > lists) continue;
+            const double mine = key[(l << shift) + q - 1];
+            int rank = 0;
 #pragma unroll 4
-                for (int o = 0; o < lists; o++) {
-                    const double k = key[(o << shift) + q - 1];
-                    rank += k > mine || (k == mine && o < l) ? 1 : 0;
-                }
-                if (rank == place - 1) g.least = mine;
+            for (int o = 0; o < lists; o++) {
+                const double k = key[(o << shift) + q - 1];
+                rank += k > mine || (k == mine && o < l) ? 1 : 0;
             }
+            if (rank == place - 1) atomicMax(&g.least, sortable(mine));
         }
         __syncthreads();
         // (those within kNear below the bound too: they may have to be told from the last ones)
-        const double least = g.least - g.slack;
+        const double least = unsortable(g.least) - g.slack;
         for (int e = tid; e < most; e += kBeamThreads) {
             const int l = e >> shift;
             if ((e & ((1 << shift) - 1)) < g.count[l] && !(key[e] < least)) {
                 const int at = atomicAdd(&g.survivors, 1);
-                sv_key[at] = sortable(key[e]); sv_raw[at] = raw[e]; sv_row[at] = g.row[l];
+                sv[at] = make_ulonglong2(sortable(key[e]), raw[e]); sv_row[at] = g.row[l];
             }
         }
         __syncthreads();
@@ -551,14 +555,14 @@ beam_choose_kernel(const __grid_constant__ BeamArgs A)
             unsigned long long mine = 0ull;
             if (a < M) {
                 const int w = sv_row[a];
-                mine = sv_key[a];
-                const unsigned long long mine_raw = sv_raw[a];
+                const ulonglong2 own = sv[a];
+                mine = own.x;
 #pragma unroll 4
                 for (int o = tid & (team - 1); o < M; o += team) {
                     const int v = sv_row[o];
-                    const unsigned long long k = sv_key[o];
-                    const bool ahead = v == w ? sv_raw[o] > mine_raw : (k > mine || (k == mine && v < w));
-                    rank += ahead ? 1 : 0;
+                    const ulonglong2 k = sv[o];
+                    const bool within = k.y > own.y, across = k.x > own.x || (k.x == own.x && v < w);
+                    rank += (v == w ? within : across) ? 1 : 0;
                 }
             }
             __syncwarp();
@@ -578,7 +582,7 @@ beam_choose_kernel(const __grid_constant__ BeamArgs A)
         for (int i = tid; i + 1 < min(M, K + 1); i += kBeamThreads) close(g.best_at[i], g.best_at[i + 1], g.best_key[i] - g.best_key[i + 1]);
         if (M > K) {
             const double last = g.best_key[K - 1];
-            for (int a = tid; a < M; a += kBeamThreads) close(a, g.best_at[K - 1], unsortable(sv_key[a]) - last);
+            for (int a = tid; a < M; a += kBeamThreads) close(a, g.best_at[K - 1], unsortable(sv[a].x) - last);
         }
         __syncthreads();
         if (!g.redo) break;
@@ -593,8 +597,8 @@ beam_choose_kernel(const __grid_constant__ BeamArgs A)
         if (!bad && i < M) {
             const int e = g.best_at[i];
             parent = sv_row[e];
-            token = (int)(0xffffffffu - (unsigned)sv_raw[e]);
-            total = (float)total_of(parent, sv_raw[e]);
+            token = (int)(0xffffffffu - (unsigned)sv[e].y);
+            total = (float)total_of(parent, sv[e].y);
             length = g.length[parent];
             ended = g.kind[parent] == kRowDone || token == A.eos;
         }
