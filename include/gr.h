@@ -345,10 +345,10 @@ int gr_beam_select(const void* logits, int dtype, int V, long long ld, int beams
  * A state is `parts` pieces (heads, say) of part_bytes bytes.  Piece p of state w of group b begins
  * b * src_group + w * src_beam + p * src_part bytes after src[i], and likewise for dst[i].
  *   src, dst   HOST arrays of `count` device pointers.  dst[i] == src[i] with equal strides reorders in place (any
- *              mapping, cycles and repeated parents included); otherwise the memory of dst[i] must not overlap that of
- *              any src.  The same dst twice (or two that begin less than part_bytes apart) is GR_E_INVALID, and so
- *              are strides that make the pieces of a dst overlap.  Within src, groups, states and pieces may coincide
- *              (stride 0), unless it is reordered in place.
+ *              mapping, cycles and repeated parents included); otherwise no dst may meet a src (from the first byte of its
+ *              pieces to the last: GR_E_INVALID).  The same dst twice (or two that begin less than part_bytes apart) is
+ *              GR_E_INVALID, and so are strides that make the pieces of a dst overlap.  Within src, groups, states and
+ *              pieces may coincide (stride 0), unless it is reordered in place.
  *   parents    [batch, beams_out] int.  -1, or any number outside 0 .. beams_in - 1: that state is left as it was.
  *   lengths    [batch, beams_in] int or NULL.  With it a piece is a run of tokens of token_bytes bytes each and only the
  *              first lengths[b, parent] tokens of each piece are copied (clamped to what the piece holds); the

@@ -563,16 +563,11 @@ def _state_layout(x: torch.Tensor, token_dim: Optional[int]):
     return parts, step * e, part * e, part // tokens * e if tokens else e
 
 
-def _span(t: torch.Tensor) -> int:
-    """Bytes from a tensor's first element to behind its last one."""
-    return (sum((n - 1) * s for n, s in zip(t.shape, t.stride())) + 1) * t.element_size() if t.numel() else 0
-
-
 def reorder_states(states, parents: torch.Tensor, lengths: Optional[torch.Tensor] = None,
                    token_dim: Optional[int] = None, out=None):
     """gr_reorder_states on torch CUDA tensors: `states` is a list of tensors [B, beams, ...] (of any types and layouts),
     parents [B, chosen] int32.  In place, with chosen <= beams, unless `out` (a list of tensors [B, chosen, ...]) is
-    given, which must not share memory with the states.  With lengths [B, beams] int32 the dimension `token_dim` of the
+    given, which must not meet the states in memory.  With lengths [B, beams] int32 the dimension `token_dim` of the
     states counts tokens, of which each parent's first lengths[b, parent] are copied.  Returns `out` or `states`."""
     states = list(states)
     to = states if out is None else list(out)
@@ -591,7 +586,7 @@ def reorder_states(states, parents: torch.Tensor, lengths: Optional[torch.Tensor
         raise GrError("states must be CUDA tensors [B, beams, ...] on the device of parents")
     W = states[0].shape[1]
     a_lengths = _need(lengths, "lengths", torch.int32, (B, W), dev, optional=True)
-    # runs of tensors of one layout: (layout, addresses of states and outs, bytes that a state and an out span)
+    # runs of tensors of one layout: (layout, addresses of states and outs)
     runs = []
 
     def layout_of(x, y):
@@ -614,11 +609,7 @@ def reorder_states(states, parents: torch.Tensor, lengths: Optional[torch.Tensor
     at = _alike(states)
     at_y = at if out is None or at is None else _alike(to)
     if at_y is not None:
-        layout = layout_of(states[0], to[0])
-        if out is None:
-            runs.append((layout, at, at, 0, 0))
-        else:
-            runs.append((layout, array.array("Q", at), array.array("Q", at_y), _span(states[0]), _span(to[0])))
+        runs.append((layout_of(states[0], to[0]), at, at_y))
     else:
         last = None
         for x, y in zip(states, to):
@@ -627,19 +618,17 @@ def reorder_states(states, parents: torch.Tensor, lengths: Optional[torch.Tensor
             kind = (x.shape, x.stride(), x.dtype, x.device, y.shape, y.stride(), y.dtype, y.device)
             if kind != last:
                 last = kind
-                runs.append((layout_of(x, y), [], [], _span(x), _span(y)))
+                runs.append((layout_of(x, y), [], []))
             runs[-1][1].append(x.data_ptr())
             runs[-1][2].append(y.data_ptr())
-    if out is not None:
-        if (min(min(r[2]) for r in runs) < max(max(r[1]) + r[3] for r in runs)
-                and min(min(r[1]) for r in runs) < max(max(r[2]) + r[4] for r in runs)
-                and any(p < q + n and q < p + m for _, _, at, _, m in runs for p in at for _, of, _, n, _ in runs for q in of)):
-            raise GrError("out shares memory with the states")
     if len(runs) > 1:
-        first = [p for r in runs if r[0].part_bytes for p in (r[1] if out is None else r[2])]
+        # (within a run the C call looks)
+        first = [p for r in runs if r[0].part_bytes for p in r[2]]
         if len(set(first)) < len(first):
             raise GrError("the same tensor twice")
-    for layout, at, at_y, _, _ in runs:
+        if out is not None and any(y.untyped_storage().data_ptr() == x.untyped_storage().data_ptr() for y in to for x in states if y.numel()):
+            raise GrError("out shares memory with the states")
+    for layout, at, at_y in runs:
         if chosen > 0 and layout.part_bytes > 0:
             _call(dev, "gr_reorder_states", gr_reorder_states, at, at_y, layout, a_parents, a_lengths)
     return to

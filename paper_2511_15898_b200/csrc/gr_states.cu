@@ -151,21 +151,38 @@ static int vec_of(unsigned long long bits) {
 
 constexpr long long kMaxBytes = 1ll << 46;        // beyond any device's memory: keeps the sums of strides in range
 
-// Whether size[i] pieces at stride[i] apart, i = 0 .. 2, of `bytes` bytes each, lie clear of one another (by nesting: each
-// stride spans all that lies within it) and within the address range; with `apart` false only the latter.
-static bool laid_out(long long bytes, const long long* stride, const int* size, bool apart)
+// Bytes that size[i] pieces at stride[i] apart, i = 0 .. 2, of `bytes` bytes each span; 0 where that leaves the address range
+// or (with `apart`) where the pieces do not lie clear of one another (by nesting: each stride spans all that lies within it).
+static long long span_of(long long bytes, const long long* stride, const int* size, bool apart)
 {
     int order[3] = {0, 1, 2};
     std::sort(order, order + 3, [&](int a, int b) { return stride[a] < stride[b]; });
-    if (bytes > kMaxBytes) return false;
+    if (bytes > kMaxBytes) return 0;
     __int128 span = bytes;
     for (int i : order) {
         if (size[i] <= 1) continue;
-        if (apart && stride[i] < span) return false;
+        if (apart && stride[i] < span) return 0;
         span += (__int128)stride[i] * (size[i] - 1);
-        if (span > kMaxBytes) return false;
+        if (span > kMaxBytes) return 0;
     }
-    return true;
+    return (long long)span;
+}
+
+// Whether any of p[i] .. p[i] + a meets any of q[j] .. q[j] + b
+static bool meet(const void* const* p, long long a, void* const* q, long long b, int count)
+{
+    uintptr_t p0 = UINTPTR_MAX, p1 = 0, q0 = UINTPTR_MAX, q1 = 0;
+    for (int i = 0; i < count; i++) {
+        p0 = std::min(p0, (uintptr_t)p[i]); p1 = std::max(p1, (uintptr_t)p[i] + (uintptr_t)a);
+        q0 = std::min(q0, (uintptr_t)q[i]); q1 = std::max(q1, (uintptr_t)q[i] + (uintptr_t)b);
+    }
+    if (p1 <= q0 || q1 <= p0) return false;
+    for (int i = 0; i < count; i++) {
+        for (int j = 0; j < count; j++) {
+            if ((uintptr_t)p[i] < (uintptr_t)q[j] + (uintptr_t)b && (uintptr_t)q[j] < (uintptr_t)p[i] + (uintptr_t)a) return true;
+        }
+    }
+    return false;
 }
 
 // GR_OK where the pointers lie at least `bytes` apart
@@ -227,7 +244,9 @@ int gr_reorder_states(const void* const* src, void* const* dst, int count, const
         return GR_E_INVALID;
     const long long to[3] = {L.dst_group, L.dst_beam, L.dst_part}, from[3] = {L.src_group, L.src_beam, L.src_part};
     const int to_size[3] = {L.batch, in_place ? L.beams_in : L.beams_out, L.parts}, from_size[3] = {L.batch, L.beams_in, L.parts};
-    if (!gr::laid_out(L.part_bytes, to, to_size, true) || !gr::laid_out(L.part_bytes, from, from_size, false)) return GR_E_INVALID;
+    const long long to_span = gr::span_of(L.part_bytes, to, to_size, true), from_span = gr::span_of(L.part_bytes, from, from_size, false);
+    if (to_span == 0 || from_span == 0) return GR_E_INVALID;
+    if (!in_place && gr::meet(src, from_span, dst, to_span, count)) return GR_E_INVALID;
     const int apart = gr::check_apart(dst, count, L.part_bytes);
     if (apart != GR_OK) return apart;
     unsigned long long bits = (unsigned long long)L.part_bytes;

@@ -64,6 +64,7 @@ def test_reorder_states():
     assert call(src=(A, A + 64), dst=(A, A + 64)) == -1            # two that overlap
     assert call(src=(A, A + 99999), dst=(A, A + 8192)) == -1       # some in place, some not
     B = A + (1 << 24)
+    assert call(dst=(A + 7551,)) == -1 and call(src=(A, A + 16384), dst=(B, A + 7040)) == -1    # a dst that meets a src (7552 bytes)
     assert call(dst=(B,), dst_beam=0) == -1 and call(dst=(B,), dst_part=64) == -1 and call(dst=(B,), dst_group=1024) == -1
     assert call(dst=(B,), dst_beam=1 << 47) == -1 and call(part_bytes=1 << 47) == -1
     assert call(batch=1 << 20, parts=1 << 12, src_group=1 << 22, dst_group=1 << 22) == -1

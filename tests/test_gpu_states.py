@@ -213,3 +213,29 @@ def test_in_a_graph_and_on_another_stream():
         G.reorder_states([x], parents)
     side.synchronize()
     assert same(x, want)
+
+
+def test_outs_that_meet_the_states_and_repeats_are_refused():
+    x = rand((2, 8, 64), torch.float32, 1)
+    parents = torch.zeros(2, 4, dtype=torch.int32, device="cuda")
+    keep = x.clone()
+    with pytest.raises(G.GrError):
+        G.reorder_states([x], parents, out=[x[:, 4:]])
+    with pytest.raises(G.GrError):
+        G.reorder_states([x, x], torch.zeros(2, 8, dtype=torch.int32, device="cuda"))
+    odd = rand((2, 8, 10), torch.float32, 2)
+    with pytest.raises(G.GrError):
+        G.reorder_states([x, odd, x], torch.zeros(2, 8, dtype=torch.int32, device="cuda"))
+    with pytest.raises(G.GrError):
+        G.reorder_states([x, odd], parents, out=[torch.empty(2, 4, 64, device="cuda"), odd[:, :4]])
+    with pytest.raises(G.GrError):
+        G.reorder_states([x], torch.zeros(2, 9, dtype=torch.int32, device="cuda"))
+    with pytest.raises(G.GrError):
+        G.copy_blocks([x[0], x[0]], parents[0], parents[1])
+    torch.cuda.synchronize()
+    assert same(x, keep)
+    # halves of one buffer do not meet
+    buf = rand((2, 2, 4, 33), torch.float32, 3)
+    G.reorder_states([buf[0]], parents, out=[buf[1]])
+    torch.cuda.synchronize()
+    assert same(buf[1], buf[0][:, :1].expand(2, 4, 33))
