@@ -57,7 +57,8 @@ struct BeamArgs {
 
 __host__ __device__ inline int beam_stride(int keep) { return (int)sizeof(BeamPart) + 8 * ((keep + 1) & ~1); }
 
-using BeamSm = ScanShared<kBeamThreads, 1024, 2048, 1>;
+// (as many listed vectors, and elements of them that pass the last threshold, as leave room for the CTAs of an SM)
+template <int NTHR> using BeamSm = ScanShared<NTHR, 4 * NTHR, 8 * NTHR, 1>;
 
 // v 2^k, k a whole number at or below 0 (what falls below 2^-1000 of v is dropped); a NaN stays one
 __device__ __forceinline__ double times_pow2(double v, float k)
@@ -79,16 +80,18 @@ __device__ __forceinline__ void keep_keys(SS& sh, int listed, unsigned long long
     __syncthreads();
 }
 
-template <typename T, int U, int CTAS>
-__global__ void __launch_bounds__(kBeamThreads, CTAS)
+template <typename T, int U, int NTHR, int CTAS>
+__global__ void __launch_bounds__(NTHR, CTAS)
 beam_stream_kernel(const __grid_constant__ BeamArgs A)
 {
     using VT = VecTraits<T>;
+    using Sm = BeamSm<NTHR>;
+    constexpr int kWarps = NTHR / 32;
     constexpr int N = VT::N, S = kChunk / (32 * N), NB = S / U;
     static_assert(S % U == 0, "a chunk is a whole number of batches");
-    __shared__ BeamSm sh;
-    __shared__ float s_ref[kBeamWarps];
-    __shared__ double s_sum[kBeamWarps];
+    __shared__ Sm sh;
+    __shared__ float s_ref[kWarps];
+    __shared__ double s_sum[kWarps];
     pdl_wait();
     GR_CHECK_FLAG_DECL;
     GR_CHECK_FLAG_INIT;
@@ -106,8 +109,8 @@ beam_stream_kernel(const __grid_constant__ BeamArgs A)
     const int head = row_head(x, 0, V, (int)sizeof(T));
     const int nch = num_chunks(V, head);
     // this part's chunks: first + warp, + stride, ...
-    const int first = part * kBeamWarps, stride = A.parts * kBeamWarps;
-    const bool use_tau = V > BeamSm::kCap;             // (else every element may be listed)
+    const int first = part * kWarps, stride = A.parts * kWarps;
+    const bool use_tau = V > Sm::kCap;             // (else every element may be listed)
     const int vec_end = head + ((V - head) / N) * N, tail = V - vec_end;
     if (tid == 0) { sh.cnt = 0; sh.tau = -3.402823466e38f; sh.reset_checks(); }
     __syncthreads();
@@ -143,7 +146,11 @@ beam_stream_kernel(const __grid_constant__ BeamArgs A)
         }
         if (!use_tau) push_edges(-3.402823466e38f);
     }
-    int r = 0, upto = use_tau ? 4 : rounds;                 // rounds up to the next threshold
+    // Rounds up to the next threshold.  About A = K + K^2 / NTHR elements of what a threshold was taken from reach it, so A of
+    // each further part of that size are listed, with a deviation of a sqrt(A)-th: twice as many have to find room.
+    const int A_K = K + K * K / NTHR;
+    int r = 0, upto = !use_tau ? rounds : 2 * 4 * NB * A_K <= Sm::kList ? 4 : 1;
+    int expected = upto * NB * A_K;
 #pragma unroll 1
     while (true) {
 #pragma unroll 1
@@ -213,12 +220,14 @@ beam_stream_kernel(const __grid_constant__ BeamArgs A)
         }
         if (r >= rounds) break;
         upto *= 4;
-        // a better threshold whenever the part read has grown fourfold, unless less is to come than has been read; and a shorter
-        // list where it would not hold what is to come
-        if (rounds < 2 * r && 5 * (K + K * K / kBeamThreads) * (rounds - r) < 2 * BeamSm::kList * r) { upto = rounds; continue; }
+        // A better threshold whenever the part read has grown fourfold, unless less is to come than has been read and there is
+        // room for it; and a shorter list where it would not hold what is to come.
+        // (Decided by expected lengths, the same for every thread: the list itself may still be growing.)
+        if (rounds < 2 * r && 2 * (expected * r + A_K * (rounds - r)) < Sm::kList * r) { upto = rounds; continue; }
         const int listed = refine_tau(sh, g0, K);
-        const int more = (K + K * K / kBeamThreads) * min(3 * r, rounds - r);
-        if (listed <= BeamSm::kList && 5 * more > 4 * (BeamSm::kList - listed) * r) keep_listed<T>(sh, listed);
+        expected = min(expected + 3 * A_K, Sm::kList);
+        const int more = A_K * min(3 * r, rounds - r);                                    // times r
+        if (listed <= Sm::kList && 2 * more > (Sm::kList - listed) * r) keep_listed<T>(sh, listed);
     }
     // ---- the part's sum
     {
@@ -230,22 +239,22 @@ beam_stream_kernel(const __grid_constant__ BeamArgs A)
     __syncthreads();
     // ---- candidates: a last threshold from the list itself, then keys of those that pass it
     int M = sh.cnt;
-    bool over = M > BeamSm::kList;
+    bool over = M > Sm::kList;
     if (!over) {
-        constexpr int kPer = (BeamSm::kList + kBeamThreads - 1) / kBeamThreads;
+        constexpr int kPer = (Sm::kList + NTHR - 1) / NTHR;
         // (the keys take the list's place: what a thread lists is in its registers before)
         ulonglong2 vv[kPer];
         int id[kPer];
         float own = -INFINITY;
 #pragma unroll
         for (int u = 0; u < kPer; u++) {
-            const int e = tid + u * kBeamThreads;
+            const int e = tid + u * NTHR;
             vv[u].x = VT::kNone; vv[u].y = VT::kNone; id[u] = 0;
-            if (e < M) { vv[u] = GR_ARRAY_AS(ulonglong2, sh.keys, e); id[u] = GR_ARRAY_AS(int, sh.keys, 4 * BeamSm::kList + e); }
+            if (e < M) { vv[u] = GR_ARRAY_AS(ulonglong2, sh.keys, e); id[u] = GR_ARRAY_AS(int, sh.keys, 4 * Sm::kList + e); }
             own = fmaxf(own, VT::largest(vv[u]));
         }
         // (a short list is ranked as it is, in less time than a threshold takes)
-        if (M > kRankAll) refine_tau(sh, own, K);
+        if (M > NTHR / 2) refine_tau(sh, own, K);
         const float tau = sh.tau;
         if (tid == 0) sh.kept = 0;
         __syncthreads();
@@ -258,14 +267,14 @@ beam_stream_kernel(const __grid_constant__ BeamArgs A)
                     const float w = VT::element(vv[u], i);
                     if (w >= tau && w > -INFINITY) {
                         const int slot = atomicAdd(&sh.kept, 1);
-                        if (slot < BeamSm::kCap) sh.keys[slot] = ckey(w, id[u] + i);
+                        if (slot < Sm::kCap) sh.keys[slot] = ckey(w, id[u] + i);
                     }
                 }
             }
         }
         __syncthreads();
         M = sh.kept;
-        over = M > BeamSm::kCap;
+        over = M > Sm::kCap;
     }
     if (over) {
         __syncthreads();
@@ -280,9 +289,9 @@ beam_stream_kernel(const __grid_constant__ BeamArgs A)
     rank_select(sh, M, nsel, [&](int rank, unsigned long long key) { rec_keys[rank] = key; });
     if (tid == 0) {
         float top = s_ref[0];
-        for (int w = 1; w < kBeamWarps; w++) top = fmaxf(top, s_ref[w]);
+        for (int w = 1; w < kWarps; w++) top = fmaxf(top, s_ref[w]);
         double sum = 0.0;
-        for (int w = 0; w < kBeamWarps; w++) {
+        for (int w = 0; w < kWarps; w++) {
             if (s_sum[w] != 0.0) sum += s_ref[w] == top ? s_sum[w] : times_pow2(s_sum[w], s_ref[w] - top);
         }
         BeamPart p = {sum, top, nsel, sh.checks() | GR_CHECK_VALUE ? kPartCheck : 0, 0};
@@ -399,7 +408,7 @@ __host__ __device__ inline size_t choose_bytes(int lists, int keep) { return ((s
 // division in the loops, and the survivors next to one another: with indices to follow and lists to divide out, ranking 71 of
 // them took 13 us, now 1.)
 template <typename T>
-__global__ void __launch_bounds__(kBeamThreads)
+__global__ void __launch_bounds__(kBeamThreads, 3)
 beam_choose_kernel(const __grid_constant__ BeamArgs A)
 {
     extern __shared__ __align__(16) unsigned char s_dyn[];
@@ -650,9 +659,17 @@ static int launch_beam(const BeamArgs& A, int batch, cudaStream_t st)
         }
     }
     // Few CTAs: a whole chunk per warp in flight, so that a short part needs one trip to memory and one threshold.
+    // More than one wave of four CTAs per SM: eight smaller ones, where they do not leave a larger part of their last wave empty
+    // or where there are more than two waves of them (a row's thresholds and its selection at the end leave gaps that seven
+    // other rows fill better than three: 1024 rows of 50257 fp32 65 -> 57 us, of 128256 110 -> 103, 4096 of 152064 bf16 316 -> 300;
+    // but 1200 rows of 128256, just over one wave of the small ones, 138 -> 152).  Their lists hold 4 A + 5 deviations up to 48 keys.
     const int ctas = batch * A.beams * A.parts;
-    if (ctas <= 2 * kSms) launch_pdl(beam_stream_kernel<T, kChunk / (32 * VecTraits<T>::N), 2>, ctas, kBeamThreads, 0, st, A);
-    else launch_pdl(beam_stream_kernel<T, 4, 4>, ctas, kBeamThreads, 0, st, A);
+    auto waves = [&](int per) { return (ctas + per * kSms - 1) / (per * kSms); };
+    const bool small = A.keep <= 48 && (ctas > 16 * kSms || (ctas > 4 * kSms && 2 * waves(8) <= waves(4)));
+    // Few CTAs: a whole chunk per warp in flight, so that a short part needs one trip to memory and one threshold.
+    if (ctas <= 2 * kSms) launch_pdl(beam_stream_kernel<T, kChunk / (32 * VecTraits<T>::N), 256, 2>, ctas, 256, 0, st, A);
+    else if (small) launch_pdl(beam_stream_kernel<T, 4, 128, 8>, ctas, 128, 0, st, A);
+    else launch_pdl(beam_stream_kernel<T, 4, 256, 4>, ctas, 256, 0, st, A);
     launch_pdl(beam_choose_kernel<T>, batch, kBeamThreads, smem, st, A);
     return GR_OK;
 }

@@ -94,6 +94,15 @@ def test_sizes(dtype, B, W, V, K):
     check(G.beam_select(x, s, K), reference(x, s, K), K, V)
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("B,W,V,K", [(90, 7, 4099, 10), (150, 8, 5003, 16), (60, 20, 2053, 48), (60, 20, 2053, 49), (1, 32, 1027, 32),
+                                     (600, 5, 1029, 10), (25, 24, 9001, 40), (1200, 1, 3001, 5)])
+def test_numbers_of_rows(dtype, B, W, V, K):
+    """Few rows, one wave of CTAs and several, by the larger CTAs and the smaller ones."""
+    x, s, _ = make(B, W, V, dtype, B + V)
+    check(G.beam_select(x, s, K), reference(x, s, K), K, V)
+
+
 @pytest.mark.parametrize("T", [0.3, 0.7, 1.0, 2.5])
 def test_temperature_and_penalty(T):
     for penalty in (0.0, 0.6, 1.0, -0.5, 32.0):
