@@ -415,6 +415,7 @@ int gr_block_plan(int* table, int rows, int width, int beams, int block_size, in
  *               block_bytes apart) is GR_E_INVALID.
  *   copy_src, copy_dst  [pairs] int, as gr_block_plan writes them: a pair with an index outside 0 .. num_blocks - 1 (-1:
  *               nothing to copy) is skipped.  Blocks that are copied to must be distinct and none may be copied from.
+ *   pairs <= 2^24 - 256; blocks up to 2^22 x 1024 bytes times the power of two (up to 16) that divides pointers, stride and size.
  * No workspace.  Any alignment works; multiples of 16 are fastest.
  */
 int gr_copy_blocks(void* const* caches, int count, int num_blocks, long long block_stride, long long block_bytes,

@@ -9,6 +9,7 @@ namespace gr {
 
 constexpr int kStatesPerLaunch = 128;      // pointers that travel as kernel arguments
 constexpr int kCopyThreads = 256;
+constexpr int kCopyColumns = 4;            // vectors of a block per thread
 
 struct ReorderArgs {
     const char* src[kStatesPerLaunch];
@@ -101,16 +102,16 @@ struct CopyArgs {
     char* cache[kStatesPerLaunch];
     const int* src; const int* dst;
     long long stride, bytes;
-    int count, num_blocks, pairs;
+    int num_blocks, pairs, chunks;
 };
 
 // Each CTA takes a segment of the pair list, keeps the pairs that copy something (in their order, which is then the same in
-// all CTAs of the segment), and takes its share of (pair, cache, chunk).
+// all CTAs of the segment), and takes its share of (pair, chunk) in one cache.
 template <typename Vec>
 __global__ void __launch_bounds__(kCopyThreads)
 copy_blocks_kernel(const __grid_constant__ CopyArgs A)
 {
-    constexpr int kVec = (int)sizeof(Vec), C = 4, kStep = kCopyThreads * kVec;
+    constexpr int kVec = (int)sizeof(Vec), C = kCopyColumns, kStep = kCopyThreads * kVec;
     __shared__ int s_src[kCopyThreads], s_dst[kCopyThreads], s_warp[kCopyThreads / 32];
     pdl_wait();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -125,15 +126,14 @@ copy_blocks_kernel(const __grid_constant__ CopyArgs A)
     for (int w = 0; w < kCopyThreads / 32; w++) { if (w < warp) at += s_warp[w]; n += s_warp[w]; }
     if (copies) { s_src[at] = from; s_dst[at] = to; }
     __syncthreads();
-    const long long chunks = (A.bytes + (long long)C * kStep - 1) / ((long long)C * kStep);
-    const long long units = chunks * A.count * n;
+    char* cache = A.cache[blockIdx.z];
+    const int units = A.chunks * n;
 #pragma unroll 1
-    for (long long u = blockIdx.x; u < units; u += gridDim.x) {
-        const long long first = (u % chunks) * C * kStep + tid * kVec;
-        const long long rest = u / chunks;
-        const int s = (int)(rest % A.count), k = (int)(rest / A.count);
-        const char* in = A.cache[s] + s_src[k] * A.stride + first;
-        char* out = A.cache[s] + s_dst[k] * A.stride + first;
+    for (int u = blockIdx.x; u < units; u += gridDim.x) {
+        const int k = u / A.chunks;
+        const long long first = (long long)(u - k * A.chunks) * C * kStep + tid * kVec;
+        const char* in = cache + s_src[k] * A.stride + first;
+        char* out = cache + s_dst[k] * A.stride + first;
         Vec v[C];
 #pragma unroll
         for (int c = 0; c < C; c++) if (first + c * kStep < A.bytes) v[c] = *reinterpret_cast<const Vec*>(in + c * kStep);
@@ -286,16 +286,18 @@ int gr_copy_blocks(void* const* caches, int count, int num_blocks, long long blo
     for (int i = 0; i < count; i++) bits |= (unsigned long long)(uintptr_t)caches[i];
     const int vec = gr::vec_of(bits);
     const int segments = (int)(((long long)pairs + gr::kCopyThreads - 1) / gr::kCopyThreads);
-    if (segments > 65535) return GR_E_TOO_LARGE;
+    const long long per = (long long)vec * gr::kCopyColumns * gr::kCopyThreads, chunks = (block_bytes + per - 1) / per;
+    if (segments > 65535 || chunks > (1 << 22)) return GR_E_TOO_LARGE;
     cudaStream_t st = (cudaStream_t)stream;
     gr::NvtxRange whole("gr_copy_blocks");
     for (int lo = 0; lo < count; lo += gr::kStatesPerLaunch) {
         gr::CopyArgs A;
         A.src = copy_src; A.dst = copy_dst; A.stride = block_stride; A.bytes = block_bytes;
         A.num_blocks = num_blocks; A.pairs = pairs;
-        A.count = std::min(count - lo, gr::kStatesPerLaunch);
-        for (int i = 0; i < A.count; i++) A.cache[i] = (char*)caches[lo + i];
-        const dim3 grid(std::max(1, 8 * gr::kSms / segments), segments);
+        A.chunks = (int)chunks;
+        const int n = std::min(count - lo, gr::kStatesPerLaunch);
+        for (int i = 0; i < n; i++) A.cache[i] = (char*)caches[lo + i];
+        const dim3 grid(std::max(1, 8 * gr::kSms / (segments * n)), segments, n);
         auto go = [&](auto kernel) {
             cudaLaunchConfig_t cfg = {};
             cudaLaunchAttribute at = {};
