@@ -603,7 +603,7 @@ def reorder_states(states, parents: torch.Tensor, lengths: Optional[torch.Tensor
         part_step_y = part_step if y is x else _state_layout(y, token_dim)[1]
         e = x.element_size()
         return StateLayout(B, W, chosen, parts, step[0] * e if B > 1 else 0, step[1] * e if W > 1 else 0, part_step,
-                           step_y[0] * e if B > 1 else 0, step_y[1] * e if (W if out is None else chosen) > 1 else 0,
+                           step_y[0] * e if B > 1 else 0, step_y[1] * e if y.shape[1] > 1 else 0,
                            part_step_y, part, token)
 
     at = _alike(states)

@@ -253,8 +253,8 @@ beam_stream_kernel(const __grid_constant__ BeamArgs A)
             if (e < M) { vv[u] = GR_ARRAY_AS(ulonglong2, sh.keys, e); id[u] = GR_ARRAY_AS(int, sh.keys, 4 * Sm::kList + e); }
             own = fmaxf(own, VT::largest(vv[u]));
         }
-        // (a short list is ranked as it is, in less time than a threshold takes)
-        if (M > NTHR / 2) refine_tau(sh, own, K);
+        // (a short list is ranked as it is, in less time than a threshold takes; not one of whole vectors from a short row)
+        if (M > NTHR / 2 || (!use_tau && M * N > kRankKeys)) refine_tau(sh, own, K);
         const float tau = sh.tau;
         if (tid == 0) sh.kept = 0;
         __syncthreads();
