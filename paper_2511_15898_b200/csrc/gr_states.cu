@@ -1,5 +1,7 @@
 // What models keep per hypothesis follows the hypotheses: gr_reorder_states (dense states, in place or into other
-// tensors) and gr_copy_blocks (blocks of a paged cache that two rows shared until one of them writes).
+// tensors) and gr_copy_blocks (blocks of a paged cache that two rows shared until one of them writes).  Both are bound by HBM:
+// 1 GB of caches for four beams in 160 us (the measured copy rate; eight beams 209 us for 1.2 GB, sixteen 251 for 1.3), 512 blocks
+// of 32 KB in 16 caches in 90 us (91 %).
 #include <algorithm>
 #include <memory>
 #include <new>
