@@ -661,16 +661,19 @@ static int launch_beam(const BeamArgs& A, int batch, cudaStream_t st)
             raised[dev] = true;
         }
     }
-    // Few CTAs: a whole chunk per warp in flight, so that a short part needs one trip to memory and one threshold.
-    // More than one wave of four CTAs per SM: eight smaller ones, where they do not leave a larger part of their last wave empty
-    // or where there are more than two waves of them (a row's thresholds and its selection at the end leave gaps that seven
-    // other rows fill better than three: 1024 rows of 50257 fp32 65 -> 57 us, of 128256 110 -> 103, 4096 of 152064 bf16 316 -> 300;
-    // but 1200 rows of 128256, just over one wave of the small ones, 138 -> 152).  Their lists hold 4 A + 5 deviations up to 48 keys.
+    // More than one wave of four CTAs per SM: eight smaller ones (a row's thresholds and its selection at the end leave gaps that
+    // seven other rows fill better than three: 1024 rows of 50257 fp32 65 -> 57 us, of 128256 110 -> 103).  In fp32 where they do not
+    // leave a larger part of their last wave empty or where there are more than two waves of them (1200 rows of 128256, just over
+    // one wave, 138 -> 152); in bf16, which waits for instructions and not for bytes, always, and twelve per SM where that saves a
+    // quarter of the waves (1200 rows of 128256 84 us by four, 89 by eight, 77 by twelve; 2000 rows 120, 113, 123; 4096 of 152064 270,
+    // 253, 244).  The smaller ones' lists hold 4 A + 5 deviations up to 48 keys.
     const int ctas = batch * A.beams * A.parts;
     auto waves = [&](int per) { return (ctas + per * kSms - 1) / (per * kSms); };
-    const bool small = A.keep <= 48 && (ctas > 16 * kSms || (ctas > 4 * kSms && 2 * waves(8) <= waves(4)));
+    constexpr bool kNarrow = sizeof(T) == 2;
+    const bool small = A.keep <= 48 && ctas > 4 * kSms && (kNarrow || ctas > 16 * kSms || 2 * waves(8) <= waves(4));
     // Few CTAs: a whole chunk per warp in flight, so that a short part needs one trip to memory and one threshold.
     if (ctas <= 2 * kSms) launch_pdl(beam_stream_kernel<T, kChunk / (32 * VecTraits<T>::N), 256, 2>, ctas, 256, 0, st, A);
+    else if (small && kNarrow && 4 * waves(12) <= 3 * waves(8)) launch_pdl(beam_stream_kernel<T, 4, 128, kNarrow ? 12 : 8>, ctas, 128, 0, st, A);
     else if (small) launch_pdl(beam_stream_kernel<T, 4, 128, 8>, ctas, 128, 0, st, A);
     else launch_pdl(beam_stream_kernel<T, 4, 256, 4>, ctas, 256, 0, st, A);
     launch_pdl(beam_choose_kernel<T>, batch, kBeamThreads, smem, st, A);
