@@ -45,7 +45,8 @@ class Pair:
 
 
 @pytest.mark.parametrize("rows,beams,width,blocks,block", [(1, 1, 1, 1, 1), (5, 1, 4, 9, 3), (12, 4, 7, 40, 8), (64, 8, 33, 500, 16),
-                                                        (96, 32, 20, 900, 5), (1030, 1, 9, 4000, 7), (60, 12, 70, 1500, 4), (6, 2, 1, 3, 16)])
+                                                        (96, 32, 20, 900, 5), (1030, 1, 9, 4000, 7), (60, 12, 70, 1500, 4), (6, 2, 1, 3, 16),
+                                                        (1200, 4, 6, 5000, 8), (4, 2, 600, 2300, 2)])
 def test_runs_of_steps(rows, beams, width, blocks, block):
     rng = random.Random(rows * 31 + block)
     p = Pair(rows, width, blocks, block, beams)
@@ -143,3 +144,27 @@ def test_in_a_graph_with_padding():
         torch.cuda.synchronize()
         want = block_pool.plan(p.table, p.lengths, p.refs, 4, 1, a, 16)
         assert out.slots.tolist() == want[0] and t.table.tolist() == p.table and t.refs.tolist() == p.refs
+
+
+def test_lengths_as_what_is_kept():
+    """A step that only appends to what is there, told so by the lengths themselves; and two tables side by side on two streams."""
+    p = Pair(6, 5, 40, 4, 2)
+    p.step([3, 9, 0, 1, 5, 2], 20)
+    want = block_pool.plan(p.table, p.lengths, p.refs, 4, 2, [1] * 6, 6, list(p.lengths), [1, 1, 0, 0, 1, 0])
+    o = G.block_plan(p.t, dev([1] * 6), 6, keep=p.t.lengths, parents=dev([1, 1, 0, 0, 1, 0]))
+    torch.cuda.synchronize()
+    assert o.slots.tolist() == want[0] and p.t.lengths.tolist() == p.lengths and p.t.refs.tolist() == p.refs
+    a, b = Pair(300, 20, 3000, 8), Pair(300, 20, 3000, 8)
+    one, two = torch.cuda.Stream(), torch.cuda.Stream()
+    steps = [dev([(r * 7 + k) % 9 for r in range(300)]) for k in range(6)]
+    torch.cuda.synchronize()
+    outs = [None, None]
+    for k in range(6):
+        for i, (pair, stream) in enumerate(((a, one), (b, two))):
+            with torch.cuda.stream(stream):
+                outs[i] = G.block_plan(pair.t, steps[k], 2400, out=outs[i])
+    torch.cuda.synchronize()
+    for k in range(6):
+        want = block_pool.plan(a.table, a.lengths, a.refs, 8, 1, steps[k].tolist(), 2400)
+    for pair, out in ((a, outs[0]), (b, outs[1])):
+        assert out.slots.tolist() == want[0] and pair.t.table.tolist() == a.table and pair.t.refs.tolist() == a.refs
