@@ -275,6 +275,7 @@ plan_kernel(const __grid_constant__ PlanArgs A)
     // ---- A: what each row keeps and asks for.  Every CTA sums the rows' tokens for itself; a thread has neighbouring rows.
     const int per = div_up(R, kPlanThreads), lo = min(R, tid * per), hi = min(R, lo + per);
     long long total;
+    bool released = false;
     {
         if (kNear) for (int i = tid; i < hash_size; i += kPlanThreads) { h_best[i] = 0ull; h_block[i] = -1; h_count[i] = 0; }
         long long sum = 0;
@@ -299,14 +300,17 @@ plan_kernel(const __grid_constant__ PlanArgs A)
             q.first_token = (int)min(from, (long long)A.max_tokens);
             q.last = -1; q.need = 0; q.copies = 0; q.start = 0; q.pad = 0;
             row[r] = q;
+            released |= q.kept < q.before;
             if (r % ctas == me) A.offsets[r] = q.first_token;
         }
         if (me == 0 && tid == 0) A.offsets[R] = (int)min(total, (long long)A.max_tokens);
     }
-    if (kNear) __syncthreads(); else plan_barrier();
+    // (near: every CTA sees all rows, and whether any of them releases a block)
+    bool releases = true;
+    if (kNear) releases = __syncthreads_or(released) != 0; else plan_barrier();
 
     // ---- B: without parents a row only releases what it does not keep, mostly nothing (a warp per row)
-    if (!A.parents) {
+    if (!A.parents && releases) {
         for (int r = me + ctas * warp; r < R; r += ctas * kPlanWarps) {
             const int before = row[r].before;
             for (int c = row[r].kept + lane; c < before; c += 32) {
@@ -321,14 +325,26 @@ plan_kernel(const __grid_constant__ PlanArgs A)
     // ---- C: who writes to a shared block, what each row needs; how many blocks are free
     const int share = (div_up(N, ctas * kPlanThreads) + 3) & ~3;
     const long long b0 = ((long long)me * kPlanThreads + tid) * share;
+    // (a thread's first row: its last block's id is on the way while the counts are looked through)
+    auto writes_within = [&](const PlanRow& q) { return q.status == GR_OK && q.ask > 0 && q.base % bs != 0; };
+    int first_last = -1;
+    if (lo < hi && mine(lo)) {
+        const PlanRow q = row[lo];
+        if (writes_within(q)) first_last = table[(long long)lo * A.width + q.base / bs];
+    }
     int free_here = 0;
-    for (int i = 0; i < share; i += 4) free_here += __popc(free_of(refs, b0 + i, N, A.wide));
+    unsigned free_bits = 0;                                  // the first 32 of the thread's blocks
+    for (int i = 0; i < share; i += 4) {
+        const unsigned m = free_of(refs, b0 + i, N, A.wide);
+        free_here += __popc(m);
+        if (i < 32) free_bits |= m << i;
+    }
     for (int r = lo; r < hi; r++) {
         if (!mine(r)) continue;
         PlanRow q = row[r];
         if (A.parents) for (int y = 0; y < A.splits; y++) if (A.bad[(size_t)y * R + r]) q.status = GR_BAD_ROW;
-        if (q.status == GR_OK && q.ask > 0 && q.base % bs != 0) {
-            const int b = table[(long long)r * A.width + q.base / bs];
+        if (writes_within(q)) {
+            const int b = r == lo ? first_last : table[(long long)r * A.width + q.base / bs];
             if (b < 0 || b >= N) q.status = GR_BAD_ROW;
             else {
                 q.last = b;
@@ -394,7 +410,7 @@ plan_kernel(const __grid_constant__ PlanArgs A)
         long long k = ahead + free_before;
         const long long upto = min(needed, avail);
         for (int i = 0; i < share && free_here > 0 && k < upto; i += 4) {
-            for (unsigned m = free_of(refs, b0 + i, N, A.wide); m && k < upto; m &= m - 1) fresh[k++] = (int)(b0 + i) + __ffs(m) - 1;
+            for (unsigned m = i < 32 ? free_bits >> i & 15u : free_of(refs, b0 + i, N, A.wide); m && k < upto; m &= m - 1) fresh[k++] = (int)(b0 + i) + __ffs(m) - 1;
         }
     }
     plan_barrier();
