@@ -19,7 +19,7 @@
 // 64-bit scores.
 //
 // HBM bounds it in fp32 (128 groups of 8 rows of 128256: 93 us, 86 % of the measured copy rate), issue slots and the exponentials' pipe
-// in bf16 (256 groups of 16 rows of 152064: 254 us, 75 %), latency where there are few rows (4 of 32000: 11.4 us).
+// in bf16 (256 groups of 16 rows of 152064: 244 us, 78 %), latency where there are few rows (4 of 32000: 11.4 us).
 #include <limits.h>
 #include <math.h>
 #include "gr_host.h"

@@ -1,23 +1,26 @@
 // What models keep per hypothesis follows the hypotheses: gr_reorder_states (dense states, in place or into other
 // tensors) and gr_copy_blocks (blocks of a paged cache that two rows shared until one of them writes).  Both are bound by HBM:
-// 1 GB of caches for four beams in 160 us (the measured copy rate; eight beams 209 us for 1.2 GB, sixteen 251 for 1.3), 512 blocks
-// of 32 KB in 16 caches in 90 us (91 %).
+// 1 GB of caches for four beams in 160 us (the measured copy rate; sixteen beams 197 us for 1.2 GB, 252 where the states lie a power
+// of two apart), 512 blocks of 32 KB in 16 caches in 90 us (91 %).
 #include <algorithm>
 #include <memory>
 #include <new>
+#include <type_traits>
 #include "gr_host.h"
 
 namespace gr {
 
 constexpr int kStatesPerLaunch = 128;      // pointers that travel as kernel arguments
 constexpr int kCopyThreads = 256;
+static_assert(kCopyThreads == 1 << 8, "a team of all threads");
 constexpr int kCopyColumns = 4;            // vectors of a block per thread
+constexpr int kMostTeams = 16;             // teams of a CTA
 
 struct ReorderArgs {
     const char* src[kStatesPerLaunch];
     char* dst[kStatesPerLaunch];
     gr_state_layout at;
-    int in_place;
+    int in_place, team_shift;              // threads of a team: 1 << team_shift
 };
 
 // the first n bytes of a vector
@@ -100,20 +103,84 @@ reorder_kernel(const __grid_constant__ ReorderArgs A, const int* __restrict__ pa
     }
 }
 
+// The same for pieces that are short: a CTA takes several of them, a team of threads for each.  (A kernel of its own: strides that
+// are not constants cost odd widths 60 us for 43.)
+template <int W, typename Vec, int C>
+__global__ void __launch_bounds__(kCopyThreads)
+reorder_short_kernel(const __grid_constant__ ReorderArgs A, const int* __restrict__ parents, const int* __restrict__ lengths)
+{
+    constexpr int kVec = (int)sizeof(Vec);
+    __shared__ const char* s_from[kMostTeams][W];
+    __shared__ int s_left[kMostTeams][W];      // bytes that are copied from the team's first column on (0: none, or the state stays)
+    pdl_wait();
+    const gr_state_layout& L = A.at;
+    const int shift = A.team_shift;
+    const int tid = threadIdx.x, team = tid >> shift, at = tid & ((1 << shift) - 1);
+    const int teams = kCopyThreads >> shift, step = kVec << shift;
+    const int pieces = L.parts * L.batch, s = blockIdx.z;
+    const long long start = (long long)blockIdx.x * C * step;
+#pragma unroll 1
+    for (int piece0 = blockIdx.y * teams; piece0 < pieces; piece0 += gridDim.y * teams) {
+        bool any = false;
+        for (int e = tid; e < teams * W; e += kCopyThreads) {
+            const int t = e / W, j = e % W, piece = piece0 + t;
+            int left = 0;
+            const char* from = nullptr;
+            if (j < L.beams_out && piece < pieces) {
+                const int b = piece / L.parts, part = piece - b * L.parts;
+                const int p = __ldg(parents + (size_t)b * L.beams_out + j);
+                if (p >= 0 && p < L.beams_in && !(A.in_place && p == j)) {
+                    long long used = L.part_bytes;
+                    if (lengths) used = min(used, max(0, __ldg(lengths + (size_t)b * L.beams_in + p)) * L.token_bytes);
+                    left = (int)min(max(used - start, 0ll), 1ll << 30);
+                    from = A.src[s] + b * L.src_group + p * L.src_beam + part * L.src_part + start;
+                }
+            }
+            s_left[t][j] = left; s_from[t][j] = from;
+            any |= left > 0;
+        }
+        if (__syncthreads_or(any)) {
+            const int piece = piece0 + team, b = piece / L.parts, part = piece - b * L.parts;
+            char* dst = A.dst[s] + b * L.dst_group + part * L.dst_part + start + at * kVec;
+            Vec v[C][W];
+#pragma unroll
+            for (int j = 0; j < W; j++) {
+#pragma unroll
+                for (int c = 0; c < C; c++) {
+                    // (a vector that holds the last used byte is read whole: pieces are a multiple of kVec long)
+                    if (at * kVec + c * step < s_left[team][j]) v[c][j] = *reinterpret_cast<const Vec*>(s_from[team][j] + at * kVec + c * step);
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < W; j++) {
+#pragma unroll
+                for (int c = 0; c < C; c++) {
+                    const int more = s_left[team][j] - at * kVec - c * step;
+                    char* to = dst + j * L.dst_beam + c * step;
+                    if (more >= kVec) *reinterpret_cast<Vec*>(to) = v[c][j];
+                    else if (more > 0) store_bytes(to, v[c][j], more);
+                }
+            }
+        }
+        if (piece0 + (int)gridDim.y * teams < pieces) __syncthreads();
+    }
+}
+
 struct CopyArgs {
     char* cache[kStatesPerLaunch];
     const int* src; const int* dst;
     long long stride, bytes;
-    int num_blocks, pairs, chunks;
+    int num_blocks, pairs, chunks, team_shift;         // chunks of a block; threads of a team: 1 << team_shift
 };
 
 // Each CTA takes a segment of the pair list, keeps the pairs that copy something (in their order, which is then the same in
-// all CTAs of the segment), and takes its share of (pair, chunk) in one cache.
+// all CTAs of the segment), and takes its share of (pair, chunk) in one cache, a team of threads
+// for each (all threads, but for short blocks).
 template <typename Vec>
 __global__ void __launch_bounds__(kCopyThreads)
 copy_blocks_kernel(const __grid_constant__ CopyArgs A)
 {
-    constexpr int kVec = (int)sizeof(Vec), C = kCopyColumns, kStep = kCopyThreads * kVec;
+    constexpr int kVec = (int)sizeof(Vec), C = kCopyColumns;
     __shared__ int s_src[kCopyThreads], s_dst[kCopyThreads], s_warp[kCopyThreads / 32];
     pdl_wait();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -129,18 +196,19 @@ copy_blocks_kernel(const __grid_constant__ CopyArgs A)
     if (copies) { s_src[at] = from; s_dst[at] = to; }
     __syncthreads();
     char* cache = A.cache[blockIdx.z];
-    const int units = A.chunks * n;
+    const int units = A.chunks * n, team = tid >> A.team_shift, at_vec = tid & ((1 << A.team_shift) - 1);
+    const int teams = kCopyThreads >> A.team_shift, step = kVec << A.team_shift;
 #pragma unroll 1
-    for (int u = blockIdx.x; u < units; u += gridDim.x) {
+    for (int u = blockIdx.x * teams + team; u < units; u += gridDim.x * teams) {
         const int k = u / A.chunks;
-        const long long first = (long long)(u - k * A.chunks) * C * kStep + tid * kVec;
+        const long long first = (long long)(u - k * A.chunks) * C * step + at_vec * kVec;
         const char* in = cache + s_src[k] * A.stride + first;
         char* out = cache + s_dst[k] * A.stride + first;
         Vec v[C];
 #pragma unroll
-        for (int c = 0; c < C; c++) if (first + c * kStep < A.bytes) v[c] = *reinterpret_cast<const Vec*>(in + c * kStep);
+        for (int c = 0; c < C; c++) if (first + c * step < A.bytes) v[c] = *reinterpret_cast<const Vec*>(in + c * step);
 #pragma unroll
-        for (int c = 0; c < C; c++) if (first + c * kStep < A.bytes) *reinterpret_cast<Vec*>(out + c * kStep) = v[c];
+        for (int c = 0; c < C; c++) if (first + c * step < A.bytes) *reinterpret_cast<Vec*>(out + c * step) = v[c];
     }
 }
 
@@ -202,24 +270,31 @@ template <int W>
 static void launch_reorder(const ReorderArgs& A, int count, int vec, const int* parents, const int* lengths, cudaStream_t st)
 {
     const gr_state_layout& L = A.at;
-    auto go = [&](auto kernel, int bytes, int columns) {
-        const long long per = (long long)bytes * columns * kCopyThreads;
+    auto go = [&](auto whole, auto shorts, int bytes, int columns) {
+        ReorderArgs B = A;
+        B.team_shift = 8;
+        while (B.team_shift > 4 && L.part_bytes <= (long long)bytes * columns << (B.team_shift - 1)) B.team_shift--;
+        const long long per = (long long)bytes * columns << B.team_shift;
+        const int teams = kCopyThreads >> B.team_shift, rows = (L.parts * L.batch + teams - 1) / teams;
         cudaLaunchConfig_t cfg = {};
         cudaLaunchAttribute at = {};
         at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
         at.val.programmaticStreamSerializationAllowed = 1;
-        cfg.gridDim = dim3((unsigned)((L.part_bytes + per - 1) / per), (unsigned)std::min(L.parts * L.batch, 65535), (unsigned)count);
+        cfg.gridDim = dim3((unsigned)((L.part_bytes + per - 1) / per), (unsigned)std::min(rows, 65535), (unsigned)count);
         cfg.blockDim = dim3(kCopyThreads); cfg.stream = st; cfg.attrs = &at; cfg.numAttrs = 1;
-        cudaLaunchKernelEx(&cfg, kernel, A, parents, lengths);
+        cudaLaunchKernelEx(&cfg, teams > 1 ? shorts : whole, B, parents, lengths);
     };
-    // (narrow columns: several of them per thread, so that as many bytes are in flight)
-    constexpr int N4 = W <= 4 ? 8 : W <= 8 ? 4 : 2, kWide = 2;
+    // Columns of 16 bytes where they fit, two per thread up to four states (1 GB of caches 186 -> 157 us), of 8 bytes beyond 16 states,
+    // whose wider ones leave one CTA an SM its registers (20 states 55 -> 44 us, 31 168 -> 142).  Narrow columns: several of them
+    // per thread, so that as many bytes are in flight.
+    constexpr int N4 = W <= 4 ? 8 : W <= 8 ? 4 : 2, kWide = W <= 4 ? 2 : 1;
+    using Wide = std::conditional_t<(W <= 16), uint4, uint2>;
     switch (vec) {
-        case 16: go(reorder_kernel<W, uint4, W <= 4 ? kWide : 1>, 16, W <= 4 ? kWide : 1); break;
-        case 8: go(reorder_kernel<W, uint2, 2>, 8, 2); break;
-        case 4: go(reorder_kernel<W, unsigned, N4>, 4, N4); break;
-        case 2: go(reorder_kernel<W, unsigned short, N4>, 2, N4); break;
-        default: go(reorder_kernel<W, unsigned char, N4>, 1, N4); break;
+        case 16: go(reorder_kernel<W, Wide, kWide>, reorder_short_kernel<W, Wide, kWide>, (int)sizeof(Wide), kWide); break;
+        case 8: go(reorder_kernel<W, uint2, kWide>, reorder_short_kernel<W, uint2, kWide>, 8, kWide); break;
+        case 4: go(reorder_kernel<W, unsigned, N4>, reorder_short_kernel<W, unsigned, N4>, 4, N4); break;
+        case 2: go(reorder_kernel<W, unsigned short, N4>, reorder_short_kernel<W, unsigned short, N4>, 2, N4); break;
+        default: go(reorder_kernel<W, unsigned char, N4>, reorder_short_kernel<W, unsigned char, N4>, 1, N4); break;
     }
 }
 
@@ -288,7 +363,9 @@ int gr_copy_blocks(void* const* caches, int count, int num_blocks, long long blo
     for (int i = 0; i < count; i++) bits |= (unsigned long long)(uintptr_t)caches[i];
     const int vec = gr::vec_of(bits);
     const int segments = (int)(((long long)pairs + gr::kCopyThreads - 1) / gr::kCopyThreads);
-    const long long per = (long long)vec * gr::kCopyColumns * gr::kCopyThreads, chunks = (block_bytes + per - 1) / per;
+    int team_shift = 8;
+    while (team_shift > 5 && block_bytes <= (long long)vec * gr::kCopyColumns << (team_shift - 1)) team_shift--;
+    const long long per = (long long)vec * gr::kCopyColumns << team_shift, chunks = (block_bytes + per - 1) / per;
     if (segments > 65535 || chunks > (1 << 22)) return GR_E_TOO_LARGE;
     cudaStream_t st = (cudaStream_t)stream;
     gr::NvtxRange whole("gr_copy_blocks");
@@ -296,7 +373,7 @@ int gr_copy_blocks(void* const* caches, int count, int num_blocks, long long blo
         gr::CopyArgs A;
         A.src = copy_src; A.dst = copy_dst; A.stride = block_stride; A.bytes = block_bytes;
         A.num_blocks = num_blocks; A.pairs = pairs;
-        A.chunks = (int)chunks;
+        A.chunks = (int)chunks; A.team_shift = team_shift;
         const int n = std::min(count - lo, gr::kStatesPerLaunch);
         for (int i = 0; i < n; i++) A.cache[i] = (char*)caches[lo + i];
         const dim3 grid(std::max(1, 8 * gr::kSms / (segments * n)), segments, n);
