@@ -17,10 +17,9 @@ from typing import Optional, Tuple
 import torch
 
 try:
-    from ._tensors import alike as _alike      # (built beside the library; without it lists are looked at one by one)
+    from . import _tensors           # (built beside the library; without it every call goes the way below)
 except ImportError:
-    def _alike(tensors):
-        return None
+    _tensors = None
 
 GR_F32, GR_BF16 = 0, 1
 GR_OK, GR_NOT_CONVERGED, GR_SUPPORT_TOO_LARGE, GR_BAD_LOGITS, GR_DRAFT_OUT_OF_SUPPORT, GR_STALE_PARAMS = range(6)
@@ -33,6 +32,7 @@ GR_MAX_BEAMS, GR_MAX_SELECT = 32, 128
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_HERE, "libgr_b200.so")
 _lib = None
+_entry = {}                # addresses of entry points, for _tensors
 
 
 class GrError(RuntimeError):
@@ -106,6 +106,8 @@ def load_library():
     lib.gr_copy_blocks.argtypes = [vp, C.c_int, C.c_int, C.c_longlong, C.c_longlong, ip, ip, C.c_int, vp]
     lib.gr_strerror.restype = C.c_char_p
     lib.gr_strerror.argtypes = [C.c_int]
+    _entry.update({n: C.cast(getattr(lib, n), C.c_void_p).value
+                   for n in ("gr_beam_select", "gr_reorder_states", "gr_block_plan", "gr_copy_blocks")})
     _lib = lib
     return lib
 
@@ -479,6 +481,20 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
     lambda index: int(torch.cuda.current_stream(index).cuda_stream))
 
 
+def _short(way: str, name: str, *args):
+    """The call of entry point `name` by the short way, where that is open: True when it was made."""
+    if _tensors is None:
+        return False
+    if _lib is None:
+        load_library()
+    rc = getattr(_tensors, way)(_entry[name], *args)
+    if rc is None:
+        return False
+    if rc != 0:
+        _check(rc, name)
+    return True
+
+
 def _call(dev: torch.device, what: str, function, *args):
     """A C entry point with the tensors' device current and that device's current stream."""
     if torch.cuda.current_device() == dev.index:
@@ -512,6 +528,10 @@ def beam_select(logits: torch.Tensor, scores: torch.Tensor, select: Optional[int
     be read from by this call: scores, lengths and done are other tensors)."""
     if not (isinstance(logits, torch.Tensor) and logits.is_cuda and logits.dim() == 3):
         raise GrError("logits must be a [B, beams, V] CUDA tensor")
+    if (out is not None and out.shape == (*logits.shape, logits.shape[1] if select is None else select)
+            and _short("select", "gr_beam_select", logits, scores, out.shape[3], temperature, lengths, done, eos, length_penalty,
+                       out.workspace, out.token, out.parent, out.score, out.length, out.done, out.status)):
+        return out
     B, W, V = logits.shape
     dev, code = logits.device, _dtype_code(logits)
     step = logits.stride()
@@ -569,6 +589,8 @@ def reorder_states(states, parents: torch.Tensor, lengths: Optional[torch.Tensor
     parents [B, chosen] int32.  In place, with chosen <= beams, unless `out` (a list of tensors [B, chosen, ...]) is
     given, which must not meet the states in memory.  With lengths [B, beams] int32 the dimension `token_dim` of the
     states counts tokens, of which each parent's first lengths[b, parent] are copied.  Returns `out` or `states`."""
+    if _short("reorder", "gr_reorder_states", states, parents, lengths, -1 if token_dim is None else token_dim, out):
+        return states if out is None else out
     states = list(states)
     to = states if out is None else list(out)
     if len(to) != len(states):
@@ -606,21 +628,16 @@ def reorder_states(states, parents: torch.Tensor, lengths: Optional[torch.Tensor
                            step_y[0] * e if B > 1 else 0, step_y[1] * e if y.shape[1] > 1 else 0,
                            part_step_y, part, token)
 
-    at = _alike(states)
-    at_y = at if out is None or at is None else _alike(to)
-    if at_y is not None:
-        runs.append((layout_of(states[0], to[0]), at, at_y))
-    else:
-        last = None
-        for x, y in zip(states, to):
-            if not isinstance(x, torch.Tensor) or not isinstance(y, torch.Tensor):
-                raise GrError("states must be CUDA tensors [B, beams, ...] on the device of parents")
-            kind = (x.shape, x.stride(), x.dtype, x.device, y.shape, y.stride(), y.dtype, y.device)
-            if kind != last:
-                last = kind
-                runs.append((layout_of(x, y), [], []))
-            runs[-1][1].append(x.data_ptr())
-            runs[-1][2].append(y.data_ptr())
+    last = None
+    for x, y in zip(states, to):
+        if not isinstance(x, torch.Tensor) or not isinstance(y, torch.Tensor):
+            raise GrError("states must be CUDA tensors [B, beams, ...] on the device of parents")
+        kind = (x.shape, x.stride(), x.dtype, x.device, y.shape, y.stride(), y.dtype, y.device)
+        if kind != last:
+            last = kind
+            runs.append((layout_of(x, y), [], []))
+        runs[-1][1].append(x.data_ptr())
+        runs[-1][2].append(y.data_ptr())
     if len(runs) > 1:
         # (within a run the C call looks)
         first = [p for r in runs if r[0].part_bytes for p in r[2]]
@@ -668,6 +685,12 @@ def block_plan(tables: BlockTables, append: torch.Tensor, max_tokens: int, keep:
                parents: Optional[torch.Tensor] = None, out: Optional[BlockPlan] = None) -> BlockPlan:
     """gr_block_plan on torch CUDA tensors: `tables` is updated in place; append, keep [rows] int32, parents [rows] or
     [rows / beams, beams] int32 (row numbers within the group, as beam_select returns them)."""
+    if (out is not None and isinstance(tables.table, torch.Tensor) and isinstance(tables.refs, torch.Tensor)
+            and out.shape == (*tables.table.shape[:1], *tables.refs.shape, max_tokens)
+            and _short("plan", "gr_block_plan", tables.table, tables.lengths, tables.refs, tables.block_size, tables.beams, append,
+                       max_tokens, keep, parents, out.workspace, out.slots, out.positions, out.offsets, out.copy_src,
+                       out.copy_dst, out.status)):
+        return out
     if not isinstance(tables.table, torch.Tensor) or tables.table.dim() != 2:
         raise GrError("table must be a [rows, width] CUDA tensor of torch.int32")
     R, width = tables.table.shape
@@ -701,6 +724,8 @@ def block_plan(tables: BlockTables, append: torch.Tensor, max_tokens: int, keep:
 def copy_blocks(caches, copy_src: torch.Tensor, copy_dst: torch.Tensor) -> None:
     """gr_copy_blocks on torch CUDA tensors: `caches` is a list of tensors [num_blocks, ...] whose blocks are contiguous,
     copy_src and copy_dst [pairs] int32 as block_plan returns them."""
+    if _short("copy", "gr_copy_blocks", caches, copy_src, copy_dst):
+        return
     caches = list(caches)
     if not caches:
         return
@@ -722,19 +747,15 @@ def copy_blocks(caches, copy_src: torch.Tensor, copy_dst: torch.Tensor) -> None:
         e = x.element_size()
         return shape[0], (step[0] if shape[0] > 1 else per) * e, per * e
 
-    at = _alike(caches)
-    if at is not None:
-        runs.append(layout_of(caches[0]) + (at,))
-    else:
-        last = None
-        for x in caches:
-            if not isinstance(x, torch.Tensor):
-                raise GrError("caches must be CUDA tensors [num_blocks, ...] on the device of copy_src")
-            kind = (x.shape, x.stride(), x.dtype, x.device)
-            if kind != last:
-                last = kind
-                runs.append(layout_of(x) + ([],))
-            runs[-1][3].append(x.data_ptr())
+    last = None
+    for x in caches:
+        if not isinstance(x, torch.Tensor):
+            raise GrError("caches must be CUDA tensors [num_blocks, ...] on the device of copy_src")
+        kind = (x.shape, x.stride(), x.dtype, x.device)
+        if kind != last:
+            last = kind
+            runs.append(layout_of(x) + ([],))
+        runs[-1][3].append(x.data_ptr())
     if len(runs) > 1:
         first = [p for r in runs if r[2] for p in r[3]]
         if len(set(first)) < len(first):

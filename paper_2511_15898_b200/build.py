@@ -18,7 +18,7 @@ HEADERS = [os.path.join(CSRC, "gr_common.cuh"), os.path.join(CSRC, "gr_prep.cuh"
            os.path.join(ROOT, "include", "gr.h")]
 
 
-# the binding's view of lists of tensors: a Python module on torch's headers
+# the binding's short way for tensors: a Python module on torch's headers
 TENSORS_SOURCE = os.path.join(CSRC, "gr_tensors.cpp")
 TENSORS = os.path.join(HERE, "_tensors.so")
 
@@ -33,8 +33,8 @@ def _build_tensors(force: bool = False):
         return None
     lib = os.path.join(os.path.dirname(torch.__file__), "lib")
     cmd = (["g++", "-O2", "-std=c++17", "-shared", "-fPIC", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}"]
-           + [a for p in include_paths() + [sysconfig.get_paths()["include"]] for a in ("-isystem", p)]
-           + [TENSORS_SOURCE, "-L" + lib, "-ltorch_python", "-ltorch_cpu", "-lc10", "-Wl,-rpath," + lib, "-o", TENSORS])
+           + [a for p in include_paths() + [sysconfig.get_paths()["include"], os.path.join(_cuda_home(), "include")] for a in ("-isystem", p)]
+           + ["-I", os.path.join(ROOT, "include"), TENSORS_SOURCE, "-L" + lib, "-ltorch_python", "-ltorch_cpu", "-lc10_cuda", "-lc10", "-Wl,-rpath," + lib, "-o", TENSORS])
     return subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
 
 
@@ -43,6 +43,10 @@ def _nvcc() -> str:
         if cand and (os.path.sep not in cand or os.path.exists(cand)):
             return cand
     return "nvcc"
+
+
+def _cuda_home() -> str:
+    return os.path.dirname(os.path.dirname(_nvcc())) if os.path.sep in _nvcc() else "/usr/local/cuda"
 
 
 def needs_build(check: bool = False) -> bool:
