@@ -42,8 +42,8 @@ struct PlanArgs {
     long long* slots; int* positions; int* offsets; int* copy_src; int* copy_dst; int* status;
     PlanRow* row;
     unsigned long long* best; int* writers;     // per block: the writer with the most tokens in it; number of writers
-    int* fresh;                                  // the free blocks with the smallest ids, as many as are needed
-    int* part;                                   // free blocks by CTA
+    int* fresh;                                  // each CTA's free blocks, by id, from the number of its first block on
+    int* part;                                   // how many free blocks each CTA has
     unsigned char* bad;                          // per part of a group's columns and row: a held id outside the pool was met
     int rows, width, beams, block, num_blocks, max_tokens;
     int wide, split;                             // refs, slots and positions lie on 16 bytes; slots by a kernel of their own
@@ -185,14 +185,25 @@ fork_kernel(const __grid_constant__ PlanArgs A)
     if (tid < G) A.bad[(size_t)blockIdx.y * A.rows + r0 + tid] = (unsigned char)s_bad[tid];
 }
 
+// blocks that a CTA looks through
+__host__ __device__ inline int plan_share(int num_blocks) { return (div_up(num_blocks, kPlanCluster * kPlanThreads) + 3) & ~3; }
+// the k-th free block by id, out of the CTAs' lists
+__device__ __forceinline__ int fresh_at(GR_PTR(int) fresh, const int* count, int share, int k)
+{
+    long long from = 0;
+#pragma unroll 1
+    for (int i = 0; i < kPlanCluster - 1 && k >= count[i]; i++) { k -= count[i]; from += (long long)kPlanThreads * share; }
+    return fresh[from + k];
+}
+
 // a writer of a shared block that is about to be written to: by its tokens in the block, then the lowest row
 __device__ __forceinline__ unsigned long long writer_rank(int tokens, int r) { return ((unsigned long long)tokens << 32) | (0xffffffffu - (unsigned)r); }
 
 // Slots of the appended tokens, K neighbouring ones per thread (four where there are many: one search for the row, one store of
 // each kind for them).
-// `first(r)`: number of row r's first token; `at(r)`: the row.
-template <int K, class First, class Row>
-__device__ __forceinline__ void write_slots(const PlanArgs& A, GR_PTR(int) fresh, int total, long long thread, long long threads, First first, Row at)
+// `fresh(k)`: the k-th free block; `first(r)`: number of row r's first token; `at(r)`: the row.
+template <int K, class Block, class First, class Row>
+__device__ __forceinline__ void write_slots(const PlanArgs& A, Block fresh, int total, long long thread, long long threads, First first, Row at)
 {
     const int bs = A.block, R = A.rows;
     for (long long i0 = K * thread; i0 < A.max_tokens; i0 += K * threads) {
@@ -224,8 +235,8 @@ __device__ __forceinline__ void write_slots(const PlanArgs& A, GR_PTR(int) fresh
             else {
                 const int c = position[k] / bs;
                 within = position[k] - c * bs;
-                if (c >= q.kept) block = fresh[q.start + q.copies + c - q.kept];
-                else block = q.copies ? fresh[q.start] : q.last;
+                if (c >= q.kept) block = fresh(q.start + q.copies + c - q.kept);
+                else block = q.copies ? fresh(q.start) : q.last;
                 entered = true;
             }
             slot[k] = (long long)block * bs + within;
@@ -250,6 +261,7 @@ plan_kernel(const __grid_constant__ PlanArgs A)
 {
     extern __shared__ __align__(16) unsigned char s_dyn[];
     __shared__ long long s_part_raw[kPlanWarps + 1];
+    __shared__ int s_free[kPlanCluster];
     pdl_wait();
     GR_CHECK_FLAG_DECL;
     GR_CHECK_FLAG_INIT;
@@ -323,7 +335,7 @@ plan_kernel(const __grid_constant__ PlanArgs A)
     }
 
     // ---- C: who writes to a shared block, what each row needs; how many blocks are free
-    const int share = (div_up(N, ctas * kPlanThreads) + 3) & ~3;
+    const int share = plan_share(N);
     const long long b0 = ((long long)me * kPlanThreads + tid) * share;
     // (a thread's first row: its last block's id is on the way while the counts are looked through)
     auto writes_within = [&](const PlanRow& q) { return q.status == GR_OK && q.ask > 0 && q.base % bs != 0; };
@@ -387,17 +399,27 @@ plan_kernel(const __grid_constant__ PlanArgs A)
         sum += q.need;
         row[r] = q;
     }
-    // ---- D: the rows' places among the needed blocks; the free blocks by number
-    long long needed, place = 0;
+    // ---- D: the free blocks by id, each CTA its own (no more than are needed, where that is known); the rows' places among the
+    // needed blocks
+    long long needed = N, place = 0;
     if (kNear) place = cta_scan(sum, s_part, needed);
+    {
+        long long k = free_before;
+        const long long mine0 = (long long)me * kPlanThreads * share;
+        for (int i = 0; i < share && free_here > 0 && k < needed; i += 4) {
+            for (unsigned m = i < 32 ? free_bits >> i & 15u : free_of(refs, b0 + i, N, A.wide); m && k < needed; m &= m - 1) fresh[mine0 + k++] = (int)(b0 + i) + __ffs(m) - 1;
+        }
+    }
     plan_barrier();
+    if (tid < kPlanCluster) s_free[tid] = A.part[tid];
+    __syncthreads();
     if (!kNear) {
         sum = 0;
         for (int r = lo; r < hi; r++) sum += row[r].need;
         place = cta_scan(sum, s_part, needed);
     }
-    long long avail = 0, ahead = 0;
-    for (int i = 0; i < ctas; i++) { const int f = A.part[i]; if (i < me) ahead += f; avail += f; }
+    long long avail = 0;
+    for (int i = 0; i < kPlanCluster; i++) avail += s_free[i];
     for (int r = lo; r < hi; r++) {
         const int n = row[r].need;
         const long long from = place;
@@ -406,14 +428,9 @@ plan_kernel(const __grid_constant__ PlanArgs A)
         if (n > 0 && place > avail) { row[r].status = GR_NO_BLOCKS; row[r].ask = 0; row[r].copies = 0; row[r].start = 0; }
         else row[r].start = (int)from;
     }
-    {
-        long long k = ahead + free_before;
-        const long long upto = min(needed, avail);
-        for (int i = 0; i < share && free_here > 0 && k < upto; i += 4) {
-            for (unsigned m = i < 32 ? free_bits >> i & 15u : free_of(refs, b0 + i, N, A.wide); m && k < upto; m &= m - 1) fresh[k++] = (int)(b0 + i) + __ffs(m) - 1;
-        }
-    }
-    plan_barrier();
+    // (near: nothing that another CTA changes from here on is read again)
+    if (kNear) __syncthreads(); else plan_barrier();
+    auto block_at = [&](int k) { return fresh_at(fresh, s_free, share, k); };
 
     // ---- E: rows take their blocks, a warp for each; tokens get their slots
     for (int r = me + ctas * warp; r < R; r += ctas * kPlanWarps) {
@@ -421,14 +438,14 @@ plan_kernel(const __grid_constant__ PlanArgs A)
         const long long line = (long long)r * A.width;
         const int after = div_up(q.base + q.ask, bs);
         for (int c = q.kept + lane; c < after; c += 32) {
-            const int b = fresh[q.start + q.copies + c - q.kept];
+            const int b = block_at(q.start + q.copies + c - q.kept);
             table[line + c] = b;
             refs[b] = 1;
         }
         if (lane == 0) {
             int src = -1, dst = -1;
             if (q.copies) {
-                src = q.last; dst = fresh[q.start];
+                src = q.last; dst = block_at(q.start);
                 count_add(A.refs, N, src, -1);
                 refs[dst] = 1;
                 table[line + q.base / bs] = dst;
@@ -447,8 +464,8 @@ plan_kernel(const __grid_constant__ PlanArgs A)
         const long long thread = (long long)me + (long long)ctas * tid, threads = (long long)ctas * kPlanThreads;
         auto first = [&](int r) { return row[r].first_token; };
         auto at = [&](int r) { return (PlanRow)row[r]; };
-        if (A.max_tokens <= 2 * threads) write_slots<1>(A, fresh, end, thread, threads, first, at);
-        else write_slots<4>(A, fresh, end, thread, threads, first, at);
+        if (A.max_tokens <= 2 * threads) write_slots<1>(A, block_at, end, thread, threads, first, at);
+        else write_slots<4>(A, block_at, end, thread, threads, first, at);
     }
 }
 
@@ -456,15 +473,15 @@ plan_kernel(const __grid_constant__ PlanArgs A)
 __global__ void __launch_bounds__(kSlotThreads)
 slots_kernel(const __grid_constant__ PlanArgs A)
 {
-    __shared__ int s_first[kPlanNear];
+    __shared__ int s_first[kPlanNear], s_free[kPlanCluster];
     pdl_wait();
     const bool near = A.rows <= kPlanNear;
-    if (near) {
-        for (int r = threadIdx.x; r < A.rows; r += kSlotThreads) s_first[r] = A.row[r].first_token;
-        __syncthreads();
-    }
+    if (threadIdx.x < kPlanCluster) s_free[threadIdx.x] = A.part[threadIdx.x];
+    if (near) for (int r = threadIdx.x; r < A.rows; r += kSlotThreads) s_first[r] = A.row[r].first_token;
+    __syncthreads();
     GR_PTR(int) fresh = GR_MKPTR(int, A.fresh, A.num_blocks, nullptr);
-    write_slots<4>(A, fresh, A.offsets[A.rows], (long long)blockIdx.x * kSlotThreads + threadIdx.x, (long long)gridDim.x * kSlotThreads,
+    const int share = plan_share(A.num_blocks);
+    write_slots<4>(A, [&](int k) { return fresh_at(fresh, s_free, share, k); }, A.offsets[A.rows], (long long)blockIdx.x * kSlotThreads + threadIdx.x, (long long)gridDim.x * kSlotThreads,
                 [&](int r) { return near ? s_first[r] : A.row[r].first_token; }, [&](int r) { return A.row[r]; });
 }
 
