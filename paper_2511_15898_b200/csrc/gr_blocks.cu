@@ -4,9 +4,9 @@
 // write to it, how many blocks the rows before need, how many of the blocks before are free.  One cluster of CTAs goes through
 // the phases between those sums, separated by cluster barriers, instead of a chain of launches.  Around it two kernels for all
 // SMs, where there is work for them: tables that follow parents (before), and slot maps of many tokens (after).
-// Latency bounds all of it: 256 rows of a pool of 32768 blocks, a token each, 18 k cycles (9.9 us replayed; with 1024 threads per
-// CTA and rows in global memory between the phases 23.7), 48 prompts of 8000 tokens 14.1 (slots by the cluster alone: 56), 64 x 8
-// forked rows 16.8 (forked by the cluster: 24).
+// Latency bounds all of it: 256 rows of a pool of 32768 blocks, a token each, 17 k cycles (9.2 us replayed; with 1024 threads per
+// CTA and rows in global memory between the phases 23.7), 48 prompts of 8000 tokens 14.2 (slots by the cluster alone: 56), 64 x 8
+// forked rows 16.0 (forked by the cluster: 24).
 #include <limits.h>
 #include <algorithm>
 #include "gr_host.h"
