@@ -379,7 +379,7 @@ __device__ __noinline__ double row_lse(const T* x, int V, double temp, float kno
             const double p = z * fma(z, fma(z, fma(z, fma(z, c5, c4), c3), c2), c1);
             const double t = table[k & 63];
             const double f = __hiloint2double(__double2hiint(t) + ((k >> 6) << 20), __double2loint(t));
-            const double e = k > -64000 ? fma(f, p, f) : 0.0;
+            const double e = k > -64000 && v[u] > -INFINITY ? fma(f, p, f) : 0.0;
             if (u & 1) sum1 += e; else sum0 += e;
         }
     }
@@ -455,7 +455,6 @@ beam_choose_kernel(const __grid_constant__ BeamArgs A)
     }
     __syncthreads();
     // ---- rows
-    const double inv_temp = 1.0 / A.temp;
     if (tid < 32) {
         if (tid < W) {
             const int w = tid;
@@ -478,7 +477,7 @@ beam_choose_kernel(const __grid_constant__ BeamArgs A)
                 // to within a few units: in fp64.  (Not where every token is masked: nothing depends on that sum.)
                 float first = -INFINITY;
                 for (int l = w * P; l < (w + 1) * P; l++) if (g.count[l] > 0) first = fmaxf(first, fkey_inv((unsigned)(raw[l << shift] >> 32)));
-                g.peak[w] = fminf(1.f, __expf((float)((double)first * inv_temp - lse)));
+                g.peak[w] = fminf(1.f, __expf((float)((double)first / A.temp - lse)));
                 if (!(fabsf(top) <= kLargestRef) || !(sum < INFINITY)) g.again[w] = listed > 0 || sum != 0.0 ? 2 : 0;
             } else if (g.kind[w] == kRowDone) {
                 // a finished hypothesis has one continuation, in its first part's list
@@ -494,8 +493,10 @@ beam_choose_kernel(const __grid_constant__ BeamArgs A)
         if (tid == 0) g.slack = largest;
     }
     __syncthreads();
+    // (the quotient as in the sum's reference: with a product by 1 / T the largest logit's would be off it by a rounding, which for
+    // quotients of 10^16 and more is as large as any difference)
     auto total_of = [&](int w, unsigned long long k) {
-        return g.kind[w] == kRowDone ? g.score[w] : g.score[w] + ((double)fkey_inv((unsigned)(k >> 32)) * inv_temp - g.lse[w]);
+        return g.kind[w] == kRowDone ? g.score[w] : g.score[w] + ((double)fkey_inv((unsigned)(k >> 32)) / A.temp - g.lse[w]);
     };
     int M = 0;
 #pragma unroll 1

@@ -185,6 +185,21 @@ def test_large_offsets_and_spreads():
         check(G.beam_select(y, s, 9), reference(y, s, 9), 9, 7001)
 
 
+@pytest.mark.parametrize("T", [1e-30, 1e-3, 1e6, 1e37, 3e38])
+def test_extreme_temperatures_and_masks(T):
+    # (half of the tokens masked: a product with -infinity, or with a mask clamped to a number, must not count)
+    for dtype in (torch.float32, torch.bfloat16):
+        x, s, _ = make(3, 4, 3001, dtype, 15)
+        x[:, :, ::2] = -math.inf
+        x[1, 2] = -math.inf
+        x[2, 3, 1] = torch.finfo(dtype).max
+        check(G.beam_select(x, s, 9, T), reference(x, s, 9, T), 9, 3001)
+        # the same with rows whose sums are taken again
+        s[:] = -2.0
+        x[:, 1] = x[:, 0]
+        check(G.beam_select(x, s, 9, T), reference(x, s, 9, T), 9, 3001)
+
+
 def test_ascending_rows_and_long_lists():
     for dtype in (torch.float32, torch.bfloat16):
         x, s, _ = make(2, 3, 60001, dtype, 4)
