@@ -103,6 +103,24 @@ def test_numbers_of_rows(dtype, B, W, V, K):
     check(G.beam_select(x, s, K), reference(x, s, K), K, V)
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("B,W", [(700, 1), (160, 8), (40, 3)])
+def test_ties_masks_and_order_among_many_rows(dtype, B, W):
+    V, K = 6001, 12
+    x, s, g = make(B, W, V, dtype, B)
+    x[0] = 1.5                                             # nothing but ties
+    x[1, :, 9:] = torch.finfo(dtype).min                   # fewer tokens than are asked for beside the masked ones
+    x[2] = x[2].sort(dim=1).values
+    x[3, :, 5:] = -math.inf
+    x[4] = -math.inf
+    x[5, 0] = x[5, 0].sort(descending=True).values
+    x[6] = torch.round(x[6])                               # many ties at the border
+    s[7] = -math.inf
+    x[8, W - 1, V - 1] = math.nan
+    x[9, :, 1:4] = 40.0                                    # peaks
+    check(G.beam_select(x, s, K), reference(x, s, K), K, V)
+
+
 @pytest.mark.parametrize("T", [0.3, 0.7, 1.0, 2.5])
 def test_temperature_and_penalty(T):
     for penalty in (0.0, 0.6, 1.0, -0.5, 32.0):
