@@ -512,7 +512,7 @@ class Beams:
     token: torch.Tensor      # [B, select] int32
     parent: torch.Tensor     # [B, select] int32
     score: torch.Tensor      # [B, select] float32
-    length: torch.Tensor     # [B, select] int32 (zeros unless lengths were given)
+    length: torch.Tensor     # [B, select] int32 (written by calls with lengths; zeros before)
     done: torch.Tensor       # [B, select] bool
     status: torch.Tensor     # [B] int32
     workspace: torch.Tensor  # uint8, scratch

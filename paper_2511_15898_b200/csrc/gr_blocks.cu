@@ -174,7 +174,8 @@ fork_kernel(const __grid_constant__ PlanArgs A)
         for (int j = 0; j < W; j++) {
             if (j >= G) break;
             const bool held = c < s_row[j].before, holds = c < s_row[j].kept;
-            if (holds && (now[j] < 0 || now[j] >= N)) s_bad[j] = 1;
+            // (only of a row that goes on from another: how much of the others' is looked at depends on their neighbours)
+            if (holds && s_row[j].parent != r0 + j && (now[j] < 0 || now[j] >= N)) s_bad[j] = 1;
             if (held ? was[j] == now[j] : !holds) continue;
             if (held) count_add(A.refs, N, was[j], -1);
             if (holds) count_add(A.refs, N, now[j], 1);

@@ -111,6 +111,21 @@ def test_rows_that_cannot_be_served():
     assert t.refs.tolist() == [1, 1, 1, 1, 0, 0, 0, 0] and t.table[5].tolist() == [-1] * 4
 
 
+@pytest.mark.parametrize("others", [[1, 2, 3], [1, 3, 2]])
+def test_ids_outside_the_pool_where_rows_go_on_from_themselves(others):
+    # row 0 goes on from itself: whether its first block's id makes sense is not looked at, whatever its neighbours do
+    t = G.BlockTables.empty(4, 4, 16, 4, 4)
+    t.lengths.copy_(dev([8, 8, 8, 8]))
+    t.table[:, :2] = dev([[99, 0], [1, 2], [3, 4], [5, 6]])
+    t.refs[:7] = 1
+    o = G.block_plan(t, dev([1] * 4), 4, parents=dev([0] + others))
+    assert o.status.tolist() == [0] * 4
+    assert t.table[:, 2].tolist() == [7, 8, 9, 10] and t.table[0, :2].tolist() == [99, 0]
+    # a row that goes on from row 0 is refused
+    o = G.block_plan(t, dev([1] * 4), 4, parents=dev([0, 0, 2, 3]))
+    assert o.status.tolist() == [0, 10, 0, 0]
+
+
 def test_empty_and_large():
     t = G.BlockTables.empty(0, 4, 8, 4)
     o = G.block_plan(t, dev([]), 5)
