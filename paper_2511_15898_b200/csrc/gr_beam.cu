@@ -83,6 +83,113 @@ __device__ __forceinline__ void keep_keys(SS& sh, int listed, unsigned long long
     __syncthreads();
 }
 
+// push_vector; a list that is full puts the threshold out of reach, as what follows would wait for its counter in vain (128 groups of 8
+// rows of 128256 with one token unmasked 272 -> 251 us).  Decides nothing but that: the list is taken for over in any case.
+template <class SS>
+__device__ __forceinline__ void push_or_stop(SS& sh, const ulonglong2& v, int id) {
+    const int slot = atomicAdd(&sh.cnt, 1);
+    if (slot < SS::kList) {
+        GR_ARRAY_AS(ulonglong2, sh.keys, slot) = v;
+        GR_ARRAY_AS(int, sh.keys, 4 * SS::kList + slot) = id;
+    } else *((volatile float*)&sh.tau) = INFINITY;
+}
+
+// Where the list did not hold what passed: mostly ties, of a value that masks tokens or of few values in all.  The K-th largest
+// of the threads' largest logits, to the last bit, is a value t that K elements reach.  What is above it is listed in one more
+// pass, and what holds t as long as that is not much; else the places that are left go to the first ids that hold t, looked for from
+// the first of them on.  The number of keys in sh.keys, or -1 where the elements above t are too many (then few threads met them all).
+// (By radix passes alone those rows 1791 us, rows of whole numbers 1305 for 188, in bf16 1174 for 143.)
+template <typename T, class SS>
+__device__ __noinline__ int tied_select(SS& sh, const T* x, int V, int head, int nch, int first, int stride, int K, float largest)
+{
+    using VT = VecTraits<T>;
+    constexpr int N = VT::N, S = kChunk / (32 * N), U = S < 4 ? S : 4, kWarps = SS::kThr / 32;
+    constexpr int kAbove = SS::kCap / 2, kTies = SS::kCap / 4, kAhead = 4;
+    static_assert(S % U == 0 && kTies >= GR_MAX_SELECT, "keys");
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int vec_end = head + ((V - head) / N) * N;
+    const unsigned mine = fkey(largest);
+    unsigned t = 0;
+#pragma unroll 1
+    for (unsigned bit = 1u << 31; bit; bit >>= 1) if (__syncthreads_count(mine >= (t | bit)) >= K) t |= bit;
+    if (tid == 0) { sh.kept = 0; sh.cnt = 0; sh.need = V; }
+    __syncthreads();
+    int id = V;                                            // the first that holds t
+    auto look = [&](float v, int i) {
+        const unsigned k = fkey(v);
+        if (k > t) {
+            const int slot = atomicAdd(&sh.kept, 1);
+            if (slot < kAbove) sh.keys[slot] = ckey(v, i);
+        } else if (k == t) {
+            id = min(id, i);
+            if (*((volatile int*)&sh.cnt) <= kTies) {
+                const int slot = atomicAdd(&sh.cnt, 1);
+                if (slot < kTies) sh.keys[kAbove + slot] = ckey(v, i);
+            }
+        }
+    };
+#pragma unroll 1
+    for (int c = first + warp; c < nch; c += stride) {
+        if (c == 0 && lane < head) look(load_logit<T>(x, lane), lane);
+        if (c == nch - 1 && vec_end + lane < V) look(load_logit<T>(x, vec_end + lane), vec_end + lane);
+#pragma unroll 1
+        for (int u0 = 0; u0 < S; u0 += U) {
+            const int base = head + c * kChunk + (u0 * 32 + lane) * N;
+            ulonglong2 v[U];
+#pragma unroll
+            for (int u = 0; u < U; u++) if (base + u * 32 * N + N <= vec_end) v[u] = ldg_stream(x + base + u * 32 * N);
+#pragma unroll
+            for (int u = 0; u < U; u++) {
+                if (base + u * 32 * N + N > vec_end || fkey(VT::largest(v[u])) < t) continue;
+#pragma unroll
+                for (int i = 0; i < N; i++) look(VT::element(v[u], i), base + u * 32 * N + i);
+            }
+        }
+    }
+    id = __reduce_min_sync(0xffffffffu, id);
+    if (lane == 0) atomicMin(&sh.need, id);
+    __syncthreads();
+    int have = sh.kept;
+    const int from = sh.need, ties = sh.cnt;
+    if (have > kAbove) return -1;
+    if (have >= K || t <= fkey(-INFINITY)) return have;    // (masked tokens are no continuations)
+    if (ties <= kTies) {
+        // (they move to places at or before their own: a round's are read before any of them is written)
+#pragma unroll 1
+        for (int e0 = 0; e0 < ties; e0 += SS::kThr) {
+            const int e = e0 + tid;
+            const unsigned long long k = e < ties ? sh.keys[kAbove + e] : 0ull;
+            __syncthreads();
+            if (e < ties) sh.keys[have + e] = k;
+            __syncthreads();
+        }
+        return have + ties;
+    }
+#pragma unroll 1
+    for (int c = first; c < nch && have < K; c += stride) {
+        const int end = chunk_end(min(c + kWarps, nch) - 1, head, nch, V);
+#pragma unroll 1
+        for (int i0 = max(chunk_begin(c, head), from); i0 < end && have < K; i0 += kAhead * SS::kThr) {
+            float v[kAhead];
+#pragma unroll
+            for (int u = 0; u < kAhead; u++) v[u] = i0 + u * SS::kThr + tid < end ? load_logit<T>(x, i0 + u * SS::kThr + tid) : NAN;
+#pragma unroll
+            for (int u = 0; u < kAhead; u++) {
+                if (have >= K) break;
+                const bool holds = v[u] == v[u] && fkey(v[u]) == t;
+                const unsigned mask = __ballot_sync(0xffffffffu, holds);
+                if (lane == 0) sh.hist[warp] = __popc(mask);
+                __syncthreads();
+                int at = have + __popc(mask & ((1u << lane) - 1u));
+                for (int w = 0; w < kWarps; w++) { const int n = sh.hist[w]; if (w < warp) at += n; have += n; }
+                if (holds && at < K) sh.keys[at] = ckey(v[u], i0 + u * SS::kThr + tid);
+                __syncthreads();
+            }
+        }
+    }
+    return min(have, K);                                   // (of the last round's ties those that were listed)
+}
+
 template <typename T, int U, int NTHR, int CTAS>
 __global__ void __launch_bounds__(NTHR, CTAS)
 beam_stream_kernel(const __grid_constant__ BeamArgs A)
@@ -202,7 +309,7 @@ beam_stream_kernel(const __grid_constant__ BeamArgs A)
                     acc += (double)(f_lo(sum2) + f_hi(sum2));
                     if (most >= tau) {
 #pragma unroll
-                        for (int u = 0; u < U; u++) if (each[u] >= tau) push_vector(sh, v[u], base + u * 32 * N);
+                        for (int u = 0; u < U; u++) if (each[u] >= tau) push_or_stop(sh, v[u], base + u * 32 * N);
                     }
                 };
                 if (whole) batch(std::true_type());
@@ -215,7 +322,7 @@ beam_stream_kernel(const __grid_constant__ BeamArgs A)
                     if (cvalid) {
 #pragma unroll
                         for (int u = 0; u < U; u++) {
-                            if ((whole || base + u * 32 * N + N <= vec_end) && VT::largest(v[u]) >= t1) push_vector(sh, v[u], base + u * 32 * N);
+                            if ((whole || base + u * 32 * N + N <= vec_end) && VT::largest(v[u]) >= t1) push_or_stop(sh, v[u], base + u * 32 * N);
                         }
                     }
                 }
@@ -281,6 +388,11 @@ beam_stream_kernel(const __grid_constant__ BeamArgs A)
     }
     if (over) {
         __syncthreads();
+        M = tied_select<T>(sh, x, V, head, nch, first, stride, K, g0);
+        over = M < 0;
+    }
+    if (over) {
+        __syncthreads();
         exact_select_slow<T>(sh, x, V, head, nch, first, stride, K);
         // (masked tokens come last in that order; they are not continuations)
         const unsigned long long masked = ((unsigned long long)fkey(-INFINITY) << 32) | 0xffffffffull;
@@ -319,7 +431,6 @@ struct BeamGroup {
     float peak[GR_MAX_BEAMS];                  // probability of the row's first token
     unsigned long long least;                  // a bound below the last key that is taken (as an integer that orders like it)
     double slack;                              // the largest distance of keys at which sums are taken again
-    double best_key[GR_MAX_SELECT + 1];
     int best_at[GR_MAX_SELECT + 1];
 };
 constexpr int kRowNone = 0, kRowDone = 1, kRowLive = 2;
@@ -580,22 +691,27 @@ beam_choose_kernel(const __grid_constant__ BeamArgs A)
             }
             __syncwarp();
             for (int o = 1; o < team; o <<= 1) rank += __shfl_xor_sync(0xffffffffu, rank, o);
-            if (a < M && (tid & (team - 1)) == 0 && rank <= K) { g.best_key[rank] = unsortable(mine); g.best_at[rank] = a; }
+            if (a < M && (tid & (team - 1)) == 0 && rank <= K) g.best_at[rank] = a;
         }
         __syncthreads();
-        // ---- continuations of different rows that lie too close for the streamed sums
-        auto close = [&](int e, int f, double apart) {
+        // ---- continuations of different rows that lie too close for the streamed sums: neighbours, and those near the last one.  (A
+        // token masked by a value like -1e30 has its quotient as total, whatever the sum: less than a quarter of a unit in its last
+        // place is added to it.)
+        const int pairs = min(M, K + 1) - 1;
+#pragma unroll 1
+        for (int i = tid; i < (M > K ? pairs + M : pairs); i += kBeamThreads) {
+            const int e = i < pairs ? g.best_at[i] : i - pairs, f = g.best_at[i < pairs ? i + 1 : K - 1];
             const int w = sv_row[e], v = sv_row[f];
-            if (w == v) return;
+            if (w == v) continue;
             const double near_w = g.inv_scale[w] * (kNear + kNearPeak * (double)g.peak[w]), near_v = g.inv_scale[v] * (kNear + kNearPeak * (double)g.peak[v]);
-            if (fabs(apart) > fmax(near_w, near_v)) return;
-            if (g.kind[w] == kRowLive && !g.exact[w]) { g.again[w] = 1; g.redo = 1; }
-            if (g.kind[v] == kRowLive && !g.exact[v]) { g.again[v] = 1; g.redo = 1; }
-        };
-        for (int i = tid; i + 1 < min(M, K + 1); i += kBeamThreads) close(g.best_at[i], g.best_at[i + 1], g.best_key[i] - g.best_key[i + 1]);
-        if (M > K) {
-            const double last = g.best_key[K - 1];
-            for (int a = tid; a < M; a += kBeamThreads) close(a, g.best_at[K - 1], unsortable(sv[a].x) - last);
+            if (fabs(unsortable(sv[e].x) - unsortable(sv[f].x)) > fmax(near_w, near_v)) continue;
+#pragma unroll 1
+            for (int side = 0; side < 2; side++) {
+                const int at = side ? f : e, row = side ? v : w;
+                const double x = (double)fkey_inv((unsigned)(sv[at].y >> 32)) / A.temp;
+                if (g.kind[row] != kRowLive || g.exact[row] || fabs(x) > 72057594037927936.0 * (1.0 + fabs(g.lse[row]) + fabs(g.score[row]))) continue;  // 2^56
+                g.again[row] = 1; g.redo = 1;
+            }
         }
         __syncthreads();
         if (!g.redo) break;

@@ -121,6 +121,36 @@ def test_ties_masks_and_order_among_many_rows(dtype, B, W):
     check(G.beam_select(x, s, K), reference(x, s, K), K, V)
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("B,W,V,K,ld", [(1, 1, 40000, 8, 40000), (3, 2, 20011, 40, 20013), (700, 1, 9001, 5, 9001), (2, 4, 70001, 128, 70002)])
+def test_more_ties_than_are_listed(dtype, B, W, V, K, ld):
+    low = torch.finfo(dtype).min
+    g = torch.Generator(device="cuda").manual_seed(V)
+    x = torch.randn(B * W, ld, device="cuda", generator=g).to(dtype)[:, :V]
+    r = 0
+
+    def row():
+        nonlocal r
+        r += 1
+        return x[(r - 1) % (B * W)]
+
+    row()[K - 2:] = low                                    # fewer unmasked tokens than are asked for: the first masked ones follow
+    y = row(); y[:V - 3] = low                             # ... at the end of the row
+    y = row(); y[:] = -10000.5; y[V // 2] = 1.0            # another value than the type's lowest
+    y = row(); y[:] = -math.inf; y[V // 3:] = -1e9; y[V - 1] = 2.0
+    y = row(); y[:] = 0.0; y[1::2] = -0.0                  # the two zeros are one value
+    y = row(); y[:] = torch.round(y * 0.5)                 # few values in all
+    # a few threads meet all that is above the others' values (vectors that lie a warp apart)
+    n = 4 if dtype == torch.float32 else 8
+    y = row(); y[:] = 0.0
+    for i in range(n):
+        z = y[i::32 * n]
+        z.copy_(torch.randn(z.shape, device="cuda", generator=g).abs() + 1)
+    s = torch.zeros(B, W, device="cuda")
+    full = torch.as_strided(x, (B, W, V), (W * ld, ld, 1))
+    check(G.beam_select(full, s, K), reference(full, s, K), K, V)
+
+
 @pytest.mark.parametrize("T", [0.3, 0.7, 1.0, 2.5])
 def test_temperature_and_penalty(T):
     for penalty in (0.0, 0.6, 1.0, -0.5, 32.0):
