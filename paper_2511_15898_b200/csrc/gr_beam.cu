@@ -18,8 +18,8 @@
 // continuations lie closer than kNear + kNearPeak p the rows' sums are taken again in fp64, so that the order is that of the
 // 64-bit scores.
 //
-// HBM bounds it in fp32 (128 groups of 8 rows of 128256: 93 us, 86 % of the measured copy rate), issue slots and the exponentials' pipe
-// in bf16 (256 groups of 16 rows of 152064: 244 us, 78 %), latency where there are few rows (4 of 32000: 11.4 us).
+// HBM bounds it in fp32 (128 groups of 8 rows of 128256: 93 us, 87 % of the measured copy rate), issue slots and the exponentials' pipe
+// in bf16 (256 groups of 16 rows of 152064: 244 us, 79 %), latency where there are few rows (4 of 32000: 11.4 us).
 #include <limits.h>
 #include <math.h>
 #include "gr_host.h"

@@ -1,7 +1,7 @@
 // What models keep per hypothesis follows the hypotheses: gr_reorder_states (dense states, in place or into other
 // tensors) and gr_copy_blocks (blocks of a paged cache that two rows shared until one of them writes).  Both are bound by HBM:
 // 1 GB of caches for four beams in 160 us (the measured copy rate; sixteen beams 197 us for 1.2 GB, 252 where the states lie a power
-// of two apart), 512 blocks of 32 KB in 16 caches in 90 us (91 %).
+// of two apart), 512 blocks of 32 KB in 16 caches in 90 us (92 %).
 #include <algorithm>
 #include <memory>
 #include <new>
