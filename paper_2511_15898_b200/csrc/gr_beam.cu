@@ -417,7 +417,7 @@ beam_stream_kernel(const __grid_constant__ BeamArgs A)
 // ---------------------------------------------------------------- the group's choice
 
 struct BeamGroup {
-    double lse[GR_MAX_BEAMS], inv_scale[GR_MAX_BEAMS], score[GR_MAX_BEAMS];
+    double lse[GR_MAX_BEAMS], scale[GR_MAX_BEAMS], score[GR_MAX_BEAMS];
     double red[kBeamWarps], table[64];
     double part_sum[kBeamMaxLists];
     float part_ref[kBeamMaxLists];
@@ -505,6 +505,18 @@ __device__ __noinline__ double row_lse(const T* x, int V, double temp, float kno
     return top / temp + m_log(all);
 }
 
+// n^a, a >= 0: products for whole numbers a, with a square root for half ones, so that equal keys come out equal (pow is off by a
+// unit in the last place in one of twenty cases, at a = 1 too)
+__device__ __noinline__ double length_power(int n, double a)
+{
+    const double twice = 2.0 * a;
+    if (twice != floor(twice) || twice > 64.0) return pow((double)n, a);
+    double r = 1.0, base = (double)n;
+    const int k = (int)twice;
+    for (int e = k >> 1; e; e >>= 1, base *= base) if (e & 1) r *= base;
+    return k & 1 ? r * sqrt((double)n) : r;
+}
+
 // order-preserving map double -> integer (integers compare faster), and back; the two zeros get one key
 __device__ __forceinline__ unsigned long long sortable(double v) {
     const unsigned long long u = (unsigned long long)__double_as_longlong(v + 0.0);
@@ -554,6 +566,11 @@ beam_choose_kernel(const __grid_constant__ BeamArgs A)
         if (i < keep) raw[e] = reinterpret_cast<const unsigned long long*>(recs + (size_t)l * stride + sizeof(BeamPart))[i];
     }
     static_assert(GR_MAX_BEAMS <= 32, "a lane of the first warp for each row");
+    // (a quotient, as the key is defined: by a product with 1 / L^a the keys -49 / 49 and -1 / 1 would differ)
+    auto key_of = [&](int w, double total) {
+        if (A.penalty == 0.0) return total;
+        return A.penalty > 0.0 ? total / g.scale[w] : fmax(total * g.scale[w], -1.7976931348623157e308);
+    };
     float score = -INFINITY;
     bool fin = false;
     if (tid < W) {
@@ -561,7 +578,7 @@ beam_choose_kernel(const __grid_constant__ BeamArgs A)
         const int n = A.lengths ? A.lengths[b * W + tid] : 0;
         fin = A.done && A.done[b * W + tid];
         g.length[tid] = max(1, fin ? n : (n < INT_MAX ? n + 1 : n));
-        g.inv_scale[tid] = A.penalty != 0.0 ? 1.0 / pow((double)g.length[tid], A.penalty) : 1.0;
+        g.scale[tid] = A.penalty != 0.0 ? length_power(g.length[tid], fabs(A.penalty)) : 1.0;
         if (!(score < INFINITY)) g.bad = 1;
     }
     __syncthreads();
@@ -598,7 +615,7 @@ beam_choose_kernel(const __grid_constant__ BeamArgs A)
             g.lse[w] = lse;
             if (g.again[w]) g.redo = 1;
         }
-        double largest = tid < W ? g.inv_scale[tid] * (kNear + kNearPeak * (double)g.peak[tid]) : 0.0;
+        double largest = tid < W ? key_of(tid, kNear + kNearPeak * (double)g.peak[tid]) : 0.0;
 #pragma unroll 1
         for (int o = 16; o > 0; o >>= 1) largest = fmax(largest, __shfl_xor_sync(0xffffffffu, largest, o));
         if (tid == 0) g.slack = largest;
@@ -636,7 +653,7 @@ beam_choose_kernel(const __grid_constant__ BeamArgs A)
         // smallest power of two that leaves at most half of the lists above it
         for (int e = tid; e < most; e += kBeamThreads) {
             const int l = e >> shift, i = e & ((1 << shift) - 1), w = g.row[l];
-            key[e] = i < g.count[l] ? total_of(w, raw[e]) * g.inv_scale[w] : -INFINITY;
+            key[e] = i < g.count[l] ? key_of(w, total_of(w, raw[e])) : -INFINITY;
         }
         // (few lists: every power of two, and the largest of the bounds)
         int lg0 = 0;
@@ -703,7 +720,7 @@ beam_choose_kernel(const __grid_constant__ BeamArgs A)
             const int e = i < pairs ? g.best_at[i] : i - pairs, f = g.best_at[i < pairs ? i + 1 : K - 1];
             const int w = sv_row[e], v = sv_row[f];
             if (w == v) continue;
-            const double near_w = g.inv_scale[w] * (kNear + kNearPeak * (double)g.peak[w]), near_v = g.inv_scale[v] * (kNear + kNearPeak * (double)g.peak[v]);
+            const double near_w = key_of(w, kNear + kNearPeak * (double)g.peak[w]), near_v = key_of(v, kNear + kNearPeak * (double)g.peak[v]);
             if (fabs(unsortable(sv[e].x) - unsortable(sv[f].x)) > fmax(near_w, near_v)) continue;
 #pragma unroll 1
             for (int side = 0; side < 2; side++) {
