@@ -1,27 +1,36 @@
 // gr_beam_select: the best continuations of groups of hypotheses.
 //
-// Two kernels.  The first streams the logit rows once, every row in one or several parts of a CTA each: a part leaves its
+// The first kernel streams the logit rows once, every row in one or several parts of a CTA each: a part leaves its
 // `select` largest logits in descending order and the sum of its exponentials.  The second, a CTA per group, puts the sums
-// together, turns the listed logits into scores and ranks them.
+// together, turns the listed logits into scores and ranks them.  Groups in which two continuations lie too close for the sums are
+// left to a third, a cluster of CTAs per group, that takes sums again in 64 bits (few groups: it makes the choice of all).
 //
 // The sum.  With s = log2(e) / T split into two fp32 numbers (s_hi + s_lo, both positive) an element contributes
 // 2^(x s - R), R a whole number near x s of the largest element met: two FMAs and one ex2 an element, no
 // systematic error from the rounding of s (which alone costs 4e-7 of a log-sum over 10^5 ids), exact factors between sums of
 // different R, fp32 sums over one batch of vectors, fp64 from there on.  R is one for a warp and follows the maximum only where
 // that is kRise above it (more would cost accuracy: the products' rounding grows with the distance from R).  An element that is -infinity gives 0; NaN and
-// +infinity make the sum NaN, as does a maximum whose product with s overflows: such rows' sums are taken again in fp64 by the
-// second kernel, which tells the two apart.
+// +infinity make the sum NaN, as does a maximum whose product with s overflows: such rows' sums are taken again in fp64, where the
+// two are told apart.
 //
-// The order.  Within a row it is that of the logits.  Between rows scores are compared in fp64.  Two rows' streamed sums are off
-// from one another by up to 1.2e-7 + 7e-7 p in the logarithm, p the larger probability of a first token of the two (measured on 100 kinds of
-// rows: ex2 and the products round each element by a part in 10^7 and more, which a sum of many averages out); where two
-// continuations lie closer than kNear + kNearPeak p the rows' sums are taken again in fp64, so that the order is that of the
-// 64-bit scores.
+// The order.  Within a row it is that of the logits.  Between rows scores are compared in fp64, and where two continuations lie
+// closer than the bounds of their rows' errors the sums are taken again in fp64, so that the order is that of the 64-bit scores.
+// (Neighbours in the order are looked at, and what lies near the last that is taken: were any two in the wrong order, two neighbours
+// would be, of different rows.)  The bound of a streamed log-sum, with Z = sum 2^(x s - R) and p the elements' shares of it:
+//   ex2          1.46e-7, the largest relative error over all arguments from -126 to 2 (documented: 2^-22)
+//   fp32 sums    of 8 or 16 terms by vectors, and of the pair's two: 7 roundings of 2^-24 at most
+//   exponents    two roundings, of the distance y from R: half a unit in its last place is 2^-24 max(|y|, 1) at most, so
+//                2 ln 2 2^-24 E max(|y|, 1) in all, E the mean under p.  The shares' entropy, E log2(1 / p) = log2 Z + E(-y), is
+//                largest where all but the first token are alike: with p1 the first's share and q = 1 - p1 the others',
+//                E max(|y|, 1) <= p1 + q (log2(V / q) - log2 Z + 2)   (y <= 1, and R only rises).
+//   s            known to 2^-48 of itself: 2^-46 |R|.
+// Together 1e-6 to 2e-6 a row (measured on rows of one value, of two, of whole numbers and of normal ones: 5.5e-7 at most).
 //
 // HBM bounds it in fp32 (128 groups of 8 rows of 128256: 93 us, 87 % of the measured copy rate), issue slots and the exponentials' pipe
 // in bf16 (256 groups of 16 rows of 152064: 244 us, 79 %), latency where there are few rows (4 of 32000: 11.4 us).
 #include <limits.h>
 #include <math.h>
+#include <algorithm>
 #include "gr_host.h"
 #include "gr_scan.cuh"
 
@@ -33,8 +42,9 @@ constexpr int kBeamMaxParts = 16;
 constexpr int kBeamMaxLists = 256;             // rows of a group times parts
 constexpr int kBeamMaxListed = 4096;           // entries of a group's lists
 static_assert(GR_MAX_BEAMS * GR_MAX_SELECT <= kBeamMaxListed && GR_MAX_SELECT <= kMaxSupport, "lists");
-constexpr double kNear = 2e-7, kNearPeak = 1e-6;
-constexpr float kLargestRef = 16777216.f;
+constexpr double kErrSum = 1.46e-7 + 7.0 / 16777216, kErrDepth = 0.69314718055994530942 / 8388608, kErrRef = 1.0 / (1ll << 46);
+constexpr float kLargestRef = 1048576.f;       // (products of s_lo stay below 1/8, and R + kRise is a number)
+constexpr int kSettle = 8;                     // most CTAs of a cluster that takes sums again
 constexpr float kRise = 1.f;
 
 // what a part leaves: this, then its keys (ckey) in descending order
@@ -54,7 +64,7 @@ struct BeamArgs {
     int V, beams, select, keep, parts, eos;        // keep: keys per part
     float s_hi, s_lo;
     double temp, penalty;
-    char* ws;
+    char* ws; int* flags; int batch, team;         // flags: groups that are left to be settled; team: CTAs of a cluster for each
     int* out_token; int* out_parent; float* out_score; int* out_length; unsigned char* out_done; int* status;
 };
 
@@ -296,17 +306,24 @@ beam_stream_kernel(const __grid_constant__ BeamArgs A)
                     // (an element that is -infinity gives 0 whatever the reference, as long as that is finite)
                     const float down = ref == -INFINITY ? 0.f : -ref;
                     const unsigned long long down2 = f_pack(down, down);
-                    unsigned long long sum2 = 0ull;
+                    // (a vector's sum, then those of the vectors, in fp32 by halves: equal terms one after another in one sum would
+                    // round the same way each time.  By halves in bf16 too: 259 -> 271 us for 256 groups of 16 rows of 152064, by its registers)
+                    unsigned long long sum2[U];
 #pragma unroll
                     for (int u = 0; u < U; u++) {
 #pragma unroll
                         for (int i = 0; i < VT::kPairs; i++) {
                             const unsigned long long w = VT::pair(v[u], i);
                             const unsigned long long y = fma2(w, lo2, fma2(w, hi2, down2));
-                            sum2 = add2(sum2, f_pack(ex2(f_lo(y)), ex2(f_hi(y))));
+                            const unsigned long long e = f_pack(ex2(f_lo(y)), ex2(f_hi(y)));
+                            sum2[u] = i == 0 ? e : add2(sum2[u], e);
                         }
+                        if (VT::kPairs == 2) {
+#pragma unroll
+                            for (int k = 1; (u & k) && k < U; k *= 2) sum2[u] = add2(sum2[u - k], sum2[u]);
+                        } else if (u > 0) sum2[u] = add2(sum2[u - 1], sum2[u]);
                     }
-                    acc += (double)(f_lo(sum2) + f_hi(sum2));
+                    acc += (double)(f_lo(sum2[U - 1]) + f_hi(sum2[U - 1]));
                     if (most >= tau) {
 #pragma unroll
                         for (int u = 0; u < U; u++) if (each[u] >= tau) push_or_stop(sh, v[u], base + u * 32 * N);
@@ -428,39 +445,61 @@ struct BeamGroup {
     unsigned char again[GR_MAX_BEAMS];         // the row's sum is to be taken again (2: it was of no use)
     unsigned char exact[GR_MAX_BEAMS];         // ... and has been
     int bad, check, survivors, redo;
-    float peak[GR_MAX_BEAMS];                  // probability of the row's first token
+    double err[GR_MAX_BEAMS];                  // bound of the error of the row's log-sum
     unsigned long long least;                  // a bound below the last key that is taken (as an integer that orders like it)
     double slack;                              // the largest distance of keys at which sums are taken again
     int best_at[GR_MAX_SELECT + 1];
+    double share[2][kSettle];                  // what the cluster's CTAs tell one another
 };
 constexpr int kRowNone = 0, kRowDone = 1, kRowLive = 2;
 
-// log sum exp(x / T) of a row in fp64, the same for every thread; -infinity for a row that is masked as a whole; `bad` set for
-// one with a NaN or +infinity.  `top`: its largest logit where that is known (then there is no NaN in it), else NaN.  (Every
-// thread takes the elements of its index modulo the CTA's size, so that equal rows give equal sums wherever they lie.)
-// exp(-d) = 2^-n 2^(j / 64) exp(-r) by a table and five terms, |r| <= ln 2 / 128: a row of 152064 in 60 us, for 100 by exp_neg.
+// What every CTA of the cluster has to tell (the same `mine` in all of its threads), in all of them.  (Two sets of places, used in
+// turn: a CTA writes to one of them again only after all have read it, as they come to the barrier between.)
+__device__ __forceinline__ void cluster_meet() {
+    asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
+}
+__device__ __forceinline__ const double* cluster_share(BeamGroup& g, int& turn, int team, double mine)
+{
+    double* place = g.share[turn++ & 1];
+    if ((int)threadIdx.x < team) {
+        unsigned at = (unsigned)__cvta_generic_to_shared(place + blockIdx.x % team);
+        asm volatile("mapa.shared::cluster.u32 %0, %0, %1;" : "+r"(at) : "r"((unsigned)threadIdx.x));
+        asm volatile("st.shared::cluster.f64 [%0], %1;" :: "r"(at), "d"(mine) : "memory");
+    }
+    cluster_meet();
+    return place;
+}
+
+// log sum exp(x / T) of a row in fp64 by the CTAs of a cluster, the same for every thread of all of them; -infinity for a row that is
+// masked as a whole; `bad` set for one with a NaN or +infinity.  `known`: its largest logit where that is known (then there is no NaN in
+// it), else NaN.  (Every thread takes the elements of its index modulo the cluster's size, so that equal rows give equal sums wherever they lie.)
+// exp(-d) = 2^-n 2^(j / 64) exp(-r) by a table and five terms, |r| <= ln 2 / 128: a row of 152064 in 60 us by one CTA, for 100 by exp_neg, and in
+// 10 by a cluster of eight.
 template <typename T>
-__device__ __noinline__ double row_lse(const T* x, int V, double temp, float known, const double* table, double* red, int* bad)
+__device__ __noinline__ double row_lse(BeamGroup& g, int& turn, int team, const T* x, int V, double temp, float known)
 {
     constexpr int kAhead = 16;
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, first = (int)(blockIdx.x % team) * kBeamThreads + tid, step = team * kBeamThreads;
+    double* red = g.red;
     double top = (double)known;
     if (known != known) {
         float m = -INFINITY;
         int wrong = 0;
-        for (int i = tid; i < V; i += kBeamThreads) {
+        for (int i = first; i < V; i += step) {
             const float v = load_logit<T>(x, i);
             if (!(v < INFINITY)) wrong = 1;
             m = fmaxf(m, v);
         }
-        wrong = __syncthreads_or(wrong);
-        if (wrong) { if (tid == 0) *bad = 1; return 0.0; }
+        if (wrong) m = INFINITY;
         m = warp_max(m);
         if (lane == 0) red[warp] = (double)m;
         __syncthreads();
         top = red[0];
         for (int w = 1; w < kBeamWarps; w++) top = fmax(top, red[w]);
+        const double* all = cluster_share(g, turn, team, top);
+        for (int c = 0; c < team; c++) top = fmax(top, all[c]);
         __syncthreads();
+        if (top == INFINITY) { if (tid == 0) g.bad = 1; return 0.0; }
     }
     if (top == -INFINITY) return -INFINITY;
     // (kAhead elements at a time, without a branch between them: an element is a chain of twelve dependent operations.  Whole
@@ -471,13 +510,13 @@ __device__ __noinline__ double row_lse(const T* x, int V, double temp, float kno
     double sum0 = 0.0, sum1 = 0.0;
     float next[kAhead];
 #pragma unroll
-    for (int u = 0; u < kAhead; u++) next[u] = tid + u * kBeamThreads < V ? load_logit<T>(x, tid + u * kBeamThreads) : -INFINITY;
+    for (int u = 0; u < kAhead; u++) next[u] = first + u * step < V ? load_logit<T>(x, first + u * step) : -INFINITY;
 #pragma unroll 1
-    for (int i0 = tid; i0 < V; i0 += kAhead * kBeamThreads) {
+    for (int i0 = first; i0 < V; i0 += kAhead * step) {
         float v[kAhead];
 #pragma unroll
         for (int u = 0; u < kAhead; u++) {
-            const int i = i0 + (kAhead + u) * kBeamThreads;
+            const int i = i0 + (kAhead + u) * step;
             v[u] = next[u];
             next[u] = i < V ? load_logit<T>(x, i) : -INFINITY;
         }
@@ -488,7 +527,7 @@ __device__ __noinline__ double row_lse(const T* x, int V, double temp, float kno
             const int k = __double2loint(whole);
             const double z = y - (whole - magic);
             const double p = z * fma(z, fma(z, fma(z, fma(z, c5, c4), c3), c2), c1);
-            const double t = table[k & 63];
+            const double t = g.table[k & 63];
             const double f = __hiloint2double(__double2hiint(t) + ((k >> 6) << 20), __double2loint(t));
             const double e = k > -64000 && v[u] > -INFINITY ? fma(f, p, f) : 0.0;
             if (u & 1) sum1 += e; else sum0 += e;
@@ -499,10 +538,12 @@ __device__ __noinline__ double row_lse(const T* x, int V, double temp, float kno
     for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
     if (lane == 0) red[warp] = sum;
     __syncthreads();
-    double all = 0.0;
-    for (int w = 0; w < kBeamWarps; w++) all += red[w];
+    double mine = 0.0, sum_all = 0.0;
+    for (int w = 0; w < kBeamWarps; w++) mine += red[w];
+    const double* all = cluster_share(g, turn, team, mine);
+    for (int c = 0; c < team; c++) sum_all += all[c];
     __syncthreads();
-    return top / temp + m_log(all);
+    return top / temp + m_log(sum_all);
 }
 
 // n^a, a >= 0: products for whole numbers a, with a square root for half ones, so that equal keys come out equal (pow is off by a
@@ -530,20 +571,16 @@ __device__ __forceinline__ double unsortable(unsigned long long k) {
 __host__ __device__ inline int list_shift(int keep) { int s = 0; while ((1 << s) < keep) s++; return s; }
 __host__ __device__ inline size_t choose_bytes(int lists, int keep) { return ((size_t)lists << list_shift(keep)) * 36; }
 
-// One CTA per group.  (What it costs is latency: it runs once, mostly with its instructions not yet fetched.  So no integer
-// division in the loops, and the survivors next to one another: with indices to follow and lists to divide out, ranking 71 of
-// them took 13 us, now 1.)
-template <typename T>
-__global__ void __launch_bounds__(kBeamThreads, 3)
-beam_choose_kernel(const __grid_constant__ BeamArgs A)
+// One CTA per group, or (kSettles) a cluster: then all of its CTAs make the same choice, take sums again together where that is needed,
+// and the first one writes what comes out.  A CTA alone leaves such a group to be settled.  (What it costs is latency: it runs once,
+// mostly with its instructions not yet fetched.  So no integer division in the loops, and the survivors next to one another: with
+// indices to follow and lists to divide out, ranking 71 of them took 13 us, now 1.)
+template <typename T, bool kSettles>
+__device__ __forceinline__ void choose(const BeamArgs& A, BeamGroup& g, unsigned char* s_dyn, long long b, int& turn)
 {
-    extern __shared__ __align__(16) unsigned char s_dyn[];
-    __shared__ BeamGroup g;
-    pdl_wait();
     GR_CHECK_FLAG_DECL;
     GR_CHECK_FLAG_INIT;
     const int tid = threadIdx.x;
-    const long long b = blockIdx.x;
     const int W = A.beams, P = A.parts, K = A.select, keep = A.keep, lists = W * P, shift = list_shift(keep), most = lists << shift;
     GR_PTR(double) key = GR_MKPTR(double, reinterpret_cast<double*>(s_dyn), most, GR_CHECK_FLAG);
     GR_PTR(unsigned long long) raw = GR_MKPTR(unsigned long long, reinterpret_cast<unsigned long long*>(s_dyn) + most, most, GR_CHECK_FLAG);
@@ -588,7 +625,7 @@ beam_choose_kernel(const __grid_constant__ BeamArgs A)
             const int w = tid;
             g.score[w] = (double)score;
             g.kind[w] = score == -INFINITY ? kRowNone : fin ? kRowDone : kRowLive;
-            g.again[w] = 0; g.exact[w] = 0; g.peak[w] = 0.f;
+            g.again[w] = 0; g.exact[w] = 0; g.err[w] = 0.0;
             double lse = 0.0;
             if (g.kind[w] == kRowLive) {
                 float top = -INFINITY;
@@ -600,13 +637,19 @@ beam_choose_kernel(const __grid_constant__ BeamArgs A)
                     if (v != 0.0) sum += g.part_ref[l] == top ? v : times_pow2(v, g.part_ref[l] - top);
                     listed += g.count[l];
                 }
-                lse = ((double)top + log2(sum)) * 0.69314718055994530942;
+                const double units = log2(sum);
+                lse = ((double)top + units) * 0.69314718055994530942;
                 // NaN, an infinity, or logits so large that R, an fp32 number, is not the whole number near their product with s
                 // to within a few units: in fp64.  (Not where every token is masked: nothing depends on that sum.)
                 float first = -INFINITY;
                 for (int l = w * P; l < (w + 1) * P; l++) if (g.count[l] > 0) first = fmaxf(first, fkey_inv((unsigned)(raw[l << shift] >> 32)));
-                g.peak[w] = fminf(1.f, __expf((float)((double)first / A.temp - lse)));
                 if (!(fabsf(top) <= kLargestRef) || !(sum < INFINITY)) g.again[w] = listed > 0 || sum != 0.0 ? 2 : 0;
+                else if (listed > 0) {
+                    // (the shares to 1e-5 on the side of the larger bound; two units in ten for the products of s_lo)
+                    const float p = fminf(1.f, __expf((float)((double)first / A.temp - lse))), q = fminf(1.f, 1.f - p + 1e-5f);
+                    const float depth = 1.2f + q * (log2f((float)A.V / q) - (float)units + 2.f);
+                    g.err[w] = kErrSum + kErrDepth * (double)depth + kErrRef * fabs((double)top);
+                }
             } else if (g.kind[w] == kRowDone) {
                 // a finished hypothesis has one continuation, in its first part's list
                 g.count[w * P] = 1;
@@ -615,7 +658,7 @@ beam_choose_kernel(const __grid_constant__ BeamArgs A)
             g.lse[w] = lse;
             if (g.again[w]) g.redo = 1;
         }
-        double largest = tid < W ? key_of(tid, kNear + kNearPeak * (double)g.peak[tid]) : 0.0;
+        double largest = tid < W ? 2.0 * key_of(tid, g.err[tid]) : 0.0;
 #pragma unroll 1
         for (int o = 16; o > 0; o >>= 1) largest = fmax(largest, __shfl_xor_sync(0xffffffffu, largest, o));
         if (tid == 0) g.slack = largest;
@@ -630,7 +673,9 @@ beam_choose_kernel(const __grid_constant__ BeamArgs A)
 #pragma unroll 1
     while (true) {
         // ---- sums that are to be taken again
-        if (g.redo) {
+        if (!kSettles && g.redo) break;
+        if (kSettles && g.redo) {
+            cluster_meet();                                // (the others have begun)
             if (tid < 64) g.table[tid] = exp2((double)tid * (1.0 / 64.0));
             __syncthreads();
 #pragma unroll 1
@@ -640,9 +685,9 @@ beam_choose_kernel(const __grid_constant__ BeamArgs A)
                 float known = -INFINITY;
                 for (int l = w * P; l < (w + 1) * P; l++) if (g.count[l] > 0) known = fmaxf(known, fkey_inv((unsigned)(raw[l << shift] >> 32)));
                 if (g.again[w] == 2) known = __int_as_float(0x7fc00000);
-                const double lse = row_lse<T>((const T*)A.logits + (b * W + w) * A.ld, A.V, A.temp, known, g.table, g.red, &g.bad);
+                const double lse = row_lse<T>(g, turn, A.team, (const T*)A.logits + (b * W + w) * A.ld, A.V, A.temp, known);
                 __syncthreads();
-                if (tid == 0) { g.lse[w] = lse; g.again[w] = 0; g.exact[w] = 1; }
+                if (tid == 0) { g.lse[w] = lse; g.err[w] = 0.0; g.again[w] = 0; g.exact[w] = 1; }
                 __syncthreads();
             }
         }
@@ -675,7 +720,7 @@ beam_choose_kernel(const __grid_constant__ BeamArgs A)
             if (rank == place - 1) atomicMax(&g.least, sortable(mine));
         }
         __syncthreads();
-        // (those within kNear below the bound too: they may have to be told from the last ones)
+        // (those a little below the bound too: they may have to be told from the last ones)
         const double least = unsortable(g.least) - g.slack;
         for (int e = tid; e < most; e += kBeamThreads) {
             const int l = e >> shift;
@@ -720,8 +765,7 @@ beam_choose_kernel(const __grid_constant__ BeamArgs A)
             const int e = i < pairs ? g.best_at[i] : i - pairs, f = g.best_at[i < pairs ? i + 1 : K - 1];
             const int w = sv_row[e], v = sv_row[f];
             if (w == v) continue;
-            const double near_w = key_of(w, kNear + kNearPeak * (double)g.peak[w]), near_v = key_of(v, kNear + kNearPeak * (double)g.peak[v]);
-            if (fabs(unsortable(sv[e].x) - unsortable(sv[f].x)) > fmax(near_w, near_v)) continue;
+            if (fabs(unsortable(sv[e].x) - unsortable(sv[f].x)) > key_of(w, g.err[w]) + key_of(v, g.err[v])) continue;
 #pragma unroll 1
             for (int side = 0; side < 2; side++) {
                 const int at = side ? f : e, row = side ? v : w;
@@ -734,6 +778,9 @@ beam_choose_kernel(const __grid_constant__ BeamArgs A)
         if (!g.redo) break;
     }
     // ---- results
+    const bool left = !kSettles && g.redo && !g.bad;
+    if (!kSettles && tid == 0) A.flags[b] = left ? 1 : 0;
+    if (left || (kSettles && blockIdx.x % A.team != 0)) return;
     const bool bad = g.bad != 0;
     for (int i = tid; i < K; i += kBeamThreads) {
         const size_t at = (size_t)b * K + i;
@@ -756,6 +803,46 @@ beam_choose_kernel(const __grid_constant__ BeamArgs A)
 #ifdef GR_CHECK
         if (GR_CHECK_VALUE) A.status[b] = GR_CHECK_FAILED;
 #endif
+    }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kBeamThreads, 3)
+beam_choose_kernel(const __grid_constant__ BeamArgs A)
+{
+    extern __shared__ __align__(16) unsigned char s_dyn[];
+    __shared__ BeamGroup g;
+    pdl_wait();
+    int turn = 0;
+    choose<T, false>(A, g, s_dyn, blockIdx.x, turn);
+}
+
+// The groups that the choice has left (all, where there are no flags), a cluster for each in turn.
+template <typename T>
+__global__ void __launch_bounds__(kBeamThreads, 2)
+beam_settle_kernel(const __grid_constant__ BeamArgs A)
+{
+    extern __shared__ __align__(16) unsigned char s_dyn[];
+    __shared__ BeamGroup g;
+    __shared__ unsigned s_left[kBeamWarps];
+    pdl_wait();
+    int turn = 0;
+    const int tid = threadIdx.x, clusters = gridDim.x / A.team;
+#pragma unroll 1
+    for (long long b0 = blockIdx.x / A.team; b0 < A.batch; b0 += (long long)clusters * kBeamThreads) {
+        const long long b = b0 + (long long)tid * clusters;
+        const unsigned left = __ballot_sync(0xffffffffu, b < A.batch && (!A.flags || A.flags[b]));
+        if ((tid & 31) == 0) s_left[tid >> 5] = left;
+        __syncthreads();
+#pragma unroll 1
+        for (int w = 0; w < kBeamWarps; w++) {
+#pragma unroll 1
+            for (unsigned more = s_left[w]; more; more &= more - 1) {
+                choose<T, true>(A, g, s_dyn, b0 + (long long)(32 * w + __ffs(more) - 1) * clusters, turn);
+                __syncthreads();
+            }
+        }
+        __syncthreads();
     }
 }
 
@@ -784,11 +871,12 @@ static int launch_beam(const BeamArgs& A, int batch, cudaStream_t st)
 {
     const int smem = (int)choose_bytes(A.beams * A.parts, A.keep);
     static bool raised[kMaxDevices] = {false};
-    if (smem > 32 * 1024) {
+    if (smem > 24 * 1024) {
         int dev = -1;
         if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) { cudaGetLastError(); return GR_E_LAUNCH; }
         if (!raised[dev]) {
-            if (cudaFuncSetAttribute(beam_choose_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, 36 * kBeamMaxListed) != cudaSuccess) {
+            if (cudaFuncSetAttribute(beam_choose_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, 36 * kBeamMaxListed) != cudaSuccess
+                || cudaFuncSetAttribute(beam_settle_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, 36 * kBeamMaxListed) != cudaSuccess) {
                 cudaGetLastError();
                 return GR_E_LAUNCH;
             }
@@ -810,7 +898,21 @@ static int launch_beam(const BeamArgs& A, int batch, cudaStream_t st)
     else if (small && kNarrow && 4 * waves(12) <= 3 * waves(8)) launch_pdl(beam_stream_kernel<T, 4, 128, kNarrow ? 12 : 8>, ctas, 128, 0, st, A);
     else if (small) launch_pdl(beam_stream_kernel<T, 4, 128, 8>, ctas, 128, 0, st, A);
     else launch_pdl(beam_stream_kernel<T, 4, 256, 4>, ctas, 256, 0, st, A);
-    launch_pdl(beam_choose_kernel<T>, batch, kBeamThreads, smem, st, A);
+    // Few groups: a cluster chooses for each at once, of as many CTAs as leave every group's an SM.  Else a CTA for each, and then
+    // clusters for what these leave (74 groups of 4 rows of 32000: 19.7 us by clusters of two, 20.6 by a CTA each and a second
+    // launch).  A CTA of theirs to an SM: with two the launch takes 0.7 us longer where no group is left, and where all are 3.5 ms for
+    // 3.9 (256 groups of 16 equal rows of 152064).
+    BeamArgs B = A;
+    B.team = kSettle;
+    while (B.team > 2 && batch * B.team > kSms) B.team /= 2;
+    if (batch * B.team <= kSms) {
+        B.flags = nullptr;
+        launch_pdl_cluster(B.team, beam_settle_kernel<T>, batch * B.team, kBeamThreads, smem, st, B);
+    } else {
+        B.team = kSettle;
+        launch_pdl(beam_choose_kernel<T>, batch, kBeamThreads, smem, st, B);
+        launch_pdl_cluster(kSettle, beam_settle_kernel<T>, std::min(batch, kSms / kSettle) * kSettle, kBeamThreads, smem, st, B);
+    }
     return GR_OK;
 }
 
@@ -822,7 +924,7 @@ size_t gr_beam_workspace_bytes(int V, int beams, int select, int batch)
 {
     if (!gr::beam_shape_ok(V, beams, select, batch)) return 0;
     const int keep = select < V ? select : V, rows = (batch > 0 ? batch : 1) * beams;
-    return (size_t)rows * gr::beam_parts(V, rows, beams, keep) * gr::beam_stride(keep);
+    return (size_t)rows * gr::beam_parts(V, rows, beams, keep) * gr::beam_stride(keep) + 4 * (((size_t)batch + 3) & ~(size_t)3);
 }
 
 int gr_beam_select(const void* logits, int dtype, int V, long long ld, int beams, int batch, float temperature,
@@ -848,7 +950,8 @@ int gr_beam_select(const void* logits, int dtype, int V, long long ld, int beams
     A.s_hi = nextafterf((float)s, 0.f);
     if ((double)A.s_hi >= s) A.s_hi = nextafterf(A.s_hi, 0.f);
     A.s_lo = (float)(s - (double)A.s_hi);
-    A.ws = (char*)workspace;
+    A.ws = (char*)workspace; A.batch = batch;
+    A.flags = (int*)(A.ws + (size_t)(batch * beams) * A.parts * gr::beam_stride(A.keep));
     A.out_token = out_token; A.out_parent = out_parent; A.out_score = out_score; A.out_length = out_length;
     A.out_done = out_done; A.status = status;
     gr::NvtxRange whole("gr_beam_select");

@@ -1,4 +1,6 @@
-"""The order between hypotheses whose keys are equal or nearly so."""
+"""The order between hypotheses whose keys are equal or nearly so: on rows whose streamed sums err most and each in its own way
+(rows of one value or of two, where every element has the same error), next to one another at a distance of a few units of a score."""
+import math
 
 import pytest
 import torch
@@ -37,3 +39,115 @@ def test_equal_quotients_are_equal_keys(penalty):
     torch.cuda.synchronize()
     assert torch.equal(r.parent.cpu(), torch.arange(W, dtype=torch.int32).expand(B, W))
     check(r, reference(x, s, W, 1.0, n, done, 2, penalty), W, V, n)
+
+
+def near_scores(x, T, g):
+    """Scores that bring the best continuations of a group's rows within a few units in the last place of one another."""
+    B, W, _ = x.shape
+    s = torch.empty(B, W, dtype=torch.float32)
+    for b in range(B):
+        y = x[b].double().cpu() / T
+        best = y.amax(1) - torch.logsumexp(y, 1)
+        t = float(best.min()) - 0.0625
+        for w in range(W):
+            near = torch.tensor(t - float(best[w]), dtype=torch.float32)
+            unit = float(torch.nextafter(near, torch.tensor(math.inf))) - float(near)
+            s[b, w] = float(near) + unit * int(torch.randint(-3, 4, (1,), generator=g))
+    return s.cuda()
+
+
+def check_order(r, x, s, K, T=1.0, lengths=None, done=None, eos=-1, penalty=0.0):
+    """The K largest keys in descending order, each row's tokens in the order of the logits.  Two orders of a pair count where its
+    keys are one number but for the roundings of 64-bit arithmetic, which rows of one value shifted against one another make happen:
+    x / T, score and log-sum are each rounded a few times (of 2^-53 of themselves), the sum of exponentials by its additions in halves
+    and by its terms (each off by its exponent's rounding); 32 units of the largest of them together bound both sides."""
+    torch.cuda.synchronize()
+    B, W, V = x.shape
+    y = x.double() / T
+    total = s.double().unsqueeze(2) + (y - torch.logsumexp(y, 2, keepdim=True))
+    length = (lengths.double() + 1 if lengths is not None else torch.ones(B, W, device="cuda", dtype=torch.float64))
+    if done is not None:
+        total[done] = -math.inf
+        total[done, eos] = s[done].double()
+        length = length - done.double()
+    key = total / (length.clamp(min=1) ** float(torch.tensor(penalty, dtype=torch.float32))).unsqueeze(2)
+    tol = 32 * 2.0 ** -53 * (float(y.abs().max()) + float(s.abs().max()) + math.log2(V))
+    assert tol < 1e-11                                    # (the keys differ by units of fp32 scores, 1e-9 and more, or not at all)
+    at = r.parent.long() * V + r.token.long()
+    assert r.status.tolist() == [G.GR_OK] * B and int(r.parent.min()) >= 0
+    flat = key.view(B, -1)
+    got = flat.gather(1, at)
+    assert bool((got[:, 1:] <= got[:, :-1] + tol).all())
+    others = flat.scatter(1, at, -math.inf).amax(1)
+    assert bool((others <= got[:, -1] + tol).all())
+    # of each row the tokens that the logits' order begins with
+    order = x.sort(dim=2, descending=True, stable=True).indices[:, :, :K]
+    for b in range(B):
+        parents, tokens = r.parent[b].tolist(), r.token[b].tolist()
+        for w in set(parents):
+            mine = [t for p, t in zip(parents, tokens) if p == w]
+            assert mine == ([eos] if done is not None and bool(done[b, w]) else order[b, w, :len(mine)].tolist())
+
+
+def test_two_plateaus():
+    V = 131072
+    x = torch.empty(1, 2, V, device="cuda")
+    x[0, 0], x[0, 1] = -8.875, -11.625
+    x[:, :, ::512] = 0.0
+    s = torch.tensor([[-0.0625, -0.12696360051631927]], device="cuda")
+    want = reference(x, s, 16)
+    assert want[0][3].tolist() == [0] * 16                # (ahead by 8.5e-8)
+    check(G.beam_select(x, s, 16), want, 16, V)
+
+
+# (few CTAs, one wave, several waves of the smaller CTAs)
+SHAPES = [(1, 4, 131072), (3, 8, 20011), (40, 4, 30001), (40, 32, 2053), (330, 8, 4099)]
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("B,W,V", SHAPES)
+def test_rows_of_two_values(dtype, B, W, V):
+    g = torch.Generator().manual_seed(V + B)
+    x = torch.empty(B, W, V)
+    for b in range(B):
+        for w in range(W):
+            x[b, w] = -16.0 * float(torch.rand(1, generator=g))
+            x[b, w, int(torch.randint(0, 7, (1,), generator=g))::int(torch.randint(200, 700, (1,), generator=g))] = float(torch.randn(1, generator=g))
+    x = x.to(dtype).cuda()
+    s = near_scores(x, 1.0, g)
+    check_order(G.beam_select(x, s, 2 * W), x, s, 2 * W)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("T", [0.5, 1.0, 1.75])
+@pytest.mark.parametrize("B,W,V", SHAPES)
+def test_rows_of_one_value(dtype, T, B, W, V):
+    g = torch.Generator().manual_seed(V + W)
+    x = (10.0 * torch.randn(B, W, 1, generator=g)).expand(B, W, V).to(dtype).cuda()
+    s = near_scores(x, T, g)
+    # (every row's best tokens tie; the first token alone stands for the row's place)
+    x[:, :, V // 2] += 1.0
+    s2 = near_scores(x, T, g)
+    check_order(G.beam_select(x, s2, W, T), x, s2, W, T)
+    x[:, :, V // 2] = x[:, :, 0]
+    check_order(G.beam_select(x, s, W, T), x, s, W, T)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("B,W,V", SHAPES[1:])
+def test_penalties_and_finished_hypotheses(dtype, B, W, V):
+    g = torch.Generator().manual_seed(B + W)
+    x = (10.0 * torch.randn(B, W, 1, generator=g)).expand(B, W, V).to(dtype).cuda()
+    x[:, :, 5] += 3.0
+    for penalty in (1.0, 0.6):
+        n = torch.randint(0, 40, (B, W), generator=g, dtype=torch.int32)
+        done = torch.rand(B, W, generator=g) < 0.4
+        y = x.double().cpu()
+        best = y.amax(2) - torch.logsumexp(y, 2)
+        length = torch.where(done, n, n + 1).clamp(min=1).double()
+        # keys next to one another: total = key L^a
+        s = (-15.0 * length ** float(torch.tensor(penalty, dtype=torch.float32)) - torch.where(done, 0.0, best)).float()
+        s = torch.where(torch.rand(B, W, generator=g) < 0.5, s, torch.nextafter(s, torch.tensor(0.0))).cuda()
+        n, done = n.cuda(), done.cuda()
+        K = min(W + 3, int((~done).sum(1).min()) * V + 1)
+        check_order(G.beam_select(x, s, K, lengths=n, done=done, eos=9, length_penalty=penalty), x, s, K, 1.0, n, done, 9, penalty)
