@@ -21,6 +21,7 @@ struct ReorderArgs {
     char* dst[kStatesPerLaunch];
     gr_state_layout at;
     int in_place, team_shift;              // threads of a team: 1 << team_shift
+    long long tokens;                      // of a piece (with lengths)
 };
 
 // the first n bytes of a vector
@@ -56,11 +57,12 @@ reorder_kernel(const __grid_constant__ ReorderArgs A, const int* __restrict__ pa
     __shared__ int s_left[W];                  // bytes that are copied from the CTA's first column on (0: none, or the state stays)
     pdl_wait();
     const gr_state_layout& L = A.at;
-    const int tid = threadIdx.x, pieces = L.parts * L.batch;
+    const int tid = threadIdx.x;
+    const unsigned pieces = (unsigned)L.parts * (unsigned)L.batch;           // (below 2^31; the one after next may lie beyond)
     const long long start = (long long)blockIdx.x * C * kStep;
 #pragma unroll 1
-    for (int piece = blockIdx.y; piece < pieces; piece += gridDim.y) {
-        const int b = piece / L.parts, part = piece - b * L.parts, s = blockIdx.z;
+    for (unsigned piece = blockIdx.y; piece < pieces; piece += gridDim.y) {
+        const int b = (int)piece / L.parts, part = (int)piece - b * L.parts, s = blockIdx.z;
         bool any = false;
         if (tid < W) {
             int left = 0;
@@ -69,7 +71,7 @@ reorder_kernel(const __grid_constant__ ReorderArgs A, const int* __restrict__ pa
                 const int p = __ldg(parents + (size_t)b * L.beams_out + tid);
                 if (p >= 0 && p < L.beams_in && !(A.in_place && p == tid)) {
                     long long used = L.part_bytes;
-                    if (lengths) used = min(used, max(0, __ldg(lengths + (size_t)b * L.beams_in + p)) * L.token_bytes);
+                    if (lengths) used = min(A.tokens, (long long)max(0, __ldg(lengths + (size_t)b * L.beams_in + p))) * L.token_bytes;
                     left = (int)min(max(used - start, 0ll), 1ll << 30);
                     from = A.src[s] + b * L.src_group + p * L.src_beam + part * L.src_part + start;
                 }
@@ -99,7 +101,7 @@ reorder_kernel(const __grid_constant__ ReorderArgs A, const int* __restrict__ pa
                 }
             }
         }
-        if (piece + (int)gridDim.y < pieces) __syncthreads();
+        if (piece + gridDim.y < pieces) __syncthreads();
     }
 }
 
@@ -117,21 +119,22 @@ reorder_short_kernel(const __grid_constant__ ReorderArgs A, const int* __restric
     const int shift = A.team_shift;
     const int tid = threadIdx.x, team = tid >> shift, at = tid & ((1 << shift) - 1);
     const int teams = kCopyThreads >> shift, step = kVec << shift;
-    const int pieces = L.parts * L.batch, s = blockIdx.z;
+    const unsigned pieces = (unsigned)L.parts * (unsigned)L.batch, s = blockIdx.z;
     const long long start = (long long)blockIdx.x * C * step;
 #pragma unroll 1
-    for (int piece0 = blockIdx.y * teams; piece0 < pieces; piece0 += gridDim.y * teams) {
+    for (unsigned piece0 = blockIdx.y * teams; piece0 < pieces; piece0 += gridDim.y * teams) {
         bool any = false;
         for (int e = tid; e < teams * W; e += kCopyThreads) {
-            const int t = e / W, j = e % W, piece = piece0 + t;
+            const int t = e / W, j = e % W;
+            const unsigned piece = piece0 + t;
             int left = 0;
             const char* from = nullptr;
             if (j < L.beams_out && piece < pieces) {
-                const int b = piece / L.parts, part = piece - b * L.parts;
+                const int b = (int)piece / L.parts, part = (int)piece - b * L.parts;
                 const int p = __ldg(parents + (size_t)b * L.beams_out + j);
                 if (p >= 0 && p < L.beams_in && !(A.in_place && p == j)) {
                     long long used = L.part_bytes;
-                    if (lengths) used = min(used, max(0, __ldg(lengths + (size_t)b * L.beams_in + p)) * L.token_bytes);
+                    if (lengths) used = min(A.tokens, (long long)max(0, __ldg(lengths + (size_t)b * L.beams_in + p))) * L.token_bytes;
                     left = (int)min(max(used - start, 0ll), 1ll << 30);
                     from = A.src[s] + b * L.src_group + p * L.src_beam + part * L.src_part + start;
                 }
@@ -140,7 +143,8 @@ reorder_short_kernel(const __grid_constant__ ReorderArgs A, const int* __restric
             any |= left > 0;
         }
         if (__syncthreads_or(any)) {
-            const int piece = piece0 + team, b = piece / L.parts, part = piece - b * L.parts;
+            // (a team beyond the last piece has nothing to copy)
+            const int piece = (int)min(piece0 + team, pieces - 1), b = piece / L.parts, part = piece - b * L.parts;
             char* dst = A.dst[s] + b * L.dst_group + part * L.dst_part + start + at * kVec;
             Vec v[C][W];
 #pragma unroll
@@ -162,7 +166,7 @@ reorder_short_kernel(const __grid_constant__ ReorderArgs A, const int* __restric
                 }
             }
         }
-        if (piece0 + (int)gridDim.y * teams < pieces) __syncthreads();
+        if (piece0 + gridDim.y * teams < pieces) __syncthreads();
     }
 }
 
@@ -275,7 +279,7 @@ static void launch_reorder(const ReorderArgs& A, int count, int vec, const int* 
         B.team_shift = 8;
         while (B.team_shift > 4 && L.part_bytes <= (long long)bytes * columns << (B.team_shift - 1)) B.team_shift--;
         const long long per = (long long)bytes * columns << B.team_shift;
-        const int teams = kCopyThreads >> B.team_shift, rows = (L.parts * L.batch + teams - 1) / teams;
+        const int teams = kCopyThreads >> B.team_shift, rows = (L.parts * L.batch - 1) / teams + 1;
         cudaLaunchConfig_t cfg = {};
         cudaLaunchAttribute at = {};
         at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -338,6 +342,7 @@ int gr_reorder_states(const void* const* src, void* const* dst, int count, const
     for (int lo = 0; lo < count; lo += gr::kStatesPerLaunch) {
         gr::ReorderArgs A;
         A.at = L; A.in_place = in_place;
+        A.tokens = lengths ? L.part_bytes / L.token_bytes : 0;
         const int n = std::min(count - lo, gr::kStatesPerLaunch);
         for (int i = 0; i < n; i++) { A.src[i] = (const char*)src[lo + i]; A.dst[i] = (char*)dst[lo + i]; }
         if (L.beams_out <= 4) gr::launch_reorder<4>(A, n, vec, parents, lengths, st);
