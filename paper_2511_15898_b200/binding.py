@@ -476,6 +476,13 @@ def _need(t, what: str, dtype, shape=None, device=None, optional: bool = False):
     return t.data_ptr()
 
 
+def _fits(what: str, *numbers):
+    """Refuses numbers beyond the 32 bits that the C call takes (ctypes would cut them to their low bits)."""
+    for n in numbers:
+        if not -(1 << 31) <= n < 1 << 31:
+            raise GrError(f"{what}: {n} is beyond 32 bits")
+
+
 # (the handle alone: the public call makes a Stream object around it, 3 us)
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
     lambda index: int(torch.cuda.current_stream(index).cuda_stream))
@@ -539,6 +546,7 @@ def beam_select(logits: torch.Tensor, scores: torch.Tensor, select: Optional[int
     if ((V > 1 and step[2] != 1) or (B > 1 and W > 1 and step[0] != W * ld) or ld < V) and logits.numel() > 0:
         raise GrError("logits: the rows must be apart by one distance, their elements next to one another")
     K = W if select is None else int(select)
+    _fits("beam_select", B, V, K, eos)
     rows = (B, W)
     a_scores = _need(scores, "scores", torch.float32, rows, dev)
     a_lengths = _need(lengths, "lengths", torch.int32, rows, dev, optional=True)
@@ -622,6 +630,7 @@ def reorder_states(states, parents: torch.Tensor, lengths: Optional[torch.Tensor
         if y is not x and (y.shape != (B, chosen) + tuple(shape[2:]) or y.dtype is not x.dtype or y.device != dev):
             raise GrError("out must hold tensors [B, chosen, ...] like the states")
         parts, part_step, part, token = _state_layout(x, token_dim)
+        _fits("states", B, parts)
         part_step_y = part_step if y is x else _state_layout(y, token_dim)[1]
         e = x.element_size()
         return StateLayout(B, W, chosen, parts, step[0] * e if B > 1 else 0, step[1] * e if W > 1 else 0, part_step,
@@ -705,6 +714,7 @@ def block_plan(tables: BlockTables, append: torch.Tensor, max_tokens: int, keep:
     if parents is not None and parents.shape != (R,):
         if tables.beams < 1 or parents.shape != (R // tables.beams, tables.beams):
             raise GrError("parents must be [rows] or [rows / beams, beams]")
+    _fits("block_plan", R, width, N, tables.beams, tables.block_size, max_tokens)
     if out is None or out.shape != (R, N, max_tokens) or out.slots.device != dev:
         wbytes = gr_block_workspace_bytes(R, N)
         if wbytes == 0 or max_tokens < 0:
@@ -745,6 +755,7 @@ def copy_blocks(caches, copy_src: torch.Tensor, copy_dst: torch.Tensor) -> None:
         if per and (not x[0].is_contiguous() or (shape[0] > 1 and step[0] < per)):
             raise GrError("caches: a block's elements must lie next to one another, and the blocks apart")
         e = x.element_size()
+        _fits("caches", shape[0], copy_src.shape[0])
         return shape[0], (step[0] if shape[0] > 1 else per) * e, per * e
 
     last = None
