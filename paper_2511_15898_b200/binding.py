@@ -597,7 +597,7 @@ def reorder_states(states, parents: torch.Tensor, lengths: Optional[torch.Tensor
     parents [B, chosen] int32.  In place, with chosen <= beams, unless `out` (a list of tensors [B, chosen, ...]) is
     given, which must not meet the states in memory.  With lengths [B, beams] int32 the dimension `token_dim` of the
     states counts tokens, of which each parent's first lengths[b, parent] are copied.  Returns `out` or `states`."""
-    if _short("reorder", "gr_reorder_states", states, parents, lengths, -1 if token_dim is None else token_dim, out):
+    if _short("reorder", "gr_reorder_states", states, parents, lengths, token_dim, out):
         return states if out is None else out
     states = list(states)
     to = states if out is None else list(out)

@@ -73,7 +73,7 @@ bool here(c10::Device dev, void** stream)
 #define GR_TRY try {
 #define GR_CATCH } catch (...) { PyErr_Clear(); Py_RETURN_NONE; }
 
-// reorder(function, states, parents, lengths, token_dim or -1, out) -> its answer or None
+// reorder(function, states, parents, lengths, token_dim, out) -> its answer or None
 PyObject* reorder(PyObject*, PyObject* const* a, Py_ssize_t n)
 {
     GR_OR_NONE(n == 6);
@@ -85,7 +85,8 @@ PyObject* reorder(PyObject*, PyObject* const* a, Py_ssize_t n)
     const at::Tensor *y = &x, *parents, *lengths;
     const c10::Device dev = x.device();
     const bool in_place = a[5] == Py_None;
-    const long token_dim = PyLong_AsLong(a[4]);
+    const long token_dim = a[4] == Py_None ? -1 : PyLong_AsLong(a[4]);
+    GR_OR_NONE(!PyErr_Occurred() && (a[4] == Py_None || token_dim >= 0));
     GR_OR_NONE(is_plain(a[2], at::kInt, dev, false, &parents) && is_plain(a[3], at::kInt, dev, true, &lengths));
     GR_OR_NONE(x.dim() >= 2 && parents->dim() == 2 && parents->size(0) == x.size(0) && (lengths != nullptr) == (token_dim >= 0));
     GR_OR_NONE(token_dim < 0 || (token_dim >= 2 && token_dim < x.dim()));

@@ -43,3 +43,18 @@ def test_numbers_beyond_32_bits_are_refused(way):
         G.reorder_states([state], torch.zeros(1, 2, **I32), lengths=torch.ones(1, 2, **I32), token_dim=3)
     with pytest.raises(G.GrError):
         G.copy_blocks([state.view(-1, 1)], torch.zeros(1, **I32), torch.ones(1, **I32))
+
+
+def test_token_dimensions_that_are_none(way):
+    state, parents = torch.arange(48.0, device="cuda").view(2, 3, 8), torch.zeros(2, 3, **I32)
+    keep = state.clone()
+    for dim in (-1, -2, -9):
+        with pytest.raises(G.GrError):
+            G.reorder_states([state], parents, token_dim=dim)
+        with pytest.raises(G.GrError):
+            G.reorder_states([state], parents, lengths=torch.ones(2, 3, **I32), token_dim=dim)
+    with pytest.raises(Exception) as e:
+        G.reorder_states([state], parents, token_dim="2")
+    assert not isinstance(e.value, SystemError)
+    torch.cuda.synchronize()
+    assert torch.equal(state, keep)
