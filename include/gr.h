@@ -346,8 +346,8 @@ int gr_beam_select(const void* logits, int dtype, int V, long long ld, int beams
  * b * src_group + w * src_beam + p * src_part bytes after src[i], and likewise for dst[i].
  *   src, dst   HOST arrays of `count` device pointers.  dst[i] == src[i] with equal strides reorders in place (any
  *              mapping, cycles and repeated parents included); otherwise no dst may meet a src (from the first byte of its
- *              pieces to the last: GR_E_INVALID).  The same dst twice (or two that begin less than part_bytes apart) is
- *              GR_E_INVALID, and so are strides that make the pieces of a dst overlap.  Within src, groups, states and
+ *              pieces to the last: GR_E_INVALID).  Two dst that share a byte are GR_E_INVALID (one may lie between the pieces
+ *              of another), and so are strides that make the pieces of a dst overlap.  Within src, groups, states and
  *              pieces may coincide (stride 0), unless it is reordered in place.
  *   parents    [batch, beams_out] int.  -1, or any number outside 0 .. beams_in - 1: that state is left as it was.
  *   lengths    [batch, beams_in] int or NULL.  With it a piece is a run of tokens of token_bytes bytes each and only the
@@ -411,8 +411,8 @@ int gr_block_plan(int* table, int rows, int width, int beams, int block_size, in
 /*
  * gr_copy_blocks -- block copy_dst[i] of every cache becomes a copy of block copy_src[i], for the listed pairs.
  *   caches      HOST array of `count` device pointers; block k of a cache begins k * block_stride bytes after it and
- *               is block_bytes long (block_stride >= block_bytes).  The same cache twice (or two that begin less than
- *               block_bytes apart) is GR_E_INVALID.
+ *               is block_bytes long (block_stride >= block_bytes).  Two caches that share a byte are GR_E_INVALID (one may
+ *               lie between the blocks of another).
  *   copy_src, copy_dst  [pairs] int, as gr_block_plan writes them: a pair with an index outside 0 .. num_blocks - 1 (-1:
  *               nothing to copy) is skipped.  Blocks that are copied to must be distinct and none may be copied from.
  *   pairs <= 2^24 - 256; blocks up to 2^22 x 1024 bytes times the power of two (up to 16) that divides pointers, stride and size.

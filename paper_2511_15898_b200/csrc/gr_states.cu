@@ -259,14 +259,68 @@ static bool meet(const void* const* p, long long a, void* const* q, long long b,
     return false;
 }
 
-// GR_OK where the pointers lie at least `bytes` apart
-static int check_apart(const void* const* p, int count, long long bytes)
+// Where the pieces of a tensor lie: `bytes` each, size[i] of them stride[i] apart, i = 0 .. 2, innermost first; span[i]: what the levels
+// before i span.  (Clear of one another: stride[i] >= span[i].)
+struct Lattice {
+    long long bytes, stride[3], span[4];
+    int size[3];
+};
+static Lattice lattice_of(long long bytes, const long long* stride, const int* size)
+{
+    int order[3] = {0, 1, 2};
+    std::sort(order, order + 3, [&](int a, int b) { return stride[a] < stride[b]; });
+    Lattice t;
+    t.bytes = bytes; t.span[0] = bytes;
+    for (int i = 0; i < 3; i++) {
+        t.size[i] = size[order[i]];
+        t.stride[i] = t.size[i] > 1 ? stride[order[i]] : 0;
+        t.span[i + 1] = t.span[i] + t.stride[i] * (t.size[i] - 1);
+    }
+    return t;
+}
+
+// Whether a piece of one tensor meets a piece of another that lies `d` bytes behind it, by the first `levels` levels: of the outermost
+// one's differences only the two around d / stride leave the levels within anything to do.
+static bool pieces_meet(const Lattice& t, int levels, long long d)
+{
+    while (levels > 0 && t.size[levels - 1] == 1) levels--;
+    if (d >= t.span[levels] || -d >= t.span[levels]) return false;
+    if (levels == 0) return true;
+    const long long s = t.stride[levels - 1], k = d >= 0 ? d / s : -((-d + s - 1) / s);
+    for (long long c = k; c <= k + 1; c++) if (c > -t.size[levels - 1] && c < t.size[levels - 1] && pieces_meet(t, levels - 1, d - c * s)) return true;
+    return false;
+}
+
+// GR_OK where no two tensors of this layout share a byte.  Tensors beside one another are told by their first and last bytes, tensors
+// within one another mostly by the place of their pieces between two steps of a stride, the others pair by pair.
+static int check_apart(const void* const* p, int count, const Lattice& t)
 {
     std::unique_ptr<uintptr_t[]> at(new (std::nothrow) uintptr_t[count]);
     if (!at) return GR_E_TOO_LARGE;
-    for (int i = 0; i < count; i++) at[i] = (uintptr_t)p[i];
-    std::sort(at.get(), at.get() + count);
-    for (int i = 1; i < count; i++) if (at[i] - at[i - 1] < (uintptr_t)bytes) return GR_E_INVALID;
+    auto fill = [&](unsigned long long modulus) {
+        for (int i = 0; i < count; i++) at[i] = modulus ? (uintptr_t)p[i] % modulus : (uintptr_t)p[i];
+        std::sort(at.get(), at.get() + count);
+    };
+    auto apart = [&](long long bytes) {
+        for (int i = 1; i < count; i++) if (at[i] - at[i - 1] < (uintptr_t)bytes) return false;
+        return true;
+    };
+    fill(0);
+    if (apart(t.span[3])) return GR_OK;
+    if (!apart(t.bytes)) return GR_E_INVALID;
+    for (int i = 2; i >= 0; i--) {
+        // (modulo stride i, which divides all larger ones, a tensor is span[i] bytes in a row, round the end)
+        const long long s = t.stride[i];
+        bool divides = s > 0;
+        for (int j = i + 1; j < 3 && divides; j++) divides = t.stride[j] % s == 0;
+        if (!divides) continue;
+        fill((unsigned long long)s);
+        if (apart(t.span[i]) && at[0] + (uintptr_t)s - at[count - 1] >= (uintptr_t)t.span[i]) return GR_OK;
+    }
+    fill(0);
+    for (int i = 0; i < count; i++) {
+        for (int j = i + 1; j < count && at[j] - at[i] < (uintptr_t)t.span[3]; j++) if (pieces_meet(t, 3, (long long)(at[j] - at[i]))) return GR_E_INVALID;
+    }
     return GR_OK;
 }
 
@@ -317,7 +371,7 @@ int gr_reorder_states(const void* const* src, void* const* dst, int count, const
     if ((long long)L.batch * L.parts >= (1ll << 31)) return GR_E_INVALID;
     if (lengths && (L.token_bytes < 1 || L.part_bytes % L.token_bytes)) return GR_E_INVALID;
     if (count == 0 || L.batch == 0 || L.parts == 0 || L.part_bytes == 0) return GR_OK;
-    if (!src || !dst || !parents) return GR_E_NULL;
+    if (!src || !dst) return GR_E_NULL;
     for (int i = 0; i < count; i++) if (!src[i] || !dst[i]) return GR_E_NULL;
     const bool in_place = src[0] == dst[0];
     for (int i = 1; i < count; i++) if ((src[i] == dst[i]) != in_place) return GR_E_INVALID;
@@ -328,8 +382,9 @@ int gr_reorder_states(const void* const* src, void* const* dst, int count, const
     const long long to_span = gr::span_of(L.part_bytes, to, to_size, true), from_span = gr::span_of(L.part_bytes, from, from_size, false);
     if (to_span == 0 || from_span == 0) return GR_E_INVALID;
     if (!in_place && gr::meet(src, from_span, dst, to_span, count)) return GR_E_INVALID;
-    const int apart = gr::check_apart(dst, count, L.part_bytes);
+    const int apart = count > 1 ? gr::check_apart(dst, count, gr::lattice_of(L.part_bytes, to, to_size)) : GR_OK;
     if (apart != GR_OK) return apart;
+    if (!parents) return GR_E_NULL;                        // (last: without them a call looks at the rest and launches nothing)
     unsigned long long bits = (unsigned long long)L.part_bytes;
     if (L.batch > 1) bits |= (unsigned long long)(L.src_group | L.dst_group);
     if (L.beams_in > 1) bits |= (unsigned long long)L.src_beam;
@@ -360,9 +415,11 @@ int gr_copy_blocks(void* const* caches, int count, int num_blocks, long long blo
     if (count < 0 || num_blocks < 0 || pairs < 0 || block_bytes < 0 || block_stride < block_bytes) return GR_E_INVALID;
     if (num_blocks > 0 && block_stride > gr::kMaxBytes / num_blocks) return GR_E_INVALID;
     if (count == 0 || num_blocks == 0 || pairs == 0 || block_bytes == 0) return GR_OK;
-    if (!caches || !copy_src || !copy_dst) return GR_E_NULL;
+    if (!caches) return GR_E_NULL;
     for (int i = 0; i < count; i++) if (!caches[i]) return GR_E_NULL;
-    const int apart = gr::check_apart(caches, count, block_bytes);
+    const long long steps[3] = {block_stride, 0, 0};
+    const int sizes[3] = {num_blocks, 1, 1};
+    const int apart = count > 1 ? gr::check_apart(caches, count, gr::lattice_of(block_bytes, steps, sizes)) : GR_OK;
     if (apart != GR_OK) return apart;
     unsigned long long bits = (unsigned long long)(block_stride | block_bytes);
     for (int i = 0; i < count; i++) bits |= (unsigned long long)(uintptr_t)caches[i];
@@ -372,6 +429,7 @@ int gr_copy_blocks(void* const* caches, int count, int num_blocks, long long blo
     while (team_shift > 5 && block_bytes <= (long long)vec * gr::kCopyColumns << (team_shift - 1)) team_shift--;
     const long long per = (long long)vec * gr::kCopyColumns << team_shift, chunks = (block_bytes + per - 1) / per;
     if (segments > 65535 || chunks > (1 << 22)) return GR_E_TOO_LARGE;
+    if (!copy_src || !copy_dst) return GR_E_NULL;          // (last, as above)
     cudaStream_t st = (cudaStream_t)stream;
     gr::NvtxRange whole("gr_copy_blocks");
     for (int lo = 0; lo < count; lo += gr::kStatesPerLaunch) {
