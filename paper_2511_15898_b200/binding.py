@@ -28,6 +28,7 @@ GR_STATIC_MAX_BATCH = 256
 GR_PARTIAL_RULE = 6
 GR_NO_BLOCKS, GR_ROW_FULL, GR_BAD_ROW = 8, 9, 10
 GR_MAX_BEAMS, GR_MAX_SELECT = 32, 128
+_NULL = -2                 # a required pointer is NULL
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_HERE, "libgr_b200.so")
@@ -502,6 +503,40 @@ def _short(way: str, name: str, *args):
     return True
 
 
+def _starts(at: int, dims) -> torch.Tensor:
+    """Where the pieces of a tensor begin, in order: dims are (number, bytes from one to the next)."""
+    out = torch.tensor([at])
+    for n, step in dims:
+        out = (out.view(-1, 1) + torch.arange(n if step else min(n, 1)) * step).view(-1)
+    return out.sort().values
+
+
+def _share_bytes(a, b) -> bool:
+    """Whether a tensor of `a` shares a byte with one of `b`: lists of (list it came from, address, dims, bytes of a piece).  (Those of one
+    list are the C call's to look at.)"""
+    every = []
+    for side, tensors in enumerate((a, b)):
+        for run, at, dims, size in tensors:
+            if size and all(n for n, _ in dims):
+                every.append((at, at + size + sum(step * (n - 1) for n, step in dims), side, run, dims, size))
+    every.sort(key=lambda e: e[:2])
+    within = []                            # those that may reach what follows
+    for e in every:
+        within = [o for o in within if o[1] > e[0]]
+        for o in within:
+            if o[3] == e[3] or (o[2] == e[2] and a is not b):
+                continue
+            # one lies within the other: piece by piece
+            if any(torch.Size(n for n, _ in t[4]).numel() > 1 << 24 for t in (o, e)):
+                raise GrError("tensors of different layouts within one another have too many pieces to tell them apart")
+            p, q = _starts(o[0], o[4]), _starts(e[0], e[4])
+            before = torch.searchsorted(p, q + e[5]) - 1              # the last piece of one that begins before the other's ends
+            if bool(((before >= 0) & (p[before.clamp(min=0)] + o[5] > q)).any()):
+                return True
+        within.append(e)
+    return False
+
+
 def _call(dev: torch.device, what: str, function, *args):
     """A C entry point with the tensors' device current and that device's current stream."""
     if torch.cuda.current_device() == dev.index:
@@ -648,11 +683,20 @@ def reorder_states(states, parents: torch.Tensor, lengths: Optional[torch.Tensor
         runs[-1][1].append(x.data_ptr())
         runs[-1][2].append(y.data_ptr())
     if len(runs) > 1:
-        # (within a run the C call looks)
-        first = [p for r in runs if r[0].part_bytes for p in r[2]]
-        if len(set(first)) < len(first):
-            raise GrError("the same tensor twice")
-        if out is not None and any(y.untyped_storage().data_ptr() == x.untyped_storage().data_ptr() for y in to for x in states if y.numel()):
+        # nothing is launched before every call is known to be taken (without parents the C call looks at the rest and answers so)
+        mine, theirs = [], []
+        for run, (t, at, at_y) in enumerate(runs):
+            if chosen > 0 and t.part_bytes > 0:
+                rc = gr_reorder_states(at, at_y, t, 0, a_lengths, 0)
+                if out is not None and at[0] == at_y[0]:
+                    raise GrError("out shares memory with the states")
+                if rc not in (GR_OK, _NULL):
+                    _check(rc, "gr_reorder_states")
+                theirs += [(run, p, ((B, t.src_group), (W, t.src_beam), (t.parts, t.src_part)), t.part_bytes) for p in at]
+                mine += [(run, p, ((B, t.dst_group), (W if out is None else chosen, t.dst_beam), (t.parts, t.dst_part)), t.part_bytes) for p in at_y]
+        if _share_bytes(mine, mine):
+            raise GrError("two of the tensors share memory")
+        if out is not None and _share_bytes(mine, theirs):
             raise GrError("out shares memory with the states")
     for layout, at, at_y in runs:
         if chosen > 0 and layout.part_bytes > 0:
@@ -768,9 +812,15 @@ def copy_blocks(caches, copy_src: torch.Tensor, copy_dst: torch.Tensor) -> None:
             runs.append(layout_of(x) + ([],))
         runs[-1][3].append(x.data_ptr())
     if len(runs) > 1:
-        first = [p for r in runs if r[2] for p in r[3]]
-        if len(set(first)) < len(first):
-            raise GrError("the same cache twice")
+        # (as for states: nothing is launched before every call is known to be taken)
+        every = []
+        for run, (blocks, stride, size, at) in enumerate(runs):
+            rc = gr_copy_blocks(at, blocks, stride, size, 0, 0, copy_src.shape[0], 0)
+            if rc not in (GR_OK, _NULL):
+                _check(rc, "gr_copy_blocks")
+            every += [(run, p, ((blocks, stride),), size) for p in at]
+        if _share_bytes(every, every):
+            raise GrError("two of the caches share memory")
     for blocks, stride, size, at in runs:
         if size > 0:
             _call(dev, "gr_copy_blocks", gr_copy_blocks, at, blocks, stride, size, a_src, a_dst, copy_src.shape[0])

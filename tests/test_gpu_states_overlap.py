@@ -47,3 +47,44 @@ def test_one_layout():
     torch.cuda.synchronize()
     keep[6:8], keep[10:12] = keep[0:2].clone(), keep[8:10].clone()
     assert same(pool, keep)
+
+
+def test_several_layouts():
+    x = rand((2, 4, 3, 40), torch.float32, 1)
+    keep, parents = x.clone(), ints([[1, 0, 3, 3], [2, 2, 0, 1]])
+    other = rand((2, 4, 9), torch.float32, 2)
+    first = other.clone()
+    n = torch.full((2, 4), 3, dtype=torch.int32, device="cuda")
+    for call in (lambda: G.reorder_states([x, x[:, :, 1:]], parents),                                   # (one begins within the other)
+                 lambda: G.reorder_states([other, x[:, :, 0, :8], x[:, :, 0, 7:]], parents),
+                 lambda: G.reorder_states([other, x[:, :, 0].expand(2, 4, 40)[:1].expand(2, 4, 40)], parents),   # (two groups in one place)
+                 lambda: G.reorder_states([x[:, :, 0, :8], x[:, :, 0, 9:]], parents, out=[torch.zeros(2, 4, 8, device="cuda"), x[:, :, 1, 9:]]),
+                 lambda: G.reorder_states([x[:, :, 0, :8], x[:, :, 0, 9:]], parents, out=[x[:, :, 0, 20:28], torch.zeros(2, 4, 31, device="cuda")]),
+                 lambda: G.reorder_states([other, x], parents, out=[torch.zeros_like(other), x]),
+                 lambda: G.copy_blocks([other.view(8, 9), x.view(24, 40), x.view(8, 120)], ints([0]), ints([1])),
+                 lambda: G.copy_blocks([other.view(8, 9), x.view(8, 120)[:, :50], x.view(8, 120)[:, 49:]], ints([0]), ints([1]))):
+        with pytest.raises(G.GrError):
+            call()
+    torch.cuda.synchronize()
+    assert same(x, keep) and same(other, first)
+    # parts of one row of different lengths, and a tensor of its own
+    states = [x[:, :, 0, :8], x[:, :, 0, 8:], x[:, :, 1:], other]
+    want = [expected(t, parents) for t in states]
+    G.reorder_states(states[:2] + [other], parents)
+    G.reorder_states([states[2]], parents)
+    torch.cuda.synchronize()
+    assert all(same(a, b) for a, b in zip(states, want))
+    # outs beside the states in one buffer
+    buf = rand((5000,), torch.float32, 3)
+    a, b, c, d = buf[:64].view(2, 4, 8), buf[64:136].view(2, 4, 9), buf[136:200].view(2, 4, 8), buf[200:272].view(2, 4, 9)
+    want = [expected(a, parents, out=c), expected(b, parents, out=d)]
+    G.reorder_states([a, b], parents, out=[c, d])
+    torch.cuda.synchronize()
+    assert same(c, want[0]) and same(d, want[1])
+    # blocks of two sizes that lie in turn
+    pool = rand((10, 30), torch.float32, 4)
+    keep = pool.clone()
+    G.copy_blocks([pool[:, :11], pool[:, 11:], x.view(24, 40)[:10]], ints([2]), ints([7]))
+    torch.cuda.synchronize()
+    keep[7] = keep[2]
+    assert same(pool, keep)
