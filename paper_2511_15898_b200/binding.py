@@ -11,15 +11,11 @@ from __future__ import annotations
 import array
 import ctypes as C
 import dataclasses
+import importlib
 import os
 from typing import Optional, Tuple
 
 import torch
-
-try:
-    from . import _tensors           # (built beside the library; without it every call goes the way below)
-except ImportError:
-    _tensors = None
 
 GR_F32, GR_BF16 = 0, 1
 GR_OK, GR_NOT_CONVERGED, GR_SUPPORT_TOO_LARGE, GR_BAD_LOGITS, GR_DRAFT_OUT_OF_SUPPORT, GR_STALE_PARAMS = range(6)
@@ -34,6 +30,23 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_HERE, "libgr_b200.so")
 _lib = None
 _entry = {}                # addresses of entry points, for _tensors
+
+
+def _load_tensors():
+    """The compiled module beside the library, or None: then every call goes the way in Python.  (With the library and not with the
+    package, so that a process that only imports the package neither maps it nor misses one that is built later.)"""
+    importlib.invalidate_caches()
+    try:
+        from . import _tensors as module
+    except ImportError:
+        return None
+    return module
+
+
+def __getattr__(name):
+    if name == "_tensors":               # (before the library is loaded)
+        return _load_tensors()
+    raise AttributeError(name)
 
 
 class GrError(RuntimeError):
@@ -63,6 +76,7 @@ def library_path() -> str:
 def load_library():
     """dlopen the compiled library (built by paper_2511_15898_b200.build); raises if it is missing."""
     global _lib
+    global _tensors
     if _lib is not None:
         return _lib
     if not os.path.exists(_LIB_PATH):
@@ -110,6 +124,8 @@ def load_library():
     _entry.update({n: C.cast(getattr(lib, n), C.c_void_p).value
                    for n in ("gr_beam_select", "gr_reorder_states", "gr_block_plan", "gr_copy_blocks")})
     _lib = lib
+    if "_tensors" not in globals():
+        _tensors = _load_tensors()
     return lib
 
 
@@ -491,10 +507,10 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
 
 def _short(way: str, name: str, *args):
     """The call of entry point `name` by the short way, where that is open: True when it was made."""
-    if _tensors is None:
-        return False
     if _lib is None:
         load_library()
+    if _tensors is None:
+        return False
     rc = getattr(_tensors, way)(_entry[name], *args)
     if rc is None:
         return False
