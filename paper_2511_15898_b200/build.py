@@ -18,24 +18,54 @@ HEADERS = [os.path.join(CSRC, "gr_common.cuh"), os.path.join(CSRC, "gr_prep.cuh"
            os.path.join(ROOT, "include", "gr.h")]
 
 
-# the binding's short way for tensors: a Python module on torch's headers
+# The binding's short way for tensors: a Python module on torch's headers.
+# Beside it stands what it was compiled from (its sources and torch), in words.
 TENSORS_SOURCE = os.path.join(CSRC, "gr_tensors.cpp")
 TENSORS = os.path.join(HERE, "_tensors.so")
 
 
-def _build_tensors(force: bool = False):
-    """The started compilation of the module, or None where it is up to date."""
+def _tensors_of() -> str:
+    """What a module compiled now would be compiled from."""
+    import hashlib
+
+    from torch import __version__ as torch_version
+    h = hashlib.sha256()
+    for path in (TENSORS_SOURCE, os.path.join(ROOT, "include", "gr.h")):
+        with open(path, "rb") as f:
+            h.update(f.read())
+    return f"torch {torch_version} python {sys.version.split()[0]} sources {h.hexdigest()}"
+
+
+def _tensors_fresh() -> bool:
+    """Whether the module is of the present sources."""
+    try:
+        with open(TENSORS + ".txt") as f:
+            of, state = f.read().split("\n")[:2]
+    except (OSError, ValueError):
+        return False
+    return of == _tensors_of() and state == "built" and os.path.exists(TENSORS)
+
+
+def _start_tensors():
+    """The started compilation of the module."""
     import sysconfig
 
     import torch
     from torch.utils.cpp_extension import include_paths
-    if not force and os.path.exists(TENSORS) and os.path.getmtime(TENSORS) > os.path.getmtime(TENSORS_SOURCE):
-        return None
     lib = os.path.join(os.path.dirname(torch.__file__), "lib")
-    cmd = (["g++", "-O2", "-std=c++17", "-shared", "-fPIC", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}"]
+    cmd = ([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-shared", "-fPIC", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+            f'-DGR_TORCH_VERSION="{torch.__version__}"']
            + [a for p in include_paths() + [sysconfig.get_paths()["include"], os.path.join(_cuda_home(), "include")] for a in ("-isystem", p)]
            + ["-I", os.path.join(ROOT, "include"), TENSORS_SOURCE, "-L" + lib, "-ltorch_python", "-ltorch_cpu", "-lc10_cuda", "-lc10", "-Wl,-rpath," + lib, "-o", TENSORS])
     return subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+
+
+def _finish_tensors(started):
+    out, _ = started.communicate()
+    if started.returncode != 0:
+        raise RuntimeError(os.path.basename(TENSORS_SOURCE) + ":\n" + out)
+    with open(TENSORS + ".txt", "w") as f:
+        f.write(_tensors_of() + "\nbuilt\n")
 
 
 def _nvcc() -> str:
@@ -53,7 +83,7 @@ def needs_build(check: bool = False) -> bool:
     lib = LIB_CHECK if check else LIB
     if not os.path.exists(lib):
         return True
-    if not check and (not os.path.exists(TENSORS) or os.path.getmtime(TENSORS) < os.path.getmtime(TENSORS_SOURCE)):
+    if not check and not _tensors_fresh():
         return True
     t = os.path.getmtime(lib)
     deps = [os.path.join(CSRC, s) for s in SOURCES] + HEADERS
@@ -88,10 +118,7 @@ def build_library(force: bool = False, verbose: bool = False, check: bool = Fals
         if not fresh:
             jobs.append((s, subprocess.Popen([_nvcc()] + flags + ["-c", src, "-o", obj], stdout=subprocess.PIPE,
                                              stderr=subprocess.STDOUT, text=True)))
-    if not check:
-        proc = _build_tensors(force)
-        if proc is not None:
-            jobs.append((os.path.basename(TENSORS_SOURCE), proc))
+    tensors = _start_tensors() if not check and (force or not _tensors_fresh()) else None
     failed = []
     for s, proc in jobs:
         out, _ = proc.communicate()
@@ -99,6 +126,8 @@ def build_library(force: bool = False, verbose: bool = False, check: bool = Fals
             sys.stderr.write(out)
         if proc.returncode != 0:
             failed.append(s + ":\n" + out)
+    if tensors is not None:
+        _finish_tensors(tensors)
     if failed:
         raise RuntimeError("nvcc failed:\n" + "\n".join(failed))
     res = subprocess.run([_nvcc(), "-shared", "-cudart", "static", "-gencode", "arch=compute_100a,code=sm_100a"]

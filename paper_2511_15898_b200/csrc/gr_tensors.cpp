@@ -207,4 +207,10 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_tensors", nullptr, -1, methods, n
 
 }  // namespace
 
-PyMODINIT_FUNC PyInit__tensors(void) { return PyModule_Create(&module); }
+// (torch's objects are looked into directly: with another torch than the one it was compiled for the binding leaves it alone)
+PyMODINIT_FUNC PyInit__tensors(void)
+{
+    PyObject* m = PyModule_Create(&module);
+    if (m && PyModule_AddStringConstant(m, "torch_version", GR_TORCH_VERSION) != 0) Py_CLEAR(m);
+    return m;
+}

@@ -43,3 +43,23 @@ def test_a_module_that_is_built_after_the_import_is_used(tmp_path):
                  f"shutil.copy({build.TENSORS!r}, {str(package)!r})\n"
                  "G.load_library(); print(B._tensors is None)", cwd=tmp_path)
     assert out == ["True", "False"]
+
+
+def test_a_module_for_another_torch_is_left_alone():
+    assert python("import torch, paper_2511_15898_b200 as G, paper_2511_15898_b200.binding as B\n"
+                  "torch.__version__ = '1.0'; G.load_library(); print(B._tensors is None)") == ["True"]
+
+
+def test_it_is_built_again_when_what_it_is_made_of_changes(tmp_path, monkeypatch):
+    assert build._tensors_fresh() and not build.needs_build()
+    shutil.copytree(os.path.join(ROOT, "include"), tmp_path / "include")
+    with monkeypatch.context() as m:
+        m.setattr(build, "ROOT", str(tmp_path))
+        assert build._tensors_fresh()
+        with open(tmp_path / "include" / "gr.h", "a") as f:
+            f.write("\n")
+        assert not build._tensors_fresh() and build.needs_build()
+    with monkeypatch.context() as m:
+        m.setattr("torch.__version__", "1.0")
+        assert not build._tensors_fresh()
+    assert build._tensors_fresh()
