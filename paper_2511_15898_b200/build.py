@@ -18,7 +18,7 @@ HEADERS = [os.path.join(CSRC, "gr_common.cuh"), os.path.join(CSRC, "gr_prep.cuh"
            os.path.join(ROOT, "include", "gr.h")]
 
 
-# The binding's short way for tensors: a Python module on torch's headers.
+# The binding's short way for tensors: a Python module on torch's headers, which the package does without where it cannot be compiled.
 # Beside it stands what it was compiled from (its sources and torch), in words.
 TENSORS_SOURCE = os.path.join(CSRC, "gr_tensors.cpp")
 TENSORS = os.path.join(HERE, "_tensors.so")
@@ -27,8 +27,10 @@ TENSORS = os.path.join(HERE, "_tensors.so")
 def _tensors_of() -> str:
     """What a module compiled now would be compiled from."""
     import hashlib
-
-    from torch import __version__ as torch_version
+    try:
+        from torch import __version__ as torch_version
+    except ImportError:
+        torch_version = None
     h = hashlib.sha256()
     for path in (TENSORS_SOURCE, os.path.join(ROOT, "include", "gr.h")):
         with open(path, "rb") as f:
@@ -37,35 +39,46 @@ def _tensors_of() -> str:
 
 
 def _tensors_fresh() -> bool:
-    """Whether the module is of the present sources."""
+    """Whether the module, or the note that it could not be compiled, is of the present sources."""
     try:
         with open(TENSORS + ".txt") as f:
             of, state = f.read().split("\n")[:2]
     except (OSError, ValueError):
         return False
-    return of == _tensors_of() and state == "built" and os.path.exists(TENSORS)
+    return of == _tensors_of() and (state == "failed" or os.path.exists(TENSORS))
 
 
 def _start_tensors():
-    """The started compilation of the module."""
+    """The started compilation of the module, or what kept it from starting."""
     import sysconfig
-
-    import torch
-    from torch.utils.cpp_extension import include_paths
+    try:
+        import torch
+        from torch.utils.cpp_extension import include_paths
+    except ImportError as e:
+        return str(e)
     lib = os.path.join(os.path.dirname(torch.__file__), "lib")
     cmd = ([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-shared", "-fPIC", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
             f'-DGR_TORCH_VERSION="{torch.__version__}"']
            + [a for p in include_paths() + [sysconfig.get_paths()["include"], os.path.join(_cuda_home(), "include")] for a in ("-isystem", p)]
            + ["-I", os.path.join(ROOT, "include"), TENSORS_SOURCE, "-L" + lib, "-ltorch_python", "-ltorch_cpu", "-lc10_cuda", "-lc10", "-Wl,-rpath," + lib, "-o", TENSORS])
-    return subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+    try:
+        return subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+    except OSError as e:
+        return str(e)
 
 
 def _finish_tensors(started):
-    out, _ = started.communicate()
-    if started.returncode != 0:
-        raise RuntimeError(os.path.basename(TENSORS_SOURCE) + ":\n" + out)
+    if isinstance(started, str):
+        out = started
+    else:
+        out, _ = started.communicate()
+    done = not isinstance(started, str) and started.returncode == 0
+    if not done:
+        sys.stderr.write(f"{os.path.basename(TENSORS_SOURCE)} could not be compiled, the binding's calls go the way in Python:\n{out}\n")
+        if os.path.exists(TENSORS):
+            os.remove(TENSORS)
     with open(TENSORS + ".txt", "w") as f:
-        f.write(_tensors_of() + "\nbuilt\n")
+        f.write(_tensors_of() + ("\nbuilt\n" if done else "\nfailed\n"))
 
 
 def _nvcc() -> str:

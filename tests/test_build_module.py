@@ -63,3 +63,14 @@ def test_it_is_built_again_when_what_it_is_made_of_changes(tmp_path, monkeypatch
         m.setattr("torch.__version__", "1.0")
         assert not build._tensors_fresh()
     assert build._tensors_fresh()
+
+
+@pytest.mark.parametrize("compiler", ["/nowhere/g++", "false"])
+def test_the_library_is_built_without_it(tmp_path, monkeypatch, capsys, compiler):
+    monkeypatch.setenv("CXX", compiler)
+    monkeypatch.setattr(build, "LIB", str(tmp_path / "libgr_b200.so"))
+    monkeypatch.setattr(build, "TENSORS", str(tmp_path / "_tensors.so"))
+    assert os.path.exists(build.build_library()) and not os.path.exists(build.TENSORS)
+    assert "could not be compiled" in capsys.readouterr().err
+    # (not tried again until something changes)
+    assert not build.needs_build()
