@@ -40,7 +40,7 @@ def _load_tensors():
         from . import _tensors as module
     except ImportError:
         return None
-    return module if module.torch_version == torch.__version__ else None
+    return module if getattr(module, "torch_version", None) == torch.__version__ else None
 
 
 def __getattr__(name):
