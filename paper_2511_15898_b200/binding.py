@@ -570,11 +570,12 @@ class Beams:
     token: torch.Tensor      # [B, select] int32
     parent: torch.Tensor     # [B, select] int32
     score: torch.Tensor      # [B, select] float32
-    length: torch.Tensor     # [B, select] int32 (written by calls with lengths; zeros before)
+    length: torch.Tensor     # [B, select] int32 (zeros after a call without lengths)
     done: torch.Tensor       # [B, select] bool
     status: torch.Tensor     # [B] int32
     workspace: torch.Tensor  # uint8, scratch
     shape: tuple             # (B, beams, V, select)
+    counted: bool = False    # whether a call has written lengths
 
 
 def beam_select(logits: torch.Tensor, scores: torch.Tensor, select: Optional[int] = None, temperature: float = 1.0,
@@ -589,7 +590,7 @@ def beam_select(logits: torch.Tensor, scores: torch.Tensor, select: Optional[int
     if (out is not None and out.shape == (*logits.shape, logits.shape[1] if select is None else select)
             and _short("select", "gr_beam_select", logits, scores, out.shape[3], temperature, lengths, done, eos, length_penalty,
                        out.workspace, out.token, out.parent, out.score, out.length, out.done, out.status)):
-        return out
+        return _with_lengths(out, lengths)
     B, W, V = logits.shape
     dev, code = logits.device, _dtype_code(logits)
     step = logits.stride()
@@ -617,6 +618,16 @@ def beam_select(logits: torch.Tensor, scores: torch.Tensor, select: Optional[int
     _call(dev, "gr_beam_select", load_library().gr_beam_select, logits.data_ptr(), code, V, max(ld, V), W, B, temperature,
           a_scores, a_lengths, a_done, eos, length_penalty, K, out.workspace.data_ptr(), out.token.data_ptr(),
           out.parent.data_ptr(), a_score, a_length if lengths is not None else 0, a_fin, out.status.data_ptr())
+    return _with_lengths(out, lengths)
+
+
+def _with_lengths(out: Beams, lengths) -> Beams:
+    # (a call without lengths writes none: what an earlier one left is taken away.  Once counted always counted, as a captured call may
+    # write lengths again at any time.)
+    if lengths is not None:
+        out.counted = True
+    elif out.counted:
+        out.length.zero_()
     return out
 
 

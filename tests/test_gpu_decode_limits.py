@@ -58,3 +58,19 @@ def test_token_dimensions_that_are_none(way):
     assert not isinstance(e.value, SystemError)
     torch.cuda.synchronize()
     assert torch.equal(state, keep)
+
+
+def test_no_lengths_of_an_earlier_call_remain(way):
+    x, s = torch.randn(2, 3, 50, device="cuda"), torch.zeros(2, 3, device="cuda")
+    n = torch.full((2, 3), 6, **I32)
+    out = G.beam_select(x, s, 4, lengths=n)
+    assert out.length.tolist() == [[7] * 4] * 2
+    assert G.beam_select(x, s, 4, out=out).length.tolist() == [[0] * 4] * 2
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        G.beam_select(x, s, 4, lengths=n, out=out)
+    for _ in range(2):
+        graph.replay()
+        assert out.length.tolist() == [[7] * 4] * 2
+        assert G.beam_select(x, s, 4, out=out).length.tolist() == [[0] * 4] * 2
