@@ -116,20 +116,23 @@ __device__ __forceinline__ int plan_find(GR_PTR(int) h_block, int size, int b)
 
 // What row r keeps: its numbers that depend on no other row's.
 struct PlanKeep { int status, parent, base, before, kept; };
-__device__ __forceinline__ PlanKeep plan_keep(const PlanArgs& A, int r)
+__device__ __forceinline__ PlanKeep plan_keep(const PlanArgs& A, int r, int* check)
 {
+    GR_PTR(const int) lengths = GR_MKPTR(const int, A.lengths, A.rows, check);
+    GR_PTR(const int) keeps = GR_MKPTR(const int, A.keep, A.rows, check);
+    GR_PTR(const int) parents = GR_MKPTR(const int, A.parents, A.rows, check);
     const long long most = (long long)A.width * A.block;
-    const long long own = A.lengths[r];
-    const int keep = A.keep ? max(0, A.keep[r]) : INT_MAX;
+    const long long own = lengths[r];
+    const int keep = A.keep ? max(0, keeps[r]) : INT_MAX;
     PlanKeep k;
     k.status = GR_OK;
     k.parent = r;
     long long len = own;
     if (A.parents) {
-        const int p = A.parents[r];
+        const int p = parents[r];
         if (p < -1 || p >= A.beams) k.status = GR_BAD_ROW;
         k.parent = p >= 0 && p < A.beams ? r / A.beams * A.beams + p : -1;
-        len = k.parent >= 0 ? A.lengths[k.parent] : 0;
+        len = k.parent >= 0 ? lengths[k.parent] : 0;
     }
     if (len < 0 || len > most) { k.status = GR_BAD_ROW; len = min(max(len, 0ll), most); }
     k.base = min((int)len, keep);
@@ -147,12 +150,16 @@ fork_kernel(const __grid_constant__ PlanArgs A)
     __shared__ PlanKeep s_row[W];
     __shared__ int s_bad[W], s_any;
     pdl_wait();
+    GR_CHECK_FLAG_DECL;
+    GR_CHECK_FLAG_INIT;
+    GR_PTR(int) table = GR_MKPTR(int, A.table, (long long)A.rows * A.width, GR_CHECK_FLAG);
+    GR_PTR(unsigned char) bad = GR_MKPTR(unsigned char, A.bad, (long long)A.splits * A.rows, GR_CHECK_FLAG);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, G = A.beams, N = A.num_blocks;
     const int r0 = blockIdx.x * G;
     if (tid == 0) s_any = 0;
     __syncthreads();
     if (tid < G) {
-        const PlanKeep k = plan_keep(A, r0 + tid);
+        const PlanKeep k = plan_keep(A, r0 + tid, GR_CHECK_FLAG);
         s_row[tid] = k;
         s_bad[tid] = 0;
         // (the columns that there is anything to do in: of a row that goes on from itself, those it releases)
@@ -167,8 +174,8 @@ fork_kernel(const __grid_constant__ PlanArgs A)
 #pragma unroll
         for (int j = 0; j < W; j++) {
             now[j] = was[j] = -1;
-            if (j < G && c < s_row[j].kept) now[j] = A.table[(long long)s_row[j].parent * A.width + c];
-            if (j < G && c < s_row[j].before) was[j] = A.table[(long long)(r0 + j) * A.width + c];
+            if (j < G && c < s_row[j].kept) now[j] = table[(long long)s_row[j].parent * A.width + c];
+            if (j < G && c < s_row[j].before) was[j] = table[(long long)(r0 + j) * A.width + c];
         }
 #pragma unroll
         for (int j = 0; j < W; j++) {
@@ -179,11 +186,12 @@ fork_kernel(const __grid_constant__ PlanArgs A)
             if (held ? was[j] == now[j] : !holds) continue;
             if (held) count_add(A.refs, N, was[j], -1);
             if (holds) count_add(A.refs, N, now[j], 1);
-            A.table[(long long)(r0 + j) * A.width + c] = now[j];
+            table[(long long)(r0 + j) * A.width + c] = now[j];
         }
     }
     __syncthreads();
-    if (tid < G) A.bad[(size_t)blockIdx.y * A.rows + r0 + tid] = (unsigned char)s_bad[tid];
+    // (bit 1: the bounds-checked build skipped an access)
+    if (tid < G) bad[(long long)blockIdx.y * A.rows + r0 + tid] = (unsigned char)(s_bad[tid] | (GR_CHECK_VALUE ? 2 : 0));
 }
 
 // blocks that a CTA looks through
@@ -204,8 +212,10 @@ __device__ __forceinline__ unsigned long long writer_rank(int tokens, int r) { r
 // each kind for them).
 // `fresh(k)`: the k-th free block; `first(r)`: number of row r's first token; `at(r)`: the row.
 template <int K, class Block, class First, class Row>
-__device__ __forceinline__ void write_slots(const PlanArgs& A, Block fresh, int total, long long thread, long long threads, First first, Row at)
+__device__ __forceinline__ void write_slots(const PlanArgs& A, Block fresh, int total, long long thread, long long threads, First first, Row at, int* check)
 {
+    GR_PTR(long long) slots = GR_MKPTR(long long, A.slots, A.max_tokens, check);
+    GR_PTR(int) positions = GR_MKPTR(int, A.positions, A.max_tokens, check);
     const int bs = A.block, R = A.rows;
     for (long long i0 = K * thread; i0 < A.max_tokens; i0 += K * threads) {
         long long slot[K];
@@ -242,14 +252,16 @@ __device__ __forceinline__ void write_slots(const PlanArgs& A, Block fresh, int 
             }
             slot[k] = (long long)block * bs + within;
         }
+#ifndef GR_CHECK
         if (K == 4 && A.wide && i0 + K <= A.max_tokens) {
             *reinterpret_cast<longlong2*>(A.slots + i0) = make_longlong2(slot[0], slot[K / 4]);
             *reinterpret_cast<longlong2*>(A.slots + i0 + 2) = make_longlong2(slot[K / 2], slot[K - 1]);
             *reinterpret_cast<int4*>(A.positions + i0) = make_int4(position[0], position[K / 4], position[K / 2], position[K - 1]);
-        } else {
-#pragma unroll
-            for (int k = 0; k < K; k++) if (i0 + k < A.max_tokens) { A.slots[i0 + k] = slot[k]; A.positions[i0 + k] = position[k]; }
+            continue;
         }
+#endif
+#pragma unroll
+        for (int k = 0; k < K; k++) if (i0 + k < A.max_tokens) { slots[i0 + k] = slot[k]; positions[i0 + k] = position[k]; }
     }
 }
 
@@ -277,6 +289,7 @@ plan_kernel(const __grid_constant__ PlanArgs A)
     GR_PTR(unsigned long long) best = GR_MKPTR(unsigned long long, A.best, A.num_blocks, GR_CHECK_FLAG);
     GR_PTR(int) writers = GR_MKPTR(int, A.writers, A.num_blocks, GR_CHECK_FLAG);
     GR_PTR(int) fresh = GR_MKPTR(int, A.fresh, A.num_blocks, GR_CHECK_FLAG);
+    GR_PTR(unsigned char) bad = GR_MKPTR(unsigned char, A.bad, (long long)A.splits * A.rows, GR_CHECK_FLAG);
     // near: the shared blocks that are written to, by open addressing (hash_size a power of two, twice the rows at least)
     const int hash_size = kNear ? plan_hash_size(R) : 1;
     GR_PTR(unsigned long long) h_best = GR_MKPTR(unsigned long long, reinterpret_cast<unsigned long long*>(s_dyn + sizeof(PlanRow) * (kNear ? R : 0)), hash_size, GR_CHECK_FLAG);
@@ -296,14 +309,14 @@ plan_kernel(const __grid_constant__ PlanArgs A)
         // (a thread with one row: its loads do not wait for the sum)
         const bool ahead = kNear && per == 1;
         PlanKeep k;
-        if (ahead && lo < hi) k = plan_keep(A, lo);
+        if (ahead && lo < hi) k = plan_keep(A, lo, GR_CHECK_FLAG);
         long long at = cta_scan(sum, s_part, total);
         for (int r = lo; r < hi; r++) {
             const int want = A.append[r];
             const long long from = at;
             at += max(0, want);
             if (!mine(r)) continue;
-            if (!ahead) k = plan_keep(A, r);
+            if (!ahead) k = plan_keep(A, r, GR_CHECK_FLAG);
             PlanRow q;
             q.status = want < 0 ? GR_BAD_ROW : k.status;
             q.parent = k.parent; q.base = k.base; q.before = k.before; q.kept = k.kept;
@@ -355,7 +368,15 @@ plan_kernel(const __grid_constant__ PlanArgs A)
     for (int r = lo; r < hi; r++) {
         if (!mine(r)) continue;
         PlanRow q = row[r];
-        if (A.parents) for (int y = 0; y < A.splits; y++) if (A.bad[(size_t)y * R + r]) q.status = GR_BAD_ROW;
+        if (A.parents) {
+            for (int y = 0; y < A.splits; y++) {
+                const int met = bad[(long long)y * R + r];
+                if (met & 1) q.status = GR_BAD_ROW;
+#ifdef GR_CHECK
+                if (met & 2) *GR_CHECK_FLAG = 1;
+#endif
+            }
+        }
         if (writes_within(q)) {
             const int b = r == lo ? first_last : table[(long long)r * A.width + q.base / bs];
             if (b < 0 || b >= N) q.status = GR_BAD_ROW;
@@ -465,9 +486,13 @@ plan_kernel(const __grid_constant__ PlanArgs A)
         const long long thread = (long long)me + (long long)ctas * tid, threads = (long long)ctas * kPlanThreads;
         auto first = [&](int r) { return row[r].first_token; };
         auto at = [&](int r) { return (PlanRow)row[r]; };
-        if (A.max_tokens <= 2 * threads) write_slots<1>(A, block_at, end, thread, threads, first, at);
-        else write_slots<4>(A, block_at, end, thread, threads, first, at);
+        if (A.max_tokens <= 2 * threads) write_slots<1>(A, block_at, end, thread, threads, first, at, GR_CHECK_FLAG);
+        else write_slots<4>(A, block_at, end, thread, threads, first, at, GR_CHECK_FLAG);
     }
+#ifdef GR_CHECK
+    plan_barrier();
+    if (tid == 0 && GR_CHECK_VALUE && R > 0) A.status[0] = GR_CHECK_FAILED;
+#endif
 }
 
 // the slots of many tokens, by all SMs
@@ -476,14 +501,24 @@ slots_kernel(const __grid_constant__ PlanArgs A)
 {
     __shared__ int s_first[kPlanNear], s_free[kPlanCluster];
     pdl_wait();
+    GR_CHECK_FLAG_DECL;
+    GR_CHECK_FLAG_INIT;
     const bool near = A.rows <= kPlanNear;
+    GR_PTR(PlanRow) row = GR_MKPTR(PlanRow, A.row, A.rows, GR_CHECK_FLAG);
+    GR_PTR(int) fresh = GR_MKPTR(int, A.fresh, A.num_blocks, GR_CHECK_FLAG);
+    GR_PTR(int) firsts = GR_MKPTR(int, s_first, kPlanNear, GR_CHECK_FLAG);
     if (threadIdx.x < kPlanCluster) s_free[threadIdx.x] = A.part[threadIdx.x];
-    if (near) for (int r = threadIdx.x; r < A.rows; r += kSlotThreads) s_first[r] = A.row[r].first_token;
+    if (near) for (int r = threadIdx.x; r < A.rows; r += kSlotThreads) firsts[r] = row[r].first_token;
     __syncthreads();
-    GR_PTR(int) fresh = GR_MKPTR(int, A.fresh, A.num_blocks, nullptr);
     const int share = plan_share(A.num_blocks);
+    auto first = [&](int r) { return near ? (int)firsts[r] : row[r].first_token; };
+    auto at = [&](int r) { return (PlanRow)row[r]; };
     write_slots<4>(A, [&](int k) { return fresh_at(fresh, s_free, share, k); }, A.offsets[A.rows], (long long)blockIdx.x * kSlotThreads + threadIdx.x, (long long)gridDim.x * kSlotThreads,
-                [&](int r) { return near ? s_first[r] : A.row[r].first_token; }, [&](int r) { return A.row[r]; });
+                   first, at, GR_CHECK_FLAG);
+#ifdef GR_CHECK
+    __syncthreads();
+    if (threadIdx.x == 0 && GR_CHECK_VALUE && A.rows > 0) A.status[0] = GR_CHECK_FAILED;
+#endif
 }
 
 static size_t plan_layout(int rows, int num_blocks, char* ws, PlanArgs* A)

@@ -16,9 +16,25 @@ static_assert(kCopyThreads == 1 << 8, "a team of all threads");
 constexpr int kCopyColumns = 4;            // vectors of a block per thread
 constexpr int kMostTeams = 16;             // teams of a CTA
 
+// Bounds-checked build: an access outside a tensor's first and last bytes, or across a piece's end, is skipped and noted in a word that
+// gr_states_check reads (these operators have no status).
+#ifdef GR_CHECK
+__device__ int g_states_check;
+__device__ __forceinline__ bool within(const char* p, long long n, const char* base, long long span, long long column, long long piece)
+{
+    if (p >= base && p + n <= base + span && column >= 0 && column + n <= piece) return true;
+    g_states_check = 1;
+    return false;
+}
+#define GR_WITHIN(...) within(__VA_ARGS__)
+#else
+#define GR_WITHIN(...) true
+#endif
+
 struct ReorderArgs {
     const char* src[kStatesPerLaunch];
     char* dst[kStatesPerLaunch];
+    long long src_span, dst_span;          // bytes from a tensor's first to its last
     gr_state_layout at;
     int in_place, team_shift;              // threads of a team: 1 << team_shift
     long long tokens;                      // of a piece (with lengths)
@@ -87,7 +103,7 @@ reorder_kernel(const __grid_constant__ ReorderArgs A, const int* __restrict__ pa
 #pragma unroll
                 for (int c = 0; c < C; c++) {
                     // (a vector that holds the last used byte is read whole: pieces are a multiple of kVec long)
-                    if (tid * kVec + c * kStep < s_left[j]) v[c][j] = *reinterpret_cast<const Vec*>(s_from[j] + tid * kVec + c * kStep);
+                    if (tid * kVec + c * kStep < s_left[j] && GR_WITHIN(s_from[j] + tid * kVec + c * kStep, kVec, A.src[s], A.src_span, start + tid * kVec + c * kStep, L.part_bytes)) v[c][j] = *reinterpret_cast<const Vec*>(s_from[j] + tid * kVec + c * kStep);
                 }
             }
 #pragma unroll
@@ -96,6 +112,7 @@ reorder_kernel(const __grid_constant__ ReorderArgs A, const int* __restrict__ pa
                 for (int c = 0; c < C; c++) {
                     const int more = s_left[j] - tid * kVec - c * kStep;
                     char* to = dst + j * L.dst_beam + c * kStep;
+                    if (more > 0 && !GR_WITHIN(to, min(more, kVec), A.dst[s], A.dst_span, start + tid * kVec + c * kStep, L.part_bytes)) continue;
                     if (more >= kVec) *reinterpret_cast<Vec*>(to) = v[c][j];
                     else if (more > 0) store_bytes(to, v[c][j], more);
                 }
@@ -152,7 +169,7 @@ reorder_short_kernel(const __grid_constant__ ReorderArgs A, const int* __restric
 #pragma unroll
                 for (int c = 0; c < C; c++) {
                     // (a vector that holds the last used byte is read whole: pieces are a multiple of kVec long)
-                    if (at * kVec + c * step < s_left[team][j]) v[c][j] = *reinterpret_cast<const Vec*>(s_from[team][j] + at * kVec + c * step);
+                    if (at * kVec + c * step < s_left[team][j] && GR_WITHIN(s_from[team][j] + at * kVec + c * step, kVec, A.src[s], A.src_span, start + at * kVec + c * step, L.part_bytes)) v[c][j] = *reinterpret_cast<const Vec*>(s_from[team][j] + at * kVec + c * step);
                 }
             }
 #pragma unroll
@@ -161,6 +178,7 @@ reorder_short_kernel(const __grid_constant__ ReorderArgs A, const int* __restric
                 for (int c = 0; c < C; c++) {
                     const int more = s_left[team][j] - at * kVec - c * step;
                     char* to = dst + j * L.dst_beam + c * step;
+                    if (more > 0 && !GR_WITHIN(to, min(more, kVec), A.dst[s], A.dst_span, start + at * kVec + c * step, L.part_bytes)) continue;
                     if (more >= kVec) *reinterpret_cast<Vec*>(to) = v[c][j];
                     else if (more > 0) store_bytes(to, v[c][j], more);
                 }
@@ -210,9 +228,9 @@ copy_blocks_kernel(const __grid_constant__ CopyArgs A)
         char* out = cache + s_dst[k] * A.stride + first;
         Vec v[C];
 #pragma unroll
-        for (int c = 0; c < C; c++) if (first + c * step < A.bytes) v[c] = *reinterpret_cast<const Vec*>(in + c * step);
+        for (int c = 0; c < C; c++) if (first + c * step < A.bytes && GR_WITHIN(in + c * step, kVec, cache, A.stride * (A.num_blocks - 1) + A.bytes, first + c * step, A.bytes)) v[c] = *reinterpret_cast<const Vec*>(in + c * step);
 #pragma unroll
-        for (int c = 0; c < C; c++) if (first + c * step < A.bytes) *reinterpret_cast<Vec*>(out + c * step) = v[c];
+        for (int c = 0; c < C; c++) if (first + c * step < A.bytes && GR_WITHIN(out + c * step, kVec, cache, A.stride * (A.num_blocks - 1) + A.bytes, first + c * step, A.bytes)) *reinterpret_cast<Vec*>(out + c * step) = v[c];
     }
 }
 
@@ -360,6 +378,16 @@ static void launch_reorder(const ReorderArgs& A, int count, int vec, const int* 
 
 extern "C" {
 
+#ifdef GR_CHECK
+// whether an access was skipped since the last call of this (-1: it cannot be read)
+int gr_states_check(void)
+{
+    int met = -1, none = 0;
+    if (cudaMemcpyFromSymbol(&met, gr::g_states_check, sizeof(int)) != cudaSuccess || cudaMemcpyToSymbol(gr::g_states_check, &none, sizeof(int)) != cudaSuccess) return -1;
+    return met;
+}
+#endif
+
 int gr_reorder_states(const void* const* src, void* const* dst, int count, const gr_state_layout* layout,
                       const int* parents, const int* lengths, void* stream)
 {
@@ -397,6 +425,7 @@ int gr_reorder_states(const void* const* src, void* const* dst, int count, const
     for (int lo = 0; lo < count; lo += gr::kStatesPerLaunch) {
         gr::ReorderArgs A;
         A.at = L; A.in_place = in_place;
+        A.src_span = from_span; A.dst_span = to_span;
         A.tokens = lengths ? L.part_bytes / L.token_bytes : 0;
         const int n = std::min(count - lo, gr::kStatesPerLaunch);
         for (int i = 0; i < n; i++) { A.src[i] = (const char*)src[lo + i]; A.dst[i] = (char*)dst[lo + i]; }
