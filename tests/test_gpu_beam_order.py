@@ -151,3 +151,32 @@ def test_penalties_and_finished_hypotheses(dtype, B, W, V):
         n, done = n.cuda(), done.cuda()
         K = min(W + 3, int((~done).sum(1).min()) * V + 1)
         check_order(G.beam_select(x, s, K, lengths=n, done=done, eos=9, length_penalty=penalty), x, s, K, 1.0, n, done, 9, penalty)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_long_lists_in_many_groups(dtype):
+    """As many groups as leave what they cannot tell apart to clusters, with the longest lists there are, beside groups without a doubt
+    and groups that are of no use."""
+    B, W, V, K = 90, 32, 1500, 128
+    g = torch.Generator().manual_seed(6)
+    x = (10.0 * torch.randn(B, W, 1, generator=g)).expand(B, W, V).to(dtype)
+    x = x + torch.randn(B, W, V, generator=g).to(dtype) * (torch.arange(B) % 3 == 0).view(B, 1, 1)
+    x = x.cuda()
+    s = near_scores(x, 1.0, g)
+    x[7, 3, 11] = math.nan
+    s[8] = -math.inf
+    x[9] = 1e32 * (1 + torch.rand(W, V, generator=g).to(dtype).cuda())
+    r = G.beam_select(x, s, K)
+    want = torch.tensor([G.GR_OK] * B)
+    want[7] = G.GR_BAD_LOGITS
+    assert torch.equal(r.status.cpu().long(), want)
+    assert r.token[7:9].unique().tolist() == [-1] and r.parent[7:9].unique().tolist() == [-1]
+    good = [b for b in range(B) if b not in (7, 8, 9)]
+
+    def part(rows):
+        return type(r)(*[getattr(r, n)[rows] for n in ("token", "parent", "score", "length", "done", "status")], r.workspace, r.shape)
+
+    check_order(part(good), x[good], s[good], K)
+    one, t = x[9:10].contiguous(), s[9:10].contiguous()
+    for got in (part([9]), G.beam_select(one, t, K)):
+        check(got, reference(one, t, K), K, V)
