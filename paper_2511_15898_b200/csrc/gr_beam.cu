@@ -445,7 +445,7 @@ struct BeamGroup {
     unsigned char again[GR_MAX_BEAMS];         // the row's sum is to be taken again (2: it was of no use)
     unsigned char exact[GR_MAX_BEAMS];         // ... and has been
     int bad, check, survivors, redo;
-    double err[GR_MAX_BEAMS];                  // bound of the error of the row's log-sum
+    double err[GR_MAX_BEAMS];                  // bound of the error of the row's keys by that of its log-sum
     unsigned long long least;                  // a bound below the last key that is taken (as an integer that orders like it)
     double slack;                              // the largest distance of keys at which sums are taken again
     int best_at[GR_MAX_SELECT + 1];
@@ -648,7 +648,7 @@ __device__ __forceinline__ void choose(const BeamArgs& A, BeamGroup& g, unsigned
                     // (the shares to 1e-5 on the side of the larger bound; two units in ten for the products of s_lo)
                     const float p = fminf(1.f, __expf((float)((double)first / A.temp - lse))), q = fminf(1.f, 1.f - p + 1e-5f);
                     const float depth = 1.2f + q * (log2f((float)A.V / q) - (float)units + 2.f);
-                    g.err[w] = kErrSum + kErrDepth * (double)depth + kErrRef * fabs((double)top);
+                    g.err[w] = key_of(w, kErrSum + kErrDepth * (double)depth + kErrRef * fabs((double)top));
                 }
             } else if (g.kind[w] == kRowDone) {
                 // a finished hypothesis has one continuation, in its first part's list
@@ -658,7 +658,7 @@ __device__ __forceinline__ void choose(const BeamArgs& A, BeamGroup& g, unsigned
             g.lse[w] = lse;
             if (g.again[w]) g.redo = 1;
         }
-        double largest = tid < W ? 2.0 * key_of(tid, g.err[tid]) : 0.0;
+        double largest = tid < W ? 2.0 * g.err[tid] : 0.0;
 #pragma unroll 1
         for (int o = 16; o > 0; o >>= 1) largest = fmax(largest, __shfl_xor_sync(0xffffffffu, largest, o));
         if (tid == 0) g.slack = largest;
@@ -765,7 +765,7 @@ __device__ __forceinline__ void choose(const BeamArgs& A, BeamGroup& g, unsigned
             const int e = i < pairs ? g.best_at[i] : i - pairs, f = g.best_at[i < pairs ? i + 1 : K - 1];
             const int w = sv_row[e], v = sv_row[f];
             if (w == v) continue;
-            if (fabs(unsortable(sv[e].x) - unsortable(sv[f].x)) > key_of(w, g.err[w]) + key_of(v, g.err[v])) continue;
+            if (fabs(unsortable(sv[e].x) - unsortable(sv[f].x)) > g.err[w] + g.err[v]) continue;
 #pragma unroll 1
             for (int side = 0; side < 2; side++) {
                 const int at = side ? f : e, row = side ? v : w;
