@@ -314,8 +314,8 @@ int gr_read_slice(const void* params, const int* draft_tokens, int batch, int n,
  * a finished hypothesis (done[b, w] != 0) has the one continuation `eos`, with total = scores[b, w] and
  * L = max(1, lengths[b, w]); its logits are not read.  The `select` largest keys are returned in descending
  * order; equal keys: the smaller w first, then the larger logit, then the smaller v.  Keys are compared as
- * 64-bit values; where two hypotheses' continuations come so close that the streaming pass's sums may not tell
- * them apart, their rows' sums are taken again in 64 bits.
+ * 64-bit values (of temperature and length_penalty as the call takes them, rounded to float); where two hypotheses'
+ * continuations come closer than the bounds of the streaming pass's errors, their rows' sums are taken again in 64 bits.
  *   logits   [batch, beams, V], dtype GR_F32 or GR_BF16: row (b, w) begins (b * beams + w) * ld elements after
  *            the base pointer (aligned to the element), ld >= V.  -infinity masks a token: it is never returned, and
  *            a row may be masked as a whole.  NaN or +infinity in a row that is read: GR_BAD_LOGITS.
@@ -400,7 +400,8 @@ int gr_reorder_states(const void* const* src, void* const* dst, int count, const
  *   status    out [rows].
  *   workspace gr_block_workspace_bytes() bytes, 16-byte aligned.
  *   rows a multiple of beams, 1 <= beams <= GR_MAX_BEAMS (beams only matters with parents), rows <= 2^20,
- *   rows * width < 2^31, num_blocks <= 2^26, width * block_size < 2^31.  The arrays must not overlap one another.
+ *   rows * width < 2^31, num_blocks <= 2^26, width * block_size < 2^31.  The arrays must not overlap one another (but keep
+ *             may be lengths).
  */
 size_t gr_block_workspace_bytes(int rows, int num_blocks);
 int gr_block_plan(int* table, int rows, int width, int beams, int block_size, int* lengths, int* refs, int num_blocks,

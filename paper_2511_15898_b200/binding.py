@@ -583,7 +583,7 @@ def beam_select(logits: torch.Tensor, scores: torch.Tensor, select: Optional[int
                 length_penalty: float = 0.0, out: Optional[Beams] = None) -> Beams:
     """gr_beam_select on torch CUDA tensors: logits [B, beams, V] float32 or bfloat16 (rows at any one distance, elements
     next to one another), scores [B, beams] float32, lengths [B, beams] int32, done [B, beams] bool or uint8.  `select`
-    defaults to the number of beams.  `out`: a result of an earlier call of the same shape, written again (it must not
+    defaults to the number of beams; temperature and length_penalty are rounded to float32, as the C call takes them.  `out`: a result of an earlier call of the same shape, written again (it must not
     be read from by this call: scores, lengths and done are other tensors)."""
     if not (isinstance(logits, torch.Tensor) and logits.is_cuda and logits.dim() == 3):
         raise GrError("logits must be a [B, beams, V] CUDA tensor")
@@ -657,7 +657,7 @@ def reorder_states(states, parents: torch.Tensor, lengths: Optional[torch.Tensor
                    token_dim: Optional[int] = None, out=None):
     """gr_reorder_states on torch CUDA tensors: `states` is a list of tensors [B, beams, ...] (of any types and layouts),
     parents [B, chosen] int32.  In place, with chosen <= beams, unless `out` (a list of tensors [B, chosen, ...]) is
-    given, which must not meet the states in memory.  With lengths [B, beams] int32 the dimension `token_dim` of the
+    given, which must not meet the states in memory.  Tensors that share a byte with one another are refused.  With lengths [B, beams] int32 the dimension `token_dim` of the
     states counts tokens, of which each parent's first lengths[b, parent] are copied.  Returns `out` or `states`."""
     if _short("reorder", "gr_reorder_states", states, parents, lengths, token_dim, out):
         return states if out is None else out
@@ -764,7 +764,7 @@ class BlockPlan:
 def block_plan(tables: BlockTables, append: torch.Tensor, max_tokens: int, keep: Optional[torch.Tensor] = None,
                parents: Optional[torch.Tensor] = None, out: Optional[BlockPlan] = None) -> BlockPlan:
     """gr_block_plan on torch CUDA tensors: `tables` is updated in place; append, keep [rows] int32, parents [rows] or
-    [rows / beams, beams] int32 (row numbers within the group, as beam_select returns them)."""
+    [rows / beams, beams] int32 (row numbers within the group, as beam_select returns them).  keep may be tables.lengths itself."""
     if (out is not None and isinstance(tables.table, torch.Tensor) and isinstance(tables.refs, torch.Tensor)
             and out.shape == (*tables.table.shape[:1], *tables.refs.shape, max_tokens)
             and _short("plan", "gr_block_plan", tables.table, tables.lengths, tables.refs, tables.block_size, tables.beams, append,
@@ -804,7 +804,7 @@ def block_plan(tables: BlockTables, append: torch.Tensor, max_tokens: int, keep:
 
 def copy_blocks(caches, copy_src: torch.Tensor, copy_dst: torch.Tensor) -> None:
     """gr_copy_blocks on torch CUDA tensors: `caches` is a list of tensors [num_blocks, ...] whose blocks are contiguous,
-    copy_src and copy_dst [pairs] int32 as block_plan returns them."""
+    copy_src and copy_dst [pairs] int32 as block_plan returns them.  Caches that share a byte with one another are refused."""
     if _short("copy", "gr_copy_blocks", caches, copy_src, copy_dst):
         return
     caches = list(caches)

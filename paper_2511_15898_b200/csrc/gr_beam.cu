@@ -26,8 +26,8 @@
 //   s            known to 2^-48 of itself: 2^-46 |R|.
 // Together 1e-6 to 2e-6 a row (measured on rows of one value, of two, of whole numbers and of normal ones: 5.5e-7 at most).
 //
-// HBM bounds it in fp32 (128 groups of 8 rows of 128256: 93 us, 87 % of the measured copy rate), issue slots and the exponentials' pipe
-// in bf16 (256 groups of 16 rows of 152064: 244 us, 79 %), latency where there are few rows (4 of 32000: 11.4 us).
+// HBM bounds it in fp32 (128 groups of 8 rows of 128256: 95 us, 86 % of the measured copy rate), issue slots and the exponentials' pipe
+// in bf16 (256 groups of 16 rows of 152064: 245 us, 78 %), latency where there are few rows (4 of 32000: 12.1 us).
 #include <limits.h>
 #include <math.h>
 #include <algorithm>
@@ -307,7 +307,7 @@ beam_stream_kernel(const __grid_constant__ BeamArgs A)
                     const float down = ref == -INFINITY ? 0.f : -ref;
                     const unsigned long long down2 = f_pack(down, down);
                     // (a vector's sum, then those of the vectors, in fp32 by halves: equal terms one after another in one sum would
-                    // round the same way each time.  By halves in bf16 too: 259 -> 271 us for 256 groups of 16 rows of 152064, by its registers)
+                    // round the same way each time.  By halves in bf16 too: 262 -> 279 us for 256 groups of 16 rows of 152064, by its registers)
                     unsigned long long sum2[U];
 #pragma unroll
                     for (int u = 0; u < U; u++) {
@@ -884,11 +884,11 @@ static int launch_beam(const BeamArgs& A, int batch, cudaStream_t st)
         }
     }
     // More than one wave of four CTAs per SM: eight smaller ones (a row's thresholds and its selection at the end leave gaps that
-    // seven other rows fill better than three: 1024 rows of 50257 fp32 65 -> 57 us, of 128256 110 -> 103).  In fp32 where they do not
+    // seven other rows fill better than three: 1024 rows of 50257 fp32 58 -> 49 us, of 128256 115 -> 108).  In fp32 where they do not
     // leave a larger part of their last wave empty or where there are more than two waves of them (1200 rows of 128256, just over
-    // one wave, 138 -> 152); in bf16, which waits for instructions and not for bytes, always, and twelve per SM where that saves a
-    // quarter of the waves (1200 rows of 128256 84 us by four, 89 by eight, 77 by twelve; 2000 rows 120, 113, 123; 4096 of 152064 270,
-    // 253, 244).  The smaller ones' lists hold 4 A + 5 deviations up to 48 keys.
+    // one wave, 131 -> 143); in bf16, which waits for instructions and not for bytes, always, and twelve per SM where that saves a
+    // quarter of the waves (1200 rows of 128256 88 us by four, 93 by eight, 81 by twelve; 2000 rows 124, 117, 126; 4096 of 152064 261,
+    // 244, 233).  The smaller ones' lists hold 4 A + 5 deviations up to 48 keys.
     const int ctas = batch * A.beams * A.parts;
     auto waves = [&](int per) { return (ctas + per * kSms - 1) / (per * kSms); };
     constexpr bool kNarrow = sizeof(T) == 2;
