@@ -24,6 +24,7 @@
 //                largest where all but the first token are alike: with p1 the first's share and q = 1 - p1 the others',
 //                E max(|y|, 1) <= p1 + q (log2(V / q) - log2 Z + 2)   (y <= 1, and R only rises).
 //   s            known to 2^-48 of itself: 2^-46 |R|.
+// and of a key 2^-51 of itself, as 64-bit roundings may fall on the other side.
 // Together 1e-6 to 2e-6 a row (measured on rows of one value, of two, of whole numbers and of normal ones: 5.5e-7 at most).
 //
 // HBM bounds it in fp32 (128 groups of 8 rows of 128256: 95 us, 86 % of the measured copy rate), issue slots and the exponentials' pipe
@@ -43,6 +44,7 @@ constexpr int kBeamMaxLists = 256;             // rows of a group times parts
 constexpr int kBeamMaxListed = 4096;           // entries of a group's lists
 static_assert(GR_MAX_BEAMS * GR_MAX_SELECT <= kBeamMaxListed && GR_MAX_SELECT <= kMaxSupport, "lists");
 constexpr double kErrSum = 1.46e-7 + 7.0 / 16777216, kErrDepth = 0.69314718055994530942 / 8388608, kErrRef = 1.0 / (1ll << 46);
+constexpr double kErrKey = 1.0 / (1ll << 51);  // a key's roundings, in which an error of the sum may tell
 constexpr float kLargestRef = 1048576.f;       // (products of s_lo stay below 1/8, and R + kRise is a number)
 constexpr int kSettle = 8;                     // most CTAs of a cluster that takes sums again
 constexpr float kRise = 1.f;
@@ -721,7 +723,7 @@ __device__ __forceinline__ void choose(const BeamArgs& A, BeamGroup& g, unsigned
         }
         __syncthreads();
         // (those a little below the bound too: they may have to be told from the last ones)
-        const double least = unsortable(g.least) - g.slack;
+        const double bound = unsortable(g.least), least = bound - (g.slack + 2.0 * kErrKey * fabs(bound));
         for (int e = tid; e < most; e += kBeamThreads) {
             const int l = e >> shift;
             if ((e & ((1 << shift) - 1)) < g.count[l] && !(key[e] < least)) {
@@ -765,7 +767,8 @@ __device__ __forceinline__ void choose(const BeamArgs& A, BeamGroup& g, unsigned
             const int e = i < pairs ? g.best_at[i] : i - pairs, f = g.best_at[i < pairs ? i + 1 : K - 1];
             const int w = sv_row[e], v = sv_row[f];
             if (w == v) continue;
-            if (fabs(unsortable(sv[e].x) - unsortable(sv[f].x)) > g.err[w] + g.err[v]) continue;
+            const double key_e = unsortable(sv[e].x), key_f = unsortable(sv[f].x);
+            if (fabs(key_e - key_f) > g.err[w] + g.err[v] + kErrKey * (fabs(key_e) + fabs(key_f))) continue;
 #pragma unroll 1
             for (int side = 0; side < 2; side++) {
                 const int at = side ? f : e, row = side ? v : w;

@@ -180,3 +180,22 @@ def test_long_lists_in_many_groups(dtype):
     one, t = x[9:10].contiguous(), s[9:10].contiguous()
     for got in (part([9]), G.beam_select(one, t, K)):
         check(got, reference(one, t, K), K, V)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_totals_whose_units_are_larger_than_the_errors_of_sums(dtype):
+    """Totals of -1e11, which 64 bits hold to 1.5e-5: rows of equal log-probabilities tie, though an error of 1e-7 may carry one of them
+    to the next number."""
+    B, W, V = 400, 8, 3001
+    g = torch.Generator().manual_seed(9)
+    x = (torch.randint(-64, 65, (B, W, 1), generator=g) / 8.0).expand(B, W, V).contiguous()
+    x[:, :, V // 3] += torch.randint(4, 40, (B, 1), generator=g) / 8.0
+    if dtype == torch.float32:
+        x[:, :, V // 3] += torch.randint(0, 1024, (B, 1), generator=g) / 8192.0
+    y = x.to(dtype)
+    assert torch.equal(y.float(), x)
+    y, s = y.cuda(), torch.full((B, W), -1e11, device="cuda")
+    r = G.beam_select(y, s, W)
+    torch.cuda.synchronize()
+    assert torch.equal(r.parent.cpu(), torch.arange(W, dtype=torch.int32).expand(B, W))
+    assert r.token.unique().tolist() == [V // 3]
