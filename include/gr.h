@@ -304,6 +304,7 @@ int gr_read_slice(const void* params, const int* draft_tokens, int batch, int n,
  * tokens), and what a serving loop does with the outcome of either rule -- hypotheses, drafted or searched,
  * go on from a parent's state, in dense states (gr_reorder_states) or in a paged cache (gr_block_plan,
  * gr_copy_blocks).  (The paper has no counterpart.)  Conventions as above.
+ * A workspace is scratch of one call: calls that may run at the same time (other streams, captured graphs) need one each.
  * ------------------------------------------------------------------------------------------------
  *
  * gr_beam_select -- the best continuations of every group of `beams` hypotheses.
