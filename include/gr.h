@@ -34,6 +34,9 @@ extern "C" {
 /* element type of the logits */
 #define GR_F32  0
 #define GR_BF16 1
+/* further element types of caches, and of what goes in and comes out of them */
+#define GR_F16  2
+#define GR_Q4   3
 
 /* per-instance status values (status arrays, device memory) */
 #define GR_OK                    0
@@ -51,7 +54,8 @@ extern "C" {
 #define GR_NO_BLOCKS             8  /* gr_block_plan: the pool has too few free blocks for the row         */
 #define GR_ROW_FULL              9  /* gr_block_plan: more tokens than the row's table or the slot map hold */
 #define GR_BAD_ROW              10  /* gr_block_plan: a negative count, a length beyond the table, a parent outside
-                                       the group, or a block id outside the pool                            */
+                                       the group, or a block id outside the pool; gr_cache_attend: a position
+                                       beyond the table, or a block id outside the pool                     */
 
 /* host-side argument errors (return values) */
 #define GR_E_INVALID   (-1)  /* a size, temperature or option is out of range */
@@ -64,7 +68,11 @@ extern "C" {
 #define GR_MAX_SUPPORT 128   /* largest draft support for which the convex programs are solved */
 #define GR_MAX_DRAFTS  32    /* largest n                                                     */
 #define GR_MAX_BEAMS   32    /* largest number of hypotheses in a group                       */
-#define GR_MAX_SELECT  128   /* most continuations gr_beam_select returns for a group         */
+#define GR_MAX_SELECT  128   /* most continuations gr_beam_select returns for a group, alternatives gr_token_logprobs returns */
+#define GR_MAX_GIVEN   64    /* most tokens a row of gr_token_logprobs                        */
+#define GR_MAX_HEADS   1024  /* most heads of a cache, and of queries                         */
+#define GR_MAX_DIM     512   /* largest dim of a head in a 16- or 32-bit cache                */
+#define GR_MAX_DIM_Q4  256   /* in a 4-bit cache                                              */
 
 /*
  * Solver options (host struct, read during the call).  NULL selects the defaults.
@@ -422,6 +430,68 @@ int gr_block_plan(int* table, int rows, int width, int beams, int block_size, in
  */
 int gr_copy_blocks(void* const* caches, int count, int num_blocks, long long block_stride, long long block_bytes,
                    const int* copy_src, const int* copy_dst, int pairs, void* stream);
+
+/*
+ * ------------------------------------------------------------------------------------------------
+ * Filling and reading a paged cache: what gr_block_plan's slots, positions and offsets are for.
+ *
+ * A cache holds keys and values of `heads` heads of `dim` elements for num_blocks blocks of block_size tokens; slot
+ * z is token z % block_size of block z / block_size.
+ *   format GR_F32, GR_BF16, GR_F16: two arrays, in each of which (block, token, head) begins block * block_stride + token * token_stride +
+ *       head * head_stride elements after the pointer.  dim even, <= GR_MAX_DIM.  No two places may share an element.
+ *   format GR_Q4: one array (`keys`; `values` is not looked at), aligned to 16 bytes; block b begins b * block_stride BYTES after it (a
+ *       multiple of 16; the other strides are not looked at) and holds, for each head, block_size / 8 octets of 9 dim bytes,
+ *       one after another.  dim a multiple of 32, <= GR_MAX_DIM_Q4, block_size a multiple of 8.
+ *       Groups of 32 dims share a 16-bit scale s; a number x is held as a code u of 4 bits that stands for s (u - 8):
+ *       s = fp16(-x* / 8), x* the group's element of largest magnitude (of +a and -a the positive one; beyond 524032: clamped), u = 8 + x / s
+ *       rounded to the nearest whole number (ties to even), from 0 to 15.  4.5 bits an element.  A group with a NaN or an infinity
+ *       has the scale NaN.  With J = dim / 32, an octet (eight tokens of a head) holds, one after another,
+ *         keys' codes    [8 tokens][4][J] words: word (t, j): dims 32 j + 8 t .. + 7, the first in its lowest bits
+ *         keys' scales   [8 tokens][J] fp16
+ *         values' codes  [8][4 pairs of tokens][J][2 tokens] 16-bit words: word (g, ., j, .): dims 32 j + 4 g .. + 3
+ *         values' scales [4 pairs of tokens][J][2 tokens] fp16
+ *       A block is whole bytes of its own, as gr_copy_blocks wants it; bytes of different tokens are different bytes.
+ *   heads <= GR_MAX_HEADS.
+ */
+typedef struct gr_cache_layout {
+    int       format, heads, dim, block_size, num_blocks;
+    long long block_stride, token_stride, head_stride;
+} gr_cache_layout;
+
+/*
+ * gr_cache_append -- new tokens' keys and values go to their slots, keys and queries rotated by the tokens' positions on the way.
+ *
+ * Token i with slot z = slots[i] (outside the cache, -1 say: nothing is written to the cache) and position p = positions[i]:
+ * of the first `rot` dims of a key or query, pair c is turned by the angle p * frequencies[c],
+ *   a' = a cos - b sin,  b' = b cos + a sin,
+ * with (a, b) dims (c, c + rot / 2), or (2 c, 2 c + 1) if `interleaved`.  The angle is a 64-bit number, its cosine and sine are rounded to
+ * 32 bits, products and sums are rounded to 32 bits one by one, the result once more, to what holds it.
+ *   k, v      [tokens, heads, dim] of type dtype (GR_F32, GR_BF16, GR_F16): (i, h) begins i * k_token + h * k_head elements after k.
+ *   q, q_out  [tokens, q_heads, dim] likewise, of the same type; q_heads 0: there are none.  Queries of tokens with a negative position
+ *             are left as they were in q_out.  q_out may be q, with equal strides; no other array that is written may share a byte with one that
+ *             is read or another that is written, and no two places of q_out may share one.
+ *   slots     [tokens], no slot twice.     positions [tokens]: not looked at (and may be NULL) without frequencies, that is rot 0.
+ *   rot       even, 0 .. dim.              frequencies [rot / 2] double.
+ * Any alignment to the element works; pointers and strides that are multiples of 16 bytes are fastest.
+ */
+typedef struct gr_cache_tokens {
+    const void *k, *v, *q;
+    void*     q_out;
+    int       dtype, q_heads;
+    long long k_token, k_head, v_token, v_head, q_token, q_head, out_token, out_head;
+} gr_cache_tokens;
+int gr_cache_append(void* keys, void* values, const gr_cache_layout* layout, const gr_cache_tokens* in, int tokens,
+                    const long long* slots, const int* positions, const double* frequencies, int rot, int interleaved,
+                    void* stream);
+
+/*
+ * gr_cache_read -- keys and values of listed slots, as numbers: k[i], v[i] become what slot slots[i] holds, rounded once to dtype (GR_F32,
+ * GR_BF16, GR_F16); zeros for a slot outside the cache.  A slot may be listed any number of times.
+ *   k, v   [tokens, heads, dim]: (i, h) begins i * k_token + h * k_head elements after k, and likewise for v.  No two places may share an element.
+ */
+int gr_cache_read(const void* keys, const void* values, const gr_cache_layout* layout, const long long* slots, int tokens,
+                  int dtype, void* k, long long k_token, long long k_head, void* v, long long v_token, long long v_head,
+                  void* stream);
 
 /* Text for a GR_* / GR_E_* code (host pointer to a static string). */
 const char* gr_strerror(int code);

@@ -8,6 +8,8 @@ from .binding import (GR_F32, GR_BF16, GR_OK, GR_NOT_CONVERGED, GR_SUPPORT_TOO_L
                       GR_NO_BLOCKS, GR_ROW_FULL, GR_BAD_ROW, GR_MAX_BEAMS, GR_MAX_SELECT, StateLayout,
                       gr_beam_workspace_bytes, gr_beam_select, gr_reorder_states, gr_block_workspace_bytes,
                       gr_block_plan, gr_copy_blocks, Beams, beam_select, reorder_states, BlockTables, BlockPlan,
-                      block_plan, copy_blocks)
+                      block_plan, copy_blocks,
+                      GR_F16, GR_Q4, GR_MAX_GIVEN, GR_MAX_HEADS, GR_MAX_DIM, GR_MAX_DIM_Q4, CacheLayout, CacheTokens, gr_cache_append,
+                      gr_cache_read, KVCache, cache_append, cache_read)
 
 __all__ = [n for n in dir() if not n.startswith("_")]

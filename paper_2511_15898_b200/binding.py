@@ -18,12 +18,14 @@ from typing import Optional, Tuple
 import torch
 
 GR_F32, GR_BF16 = 0, 1
+GR_F16, GR_Q4 = 2, 3
 GR_OK, GR_NOT_CONVERGED, GR_SUPPORT_TOO_LARGE, GR_BAD_LOGITS, GR_DRAFT_OUT_OF_SUPPORT, GR_STALE_PARAMS = range(6)
 GR_MAX_SUPPORT, GR_MAX_DRAFTS = 128, 32
 GR_STATIC_MAX_BATCH = 256
 GR_PARTIAL_RULE = 6
 GR_NO_BLOCKS, GR_ROW_FULL, GR_BAD_ROW = 8, 9, 10
 GR_MAX_BEAMS, GR_MAX_SELECT = 32, 128
+GR_MAX_GIVEN, GR_MAX_HEADS, GR_MAX_DIM, GR_MAX_DIM_Q4 = 64, 1024, 512, 256
 _NULL = -2                 # a required pointer is NULL
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -67,6 +69,18 @@ class StateLayout(C.Structure):
     _fields_ = ([(n, C.c_int) for n in ("batch", "beams_in", "beams_out", "parts")]
                 + [(n, C.c_longlong) for n in ("src_group", "src_beam", "src_part", "dst_group", "dst_beam", "dst_part",
                                                "part_bytes", "token_bytes")])
+
+
+class CacheLayout(C.Structure):
+    """gr_cache_layout: where a cache keeps a slot's heads (strides in elements; of a 4-bit cache block_stride alone, in bytes)."""
+    _fields_ = ([(n, C.c_int) for n in ("format", "heads", "dim", "block_size", "num_blocks")]
+                + [(n, C.c_longlong) for n in ("block_stride", "token_stride", "head_stride")])
+
+
+class CacheTokens(C.Structure):
+    """gr_cache_tokens: new tokens' keys, values and queries (strides in elements)."""
+    _fields_ = ([(n, C.c_void_p) for n in ("k", "v", "q", "q_out")] + [(n, C.c_int) for n in ("dtype", "q_heads")]
+                + [(n, C.c_longlong) for n in ("k_token", "k_head", "v_token", "v_head", "q_token", "q_head", "out_token", "out_head")])
 
 
 def library_path() -> str:
@@ -119,6 +133,11 @@ def load_library():
                                   ip, ip, ip, ip, vp]
     lib.gr_copy_blocks.restype = C.c_int
     lib.gr_copy_blocks.argtypes = [vp, C.c_int, C.c_int, C.c_longlong, C.c_longlong, ip, ip, C.c_int, vp]
+    lib.gr_cache_append.restype = C.c_int
+    lib.gr_cache_append.argtypes = [vp, vp, C.POINTER(CacheLayout), C.POINTER(CacheTokens), C.c_int, vp, ip, dp, C.c_int, C.c_int, vp]
+    lib.gr_cache_read.restype = C.c_int
+    lib.gr_cache_read.argtypes = [vp, vp, C.POINTER(CacheLayout), vp, C.c_int, C.c_int, vp, C.c_longlong, C.c_longlong, vp,
+                                  C.c_longlong, C.c_longlong, vp]
     lib.gr_strerror.restype = C.c_char_p
     lib.gr_strerror.argtypes = [C.c_int]
     _entry.update({n: C.cast(getattr(lib, n), C.c_void_p).value
@@ -233,6 +252,19 @@ def gr_copy_blocks(caches, num_blocks: int, block_stride: int, block_bytes: int,
     a = caches if isinstance(caches, bytes) else array.array("Q", caches).tobytes()
     return load_library().gr_copy_blocks(a, len(a) // 8, num_blocks, block_stride, block_bytes, copy_src, copy_dst, pairs,
                                          stream)
+
+
+def gr_cache_append(keys: int, values: int, layout: Optional[CacheLayout], tokens_in: Optional[CacheTokens], tokens: int, slots: int,
+                    positions: int, frequencies: int, rot: int, interleaved: int, stream: int) -> int:
+    return load_library().gr_cache_append(keys, values, C.byref(layout) if layout is not None else None,
+                                          C.byref(tokens_in) if tokens_in is not None else None, tokens, slots, positions,
+                                          frequencies, rot, interleaved, stream)
+
+
+def gr_cache_read(keys: int, values: int, layout: Optional[CacheLayout], slots: int, tokens: int, dtype: int, k: int, k_token: int,
+                  k_head: int, v: int, v_token: int, v_head: int, stream: int) -> int:
+    return load_library().gr_cache_read(keys, values, C.byref(layout) if layout is not None else None, slots, tokens, dtype, k,
+                                        k_token, k_head, v, v_token, v_head, stream)
 
 
 # ---------------------------------------------------------------- torch tensors
@@ -851,3 +883,137 @@ def copy_blocks(caches, copy_src: torch.Tensor, copy_dst: torch.Tensor) -> None:
     for blocks, stride, size, at in runs:
         if size > 0:
             _call(dev, "gr_copy_blocks", gr_copy_blocks, at, blocks, stride, size, a_src, a_dst, copy_src.shape[0])
+
+
+# ---------------------------------------------------------------- filling and reading a paged cache
+
+_CODES = {torch.float32: GR_F32, torch.bfloat16: GR_BF16, torch.float16: GR_F16}
+
+
+@dataclasses.dataclass
+class KVCache:
+    """A layer's keys and values in blocks, slot z at z % block_size of block z // block_size.  In 16 or 32 bits keys and values are
+    [num_blocks, block_size, heads, dim], apart by any strides; in 4 bits `keys` holds both, [num_blocks, heads, block_size / 8, 9 dim]
+    bytes (gr.h says where what is)."""
+    keys: torch.Tensor
+    values: Optional[torch.Tensor]
+    block_size: int
+    heads: int
+    dim: int
+
+    @staticmethod
+    def empty(num_blocks: int, block_size: int, heads: int, dim: int, dtype=torch.bfloat16, device="cuda") -> "KVCache":
+        """Zeros, of type float32, bfloat16 or float16; uint8: in 4 bits."""
+        if dtype is torch.uint8:
+            if block_size % 8 or dim % 32:
+                raise GrError("a cache in 4 bits has blocks of a multiple of 8 tokens and heads of a multiple of 32 dims")
+            return KVCache(torch.zeros(num_blocks, heads, block_size // 8, 9 * dim, dtype=dtype, device=device), None, block_size, heads, dim)
+        if dtype not in _CODES:
+            raise GrError("a cache is of float32, bfloat16 or float16, or in 4 bits (uint8)")
+        shape = (num_blocks, block_size, heads, dim)
+        return KVCache(torch.zeros(shape, dtype=dtype, device=device), torch.zeros(shape, dtype=dtype, device=device), block_size, heads, dim)
+
+    def tensors(self):
+        """What copy_blocks copies of it."""
+        return [self.keys] if self.values is None else [self.keys, self.values]
+
+
+def _cache(cache: KVCache):
+    """(address of the keys, address of the values, layout) of a cache."""
+    k, v = cache.keys, cache.values
+    if not (isinstance(k, torch.Tensor) and k.is_cuda and k.dim() == 4):
+        raise GrError("cache: keys must be a CUDA tensor of four dimensions")
+    bs, H, D = cache.block_size, cache.heads, cache.dim
+    _fits("cache", k.shape[0], bs, H, D)
+    step = k.stride()
+    if k.dtype is torch.uint8:
+        if v is not None or k.shape[1:] != (H, bs // 8, 9 * D) or bs % 8 or D % 32:
+            raise GrError("cache: in 4 bits keys is [num_blocks, heads, block_size / 8, 9 dim] and values None")
+        if k.numel() and not k[0].is_contiguous():
+            raise GrError("cache: a block's bytes must lie next to one another")
+        block = H * (bs // 8) * 9 * D
+        return k.data_ptr(), 0, CacheLayout(GR_Q4, H, D, bs, k.shape[0], step[0] if k.shape[0] > 1 else block, 0, 0)
+    if k.dtype not in _CODES:
+        raise GrError("cache: keys and values are float32, bfloat16 or float16, or uint8 in 4 bits")
+    if not isinstance(v, torch.Tensor) or v.shape != k.shape or v.dtype is not k.dtype or v.device != k.device or v.stride() != step:
+        raise GrError("cache: keys and values must be alike")
+    if k.shape[1:] != (bs, H, D) or (D > 1 and step[3] != 1):
+        raise GrError("cache: keys and values are [num_blocks, block_size, heads, dim], a head's elements next to one another")
+    return k.data_ptr(), v.data_ptr(), CacheLayout(_CODES[k.dtype], H, D, bs, k.shape[0], step[0], step[1], step[2])
+
+
+def _rows(t, what: str, shape, dtype, device):
+    """(address, distance of tokens, distance of heads) of a [tokens, heads, dim] tensor."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dim() != 3 or t.dtype is not dtype or t.device != device:
+        raise GrError(f"{what}: expected a [tokens, heads, dim] CUDA tensor of {dtype} on {device}")
+    if t.shape != shape:
+        raise GrError(f"{what}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
+    step = t.stride()
+    if shape[2] > 1 and step[2] != 1:
+        raise GrError(f"{what}: a head's elements must lie next to one another")
+    return t.data_ptr(), step[0], step[1]
+
+
+def cache_append(cache: KVCache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, positions: Optional[torch.Tensor] = None,
+                 frequencies: Optional[torch.Tensor] = None, interleaved: bool = False, q: Optional[torch.Tensor] = None,
+                 q_out: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
+    """gr_cache_append on torch CUDA tensors: k, v [tokens, heads, dim] of float32, bfloat16 or float16 go to slots [tokens] int64 (-1:
+    nowhere) of the cache, as block_plan gives them.  With frequencies [rot / 2] float64 and positions [tokens] int32 the first rot dims of
+    keys and queries are rotated: pairs (c, c + rot / 2), or (2 c, 2 c + 1) if interleaved.  q [tokens, any heads, dim]: queries to be rotated into q_out,
+    which may be q itself (default: a new tensor, zeros where positions are negative).  Returns q_out."""
+    a_keys, a_values, layout = _cache(cache)
+    dev = cache.keys.device
+    if not isinstance(k, torch.Tensor) or k.dim() != 3 or k.dtype not in _CODES:
+        raise GrError("k must be a [tokens, heads, dim] CUDA tensor of float32, bfloat16 or float16")
+    T, dt = k.shape[0], k.dtype
+    _fits("cache_append", T)
+    shape = (T, cache.heads, cache.dim)
+    k_at, v_at = _rows(k, "k", shape, dt, dev), _rows(v, "v", shape, dt, dev)
+    a_slots = _need(slots, "slots", torch.int64, (T,), dev)
+    rot = 0
+    if frequencies is not None:
+        if positions is None:
+            raise GrError("frequencies and positions go together")
+        if not isinstance(frequencies, torch.Tensor) or frequencies.dim() != 1 or 2 * frequencies.numel() > cache.dim:
+            raise GrError("frequencies must be [rot / 2], with rot at most the heads' dim")
+        rot = 2 * frequencies.numel()
+    a_freq = _need(frequencies, "frequencies", torch.float64, None, dev, optional=True)
+    a_pos = _need(positions, "positions", torch.int32, (T,), dev, optional=True)
+    q_at = out_at = (0, 0, 0)
+    heads = 0
+    if q is not None:
+        if not isinstance(q, torch.Tensor) or q.dim() != 3:
+            raise GrError("q must be a [tokens, heads, dim] CUDA tensor")
+        heads = q.shape[1]
+        shape = (T, heads, cache.dim)
+        q_at = _rows(q, "q", shape, dt, dev)
+        if q_out is None:
+            q_out = torch.zeros(shape, dtype=dt, device=dev)
+        out_at = _rows(q_out, "q_out", shape, dt, dev)
+    elif q_out is not None:
+        raise GrError("q_out without q")
+    tokens_in = CacheTokens(k_at[0], v_at[0], q_at[0], out_at[0], _CODES[dt], heads, *k_at[1:], *v_at[1:], *q_at[1:], *out_at[1:])
+    _call(dev, "gr_cache_append", gr_cache_append, a_keys, a_values, layout, tokens_in, T, a_slots, a_pos, a_freq, rot, int(interleaved))
+    return q_out
+
+
+def cache_read(cache: KVCache, slots: torch.Tensor, dtype=torch.bfloat16, out=None):
+    """gr_cache_read on torch CUDA tensors: keys and values [tokens, heads, dim] of slots [tokens] int64 (zeros for a slot outside the
+    cache), of float32, bfloat16 or float16.  `out`: a pair of such tensors, to be written."""
+    a_keys, a_values, layout = _cache(cache)
+    dev = cache.keys.device
+    if not isinstance(slots, torch.Tensor) or slots.dim() != 1:
+        raise GrError("slots must be a [tokens] CUDA tensor of torch.int64")
+    a_slots = _need(slots, "slots", torch.int64, None, dev)
+    shape = (slots.shape[0], cache.heads, cache.dim)
+    _fits("cache_read", shape[0])
+    if out is None:
+        if dtype not in _CODES:
+            raise GrError("cache_read gives float32, bfloat16 or float16")
+        out = tuple(torch.empty(shape, dtype=dtype, device=dev) for _ in range(2))
+    k, v = out
+    if not isinstance(k, torch.Tensor) or k.dtype not in _CODES:
+        raise GrError("cache_read gives float32, bfloat16 or float16")
+    k_at, v_at = _rows(k, "out", shape, k.dtype, dev), _rows(v, "out", shape, k.dtype, dev)
+    _call(dev, "gr_cache_read", gr_cache_read, a_keys, a_values, layout, a_slots, shape[0], _CODES[k.dtype], *k_at, *v_at)
+    return k, v
