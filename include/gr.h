@@ -493,6 +493,53 @@ int gr_cache_read(const void* keys, const void* values, const gr_cache_layout* l
                   int dtype, void* k, long long k_token, long long k_head, void* v, long long v_token, long long v_head,
                   void* stream);
 
+/*
+ * gr_cache_attend -- attention of each row's query tokens over the row's tokens in a 4-bit cache.
+ *
+ * Query tokens offsets[r] .. offsets[r + 1] - 1 of row r have the positions positions[offsets[r]], + 1, + 2, ... (only the first is
+ * read; negative: all of them see nothing), as gr_block_plan leaves its appended tokens: one for a decoding step, a run of drafted ones, a
+ * prompt's.  The query of head i of a token at position p becomes
+ *   out = sum_t w_t v_t / sum_t w_t,   w_t = exp(scale q . k_t),   over the row's tokens t with p - window < t <= p  (window 0: t <= p),
+ * k_t, v_t those of key head i / (q_heads / heads) that slot table[r, t / block_size] * block_size + t % block_size holds.
+ * What is held in other places does not tell, whatever it is.  A query that sees nothing gets zeros.
+ *   q, out    [tokens, q_heads, dim], GR_BF16 or GR_F16: (i, h) begins i * q_token + h * q_head elements after q, i * out_token + h * out_head after out.
+ *             out must not meet q or the cache in memory, and no two of its places may share an element.  What lies behind the last row's
+ *             tokens is left as it was.
+ *   cache     of format GR_Q4, as in gr_cache_append.
+ *   table     [rows, width] int;  offsets [rows + 1] int, ascending, 0 .. tokens;  positions [tokens] int.
+ *   heads divides q_heads.  window >= 0.  scale finite.  rows <= 2^20, rows * width < 2^31, width * block_size < 2^31 - 256,
+ *             tokens * (q_heads / heads) < 2^31 - 256.
+ *   workspace gr_attend_workspace_bytes() bytes, aligned to 32.
+ *   status    out [rows]: GR_OK; GR_BAD_ROW where offsets are none, a position is beyond the table, or a block id of a token that is looked at is outside the
+ *             pool (such tokens are left out); GR_CHECK_FAILED in all rows when a copy did not arrive in two seconds (out is then not to be used).
+ */
+size_t gr_attend_workspace_bytes(int heads, int q_heads, int dim, int rows, int tokens);
+int gr_cache_attend(const void* q, int dtype, int q_heads, long long q_token, long long q_head, const void* cache,
+                    const gr_cache_layout* layout, const int* table, int width, int rows, const int* offsets,
+                    const int* positions, int tokens, float scale, int window, void* workspace, void* out,
+                    long long out_token, long long out_head, int* status, void* stream);
+
+/*
+ * ------------------------------------------------------------------------------------------------
+ * gr_token_logprobs -- log probabilities of given tokens under logit rows, the rows' entropies and their likeliest tokens.
+ *
+ * Of row i, with x = logits[i, v] / temperature and lse = log sum_v exp(x_v):
+ *   logprob[i, j] = x_t - lse for t = tokens[i, j] (-infinity for one outside 0 .. V - 1),
+ *   entropy[i]    = - sum_v p_v log p_v,  p_v = exp(x_v - lse),
+ *   top_token[i]  the `top` tokens of largest logits in descending order (equal logits: the smaller id first), top_logprob[i] theirs.
+ *   logits   [rows, V], dtype GR_F32 or GR_BF16: row i begins i * ld elements after the pointer (aligned to the element), ld >= V.
+ *            -infinity masks a token: its log probability is -infinity and it is not among the likeliest; so are all of a row that is masked as a
+ *            whole, whose entropy is 0.  NaN or +infinity: GR_BAD_LOGITS, log probabilities and entropy NaN, no likeliest.
+ *   tokens   [rows, given] int, given 0 .. GR_MAX_GIVEN (0: NULL, as logprob may be).
+ *   top      0 .. GR_MAX_SELECT (0: top_token and top_logprob may be NULL).  Places that no token is left for: -1, -infinity.
+ *   logprob [rows, given], entropy [rows] (or NULL), top_token, top_logprob [rows, top], status [rows]: out, apart from one another and from
+ *            what is read.  status: GR_OK or GR_BAD_LOGITS.
+ *   V <= 2^21, rows <= 2^26, temperature > 0.  No workspace.
+ */
+int gr_token_logprobs(const void* logits, int dtype, int V, long long ld, int rows, float temperature, const int* tokens,
+                      int given, int top, float* logprob, float* entropy, int* top_token, float* top_logprob, int* status,
+                      void* stream);
+
 /* Text for a GR_* / GR_E_* code (host pointer to a static string). */
 const char* gr_strerror(int code);
 

@@ -10,6 +10,7 @@ from .binding import (GR_F32, GR_BF16, GR_OK, GR_NOT_CONVERGED, GR_SUPPORT_TOO_L
                       gr_block_plan, gr_copy_blocks, Beams, beam_select, reorder_states, BlockTables, BlockPlan,
                       block_plan, copy_blocks,
                       GR_F16, GR_Q4, GR_MAX_GIVEN, GR_MAX_HEADS, GR_MAX_DIM, GR_MAX_DIM_Q4, CacheLayout, CacheTokens, gr_cache_append,
-                      gr_cache_read, KVCache, cache_append, cache_read)
+                      gr_cache_read, KVCache, cache_append, cache_read, gr_attend_workspace_bytes, gr_cache_attend, Attended, cache_attend,
+                      gr_token_logprobs, Logprobs, token_logprobs)
 
 __all__ = [n for n in dir() if not n.startswith("_")]

@@ -138,6 +138,13 @@ def load_library():
     lib.gr_cache_read.restype = C.c_int
     lib.gr_cache_read.argtypes = [vp, vp, C.POINTER(CacheLayout), vp, C.c_int, C.c_int, vp, C.c_longlong, C.c_longlong, vp,
                                   C.c_longlong, C.c_longlong, vp]
+    lib.gr_attend_workspace_bytes.restype = C.c_size_t
+    lib.gr_attend_workspace_bytes.argtypes = [C.c_int] * 5
+    lib.gr_cache_attend.restype = C.c_int
+    lib.gr_cache_attend.argtypes = [vp, C.c_int, C.c_int, C.c_longlong, C.c_longlong, vp, C.POINTER(CacheLayout), ip, C.c_int, C.c_int, ip,
+                                    ip, C.c_int, C.c_float, C.c_int, vp, vp, C.c_longlong, C.c_longlong, ip, vp]
+    lib.gr_token_logprobs.restype = C.c_int
+    lib.gr_token_logprobs.argtypes = [vp, C.c_int, C.c_int, C.c_longlong, C.c_int, C.c_float, ip, C.c_int, C.c_int, fp, fp, ip, fp, ip, vp]
     lib.gr_strerror.restype = C.c_char_p
     lib.gr_strerror.argtypes = [C.c_int]
     _entry.update({n: C.cast(getattr(lib, n), C.c_void_p).value
@@ -265,6 +272,24 @@ def gr_cache_read(keys: int, values: int, layout: Optional[CacheLayout], slots: 
                   k_head: int, v: int, v_token: int, v_head: int, stream: int) -> int:
     return load_library().gr_cache_read(keys, values, C.byref(layout) if layout is not None else None, slots, tokens, dtype, k,
                                         k_token, k_head, v, v_token, v_head, stream)
+
+
+def gr_attend_workspace_bytes(heads: int, q_heads: int, dim: int, rows: int, tokens: int) -> int:
+    return int(load_library().gr_attend_workspace_bytes(heads, q_heads, dim, rows, tokens))
+
+
+def gr_cache_attend(q: int, dtype: int, q_heads: int, q_token: int, q_head: int, cache: int, layout: Optional[CacheLayout], table: int,
+                    width: int, rows: int, offsets: int, positions: int, tokens: int, scale: float, window: int, workspace: int, out: int,
+                    out_token: int, out_head: int, status: int, stream: int) -> int:
+    return load_library().gr_cache_attend(q, dtype, q_heads, q_token, q_head, cache, C.byref(layout) if layout is not None else None,
+                                          table, width, rows, offsets, positions, tokens, scale, window, workspace, out, out_token,
+                                          out_head, status, stream)
+
+
+def gr_token_logprobs(logits: int, dtype: int, V: int, ld: int, rows: int, temperature: float, tokens: int, given: int, top: int,
+                      logprob: int, entropy: int, top_token: int, top_logprob: int, status: int, stream: int) -> int:
+    return load_library().gr_token_logprobs(logits, dtype, V, ld, rows, temperature, tokens, given, top, logprob, entropy, top_token,
+                                            top_logprob, status, stream)
 
 
 # ---------------------------------------------------------------- torch tensors
@@ -1017,3 +1042,92 @@ def cache_read(cache: KVCache, slots: torch.Tensor, dtype=torch.bfloat16, out=No
     k_at, v_at = _rows(k, "out", shape, k.dtype, dev), _rows(v, "out", shape, k.dtype, dev)
     _call(dev, "gr_cache_read", gr_cache_read, a_keys, a_values, layout, a_slots, shape[0], _CODES[k.dtype], *k_at, *v_at)
     return k, v
+
+
+@dataclasses.dataclass
+class Attended:
+    """Result of cache_attend."""
+    out: torch.Tensor        # [tokens, heads, dim], of the queries' type
+    status: torch.Tensor     # [rows] int32
+    workspace: torch.Tensor  # uint8, scratch
+    shape: tuple             # (tokens, heads, dim, rows, heads of the cache, type)
+
+
+def cache_attend(q: torch.Tensor, cache: KVCache, table: torch.Tensor, offsets: torch.Tensor, positions: torch.Tensor,
+                 scale: Optional[float] = None, window: int = 0, out: Optional[Attended] = None) -> Attended:
+    """gr_cache_attend on torch CUDA tensors: queries q [tokens, heads, dim] bfloat16 or float16 (a multiple of the cache's heads), a cache in 4
+    bits, the rows' block table [rows, width] int32, and, as block_plan returns them, offsets [rows + 1] (row r's queries are
+    offsets[r] .. offsets[r + 1] - 1) and positions [tokens] int32.  `scale` defaults to dim ** -0.5; with a window a query sees that many
+    tokens, itself the last.  `out`: a result of an earlier call of the same shape, written again; what lies behind the last row's tokens stays."""
+    a_cache, _, layout = _cache(cache)
+    if layout.format != GR_Q4:
+        raise GrError("cache_attend wants a cache in 4 bits")
+    dev = cache.keys.device
+    if not isinstance(q, torch.Tensor) or q.dim() != 3 or q.dtype not in (torch.bfloat16, torch.float16):
+        raise GrError("q must be a [tokens, heads, dim] CUDA tensor of bfloat16 or float16")
+    T, Hq, D = q.shape
+    q_at = _rows(q, "q", (T, Hq, cache.dim), q.dtype, dev)
+    if not isinstance(table, torch.Tensor) or table.dim() != 2:
+        raise GrError("table must be a [rows, width] CUDA tensor of torch.int32")
+    R, width = table.shape
+    a_table = _need(table, "table", torch.int32, None, dev)
+    a_off = _need(offsets, "offsets", torch.int32, (R + 1,), dev)
+    a_pos = _need(positions, "positions", torch.int32, (T,), dev)
+    _fits("cache_attend", T, Hq, R, width, window)
+    shape = (T, Hq, D, R, cache.heads, q.dtype)
+    if out is None or out.shape != shape or out.out.device != dev:
+        wbytes = gr_attend_workspace_bytes(cache.heads, Hq, D, R, T)
+        if wbytes == 0:
+            raise GrError("invalid shape")
+        out = Attended(torch.zeros(T, Hq, D, dtype=q.dtype, device=dev), torch.empty(R, dtype=torch.int32, device=dev),
+                       torch.empty(wbytes, dtype=torch.uint8, device=dev), shape)
+    out_at = _rows(out.out, "out", q.shape, q.dtype, dev)
+    _call(dev, "gr_cache_attend", gr_cache_attend, q_at[0], _CODES[q.dtype], Hq, *q_at[1:], a_cache, layout, a_table, width, R, a_off, a_pos,
+          T, D ** -0.5 if scale is None else scale, window, out.workspace.data_ptr(), *out_at, out.status.data_ptr())
+    return out
+
+
+# ---------------------------------------------------------------- log probabilities
+
+@dataclasses.dataclass
+class Logprobs:
+    """Result of token_logprobs."""
+    logprob: torch.Tensor      # [rows, given] float32
+    entropy: torch.Tensor      # [rows] float32
+    top_token: torch.Tensor    # [rows, top] int32, -1: none left
+    top_logprob: torch.Tensor  # [rows, top] float32
+    status: torch.Tensor       # [rows] int32
+    shape: tuple               # (rows, given, top)
+
+
+def token_logprobs(logits: torch.Tensor, tokens: Optional[torch.Tensor] = None, top: int = 0, temperature: float = 1.0,
+                   out: Optional[Logprobs] = None) -> Logprobs:
+    """gr_token_logprobs on torch CUDA tensors: logits [rows, V] float32 or bfloat16 (rows at any one distance, elements next to one another), tokens
+    [rows, given] or [rows] int32 (None: none).  The temperature is rounded to float32, as the C call takes it.  `out`: a result of an earlier call of
+    the same shape, written again."""
+    if not (isinstance(logits, torch.Tensor) and logits.is_cuda and logits.dim() == 2):
+        raise GrError("logits must be a [rows, V] CUDA tensor")
+    R, V = logits.shape
+    dev, code = logits.device, _dtype_code(logits)
+    step = logits.stride()
+    ld = step[0] if R > 1 else V
+    if logits.numel() > 0 and ((V > 1 and step[1] != 1) or ld < V):
+        raise GrError("logits: the rows must not overlap, their elements lie next to one another")
+    if tokens is not None and isinstance(tokens, torch.Tensor) and tokens.dim() == 1:
+        tokens = tokens.view(-1, 1) if tokens.is_contiguous() else tokens.unsqueeze(1)
+    if tokens is not None and (not isinstance(tokens, torch.Tensor) or tokens.dim() != 2 or tokens.shape[0] != R):
+        raise GrError("tokens must be [rows, given] or [rows] int32")
+    given = 0 if tokens is None else tokens.shape[1]
+    a_tokens = _need(tokens, "tokens", torch.int32, None, dev, optional=True)
+    _fits("token_logprobs", R, V, given, top)
+    if out is None or out.shape != (R, given, top) or out.status.device != dev:
+        if top < 0:
+            raise GrError("top must not be negative")
+        f32, i32 = dict(dtype=torch.float32, device=dev), dict(dtype=torch.int32, device=dev)
+        out = Logprobs(torch.empty(R, given, **f32), torch.empty(R, **f32), torch.empty(R, top, **i32), torch.empty(R, top, **f32),
+                       torch.empty(R, **i32), (R, given, top))
+    if R > 0 and a_tokens and a_tokens == out.top_token.data_ptr() and top > 0:
+        raise GrError("tokens is a tensor of `out`, which this call writes")
+    _call(dev, "gr_token_logprobs", load_library().gr_token_logprobs, logits.data_ptr(), code, V, max(ld, V), R, temperature, a_tokens, given, top,
+          out.logprob.data_ptr(), out.entropy.data_ptr(), out.top_token.data_ptr(), out.top_logprob.data_ptr(), out.status.data_ptr())
+    return out

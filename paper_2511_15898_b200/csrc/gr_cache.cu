@@ -506,27 +506,6 @@ read4_kernel(const __grid_constant__ ReadArgs R)
 
 // ---------------------------------------------------------------- host
 
-// Whether places of `count` strided dimensions lie apart, each `unit` elements long.
-static bool apart(long long unit, const long long* step, const long long* size, int count)
-{
-    int order[3] = {0, 1, 2};
-    std::sort(order, order + count, [&](int a, int b) { return step[a] < step[b]; });
-    long long span = unit;
-    for (int i = 0; i < count; i++) {
-        const long long s = step[order[i]], n = size[order[i]];
-        if (n <= 1) continue;
-        if (s < span || s > (1ll << 58) / n) return false;
-        span += s * (n - 1);
-    }
-    return true;
-}
-
-// Whether strides of what is read are numbers that `tokens` and `heads` of them can be counted off by.
-static bool counted(long long token, long long head, int tokens, int heads)
-{
-    return token >= 0 && head >= 0 && token <= (1ll << 58) / std::max(1, tokens) && head <= (1ll << 58) / std::max(1, heads);
-}
-
 int check_cache(const void* keys, const void* values, const gr_cache_layout* layout)
 {
     if (!layout) return GR_E_NULL;
@@ -548,30 +527,6 @@ int check_cache(const void* keys, const void* values, const gr_cache_layout* lay
     const uintptr_t mask = four ? 15 : type_size(L.format) - 1;
     if (((uintptr_t)keys & mask) || (!four && ((uintptr_t)values & mask))) return GR_E_ALIGN;
     return GR_OK;
-}
-
-// First byte and the one behind the last of strided places.
-struct Span { uintptr_t lo, hi; };
-static Span span_of(const void* p, long long unit, const long long* step, const long long* size, int count)
-{
-    for (int i = 0; i < count; i++) { if (size[i] <= 0) return {0, 0}; unit += step[i] * (size[i] - 1); }
-    return {(uintptr_t)p, (uintptr_t)p + (uintptr_t)unit};
-}
-static bool meet(Span a, Span b) { return a.lo < b.hi && b.lo < a.hi; }
-static Span cache_span(const void* p, const gr_cache_layout& L)
-{
-    if (L.format == GR_Q4) {
-        const long long step[1] = {L.block_stride}, size[1] = {L.num_blocks};
-        return span_of(p, (long long)L.heads * (L.block_size / 8) * octet_bytes(L.dim), step, size, 1);
-    }
-    const int e = type_size(L.format);
-    const long long step[3] = {L.block_stride * e, L.token_stride * e, L.head_stride * e}, size[3] = {L.num_blocks, L.block_size, L.heads};
-    return span_of(p, (long long)L.dim * e, step, size, 3);
-}
-static Span rows_span(const void* p, int e, int dim, long long token, long long head, int tokens, int heads)
-{
-    const long long step[2] = {token * e, head * e}, size[2] = {tokens, heads};
-    return span_of(p, (long long)dim * e, step, size, 2);
 }
 
 // How a call's tokens are dealt out: windows of one token where there are few, with the heads in several CTAs until an SM has two.
@@ -654,15 +609,6 @@ static void launch_read4(ReadArgs& R, bool vec, cudaStream_t st)
 {
     if (vec) launch_read4_of<T, true>(R, st); else launch_read4_of<T, false>(R, st);
 }
-
-// The elements that pointers and strides (of `e` bytes an element) let an access take: 8 (16 bytes), 4 or 1.
-struct Align {
-    unsigned long long bits = 0;
-    void add(const void* p, int e, std::initializer_list<long long> strides) {
-        bits |= (unsigned long long)(uintptr_t)p;
-        for (long long s : strides) bits |= (unsigned long long)s * (unsigned long long)e;
-    }
-};
 
 }  // namespace gr
 

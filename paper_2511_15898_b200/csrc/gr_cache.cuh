@@ -6,6 +6,8 @@
 // so that lane (g, t) of a warp finds its share of the operands of a 16 x 8 x 16 product, of a tile whose first eight rows (keys:
 // tokens, values: depth) are this octet's, in J consecutive words at place 4 g + t, codes and scales alike; a token's bytes are its own.
 #pragma once
+#include <algorithm>
+#include <initializer_list>
 #include "gr_common.cuh"
 
 namespace gr {
@@ -29,6 +31,60 @@ template <typename T, int N> struct __align__(sizeof(T) * N) Pack { T x[N]; };
 
 __host__ inline bool known_type(int t) { return t == GR_F32 || t == GR_BF16 || t == GR_F16; }
 __host__ inline int type_size(int t) { return t == GR_F32 ? 4 : 2; }
+
+// Whether places of `count` strided dimensions lie apart, each `unit` elements long.
+inline bool apart(long long unit, const long long* step, const long long* size, int count)
+{
+    int order[3] = {0, 1, 2};
+    std::sort(order, order + count, [&](int a, int b) { return step[a] < step[b]; });
+    long long span = unit;
+    for (int i = 0; i < count; i++) {
+        const long long s = step[order[i]], n = size[order[i]];
+        if (n <= 1) continue;
+        if (s < span || s > (1ll << 58) / n) return false;
+        span += s * (n - 1);
+    }
+    return true;
+}
+
+// Whether strides of what is read are numbers that `tokens` and `heads` of them can be counted off by.
+inline bool counted(long long token, long long head, int tokens, int heads)
+{
+    return token >= 0 && head >= 0 && token <= (1ll << 58) / std::max(1, tokens) && head <= (1ll << 58) / std::max(1, heads);
+}
+
+// First byte and the one behind the last of strided places.
+struct Span { uintptr_t lo, hi; };
+inline Span span_of(const void* p, long long unit, const long long* step, const long long* size, int count)
+{
+    for (int i = 0; i < count; i++) { if (size[i] <= 0) return {0, 0}; unit += step[i] * (size[i] - 1); }
+    return {(uintptr_t)p, (uintptr_t)p + (uintptr_t)unit};
+}
+inline bool meet(Span a, Span b) { return a.lo < b.hi && b.lo < a.hi; }
+inline Span cache_span(const void* p, const gr_cache_layout& L)
+{
+    if (L.format == GR_Q4) {
+        const long long step[1] = {L.block_stride}, size[1] = {L.num_blocks};
+        return span_of(p, (long long)L.heads * (L.block_size / 8) * octet_bytes(L.dim), step, size, 1);
+    }
+    const int e = type_size(L.format);
+    const long long step[3] = {L.block_stride * e, L.token_stride * e, L.head_stride * e}, size[3] = {L.num_blocks, L.block_size, L.heads};
+    return span_of(p, (long long)L.dim * e, step, size, 3);
+}
+inline Span rows_span(const void* p, int e, int dim, long long token, long long head, int tokens, int heads)
+{
+    const long long step[2] = {token * e, head * e}, size[2] = {tokens, heads};
+    return span_of(p, (long long)dim * e, step, size, 2);
+}
+
+// The elements that pointers and strides (of `e` bytes an element) let an access take: 8 (16 bytes), 4 or 1.
+struct Align {
+    unsigned long long bits = 0;
+    void add(const void* p, int e, std::initializer_list<long long> strides) {
+        bits |= (unsigned long long)(uintptr_t)p;
+        for (long long s : strides) bits |= (unsigned long long)s * (unsigned long long)e;
+    }
+};
 
 // What a layout has to satisfy (`keys` aligned as its format asks for); GR_OK or the GR_E_* code.
 int check_cache(const void* keys, const void* values, const gr_cache_layout* layout);

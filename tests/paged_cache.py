@@ -104,3 +104,52 @@ def to_numpy(t):
 def cast(x, dtype):
     """float64 numbers rounded to a torch type, as float64."""
     return torch.from_numpy(np.ascontiguousarray(x)).to(dtype).double().numpy()
+
+
+def all4(data):
+    """(keys, values, their scales) [slots, heads, dim] float64 of a whole cache [blocks, heads, block / 8, 9 dim] uint8."""
+    N, H, O, size = data.shape
+    dim = size // 9
+    byte, shift, word = tables(dim)
+    scales = np.ascontiguousarray(data).view(np.float16).astype(np.float64)
+    out = []
+    for kind in range(2):
+        code = (data[..., byte[kind]] >> shift[kind]) & 15
+        s = scales[..., word[kind]]
+        out += [(code.astype(np.float64) - 8) * s, s]
+    k, ks, v, vs = (x.transpose(0, 2, 3, 1, 4).reshape(N * O * 8, H, dim) for x in out)
+    return k, v, ks, vs
+
+
+def attention(q, held, block_size, table, offsets, positions, scale, window):
+    """What gr_cache_attend computes, in 64 bits, and a bound of its error before the rounding to the output's type.
+
+    x = scale q.k is summed in 32 bits, from codes 0 .. 15 and the sum of the queries times 8, both up to A = scale sum |q| 16 |s|: eight
+    roundings of 2^-23 A.  p is rounded to 11 bits, p s once more (2^-12 of each, at codes up to 15, and 2^-12 of p where 8 times their sum is
+    taken off: 38 2^-12 p |s|; below 2^-14 by 2^-25 instead); sums of n / 16 products and eight joins round 2^-22 of 16 p |s| each."""
+    T, Hq, D = q.shape
+    k, v, ks, vs = held
+    H = k.shape[1]
+    out, bound = np.zeros((T, Hq, D)), np.zeros((T, Hq, D))
+    for r in range(len(offsets) - 1):
+        for i in range(offsets[r], offsets[r + 1]):
+            p0 = int(positions[offsets[r]])
+            p = p0 + i - int(offsets[r])
+            if p0 < 0:
+                continue
+            t = np.arange(max(0, p - window + 1) if window else 0, min(p + 1, table.shape[1] * block_size))
+            block = table[r, t // block_size]
+            t = t[(block >= 0) & (block * block_size < len(k))]
+            z = table[r, t // block_size] * block_size + t % block_size
+            if not len(z):
+                continue
+            for h in range(Hq):
+                g = h // (Hq // H)
+                x = scale * (k[z, g] @ q[i, h])
+                dx = 8 * 2.0 ** -23 * (abs(scale) * 16 * np.abs(ks[z, g]) @ np.abs(q[i, h])).max()
+                w = np.exp(x - x.max())
+                out[i, h] = w @ v[z, g] / w.sum()
+                s = np.abs(vs[z, g])
+                bound[i, h] = ((38 * 2.0 ** -12 + 16 * (len(z) / 16 + 8) * 2.0 ** -22) * (w @ s) + 2.0 ** -25 * 38 * (1 + s).sum(0)
+                               + (2 * dx + 2.0 ** -20) * (w @ np.abs(v[z, g]))) / w.sum()
+    return out, bound

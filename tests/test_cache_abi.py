@@ -79,6 +79,34 @@ def test_read():
     assert call(tokens=0) == 0
 
 
+def test_attend():
+    ok = dict(q=B, dtype=G.GR_BF16, heads=8, qt=512, qh=64, cache=A, table=F, width=4, rows=3, off=F, pos=F, tokens=5, scale=0.1, window=0,
+              ws=C, out=D, ot=512, oh=64, status=E)
+
+    def call(four=True, lay=None, **kw):
+        a = dict(ok); a.update(kw)
+        return G.gr_cache_attend(a["q"], a["dtype"], a["heads"], a["qt"], a["qh"], a["cache"], _layout(four, **(lay or {})), a["table"], a["width"], a["rows"],
+                                 a["off"], a["pos"], a["tokens"], a["scale"], a["window"], a["ws"], a["out"], a["ot"], a["oh"], a["status"], 0)
+
+    for bad in _BAD_FOUR:
+        assert call(lay=bad) == -1, bad
+    assert call(four=False) == -1                          # 16 bits
+    assert G.gr_cache_attend(B, 1, 8, 512, 64, A, None, F, 4, 3, F, F, 5, 0.1, 0, C, D, 512, 64, E, 0) == -2
+    assert call(dtype=G.GR_F32) == -1 and call(dtype=G.GR_Q4) == -1 and call(heads=7) == -1 and call(heads=0) == -1 and call(heads=1026) == -1
+    assert call(rows=-1) == -1 and call(tokens=-1) == -1 and call(width=-1) == -1 and call(window=-1) == -1 and call(rows=(1 << 20) + 1) == -1
+    assert call(width=1 << 27) == -1 and call(rows=1 << 20, width=1 << 11) == -1 and call(tokens=1 << 29) == -1
+    assert call(scale=float("nan")) == -1 and call(scale=float("inf")) == -1
+    assert call(qt=-1) == -1 and call(qh=-1) == -1 and call(qt=1 << 60) == -1 and call(oh=63) == -1 and call(ot=511) == -1
+    for name in ("q", "cache", "table", "off", "pos", "ws", "out", "status"):
+        assert call(**{name: 0}) == -2, name
+    assert call(q=B + 1) == -3 and call(out=D + 1) == -3 and call(ws=C + 16) == -3 and call(cache=A + 8) == -3
+    assert call(out=A + 64) == -1 and call(out=B) == -1 and call(out=B + 4 * 1024) == -1
+    assert call(rows=0) == 0 and call(rows=0, q=0, ws=0) == 0
+    assert G.gr_attend_workspace_bytes(2, 8, 64, 3, 5) > 0
+    for bad in ((0, 8, 64, 3, 5), (3, 8, 64, 3, 5), (2, 8, 48, 3, 5), (2, 8, 288, 3, 5), (2, 8, 64, -1, 5), (2, 8, 64, 3, -5)):
+        assert G.gr_attend_workspace_bytes(*bad) == 0, bad
+
+
 def test_tensor_front_ends_want_cuda_tensors():
     x = torch.zeros(2, 1, 32)
     with pytest.raises(G.GrError):
@@ -113,3 +141,22 @@ def test_the_model_of_the_cache():
     for got, x in zip(P.read4(data, 16, slots), (k, v)):
         step = np.abs(x.reshape(5, 2, 2, 32)).max(-1).repeat(32, -1).reshape(5, 2, 64) / 8
         assert (np.abs(got - x) <= step * (1 + 2.0 ** -9)).all()
+
+
+def test_token_logprobs():
+    ok = dict(logits=A, dtype=G.GR_F32, V=1000, ld=1000, rows=4, T=1.0, tokens=B, given=2, top=5, lp=C, ent=D, tok=E, tlp=F, st=F)
+
+    def call(**kw):
+        a = dict(ok); a.update(kw)
+        return G.gr_token_logprobs(a["logits"], a["dtype"], a["V"], a["ld"], a["rows"], a["T"], a["tokens"], a["given"], a["top"], a["lp"], a["ent"],
+                                   a["tok"], a["tlp"], a["st"], 0)
+
+    assert call(V=0) == -1 and call(V=(1 << 21) + 1, ld=1 << 22) == -1 and call(ld=999) == -1 and call(dtype=G.GR_F16) == -1 and call(dtype=G.GR_Q4) == -1
+    assert call(rows=-1) == -1 and call(rows=(1 << 26) + 1) == -1 and call(T=0.0) == -1 and call(T=-1.0) == -1 and call(T=float("nan")) == -1 and call(T=float("inf")) == -1
+    assert call(given=-1) == -1 and call(given=65) == -1 and call(top=-1) == -1 and call(top=129) == -1
+    for name in ("logits", "tokens", "lp", "tok", "tlp", "st"):
+        assert call(**{name: 0}) == -2, name
+    assert call(logits=A + 2) == -3 and call(logits=A + 1, dtype=G.GR_BF16) == -3
+    assert call(rows=0) == 0 and call(rows=0, logits=0) == 0
+    with pytest.raises(G.GrError):
+        G.token_logprobs(torch.zeros(2, 5))
