@@ -472,6 +472,7 @@ typedef struct gr_cache_layout {
  *             is read or another that is written, and no two places of q_out may share one.
  *   slots     [tokens], no slot twice.     positions [tokens]: not looked at (and may be NULL) without frequencies, that is rot 0.
  *   rot       even, 0 .. dim.              frequencies [rot / 2] double.
+ *   Strides of k, v and q below 2^31.
  * Any alignment to the element works; pointers and strides that are multiples of 16 bytes are fastest.
  */
 typedef struct gr_cache_tokens {
@@ -507,7 +508,7 @@ int gr_cache_read(const void* keys, const void* values, const gr_cache_layout* l
  *             tokens is left as it was.
  *   cache     of format GR_Q4, as in gr_cache_append.
  *   table     [rows, width] int;  offsets [rows + 1] int, ascending, 0 .. tokens;  positions [tokens] int.
- *   heads divides q_heads.  window >= 0.  scale finite.  rows <= 2^20, rows * width < 2^31, width * block_size < 2^31 - 256,
+ *   heads divides q_heads.  Strides of q below 2^31.  window >= 0.  scale finite.  rows <= 2^20, rows * width < 2^31, width * block_size < 2^31 - 256,
  *             tokens * (q_heads / heads) < 2^31 - 256.
  *   workspace gr_attend_workspace_bytes() bytes, aligned to 32.
  *   status    out [rows]: GR_OK; GR_BAD_ROW where offsets are none, a position is beyond the table, or a block id of a token that is looked at is outside the

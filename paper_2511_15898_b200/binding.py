@@ -148,7 +148,8 @@ def load_library():
     lib.gr_strerror.restype = C.c_char_p
     lib.gr_strerror.argtypes = [C.c_int]
     _entry.update({n: C.cast(getattr(lib, n), C.c_void_p).value
-                   for n in ("gr_beam_select", "gr_reorder_states", "gr_block_plan", "gr_copy_blocks")})
+                   for n in ("gr_beam_select", "gr_reorder_states", "gr_block_plan", "gr_copy_blocks", "gr_cache_append", "gr_cache_read",
+                             "gr_cache_attend", "gr_token_logprobs")})
     _lib = lib
     if "_tensors" not in globals():
         _tensors = _load_tensors()
@@ -986,6 +987,9 @@ def cache_append(cache: KVCache, k: torch.Tensor, v: torch.Tensor, slots: torch.
     nowhere) of the cache, as block_plan gives them.  With frequencies [rot / 2] float64 and positions [tokens] int32 the first rot dims of
     keys and queries are rotated: pairs (c, c + rot / 2), or (2 c, 2 c + 1) if interleaved.  q [tokens, any heads, dim]: queries to be rotated into q_out,
     which may be q itself (default: a new tensor, zeros where positions are negative).  Returns q_out."""
+    if _short("append", "gr_cache_append", cache.keys, cache.values, cache.block_size, cache.heads, cache.dim, k, v, slots, positions, frequencies,
+              interleaved, q, q_out):
+        return q_out
     a_keys, a_values, layout = _cache(cache)
     dev = cache.keys.device
     if not isinstance(k, torch.Tensor) or k.dim() != 3 or k.dtype not in _CODES:
@@ -1025,6 +1029,15 @@ def cache_append(cache: KVCache, k: torch.Tensor, v: torch.Tensor, slots: torch.
 def cache_read(cache: KVCache, slots: torch.Tensor, dtype=torch.bfloat16, out=None):
     """gr_cache_read on torch CUDA tensors: keys and values [tokens, heads, dim] of slots [tokens] int64 (zeros for a slot outside the
     cache), of float32, bfloat16 or float16.  `out`: a pair of such tensors, to be written."""
+    if _lib is None:
+        load_library()
+    if _tensors is not None and (out is None or len(out) == 2):
+        got = _tensors.read(_entry["gr_cache_read"], cache.keys, cache.values, cache.block_size, cache.heads, cache.dim, slots, dtype,
+                            *(out if out is not None else (None, None)))
+        if isinstance(got, tuple):
+            return got
+        if got is not None:
+            _check(got, "gr_cache_read")
     a_keys, a_values, layout = _cache(cache)
     dev = cache.keys.device
     if not isinstance(slots, torch.Tensor) or slots.dim() != 1:
@@ -1059,6 +1072,10 @@ def cache_attend(q: torch.Tensor, cache: KVCache, table: torch.Tensor, offsets: 
     bits, the rows' block table [rows, width] int32, and, as block_plan returns them, offsets [rows + 1] (row r's queries are
     offsets[r] .. offsets[r + 1] - 1) and positions [tokens] int32.  `scale` defaults to dim ** -0.5; with a window a query sees that many
     tokens, itself the last.  `out`: a result of an earlier call of the same shape, written again; what lies behind the last row's tokens stays."""
+    if (out is not None and out.shape[4] == cache.heads
+            and _short("attend", "gr_cache_attend", q, cache.keys, cache.values, cache.block_size, cache.heads, cache.dim, table, offsets, positions,
+                       scale, window, out.workspace, out.out, out.status)):
+        return out
     a_cache, _, layout = _cache(cache)
     if layout.format != GR_Q4:
         raise GrError("cache_attend wants a cache in 4 bits")
@@ -1105,6 +1122,10 @@ def token_logprobs(logits: torch.Tensor, tokens: Optional[torch.Tensor] = None, 
     """gr_token_logprobs on torch CUDA tensors: logits [rows, V] float32 or bfloat16 (rows at any one distance, elements next to one another), tokens
     [rows, given] or [rows] int32 (None: none).  The temperature is rounded to float32, as the C call takes it.  `out`: a result of an earlier call of
     the same shape, written again."""
+    if (out is not None and out.shape[2] == top
+            and _short("logprobs", "gr_token_logprobs", logits, tokens, top, temperature, out.logprob, out.entropy, out.top_token, out.top_logprob,
+                       out.status)):
+        return out
     if not (isinstance(logits, torch.Tensor) and logits.is_cuda and logits.dim() == 2):
         raise GrError("logits must be a [rows, V] CUDA tensor")
     R, V = logits.shape

@@ -15,18 +15,22 @@
 namespace gr {
 
 constexpr int kCacheThreads = 256, kCacheWarps = kCacheThreads / 32;
-constexpr int kCacheWindow = 8;                // tokens of a CTA where there are many
+constexpr int kCacheWindow = 32;               // most tokens of a CTA
+constexpr int kCacheSeen = kCacheWindow + 7;   // and those that it looks at
 constexpr int kCacheMany = 16 * kSms;          // from so many tokens on
 
 struct CacheArgs {
     char* keys; char* values;
     long long block_stride, token_stride, head_stride;     // elements of the cache (4 bits: bytes, the first only)
-    int heads, dim, block, num_blocks;
+    int heads, dim, block, num_blocks, four;
     gr_cache_tokens x;
     int tokens, window, split;                 // split: CTAs that share a window's rows
     const long long* slots; const int* positions; const double* freq;
     int half, interleaved;                     // half: pairs of dims that are rotated
     int team, queries_vec;                     // team: threads of a row
+    // whole quotients that loops go on by, and 1 / n for first places (small numbers: exact with a half added)
+    int by_half, by_heads, by_queries;
+    float of_half, of_heads, of_queries;
 };
 
 // ---------------------------------------------------------------- angles
@@ -34,7 +38,9 @@ struct CacheArgs {
 // sine and cosine of a, rounded to fp32
 __device__ __forceinline__ float2 cos_sin(double a)
 {
-    const double k = rint(a * 0.63661977236758134308);                     // 2 / pi
+    // (whole numbers by the sum with 1.5 2^52, whose low word they are: conversions have a fraction of the multiplications' rate; the
+    // quadrant counts up to 2^51 of them)
+    const double magic = 6755399441055744.0, whole = fma(a, 0.63661977236758134308, magic), k = whole - magic;     // 2 / pi
     double r = fma(-k, 1.57079632679489655800e+00, a);                      // pi / 2 in two parts
     r = fma(-k, 6.12323399573676603587e-17, r);
     const double z = r * r;
@@ -48,19 +54,55 @@ __device__ __forceinline__ float2 cos_sin(double a)
     s = fma(s, z, -1.0 / 6.0);          c = fma(c, z, 1.0 / 24.0);
     s = fma(s * z, r, r);               c = fma(c, z, -0.5);
     c = fma(c, z, 1.0);
-    const int quadrant = (int)((long long)k & 3);
+    const int quadrant = __double2loint(whole) & 3;
     const double cq = quadrant & 1 ? s : c, sq = quadrant & 1 ? c : s;
     return make_float2((float)(quadrant == 1 || quadrant == 2 ? -cq : cq), (float)(quadrant >= 2 ? -sq : sq));
 }
 
-// (cos, sin) of the pairs of `n` tokens from `i0` on into cs[n][half]
-__device__ __forceinline__ void fill_angles(const CacheArgs& A, float2* cs, int i0, int n)
+// A window's tokens, in shared memory: where each goes, and (cos, sin) of its pairs behind that.  Windows of a 4-bit cache look at the
+// seven tokens behind them too, which a run that begins in the window may hold.
+struct Tokens {
+    long long slot[kCacheSeen];
+    long long at[kCacheSeen];                  // elements (4 bits: bytes, of the octet) from the cache's beginning to the token's first head; -1: nowhere
+    double angle[kCacheSeen];                  // the position, as a factor
+    int position[kCacheSeen];
+    int runs, first[kCacheWindow], size[kCacheWindow];     // 4 bits: runs that begin in the window, by their first token
+};
+__device__ __forceinline__ void window_tokens(const CacheArgs& A, Tokens& w, int i0, int n)
 {
-    for (int e = threadIdx.x; e < n * A.half; e += kCacheThreads) {
-        const int tok = e / A.half, f = e - tok * A.half;
-        cs[e] = cos_sin((double)A.positions[i0 + tok] * A.freq[f]);
+    const int t = threadIdx.x;
+    if (t < n) {
+        const long long slot = A.slots[i0 + t];
+        const int position = A.positions ? A.positions[i0 + t] : 0;
+        w.position[t] = position; w.angle[t] = (double)position;
+        w.slot[t] = slot;
+        long long at = -1;
+        if (slot >= 0 && slot < (long long)A.num_blocks * A.block) {
+            // (32 bits divide in a quarter of the time)
+            const long long block = slot >> 32 ? slot / A.block : (long long)((unsigned)slot / (unsigned)A.block);
+            const int in = (int)(slot - block * A.block);
+            at = block * A.block_stride + (A.four ? (long long)(in >> 3) * octet_bytes(A.dim) : in * A.token_stride);
+        }
+        w.at[t] = at;
     }
-    if (A.half > 0) __syncthreads();
+    __syncthreads();
+}
+// Of tokens from..to - 1: cs[token][pairs], with room so that threads eight pairs apart meet different banks.
+__host__ __device__ inline int angle_step(int half) { return (half + 1) / 2 * 2 + 2 * ((half + 7) >> 3); }
+__device__ __forceinline__ int angle_at(int f) { return f + 2 * (f >> 3); }
+__device__ __forceinline__ void window_angles(const CacheArgs& A, const Tokens& w, float2* cs, int from, int to)
+{
+    if (A.half == 0) return;
+    const int step = angle_step(A.half);
+    // (a thread's pair and token go on by fixed steps: no divisions in the loop)
+    int tok = (int)(((float)threadIdx.x + 0.5f) * A.of_half), f = threadIdx.x - tok * A.half;
+    const int by_tok = A.by_half, by_f = kCacheThreads - by_tok * A.half;
+    for (tok += from; tok < to;) {
+        cs[tok * step + angle_at(f)] = cos_sin(w.angle[tok] * A.freq[f]);
+        tok += by_tok; f += by_f;
+        if (f >= A.half) { f -= A.half; tok++; }
+    }
+    __syncthreads();
 }
 
 // a rotated number: x the element itself, y the other of its pair
@@ -70,20 +112,67 @@ __device__ __forceinline__ float turned(float x, float y, float2 cs, bool second
     return second ? __fadd_rn(p, q) : __fsub_rn(p, q);
 }
 
+// N elements as they are held, as numbers and back: 16-bit ones by words of two
+template <typename T, int N> struct Raw { T x[N]; };
+template <int N> struct Raw<__nv_bfloat16, N> { unsigned w[(N + 1) / 2]; };
+template <int N> struct Raw<__half, N> { unsigned w[(N + 1) / 2]; };
 template <typename T, int N>
-__device__ __forceinline__ void load_n(float (&x)[N], const T* p)
+__device__ __forceinline__ Raw<T, N> load_raw(const T* p)
 {
-    const Pack<T, N> v = *reinterpret_cast<const Pack<T, N>*>(p);
+    Raw<T, N> r;
+    if constexpr (sizeof(T) == 2 && N == 1) r.w[0] = *reinterpret_cast<const unsigned short*>(p);
+    else {
+        constexpr int kWords = N * (int)sizeof(T) / 4, kEach = kWords < 4 ? kWords : 4;
+        unsigned* to = reinterpret_cast<unsigned*>(&r);
 #pragma unroll
-    for (int i = 0; i < N; i++) x[i] = to_f32(v.x[i]);
+        for (int i = 0; i < kWords; i += kEach) {
+            const Pack<unsigned, kEach> v = *reinterpret_cast<const Pack<unsigned, kEach>*>(reinterpret_cast<const unsigned*>(p) + i);
+#pragma unroll
+            for (int z = 0; z < kEach; z++) to[i + z] = v.x[z];
+        }
+    }
+    return r;
 }
+template <int N> __device__ __forceinline__ void unpack(float (&x)[N], const Raw<float, N>& r)
+{
+#pragma unroll
+    for (int i = 0; i < N; i++) x[i] = r.x[i];
+}
+template <int N> __device__ __forceinline__ void unpack(float (&x)[N], const Raw<__nv_bfloat16, N>& r)
+{
+#pragma unroll
+    for (int i = 0; i < N; i++) x[i] = __uint_as_float(i & 1 ? r.w[i / 2] & 0xffff0000u : r.w[i / 2] << 16);
+}
+template <int N> __device__ __forceinline__ void unpack(float (&x)[N], const Raw<__half, N>& r)
+{
+#pragma unroll
+    for (int i = 0; i < N; i++) {
+        const __half2 h = *reinterpret_cast<const __half2*>(&r.w[i / 2]);
+        x[i] = i & 1 ? __high2float(h) : __low2float(h);
+    }
+}
+__device__ __forceinline__ unsigned two_of(float a, float b, __nv_bfloat16) { const __nv_bfloat162 h = __floats2bfloat162_rn(a, b); return *reinterpret_cast<const unsigned*>(&h); }
+__device__ __forceinline__ unsigned two_of(float a, float b, __half) { const __half2 h = __floats2half2_rn(a, b); return *reinterpret_cast<const unsigned*>(&h); }
 template <typename T, int N>
 __device__ __forceinline__ void store_n(T* p, const float (&x)[N])
 {
-    Pack<T, N> v;
+    if constexpr (N == 1) *p = from_f32<T>(x[0]);
+    else {
+        constexpr int kWords = N * (int)sizeof(T) / 4, kEach = kWords < 4 ? kWords : 4;
+        unsigned w[kWords];
 #pragma unroll
-    for (int i = 0; i < N; i++) v.x[i] = from_f32<T>(x[i]);
-    *reinterpret_cast<Pack<T, N>*>(p) = v;
+        for (int i = 0; i < kWords; i++) {
+            if constexpr (sizeof(T) == 4) w[i] = __float_as_uint(x[i]);
+            else w[i] = two_of(x[2 * i], x[2 * i + 1], T());
+        }
+#pragma unroll
+        for (int i = 0; i < kWords; i += kEach) {
+            Pack<unsigned, kEach> v;
+#pragma unroll
+            for (int z = 0; z < kEach; z++) v.x[z] = w[i + z];
+            *reinterpret_cast<Pack<unsigned, kEach>*>(reinterpret_cast<unsigned*>(p) + i) = v;
+        }
+    }
 }
 
 // ---------------------------------------------------------------- 16- and 32-bit caches, and queries
@@ -102,27 +191,34 @@ __device__ __forceinline__ Pieces pieces_of(int e, int D, int half, bool interle
     return Pieces{2 * half + (e - turned) * N, half + D / 2 + (e - turned) * N, 0};
 }
 
+// (cs: of the token)
 template <int N>
 __device__ __forceinline__ void turn_pieces(float (&a)[N], float (&b)[N], const Pieces& p, const float2* cs, int half, bool interleaved)
 {
     if (p.turn == 1) {
-        const int f = interleaved ? p.c0 / 2 : p.c0;
+        // (N pairs from a multiple of N on: next to one another)
+        const float2* at = cs + angle_at(interleaved ? p.c0 / 2 : p.c0);
 #pragma unroll
-        for (int i = 0; i < N; i++) {
-            const float2 t = cs[f + i];
+        for (int i = 0; i < N; i += 2) {
+            const float4 t = N > 1 ? *reinterpret_cast<const float4*>(at + i) : make_float4(at[i].x, at[i].y, 0.f, 0.f);
             const float x = a[i], y = b[i];
-            a[i] = turned(x, y, t, false); b[i] = turned(y, x, t, true);
+            a[i] = turned(x, y, make_float2(t.x, t.y), false); b[i] = turned(y, x, make_float2(t.x, t.y), true);
+            if (N > 1) {
+                const float x1 = a[i + (N > 1)], y1 = b[i + (N > 1)];
+                a[i + (N > 1)] = turned(x1, y1, make_float2(t.z, t.w), false); b[i + (N > 1)] = turned(y1, x1, make_float2(t.z, t.w), true);
+            }
         }
     } else if (p.turn == 2) {
+        const float2 *at = cs + angle_at(p.c0 / 2), *bt = cs + angle_at(p.c1 / 2);
 #pragma unroll
         for (int i = 0; i + 1 < N; i += 2) {
             if (p.c0 + i < 2 * half) {
-                const float2 t = cs[(p.c0 + i) / 2];
+                const float2 t = at[i / 2];
                 const float x = a[i], y = a[i + 1];
                 a[i] = turned(x, y, t, false); a[i + 1] = turned(y, x, t, true);
             }
             if (p.c1 + i < 2 * half) {
-                const float2 t = cs[(p.c1 + i) / 2];
+                const float2 t = bt[i / 2];
                 const float x = b[i], y = b[i + 1];
                 b[i] = turned(x, y, t, false); b[i + 1] = turned(y, x, t, true);
             }
@@ -130,239 +226,345 @@ __device__ __forceinline__ void turn_pieces(float (&a)[N], float (&b)[N], const 
     }
 }
 
-// The rows of a window's tokens: keys and values (but for a 4-bit cache, whose queries alone come here), queries.
-template <typename T, typename C, int N, bool kQueries>
-__device__ __forceinline__ void append_rows(const CacheArgs& A, const float2* cs, int i0, int n, int part)
+// The rows of a window's tokens: keys and values (but for a 4-bit cache, whose queries alone come here), queries.  A team takes a row (a
+// head of keys, values or queries) of two tokens at a time; rows and pairs of tokens go on by fixed steps, without divisions.  With kEarly
+// what a team reads first, which depends on neither slots nor angles, is under way while `before` (the window's prologue) runs: for few tokens, where
+// that is a trip to memory less; where there are many, those without a place are not read.
+template <typename T, typename C, int N, bool kQueries, bool kEarly, class F>
+__device__ __forceinline__ void append_rows(const CacheArgs& A, const Tokens& w, const float2* cs, int i0, int n, int part, F before)
 {
-    constexpr int kRows = 2;                               // in flight for each team
-    const int D = A.dim, chunks = D / (2 * N), team = A.team, in_team = threadIdx.x & (team - 1);
-    const int per = (kQueries ? 0 : 2 * A.heads) + A.x.q_heads, total = n * per, teams = kCacheThreads / team;
-    const long long places = (long long)A.num_blocks * A.block;
-    for (int r0 = part * teams + threadIdx.x / team; r0 < total; r0 += kRows * A.split * teams) {
-        const T* src[kRows];
-        void* dst[kRows];
-        int tok[kRows], kind[kRows];                       // kind: 0 nothing, 1 keys, 2 values, 3 queries
+    constexpr int kTok = kEarly ? 1 : 2;
+    const int D = A.dim, chunks = D / (2 * N), team = A.team, in_team = threadIdx.x & (team - 1), teams = kCacheThreads / team;
+    const int kv = kQueries ? 0 : 2 * A.heads, per = kv + A.x.q_heads, stride = A.split * teams, step = angle_step(A.half);
+    const int by_tok = stride / per, by_row = stride - by_tok * per;
+    int row = part * teams + threadIdx.x / team, tok = row / per;
+    row -= tok * per;
+    tok *= kTok;
+    bool early = kEarly;
+    do {
+        // (a row's kind, and where it begins)
+        const bool live = tok < n, values = row >= A.heads && row < kv, queries = row >= kv;
+        const int head = queries ? row - kv : values ? row - A.heads : row, half = values ? 0 : A.half;
+        const bool interleaved = !values && A.interleaved;
+        const long long src_step = queries ? A.x.q_token : values ? A.x.v_token : A.x.k_token;
+        const T* src = (const T*)(queries ? A.x.q : values ? A.x.v : A.x.k) + (long long)head * (queries ? A.x.q_head : values ? A.x.v_head : A.x.k_head) + (i0 + tok) * src_step;
+        for (int e = in_team; e < chunks || early; e += team) {
+            const Pieces p = pieces_of<N>(e, D, half, interleaved);
+            Raw<T, N> a[kTok], b[kTok];
+            bool some[kTok];
 #pragma unroll
-        for (int u = 0; u < kRows; u++) {
-            const int r = r0 + u * A.split * teams;
-            kind[u] = 0; src[u] = nullptr; dst[u] = nullptr; tok[u] = 0;
-            if (r >= total) continue;
-            tok[u] = r / per;
-            int row = r - tok[u] * per;
-            const long long i = i0 + tok[u];
-            if (!kQueries && row < 2 * A.heads) {
-                const bool second = row >= A.heads;
-                if (second) row -= A.heads;
-                const long long slot = A.slots[i];
-                if (slot >= 0 && slot < places) {
-                    const long long block = slot / A.block, at = slot - block * A.block;
-                    const long long to = block * A.block_stride + at * A.token_stride + row * A.head_stride;
-                    kind[u] = second ? 2 : 1;
-                    src[u] = second ? (const T*)A.x.v + i * A.x.v_token + row * A.x.v_head : (const T*)A.x.k + i * A.x.k_token + row * A.x.k_head;
-                    dst[u] = (C*)(second ? A.values : A.keys) + to;
-                }
-            } else {
-                if (!kQueries) row -= 2 * A.heads;
-                if (!A.positions || A.positions[i] >= 0) {
-                    kind[u] = 3;
-                    src[u] = (const T*)A.x.q + i * A.x.q_token + row * A.x.q_head;
-                    dst[u] = (T*)A.x.q_out + i * A.x.out_token + row * A.x.out_head;
+            for (int u = 0; u < kTok; u++) {
+                some[u] = tok + u < n && e < chunks && (early || (queries ? w.position[tok + u] >= 0 : w.at[tok + u] >= 0));
+                if (some[u]) { a[u] = load_raw<T, N>(src + u * src_step + p.c0); b[u] = load_raw<T, N>(src + u * src_step + p.c1); }
+            }
+            if (early) {
+                before();
+                early = false;
+                if (live) some[0] = some[0] && (queries ? w.position[tok] >= 0 : w.at[tok] >= 0);
+            }
+#pragma unroll
+            for (int u = 0; u < kTok; u++) {
+                if (!some[u]) continue;
+                float x[N], y[N];
+                unpack(x, a[u]); unpack(y, b[u]);
+                turn_pieces<N>(x, y, p, cs + (tok + u) * step, half, interleaved);
+                if (queries) {
+                    T* to = (T*)A.x.q_out + (long long)head * A.x.out_head + (i0 + tok + u) * A.x.out_token;
+                    store_n<T, N>(to + p.c0, x); store_n<T, N>(to + p.c1, y);
+                } else {
+                    C* to = (C*)(values ? A.values : A.keys) + (long long)head * A.head_stride + w.at[tok + u];
+                    store_n<C, N>(to + p.c0, x); store_n<C, N>(to + p.c1, y);
                 }
             }
         }
+        tok += kTok * by_tok; row += by_row;
+        if (row >= per) { row -= per; tok += kTok; }
+    } while (tok < n);
+}
+
+// Rows of one kind (keys, values or queries) of a window of many tokens, two tokens of a head at a time by a team.
+template <typename T, typename C, int N, bool kCache, bool kTurn>
+__device__ __forceinline__ void append_kind(const CacheArgs& A, const Tokens& w, const float2* cs, int i0, int n, int part, const T* src, int src_token, int src_head,
+                                            C* dst, long long dst_token, long long dst_head, int heads, int by_pair, float of_heads)
+{
+    const int D = A.dim, chunks = D / (2 * N), team = A.team, in_team = threadIdx.x & (team - 1), teams = kCacheThreads / team, stride = A.split * teams;
+    const int half = kTurn ? A.half : 0, step = angle_step(half);
+    const bool interleaved = kTurn && A.interleaved;
+    const int by_head = stride - by_pair * heads;
+    int head = part * teams + threadIdx.x / team, tok = (int)(((float)head + 0.5f) * of_heads);
+    head -= tok * heads;
+    tok *= 2;
+    for (; tok < n; tok += 2 * by_pair, head += by_head) {
+        if (head >= heads) { head -= heads; tok += 2; if (tok >= n) break; }
+        const T* from = src + (long long)head * src_head + (long long)(i0 + tok) * src_token;
+        C* to = dst + (long long)head * dst_head;
         for (int e = in_team; e < chunks; e += team) {
-            const Pieces turn = pieces_of<N>(e, D, A.half, A.interleaved), plain = pieces_of<N>(e, D, 0, false);
-            float a[kRows][N], b[kRows][N];
+            const Pieces p = pieces_of<N>(e, D, half, interleaved);
+            Raw<T, N> a[2], b[2];
+            bool some[2];
+            long long at[2];
 #pragma unroll
-            for (int u = 0; u < kRows; u++) {
-                const Pieces& p = kind[u] == 2 ? plain : turn;
-                if (kind[u]) { load_n<T, N>(a[u], src[u] + p.c0); load_n<T, N>(b[u], src[u] + p.c1); }
+            for (int u = 0; u < 2; u++) {
+                some[u] = tok + u < n;
+                if (some[u]) {
+                    at[u] = kCache ? w.at[tok + u] : (long long)(i0 + tok + u) * dst_token;
+                    some[u] = kCache ? at[u] >= 0 : w.position[tok + u] >= 0;
+                }
+                if (some[u]) { a[u] = load_raw<T, N>(from + u * src_token + p.c0); b[u] = load_raw<T, N>(from + u * src_token + p.c1); }
             }
 #pragma unroll
-            for (int u = 0; u < kRows; u++) {
-                if (!kind[u]) continue;
-                const Pieces& p = kind[u] == 2 ? plain : turn;
-                if (kind[u] != 2) turn_pieces<N>(a[u], b[u], p, cs + tok[u] * A.half, A.half, A.interleaved);
-                if (kind[u] == 3) { store_n<T, N>((T*)dst[u] + p.c0, a[u]); store_n<T, N>((T*)dst[u] + p.c1, b[u]); }
-                else { store_n<C, N>((C*)dst[u] + p.c0, a[u]); store_n<C, N>((C*)dst[u] + p.c1, b[u]); }
+            for (int u = 0; u < 2; u++) {
+                if (!some[u]) continue;
+                float x[N], y[N];
+                unpack(x, a[u]); unpack(y, b[u]);
+                if (kTurn) turn_pieces<N>(x, y, p, cs + (tok + u) * step, half, interleaved);
+                store_n<C, N>(to + at[u] + p.c0, x); store_n<C, N>(to + at[u] + p.c1, y);
             }
         }
     }
 }
 
-template <typename T, typename C, int N>
-__global__ void __launch_bounds__(kCacheThreads)
+template <typename T, typename C, int N, bool kFew>
+__global__ void __launch_bounds__(kCacheThreads, 4)
 append_kernel(const __grid_constant__ CacheArgs A)
 {
-    extern __shared__ float2 cs[];
+    extern __shared__ __align__(16) float2 cs[];
+    __shared__ Tokens w;
     pdl_wait();
     const int i0 = blockIdx.x * A.window, n = min(A.window, A.tokens - i0);
-    fill_angles(A, cs, i0, n);
-    append_rows<T, C, N, false>(A, cs, i0, n, blockIdx.y);
+    auto prologue = [&] { window_tokens(A, w, i0, n); window_angles(A, w, cs, 0, n); };
+    if (!kFew) {
+        prologue();
+        const gr_cache_tokens& x = A.x;
+        append_kind<T, C, N, true, true>(A, w, cs, i0, n, blockIdx.y, (const T*)x.k, (int)x.k_token, (int)x.k_head, (C*)A.keys, 0, A.head_stride, A.heads, A.by_heads, A.of_heads);
+        append_kind<T, C, N, true, false>(A, w, cs, i0, n, blockIdx.y, (const T*)x.v, (int)x.v_token, (int)x.v_head, (C*)A.values, 0, A.head_stride, A.heads, A.by_heads, A.of_heads);
+        if (x.q_heads > 0)
+            append_kind<T, T, N, false, true>(A, w, cs, i0, n, blockIdx.y, (const T*)x.q, (int)x.q_token, (int)x.q_head, (T*)x.q_out, x.out_token, x.out_head, x.q_heads, A.by_queries, A.of_queries);
+    } else append_rows<T, C, N, false, true>(A, w, cs, i0, n, blockIdx.y, prologue);
 }
 
 // ---------------------------------------------------------------- a 4-bit cache
 
-// The run of tokens that begins at i, if one does: tokens i, i + 1, ... that lie one after another in one octet.  0: the token before
-// has it, or it has no place.
-__device__ __forceinline__ int run_at(const CacheArgs& A, int i, long long& slot)
+// The runs that begin in a window of n tokens, of m that are looked at: tokens i, i + 1, ... that lie one after another in one octet, i the
+// window's first where the one before has no such run.
+__device__ __forceinline__ void window_runs(const CacheArgs& A, Tokens& w, int i0, int n, int m)
 {
-    const long long places = (long long)A.num_blocks * A.block;
-    slot = A.slots[i];
-    if (slot < 0 || slot >= places) return 0;
-    if ((slot & 7) != 0 && i > 0 && A.slots[i - 1] == slot - 1) return 0;
-    int n = 1;
-    while (n < 8 - (int)(slot & 7) && i + n < A.tokens && A.slots[i + n] == slot + n) n++;
-    return n;
+    if (threadIdx.x < 32) {
+        const int t = threadIdx.x;
+        bool begins = false;
+        int size = 0;
+        if (t < n && w.at[t] >= 0) {
+            const long long slot = w.slot[t];
+            const int in = (int)(slot & 7);
+            begins = in == 0 || (t > 0 ? w.slot[t - 1] != slot - 1 : i0 == 0 || A.slots[i0 - 1] != slot - 1);
+            size = 1;
+            while (size < 8 - in && t + size < m && w.slot[t + size] == slot + size) size++;
+        }
+        const unsigned mask = __ballot_sync(0xffffffffu, begins);
+        if (begins) {
+            const int k = __popc(mask & ((1u << t) - 1u));
+            w.first[k] = t; w.size[k] = size;
+        }
+        if (t == 0) w.runs = __popc(mask);
+    }
+    __syncthreads();
 }
 
-// Code of x, in units of s: the whole number nearest to x / s from -8 to 7 (ties to even), decided by the sign of x - (m + 1/2) s,
-// which one fused operation gives exactly; then + 8.
-__device__ __forceinline__ unsigned code_of(float x, float s, float inverse)
-{
-    const float m = floorf(fminf(fmaxf(x * inverse, -9.f), 8.f));
-    const float d = fmaf(-(m + 0.5f), s, x), up = s < 0.f ? -d : d;
-    const int w = (int)m;
-    return (unsigned)(min(max(w + (up > 0.f || (up == 0.f && (w & 1)) ? 1 : 0), -8), 7) + 8);
-}
-
-// The half word of codes of four dims x of a group of eight lanes, and the group's scale: that of the element of largest magnitude
+// The word of codes of eight dims x (as pairs) of a group of four lanes, and the group's scale: that of the element of largest magnitude
 // (the positive one of two), for which the code is 0, that is -8, as fp16.  A group with a NaN or an infinity gets the scale NaN.
-__device__ __forceinline__ unsigned short quantise(const float (&x)[4], unsigned short& scale)
+__device__ __forceinline__ unsigned quantise(const unsigned long long (&x)[4], unsigned& scale)
 {
-    float hi = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), lo = fminf(fminf(x[0], x[1]), fminf(x[2], x[3]));
-    const bool bad = !(fabsf(x[0]) < INFINITY && fabsf(x[1]) < INFINITY && fabsf(x[2]) < INFINITY && fabsf(x[3]) < INFINITY);
+    // (a NaN stays the largest; magnitudes order as their bits, the sign goes below them)
+    float hi = f_lo(x[0]), lo = hi;
 #pragma unroll
-    for (int o = 1; o < 8; o *= 2) {
-        hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
-        lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
+    for (int i = 1; i < 8; i++) {
+        const float v = i & 1 ? f_hi(x[i / 2]) : f_lo(x[i / 2]);
+        asm("max.NaN.f32 %0, %0, %1;" : "+f"(hi) : "f"(v));
+        lo = fminf(lo, v);
     }
-    const unsigned met = __ballot_sync(0xffffffffu, bad) >> (threadIdx.x & 24) & 0xffu;
-    const __half h = __float2half_rn(fminf(fmaxf((hi >= -lo ? hi : lo) * -0.125f, -65504.f), 65504.f));
-    const float s = __half2float(h), inverse = 1.f / s;
-    scale = met ? 0x7fffu : __half_as_ushort(h);
-    if (met || s == 0.f) return 0x8888u;
-    return (unsigned short)(code_of(x[0], s, inverse) | code_of(x[1], s, inverse) << 4 | code_of(x[2], s, inverse) << 8 | code_of(x[3], s, inverse) << 12);
+    const float peak = -lo > hi ? lo : hi;
+    unsigned most = __funnelshift_l(~__float_as_uint(peak), __float_as_uint(peak), 1);
+    most = max(most, __shfl_xor_sync(0xffffffffu, most, 1));
+    most = max(most, __shfl_xor_sync(0xffffffffu, most, 2));
+    const bool met = most >= 0xff000000u;
+    const __half h = __float2half_rn(fminf(__uint_as_float(most >> 1) * 0.125f, 65504.f));
+    scale = met ? 0x7fffu : (unsigned)__half_as_ushort(h) | (most & 1) << 15;
+    if (met || (scale & 0x7fffu) == 0) return 0x88888888u;
+    const float s = __half2float(__ushort_as_half((unsigned short)scale));
+    float inverse;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inverse) : "f"(s));
+    // The whole number w nearest to x / s by the approximate quotient (8 is added in units of the sum's last place), or one next to that: x - w s is
+    // exact in one fused operation, and where it is more than half of s, or half of it and w odd, its sign says which.
+    const float magic = 12582912.f + 8.f, half = 0.5f * fabsf(s);
+    const unsigned long long inverse2 = f_pack(inverse, inverse), magic2 = f_pack(magic, magic), s2 = f_pack(-s, -s), back2 = f_pack(-magic, -magic);
+    int code[8];
+    unsigned long long left[4];
+    float most_left = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+        const unsigned long long y = fma2(x[i], inverse2, magic2);
+        left[i] = fma2(add2(y, back2), s2, x[i]);
+        most_left = fmaxf(most_left, fmaxf(fabsf(f_lo(left[i])), fabsf(f_hi(left[i]))));
+        code[2 * i] = (int)(unsigned)y - (int)__float_as_uint(12582912.f);
+        code[2 * i + 1] = (int)(unsigned)(y >> 32) - (int)__float_as_uint(12582912.f);
+    }
+    // (fp16 scales below 2^-14 are so coarse that quotients below -8 come up)
+    if (most_left >= half || (scale & 0x7c00u) == 0) {
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            const float r = i & 1 ? f_hi(left[i / 2]) : f_lo(left[i / 2]);
+            if (fabsf(r) > half || (fabsf(r) == half && (code[i] & 1))) code[i] += (r < 0.f) != (s < 0.f) ? -1 : 1;
+            code[i] = max(code[i], 0);
+        }
+    }
+    unsigned w = (unsigned)min(code[7], 15);
+#pragma unroll
+    for (int i = 6; i >= 0; i--) w = w * 16u + (unsigned)min(code[i], 15);
+    return w;
 }
 
-// four elements from c on of a row, rotated
-template <typename T, bool kVec>
-__device__ __forceinline__ void load_four(float (&x)[4], const T* row, int c)
+// x cos + y sin of eight elements next to one another and their partners (sin of the sign that the elements' side of the pairs has), products rounded
+// one by one
+__device__ __forceinline__ unsigned long long turned2(unsigned long long x, unsigned long long y, float c0, float s0, float c1, float s1)
 {
-    if (kVec) load_n<T, 4>(x, row + c);
-    else {
-#pragma unroll
-        for (int i = 0; i < 4; i++) x[i] = to_f32(row[c + i]);
-    }
-}
-template <typename T, bool kVec>
-__device__ __forceinline__ void load_partners(float (&y)[4], const float (&x)[4], const T* row, int c, int half, bool interleaved)
-{
-    if (interleaved) {
-#pragma unroll
-        for (int i = 0; i < 4; i++) y[i] = x[i ^ 1];
-    } else if (kVec) {
-        if (c < 2 * half) load_n<T, 4>(y, row + (c < half ? c + half : c - half));
-    } else {
-#pragma unroll
-        for (int i = 0; i < 4; i++) if (c + i < 2 * half) y[i] = to_f32(row[c + i < half ? c + i + half : c + i - half]);
-    }
+    return add2(mul2(x, f_pack(c0, c1)), mul2(y, f_pack(s0, s1)));
 }
 
 template <typename T, bool kVec>
-__global__ void __launch_bounds__(kCacheThreads)
+__global__ void __launch_bounds__(kCacheThreads, 4)
 append4_kernel(const __grid_constant__ CacheArgs A)
 {
-    extern __shared__ float2 cs[];
+    extern __shared__ __align__(16) float2 cs[];
+    __shared__ Tokens w;
     pdl_wait();
-    const int w0 = blockIdx.x * A.window, wn = min(A.window, A.tokens - w0);
+    const int w0 = blockIdx.x * A.window, wn = min(A.window, A.tokens - w0), wm = min(A.window + 7, A.tokens - w0);
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, D = A.dim, J = D / 32, half = A.half;
-    for (int i0 = w0; i0 < w0 + wn; i0++) {
-        long long slot;
-        const int n = run_at(A, i0, slot);
-        if (n == 0) continue;                              // (the same for all threads)
-        const int first = (int)(slot & 7);
-        if (i0 > w0) __syncthreads();                      // (the angles of the run before are done with)
-        fill_angles(A, cs, i0, n);
-        const long long block = slot / A.block;
-        char* base = A.keys + block * A.block_stride + (long long)((int)(slot - block * A.block) >> 3) * octet_bytes(D);
-        const long long head_bytes = (long long)(A.block >> 3) * octet_bytes(D);
-        // (head, keys or values) by warps; a lane has four dims, half a word of keys, a half word of values
-        for (int e = blockIdx.y * kCacheWarps + warp; e < 2 * A.heads; e += A.split * kCacheWarps) {
-            const bool second = e >= A.heads;
-            const int head = second ? e - A.heads : e;
-            char* octet = base + head * head_bytes;
-            const T* row = second ? (const T*)A.x.v + i0 * A.x.v_token + head * A.x.v_head : (const T*)A.x.k + i0 * A.x.k_token + head * A.x.k_head;
-            const long long step = second ? A.x.v_token : A.x.k_token;
-            for (int c0 = 0; c0 < D; c0 += 128) {
-                const int c = c0 + 4 * lane, j = c >> 5, r = lane & 7;
-                const bool in = c < D;
-#pragma unroll 1
-                for (int o0 = first & 4; o0 < first + n; o0 += 4) {      // four of the octet's places at a time
-                    float x[4][4], y[4][4];
-                    bool some[4];
+    window_tokens(A, w, w0, wm);
+    window_runs(A, w, w0, wn, wm);
+    // (the tokens of the runs, and of the queries)
+    if (w.runs > 0 || A.x.q_heads > 0) {
+        const int last = w.runs > 0 ? w.first[w.runs - 1] + w.size[w.runs - 1] : 0;
+        window_angles(A, w, cs, A.x.q_heads > 0 ? 0 : w.first[0], A.x.q_heads > 0 ? max(last, wn) : last);
+    }
+    const long long head_bytes = (long long)(A.block >> 3) * octet_bytes(D);
+    // Of each run a head's keys or values by warps, a pair of the octet's places by each of four, a token of the pair by half a warp, eight dims
+    // by a lane: a word of keys; of values two half words, of which the two tokens' lanes exchange one, so that each writes a word.
+    const int mine = lane >> 4, l = lane & 15, o0 = 2 * (warp & 3);
+    for (int run = 0; run < w.runs; run++) {
+        const int tok = w.first[run], n = w.size[run], first = (int)(w.slot[tok] & 7), at = tok + o0 - first + mine;      // at: this half warp's token in the window
+        if (o0 + 1 < first || o0 >= first + n) continue;
+        const bool has = o0 + mine >= first && o0 + mine < first + n, both = o0 >= first && o0 + 1 < first + n;
+        const float2* angle = cs + at * angle_step(half);
+        const int every = 2 * A.split, from = 2 * blockIdx.y + (warp >> 2);
+        for (int c0 = 0; c0 < D; c0 += 128) {
+            const int c = c0 + 8 * l, j = c >> 5, t = l & 3;
+            const bool in = c < D && has;
+            // ---- keys
+            {
+                const T* row = (const T*)A.x.k + (long long)from * A.x.k_head + (long long)(w0 + at) * A.x.k_token;
+                char* octet = A.keys + w.at[tok] + from * head_bytes;
+                const bool turns = in && c < 2 * half, two = c >= half, pairs = turns && kVec && !A.interleaved;
+                const int other = two ? c - half : c + half;
+                const float sign = two ? 1.f : -1.f;
+                Raw<T, 8> x_next, y_next;
+                if (kVec && in && from < A.heads) { x_next = load_raw<T, 8>(row + c); if (pairs) y_next = load_raw<T, 8>(row + other); }
+                for (int head = from; head < A.heads; head += every) {
+                    float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+                    unsigned long long x2[4];
+                    const T* here = row;
+                    row += (long long)every * A.x.k_head;
+                    if (in) {
+                        if (kVec) {
+                            // (a head ahead)
+                            const Raw<T, 8> x_raw = x_next, y_raw = y_next;
+                            if (head + every < A.heads) { x_next = load_raw<T, 8>(row + c); if (pairs) y_next = load_raw<T, 8>(row + other); }
+                            unpack(x, x_raw);
+                            if (pairs) {
+                                // (the eight are on one side of their pairs: a difference is a sum with a number of the other sign)
+                                float y[8];
+                                unpack(y, y_raw);
+                                const float4* z = reinterpret_cast<const float4*>(angle + angle_at(two ? c - half : c));
 #pragma unroll
-                    for (int u = 0; u < 4; u++) {
-                        const int t = o0 + u - first;
-                        some[u] = t >= 0 && t < n;
-#pragma unroll
-                        for (int i = 0; i < 4; i++) { x[u][i] = 0.f; y[u][i] = 0.f; }
-                        if (some[u] && in) {
-                            load_four<T, kVec>(x[u], row + t * step, c);
-                            if (!second && c < 2 * half) load_partners<T, kVec>(y[u], x[u], row + t * step, c, half, A.interleaved);
-                        }
-                    }
-                    unsigned short code[4], scale[4];
-#pragma unroll
-                    for (int u = 0; u < 4; u++) {
-                        if (!second && some[u]) {
-                            const float2* at = cs + (o0 + u - first) * half;
-#pragma unroll
-                            for (int i = 0; i < 4; i++) {
-                                const int d = c + i;
-                                if (d >= 2 * half) continue;
-                                const bool two = A.interleaved ? d & 1 : d >= half;
-                                x[u][i] = turned(x[u][i], y[u][i], at[A.interleaved ? d >> 1 : two ? d - half : d], two);
-                            }
-                        }
-                        code[u] = quantise(x[u], scale[u]);
-                    }
-                    if (!in) continue;
-                    if (!second) {
-#pragma unroll
-                        for (int u = 0; u < 4; u++) {
-                            if (!some[u]) continue;
-                            *(unsigned short*)(octet + (o0 + u) * (D / 2) + ((r >> 1) * J + j) * 4 + (r & 1) * 2) = code[u];
-                            if (r == 0) *(unsigned short*)(octet + octet_kscale(D) + ((o0 + u) * J + j) * 2) = scale[u];
-                        }
-                    } else {
-#pragma unroll
-                        for (int u = 0; u < 4; u += 2) {
-                            const int pair = (o0 + u) >> 1;
-                            char* at = octet + octet_vcode(D) + ((r * 4 + pair) * J + j) * 4;
-                            char* sc = octet + octet_vscale(D) + (pair * J + j) * 4;
-                            if (some[u] && some[u + 1]) {
-                                *(unsigned*)at = code[u] | (unsigned)code[u + 1] << 16;
-                                if (r == 0) *(unsigned*)sc = scale[u] | (unsigned)scale[u + 1] << 16;
-                            } else {
-#pragma unroll
-                                for (int z = 0; z < 2; z++) {
-                                    if (!some[u + z]) continue;
-                                    *(unsigned short*)(at + 2 * z) = code[u + z];
-                                    if (r == 0) *(unsigned short*)(sc + 2 * z) = scale[u + z];
+                                for (int i = 0; i < 8; i += 2) {
+                                    const float4 q = z[i / 2];
+                                    const unsigned long long r = turned2(f_pack(x[i], x[i + 1]), mul2(f_pack(y[i], y[i + 1]), f_pack(sign, sign)), q.x, q.y, q.z, q.w);
+                                    x[i] = f_lo(r); x[i + 1] = f_hi(r);
                                 }
                             }
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < 8; i++) x[i] = to_f32(here[c + i]);
+                        }
+                        if (turns && A.interleaved) {
+#pragma unroll
+                            for (int i = 0; i < 8; i += 2) {
+                                if (c + i >= 2 * half) continue;
+                                const float2 z = angle[angle_at((c + i) >> 1)];
+                                const float a = x[i], b = x[i + 1];
+                                x[i] = turned(a, b, z, false); x[i + 1] = turned(b, a, z, true);
+                            }
+                        } else if (turns && !kVec) {
+#pragma unroll
+                            for (int i = 0; i < 8; i++) {
+                                const int d = c + i;
+                                if (d < 2 * half) x[i] = turned(x[i], to_f32(here[d < half ? d + half : d - half]), angle[angle_at(d >= half ? d - half : d)], d >= half);
+                            }
                         }
                     }
+#pragma unroll
+                    for (int i = 0; i < 4; i++) x2[i] = f_pack(x[2 * i], x[2 * i + 1]);
+                    unsigned scale;
+                    const unsigned code = quantise(x2, scale);
+                    if (in) {
+                        *(unsigned*)(octet + (o0 + mine) * (D / 2) + (t * J + j) * 4) = code;
+                        if (t == 0) *(unsigned short*)(octet + octet_kscale(D) + ((o0 + mine) * J + j) * 2) = (unsigned short)scale;
+                    }
+                    octet += every * head_bytes;
+                }
+            }
+            // ---- values
+            {
+                const T* row = (const T*)A.x.v + (long long)from * A.x.v_head + (long long)(w0 + at) * A.x.v_token;
+                char* octet = A.keys + w.at[tok] + from * head_bytes;
+                Raw<T, 8> x_next;
+                if (kVec && in && from < A.heads) x_next = load_raw<T, 8>(row + c);
+                for (int head = from; head < A.heads; head += every) {
+                    float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+                    const T* here = row;
+                    row += (long long)every * A.x.v_head;
+                    if (in) {
+                        if (kVec) {
+                            const Raw<T, 8> x_raw = x_next;
+                            if (head + every < A.heads) x_next = load_raw<T, 8>(row + c);
+                            unpack(x, x_raw);
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < 8; i++) x[i] = to_f32(here[c + i]);
+                        }
+                    }
+                    unsigned long long x2[4];
+#pragma unroll
+                    for (int i = 0; i < 4; i++) x2[i] = f_pack(x[2 * i], x[2 * i + 1]);
+                    unsigned scale;
+                    const unsigned code = quantise(x2, scale), other = __shfl_xor_sync(0xffffffffu, code, 16);
+                    // half words 2 t and 2 t + 1 of this token: the first token's lane writes the former of both, the second's the latter
+                    char* to = octet + octet_vcode(D) + (((2 * t + mine) * 4 + (o0 >> 1)) * J + j) * 4;
+                    if (both) {
+                        if (in) *(unsigned*)to = mine ? __byte_perm(other, code, 0x7632) : __byte_perm(code, other, 0x5410);
+                    } else if (in) {
+                        char* own = octet + octet_vcode(D) + ((2 * t * 4 + (o0 >> 1)) * J + j) * 4 + 2 * mine;
+                        *(unsigned short*)own = (unsigned short)code;
+                        *(unsigned short*)(own + 16 * J) = (unsigned short)(code >> 16);
+                    }
+                    if (in && t == 0) *(unsigned short*)(octet + octet_vscale(D) + ((o0 >> 1) * J + j) * 4 + 2 * mine) = (unsigned short)scale;
+                    octet += every * head_bytes;
                 }
             }
         }
     }
     if (A.x.q_heads > 0) {
-        __syncthreads();
-        fill_angles(A, cs, w0, wn);
-        if (A.queries_vec) append_rows<T, T, 4, true>(A, cs, w0, wn, blockIdx.y);
-        else append_rows<T, T, 1, true>(A, cs, w0, wn, blockIdx.y);
+        if (A.queries_vec) append_rows<T, T, 4, true, false>(A, w, cs, w0, wn, blockIdx.y, [] {});
+        else append_rows<T, T, 1, true, false>(A, w, cs, w0, wn, blockIdx.y, [] {});
     }
 }
 
@@ -379,11 +581,13 @@ __global__ void __launch_bounds__(kCacheThreads)
 read_kernel(const __grid_constant__ ReadArgs R)
 {
     constexpr int kRows = 4;
+    __shared__ Tokens w;
     const CacheArgs& A = R.c;
     pdl_wait();
     const int i0 = blockIdx.x * A.window, n = min(A.window, A.tokens - i0), D = A.dim;
-    const int chunks = D / N, team = A.team, in_team = threadIdx.x & (team - 1), teams = kCacheThreads / team, total = n * 2 * A.heads;
-    const long long places = (long long)A.num_blocks * A.block;
+    const int chunks = D / N, team = A.team, in_team = threadIdx.x & (team - 1), teams = kCacheThreads / team, per = 2 * A.heads, total = n * per;
+    window_tokens(A, w, i0, n);
+    const float by_per = 1.f / (float)per;
     for (int r0 = blockIdx.y * teams + threadIdx.x / team; r0 < total; r0 += kRows * A.split * teams) {
         const C* src[kRows];
         T* dst[kRows];
@@ -392,79 +596,89 @@ read_kernel(const __grid_constant__ ReadArgs R)
             const int r = r0 + u * A.split * teams;
             src[u] = nullptr; dst[u] = nullptr;
             if (r >= total) continue;
-            const int tok = r / (2 * A.heads), row = r - tok * 2 * A.heads;
+            const int tok = (int)(((float)r + 0.5f) * by_per), row = r - tok * per;
             const bool second = row >= A.heads;
             const int head = second ? row - A.heads : row;
-            const long long i = i0 + tok, slot = A.slots[i];
+            const long long i = i0 + tok;
             dst[u] = second ? (T*)R.v + i * R.v_token + head * R.v_head : (T*)R.k + i * R.k_token + head * R.k_head;
-            if (slot >= 0 && slot < places) {
-                const long long block = slot / A.block, at = slot - block * A.block;
-                src[u] = (const C*)(second ? A.values : A.keys) + block * A.block_stride + at * A.token_stride + head * A.head_stride;
-            }
+            if (w.at[tok] >= 0) src[u] = (const C*)(second ? A.values : A.keys) + w.at[tok] + head * A.head_stride;
         }
         for (int e = in_team; e < chunks; e += team) {
-            float x[kRows][N];
+            Raw<C, N> x[kRows];
+#pragma unroll
+            for (int u = 0; u < kRows; u++) if (src[u]) x[u] = load_raw<C, N>(src[u] + e * N);
 #pragma unroll
             for (int u = 0; u < kRows; u++) {
+                if (!dst[u]) continue;
+                float y[N];
+                unpack(y, x[u]);
 #pragma unroll
-                for (int i = 0; i < N; i++) x[u][i] = 0.f;
-                if (src[u]) load_n<C, N>(x[u], src[u] + e * N);
+                for (int i = 0; i < N; i++) y[i] = src[u] ? y[i] : 0.f;
+                store_n<T, N>(dst[u] + e * N, y);
             }
-#pragma unroll
-            for (int u = 0; u < kRows; u++) if (dst[u]) store_n<T, N>(dst[u] + e * N, x[u]);
         }
     }
 }
 
-// Of a run of an octet a warp takes (head, keys or values): a lane the words of token lane / 4 (keys), of a pair of tokens (values).
-template <typename T, int J, bool kVec>
-__device__ __forceinline__ void read_octet(const char* octet, bool second, T* out, long long step, int first, int n, int lane)
+template <int J, typename W>
+__device__ __forceinline__ void load_run(W (&w)[J], const W* p)        // J words, aligned to all of them as far as J is even
 {
-    constexpr int D = 32 * J, kWords = J % 4 == 0 ? 4 : J % 2 == 0 ? 2 : 1;
-    const int g = lane >> 2, t = lane & 3;
-    unsigned w[J];
-    const unsigned* code = (const unsigned*)(octet + (second ? octet_vcode(D) : 0)) + lane * J;
+    constexpr int N = J % 4 == 0 ? 4 : J % 2 == 0 ? 2 : 1;
 #pragma unroll
-    for (int i = 0; i < J; i += kWords) {
-        const Pack<unsigned, kWords> p = *reinterpret_cast<const Pack<unsigned, kWords>*>(code + i);
+    for (int i = 0; i < J; i += N) {
+        const Pack<W, N> v = *reinterpret_cast<const Pack<W, N>*>(p + i);
 #pragma unroll
-        for (int z = 0; z < kWords; z++) w[i + z] = p.x[z];
+        for (int z = 0; z < N; z++) w[i + z] = v.x[z];
     }
-    if (!second) {
-        if (g < first || g >= first + n) return;
-        const __half* scale = (const __half*)(octet + octet_kscale(D)) + g * J;
-        T* to = out + (long long)(g - first) * step + 8 * t;
+}
+
+// Of a run of an octet a warp takes a head: a lane the words of token lane / 4 (keys) and of a pair of tokens (values).  s (u - 8) is
+// 16 s (1 + u / 16) - 24 s, u put into the fraction of 1: exact before its one rounding.
+template <typename T, int J, bool kVec>
+__device__ __forceinline__ void read_octet(const char* octet, T* k, T* v, long long k_step, long long v_step, int first, int n, int lane)
+{
+    constexpr int D = 32 * J;
+    const int g = lane >> 2, t = lane & 3;
+    unsigned kw[J], vw[J], vs[J];
+    unsigned short ks[J];
+    load_run<J>(kw, (const unsigned*)octet + lane * J);
+    load_run<J>(vw, (const unsigned*)(octet + octet_vcode(D)) + lane * J);
+    load_run<J>(ks, (const unsigned short*)(octet + octet_kscale(D)) + g * J);
+    load_run<J>(vs, (const unsigned*)(octet + octet_vscale(D)) + t * J);
+    auto number = [](unsigned word, int place, float s16, float s24) {       // the code at bits `place` .. + 3
+        const unsigned b = place < 19 ? word << (19 - place) : word >> (place - 19);
+        return fmaf(__uint_as_float(b & 0x00780000u | 0x3f800000u), s16, s24);
+    };
+    if (g >= first && g < first + n) {
+        T* to = k + (long long)(g - first) * k_step + 8 * t;
 #pragma unroll
         for (int j = 0; j < J; j++) {
-            const float s = __half2float(scale[j]);
+            const float s = __half2float(__ushort_as_half(ks[j])), s16 = 16.f * s, s24 = -24.f * s;
             float x[8];
 #pragma unroll
-            for (int i = 0; i < 8; i++) x[i] = (float)((int)(w[j] >> (4 * i) & 15u) - 8) * s;
+            for (int i = 0; i < 8; i++) x[i] = number(kw[j], 4 * i, s16, s24);
             if (kVec) store_n<T, 8>(to + 32 * j, x);
             else {
 #pragma unroll
                 for (int i = 0; i < 8; i++) to[32 * j + i] = from_f32<T>(x[i]);
             }
         }
-    } else {
-        const __half2* scale = (const __half2*)(octet + octet_vscale(D)) + t * J;
+    }
 #pragma unroll
-        for (int z = 0; z < 2; z++) {
-            const int tok = 2 * t + z;
-            if (tok < first || tok >= first + n) continue;
-            T* to = out + (long long)(tok - first) * step + 4 * g;
+    for (int z = 0; z < 2; z++) {
+        const int tok = 2 * t + z;
+        if (tok < first || tok >= first + n) continue;
+        T* to = v + (long long)(tok - first) * v_step + 4 * g;
 #pragma unroll
-            for (int j = 0; j < J; j++) {
-                const __half2 h = scale[j];
-                const float s = z ? __high2float(h) : __low2float(h);
-                float x[4];
+        for (int j = 0; j < J; j++) {
+            const float s = __half2float(__ushort_as_half((unsigned short)(vs[j] >> (16 * z)))), s16 = 16.f * s, s24 = -24.f * s;
+            float x[4];
 #pragma unroll
-                for (int i = 0; i < 4; i++) x[i] = (float)((int)(w[j] >> (16 * z + 4 * i) & 15u) - 8) * s;
-                if (kVec) store_n<T, 4>(to + 32 * j, x);
-                else {
+            for (int i = 0; i < 4; i++) x[i] = number(vw[j], 16 * z + 4 * i, s16, s24);
+            if (kVec) store_n<T, 4>(to + 32 * j, x);
+            else {
 #pragma unroll
-                    for (int i = 0; i < 4; i++) to[32 * j + i] = from_f32<T>(x[i]);
-                }
+                for (int i = 0; i < 4; i++) to[32 * j + i] = from_f32<T>(x[i]);
             }
         }
     }
@@ -475,31 +689,29 @@ __global__ void __launch_bounds__(kCacheThreads)
 read4_kernel(const __grid_constant__ ReadArgs R)
 {
     const CacheArgs& A = R.c;
+    __shared__ Tokens w;
     pdl_wait();
-    const int w0 = blockIdx.x * A.window, wn = min(A.window, A.tokens - w0);
+    const int w0 = blockIdx.x * A.window, wn = min(A.window, A.tokens - w0), wm = min(A.window + 7, A.tokens - w0);
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     constexpr int D = 32 * J;
-    const long long places = (long long)A.num_blocks * A.block, head_bytes = (long long)(A.block >> 3) * octet_bytes(D);
-    for (int i0 = w0; i0 < w0 + wn; i0++) {
-        long long slot;
-        const int n = run_at(A, i0, slot);
-        if (n == 0) {
-            if (slot >= 0 && slot < places) continue;
-            // (no place: zeros)
-            for (int e = blockIdx.y * kCacheThreads + threadIdx.x; e < 2 * A.heads * D; e += A.split * kCacheThreads) {
-                const int row = e / D, d = e - row * D;
-                if (row < A.heads) ((T*)R.k)[i0 * R.k_token + row * R.k_head + d] = from_f32<T>(0.f);
-                else ((T*)R.v)[i0 * R.v_token + (row - A.heads) * R.v_head + d] = from_f32<T>(0.f);
-            }
-            continue;
-        }
-        const long long block = slot / A.block;
-        const char* base = A.keys + block * A.block_stride + (long long)((int)(slot - block * A.block) >> 3) * octet_bytes(D);
-        for (int e = blockIdx.y * kCacheWarps + warp; e < 2 * A.heads; e += A.split * kCacheWarps) {
-            const int head = e >> 1;
-            const bool second = e & 1;
-            T* out = second ? (T*)R.v + i0 * R.v_token + head * R.v_head : (T*)R.k + i0 * R.k_token + head * R.k_head;
-            read_octet<T, J, kVec>(base + head * head_bytes, second, out, second ? R.v_token : R.k_token, (int)(slot & 7), n, lane);
+    window_tokens(A, w, w0, wm);
+    window_runs(A, w, w0, wn, wm);
+    const long long head_bytes = (long long)(A.block >> 3) * octet_bytes(D);
+    for (int item = blockIdx.y * kCacheWarps + warp; item < w.runs * A.heads; item += A.split * kCacheWarps) {
+        const int run = item / A.heads, head = item - run * A.heads, tok = w.first[run];
+        const long long i = w0 + tok;
+        read_octet<T, J, kVec>(A.keys + w.at[tok] + head * head_bytes, (T*)R.k + i * R.k_token + head * R.k_head, (T*)R.v + i * R.v_token + head * R.v_head,
+                               R.k_token, R.v_token, (int)(w.slot[tok] & 7), w.size[run], lane);
+    }
+    // (no place: zeros)
+    const float none[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    for (int tok = 0; tok < wn; tok++) {
+        if (w.at[tok] >= 0) continue;
+        const long long i = w0 + tok;
+        for (int row = blockIdx.y * kCacheWarps + warp; row < 2 * A.heads; row += A.split * kCacheWarps) {
+            T* to = row < A.heads ? (T*)R.k + i * R.k_token + row * R.k_head : (T*)R.v + i * R.v_token + (row - A.heads) * R.v_head;
+            if (kVec) { if (8 * lane < D) store_n<T, 8>(to + 8 * lane, none); }
+            else for (int d = lane; d < D; d += 32) to[d] = from_f32<T>(0.f);
         }
     }
 }
@@ -529,12 +741,21 @@ int check_cache(const void* keys, const void* values, const gr_cache_layout* lay
     return GR_OK;
 }
 
-// How a call's tokens are dealt out: windows of one token where there are few, with the heads in several CTAs until an SM has two.
-static void deal(CacheArgs& A, int rows_of_token)
+// How a call's tokens are dealt out: windows of one token where there are few, with the heads in several CTAs until an SM has two; of `most`
+// where that leaves every SM four, else of eight.
+static void deal(CacheArgs& A, int rows_of_token, int most)
 {
-    A.window = A.tokens >= kCacheMany ? kCacheWindow : 1;
+    A.window = A.tokens >= 4 * kSms * most ? most : A.tokens >= kCacheMany ? 8 : 1;
     const int windows = (A.tokens + A.window - 1) / A.window;
     A.split = std::max(1, std::min((2 * kSms + windows - 1) / windows, (rows_of_token + kCacheWarps - 1) / kCacheWarps));
+}
+
+// (after the team is known)
+static void quotients(CacheArgs& A)
+{
+    const int stride = A.split * (kCacheThreads / A.team), half = std::max(1, A.half), queries = std::max(1, A.x.q_heads);
+    A.by_half = kCacheThreads / half; A.by_heads = stride / A.heads; A.by_queries = stride / queries;
+    A.of_half = 1.f / (float)half; A.of_heads = 1.f / (float)A.heads; A.of_queries = 1.f / (float)queries;
 }
 
 template <class Args>
@@ -551,13 +772,19 @@ static void launch_cache(void (*kernel)(Args), const Args& args, const CacheArgs
 
 static int pow2_up(int n) { int p = 1; while (p < n) p *= 2; return std::min(p, 32); }
 
+template <typename T, typename C, bool kFew>
+static void launch_append_of(CacheArgs& A, int n, int smem, cudaStream_t st)
+{
+    A.team = pow2_up(A.dim / (2 * n));
+    quotients(A);
+    if (sizeof(T) == 2 && sizeof(C) == 2 && n == 8) launch_cache(append_kernel<T, C, sizeof(T) == 2 && sizeof(C) == 2 ? 8 : 4, kFew>, A, A, smem, st);
+    else if (n == 4) launch_cache(append_kernel<T, C, 4, kFew>, A, A, smem, st);
+    else launch_cache(append_kernel<T, C, 1, kFew>, A, A, smem, st);
+}
 template <typename T, typename C>
 static void launch_append(CacheArgs& A, int n, int smem, cudaStream_t st)
 {
-    A.team = pow2_up(A.dim / (2 * n));
-    if (sizeof(T) == 2 && sizeof(C) == 2 && n == 8) launch_cache(append_kernel<T, C, sizeof(T) == 2 && sizeof(C) == 2 ? 8 : 4>, A, A, smem, st);
-    else if (n == 4) launch_cache(append_kernel<T, C, 4>, A, A, smem, st);
-    else launch_cache(append_kernel<T, C, 1>, A, A, smem, st);
+    if (A.window == 1) launch_append_of<T, C, true>(A, n, smem, st); else launch_append_of<T, C, false>(A, n, smem, st);
 }
 template <typename T>
 static void launch_append_to(CacheArgs& A, int format, int n, int smem, cudaStream_t st)
@@ -571,6 +798,7 @@ static void launch_append4(CacheArgs& A, bool vec, int n, int smem, cudaStream_t
 {
     A.queries_vec = n >= 4;
     A.team = pow2_up(A.dim / (2 * (n >= 4 ? 4 : 1)));
+    quotients(A);
     if (vec) launch_cache(append4_kernel<T, true>, A, A, smem, st);
     else launch_cache(append4_kernel<T, false>, A, A, smem, st);
 }
@@ -665,18 +893,19 @@ int gr_cache_append(void* keys, void* values, const gr_cache_layout* layout, con
     cudaStream_t st = (cudaStream_t)stream;
     gr::NvtxRange whole("gr_cache_append");
     if (four) {
-        const bool vec = kv.bits % (unsigned long long)(4 * e) == 0 && (interleaved || (rot / 2) % 4 == 0);
+        const bool vec = kv.bits % 16 == 0 && (interleaved || (rot / 2) % 8 == 0);
         const int n = fits(4, q.bits, 0) ? 4 : 1;
-        gr::deal(A, 2 * L.heads + (X.q_heads + 3) / 4);
-        const int smem = gr::kCacheWindow * A.half * (int)sizeof(float2);
+        A.four = 1;
+        gr::deal(A, 8 * L.heads + (X.q_heads + 3) / 4, 16);
+        const int smem = (A.window + 7) * gr::angle_step(A.half) * (int)sizeof(float2);
         if (X.dtype == GR_F32) gr::launch_append4<float>(A, vec, n, smem, st);
         else if (X.dtype == GR_BF16) gr::launch_append4<__nv_bfloat16>(A, vec, n, smem, st);
         else gr::launch_append4<__half>(A, vec, n, smem, st);
     } else {
         const unsigned long long own = kv.bits | q.bits;
         const int n = e == 2 && gr::type_size(L.format) == 2 && fits(8, own, c.bits) ? 8 : fits(4, own, c.bits) ? 4 : 1;
-        gr::deal(A, (2 * L.heads + X.q_heads + 3) / 4);
-        const int smem = A.window * A.half * (int)sizeof(float2);
+        gr::deal(A, (2 * L.heads + X.q_heads + 3) / 4, 8);
+        const int smem = A.window * gr::angle_step(A.half) * (int)sizeof(float2);
         if (X.dtype == GR_F32) gr::launch_append_to<float>(A, L.format, n, smem, st);
         else if (X.dtype == GR_BF16) gr::launch_append_to<__nv_bfloat16>(A, L.format, n, smem, st);
         else gr::launch_append_to<__half>(A, L.format, n, smem, st);
@@ -714,7 +943,8 @@ int gr_cache_read(const void* keys, const void* values, const gr_cache_layout* l
     cudaStream_t st = (cudaStream_t)stream;
     gr::NvtxRange whole("gr_cache_read");
     if (L.format == GR_Q4) {
-        gr::deal(A, 2 * L.heads);
+        A.four = 1;
+        gr::deal(A, L.heads, 16);
         const bool vec = out.bits % (unsigned long long)(8 * e) == 0;
         if (dtype == GR_F32) gr::launch_read4<float>(R, vec, st);
         else if (dtype == GR_BF16) gr::launch_read4<__nv_bfloat16>(R, vec, st);
@@ -724,7 +954,7 @@ int gr_cache_read(const void* keys, const void* values, const gr_cache_layout* l
         c.add(keys, ce, {L.block_stride, L.token_stride, L.head_stride}); c.add(values, ce, {L.block_stride, L.token_stride, L.head_stride});
         auto fits = [&](int n) { return out.bits % (unsigned long long)(n * e) == 0 && c.bits % (unsigned long long)(n * ce) == 0 && L.dim % n == 0; };
         const int n = e == 2 && ce == 2 && fits(8) ? 8 : fits(4) ? 4 : 1;
-        gr::deal(A, (2 * L.heads + 3) / 4);
+        gr::deal(A, (2 * L.heads + 3) / 4, 8);
         if (L.format == GR_F32) gr::launch_read_to<float>(R, dtype, n, st);
         else if (L.format == GR_BF16) gr::launch_read_to<__nv_bfloat16>(R, dtype, n, st);
         else gr::launch_read_to<__half>(R, dtype, n, st);

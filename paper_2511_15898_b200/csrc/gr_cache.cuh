@@ -47,10 +47,10 @@ inline bool apart(long long unit, const long long* step, const long long* size, 
     return true;
 }
 
-// Whether strides of what is read are numbers that `tokens` and `heads` of them can be counted off by.
+// Whether strides of what is read are ones (31 bits; that of a single token or head is not looked at).
 inline bool counted(long long token, long long head, int tokens, int heads)
 {
-    return token >= 0 && head >= 0 && token <= (1ll << 58) / std::max(1, tokens) && head <= (1ll << 58) / std::max(1, heads);
+    return (tokens <= 1 || (token >= 0 && token < (1ll << 31))) && (heads <= 1 || (head >= 0 && head < (1ll << 31)));
 }
 
 // First byte and the one behind the last of strided places.

@@ -3,11 +3,14 @@
 // Every function answers None where anything is not as it expects (another device than the current one, a list of different
 // layouts, a wrong type ...): the binding's own way then looks closer, and raises or makes the call.
 #include <Python.h>
+#include <math.h>
 #include <string.h>
 #include <vector>
 #include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
+#include <torch/csrc/Dtype.h>
 #include <torch/csrc/autograd/python_variable.h>
+#include <ATen/Functions.h>
 #include "gr.h"
 
 namespace {
@@ -200,8 +203,181 @@ PyObject* select_(PyObject*, PyObject* const* a, Py_ssize_t n)
     GR_CATCH
 }
 
+// ---------------------------------------------------------------- paged caches
+
+int type_code(at::ScalarType t) { return t == at::kFloat ? GR_F32 : t == at::kBFloat16 ? GR_BF16 : t == at::kHalf ? GR_F16 : -1; }
+
+// the layout of a cache (keys, values, block_size, heads, dim); its keys
+const at::Tensor* cache_of(PyObject* const* a, gr_cache_layout* L, void** values)
+{
+    const at::Tensor* k = tensor(a[0]);
+    if (!k || !k->is_cuda() || k->layout() != at::kStrided || k->dim() != 4 || k->numel() == 0) return nullptr;
+    const long block = PyLong_AsLong(a[2]), heads = PyLong_AsLong(a[3]), dim = PyLong_AsLong(a[4]);
+    if (PyErr_Occurred() || block < 1 || block >= (1l << 31) || heads < 1 || heads > GR_MAX_HEADS || dim < 1 || dim > GR_MAX_DIM || k->size(0) >= (1ll << 31)) return nullptr;
+    L->heads = (int)heads; L->dim = (int)dim; L->block_size = (int)block; L->num_blocks = (int)k->size(0);
+    L->token_stride = L->head_stride = 0;
+    *values = nullptr;
+    if (k->scalar_type() == at::kByte) {
+        if (a[1] != Py_None || block % 8 || dim % 32 || k->size(1) != heads || k->size(2) != block / 8 || k->size(3) != 9 * dim) return nullptr;
+        long long per = 1;
+        for (long d = 3; d >= 1; d--) { if (k->size(d) > 1 && k->stride(d) != per) return nullptr; per *= k->size(d); }
+        L->format = GR_Q4; L->block_stride = k->size(0) > 1 ? k->stride(0) : per;
+        return k;
+    }
+    const at::Tensor* v = tensor(a[1]);
+    L->format = type_code(k->scalar_type());
+    if (L->format < 0 || !v || v->device() != k->device() || v->scalar_type() != k->scalar_type() || v->sizes() != k->sizes() || v->strides() != k->strides()) return nullptr;
+    if (k->size(1) != block || k->size(2) != heads || k->size(3) != dim || (dim > 1 && k->stride(3) != 1)) return nullptr;
+    L->block_stride = k->stride(0); L->token_stride = k->stride(1); L->head_stride = k->stride(2);
+    *values = v->data_ptr();
+    return k;
+}
+// a [tokens, heads, dim] tensor of this type and device whose heads' elements lie next to one another
+const at::Tensor* rows_of(PyObject* o, at::ScalarType kind, c10::Device dev, long long tokens, long long heads, long long dim)
+{
+    const at::Tensor* t = tensor(o);
+    return t && t->is_cuda() && t->layout() == at::kStrided && t->device() == dev && t->scalar_type() == kind && t->dim() == 3 && t->size(0) == tokens
+           && t->size(1) == heads && t->size(2) == dim && (dim == 1 || t->stride(2) == 1) ? t : nullptr;
+}
+
+// append(function, keys, values, block_size, heads, dim, k, v, slots, positions, frequencies, interleaved, q, q_out) -> its answer or None
+PyObject* append(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    GR_OR_NONE(n == 14);
+    GR_TRY
+    auto* f = reinterpret_cast<decltype(&gr_cache_append)>(PyLong_AsVoidPtr(a[0]));
+    gr_cache_layout L;
+    void* values;
+    const at::Tensor *keys = cache_of(a + 1, &L, &values), *k = tensor(a[6]), *slots, *positions, *freq;
+    GR_OR_NONE(f && keys && k && k->dim() == 3 && type_code(k->scalar_type()) >= 0 && k->size(0) < (1ll << 31));
+    const c10::Device dev = keys->device();
+    const long long T = k->size(0);
+    const at::Tensor* v = rows_of(a[7], k->scalar_type(), dev, T, L.heads, L.dim);
+    GR_OR_NONE(v && rows_of(a[6], k->scalar_type(), dev, T, L.heads, L.dim));
+    GR_OR_NONE(is_plain(a[8], at::kLong, dev, false, &slots) && is_plain(a[9], at::kInt, dev, true, &positions) && is_plain(a[10], at::kDouble, dev, true, &freq));
+    GR_OR_NONE(slots->dim() == 1 && slots->size(0) == T && (!positions || (positions->dim() == 1 && positions->size(0) == T)));
+    GR_OR_NONE(!freq || (positions && freq->dim() == 1 && 2 * freq->size(0) <= L.dim));
+    gr_cache_tokens X = {};
+    X.k = k->data_ptr(); X.v = v->data_ptr(); X.dtype = type_code(k->scalar_type());
+    X.k_token = k->stride(0); X.k_head = k->stride(1); X.v_token = v->stride(0); X.v_head = v->stride(1);
+    if (a[12] != Py_None) {
+        const at::Tensor* q = tensor(a[12]);
+        GR_OR_NONE(q && q->dim() == 3 && q->size(1) <= GR_MAX_HEADS);
+        const at::Tensor* out = rows_of(a[13], k->scalar_type(), dev, T, q->size(1), L.dim);
+        GR_OR_NONE(out && rows_of(a[12], k->scalar_type(), dev, T, q->size(1), L.dim));
+        X.q = q->data_ptr(); X.q_out = out->data_ptr(); X.q_heads = (int)q->size(1);
+        X.q_token = q->stride(0); X.q_head = q->stride(1); X.out_token = out->stride(0); X.out_head = out->stride(1);
+    } else GR_OR_NONE(a[13] == Py_None);
+    const int interleaved = PyObject_IsTrue(a[11]);
+    void* stream;
+    GR_OR_NONE(interleaved >= 0 && here(dev, &stream));
+    return PyLong_FromLong(f(keys->data_ptr(), values, &L, &X, (int)T, address<long long>(slots), address<int>(positions), address<double>(freq),
+                             freq ? 2 * (int)freq->size(0) : 0, interleaved, stream));
+    GR_CATCH
+}
+
+// read(function, keys, values, block_size, heads, dim, slots, dtype, k, v) -> (k, v), its answer where that is not 0, or None.  Without k and v: new ones of
+// type dtype.
+PyObject* read(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    GR_OR_NONE(n == 10);
+    GR_TRY
+    auto* f = reinterpret_cast<decltype(&gr_cache_read)>(PyLong_AsVoidPtr(a[0]));
+    gr_cache_layout L;
+    void* values;
+    const at::Tensor *keys = cache_of(a + 1, &L, &values), *slots;
+    GR_OR_NONE(f && keys && is_plain(a[6], at::kLong, keys->device(), false, &slots) && slots->dim() == 1 && slots->size(0) < (1ll << 31));
+    const c10::Device dev = keys->device();
+    const long long T = slots->size(0);
+    void* stream;
+    GR_OR_NONE(here(dev, &stream));
+    at::Tensor k, v;
+    if (a[8] == Py_None) {
+        GR_OR_NONE(a[9] == Py_None && THPDtype_Check(a[7]));
+        const at::ScalarType kind = reinterpret_cast<THPDtype*>(a[7])->scalar_type;
+        GR_OR_NONE(type_code(kind) >= 0);
+        const auto as = at::TensorOptions().dtype(kind).device(dev);
+        k = at::empty({T, L.heads, L.dim}, as);
+        v = at::empty({T, L.heads, L.dim}, as);
+    } else {
+        const at::Tensor* out = tensor(a[8]);
+        GR_OR_NONE(out && type_code(out->scalar_type()) >= 0);
+        const at::Tensor *x = rows_of(a[8], out->scalar_type(), dev, T, L.heads, L.dim), *y = rows_of(a[9], out->scalar_type(), dev, T, L.heads, L.dim);
+        GR_OR_NONE(x && y);
+        k = *x; v = *y;
+    }
+    const int rc = f(keys->data_ptr(), values, &L, address<long long>(slots), (int)T, type_code(k.scalar_type()), k.data_ptr(), k.stride(0), k.stride(1),
+                     v.data_ptr(), v.stride(0), v.stride(1), stream);
+    if (rc != GR_OK) return PyLong_FromLong(rc);
+    PyObject *x = THPVariable_Wrap(k), *y = THPVariable_Wrap(v), *both = x && y ? PyTuple_Pack(2, x, y) : nullptr;
+    Py_XDECREF(x); Py_XDECREF(y);
+    return both;
+    GR_CATCH
+}
+
+// attend(function, q, keys, values, block_size, heads, dim, table, offsets, positions, scale, window, workspace, out, status) -> its answer or None.
+// (The last three are the binding's own, made for the shape.)
+PyObject* attend(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    GR_OR_NONE(n == 15);
+    GR_TRY
+    auto* f = reinterpret_cast<decltype(&gr_cache_attend)>(PyLong_AsVoidPtr(a[0]));
+    gr_cache_layout L;
+    void* values;
+    const at::Tensor *q = tensor(a[1]), *keys = cache_of(a + 2, &L, &values), *table, *offsets, *positions;
+    GR_OR_NONE(f && q && keys && L.format == GR_Q4 && q->dim() == 3 && (q->scalar_type() == at::kBFloat16 || q->scalar_type() == at::kHalf));
+    const c10::Device dev = keys->device();
+    const long long T = q->size(0), heads = q->size(1);
+    GR_OR_NONE(T < (1ll << 31) && heads <= GR_MAX_HEADS && rows_of(a[1], q->scalar_type(), dev, T, heads, L.dim));
+    GR_OR_NONE(is_plain(a[7], at::kInt, dev, false, &table) && is_plain(a[8], at::kInt, dev, false, &offsets) && is_plain(a[9], at::kInt, dev, false, &positions));
+    GR_OR_NONE(table->dim() == 2 && table->size(0) < (1ll << 31) - 1 && table->size(1) < (1ll << 31) && offsets->dim() == 1 && offsets->size(0) == table->size(0) + 1
+               && positions->dim() == 1 && positions->size(0) == T);
+    const at::Tensor *workspace = tensor(a[12]), *out = rows_of(a[13], q->scalar_type(), dev, T, heads, L.dim), *status = tensor(a[14]);
+    GR_OR_NONE(workspace && out && status && workspace->device() == dev && status->device() == dev && status->numel() == table->size(0));
+    const double scale = a[10] == Py_None ? pow((double)L.dim, -0.5) : PyFloat_AsDouble(a[10]);
+    const long window = PyLong_AsLong(a[11]);
+    GR_OR_NONE(!PyErr_Occurred() && window >= 0 && window < (1l << 31));
+    void* stream;
+    GR_OR_NONE(here(dev, &stream));
+    return PyLong_FromLong(f(q->data_ptr(), type_code(q->scalar_type()), (int)heads, q->stride(0), q->stride(1), keys->data_ptr(), &L, address<int>(table),
+                             (int)table->size(1), (int)table->size(0), address<int>(offsets), address<int>(positions), (int)T, (float)scale, (int)window,
+                             workspace->data_ptr(), out->data_ptr(), out->stride(0), out->stride(1), address<int>(status), stream));
+    GR_CATCH
+}
+
+// logprobs(function, logits, tokens, top, temperature, logprob, entropy, top_token, top_logprob, status) -> its answer or None.  (The last five are the
+// binding's own, made for the shape.)
+PyObject* logprobs(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    GR_OR_NONE(n == 10);
+    GR_TRY
+    auto* f = reinterpret_cast<decltype(&gr_token_logprobs)>(PyLong_AsVoidPtr(a[0]));
+    const at::Tensor *x = tensor(a[1]), *tokens, *own[5];
+    GR_OR_NONE(f && x && x->is_cuda() && x->dim() == 2 && x->layout() == at::kStrided && x->numel() > 0);
+    GR_OR_NONE(x->scalar_type() == at::kFloat || x->scalar_type() == at::kBFloat16);
+    const c10::Device dev = x->device();
+    const long long R = x->size(0), V = x->size(1), ld = R > 1 ? x->stride(0) : V;
+    GR_OR_NONE((V == 1 || x->stride(1) == 1) && ld >= V && R < (1ll << 31) && V < (1ll << 31));
+    GR_OR_NONE(is_plain(a[2], at::kInt, dev, true, &tokens) && (!tokens || ((tokens->dim() == 1 || tokens->dim() == 2) && tokens->size(0) == R)));
+    const long long given = !tokens ? 0 : tokens->dim() == 1 ? 1 : tokens->size(1);
+    const long top = PyLong_AsLong(a[3]);
+    const double temperature = PyFloat_AsDouble(a[4]);
+    GR_OR_NONE(!PyErr_Occurred() && top >= 0 && top <= GR_MAX_SELECT && given <= GR_MAX_GIVEN);
+    for (int i = 0; i < 5; i++) GR_OR_NONE((own[i] = tensor(a[5 + i])) && own[i]->device() == dev);
+    GR_OR_NONE(own[0]->numel() == R * given && own[1]->numel() == R && own[2]->numel() == R * top && own[3]->numel() == R * top && own[4]->numel() == R);
+    GR_OR_NONE(!tokens || top == 0 || tokens->data_ptr() != own[2]->data_ptr());
+    void* stream;
+    GR_OR_NONE(here(dev, &stream));
+    return PyLong_FromLong(f(x->data_ptr(), x->scalar_type() == at::kFloat ? GR_F32 : GR_BF16, (int)V, ld, (int)R, (float)temperature, address<int>(tokens),
+                             (int)given, (int)top, address<float>(own[0]), address<float>(own[1]), address<int>(own[2]), address<float>(own[3]),
+                             address<int>(own[4]), stream));
+    GR_CATCH
+}
+
 PyMethodDef methods[] = {{"reorder", (PyCFunction)(void (*)(void))reorder, METH_FASTCALL, nullptr}, {"copy", (PyCFunction)(void (*)(void))copy, METH_FASTCALL, nullptr},
                          {"plan", (PyCFunction)(void (*)(void))plan, METH_FASTCALL, nullptr}, {"select", (PyCFunction)(void (*)(void))select_, METH_FASTCALL, nullptr},
+                         {"append", (PyCFunction)(void (*)(void))append, METH_FASTCALL, nullptr}, {"read", (PyCFunction)(void (*)(void))read, METH_FASTCALL, nullptr},
+                         {"attend", (PyCFunction)(void (*)(void))attend, METH_FASTCALL, nullptr}, {"logprobs", (PyCFunction)(void (*)(void))logprobs, METH_FASTCALL, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_tensors", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
