@@ -10,11 +10,11 @@
 // tokens to a key head wastes nothing.  Rounded to fewer bits: p (11 bits) and p s (11 bits) before the second product; both are relative to
 // themselves, 2^-12 each, against an output of 8 or 11 bits.  x, m, sums of p and both products are fp32.
 //
-// Work.  A unit is 64 tokens of a (row, head, tile of query rows); the units of the call in that order are cut into equal shares, one to a CTA,
-// however ragged the rows are.  A warp brings a unit's octets into a ring in shared memory (cp.async.bulk, one per octet), four warps
-// take 16 tokens each (or, where there are many query rows, the same 64 tokens for 16 query rows each).  What a CTA does not finish it
-// leaves as (m, sum, product) in the workspace; a second kernel joins the pieces in the order of the tokens, so results do not depend
-// on which CTA was first.
+// Work.  A unit is 128 tokens of a (row, head, tile of query rows), or 64; the units of the call in that order are cut into equal shares, one to
+// a CTA of four warps, however ragged the rows are.  Up to 16 query rows: a warp takes 32 of a unit's tokens for all of them and brings them itself, the next ones
+// while it works on these (cp.async.bulk, an octet each, into a ring of its own).  More: all warps take the unit's 64 tokens, each for 16
+// query rows, from one ring that the first one fills.  What a CTA does not finish it leaves as (m, sum, product) in the workspace;
+// a second kernel joins the pieces in the order of the tokens, so results do not depend on which CTA was first.
 #include <math.h>
 #include <algorithm>
 #include "gr_host.h"
@@ -22,9 +22,9 @@
 
 namespace gr {
 
-constexpr int kTile = 64;                      // tokens of a unit
-constexpr int kEaters = 4;                     // warps that compute; one more brings the octets
-constexpr int kAttendThreads = 32 * (kEaters + 1);
+constexpr int kEaters = 4;                     // warps of a CTA
+constexpr int kAttendThreads = 32 * kEaters;
+constexpr int kBite = 32;                      // tokens that a warp takes at a time
 constexpr int kJoinThreads = 256;
 constexpr unsigned long long kWaitNs = 2000000000ull;      // longest wait for a copy or a free place in the ring
 
@@ -34,6 +34,7 @@ struct AttendArgs {
     const char* cache; long long block_stride, head_bytes;
     const int* table; const int* offsets; const int* positions; int* status;
     int dtype, q_vec, out_vec, tokens, heads, group, octets, num_blocks, width, rows, window, most;     // octets: of a block; most: tokens that a table's row has room for
+    unsigned by_octets; int shift;             // quotients by octets
     float scale;                               // with log2(e)
     char* ws; int ctas;
 };
@@ -44,16 +45,20 @@ static_assert(sizeof(AttendNote) == 32, "workspace layout");
 
 template <int J, int NT, bool kRows>
 struct Shape {
-    static constexpr int D = 32 * J, kTileRows = 8 * NT * (kRows ? kEaters : 1), kOctet = octet_bytes(D), kUnit = kTile / 8 * kOctet;
+    static constexpr int D = 32 * J, kTileRows = 8 * NT * (kRows ? kEaters : 1), kOctet = octet_bytes(D);
+    static constexpr int kTile = kRows ? 64 : kBite * kEaters;             // tokens of a unit
+    static constexpr int kStage = (kRows ? kTile : kBite) / 8 * kOctet;    // bytes of a place in a ring
+    static constexpr int kRings = kRows ? 1 : kEaters;
     static constexpr int kStep = D + 4;        // floats from one row of the joined results to the next: threads of a quarter warp meet all banks
-    static constexpr int kJoin = kRows ? 0 : kEaters * 8 * NT * kStep * 4;
-    static constexpr int kCtas = NT == 1 ? (J <= 2 ? 4 : J <= 4 ? 3 : 2) : (J <= 2 ? 3 : 2);      // resident per SM, by registers
-    static constexpr int kRoom = 227 * 1024 / kCtas - 2048 - kJoin;
-    static constexpr int kStages = kRoom / kUnit < 8 ? kRoom / kUnit : 8;
-    static constexpr int kSmem = kStages * kUnit + kJoin;
+    static constexpr int kJoin = kRows ? 0 : 2 * 8 * NT * kStep * 4;
+    // resident CTAs per SM, by registers: 128, 168 or 255 a thread
+    static constexpr int kCtas = NT == 1 ? (J <= 4 ? 4 : J <= 6 ? 3 : 2) : (J <= 1 ? 4 : J <= 3 ? 3 : 2);
+    static constexpr int kRoom = 227 * 1024 / kCtas - 2560 - kJoin;
+    static constexpr int kStages = kRoom / (kRings * kStage) < 4 ? kRoom / (kRings * kStage) : 4;
+    static constexpr int kSmem = kStages * kRings * kStage + kJoin;
     static_assert(kStages >= 2, "a ring");
 };
-constexpr int kMaxStages = 8;
+constexpr int kMaxStages = 4;
 __host__ __device__ inline size_t piece_floats(int tile_rows, int dim) { return (size_t)tile_rows * (dim + 2); }
 
 // ---------------------------------------------------------------- instructions
@@ -86,11 +91,14 @@ __device__ __forceinline__ void bulk_load(unsigned to, const void* from, unsigne
 {
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(to), "l"(from), "r"(bytes), "r"(bar) : "memory");
 }
-__device__ __forceinline__ void eaters_sync() { asm volatile("bar.sync 1, %0;" ::"n"(32 * kEaters) : "memory"); }
+__device__ __forceinline__ void mma(float (&d)[4], unsigned a0, unsigned a1, unsigned a2, unsigned a3, unsigned b0, unsigned b1, float c0, float c1, float c2, float c3)
+{
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %11, %12, %13};"
+        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(c0), "f"(c1), "f"(c2), "f"(c3));
+}
 __device__ __forceinline__ void mma(float (&d)[4], unsigned a0, unsigned a1, unsigned a2, unsigned a3, unsigned b0, unsigned b1)
 {
-    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+    mma(d, a0, a1, a2, a3, b0, b1, d[0], d[1], d[2], d[3]);
 }
 __device__ __forceinline__ unsigned transposed(unsigned v)
 {
@@ -117,12 +125,24 @@ __device__ __forceinline__ void load_words(unsigned (&w)[J], const char* p)     
     }
 }
 
+template <int J>
+__device__ __forceinline__ void load_halves(unsigned short (&w)[J], const char* p)
+{
+    constexpr int W = J % 4 == 0 ? 4 : J % 2 == 0 ? 2 : 1;
+#pragma unroll
+    for (int i = 0; i < J; i += W) {
+        const Pack<unsigned short, W> v = *reinterpret_cast<const Pack<unsigned short, W>*>(p + 2 * i);
+#pragma unroll
+        for (int z = 0; z < W; z++) w[i + z] = v.x[z];
+    }
+}
+
 // ---------------------------------------------------------------- the order of the work
 
-// A place in the call's units: an item is (row, head, tile of query rows), of `count` units of which `at` are behind.
+// A place in the call's units: an item is (row, head, tile of query rows), of `count` units of which `at` are behind.  (kTile: tokens of a unit.)
 struct Walk {
     int r, token, n, p0;                       // row; its first query token, their number, the first one's position
-    int h, y, lo, hi, first, count, at;        // first: the item's first unit of 64 tokens; [lo, hi): tokens that any of its query rows sees
+    int h, y, lo, hi, first, count, at;        // first: the item's first unit of the row's; [lo, hi): tokens that any of its query rows sees
 };
 __device__ __forceinline__ void walk_row(Walk& w, const AttendArgs& A)
 {
@@ -130,7 +150,7 @@ __device__ __forceinline__ void walk_row(Walk& w, const AttendArgs& A)
     w.n = min(max(A.offsets[w.r + 1], w.token), A.tokens) - w.token;
     w.p0 = w.n > 0 ? A.positions[w.token] : -1;
 }
-template <int kTileRows>
+template <int kTileRows, int kTile>
 __device__ __forceinline__ void walk_item(Walk& w, const AttendArgs& A)
 {
     const int first = w.y * kTileRows / A.group, last = (min(w.n * A.group, (w.y + 1) * kTileRows) - 1) / A.group;
@@ -141,14 +161,14 @@ __device__ __forceinline__ void walk_item(Walk& w, const AttendArgs& A)
     w.count = w.hi > w.lo ? (w.hi + kTile - 1) / kTile - w.first : 1;        // (a row that sees nothing: a unit of nothing, which writes its zeros)
 }
 // units of a head of row w.r
-template <int kTileRows>
+template <int kTileRows, int kTile>
 __device__ __forceinline__ int row_units(Walk& w, const AttendArgs& A)
 {
     int sum = 0;
-    for (w.y = 0; w.y * kTileRows < w.n * A.group; w.y++) { walk_item<kTileRows>(w, A); sum += w.count; }
+    for (w.y = 0; w.y * kTileRows < w.n * A.group; w.y++) { walk_item<kTileRows, kTile>(w, A); sum += w.count; }
     return sum;
 }
-template <int kTileRows>
+template <int kTileRows, int kTile>
 __device__ __forceinline__ void walk_next(Walk& w, const AttendArgs& A)
 {
     w.at = 0;
@@ -159,7 +179,7 @@ __device__ __forceinline__ void walk_next(Walk& w, const AttendArgs& A)
             do { if (++w.r >= A.rows) return; walk_row(w, A); } while (w.n == 0);
         }
     }
-    walk_item<kTileRows>(w, A);
+    walk_item<kTileRows, kTile>(w, A);
 }
 
 // ---------------------------------------------------------------- a warp's share
@@ -168,8 +188,8 @@ template <int J, int NT>
 struct State {
     unsigned q[NT][J][4];                      // the queries as operands, scaled
     float down[NT][J][2];                      // -8 2^-24 times the queries' sums
-    float f[NT][2];                            // from products to x
-    float m[NT][2], ref[NT][2], l[NT][2];      // ref: m, or 0 where that is -infinity
+    float f[NT][2];                            // from products to x, positive
+    float m[NT][2], ref[NT][2], l[NT][2];      // m: the largest product; ref: its x, or 0 where there is none
     float o[NT][2 * J][4], off[NT][4];
 };
 
@@ -207,8 +227,8 @@ __device__ __forceinline__ void load_queries(State<J, NT>& s, const AttendArgs& 
         most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 2));
         int up = 140 - (int)(__float_as_uint(most) >> 23) + 127;             // exponent field of 2^(13 - exponent of most)
         up = most > 0.f && most < INFINITY ? min(max(up, 1), 254) : 127;
-        const float by = __uint_as_float((unsigned)up << 23);
-        const float back = A.scale * 16777216.f / by;
+        const float by = copysignf(__uint_as_float((unsigned)up << 23), A.scale);        // (a negative scale turns the queries around)
+        const float back = fmaxf(A.scale * 16777216.f / by, 1e-30f);
         s.f[x][0] = __shfl_sync(0xffffffffu, back, 8 * t); s.f[x][1] = __shfl_sync(0xffffffffu, back, 8 * t + 4);
 #pragma unroll
         for (int j = 0; j < J; j++) {
@@ -236,65 +256,75 @@ __device__ __forceinline__ void load_queries(State<J, NT>& s, const AttendArgs& 
     }
 }
 
-// 16 tokens from `token` on, two octets at `at`.  kAll: every query row sees them all.  Else `have` says which of the two octets
+// 32 tokens from `token` on, four octets at `at`.  kAll: every query row sees them all.  Else `have` says which of the octets
 // are there, and each query row's own range which of the tokens it sees; what it does not see stays out whatever is held there.
 template <int J, int NT, bool kAll>
 __device__ __forceinline__ void eat(State<J, NT>& s, const char* at, int lane, const AttendArgs& A, const Walk& w, int row, int token, unsigned have)
 {
     constexpr int D = 32 * J, kOctet = octet_bytes(D);
     const int g = lane >> 2, t = lane & 3;
-    float x[NT][4];
-    {
-        unsigned k0[J], k1[J];
-        load_words<J>(k0, at + 4 * J * lane);
-        load_words<J>(k1, at + kOctet + 4 * J * lane);
-        const __half* s0 = (const __half*)(at + octet_kscale(D)) + g * J;
-        const __half* s1 = (const __half*)(at + kOctet + octet_kscale(D)) + g * J;
+    float x[NT][2][4];
 #pragma unroll
-        for (int n = 0; n < NT; n++) { x[n][0] = x[n][1] = x[n][2] = x[n][3] = 0.f; }
+    for (int b = 0; b < 2; b++) {
+        const char* from = at + 2 * b * kOctet;
+        unsigned k0[J], k1[J];
+        unsigned short s0[J], s1[J];
+        load_words<J>(k0, from + 4 * J * lane);
+        load_words<J>(k1, from + kOctet + 4 * J * lane);
+        load_halves<J>(s0, from + octet_kscale(D) + 2 * J * g);
+        load_halves<J>(s1, from + kOctet + octet_kscale(D) + 2 * J * g);
 #pragma unroll
         for (int j = 0; j < J; j++) {
-            const float a = __half2float(s0[j]), b = __half2float(s1[j]);
+            const float c = __half2float(__ushort_as_half(s0[j])), e = __half2float(__ushort_as_half(s1[j]));
             const unsigned u0 = k0[j] >> 8, u1 = k1[j] >> 8;
 #pragma unroll
             for (int n = 0; n < NT; n++) {
-                float d[4] = {s.down[n][j][0], s.down[n][j][1], s.down[n][j][0], s.down[n][j][1]};
-                mma(d, k0[j] & 0x000f000fu, k1[j] & 0x000f000fu, k0[j] & 0x00f000f0u, k1[j] & 0x00f000f0u, s.q[n][j][0], s.q[n][j][1]);
+                float d[4];
+                mma(d, k0[j] & 0x000f000fu, k1[j] & 0x000f000fu, k0[j] & 0x00f000f0u, k1[j] & 0x00f000f0u, s.q[n][j][0], s.q[n][j][1],
+                    s.down[n][j][0], s.down[n][j][1], s.down[n][j][0], s.down[n][j][1]);
                 mma(d, u0 & 0x000f000fu, u1 & 0x000f000fu, u0 & 0x00f000f0u, u1 & 0x00f000f0u, s.q[n][j][2], s.q[n][j][3]);
-                x[n][0] = fmaf(a, d[0], x[n][0]); x[n][1] = fmaf(a, d[1], x[n][1]);
-                x[n][2] = fmaf(b, d[2], x[n][2]); x[n][3] = fmaf(b, d[3], x[n][3]);
+                if (j == 0) { x[n][b][0] = c * d[0]; x[n][b][1] = c * d[1]; x[n][b][2] = e * d[2]; x[n][b][3] = e * d[3]; }
+                else {
+                    x[n][b][0] = fmaf(c, d[0], x[n][b][0]); x[n][b][1] = fmaf(c, d[1], x[n][b][1]);
+                    x[n][b][2] = fmaf(e, d[2], x[n][b][2]); x[n][b][3] = fmaf(e, d[3], x[n][b][3]);
+                }
             }
         }
     }
     bool more = false;
 #pragma unroll
     for (int n = 0; n < NT; n++) {
+        if (!kAll) {
 #pragma unroll
-        for (int z = 0; z < 4; z++) {
-            x[n][z] *= s.f[n][z & 1];
-            if (!kAll) {
-                const int i = row + 8 * n + 2 * t + (z & 1), tok = token + g + 8 * (z >> 1);
+            for (int z = 0; z < 2; z++) {
+                const int i = row + 8 * n + 2 * t + z;
                 const long long p = (long long)w.p0 + i / A.group;
-                const bool sees = (have >> (z >> 1) & 1) && i < w.n * A.group && w.p0 >= 0 && tok <= p && tok < A.most && (A.window <= 0 || tok > p - A.window);
-                if (!sees) x[n][z] = -INFINITY;
+#pragma unroll
+                for (int y = 0; y < 4; y++) {
+                    const int tok = token + g + 8 * y;
+                    const bool sees = (have >> y & 1) && i < w.n * A.group && w.p0 >= 0 && tok <= p && tok < A.most && (A.window <= 0 || tok > p - A.window);
+                    if (!sees) x[n][y >> 1][(y & 1) * 2 + z] = -INFINITY;
+                }
             }
         }
-        more |= fmaxf(x[n][0], x[n][2]) > s.m[n][0] || fmaxf(x[n][1], x[n][3]) > s.m[n][1];
+        more |= fmaxf(fmaxf(x[n][0][0], x[n][0][2]), fmaxf(x[n][1][0], x[n][1][2])) > s.m[n][0]
+                || fmaxf(fmaxf(x[n][0][1], x[n][0][3]), fmaxf(x[n][1][1], x[n][1][3])) > s.m[n][1];
     }
     if (__any_sync(0xffffffffu, more)) {
-        // the largest x has grown: what has been added up moves to the new one
+        // the largest product has grown: what has been added up moves to the new one
 #pragma unroll
         for (int n = 0; n < NT; n++) {
             float by[2];
 #pragma unroll
             for (int z = 0; z < 2; z++) {
-                float m = fmaxf(x[n][z], x[n][z + 2]);
+                float m = fmaxf(fmaxf(x[n][0][z], x[n][0][z + 2]), fmaxf(x[n][1][z], x[n][1][z + 2]));
 #pragma unroll
                 for (int o = 4; o < 32; o *= 2) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
                 m = fmaxf(m, s.m[n][z]);
-                by[z] = s.m[n][z] == -INFINITY ? 1.f : exp2_of(s.m[n][z] - m);       // (nothing has been added up)
+                const float ref = m == -INFINITY ? 0.f : m * s.f[n][z];
+                by[z] = s.m[n][z] == -INFINITY ? 1.f : exp2_of(s.ref[n][z] - ref);       // (nothing has been added up)
                 s.m[n][z] = m;
-                s.ref[n][z] = m == -INFINITY ? 0.f : m;
+                s.ref[n][z] = ref;
                 s.l[n][z] *= by[z];
             }
 #pragma unroll
@@ -305,56 +335,80 @@ __device__ __forceinline__ void eat(State<J, NT>& s, const char* at, int lane, c
             }
         }
     }
-    unsigned p0[NT], p1[NT];
+    unsigned p[NT][2][2];
 #pragma unroll
     for (int n = 0; n < NT; n++) {
-        float p[4];
 #pragma unroll
-        for (int z = 0; z < 4; z++) p[z] = exp2_of(x[n][z] - s.ref[n][z & 1]);
-        s.l[n][0] += p[0] + p[2];
-        s.l[n][1] += p[1] + p[3];
-        p0[n] = transposed(pack_h2(p[0], p[1]));
-        p1[n] = transposed(pack_h2(p[2], p[3]));
-    }
-    const char* v = at + octet_vcode(D);
-    unsigned v0[J], v1[J], z0[J], z1[J];
-    load_words<J>(v0, v + 4 * J * lane);
-    load_words<J>(v1, v + kOctet + 4 * J * lane);
-    const char* sc = at + octet_vscale(D);
-    load_words<J>(z0, sc + 4 * J * t);
-    load_words<J>(z1, sc + kOctet + 4 * J * t);
-    if (kAll) {
-        // row j of the operand: group j's scales
-        const unsigned a0 = g < J ? *(const unsigned*)(sc + 4 * (J * t + g)) : 0u, a2 = g < J ? *(const unsigned*)(sc + kOctet + 4 * (J * t + g)) : 0u;
+        for (int b = 0; b < 2; b++) {
+            float e[4];
 #pragma unroll
-        for (int n = 0; n < NT; n++) mma(s.off[n], a0, 0u, a2, 0u, p0[n], p1[n]);
-    }
-#pragma unroll
-    for (int j = 0; j < J; j++) {
-        const unsigned u0 = v0[j] >> 8, u1 = v1[j] >> 8;
-#pragma unroll
-        for (int n = 0; n < NT; n++) {
-            unsigned b0 = mul_h2(p0[n], z0[j]), b1 = mul_h2(p1[n], z1[j]);
-            if (!kAll) {
-                // (0 stays 0 whatever the scale is)
-                b0 &= __hneu2_mask(*reinterpret_cast<const __half2*>(&p0[n]), __half2half2(__ushort_as_half(0)));
-                b1 &= __hneu2_mask(*reinterpret_cast<const __half2*>(&p1[n]), __half2half2(__ushort_as_half(0)));
-                const unsigned one = g == j ? 0x3c003c00u : 0u;
-                mma(s.off[n], one, 0u, one, 0u, b0, b1);
+            for (int z = 0; z < 4; z++) {
+                e[z] = exp2_of(fmaf(x[n][b][z], s.f[n][z & 1], -s.ref[n][z & 1]));
+                s.l[n][z & 1] += e[z];
             }
-            mma(s.o[n][2 * j], v0[j] & 0x000f000fu, v0[j] & 0x00f000f0u, v1[j] & 0x000f000fu, v1[j] & 0x00f000f0u, b0, b1);
-            mma(s.o[n][2 * j + 1], u0 & 0x000f000fu, u0 & 0x00f000f0u, u1 & 0x000f000fu, u1 & 0x00f000f0u, b0, b1);
+            p[n][b][0] = transposed(pack_h2(e[0], e[1]));
+            p[n][b][1] = transposed(pack_h2(e[2], e[3]));
+        }
+    }
+#pragma unroll
+    for (int b = 0; b < 2; b++) {
+        const char* v = at + 2 * b * kOctet + octet_vcode(D);
+        const char* sc = at + 2 * b * kOctet + octet_vscale(D);
+        unsigned v0[J], v1[J], z0[J], z1[J];
+        load_words<J>(v0, v + 4 * J * lane);
+        load_words<J>(v1, v + kOctet + 4 * J * lane);
+        load_words<J>(z0, sc + 4 * J * t);
+        load_words<J>(z1, sc + kOctet + 4 * J * t);
+        if (kAll) {
+            // row j of the operand: group j's scales
+            const unsigned a0 = g < J ? *(const unsigned*)(sc + 4 * (J * t + g)) : 0u, a2 = g < J ? *(const unsigned*)(sc + kOctet + 4 * (J * t + g)) : 0u;
+#pragma unroll
+            for (int n = 0; n < NT; n++) mma(s.off[n], a0, 0u, a2, 0u, p[n][b][0], p[n][b][1]);
+        }
+#pragma unroll
+        for (int j = 0; j < J; j++) {
+            const unsigned u0 = v0[j] >> 8, u1 = v1[j] >> 8;
+#pragma unroll
+            for (int n = 0; n < NT; n++) {
+                unsigned b0 = mul_h2(p[n][b][0], z0[j]), b1 = mul_h2(p[n][b][1], z1[j]);
+                if (!kAll) {
+                    // (0 stays 0 whatever the scale is)
+                    b0 &= __hneu2_mask(*reinterpret_cast<const __half2*>(&p[n][b][0]), __half2half2(__ushort_as_half(0)));
+                    b1 &= __hneu2_mask(*reinterpret_cast<const __half2*>(&p[n][b][1]), __half2half2(__ushort_as_half(0)));
+                    const unsigned one = g == j ? 0x3c003c00u : 0u;
+                    mma(s.off[n], one, 0u, one, 0u, b0, b1);
+                }
+                mma(s.o[n][2 * j], v0[j] & 0x000f000fu, v0[j] & 0x00f000f0u, v1[j] & 0x000f000fu, v1[j] & 0x00f000f0u, b0, b1);
+                mma(s.o[n][2 * j + 1], u0 & 0x000f000fu, u0 & 0x00f000f0u, u1 & 0x000f000fu, u1 & 0x00f000f0u, b0, b1);
+            }
         }
     }
 }
 
-// dims 32 j + 4 g .. + 3 of query row 2 t + z of tile x, before the division by the sum
+// The products become results, before the division by the sum: o[x][2 j][z], o[x][2 j][z + 2], o[x][2 j + 1][z], o[x][2 j + 1][z + 2] the dims
+// 32 j + 4 g .. + 3 of query row 2 t + z of tile x; sums of p over all lanes.
 template <int J, int NT>
-__device__ __forceinline__ void result(const State<J, NT>& s, int x, int j, int z, int lane, float (&v)[4])
+__device__ __forceinline__ void results(State<J, NT>& s, int lane)
 {
-    const float down = -8.f * __shfl_sync(0xffffffffu, s.off[x][z], 4 * j + (lane & 3));
-    v[0] = fmaf(s.o[x][2 * j][z], 16777216.f, down); v[1] = fmaf(s.o[x][2 * j][z + 2], 1048576.f, down);
-    v[2] = fmaf(s.o[x][2 * j + 1][z], 16777216.f, down); v[3] = fmaf(s.o[x][2 * j + 1][z + 2], 1048576.f, down);
+#pragma unroll
+    for (int x = 0; x < NT; x++)
+#pragma unroll
+        for (int z = 0; z < 2; z++) {
+#pragma unroll
+            for (int o = 4; o < 32; o *= 2) s.l[x][z] += __shfl_xor_sync(0xffffffffu, s.l[x][z], o);
+#pragma unroll
+            for (int j = 0; j < J; j++) {
+                const float down = -8.f * __shfl_sync(0xffffffffu, s.off[x][z], 4 * j + (lane & 3));
+                s.o[x][2 * j][z] = fmaf(s.o[x][2 * j][z], 16777216.f, down); s.o[x][2 * j][z + 2] = fmaf(s.o[x][2 * j][z + 2], 1048576.f, down);
+                s.o[x][2 * j + 1][z] = fmaf(s.o[x][2 * j + 1][z], 16777216.f, down); s.o[x][2 * j + 1][z + 2] = fmaf(s.o[x][2 * j + 1][z + 2], 1048576.f, down);
+            }
+        }
+}
+template <int J, int NT>
+__device__ __forceinline__ void times(State<J, NT>& s, int x, int z, float by)
+{
+#pragma unroll
+    for (int j = 0; j < 2 * J; j++) { s.o[x][j][z] *= by; s.o[x][j][z + 2] *= by; }
 }
 
 __device__ __forceinline__ void store_out(const AttendArgs& A, long long at, const float (&v)[4])
@@ -380,22 +434,70 @@ __device__ __forceinline__ long long out_at(const AttendArgs& A, int token, int 
 
 // ---------------------------------------------------------------- first kernel
 
+// Brings octets into a ring, ahead of what is eaten: a warp's place in the units, and the block ids of the next ones.
+template <int J, int NT, bool kRows>
+struct Feeder {
+    using S = Shape<J, NT, kRows>;
+    static constexpr int kOctets = S::kStage / S::kOctet;
+    const char* head;                          // the cache from the item's head on
+    long long row;                             // the table's row
+    int token, hi, lo, left, id, in;           // token: of this lane's octet in the next unit; left: units of the item; id, in: its block, and place there
+
+    __device__ __forceinline__ void begin(const AttendArgs& A, const Walk& w, long long units, int skip, int lane)
+    {
+        head = A.cache + (long long)w.h * A.head_bytes;
+        row = (long long)w.r * A.width;
+        token = (w.first + w.at) * S::kTile + skip + 8 * lane;
+        hi = w.hi; lo = w.lo;
+        left = (int)min((long long)(w.count - w.at), units);
+        look(A, lane);
+    }
+    __device__ __forceinline__ void look(const AttendArgs& A, int lane)
+    {
+        id = -1;
+        if (lane < kOctets && token < hi && token + 8 > lo) {
+            // (blocks of a multiple of eight tokens; the quotient by a product with the reciprocal, rounded up)
+            const unsigned octet = (unsigned)token >> 3, block = A.octets == 1 ? octet : __umulhi(octet, A.by_octets) >> A.shift;
+            in = (int)(octet - block * (unsigned)A.octets);
+            if ((int)block < A.width) id = A.table[row + block];
+        }
+    }
+    // into place `place` of the ring; `have`: which octets it will hold
+    __device__ __forceinline__ void bring(const AttendArgs& A, char* place, unsigned long long* full, unsigned* have, int lane)
+    {
+        const bool want = id >= 0 && id < A.num_blocks;
+        const unsigned mask = __ballot_sync(0xffffffffu, want);
+        const unsigned bar = smem_addr(full);
+        if (lane == 0) {
+            *have = mask;
+            bar_expect(bar, __popc(mask) * S::kOctet);
+        }
+        __syncwarp();
+        if (want) bulk_load(smem_addr(place) + lane * S::kOctet, head + id * A.block_stride + (long long)in * S::kOctet, S::kOctet, bar);
+        token += S::kTile;
+        left--;
+    }
+};
+
 template <int J, int NT, bool kRows>
 __global__ void __launch_bounds__(kAttendThreads, Shape<J, NT, kRows>::kCtas)
 attend_kernel(const __grid_constant__ AttendArgs A)
 {
     using S = Shape<J, NT, kRows>;
-    constexpr int D = S::D, kTileRows = S::kTileRows, kStages = S::kStages, kOctet = S::kOctet;
-    extern __shared__ __align__(128) char ring[];
-    __shared__ __align__(8) unsigned long long s_full[kMaxStages], s_free[kMaxStages];
-    __shared__ unsigned s_have[kMaxStages];
+    constexpr int D = S::D, kTileRows = S::kTileRows, kStages = S::kStages, kTile = S::kTile;
+    extern __shared__ __align__(128) char rings[];
+    __shared__ __align__(8) unsigned long long s_full[S::kRings][kMaxStages], s_free[kMaxStages];
+    __shared__ unsigned s_have[S::kRings][kMaxStages];
     __shared__ float s_m[kEaters][8 * NT], s_l[kEaters][8 * NT];
-    __shared__ long long s_scan[kEaters + 1], s_from, s_to, s_total, s_ctas;
-    __shared__ Walk s_walk;
+    __shared__ long long s_scan[kEaters], s_from, s_to, s_total, s_ctas;
+    __shared__ Walk s_eat[kEaters], s_feed[kEaters];       // each warp's own
     __shared__ int s_failed;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     if (tid == 0) {
-        for (int i = 0; i < kStages; i++) { bar_init(smem_addr(&s_full[i]), 1); bar_init(smem_addr(&s_free[i]), kEaters); }
+        for (int i = 0; i < kStages; i++) {
+            for (int r = 0; r < S::kRings; r++) bar_init(smem_addr(&s_full[r][i]), 1);
+            bar_init(smem_addr(&s_free[i]), kEaters);
+        }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         s_failed = 0;
     }
@@ -408,7 +510,7 @@ attend_kernel(const __grid_constant__ AttendArgs A)
         for (int r = tid * per; r < min((tid + 1) * per, A.rows); r++) {
             w.r = r;
             walk_row(w, A);
-            mine += (long long)row_units<kTileRows>(w, A) * A.heads;
+            mine += (long long)row_units<kTileRows, kTile>(w, A) * A.heads;
         }
         long long upto = mine;
 #pragma unroll
@@ -417,7 +519,7 @@ attend_kernel(const __grid_constant__ AttendArgs A)
         __syncthreads();
         long long total = 0;
 #pragma unroll
-        for (int i = 0; i <= kEaters; i++) { if (i < warp) upto += s_scan[i]; total += s_scan[i]; }
+        for (int i = 0; i < kEaters; i++) { if (i < warp) upto += s_scan[i]; total += s_scan[i]; }
         const long long ctas = min((long long)A.ctas, total);
         const long long from = ctas > 0 && blockIdx.x < ctas ? total * blockIdx.x / ctas : 0, to = ctas > 0 && blockIdx.x < ctas ? total * (blockIdx.x + 1) / ctas : 0;
         if (tid == 0) { s_from = from; s_to = to; s_total = total; s_ctas = ctas; }
@@ -427,195 +529,199 @@ attend_kernel(const __grid_constant__ AttendArgs A)
             for (int r = tid * per;; r++) {
                 w.r = r;
                 walk_row(w, A);
-                const int units = row_units<kTileRows>(w, A);
+                const int units = row_units<kTileRows, kTile>(w, A);
                 if (left >= (long long)units * A.heads) { left -= (long long)units * A.heads; continue; }
                 w.h = (int)(left / units);
                 left -= (long long)w.h * units;
                 for (w.y = 0;; w.y++) {
-                    walk_item<kTileRows>(w, A);
+                    walk_item<kTileRows, kTile>(w, A);
                     if (left < w.count) break;
                     left -= w.count;
                 }
                 w.at = (int)left;
                 break;
             }
-            s_walk = w;
+#pragma unroll
+            for (int i = 0; i < kEaters; i++) { s_eat[i] = w; s_feed[i] = w; }
         }
     }
     __syncthreads();
-    const long long from = s_from, to = s_to;
+    const long long from = s_from;
+    const int total = (int)(s_to - from);      // (a share of 2^31 units would take hours)
     AttendNote* note = reinterpret_cast<AttendNote*>(A.ws) + blockIdx.x;
-    if (from >= to) {
+    if (total <= 0) {
         if (tid == 0) *note = AttendNote{0, 0, 0, 0, 0, 0, 0, 0};
         return;
     }
-    Walk w = s_walk;
-    bool ok = true;                            // (false: a wait ran out; from there on nothing is waited for, nothing is brought, and the call says so)
+    bool ok = true;                            // (false: a wait ran out; from there on nothing is waited for or brought, and the call says so)
+    const bool feeds = !kRows || warp == 0;
+    char* ring = rings + (kRows ? 0 : warp * kStages * S::kStage);
+    unsigned long long* full = s_full[kRows ? 0 : warp];
+    unsigned* held = s_have[kRows ? 0 : warp];
+    Feeder<J, NT, kRows> feeder;
+    int fed = 0;
+    auto feed = [&]() {
+        feeder.bring(A, ring + fed % kStages * S::kStage, full + fed % kStages, held + fed % kStages, lane);
+        fed++;
+        if (fed == total) return;
+        if (feeder.left == 0) {
+            Walk w = s_feed[warp];
+            __syncwarp();
+            walk_next<kTileRows, kTile>(w, A);
+            if (lane == 0) s_feed[warp] = w;
+            __syncwarp();
+            feeder.begin(A, w, total - fed, kRows ? 0 : kBite * warp, lane);
+        } else feeder.look(A, lane);
+    };
+    if (feeds) {
+        feeder.begin(A, s_feed[warp], total, kRows ? 0 : kBite * warp, lane);
+        for (int i = 0; i < kStages && fed < total; i++) feed();
+    }
 
-    if (warp == kEaters) {
-        // ---- brings the octets
-        int held = -1, row_of = -1, blocks_from = 0;
-        long long u = from;
-        int issued = 0;
-        while (u < to && ok) {
-            const int upto = (int)min((long long)w.count, (long long)w.at + (to - u));
-            for (; w.at < upto && ok; w.at++, u++, issued++) {
-                const int stage = issued % kStages, turn = issued / kStages;
-                const int token = (w.first + w.at) * kTile + 8 * lane;
-                bool want = lane < kTile / 8 && token < w.hi && token + 8 > w.lo;
-                const int octet = token >> 3, block = octet / A.octets;
-                // block ids of the row, 32 at a time
-                const int first = __shfl_sync(0xffffffffu, block, 0), last = min(__shfl_sync(0xffffffffu, block, kTile / 8 - 1), A.width - 1);
-                if (w.r != row_of || first < blocks_from || last >= blocks_from + 32) {
-                    row_of = w.r; blocks_from = first;
-                    held = first + lane < A.width ? A.table[(long long)w.r * A.width + first + lane] : -1;
-                }
-                const int id = __shfl_sync(0xffffffffu, held, min(max(block - blocks_from, 0), 31));
-                want = want && block < A.width && id >= 0 && id < A.num_blocks;
-                const unsigned have = __ballot_sync(0xffffffffu, want);
-                if (turn > 0) ok = bar_wait(smem_addr(&s_free[stage]), (turn - 1) & 1);
-                ok = __all_sync(0xffffffffu, ok);
-                if (!ok) break;
-                const unsigned bar = smem_addr(&s_full[stage]);
-                if (lane == 0) {
-                    s_have[stage] = have;
-                    bar_expect(bar, __popc(have) * kOctet);
-                }
-                __syncwarp();
-                if (want)
-                    bulk_load(smem_addr(ring) + stage * S::kUnit + lane * kOctet,
-                              A.cache + id * A.block_stride + w.h * A.head_bytes + (long long)(octet - block * A.octets) * kOctet, kOctet, bar);
-            }
-            if (w.at == w.count && u < to) walk_next<kTileRows>(w, A);
-        }
-        // (its copies end before it does, whether or not they were waited for)
-        for (int i = max(0, issued - kStages); i < issued; i++) ok &= bar_wait(smem_addr(&s_full[i % kStages]), (i / kStages) & 1);
-        if (!ok && lane == 0) *(volatile int*)&s_failed = 1;
-    } else {
-        State<J, NT> s;
-        long long u = from;
-        int eaten = 0;
-        AttendNote left = {0, 0, 0, 0, 0, 0, 0, 0};
-        float* pieces = reinterpret_cast<float*>(A.ws + (size_t)A.ctas * sizeof(AttendNote));
-        while (u < to) {
-            const int row = w.y * kTileRows + (kRows ? warp * 8 * NT : 0);     // this warp's first query row
-            load_queries<J, NT>(s, A, w, row, lane);
-            // tokens that all of the item's query rows see
-            const int last_row = min(w.n * A.group, (w.y + 1) * kTileRows) - 1;
-            const int all_hi = w.p0 < 0 ? 0 : (int)min((long long)w.p0 + w.y * kTileRows / A.group + 1, (long long)A.most);
-            const int all_lo = A.window > 0 ? (int)min(max((long long)w.p0 + last_row / A.group - A.window + 1, 0ll), (long long)A.most) : 0;
-            const int begin = w.at, upto = (int)min((long long)w.count, (long long)w.at + (to - u));
-            for (; w.at < upto; w.at++, u++, eaten++) {
-                const int stage = eaten % kStages;
-                if (ok) ok = __all_sync(0xffffffffu, bar_wait(smem_addr(&s_full[stage]), (eaten / kStages) & 1));
-                if (ok) {
-                    const unsigned have = s_have[stage];
+    State<J, NT> s;
+    AttendNote left = {0, 0, 0, 0, 0, 0, 0, 0};
+    float* pieces = reinterpret_cast<float*>(A.ws + (size_t)A.ctas * sizeof(AttendNote));
+    const Walk& w = s_eat[warp];
+    int done = 0;
+    while (done < total) {
+        const int row = w.y * kTileRows + (kRows ? warp * 8 * NT : 0);         // this warp's first query row
+        load_queries<J, NT>(s, A, w, row, lane);
+        const int item_rows = min(kTileRows, w.n * A.group - w.y * kTileRows), last_row = w.y * kTileRows + item_rows - 1;
+        const bool idle = kRows && row > last_row;
+        // tokens that all of the item's query rows see
+        const int all_hi = w.p0 < 0 ? 0 : (int)min((long long)w.p0 + w.y * kTileRows / A.group + 1, (long long)A.most);
+        const int all_lo = A.window > 0 ? (int)min(max((long long)w.p0 + last_row / A.group - A.window + 1, 0ll), (long long)A.most) : 0;
+        const int begin = w.at, count = w.count, upto = min(count, begin + total - done);
+        int token = (w.first + begin) * kTile + (kRows ? 0 : kBite * warp);
+        for (int at = begin; at < upto; at++, done++, token += kTile) {
+            const int stage = done % kStages;
+            if (ok) ok = __all_sync(0xffffffffu, bar_wait(smem_addr(full + stage), (done / kStages) & 1));
+            if (ok && !idle) {
+                const unsigned have = held[stage];
+                const char* octets = ring + stage * S::kStage;
 #pragma unroll 1
-                    for (int sub = kRows ? 0 : warp; sub < (kRows ? kTile / 16 : warp + 1); sub++) {
-                        const unsigned both = have >> (2 * sub) & 3;
-                        const int token = (w.first + w.at) * kTile + 16 * sub;
-                        const char* at = ring + stage * S::kUnit + 2 * sub * kOctet;
-                        if (kRows && row > last_row) break;
-                        if (both == 3 && token >= all_lo && token + 16 <= all_hi) eat<J, NT, true>(s, at, lane, A, w, row, token, both);
-                        else if (both) eat<J, NT, false>(s, at, lane, A, w, row, token, both);
-                    }
+                for (int b = 0; b < (kRows ? kTile / kBite : 1); b++) {
+                    const unsigned four = have >> (4 * b) & 15;
+                    if (four == 15 && token + kBite * b >= all_lo && token + kBite * (b + 1) <= all_hi)
+                        eat<J, NT, true>(s, octets + 4 * b * S::kOctet, lane, A, w, row, token + kBite * b, four);
+                    else if (four) eat<J, NT, false>(s, octets + 4 * b * S::kOctet, lane, A, w, row, token + kBite * b, four);
                 }
-                __syncwarp();
-                if (lane == 0) bar_arrive(smem_addr(&s_free[stage]));
             }
-            // ---- the item's end, or this CTA's
-            const bool complete = begin == 0 && upto == w.count;
-            const int rows = min(kTileRows, w.n * A.group - w.y * kTileRows);
-            float* piece = pieces + (2 * (size_t)blockIdx.x + (begin == 0 ? 1 : 0)) * piece_floats(kTileRows, D);
+            __syncwarp();
+            if (kRows) {
+                // (the ring's places are filled again a unit late: by then all warps are mostly done with them)
+                if (feeds && ok && done > 0 && fed < total) {
+                    const int last = done - 1;
+                    ok = __all_sync(0xffffffffu, bar_wait(smem_addr(&s_free[last % kStages]), (last / kStages) & 1));
+                    if (ok) feed();
+                }
+                if (lane == 0) bar_arrive(smem_addr(&s_free[stage]));
+            } else if (ok && fed < total) feed();
+        }
+        // ---- the item's end, or this CTA's
+        const bool complete = begin == 0 && upto == count;
+        float* piece = pieces + (2 * (size_t)blockIdx.x + (begin == 0 ? 1 : 0)) * piece_floats(kTileRows, D);
+        const int g = lane >> 2, t = lane & 3;
+        results<J, NT>(s, lane);
+        if (!kRows) {
+            // the warps' results to the first one's: half of them to the others, twice
+            if (g == 0) {
+#pragma unroll
+                for (int x = 0; x < NT; x++)
+#pragma unroll
+                    for (int z = 0; z < 2; z++) {
+                        s_m[warp][8 * x + 2 * t + z] = s.m[x][z] == -INFINITY ? -INFINITY : s.ref[x][z];
+                        s_l[warp][8 * x + 2 * t + z] = s.l[x][z];
+                    }
+            }
+            __syncthreads();
+            float* join = reinterpret_cast<float*>(rings + S::kRings * kStages * S::kStage) + (warp & 1) * 8 * NT * S::kStep;
 #pragma unroll
             for (int x = 0; x < NT; x++)
 #pragma unroll
-                for (int z = 0; z < 2; z++)
-#pragma unroll
-                    for (int o = 4; o < 32; o *= 2) s.l[x][z] += __shfl_xor_sync(0xffffffffu, s.l[x][z], o);
-            const int g = lane >> 2, t = lane & 3;
-            if (kRows) {
-#pragma unroll
-                for (int x = 0; x < NT; x++)
-#pragma unroll
-                    for (int z = 0; z < 2; z++) {
-                        const int i = warp * 8 * NT + 8 * x + 2 * t + z;
-                        const float by = !complete ? 1.f : s.l[x][z] == 0.f ? 0.f : 1.f / s.l[x][z];
-                        if (!complete && i < rows && g == 0) { piece[i] = s.m[x][z]; piece[kTileRows + i] = s.l[x][z]; }
-                        const long long at = complete && i < rows ? out_at(A, w.token, w.y * kTileRows + i, w.h) : 0;
-#pragma unroll
-                        for (int j = 0; j < J; j++) {
-                            float v[4];
-                            result<J, NT>(s, x, j, z, lane, v);
-                            if (i >= rows) continue;
-#pragma unroll
-                            for (int e = 0; e < 4; e++) v[e] *= by;
-                            if (complete) store_out(A, at + 32 * j + 4 * g, v);
-                            else *reinterpret_cast<float4*>(piece + 2 * kTileRows + i * D + 32 * j + 4 * g) = make_float4(v[0], v[1], v[2], v[3]);
-                        }
-                    }
-            } else {
-                if (g == 0) {
-#pragma unroll
-                    for (int x = 0; x < NT; x++)
-#pragma unroll
-                        for (int z = 0; z < 2; z++) { s_m[warp][8 * x + 2 * t + z] = s.m[x][z]; s_l[warp][8 * x + 2 * t + z] = s.l[x][z]; }
-                }
-                eaters_sync();
-                float* join = reinterpret_cast<float*>(ring + kStages * S::kUnit);
-#pragma unroll
-                for (int x = 0; x < NT; x++)
-#pragma unroll
-                    for (int z = 0; z < 2; z++) {
-                        const int i = 8 * x + 2 * t + z;
-                        float m = -INFINITY;
-#pragma unroll
-                        for (int k = 0; k < kEaters; k++) m = fmaxf(m, s_m[k][i]);
-                        const float by = s.m[x][z] == -INFINITY ? (s.l[x][z] == 0.f ? 0.f : 1.f) : exp2_of(s.m[x][z] - m);
-#pragma unroll
-                        for (int j = 0; j < J; j++) {
-                            float v[4];
-                            result<J, NT>(s, x, j, z, lane, v);
-                            *reinterpret_cast<float4*>(join + (warp * 8 * NT + i) * S::kStep + 32 * j + 4 * g) = make_float4(v[0] * by, v[1] * by, v[2] * by, v[3] * by);
-                        }
-                    }
-                eaters_sync();
-                for (int e = tid; e < rows * (D / 4); e += 32 * kEaters) {
-                    const int i = e / (D / 4), c = 4 * (e - i * (D / 4));
-                    float m = -INFINITY, l = 0.f, v[4] = {0.f, 0.f, 0.f, 0.f};
+                for (int z = 0; z < 2; z++) {
+                    const int i = 8 * x + 2 * t + z;
+                    float m = -INFINITY, l = 0.f;
 #pragma unroll
                     for (int k = 0; k < kEaters; k++) m = fmaxf(m, s_m[k][i]);
 #pragma unroll
-                    for (int k = 0; k < kEaters; k++) {
-                        l += s_m[k][i] == -INFINITY ? s_l[k][i] : s_l[k][i] * exp2_of(s_m[k][i] - m);      // (0, or NaN)
-                        const float4 z = *reinterpret_cast<const float4*>(join + (k * 8 * NT + i) * S::kStep + c);
-                        v[0] += z.x; v[1] += z.y; v[2] += z.z; v[3] += z.w;
-                    }
-                    if (complete) {
-                        const float by = l == 0.f ? 0.f : 1.f / l;
+                    for (int k = 0; k < kEaters; k++) l += s_m[k][i] == -INFINITY ? s_l[k][i] : s_l[k][i] * exp2_of(s_m[k][i] - m);      // (0, or NaN)
+                    if (s.m[x][z] != -INFINITY) times(s, x, z, exp2_of(s.ref[x][z] - m));
+                    s.m[x][z] = m; s.l[x][z] = l;
+                }
 #pragma unroll
-                        for (int z = 0; z < 4; z++) v[z] *= by;
-                        store_out(A, out_at(A, w.token, w.y * kTileRows + i, w.h) + c, v);
-                    } else {
-                        if (c == 0) { piece[i] = m; piece[kTileRows + i] = l; }
-                        *reinterpret_cast<float4*>(piece + 2 * kTileRows + i * D + c) = make_float4(v[0], v[1], v[2], v[3]);
+            for (int step = 2; step > 0; step >>= 1) {
+                if (warp >= step && warp < 2 * step) {
+#pragma unroll
+                    for (int x = 0; x < NT; x++)
+#pragma unroll
+                        for (int z = 0; z < 2; z++)
+#pragma unroll
+                            for (int j = 0; j < J; j++)
+                                *reinterpret_cast<float4*>((step == 1 ? join - 8 * NT * S::kStep : join) + (8 * x + 2 * t + z) * S::kStep + 32 * j + 4 * g) =
+                                    make_float4(s.o[x][2 * j][z], s.o[x][2 * j][z + 2], s.o[x][2 * j + 1][z], s.o[x][2 * j + 1][z + 2]);
+                }
+                __syncthreads();
+                if (warp < step) {
+#pragma unroll
+                    for (int x = 0; x < NT; x++)
+#pragma unroll
+                        for (int z = 0; z < 2; z++)
+#pragma unroll
+                            for (int j = 0; j < J; j++) {
+                                const float4 v = *reinterpret_cast<const float4*>(join + (8 * x + 2 * t + z) * S::kStep + 32 * j + 4 * g);
+                                s.o[x][2 * j][z] += v.x; s.o[x][2 * j][z + 2] += v.y; s.o[x][2 * j + 1][z] += v.z; s.o[x][2 * j + 1][z + 2] += v.w;
+                            }
+                }
+                __syncthreads();
+            }
+        }
+        if (kRows || warp == 0) {
+#pragma unroll
+            for (int x = 0; x < NT; x++)
+#pragma unroll
+                for (int z = 0; z < 2; z++) {
+                    const int i = (kRows ? warp * 8 * NT : 0) + 8 * x + 2 * t + z;
+                    if (i >= item_rows) continue;
+                    if (!complete) {
+                        if (g == 0) { piece[i] = kRows && s.m[x][z] != -INFINITY ? s.ref[x][z] : s.m[x][z]; piece[kTileRows + i] = s.l[x][z]; }
+#pragma unroll
+                        for (int j = 0; j < J; j++)
+                            *reinterpret_cast<float4*>(piece + 2 * kTileRows + i * D + 32 * j + 4 * g) =
+                                make_float4(s.o[x][2 * j][z], s.o[x][2 * j][z + 2], s.o[x][2 * j + 1][z], s.o[x][2 * j + 1][z + 2]);
+                        continue;
+                    }
+                    const float by = s.l[x][z] == 0.f ? 0.f : 1.f / s.l[x][z];
+                    const long long to = out_at(A, w.token, w.y * kTileRows + i, w.h) + 4 * g;
+#pragma unroll
+                    for (int j = 0; j < J; j++) {
+                        const float v[4] = {s.o[x][2 * j][z] * by, s.o[x][2 * j][z + 2] * by, s.o[x][2 * j + 1][z] * by, s.o[x][2 * j + 1][z + 2] * by};
+                        store_out(A, to + 32 * j, v);
                     }
                 }
-                eaters_sync();
-            }
-            if (begin == 0 && !complete) {
-                // the CTA with the item's last unit
-                const long long end = u - upto + w.count - 1, total = s_total, ctas = s_ctas;
-                long long c = end * ctas / total;
-                while (total * (c + 1) / ctas <= end) c++;
-                left = AttendNote{1, w.token, w.y * kTileRows, rows, w.h, (int)c, 0, 0};
-            }
-            if (w.at == w.count && u < to) walk_next<kTileRows>(w, A);
         }
-        if (!ok && lane == 0) *(volatile int*)&s_failed = 1;
-        eaters_sync();
-        if (tid == 0) { left.failed = *(volatile int*)&s_failed; *note = left; }
+        if (begin == 0 && !complete) {
+            // the CTA with the item's last unit
+            const long long end = from + done - upto + count - 1, all = s_total, ctas = s_ctas;
+            long long c = end * ctas / all;
+            while (all * (c + 1) / ctas <= end) c++;
+            left = AttendNote{1, w.token, w.y * kTileRows, item_rows, w.h, (int)c, 0, 0};
+        }
+        if (upto == count && done < total) {
+            Walk next = w;
+            __syncwarp();
+            walk_next<kTileRows, kTile>(next, A);
+            if (lane == 0) s_eat[warp] = next;
+            __syncwarp();
+        }
     }
+    if (feeds) {
+        // (its copies end before it does, whether or not they were waited for)
+        for (int i = max(0, fed - kStages); i < fed; i++) ok &= bar_wait(smem_addr(full + i % kStages), (i / kStages) & 1);
+    }
+    if (!ok && lane == 0) *(volatile int*)&s_failed = 1;
+    __syncthreads();
+    if (tid == 0) { left.failed = *(volatile int*)&s_failed; *note = left; }
 }
 
 // ---------------------------------------------------------------- second kernel
@@ -755,6 +861,9 @@ int gr_cache_attend(const void* q, int dtype, int q_heads, long long q_token, lo
     A.table = table; A.offsets = offsets; A.positions = positions; A.status = status;
     A.dtype = dtype; A.tokens = tokens; A.heads = L.heads; A.group = q_heads / L.heads; A.width = width; A.rows = rows; A.window = window;
     A.most = width * L.block_size;
+    // n / octets for n < 2^28: ceil(2^(32 + shift) / octets) n / 2^(32 + shift), with 2^shift the power of two at or above half of octets
+    while (A.octets > 2 << A.shift) A.shift++;
+    A.by_octets = A.octets > 1 ? (unsigned)(((1ull << (32 + A.shift)) + (unsigned)A.octets - 1) / (unsigned)A.octets) : 0u;
     A.scale = scale * 1.44269504088896340736f;
     A.ws = (char*)workspace;
     gr::Align in, to;
