@@ -25,7 +25,7 @@ namespace gr {
 constexpr int kEaters = 4;                     // warps of a CTA
 constexpr int kAttendThreads = 32 * kEaters;
 constexpr int kBite = 32;                      // tokens that a warp takes at a time
-constexpr int kJoinThreads = 256;
+constexpr int kJoinThreads = 256, kJoinWarps = kJoinThreads / 32;
 constexpr unsigned long long kWaitNs = 2000000000ull;      // longest wait for a copy or a free place in the ring
 
 struct AttendArgs {
@@ -53,7 +53,7 @@ struct Shape {
     static constexpr int kJoin = kRows ? 0 : 2 * 8 * NT * kStep * 4;
     // resident CTAs per SM, by registers: 128, 168 or 255 a thread
     static constexpr int kCtas = NT == 1 ? (J <= 4 ? 4 : J <= 6 ? 3 : 2) : (J <= 1 ? 4 : J <= 3 ? 3 : 2);
-    static constexpr int kRoom = 227 * 1024 / kCtas - 2560 - kJoin;
+    static constexpr int kRoom = 227 * 1024 / kCtas - 2048 - kJoin;
     static constexpr int kStages = kRoom / (kRings * kStage) < 4 ? kRoom / (kRings * kStage) : 4;
     static constexpr int kSmem = kStages * kRings * kStage + kJoin;
     static_assert(kStages >= 2, "a ring");
@@ -83,9 +83,7 @@ __device__ __noinline__ bool bar_wait_long(unsigned bar, unsigned parity)
 }
 __device__ __forceinline__ bool bar_wait(unsigned bar, unsigned parity)
 {
-#pragma unroll 1
-    for (int i = 0; i < 32; i++) if (bar_try(bar, parity)) return true;
-    return bar_wait_long(bar, parity);
+    return bar_try(bar, parity) || bar_wait_long(bar, parity);
 }
 __device__ __forceinline__ void bulk_load(unsigned to, const void* from, unsigned bytes, unsigned bar)
 {
@@ -99,6 +97,11 @@ __device__ __forceinline__ void mma(float (&d)[4], unsigned a0, unsigned a1, uns
 __device__ __forceinline__ void mma(float (&d)[4], unsigned a0, unsigned a1, unsigned a2, unsigned a3, unsigned b0, unsigned b1)
 {
     mma(d, a0, a1, a2, a3, b0, b1, d[0], d[1], d[2], d[3]);
+}
+__device__ __forceinline__ void mma8(float (&d)[4], unsigned a0, unsigned a1, unsigned b)
+{
+    asm("mma.sync.aligned.m16n8k8.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5}, {%6}, {%0, %1, %2, %3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(b));
 }
 __device__ __forceinline__ unsigned transposed(unsigned v)
 {
@@ -125,16 +128,23 @@ __device__ __forceinline__ void load_words(unsigned (&w)[J], const char* p)     
     }
 }
 
+// J fp16 numbers, two to a word, aligned to 2 J bytes
 template <int J>
-__device__ __forceinline__ void load_halves(unsigned short (&w)[J], const char* p)
+__device__ __forceinline__ void load_halves(unsigned (&w)[(J + 1) / 2], const char* p)
 {
-    constexpr int W = J % 4 == 0 ? 4 : J % 2 == 0 ? 2 : 1;
+    if constexpr (J % 2 == 0) load_words<J / 2>(w, p);
+    else {
 #pragma unroll
-    for (int i = 0; i < J; i += W) {
-        const Pack<unsigned short, W> v = *reinterpret_cast<const Pack<unsigned short, W>*>(p + 2 * i);
-#pragma unroll
-        for (int z = 0; z < W; z++) w[i + z] = v.x[z];
+        for (int i = 0; i < J; i++) {
+            const unsigned h = *reinterpret_cast<const unsigned short*>(p + 2 * i);
+            w[i / 2] = i & 1 ? w[i / 2] | h << 16 : h;
+        }
     }
+}
+__device__ __forceinline__ float half_of(const unsigned* w, int i)
+{
+    const __half2 h = *reinterpret_cast<const __half2*>(w + i / 2);
+    return i & 1 ? __high2float(h) : __low2float(h);
 }
 
 // ---------------------------------------------------------------- the order of the work
@@ -182,12 +192,18 @@ __device__ __forceinline__ void walk_next(Walk& w, const AttendArgs& A)
     walk_item<kTileRows, kTile>(w, A);
 }
 
+// where share i of `parts` of the units begins (32 bits divide in a fraction of the time)
+__device__ __forceinline__ long long share_of(long long total, int i, long long parts)
+{
+    return total < (1 << 20) ? (long long)((unsigned)total * (unsigned)i / (unsigned)parts) : total * i / parts;
+}
+
 // ---------------------------------------------------------------- a warp's share
 
 template <int J, int NT>
 struct State {
-    unsigned q[NT][J][4];                      // the queries as operands, scaled
-    float down[NT][J][2];                      // -8 2^-24 times the queries' sums
+    uint4 q[NT][J];                            // the queries as operands, scaled
+    unsigned sum[NT][(J + 3) / 4];             // -8 2^-24 times the queries' sums by groups, in two fp16 parts, as operands (group t, t + 4)
     float f[NT][2];                            // from products to x, positive
     float m[NT][2], ref[NT][2], l[NT][2];      // m: the largest product; ref: its x, or 0 where there is none
     float o[NT][2 * J][4], off[NT][4];
@@ -231,19 +247,20 @@ __device__ __forceinline__ void load_queries(State<J, NT>& s, const AttendArgs& 
         const float back = fmaxf(A.scale * 16777216.f / by, 1e-30f);
         s.f[x][0] = __shfl_sync(0xffffffffu, back, 8 * t); s.f[x][1] = __shfl_sync(0xffffffffu, back, 8 * t + 4);
 #pragma unroll
+        for (int j = 0; j < J; j += 4) s.sum[x][j / 4] = 0u;
+#pragma unroll
         for (int j = 0; j < J; j++) {
             float sum = 0.f;
 #pragma unroll
             for (int e = 0; e < 8; e++) { v[j][e] *= by; sum += v[j][e]; }
-#pragma unroll
-            for (int z = 0; z < 2; z++) {
-                s.q[x][j][2 * z] = pack_h2(v[j][2 * z], v[j][2 * z + 4]);
-                s.q[x][j][2 * z + 1] = pack_h2(v[j][2 * z + 1] * 0.0625f, v[j][2 * z + 5] * 0.0625f);
-            }
+            s.q[x][j] = make_uint4(pack_h2(v[j][0], v[j][4]), pack_h2(v[j][1] * 0.0625f, v[j][5] * 0.0625f),
+                                   pack_h2(v[j][2], v[j][6]), pack_h2(v[j][3] * 0.0625f, v[j][7] * 0.0625f));
             sum += __shfl_xor_sync(0xffffffffu, sum, 1);
             sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+            // (below 2^-2; what the second part leaves is at most 2^-25, an eighth of a unit of the largest of the 32 products)
             sum *= -8.f / 16777216.f;
-            s.down[x][j][0] = __shfl_sync(0xffffffffu, sum, 8 * t); s.down[x][j][1] = __shfl_sync(0xffffffffu, sum, 8 * t + 4);
+            const float high = __half2float(__float2half_rn(sum));
+            if (t == (j & 3)) s.sum[x][j / 4] = pack_h2(high, sum - high);
         }
 #pragma unroll
         for (int z = 0; z < 2; z++) { s.m[x][z] = -INFINITY; s.ref[x][z] = 0.f; s.l[x][z] = 0.f; }
@@ -264,29 +281,47 @@ __device__ __forceinline__ void eat(State<J, NT>& s, const char* at, int lane, c
     constexpr int D = 32 * J, kOctet = octet_bytes(D);
     const int g = lane >> 2, t = lane & 3;
     float x[NT][2][4];
+    {
+        // what 8 is taken off for: group by group the scale times the queries' sum
 #pragma unroll
-    for (int b = 0; b < 2; b++) {
-        const char* from = at + 2 * b * kOctet;
-        unsigned k0[J], k1[J];
-        unsigned short s0[J], s1[J];
-        load_words<J>(k0, from + 4 * J * lane);
-        load_words<J>(k1, from + kOctet + 4 * J * lane);
-        load_halves<J>(s0, from + octet_kscale(D) + 2 * J * g);
-        load_halves<J>(s1, from + kOctet + octet_kscale(D) + 2 * J * g);
+        for (int b = 0; b < 2; b++) {
+            const char* from = at + 2 * b * kOctet + octet_kscale(D) + 2 * J * g;
 #pragma unroll
-        for (int j = 0; j < J; j++) {
-            const float c = __half2float(__ushort_as_half(s0[j])), e = __half2float(__ushort_as_half(s1[j]));
-            const unsigned u0 = k0[j] >> 8, u1 = k1[j] >> 8;
+            for (int j = 0; j < J; j += 4) {
+                const unsigned short h0 = j + t < J ? *(const unsigned short*)(from + 2 * (j + t)) : (unsigned short)0;
+                const unsigned short h1 = j + t < J ? *(const unsigned short*)(from + kOctet + 2 * (j + t)) : (unsigned short)0;
 #pragma unroll
-            for (int n = 0; n < NT; n++) {
-                float d[4];
-                mma(d, k0[j] & 0x000f000fu, k1[j] & 0x000f000fu, k0[j] & 0x00f000f0u, k1[j] & 0x00f000f0u, s.q[n][j][0], s.q[n][j][1],
-                    s.down[n][j][0], s.down[n][j][1], s.down[n][j][0], s.down[n][j][1]);
-                mma(d, u0 & 0x000f000fu, u1 & 0x000f000fu, u0 & 0x00f000f0u, u1 & 0x00f000f0u, s.q[n][j][2], s.q[n][j][3]);
-                if (j == 0) { x[n][b][0] = c * d[0]; x[n][b][1] = c * d[1]; x[n][b][2] = e * d[2]; x[n][b][3] = e * d[3]; }
-                else {
-                    x[n][b][0] = fmaf(c, d[0], x[n][b][0]); x[n][b][1] = fmaf(c, d[1], x[n][b][1]);
-                    x[n][b][2] = fmaf(e, d[2], x[n][b][2]); x[n][b][3] = fmaf(e, d[3], x[n][b][3]);
+                for (int n = 0; n < NT; n++) {
+                    if (j == 0) x[n][b][0] = x[n][b][1] = x[n][b][2] = x[n][b][3] = 0.f;
+                    mma8(x[n][b], h0 * 0x10001u, h1 * 0x10001u, s.sum[n][j / 4]);
+                }
+            }
+        }
+        constexpr int kAtOnce = 1;
+#pragma unroll
+        for (int b0 = 0; b0 < 2; b0 += kAtOnce) {
+            unsigned k[kAtOnce][2][J], sc[kAtOnce][2][(J + 1) / 2];
+#pragma unroll
+            for (int b = 0; b < kAtOnce; b++)
+#pragma unroll
+                for (int o = 0; o < 2; o++) {
+                    const char* from = at + (2 * (b0 + b) + o) * kOctet;
+                    load_words<J>(k[b][o], from + 4 * J * lane);
+                    load_halves<J>(sc[b][o], from + octet_kscale(D) + 2 * J * g);
+                }
+#pragma unroll
+            for (int j = 0; j < J; j++) {
+#pragma unroll
+                for (int b = 0; b < kAtOnce; b++) {
+                    const float c = half_of(sc[b][0], j), e = half_of(sc[b][1], j);
+                    const unsigned w0 = k[b][0][j], w1 = k[b][1][j], u0 = w0 >> 8, u1 = w1 >> 8;
+#pragma unroll
+                    for (int n = 0; n < NT; n++) {
+                        float d[4], (&y)[4] = x[n][b0 + b];
+                        mma(d, w0 & 0x000f000fu, w1 & 0x000f000fu, w0 & 0x00f000f0u, w1 & 0x00f000f0u, s.q[n][j].x, s.q[n][j].y, 0.f, 0.f, 0.f, 0.f);
+                        mma(d, u0 & 0x000f000fu, u1 & 0x000f000fu, u0 & 0x00f000f0u, u1 & 0x00f000f0u, s.q[n][j].z, s.q[n][j].w);
+                        y[0] = fmaf(c, d[0], y[0]); y[1] = fmaf(c, d[1], y[1]); y[2] = fmaf(e, d[2], y[2]); y[3] = fmaf(e, d[3], y[3]);
+                    }
                 }
             }
         }
@@ -434,48 +469,57 @@ __device__ __forceinline__ long long out_at(const AttendArgs& A, int token, int 
 
 // ---------------------------------------------------------------- first kernel
 
-// Brings octets into a ring, ahead of what is eaten: a warp's place in the units, and the block ids of the next ones.
+// Brings octets into a ring, ahead of what is eaten: a warp's place in the units (in shared memory, for registers), and the block ids of the next ones.
+struct FeedItem {
+    const char* head;                          // the cache from the item's head on
+    const int* row;                            // the table's row
+    int hi, lo, left;                          // tokens that are wanted; units of the item that are left
+};
 template <int J, int NT, bool kRows>
 struct Feeder {
     using S = Shape<J, NT, kRows>;
     static constexpr int kOctets = S::kStage / S::kOctet;
-    const char* head;                          // the cache from the item's head on
-    long long row;                             // the table's row
-    int token, hi, lo, left, id, in;           // token: of this lane's octet in the next unit; left: units of the item; id, in: its block, and place there
+    int token, id, in;                         // of this lane's octet in the next unit: first token, block, place in that
 
-    __device__ __forceinline__ void begin(const AttendArgs& A, const Walk& w, long long units, int skip, int lane)
+    __device__ __forceinline__ void begin(FeedItem& f, const AttendArgs& A, const Walk& w, int units, int skip, int lane)
     {
-        head = A.cache + (long long)w.h * A.head_bytes;
-        row = (long long)w.r * A.width;
+        if (lane == 0) f = FeedItem{A.cache + (long long)w.h * A.head_bytes, A.table + (long long)w.r * A.width, w.hi, w.lo, min(w.count - w.at, units)};
         token = (w.first + w.at) * S::kTile + skip + 8 * lane;
-        hi = w.hi; lo = w.lo;
-        left = (int)min((long long)(w.count - w.at), units);
-        look(A, lane);
+        __syncwarp();
+        look(f, A, lane);
     }
-    __device__ __forceinline__ void look(const AttendArgs& A, int lane)
+    __device__ __forceinline__ void look(const FeedItem& f, const AttendArgs& A, int lane)
     {
         id = -1;
-        if (lane < kOctets && token < hi && token + 8 > lo) {
+        if (lane < kOctets && token < f.hi && token + 8 > f.lo) {
             // (blocks of a multiple of eight tokens; the quotient by a product with the reciprocal, rounded up)
             const unsigned octet = (unsigned)token >> 3, block = A.octets == 1 ? octet : __umulhi(octet, A.by_octets) >> A.shift;
             in = (int)(octet - block * (unsigned)A.octets);
-            if ((int)block < A.width) id = A.table[row + block];
+            if ((int)block < A.width) id = f.row[block];
         }
     }
-    // into place `place` of the ring; `have`: which octets it will hold
-    __device__ __forceinline__ void bring(const AttendArgs& A, char* place, unsigned long long* full, unsigned* have, int lane)
+    // into place `place` of the ring; `have`: which octets it will hold; whether that was the item's last unit.  (Octets next to one another in a block
+    // by one copy: the instruction takes one address a warp, lanes with one each go through it in turn.)
+    __device__ __forceinline__ bool bring(FeedItem& f, const AttendArgs& A, char* place, unsigned long long* full, unsigned* have, int lane)
     {
         const bool want = id >= 0 && id < A.num_blocks;
-        const unsigned mask = __ballot_sync(0xffffffffu, want);
+        const unsigned mask = __ballot_sync(0xffffffffu, want), starts = __ballot_sync(0xffffffffu, want && (lane == 0 || in == 0 || !(mask >> ((lane - 1) & 31) & 1)));
         const unsigned bar = smem_addr(full);
+        const int left = f.left - 1;
+        __syncwarp();
         if (lane == 0) {
             *have = mask;
+            f.left = left;
             bar_expect(bar, __popc(mask) * S::kOctet);
         }
         __syncwarp();
-        if (want) bulk_load(smem_addr(place) + lane * S::kOctet, head + id * A.block_stride + (long long)in * S::kOctet, S::kOctet, bar);
+        if (starts >> lane & 1) {
+            // up to the next start, or the first that is not wanted
+            const unsigned stop = (starts | ~mask) & ~((2u << lane) - 1u);
+            bulk_load(smem_addr(place) + lane * S::kOctet, f.head + id * A.block_stride + (long long)in * S::kOctet, (__ffs(stop) - 1 - lane) * S::kOctet, bar);
+        }
         token += S::kTile;
-        left--;
+        return left == 0;
     }
 };
 
@@ -491,6 +535,7 @@ attend_kernel(const __grid_constant__ AttendArgs A)
     __shared__ float s_m[kEaters][8 * NT], s_l[kEaters][8 * NT];
     __shared__ long long s_scan[kEaters], s_from, s_to, s_total, s_ctas;
     __shared__ Walk s_eat[kEaters], s_feed[kEaters];       // each warp's own
+    __shared__ FeedItem s_item[kEaters];
     __shared__ int s_failed;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     if (tid == 0) {
@@ -521,7 +566,8 @@ attend_kernel(const __grid_constant__ AttendArgs A)
 #pragma unroll
         for (int i = 0; i < kEaters; i++) { if (i < warp) upto += s_scan[i]; total += s_scan[i]; }
         const long long ctas = min((long long)A.ctas, total);
-        const long long from = ctas > 0 && blockIdx.x < ctas ? total * blockIdx.x / ctas : 0, to = ctas > 0 && blockIdx.x < ctas ? total * (blockIdx.x + 1) / ctas : 0;
+        const bool works = blockIdx.x < ctas;
+        const long long from = works ? share_of(total, blockIdx.x, ctas) : 0, to = works ? share_of(total, blockIdx.x + 1, ctas) : 0;
         if (tid == 0) { s_from = from; s_to = to; s_total = total; s_ctas = ctas; }
         if (from < to && upto - mine <= from && from < upto) {
             // (one thread's rows hold the share's first unit)
@@ -559,23 +605,22 @@ attend_kernel(const __grid_constant__ AttendArgs A)
     unsigned long long* full = s_full[kRows ? 0 : warp];
     unsigned* held = s_have[kRows ? 0 : warp];
     Feeder<J, NT, kRows> feeder;
-    int fed = 0;
-    auto feed = [&]() {
-        feeder.bring(A, ring + fed % kStages * S::kStage, full + fed % kStages, held + fed % kStages, lane);
-        fed++;
-        if (fed == total) return;
-        if (feeder.left == 0) {
+    // unit `next` of the share
+    auto feed = [&](int next) {
+        const int place = next % kStages;
+        const bool end = feeder.bring(s_item[warp], A, ring + place * S::kStage, full + place, held + place, lane);
+        if (next + 1 == total) return;
+        if (end) {
             Walk w = s_feed[warp];
             __syncwarp();
             walk_next<kTileRows, kTile>(w, A);
             if (lane == 0) s_feed[warp] = w;
-            __syncwarp();
-            feeder.begin(A, w, total - fed, kRows ? 0 : kBite * warp, lane);
-        } else feeder.look(A, lane);
+            feeder.begin(s_item[warp], A, w, total - next - 1, kRows ? 0 : kBite * warp, lane);
+        } else feeder.look(s_item[warp], A, lane);
     };
     if (feeds) {
-        feeder.begin(A, s_feed[warp], total, kRows ? 0 : kBite * warp, lane);
-        for (int i = 0; i < kStages && fed < total; i++) feed();
+        feeder.begin(s_item[warp], A, s_feed[warp], total, kRows ? 0 : kBite * warp, lane);
+        for (int i = 0; i < kStages && i < total; i++) feed(i);
     }
 
     State<J, NT> s;
@@ -610,13 +655,13 @@ attend_kernel(const __grid_constant__ AttendArgs A)
             __syncwarp();
             if (kRows) {
                 // (the ring's places are filled again a unit late: by then all warps are mostly done with them)
-                if (feeds && ok && done > 0 && fed < total) {
+                if (feeds && ok && done > 0 && done - 1 + kStages < total) {
                     const int last = done - 1;
                     ok = __all_sync(0xffffffffu, bar_wait(smem_addr(&s_free[last % kStages]), (last / kStages) & 1));
-                    if (ok) feed();
+                    if (ok) feed(last + kStages);
                 }
                 if (lane == 0) bar_arrive(smem_addr(&s_free[stage]));
-            } else if (ok && fed < total) feed();
+            } else if (ok && done + kStages < total) feed(done + kStages);
         }
         // ---- the item's end, or this CTA's
         const bool complete = begin == 0 && upto == count;
@@ -635,7 +680,8 @@ attend_kernel(const __grid_constant__ AttendArgs A)
                     }
             }
             __syncthreads();
-            float* join = reinterpret_cast<float*>(rings + S::kRings * kStages * S::kStage) + (warp & 1) * 8 * NT * S::kStep;
+            float* join = reinterpret_cast<float*>(rings + S::kRings * kStages * S::kStage);
+            float* mine = join + (warp & 1) * 8 * NT * S::kStep;
 #pragma unroll
             for (int x = 0; x < NT; x++)
 #pragma unroll
@@ -652,13 +698,14 @@ attend_kernel(const __grid_constant__ AttendArgs A)
 #pragma unroll
             for (int step = 2; step > 0; step >>= 1) {
                 if (warp >= step && warp < 2 * step) {
+                    float* to = step == 1 ? join : mine;
 #pragma unroll
                     for (int x = 0; x < NT; x++)
 #pragma unroll
                         for (int z = 0; z < 2; z++)
 #pragma unroll
                             for (int j = 0; j < J; j++)
-                                *reinterpret_cast<float4*>((step == 1 ? join - 8 * NT * S::kStep : join) + (8 * x + 2 * t + z) * S::kStep + 32 * j + 4 * g) =
+                                *reinterpret_cast<float4*>(to + (8 * x + 2 * t + z) * S::kStep + 32 * j + 4 * g) =
                                     make_float4(s.o[x][2 * j][z], s.o[x][2 * j][z + 2], s.o[x][2 * j + 1][z], s.o[x][2 * j + 1][z + 2]);
                 }
                 __syncthreads();
@@ -669,7 +716,7 @@ attend_kernel(const __grid_constant__ AttendArgs A)
                         for (int z = 0; z < 2; z++)
 #pragma unroll
                             for (int j = 0; j < J; j++) {
-                                const float4 v = *reinterpret_cast<const float4*>(join + (8 * x + 2 * t + z) * S::kStep + 32 * j + 4 * g);
+                                const float4 v = *reinterpret_cast<const float4*>(mine + (8 * x + 2 * t + z) * S::kStep + 32 * j + 4 * g);
                                 s.o[x][2 * j][z] += v.x; s.o[x][2 * j][z + 2] += v.y; s.o[x][2 * j + 1][z] += v.z; s.o[x][2 * j + 1][z + 2] += v.w;
                             }
                 }
@@ -704,7 +751,7 @@ attend_kernel(const __grid_constant__ AttendArgs A)
             // the CTA with the item's last unit
             const long long end = from + done - upto + count - 1, all = s_total, ctas = s_ctas;
             long long c = end * ctas / all;
-            while (all * (c + 1) / ctas <= end) c++;
+            while (share_of(all, (int)c + 1, ctas) <= end) c++;
             left = AttendNote{1, w.token, w.y * kTileRows, item_rows, w.h, (int)c, 0, 0};
         }
         if (upto == count && done < total) {
@@ -717,7 +764,7 @@ attend_kernel(const __grid_constant__ AttendArgs A)
     }
     if (feeds) {
         // (its copies end before it does, whether or not they were waited for)
-        for (int i = max(0, fed - kStages); i < fed; i++) ok &= bar_wait(smem_addr(full + i % kStages), (i / kStages) & 1);
+        for (int i = max(0, total - kStages); i < total; i++) ok &= bar_wait(smem_addr(full + i % kStages), (i / kStages) & 1);
     }
     if (!ok && lane == 0) *(volatile int*)&s_failed = 1;
     __syncthreads();
@@ -726,46 +773,78 @@ attend_kernel(const __grid_constant__ AttendArgs A)
 
 // ---------------------------------------------------------------- second kernel
 
-// Joins the pieces of the item that CTA blockIdx.x began and did not finish, a warp per query row; and says of every row whether its
-// positions and block ids are ones.
+// Joins the pieces of the item that CTA blockIdx.x began and did not finish, a query row to a warp, in the order of the tokens.  The last
+// blockIdx.y says of every row of the call whether its positions and block ids are ones.
+template <int V>                               // vectors of a query row to a lane
 __global__ void __launch_bounds__(kJoinThreads)
 attend_join_kernel(const __grid_constant__ AttendArgs A, int tile_rows, int dim)
 {
     pdl_wait();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const AttendNote* notes = reinterpret_cast<const AttendNote*>(A.ws);
-    if (blockIdx.x < A.ctas) {
+    if (blockIdx.y + 1 < gridDim.y) {
         const AttendNote note = notes[blockIdx.x];
-        if (note.valid) {
-            const float* pieces = reinterpret_cast<const float*>(A.ws + (size_t)A.ctas * sizeof(AttendNote));
-            const size_t size = piece_floats(tile_rows, dim);
-            const int count = note.last - (int)blockIdx.x + 1;
-            // piece k: of this CTA the one it began, of the k-th behind it the one it went on with
-            auto piece = [&](int k) { return pieces + (k == 0 ? 2 * (size_t)blockIdx.x + 1 : 2 * ((size_t)blockIdx.x + k)) * size; };
-            for (int i = warp; i < note.rows; i += kJoinThreads / 32) {
-                float m = -INFINITY, l = 0.f;
-                for (int k = lane; k < count; k += 32) m = fmaxf(m, piece(k)[i]);
+        const int i = blockIdx.y * kJoinWarps + warp, first = blockIdx.x;
+        if (!note.valid || i >= note.rows) return;
+        const float* pieces = reinterpret_cast<const float*>(A.ws + (size_t)A.ctas * sizeof(AttendNote));
+        const size_t size = piece_floats(tile_rows, dim);
+        const int count = note.last - first + 1;
+        // piece k: of the item's first CTA the one it began, of the k-th behind it the one it went on with
+        auto piece = [&](int k) { return pieces + (k == 0 ? 2 * (size_t)first + 1 : 2 * ((size_t)first + k)) * size; };
+        constexpr int kAhead = 8 / V;          // pieces on their way at a time
+        float4 v[kAhead][V];
+        auto load = [&](int k0) {
 #pragma unroll
-                for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-                float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-                for (int k = 0; k < count; k++) {
-                    const float* p = piece(k);
-                    const float by = p[i] == -INFINITY ? 1.f : exp2_of(p[i] - m);        // (0 or NaN throughout where p[i] is -infinity)
-                    l = fmaf(p[tile_rows + i], by, l);
+            for (int u = 0; u < kAhead; u++)
 #pragma unroll
-                    for (int z = 0; z < 8; z++) if (32 * z < dim) v[z] = fmaf(p[2 * tile_rows + i * dim + 32 * z + lane], by, v[z]);
-                }
-                const float by = l == 0.f ? 0.f : 1.f / l;
-                const long long at = out_at(A, note.token, note.row + i, note.head);
+                for (int z = 0; z < V; z++)
+                    if (k0 + u < count) v[u][z] = *reinterpret_cast<const float4*>(piece(k0 + u) + 2 * tile_rows + i * dim + min(4 * (lane + 32 * z), dim - 4));
+        };
+        load(0);
+        float m = -INFINITY, l = 0.f;
+        float4 sum[V];
 #pragma unroll
-                for (int z = 0; z < 8; z++) {
-                    if (32 * z >= dim) continue;
-                    if (A.dtype == GR_BF16) ((__nv_bfloat16*)A.out)[at + 32 * z + lane] = __float2bfloat16_rn(v[z] * by);
-                    else ((__half*)A.out)[at + 32 * z + lane] = __float2half_rn(v[z] * by);
+        for (int z = 0; z < V; z++) sum[z] = make_float4(0.f, 0.f, 0.f, 0.f);
+        // (the largest of up to 32 pieces at a time: what has been added up moves there)
+        for (int k0 = 0; k0 < count; k0 += 32) {
+            float pm = -INFINITY, pl = 0.f;
+            if (k0 + lane < count) { const float* p = piece(k0 + lane); pm = p[i]; pl = p[tile_rows + i]; }
+            float top = pm;
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+            top = fmaxf(top, m);
+            const float down = m == -INFINITY ? 1.f : exp2_of(m - top), by = pm == -INFINITY ? 1.f : exp2_of(pm - top);      // (0 or NaN throughout where m is -infinity)
+            pl *= by;
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) pl += __shfl_xor_sync(0xffffffffu, pl, o);
+            l = fmaf(l, down, pl);
+            m = top;
+#pragma unroll
+            for (int z = 0; z < V; z++) { sum[z].x *= down; sum[z].y *= down; sum[z].z *= down; sum[z].w *= down; }
+#pragma unroll 1
+            for (int k1 = k0; k1 < min(k0 + 32, count); k1 += kAhead) {
+                if (k1 > 0) load(k1);
+#pragma unroll
+                for (int u = 0; u < kAhead; u++) {
+                    const float w = __shfl_sync(0xffffffffu, by, (k1 - k0 + u) & 31);
+                    if (k1 + u >= count) continue;
+#pragma unroll
+                    for (int z = 0; z < V; z++) {
+                        sum[z].x = fmaf(v[u][z].x, w, sum[z].x); sum[z].y = fmaf(v[u][z].y, w, sum[z].y);
+                        sum[z].z = fmaf(v[u][z].z, w, sum[z].z); sum[z].w = fmaf(v[u][z].w, w, sum[z].w);
+                    }
                 }
             }
         }
+        const float by = l == 0.f ? 0.f : 1.f / l;
+        const long long at = out_at(A, note.token, note.row + i, note.head);
+#pragma unroll
+        for (int z = 0; z < V; z++) {
+            const int d = 4 * (lane + 32 * z);
+            const float o[4] = {sum[z].x * by, sum[z].y * by, sum[z].z * by, sum[z].w * by};
+            if (d < dim) store_out(A, at + d, o);
+        }
+        return;
     }
     bool failed = false;
     for (int c = tid; c < A.ctas; c += kJoinThreads) failed |= notes[c].failed != 0;
@@ -780,7 +859,9 @@ attend_join_kernel(const __grid_constant__ AttendArgs A, int tile_rows, int dim)
             bad |= end > A.most;
             const int size = 8 * A.octets, hi = (int)min(end, (long long)A.most);
             const int lo = A.window > 0 ? (int)min(max((long long)w.p0 - A.window + 1, 0ll), (long long)hi) : 0;
-            for (int b = lo / size + tid; b * (long long)size < hi; b += kJoinThreads) {
+            const int last = (hi + size - 1) / size;
+#pragma unroll 4
+            for (int b = lo / size + tid; b < last; b += kJoinThreads) {
                 const int id = A.table[(long long)r * A.width + b];
                 bad |= id < 0 || id >= A.num_blocks;
             }
@@ -884,8 +965,14 @@ int gr_cache_attend(const void* q, int dtype, int q_heads, long long q_token, lo
             if (device < gr::kMaxDevices) set[device] = true;
         }
         if (gr::launch_pdl(kernel, A.ctas, gr::kAttendThreads, S::kSmem, st, A) != cudaSuccess) return GR_E_LAUNCH;
-        if (gr::launch_pdl(gr::attend_join_kernel, A.ctas, gr::kJoinThreads, 0, st, A, S::kTileRows, L.dim) != cudaSuccess) return GR_E_LAUNCH;
-        return GR_OK;
+        cudaLaunchConfig_t cfg = {};
+        cudaLaunchAttribute at = {};
+        at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        at.val.programmaticStreamSerializationAllowed = 1;
+        cfg.gridDim = dim3((unsigned)A.ctas, 1u + (unsigned)(S::kTileRows / gr::kJoinWarps));
+        cfg.blockDim = dim3(gr::kJoinThreads); cfg.stream = st; cfg.attrs = &at; cfg.numAttrs = 1;
+        const auto join = L.dim > 128 ? &gr::attend_join_kernel<2> : &gr::attend_join_kernel<1>;
+        return cudaLaunchKernelEx(&cfg, join, A, S::kTileRows, L.dim) == cudaSuccess ? GR_OK : GR_E_LAUNCH;
     });
     if (done != GR_OK || cudaPeekAtLastError() != cudaSuccess) { cudaGetLastError(); return GR_E_LAUNCH; }
     return GR_OK;
