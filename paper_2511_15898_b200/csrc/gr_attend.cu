@@ -1,6 +1,6 @@
 // gr_cache_attend: attention of each row's last tokens over the row's tokens in a 4-bit paged cache.
 //
-//   out = sum_t p_t v_t / sum_t p_t,  p_t = 2^(x_t - m),  x_t = scale log2(e) q . k_t,  m the largest x met,
+//   out = sum_t p_t v_t / sum_t p_t,  p_t = 2^(x_t - m),  x_t = scale log2(e) q . k_t,  m a number at or a little above the largest x met,
 // in one pass over the row's octets.  Codes are whole numbers u, values s (u - 8), so with a scale per 32 dims
 //   q . k = sum_j s_j (sum_d q_d u_d - 8 sum_d q_d),     sum_t p_t v_t = sum_t (p_t s_tj) u_td - 8 sum_t p_t s_tj,
 // and the matrix instructions take the codes as they are: four bits in the low end of an fp16 number are u 2^-24, the next four 16 u 2^-24
@@ -13,7 +13,7 @@
 // Work.  A unit is 128 tokens of a (row, head, tile of query rows), or 64; the units of the call in that order are cut into equal shares, one to
 // a CTA of four warps, however ragged the rows are.  Up to 16 query rows: a warp takes 32 of a unit's tokens for all of them and brings them itself, the next ones
 // while it works on these (cp.async.bulk, an octet each, into a ring of its own).  More: all warps take the unit's 64 tokens, each for 16
-// query rows, from one ring that the first one fills.  What a CTA does not finish it leaves as (m, sum, product) in the workspace;
+// query rows, from one ring that the first one fills, as operands that each makes a quarter of.  What a CTA does not finish it leaves as (m, sum, product) in the workspace;
 // a second kernel joins the pieces in the order of the tokens, so results do not depend on which CTA was first.
 #include <math.h>
 #include <algorithm>
@@ -22,9 +22,12 @@
 
 namespace gr {
 
-constexpr int kEaters = 4;                     // warps of a CTA
-constexpr int kAttendThreads = 32 * kEaters;
+constexpr int kEaters = 4;                     // warps of a CTA that takes up to 16 query rows
+constexpr int kMostWarps = 8;                  // of one that takes more, 8 each
 constexpr int kBite = 32;                      // tokens that a warp takes at a time
+// How far above the largest x met the reference is put (p stays at or below 1): at 0 it has to follow every few tokens, a third of the work for 36
+// query rows.  p loses 4 of the 10 binary places below 2^-4 of the largest that fp16 has before its subnormal numbers.
+constexpr float kHeadroom = 4.f;
 constexpr int kJoinThreads = 256, kJoinWarps = kJoinThreads / 32;
 constexpr unsigned long long kWaitNs = 2000000000ull;      // longest wait for a copy or a free place in the ring
 
@@ -35,6 +38,7 @@ struct AttendArgs {
     const int* table; const int* offsets; const int* positions; int* status;
     int dtype, q_vec, out_vec, tokens, heads, group, octets, num_blocks, width, rows, window, most;     // octets: of a block; most: tokens that a table's row has room for
     unsigned by_octets; int shift;             // quotients by octets
+    int tile_rows;                             // query rows of an item
     float scale;                               // with log2(e)
     char* ws; int ctas;
 };
@@ -45,18 +49,20 @@ static_assert(sizeof(AttendNote) == 32, "workspace layout");
 
 template <int J, int NT, bool kRows>
 struct Shape {
-    static constexpr int D = 32 * J, kTileRows = 8 * NT * (kRows ? kEaters : 1), kOctet = octet_bytes(D);
+    static constexpr int D = 32 * J, kOctet = octet_bytes(D), kWarps = kRows ? kMostWarps : kEaters;
     static constexpr int kTile = kRows ? 64 : kBite * kEaters;             // tokens of a unit
     static constexpr int kStage = (kRows ? kTile : kBite) / 8 * kOctet;    // bytes of a place in a ring
     static constexpr int kRings = kRows ? 1 : kEaters;
     static constexpr int kStep = D + 4;        // floats from one row of the joined results to the next: threads of a quarter warp meet all banks
     static constexpr int kJoin = kRows ? 0 : 2 * 8 * NT * kStep * 4;
-    // resident CTAs per SM, by registers: 128, 168 or 255 a thread
-    static constexpr int kCtas = NT == 1 ? (J <= 4 ? 4 : J <= 6 ? 3 : 2) : (J <= 1 ? 4 : J <= 3 ? 3 : 2);
-    static constexpr int kRoom = 227 * 1024 / kCtas - 2048 - kJoin;
-    static constexpr int kStages = kRoom / (kRings * kStage) < 4 ? kRoom / (kRings * kStage) : 4;
-    static constexpr int kSmem = kStages * kRings * kStage + kJoin;
-    static_assert(kStages >= 2, "a ring");
+    static constexpr int kOperands = kRows ? kTile / 16 * J * 2 * 1024 : 0;  // a unit's keys and values as operands
+    // resident CTAs per SM, by registers (128, 168 or 255 a thread); of many query rows as many as there is room for
+    static constexpr int kCtas = kRows ? (J <= 4 ? 2 : 1) : NT == 1 ? (J <= 4 ? 4 : J <= 6 ? 3 : 2) : (J <= 1 ? 4 : J <= 3 ? 3 : 2);
+    static constexpr int kRoom = 227 * 1024 / kCtas - 2560 - kJoin - kOperands;
+    static constexpr int kStages = kRows ? 2 : kRoom / (kRings * kStage) < 4 ? kRoom / (kRings * kStage) : 4;
+    static constexpr int kSmem = kStages * kRings * kStage + kJoin + kOperands;
+    static_assert(kStages >= 2 && kRoom >= kStages * kRings * kStage, "a ring");
+    static int ctas(int warps) { return kRows ? std::max(1, std::min((J <= 4 ? 16 : 8) / warps, 227 * 1024 / (kSmem + 2560))) : kCtas; }
 };
 constexpr int kMaxStages = 4;
 __host__ __device__ inline size_t piece_floats(int tile_rows, int dim) { return (size_t)tile_rows * (dim + 2); }
@@ -160,10 +166,10 @@ __device__ __forceinline__ void walk_row(Walk& w, const AttendArgs& A)
     w.n = min(max(A.offsets[w.r + 1], w.token), A.tokens) - w.token;
     w.p0 = w.n > 0 ? A.positions[w.token] : -1;
 }
-template <int kTileRows, int kTile>
+template <int kTile>
 __device__ __forceinline__ void walk_item(Walk& w, const AttendArgs& A)
 {
-    const int first = w.y * kTileRows / A.group, last = (min(w.n * A.group, (w.y + 1) * kTileRows) - 1) / A.group;
+    const int first = w.y * A.tile_rows / A.group, last = (min(w.n * A.group, (w.y + 1) * A.tile_rows) - 1) / A.group;
     w.hi = w.p0 < 0 ? 0 : (int)min((long long)w.p0 + last + 1, (long long)A.most);
     w.lo = A.window > 0 ? (int)max((long long)w.p0 + first - A.window + 1, 0ll) : 0;
     w.lo = min(w.lo, w.hi);
@@ -171,25 +177,25 @@ __device__ __forceinline__ void walk_item(Walk& w, const AttendArgs& A)
     w.count = w.hi > w.lo ? (w.hi + kTile - 1) / kTile - w.first : 1;        // (a row that sees nothing: a unit of nothing, which writes its zeros)
 }
 // units of a head of row w.r
-template <int kTileRows, int kTile>
+template <int kTile>
 __device__ __forceinline__ int row_units(Walk& w, const AttendArgs& A)
 {
     int sum = 0;
-    for (w.y = 0; w.y * kTileRows < w.n * A.group; w.y++) { walk_item<kTileRows, kTile>(w, A); sum += w.count; }
+    for (w.y = 0; w.y * A.tile_rows < w.n * A.group; w.y++) { walk_item<kTile>(w, A); sum += w.count; }
     return sum;
 }
-template <int kTileRows, int kTile>
+template <int kTile>
 __device__ __forceinline__ void walk_next(Walk& w, const AttendArgs& A)
 {
     w.at = 0;
-    if (++w.y * kTileRows >= w.n * A.group) {
+    if (++w.y * A.tile_rows >= w.n * A.group) {
         w.y = 0;
         if (++w.h == A.heads) {
             w.h = 0;
             do { if (++w.r >= A.rows) return; walk_row(w, A); } while (w.n == 0);
         }
     }
-    walk_item<kTileRows, kTile>(w, A);
+    walk_item<kTile>(w, A);
 }
 
 // where share i of `parts` of the units begins (32 bits divide in a fraction of the time)
@@ -205,7 +211,7 @@ struct State {
     uint4 q[NT][J];                            // the queries as operands, scaled
     unsigned sum[NT][(J + 3) / 4];             // -8 2^-24 times the queries' sums by groups, in two fp16 parts, as operands (group t, t + 4)
     float f[NT][2];                            // from products to x, positive
-    float m[NT][2], ref[NT][2], l[NT][2];      // m: the largest product; ref: its x, or 0 where there is none
+    float m[NT][2], ref[NT][2], l[NT][2];      // m: no product is above it; ref: its x, or 0 where there is none
     float o[NT][2 * J][4], off[NT][4];
 };
 
@@ -273,10 +279,31 @@ __device__ __forceinline__ void load_queries(State<J, NT>& s, const AttendArgs& 
     }
 }
 
+// Operands out of two octets' words: of keys rows are tokens, four dims of eight to a step; of values rows are dims.
+__device__ __forceinline__ uint4 key_operand(unsigned w0, unsigned w1) { return make_uint4(w0 & 0x000f000fu, w1 & 0x000f000fu, w0 & 0x00f000f0u, w1 & 0x00f000f0u); }
+__device__ __forceinline__ uint4 value_operand(unsigned w0, unsigned w1) { return make_uint4(w0 & 0x000f000fu, w0 & 0x00f000f0u, w1 & 0x000f000fu, w1 & 0x00f000f0u); }
+
+// 16 tokens' keys or values as operands: to[J][2][32 lanes]
+template <int J>
+__device__ __forceinline__ void make_operands(uint4* to, const char* at, bool values, int lane)
+{
+    constexpr int D = 32 * J, kOctet = octet_bytes(D);
+    unsigned w0[J], w1[J];
+    at += (values ? octet_vcode(D) : 0) + 4 * J * lane;
+    load_words<J>(w0, at);
+    load_words<J>(w1, at + kOctet);
+#pragma unroll
+    for (int j = 0; j < J; j++) {
+        to[2 * j * 32 + lane] = values ? value_operand(w0[j], w1[j]) : key_operand(w0[j], w1[j]);
+        to[(2 * j + 1) * 32 + lane] = values ? value_operand(w0[j] >> 8, w1[j] >> 8) : key_operand(w0[j] >> 8, w1[j] >> 8);
+    }
+}
+
 // 32 tokens from `token` on, four octets at `at`.  kAll: every query row sees them all.  Else `have` says which of the octets
 // are there, and each query row's own range which of the tokens it sees; what it does not see stays out whatever is held there.
-template <int J, int NT, bool kAll>
-__device__ __forceinline__ void eat(State<J, NT>& s, const char* at, int lane, const AttendArgs& A, const Walk& w, int row, int token, unsigned have)
+// kReady: `ready` holds the two halves' keys and values as operands (else they are made here).
+template <int J, int NT, bool kAll, bool kReady>
+__device__ __forceinline__ void eat(State<J, NT>& s, const uint4* ready, const char* at, int lane, const AttendArgs& A, const Walk& w, int row, int token, unsigned have)
 {
     constexpr int D = 32 * J, kOctet = octet_bytes(D);
     const int g = lane >> 2, t = lane & 3;
@@ -297,31 +324,27 @@ __device__ __forceinline__ void eat(State<J, NT>& s, const char* at, int lane, c
                 }
             }
         }
-        constexpr int kAtOnce = 1;
 #pragma unroll
-        for (int b0 = 0; b0 < 2; b0 += kAtOnce) {
-            unsigned k[kAtOnce][2][J], sc[kAtOnce][2][(J + 1) / 2];
+        for (int b = 0; b < 2; b++) {
+            unsigned k[2][J], sc[2][(J + 1) / 2];
 #pragma unroll
-            for (int b = 0; b < kAtOnce; b++)
-#pragma unroll
-                for (int o = 0; o < 2; o++) {
-                    const char* from = at + (2 * (b0 + b) + o) * kOctet;
-                    load_words<J>(k[b][o], from + 4 * J * lane);
-                    load_halves<J>(sc[b][o], from + octet_kscale(D) + 2 * J * g);
-                }
+            for (int o = 0; o < 2; o++) {
+                const char* from = at + (2 * b + o) * kOctet;
+                if (!kReady) load_words<J>(k[o], from + 4 * J * lane);
+                load_halves<J>(sc[o], from + octet_kscale(D) + 2 * J * g);
+            }
 #pragma unroll
             for (int j = 0; j < J; j++) {
+                const float c = half_of(sc[0], j), e = half_of(sc[1], j);
+                uint4 a0, a1;
+                if (kReady) { a0 = ready[((b * 2 * J + j) * 2) * 32 + lane]; a1 = ready[((b * 2 * J + j) * 2 + 1) * 32 + lane]; }
+                else { a0 = key_operand(k[0][j], k[1][j]); a1 = key_operand(k[0][j] >> 8, k[1][j] >> 8); }
 #pragma unroll
-                for (int b = 0; b < kAtOnce; b++) {
-                    const float c = half_of(sc[b][0], j), e = half_of(sc[b][1], j);
-                    const unsigned w0 = k[b][0][j], w1 = k[b][1][j], u0 = w0 >> 8, u1 = w1 >> 8;
-#pragma unroll
-                    for (int n = 0; n < NT; n++) {
-                        float d[4], (&y)[4] = x[n][b0 + b];
-                        mma(d, w0 & 0x000f000fu, w1 & 0x000f000fu, w0 & 0x00f000f0u, w1 & 0x00f000f0u, s.q[n][j].x, s.q[n][j].y, 0.f, 0.f, 0.f, 0.f);
-                        mma(d, u0 & 0x000f000fu, u1 & 0x000f000fu, u0 & 0x00f000f0u, u1 & 0x00f000f0u, s.q[n][j].z, s.q[n][j].w);
-                        y[0] = fmaf(c, d[0], y[0]); y[1] = fmaf(c, d[1], y[1]); y[2] = fmaf(e, d[2], y[2]); y[3] = fmaf(e, d[3], y[3]);
-                    }
+                for (int n = 0; n < NT; n++) {
+                    float d[4], (&y)[4] = x[n][b];
+                    mma(d, a0.x, a0.y, a0.z, a0.w, s.q[n][j].x, s.q[n][j].y, 0.f, 0.f, 0.f, 0.f);
+                    mma(d, a1.x, a1.y, a1.z, a1.w, s.q[n][j].z, s.q[n][j].w);
+                    y[0] = fmaf(c, d[0], y[0]); y[1] = fmaf(c, d[1], y[1]); y[2] = fmaf(e, d[2], y[2]); y[3] = fmaf(e, d[3], y[3]);
                 }
             }
         }
@@ -346,7 +369,7 @@ __device__ __forceinline__ void eat(State<J, NT>& s, const char* at, int lane, c
                 || fmaxf(fmaxf(x[n][0][1], x[n][0][3]), fmaxf(x[n][1][1], x[n][1][3])) > s.m[n][1];
     }
     if (__any_sync(0xffffffffu, more)) {
-        // the largest product has grown: what has been added up moves to the new one
+        // a product is above the reference: that moves above it, by some more, and what has been added up moves along
 #pragma unroll
         for (int n = 0; n < NT; n++) {
             float by[2];
@@ -355,7 +378,7 @@ __device__ __forceinline__ void eat(State<J, NT>& s, const char* at, int lane, c
                 float m = fmaxf(fmaxf(x[n][0][z], x[n][0][z + 2]), fmaxf(x[n][1][z], x[n][1][z + 2]));
 #pragma unroll
                 for (int o = 4; o < 32; o *= 2) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-                m = fmaxf(m, s.m[n][z]);
+                m = m > s.m[n][z] ? m + kHeadroom / s.f[n][z] : s.m[n][z];
                 const float ref = m == -INFINITY ? 0.f : m * s.f[n][z];
                 by[z] = s.m[n][z] == -INFINITY ? 1.f : exp2_of(s.ref[n][z] - ref);       // (nothing has been added up)
                 s.m[n][z] = m;
@@ -390,8 +413,10 @@ __device__ __forceinline__ void eat(State<J, NT>& s, const char* at, int lane, c
         const char* v = at + 2 * b * kOctet + octet_vcode(D);
         const char* sc = at + 2 * b * kOctet + octet_vscale(D);
         unsigned v0[J], v1[J], z0[J], z1[J];
-        load_words<J>(v0, v + 4 * J * lane);
-        load_words<J>(v1, v + kOctet + 4 * J * lane);
+        if (!kReady) {
+            load_words<J>(v0, v + 4 * J * lane);
+            load_words<J>(v1, v + kOctet + 4 * J * lane);
+        }
         load_words<J>(z0, sc + 4 * J * t);
         load_words<J>(z1, sc + kOctet + 4 * J * t);
         if (kAll) {
@@ -402,7 +427,9 @@ __device__ __forceinline__ void eat(State<J, NT>& s, const char* at, int lane, c
         }
 #pragma unroll
         for (int j = 0; j < J; j++) {
-            const unsigned u0 = v0[j] >> 8, u1 = v1[j] >> 8;
+            uint4 a0, a1;
+            if (kReady) { a0 = ready[((b * 2 * J + J + j) * 2) * 32 + lane]; a1 = ready[((b * 2 * J + J + j) * 2 + 1) * 32 + lane]; }
+            else { a0 = value_operand(v0[j], v1[j]); a1 = value_operand(v0[j] >> 8, v1[j] >> 8); }
 #pragma unroll
             for (int n = 0; n < NT; n++) {
                 unsigned b0 = mul_h2(p[n][b][0], z0[j]), b1 = mul_h2(p[n][b][1], z1[j]);
@@ -413,8 +440,8 @@ __device__ __forceinline__ void eat(State<J, NT>& s, const char* at, int lane, c
                     const unsigned one = g == j ? 0x3c003c00u : 0u;
                     mma(s.off[n], one, 0u, one, 0u, b0, b1);
                 }
-                mma(s.o[n][2 * j], v0[j] & 0x000f000fu, v0[j] & 0x00f000f0u, v1[j] & 0x000f000fu, v1[j] & 0x00f000f0u, b0, b1);
-                mma(s.o[n][2 * j + 1], u0 & 0x000f000fu, u0 & 0x00f000f0u, u1 & 0x000f000fu, u1 & 0x00f000f0u, b0, b1);
+                mma(s.o[n][2 * j], a0.x, a0.y, a0.z, a0.w, b0, b1);
+                mma(s.o[n][2 * j + 1], a1.x, a1.y, a1.z, a1.w, b0, b1);
             }
         }
     }
@@ -524,38 +551,36 @@ struct Feeder {
 };
 
 template <int J, int NT, bool kRows>
-__global__ void __launch_bounds__(kAttendThreads, Shape<J, NT, kRows>::kCtas)
+__global__ void __launch_bounds__(32 * Shape<J, NT, kRows>::kWarps, Shape<J, NT, kRows>::kCtas)
 attend_kernel(const __grid_constant__ AttendArgs A)
 {
     using S = Shape<J, NT, kRows>;
-    constexpr int D = S::D, kTileRows = S::kTileRows, kStages = S::kStages, kTile = S::kTile;
+    constexpr int D = S::D, kStages = S::kStages, kTile = S::kTile, kWarps = S::kWarps;
+    const int tile_rows = A.tile_rows, warps = kRows ? blockDim.x >> 5 : kEaters, threads = 32 * warps;
     extern __shared__ __align__(128) char rings[];
-    __shared__ __align__(8) unsigned long long s_full[S::kRings][kMaxStages], s_free[kMaxStages];
+    __shared__ __align__(8) unsigned long long s_full[S::kRings][kMaxStages];
     __shared__ unsigned s_have[S::kRings][kMaxStages];
     __shared__ float s_m[kEaters][8 * NT], s_l[kEaters][8 * NT];
-    __shared__ long long s_scan[kEaters], s_from, s_to, s_total, s_ctas;
-    __shared__ Walk s_eat[kEaters], s_feed[kEaters];       // each warp's own
-    __shared__ FeedItem s_item[kEaters];
+    __shared__ long long s_scan[kWarps], s_from, s_to, s_total, s_ctas;
+    __shared__ Walk s_eat[kWarps], s_feed[kWarps];         // each warp's own
+    __shared__ FeedItem s_item[kWarps];
     __shared__ int s_failed;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     if (tid == 0) {
-        for (int i = 0; i < kStages; i++) {
-            for (int r = 0; r < S::kRings; r++) bar_init(smem_addr(&s_full[r][i]), 1);
-            bar_init(smem_addr(&s_free[i]), kEaters);
-        }
+        for (int i = 0; i < kStages; i++) for (int r = 0; r < S::kRings; r++) bar_init(smem_addr(&s_full[r][i]), 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         s_failed = 0;
     }
     pdl_wait();
     // ---- this CTA's share of the units
     {
-        const int per = (A.rows + kAttendThreads - 1) / kAttendThreads;
+        const int per = (A.rows + threads - 1) / threads;
         long long mine = 0;
         Walk w;
         for (int r = tid * per; r < min((tid + 1) * per, A.rows); r++) {
             w.r = r;
             walk_row(w, A);
-            mine += (long long)row_units<kTileRows, kTile>(w, A) * A.heads;
+            mine += (long long)row_units<kTile>(w, A) * A.heads;
         }
         long long upto = mine;
 #pragma unroll
@@ -564,7 +589,7 @@ attend_kernel(const __grid_constant__ AttendArgs A)
         __syncthreads();
         long long total = 0;
 #pragma unroll
-        for (int i = 0; i < kEaters; i++) { if (i < warp) upto += s_scan[i]; total += s_scan[i]; }
+        for (int i = 0; i < kWarps; i++) if (i < warps) { if (i < warp) upto += s_scan[i]; total += s_scan[i]; }
         const long long ctas = min((long long)A.ctas, total);
         const bool works = blockIdx.x < ctas;
         const long long from = works ? share_of(total, blockIdx.x, ctas) : 0, to = works ? share_of(total, blockIdx.x + 1, ctas) : 0;
@@ -575,12 +600,12 @@ attend_kernel(const __grid_constant__ AttendArgs A)
             for (int r = tid * per;; r++) {
                 w.r = r;
                 walk_row(w, A);
-                const int units = row_units<kTileRows, kTile>(w, A);
+                const int units = row_units<kTile>(w, A);
                 if (left >= (long long)units * A.heads) { left -= (long long)units * A.heads; continue; }
                 w.h = (int)(left / units);
                 left -= (long long)w.h * units;
                 for (w.y = 0;; w.y++) {
-                    walk_item<kTileRows, kTile>(w, A);
+                    walk_item<kTile>(w, A);
                     if (left < w.count) break;
                     left -= w.count;
                 }
@@ -588,7 +613,7 @@ attend_kernel(const __grid_constant__ AttendArgs A)
                 break;
             }
 #pragma unroll
-            for (int i = 0; i < kEaters; i++) { s_eat[i] = w; s_feed[i] = w; }
+            for (int i = 0; i < kWarps; i++) { s_eat[i] = w; s_feed[i] = w; }
         }
     }
     __syncthreads();
@@ -613,7 +638,7 @@ attend_kernel(const __grid_constant__ AttendArgs A)
         if (end) {
             Walk w = s_feed[warp];
             __syncwarp();
-            walk_next<kTileRows, kTile>(w, A);
+            walk_next<kTile>(w, A);
             if (lane == 0) s_feed[warp] = w;
             feeder.begin(s_item[warp], A, w, total - next - 1, kRows ? 0 : kBite * warp, lane);
         } else feeder.look(s_item[warp], A, lane);
@@ -629,43 +654,48 @@ attend_kernel(const __grid_constant__ AttendArgs A)
     const Walk& w = s_eat[warp];
     int done = 0;
     while (done < total) {
-        const int row = w.y * kTileRows + (kRows ? warp * 8 * NT : 0);         // this warp's first query row
+        const int row = w.y * tile_rows + (kRows ? warp * 8 * NT : 0);         // this warp's first query row
         load_queries<J, NT>(s, A, w, row, lane);
-        const int item_rows = min(kTileRows, w.n * A.group - w.y * kTileRows), last_row = w.y * kTileRows + item_rows - 1;
+        const int item_rows = min(tile_rows, w.n * A.group - w.y * tile_rows), last_row = w.y * tile_rows + item_rows - 1;
         const bool idle = kRows && row > last_row;
         // tokens that all of the item's query rows see
-        const int all_hi = w.p0 < 0 ? 0 : (int)min((long long)w.p0 + w.y * kTileRows / A.group + 1, (long long)A.most);
+        const int all_hi = w.p0 < 0 ? 0 : (int)min((long long)w.p0 + w.y * tile_rows / A.group + 1, (long long)A.most);
         const int all_lo = A.window > 0 ? (int)min(max((long long)w.p0 + last_row / A.group - A.window + 1, 0ll), (long long)A.most) : 0;
         const int begin = w.at, count = w.count, upto = min(count, begin + total - done);
         int token = (w.first + begin) * kTile + (kRows ? 0 : kBite * warp);
         for (int at = begin; at < upto; at++, done++, token += kTile) {
             const int stage = done % kStages;
             if (ok) ok = __all_sync(0xffffffffu, bar_wait(smem_addr(full + stage), (done / kStages) & 1));
-            if (ok && !idle) {
-                const unsigned have = held[stage];
-                const char* octets = ring + stage * S::kStage;
-#pragma unroll 1
-                for (int b = 0; b < (kRows ? kTile / kBite : 1); b++) {
-                    const unsigned four = have >> (4 * b) & 15;
-                    if (four == 15 && token + kBite * b >= all_lo && token + kBite * (b + 1) <= all_hi)
-                        eat<J, NT, true>(s, octets + 4 * b * S::kOctet, lane, A, w, row, token + kBite * b, four);
-                    else if (four) eat<J, NT, false>(s, octets + 4 * b * S::kOctet, lane, A, w, row, token + kBite * b, four);
-                }
-            }
-            __syncwarp();
+            const unsigned have = ok ? held[stage] : 0u;
+            const char* octets = ring + stage * S::kStage;
             if (kRows) {
-                // (the ring's places are filled again a unit late: by then all warps are mostly done with them)
-                if (feeds && ok && done > 0 && done - 1 + kStages < total) {
-                    const int last = done - 1;
-                    ok = __all_sync(0xffffffffu, bar_wait(smem_addr(&s_free[last % kStages]), (last / kStages) & 1));
-                    if (ok) feed(last + kStages);
+                // the warps make the operands together, then all take all of them
+                // (of octets that are not there too: whatever the codes are they are numbers, and 0 times them is 0)
+                uint4* ready = reinterpret_cast<uint4*>(rings + S::kRings * kStages * S::kStage + S::kJoin);
+                for (int i = warp; i < kTile / 8; i += warps) make_operands<J>(ready + i * J * 64, octets + (i & ~1) * S::kOctet, i & 1, lane);
+                __syncthreads();
+                if (!idle) {
+#pragma unroll 1
+                    for (int b = 0; b < kTile / kBite; b++) {
+                        const unsigned four = have >> (4 * b) & 15;
+                        const uint4* from = ready + b * J * 256;
+                        if (four == 15 && token + kBite * b >= all_lo && token + kBite * (b + 1) <= all_hi)
+                            eat<J, NT, true, true>(s, from, octets + 4 * b * S::kOctet, lane, A, w, row, token + kBite * b, four);
+                        else if (four) eat<J, NT, false, true>(s, from, octets + 4 * b * S::kOctet, lane, A, w, row, token + kBite * b, four);
+                    }
                 }
-                if (lane == 0) bar_arrive(smem_addr(&s_free[stage]));
-            } else if (ok && done + kStages < total) feed(done + kStages);
+                __syncthreads();
+                if (feeds && ok && done + kStages < total) feed(done + kStages);
+            } else {
+                if (have == 15 && token >= all_lo && token + kBite <= all_hi) eat<J, NT, true, false>(s, nullptr, octets, lane, A, w, row, token, have);
+                else if (have) eat<J, NT, false, false>(s, nullptr, octets, lane, A, w, row, token, have);
+                __syncwarp();
+                if (ok && done + kStages < total) feed(done + kStages);
+            }
         }
         // ---- the item's end, or this CTA's
         const bool complete = begin == 0 && upto == count;
-        float* piece = pieces + (2 * (size_t)blockIdx.x + (begin == 0 ? 1 : 0)) * piece_floats(kTileRows, D);
+        float* piece = pieces + (2 * (size_t)blockIdx.x + (begin == 0 ? 1 : 0)) * piece_floats(tile_rows, D);
         const int g = lane >> 2, t = lane & 3;
         results<J, NT>(s, lane);
         if (!kRows) {
@@ -731,15 +761,15 @@ attend_kernel(const __grid_constant__ AttendArgs A)
                     const int i = (kRows ? warp * 8 * NT : 0) + 8 * x + 2 * t + z;
                     if (i >= item_rows) continue;
                     if (!complete) {
-                        if (g == 0) { piece[i] = kRows && s.m[x][z] != -INFINITY ? s.ref[x][z] : s.m[x][z]; piece[kTileRows + i] = s.l[x][z]; }
+                        if (g == 0) { piece[i] = kRows && s.m[x][z] != -INFINITY ? s.ref[x][z] : s.m[x][z]; piece[tile_rows + i] = s.l[x][z]; }
 #pragma unroll
                         for (int j = 0; j < J; j++)
-                            *reinterpret_cast<float4*>(piece + 2 * kTileRows + i * D + 32 * j + 4 * g) =
+                            *reinterpret_cast<float4*>(piece + 2 * tile_rows + i * D + 32 * j + 4 * g) =
                                 make_float4(s.o[x][2 * j][z], s.o[x][2 * j][z + 2], s.o[x][2 * j + 1][z], s.o[x][2 * j + 1][z + 2]);
                         continue;
                     }
                     const float by = s.l[x][z] == 0.f ? 0.f : 1.f / s.l[x][z];
-                    const long long to = out_at(A, w.token, w.y * kTileRows + i, w.h) + 4 * g;
+                    const long long to = out_at(A, w.token, w.y * tile_rows + i, w.h) + 4 * g;
 #pragma unroll
                     for (int j = 0; j < J; j++) {
                         const float v[4] = {s.o[x][2 * j][z] * by, s.o[x][2 * j][z + 2] * by, s.o[x][2 * j + 1][z] * by, s.o[x][2 * j + 1][z + 2] * by};
@@ -752,12 +782,12 @@ attend_kernel(const __grid_constant__ AttendArgs A)
             const long long end = from + done - upto + count - 1, all = s_total, ctas = s_ctas;
             long long c = end * ctas / all;
             while (share_of(all, (int)c + 1, ctas) <= end) c++;
-            left = AttendNote{1, w.token, w.y * kTileRows, item_rows, w.h, (int)c, 0, 0};
+            left = AttendNote{1, w.token, w.y * tile_rows, item_rows, w.h, (int)c, 0, 0};
         }
         if (upto == count && done < total) {
             Walk next = w;
             __syncwarp();
-            walk_next<kTileRows, kTile>(next, A);
+            walk_next<kTile>(next, A);
             if (lane == 0) s_eat[warp] = next;
             __syncwarp();
         }
@@ -874,18 +904,18 @@ attend_join_kernel(const __grid_constant__ AttendArgs A, int tile_rows, int dim)
 // ---------------------------------------------------------------- host
 
 // The kernel for a call: whether a key head's query rows (a row's tokens times its group, on average) fill more than 8 of the products' columns, more than 16.
-struct Choice { int nt; bool rows; };
+struct Choice { int nt; bool rows; int warps; };
 static Choice choose(int dim, int group, int rows, int tokens)
 {
     const double each = (double)tokens / std::max(1, rows) * group;
-    if (dim > 128) return {1, each > 8};
-    return {each > 8 ? 2 : 1, each > 16};
+    if (each > 16 || (dim > 128 && each > 8)) return {1, true, std::max(2, std::min(kMostWarps, (int)std::min((each + 7) / 8, 100.0)))};
+    return {each > 8 ? 2 : 1, false, kEaters};
 }
 template <int J, int NT, bool kRows> struct Pick { using S = Shape<J, NT, kRows>; };
 template <class F>
 static auto with_shape(int dim, Choice c, F f)
 {
-#define GR_ATTEND_J(J) case J: if (c.rows) return f(Pick<J, J <= 4 ? 2 : 1, true>()); if (c.nt == 2) return f(Pick<J, J <= 4 ? 2 : 1, false>()); return f(Pick<J, 1, false>());
+#define GR_ATTEND_J(J) case J: if (c.rows) return f(Pick<J, 1, true>()); if (c.nt == 2) return f(Pick<J, J <= 4 ? 2 : 1, false>()); return f(Pick<J, 1, false>());
     switch (dim / 32) {
         GR_ATTEND_J(1) GR_ATTEND_J(2) GR_ATTEND_J(3) GR_ATTEND_J(4) GR_ATTEND_J(5) GR_ATTEND_J(6) GR_ATTEND_J(7)
         default: if (c.rows) return f(Pick<8, 1, true>()); return f(Pick<8, 1, false>());
@@ -907,10 +937,10 @@ extern "C" {
 size_t gr_attend_workspace_bytes(int heads, int q_heads, int dim, int rows, int tokens)
 {
     if (!gr::attend_shape_ok(heads, q_heads, dim, rows, tokens)) return 0;
-    return gr::with_shape(dim, gr::choose(dim, q_heads / heads, rows, tokens), [&](auto pick) {
-        using S = typename decltype(pick)::S;
-        const size_t ctas = (size_t)gr::kSms * S::kCtas;
-        return ctas * (sizeof(gr::AttendNote) + 2 * sizeof(float) * gr::piece_floats(S::kTileRows, dim));
+    const gr::Choice c = gr::choose(dim, q_heads / heads, rows, tokens);
+    return gr::with_shape(dim, c, [&](auto pick) {
+        const size_t ctas = (size_t)gr::kSms * decltype(pick)::S::ctas(c.warps);
+        return ctas * (sizeof(gr::AttendNote) + 2 * sizeof(float) * gr::piece_floats(c.rows ? 8 * c.warps : 8 * c.nt, dim));
     });
 }
 
@@ -953,9 +983,11 @@ int gr_cache_attend(const void* q, int dtype, int q_heads, long long q_token, lo
     A.q_vec = in.bits % 16 == 0; A.out_vec = to.bits % 8 == 0;
     cudaStream_t st = (cudaStream_t)stream;
     gr::NvtxRange whole("gr_cache_attend");
-    const int done = gr::with_shape(L.dim, gr::choose(L.dim, A.group, rows, tokens), [&](auto pick) {
+    const gr::Choice c = gr::choose(L.dim, A.group, rows, tokens);
+    A.tile_rows = c.rows ? 8 * c.warps : 8 * c.nt;
+    const int done = gr::with_shape(L.dim, c, [&](auto pick) {
         using S = typename decltype(pick)::S;
-        A.ctas = gr::kSms * S::kCtas;
+        A.ctas = gr::kSms * S::ctas(c.warps);
         const auto kernel = gr::attend_of(pick);
         static bool set[gr::kMaxDevices] = {};
         int device = 0;
@@ -964,15 +996,15 @@ int gr_cache_attend(const void* q, int dtype, int q_heads, long long q_token, lo
             if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem) != cudaSuccess) return GR_E_LAUNCH;
             if (device < gr::kMaxDevices) set[device] = true;
         }
-        if (gr::launch_pdl(kernel, A.ctas, gr::kAttendThreads, S::kSmem, st, A) != cudaSuccess) return GR_E_LAUNCH;
+        if (gr::launch_pdl(kernel, A.ctas, 32 * c.warps, S::kSmem, st, A) != cudaSuccess) return GR_E_LAUNCH;
         cudaLaunchConfig_t cfg = {};
         cudaLaunchAttribute at = {};
         at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
         at.val.programmaticStreamSerializationAllowed = 1;
-        cfg.gridDim = dim3((unsigned)A.ctas, 1u + (unsigned)(S::kTileRows / gr::kJoinWarps));
+        cfg.gridDim = dim3((unsigned)A.ctas, 1u + (unsigned)((A.tile_rows + gr::kJoinWarps - 1) / gr::kJoinWarps));
         cfg.blockDim = dim3(gr::kJoinThreads); cfg.stream = st; cfg.attrs = &at; cfg.numAttrs = 1;
         const auto join = L.dim > 128 ? &gr::attend_join_kernel<2> : &gr::attend_join_kernel<1>;
-        return cudaLaunchKernelEx(&cfg, join, A, S::kTileRows, L.dim) == cudaSuccess ? GR_OK : GR_E_LAUNCH;
+        return cudaLaunchKernelEx(&cfg, join, A, A.tile_rows, L.dim) == cudaSuccess ? GR_OK : GR_E_LAUNCH;
     });
     if (done != GR_OK || cudaPeekAtLastError() != cudaSuccess) { cudaGetLastError(); return GR_E_LAUNCH; }
     return GR_OK;
