@@ -803,9 +803,10 @@ attend_kernel(const __grid_constant__ AttendArgs A)
 
 // ---------------------------------------------------------------- second kernel
 
-// Joins the pieces of the item that CTA blockIdx.x began and did not finish, a query row to a warp, in the order of the tokens.  The last
+// Joins the pieces of the item that CTA blockIdx.x began and did not finish, a query row to a warp, in the order of the tokens.  kWide, where
+// there are few items of many pieces: of the blockIdx.x-th such item, query row blockIdx.y, every eighth piece to a warp.  The last
 // blockIdx.y says of every row of the call whether its positions and block ids are ones.
-template <int V>                               // vectors of a query row to a lane
+template <int V, bool kWide>                   // V: vectors of a query row to a lane
 __global__ void __launch_bounds__(kJoinThreads)
 attend_join_kernel(const __grid_constant__ AttendArgs A, int tile_rows, int dim)
 {
@@ -813,14 +814,35 @@ attend_join_kernel(const __grid_constant__ AttendArgs A, int tile_rows, int dim)
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const AttendNote* notes = reinterpret_cast<const AttendNote*>(A.ws);
     if (blockIdx.y + 1 < gridDim.y) {
-        const AttendNote note = notes[blockIdx.x];
-        const int i = blockIdx.y * kJoinWarps + warp, first = blockIdx.x;
+        __shared__ int s_first, s_count[kJoinWarps];
+        __shared__ float4 s_sum[kWide ? kJoinWarps : 1][kWide ? 32 * V : 1];
+        int first = blockIdx.x;
+        if (kWide) {
+            // the blockIdx.x-th of the CTAs that began an item and did not finish it
+            if (tid == 0) s_first = -1;
+            int before = 0;
+            for (int c0 = 0; c0 < A.ctas; c0 += kJoinThreads) {
+                const int c = c0 + tid;
+                const bool valid = c < A.ctas && notes[c].valid;
+                const unsigned mask = __ballot_sync(0xffffffffu, valid);
+                if (lane == 0) s_count[warp] = __popc(mask);
+                __syncthreads();
+                int at = before + __popc(mask & ((1u << lane) - 1u));
+                for (int k = 0; k < kJoinWarps; k++) { if (k < warp) at += s_count[k]; before += s_count[k]; }
+                if (valid && at == (int)blockIdx.x) s_first = c;
+                __syncthreads();
+            }
+            first = s_first;
+            if (first < 0) return;
+        }
+        const AttendNote note = notes[first];
+        const int i = kWide ? (int)blockIdx.y : (int)blockIdx.y * kJoinWarps + warp;
         if (!note.valid || i >= note.rows) return;
         const float* pieces = reinterpret_cast<const float*>(A.ws + (size_t)A.ctas * sizeof(AttendNote));
         const size_t size = piece_floats(tile_rows, dim);
-        const int count = note.last - first + 1;
-        // piece k: of the item's first CTA the one it began, of the k-th behind it the one it went on with
-        auto piece = [&](int k) { return pieces + (k == 0 ? 2 * (size_t)first + 1 : 2 * ((size_t)first + k)) * size; };
+        const int all = note.last - first + 1, member = kWide ? warp : 0, every = kWide ? kJoinWarps : 1, count = (all - member + every - 1) / every;
+        // (of the k-th of this warp's:) of the item's first CTA the one it began, of the k-th behind it the one it went on with
+        auto piece = [&](int n) { const int k = member + n * every; return pieces + (k == 0 ? 2 * (size_t)first + 1 : 2 * ((size_t)first + k)) * size; };
         constexpr int kAhead = 8 / V;          // pieces on their way at a time
         float4 v[kAhead][V];
         auto load = [&](int k0) {
@@ -863,6 +885,29 @@ attend_join_kernel(const __grid_constant__ AttendArgs A, int tile_rows, int dim)
                         sum[z].x = fmaf(v[u][z].x, w, sum[z].x); sum[z].y = fmaf(v[u][z].y, w, sum[z].y);
                         sum[z].z = fmaf(v[u][z].z, w, sum[z].z); sum[z].w = fmaf(v[u][z].w, w, sum[z].w);
                     }
+                }
+            }
+        }
+        if (kWide) {
+            // the warps' shares, in their order
+            __shared__ float s_m[kJoinWarps], s_l[kJoinWarps];
+            if (lane == 0) { s_m[warp] = m; s_l[warp] = l; }
+#pragma unroll
+            for (int z = 0; z < V; z++) s_sum[warp][lane + 32 * z] = sum[z];
+            __syncthreads();
+            if (warp > 0) return;
+            float top = m;
+            for (int k = 1; k < kJoinWarps; k++) top = fmaxf(top, s_m[k]);
+            l = 0.f;
+#pragma unroll
+            for (int z = 0; z < V; z++) sum[z] = make_float4(0.f, 0.f, 0.f, 0.f);
+            for (int k = 0; k < kJoinWarps; k++) {
+                const float by = s_m[k] == -INFINITY ? 1.f : exp2_of(s_m[k] - top);
+                l = fmaf(s_l[k], by, l);
+#pragma unroll
+                for (int z = 0; z < V; z++) {
+                    const float4 v = s_sum[k][lane + 32 * z];
+                    sum[z].x = fmaf(v.x, by, sum[z].x); sum[z].y = fmaf(v.y, by, sum[z].y); sum[z].z = fmaf(v.z, by, sum[z].z); sum[z].w = fmaf(v.w, by, sum[z].w);
                 }
             }
         }
@@ -1001,9 +1046,13 @@ int gr_cache_attend(const void* q, int dtype, int q_heads, long long q_token, lo
         cudaLaunchAttribute at = {};
         at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
         at.val.programmaticStreamSerializationAllowed = 1;
-        cfg.gridDim = dim3((unsigned)A.ctas, 1u + (unsigned)((A.tile_rows + gr::kJoinWarps - 1) / gr::kJoinWarps));
+        // items that may be: few, and each has many pieces
+        const long long items = (long long)A.heads * ((long long)tokens * A.group / A.tile_rows + rows);
+        const bool wide = 4 * items <= A.ctas;
+        cfg.gridDim = wide ? dim3((unsigned)items, 1u + (unsigned)A.tile_rows) : dim3((unsigned)A.ctas, 1u + (unsigned)((A.tile_rows + gr::kJoinWarps - 1) / gr::kJoinWarps));
         cfg.blockDim = dim3(gr::kJoinThreads); cfg.stream = st; cfg.attrs = &at; cfg.numAttrs = 1;
-        const auto join = L.dim > 128 ? &gr::attend_join_kernel<2> : &gr::attend_join_kernel<1>;
+        const auto join = L.dim > 128 ? (wide ? &gr::attend_join_kernel<2, true> : &gr::attend_join_kernel<2, false>)
+                                     : (wide ? &gr::attend_join_kernel<1, true> : &gr::attend_join_kernel<1, false>);
         return cudaLaunchKernelEx(&cfg, join, A, A.tile_rows, L.dim) == cudaSuccess ? GR_OK : GR_E_LAUNCH;
     });
     if (done != GR_OK || cudaPeekAtLastError() != cudaSuccess) { cudaGetLastError(); return GR_E_LAUNCH; }

@@ -329,12 +329,12 @@ logprobs_kernel(const __grid_constant__ ProbArgs A)
     }
 }
 
-// CTAs that share a row: as many as there is room for, with a chunk per warp each.
+// CTAs that share a row: as many as there is room for, with a chunk for every other warp at least.
 static int prob_team(int V, int rows)
 {
     const int chunks = (V + kChunk - 1) / kChunk;
     int team = 1;
-    while (team < kProbCluster && 2 * team * 8 <= chunks + 7 && rows * team * 2 <= 2 * kSms) team *= 2;
+    while (team < kProbCluster && 2 * team * 4 <= chunks && rows * team * 2 <= 2 * kSms) team *= 2;
     return team;
 }
 
