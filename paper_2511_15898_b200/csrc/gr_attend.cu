@@ -419,12 +419,6 @@ __device__ __forceinline__ void eat(State<J, NT>& s, const uint4* ready, const c
         }
         load_words<J>(z0, sc + 4 * J * t);
         load_words<J>(z1, sc + kOctet + 4 * J * t);
-        if (kAll) {
-            // row j of the operand: group j's scales
-            const unsigned a0 = g < J ? *(const unsigned*)(sc + 4 * (J * t + g)) : 0u, a2 = g < J ? *(const unsigned*)(sc + kOctet + 4 * (J * t + g)) : 0u;
-#pragma unroll
-            for (int n = 0; n < NT; n++) mma(s.off[n], a0, 0u, a2, 0u, p[n][b][0], p[n][b][1]);
-        }
 #pragma unroll
         for (int j = 0; j < J; j++) {
             uint4 a0, a1;
@@ -437,9 +431,10 @@ __device__ __forceinline__ void eat(State<J, NT>& s, const uint4* ready, const c
                     // (0 stays 0 whatever the scale is)
                     b0 &= __hneu2_mask(*reinterpret_cast<const __half2*>(&p[n][b][0]), __half2half2(__ushort_as_half(0)));
                     b1 &= __hneu2_mask(*reinterpret_cast<const __half2*>(&p[n][b][1]), __half2half2(__ushort_as_half(0)));
-                    const unsigned one = g == j ? 0x3c003c00u : 0u;
-                    mma(s.off[n], one, 0u, one, 0u, b0, b1);
                 }
+                // (row j: the sums of group j, of the same rounded numbers that the codes are multiplied by, so that a rounding's error is taken u - 8 times)
+                const unsigned one = g == j ? 0x3c003c00u : 0u;
+                mma(s.off[n], one, 0u, one, 0u, b0, b1);
                 mma(s.o[n][2 * j], a0.x, a0.y, a0.z, a0.w, b0, b1);
                 mma(s.o[n][2 * j + 1], a1.x, a1.y, a1.z, a1.w, b0, b1);
             }

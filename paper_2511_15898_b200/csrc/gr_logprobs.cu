@@ -58,6 +58,35 @@ template <> struct Floor<__nv_bfloat16> {
     }
 };
 
+// The K largest of the parts' keys, part p in descending order at sh.keys[p GR_MAX_SELECT ...]: a key's rank is its place in its own part and the numbers
+// of larger keys in the others, by bisection in all of them at once.  (Only the K places of a part that may be taken: with all 128 of them, as where a
+// support is selected, eight parts of five keys took 6 us longer.)
+template <class SS, class F>
+__device__ __forceinline__ void merge_parts(SS& sh, int parts, int K, F take)
+{
+    int from = 1;
+    while (from < K) from *= 2;
+#pragma unroll 1
+    for (int e = threadIdx.x; e < parts * K; e += SS::kThr) {
+        const int part = e / K, at = e - part * K;
+        if (at >= sh.part_cnt[part]) continue;
+        const unsigned long long me = sh.keys[part * GR_MAX_SELECT + at];
+        int pos[kProbCluster];
+#pragma unroll
+        for (int p = 0; p < kProbCluster; p++) pos[p] = 0;
+#pragma unroll 1
+        for (int s = from; s > 0; s >>= 1) {
+#pragma unroll
+            for (int p = 0; p < kProbCluster; p++)
+                if (p < parts && pos[p] + s <= sh.part_cnt[p] && sh.keys[p * GR_MAX_SELECT + pos[p] + s - 1] > me) pos[p] += s;
+        }
+        int rank = 0;
+#pragma unroll
+        for (int p = 0; p < kProbCluster; p++) rank += pos[p];
+        if (rank < K) take(rank, me);
+    }
+}
+
 // (sum, mean) of a part moves to the reference `to` at or above its own
 __device__ __forceinline__ void move_to(double& sum, double& mean, float ref, float to)
 {
@@ -282,7 +311,7 @@ logprobs_kernel(const __grid_constant__ ProbArgs A)
             int listed = 0;
             for (int p = 0; p < A.team; p++) listed += s_part[p].count;
             count = min(K, listed);
-            rank_parts(sh, A.team, K, [&](int rank, unsigned long long key) { s_best[rank] = key; });
+            merge_parts(sh, A.team, K, [&](int rank, unsigned long long key) { s_best[rank] = key; });
         }
     }
     __syncthreads();
