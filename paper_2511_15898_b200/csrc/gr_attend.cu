@@ -11,10 +11,17 @@
 // themselves, 2^-12 each, against an output of 8 or 11 bits.  x, m, sums of p and both products are fp32.
 //
 // Work.  A unit is 128 tokens of a (row, head, tile of query rows), or 64; the units of the call in that order are cut into equal shares, one to
-// a CTA of four warps, however ragged the rows are.  Up to 16 query rows: a warp takes 32 of a unit's tokens for all of them and brings them itself, the next ones
-// while it works on these (cp.async.bulk, an octet each, into a ring of its own).  More: all warps take the unit's 64 tokens, each for 16
-// query rows, from one ring that the first one fills, as operands that each makes a quarter of.  What a CTA does not finish it leaves as (m, sum, product) in the workspace;
-// a second kernel joins the pieces in the order of the tokens, so results do not depend on which CTA was first.
+// a CTA, however ragged the rows are.  Up to 16 query rows: a CTA of four warps, each takes 32 of a unit's tokens for all of them and brings them
+// itself, the next ones while it works on these (cp.async.bulk into a ring of its own).  More: a CTA of up to eight warps, which
+// make the operands of 64 tokens together and each take all of them for eight query rows.  What a CTA does not finish it leaves
+// as (m, sum, product) in the workspace; a second kernel joins the pieces in the order of the tokens, so results do not depend on which CTA was first.
+//
+// What bounds it.  64 rows of 6000 tokens, 8 heads of 128 dims, 4 query heads each: 115 us, 59 % of the copy rate; 81 without the arithmetic.  16
+// tokens of a head take 330 warp instructions (80 of them the shifts and ANDs of their 256 words, 20 matrix instructions), which the
+// SMs issue at half of their rate, 16 warps of 128 registers each; three CTAs of 168 registers are as fast, five of 96 spill (149 us).  36 query rows
+// (nine tokens of four heads): 127 us where the bytes take 18; matrix instructions of this kind at their full rate would take 30, and it has the same
+// half of the issue slots, barriers between making operands and using them among them (four warps that each made their own for 16 query rows: 163).
+// One request of 900 tokens: 11 us, two launches and the chains of loads (offsets, positions, table, octets) before the first product.
 #include <math.h>
 #include <algorithm>
 #include "gr_host.h"
@@ -25,11 +32,11 @@ namespace gr {
 constexpr int kEaters = 4;                     // warps of a CTA that takes up to 16 query rows
 constexpr int kMostWarps = 8;                  // of one that takes more, 8 each
 constexpr int kBite = 32;                      // tokens that a warp takes at a time
-// How far above the largest x met the reference is put (p stays at or below 1): at 0 it has to follow every few tokens, a third of the work for 36
-// query rows.  p loses 4 of the 10 binary places below 2^-4 of the largest that fp16 has before its subnormal numbers.
+// How far above the largest x met the reference is put (p stays at or below 1): at 0 it has to follow every few tokens (36 query rows 141 -> 136 us, a
+// decode batch 115 -> 111).  Weights below 2^-10 of the largest, for 2^-14, are subnormal fp16 numbers, good to 2^-21 of it.
 constexpr float kHeadroom = 4.f;
 constexpr int kJoinThreads = 256, kJoinWarps = kJoinThreads / 32;
-constexpr unsigned long long kWaitNs = 2000000000ull;      // longest wait for a copy or a free place in the ring
+constexpr unsigned long long kWaitNs = 2000000000ull;      // longest wait for a copy
 
 struct AttendArgs {
     const void* q; void* out;
@@ -176,11 +183,11 @@ __device__ __forceinline__ void walk_item(Walk& w, const AttendArgs& A)
     w.first = w.lo / kTile;
     w.count = w.hi > w.lo ? (w.hi + kTile - 1) / kTile - w.first : 1;        // (a row that sees nothing: a unit of nothing, which writes its zeros)
 }
-// units of a head of row w.r
+// units of a head of row w.r (64 bits: a prompt of 2^21 tokens has more than 2^31)
 template <int kTile>
-__device__ __forceinline__ int row_units(Walk& w, const AttendArgs& A)
+__device__ __forceinline__ long long row_units(Walk& w, const AttendArgs& A)
 {
-    int sum = 0;
+    long long sum = 0;
     for (w.y = 0; w.y * A.tile_rows < w.n * A.group; w.y++) { walk_item<kTile>(w, A); sum += w.count; }
     return sum;
 }
@@ -575,7 +582,7 @@ attend_kernel(const __grid_constant__ AttendArgs A)
         for (int r = tid * per; r < min((tid + 1) * per, A.rows); r++) {
             w.r = r;
             walk_row(w, A);
-            mine += (long long)row_units<kTile>(w, A) * A.heads;
+            mine += row_units<kTile>(w, A) * A.heads;
         }
         long long upto = mine;
 #pragma unroll
@@ -595,10 +602,10 @@ attend_kernel(const __grid_constant__ AttendArgs A)
             for (int r = tid * per;; r++) {
                 w.r = r;
                 walk_row(w, A);
-                const int units = row_units<kTile>(w, A);
-                if (left >= (long long)units * A.heads) { left -= (long long)units * A.heads; continue; }
-                w.h = (int)(left / units);
-                left -= (long long)w.h * units;
+                const long long units = row_units<kTile>(w, A);
+                if (left >= units * A.heads) { left -= units * A.heads; continue; }
+                w.h = (left | units) >> 32 ? (int)(left / units) : (int)((unsigned)left / (unsigned)units);
+                left -= w.h * units;
                 for (w.y = 0;; w.y++) {
                     walk_item<kTile>(w, A);
                     if (left < w.count) break;
@@ -943,7 +950,8 @@ attend_join_kernel(const __grid_constant__ AttendArgs A, int tile_rows, int dim)
 
 // ---------------------------------------------------------------- host
 
-// The kernel for a call: whether a key head's query rows (a row's tokens times its group, on average) fill more than 8 of the products' columns, more than 16.
+// The kernel for a call, by a key head's query rows (a row's tokens times its group, on average): up to 8 in one tile, up to 16 in two (with heads of more
+// than 128 dims there are no registers for two); beyond, a warp for each 8.  (17 to 64 by tiles of 8 that each read the row again: 136 us for 127 at 36.)
 struct Choice { int nt; bool rows; int warps; };
 static Choice choose(int dim, int group, int rows, int tokens)
 {
@@ -995,7 +1003,7 @@ int gr_cache_attend(const void* q, int dtype, int q_heads, long long q_token, lo
     const gr_cache_layout& L = *layout;
     if ((dtype != GR_BF16 && dtype != GR_F16) || !gr::attend_shape_ok(L.heads, q_heads, L.dim, rows, tokens)) return GR_E_INVALID;
     if (width < 0 || (long long)width * L.block_size >= (1ll << 31) - 256 || (long long)rows * std::max(1, width) >= (1ll << 31)) return GR_E_INVALID;
-    if (window < 0 || !isfinite(scale)) return GR_E_INVALID;
+    if (window < 0 || !(fabsf(scale) < 1.7e38f)) return GR_E_INVALID;        // (with log2(e) still a number)
     if (!gr::counted(q_token, q_head, tokens, q_heads)) return GR_E_INVALID;
     const long long step[2] = {out_token, out_head}, size[2] = {tokens, q_heads};
     if (!gr::apart(L.dim, step, size, 2)) return GR_E_INVALID;

@@ -1,12 +1,16 @@
 // gr_cache_append and gr_cache_read: new tokens' keys and values into a paged cache, rotated by their positions on the way, and out again.
 //
-// Both move bytes.  A CTA takes the tokens of one window (one token where there are few, for latency; eight otherwise) and all their
-// heads, so that a token's angles are worked out once: position x frequency in fp64, brought to [-pi / 4, pi / 4] in fp64 (far
+// Both move bytes.  A CTA takes the tokens of one window (one token where there are few, for latency; eight or sixteen otherwise) and all
+// their heads, so that slots, runs and angles are worked out once: position x frequency in fp64, brought to [-pi / 4, pi / 4] in fp64 (far
 // positions lose nothing), sine and cosine by their Taylor series, rounded to fp32 once.  The rotation takes fp32 products and sums
-// without contraction, each rounded, so that what is held follows from the formula whatever computes it; an angle's two
-// numbers cost 30 fp64 operations, shared by all heads.
+// without contraction, each rounded, so that what is held follows from the formula whatever computes it.
 // In a 4-bit cache the unit is the octet: a run of a call's tokens that lie one after another in one octet is taken by one CTA, the
 // one whose window its first token is in, so that a prompt's octets are written whole.
+//
+// Measured (bytes that it cannot do without, against the copy rate): 9000 tokens of 12 ragged prompts, 8 heads and 32 query heads of 128 dims,
+// fp16: 41 to 44 us, 77 to 82 %; the same keys and values from bf16 into 4 bits 40 us and out of them 17, where the bytes of both take 14: instructions bound
+// both, 270 for a row of 128 numbers of two tokens at less than half of the issue rate.  65536 tokens
+// out of 4 bits as bf16: 64 us, 82 %.  One token for each of 64 rows: 2.8 us, latency.
 #include <math.h>
 #include <algorithm>
 #include "gr_host.h"
@@ -15,7 +19,7 @@
 namespace gr {
 
 constexpr int kCacheThreads = 256, kCacheWarps = kCacheThreads / 32;
-constexpr int kCacheWindow = 32;               // most tokens of a CTA
+constexpr int kCacheWindow = 16;               // most tokens of a CTA
 constexpr int kCacheSeen = kCacheWindow + 7;   // and those that it looks at
 constexpr int kCacheMany = 16 * kSms;          // from so many tokens on
 

@@ -10,7 +10,10 @@
 // value, do not make 0 times infinity.  The list of the likeliest is the beam selection's (thresholds from running maxima).
 // Rows with a NaN or +infinity leave a sum that is no number; those, and rows whose x s is beyond 2^20, are taken again in fp64.
 //
-// HBM bounds it where there are many rows; latency (a trip to memory, a threshold, the selection) where there are few.
+// HBM bounds it in fp32 (1024 rows of 128256, 20 alternatives: 95 us, 84 % of the copy rate); in bf16 (2048 rows of 152064, 8 alternatives: 149 us, 64 %)
+// instruction issue and the exponentials' pipe, half of each: 80 instructions for 8 ids of 32 lanes, eight of them exponentials.  A batch ahead in
+// registers, with six CTAs per SM for eight, takes 159 (and 124 in fp32), twelve CTAs of 40 registers 183.  Latency bounds few rows (4 of
+// 50257: 9.7 us, clusters of eight: a trip to memory, a threshold, the selection, the parts' merge).
 #include <math.h>
 #include <algorithm>
 #include "gr_host.h"
@@ -370,14 +373,17 @@ static int prob_team(int V, int rows)
 template <typename T>
 static int launch_logprobs(const ProbArgs& A, cudaStream_t st)
 {
-    // (which size of CTA when: the beam selection's rule, whose streaming pass this one's is)
+    // CTAs of 128 threads, eight to an SM, finish a wave of rows sooner than four of 256 (128256 fp32 logits, us: 600 rows 77 for 86, 1184: 102 for 107,
+    // 4200: 352 for 369; bf16, 2000: 130 for 139, 4800: 285 for 310), unless they need two waves where those take three (fp32, 1500: 164 for
+    // 144), which evens out with more waves (4800: 417 for 416).  In bf16 a wave of twelve to an SM goes before two of eight (1300 rows
+    // 97 for 107, 1700: 117 for 119), but not three of them before four (3600: 236 for 224).
     const long long ctas = (long long)A.rows * A.team;
     auto waves = [&](int per) { return (ctas + per * kSms - 1) / (per * kSms); };
     constexpr bool kNarrow = sizeof(T) == 2;
     const bool small = A.keep <= 48 && ctas > 4 * kSms && (kNarrow || ctas > 16 * kSms || 2 * waves(8) <= waves(4));
     cudaError_t rc;
     if (A.team > 1 || ctas <= 2 * kSms) rc = launch_pdl_cluster(A.team, logprobs_kernel<T, kChunk / (32 * VecTraits<T>::N), 256, 2>, (int)ctas, 256, 0, st, A);
-    else if (small && kNarrow && 4 * waves(12) <= 3 * waves(8)) rc = launch_pdl(logprobs_kernel<T, 4, 128, kNarrow ? 12 : 8>, (int)ctas, 128, 0, st, A);
+    else if (small && kNarrow && waves(12) == 1 && waves(8) == 2) rc = launch_pdl(logprobs_kernel<T, 4, 128, kNarrow ? 12 : 8>, (int)ctas, 128, 0, st, A);
     else if (small) rc = launch_pdl(logprobs_kernel<T, 4, 128, 8>, (int)ctas, 128, 0, st, A);
     else rc = launch_pdl(logprobs_kernel<T, 4, 256, 4>, (int)ctas, 256, 0, st, A);
     return rc == cudaSuccess ? GR_OK : GR_E_LAUNCH;

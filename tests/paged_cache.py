@@ -125,8 +125,9 @@ def attention(q, held, block_size, table, offsets, positions, scale, window):
     """What gr_cache_attend computes, in 64 bits, and a bound of its error before the rounding to the output's type.
 
     x = scale q.k is summed in 32 bits, from codes 0 .. 15 and the sum of the queries times 8, both up to A = scale sum |q| 16 |s|: eight
-    roundings of 2^-23 A.  p is rounded to 11 bits, p s once more (2^-12 of each, at codes up to 15, and 2^-12 of p where 8 times their sum is
-    taken off: 38 2^-12 p |s|; below 2^-14 by 2^-25 instead); sums of n / 16 products and eight joins round 2^-22 of 16 p |s| each."""
+    roundings of 2^-23 A.  p is rounded to 11 bits and p s once more, 2^-12 of each, and what comes of it is taken u - 8 times, 8 at most: 16 2^-12 p |s|.
+    Where they are below 2^-14 they are off by 2^-25 each instead, of a reference up to 2^4 above the largest p: by 2^-21 of that, (1 + |s|) 8 times.
+    Sums of n / 16 products and eight joins round 2^-22 of 16 p |s| each."""
     T, Hq, D = q.shape
     k, v, ks, vs = held
     H = k.shape[1]
@@ -150,6 +151,6 @@ def attention(q, held, block_size, table, offsets, positions, scale, window):
                 w = np.exp(x - x.max())
                 out[i, h] = w @ v[z, g] / w.sum()
                 s = np.abs(vs[z, g])
-                bound[i, h] = ((38 * 2.0 ** -12 + 16 * (len(z) / 16 + 8) * 2.0 ** -22) * (w @ s) + 2.0 ** -25 * 38 * (1 + s).sum(0)
+                bound[i, h] = ((16 * 2.0 ** -12 + 16 * (len(z) / 16 + 8) * 2.0 ** -22) * (w @ s) + 2.0 ** -21 * 8 * (1 + s).sum(0)
                                + (2 * dx + 2.0 ** -20) * (w @ np.abs(v[z, g]))) / w.sum()
     return out, bound

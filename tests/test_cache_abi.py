@@ -95,7 +95,7 @@ def test_attend():
     assert call(dtype=G.GR_F32) == -1 and call(dtype=G.GR_Q4) == -1 and call(heads=7) == -1 and call(heads=0) == -1 and call(heads=1026) == -1
     assert call(rows=-1) == -1 and call(tokens=-1) == -1 and call(width=-1) == -1 and call(window=-1) == -1 and call(rows=(1 << 20) + 1) == -1
     assert call(width=1 << 27) == -1 and call(rows=1 << 20, width=1 << 11) == -1 and call(tokens=1 << 29) == -1
-    assert call(scale=float("nan")) == -1 and call(scale=float("inf")) == -1
+    assert call(scale=float("nan")) == -1 and call(scale=float("inf")) == -1 and call(scale=2e38) == -1 and call(scale=-2e38) == -1
     assert call(qt=-1) == -1 and call(qh=-1) == -1 and call(qt=1 << 60) == -1 and call(oh=63) == -1 and call(ot=511) == -1
     for name in ("q", "cache", "table", "off", "pos", "ws", "out", "status"):
         assert call(**{name: 0}) == -2, name

@@ -301,6 +301,7 @@ def test_a_step_of_decoding():
                 keys, values = (torch.stack(x).repeat_interleave(group, 1) for x in history[r])
                 w = torch.softmax(torch.einsum("hd,thd->ht", q[i].double(), keys) * D ** -0.5, 1)
                 want = torch.einsum("ht,thd->hd", w, values)
-                # one rounding to bf16, and 2^-12 for each of two roundings of the weights at codes up to 15 steps of |v| / 8 and more
-                assert (out.out[i].double() - want).abs().max() <= 2.0 ** -9 * want.abs().max() + 38 * 2.0 ** -12 * values.abs().max() / 7
+                # one rounding to bf16 (at 2^e and more numbers are 2^(e - 7) apart, so half of that, 2^-8 of the value, not 2^-9) and two of the
+                # weights, 2^-12 each, taken up to 8 times a scale of at most |v| / 7
+                assert (out.out[i].double() - want).abs().max() <= 2.0 ** -8 * want.abs().max() + 16 * 2.0 ** -12 * values.abs().max() / 7
                 i += 1

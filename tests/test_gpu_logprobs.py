@@ -71,6 +71,7 @@ def _check(logits, tokens, top, T=1.0, rows=64):
     (1, 1, 1, 1, 1.0), (3, 2, 2, 5, 0.5), (5, 7, 1, 7, 1.0), (2, 100, 1, 0, 1.3), (4, 1023, 3, 20, 1.0), (3, 1025, 64, 128, 0.7),
     (1, 32000, 1, 5, 1.0), (2, 50257, 1, 128, 0.8), (9, 128256, 2, 20, 1.0), (20, 33001, 1, 1, 1.0), (40, 65541, 0, 10, 1.0), (300, 9001, 1, 0, 1.0),
     (700, 20011, 1, 48, 1.0), (1300, 5003, 2, 49, 0.7), (2500, 3001, 1, 8, 1.0), (1, 2097152, 1, 16, 1.0), (160, 152064, 1, 128, 1.0),
+    (1300, 5003, 1, 8, 1.0),
 ])
 def test_logprobs(R, V, given, top, T, dtype):
     g = _gen(R + V)
