@@ -498,57 +498,65 @@ __device__ __forceinline__ long long out_at(const AttendArgs& A, int token, int 
 
 // ---------------------------------------------------------------- first kernel
 
-// Brings octets into a ring, ahead of what is eaten: a warp's place in the units (in shared memory, for registers), and the block ids of the next ones.
+// Brings octets into a ring, ahead of what is eaten.  An octet of the next 32 is each lane's: where they are is looked up once for several units.  The
+// place in the units is in shared memory, for registers.
 struct FeedItem {
     const char* head;                          // the cache from the item's head on
     const int* row;                            // the table's row
-    int hi, lo, left;                          // tokens that are wanted; units of the item that are left
+    int hi, lo, units, token;                  // tokens that are wanted; units of the item; the first token to look up next
+    unsigned mask;                             // which of the 32 octets are wanted and there
 };
 template <int J, int NT, bool kRows>
 struct Feeder {
     using S = Shape<J, NT, kRows>;
-    static constexpr int kOctets = S::kStage / S::kOctet;
-    int token, id, in;                         // of this lane's octet in the next unit: first token, block, place in that
+    static constexpr int kOctets = S::kStage / S::kOctet, kUnits = 32 / kOctets;
+    const char* from;                          // this lane's octet, if a copy begins there
+    int bytes, fed;                            // of that copy, or 0; units of the item that have been brought
 
     __device__ __forceinline__ void begin(FeedItem& f, const AttendArgs& A, const Walk& w, int units, int skip, int lane)
     {
-        if (lane == 0) f = FeedItem{A.cache + (long long)w.h * A.head_bytes, A.table + (long long)w.r * A.width, w.hi, w.lo, min(w.count - w.at, units)};
-        token = (w.first + w.at) * S::kTile + skip + 8 * lane;
+        if (lane == 0)
+            f = FeedItem{A.cache + (long long)w.h * A.head_bytes, A.table + (long long)w.r * A.width, w.hi, w.lo, min(w.count - w.at, units), (w.first + w.at) * S::kTile + skip, 0u};
+        fed = 0;
         __syncwarp();
         look(f, A, lane);
     }
-    __device__ __forceinline__ void look(const FeedItem& f, const AttendArgs& A, int lane)
+    // (octets next to one another in a block and a unit by one copy: the instruction takes one address a warp, lanes with one each go through it in turn)
+    __device__ __forceinline__ void look(FeedItem& f, const AttendArgs& A, int lane)
     {
-        id = -1;
-        if (lane < kOctets && token < f.hi && token + 8 > f.lo) {
+        // (may pass 2^31 in the units behind the last)
+        const unsigned token = (unsigned)f.token + (unsigned)(lane / kOctets * S::kTile + 8 * (lane % kOctets));
+        int id = -1, in = 0;
+        if (token < (unsigned)f.hi && (int)token + 8 > f.lo) {
             // (blocks of a multiple of eight tokens; the quotient by a product with the reciprocal, rounded up)
-            const unsigned octet = (unsigned)token >> 3, block = A.octets == 1 ? octet : __umulhi(octet, A.by_octets) >> A.shift;
+            const unsigned octet = token >> 3, block = A.octets == 1 ? octet : __umulhi(octet, A.by_octets) >> A.shift;
             in = (int)(octet - block * (unsigned)A.octets);
             if ((int)block < A.width) id = f.row[block];
         }
-    }
-    // into place `place` of the ring; `have`: which octets it will hold; whether that was the item's last unit.  (Octets next to one another in a block
-    // by one copy: the instruction takes one address a warp, lanes with one each go through it in turn.)
-    __device__ __forceinline__ bool bring(FeedItem& f, const AttendArgs& A, char* place, unsigned long long* full, unsigned* have, int lane)
-    {
         const bool want = id >= 0 && id < A.num_blocks;
-        const unsigned mask = __ballot_sync(0xffffffffu, want), starts = __ballot_sync(0xffffffffu, want && (lane == 0 || in == 0 || !(mask >> ((lane - 1) & 31) & 1)));
+        const unsigned mask = __ballot_sync(0xffffffffu, want);
+        const bool start = want && (lane % kOctets == 0 || in == 0 || !(mask >> ((lane - 1) & 31) & 1));
+        // up to the next start, or the first that is not wanted
+        const unsigned stop = (__ballot_sync(0xffffffffu, start) | ~mask) & ~((2u << lane) - 1u);
+        from = f.head + (start ? id * A.block_stride + (long long)in * S::kOctet : 0);
+        bytes = start ? ((stop ? __ffs(stop) - 1 : 32) - lane) * S::kOctet : 0;
+        __syncwarp();
+        if (lane == 0) { f.mask = mask; f.token = (int)((unsigned)f.token + kUnits * S::kTile); }
+        __syncwarp();
+    }
+    // The next unit into place `place` of the ring; `have`: which octets it will hold.  Whether that was the item's last.
+    __device__ __forceinline__ bool bring(const FeedItem& f, char* place, unsigned long long* full, unsigned* have, int lane)
+    {
+        const int at = fed & (kUnits - 1);
         const unsigned bar = smem_addr(full);
-        const int left = f.left - 1;
-        __syncwarp();
         if (lane == 0) {
-            *have = mask;
-            f.left = left;
-            bar_expect(bar, __popc(mask) * S::kOctet);
+            const unsigned here = f.mask >> (at * kOctets) & ((1u << kOctets) - 1u);
+            *have = here;
+            bar_expect(bar, __popc(here) * S::kOctet);
         }
         __syncwarp();
-        if (starts >> lane & 1) {
-            // up to the next start, or the first that is not wanted
-            const unsigned stop = (starts | ~mask) & ~((2u << lane) - 1u);
-            bulk_load(smem_addr(place) + lane * S::kOctet, f.head + id * A.block_stride + (long long)in * S::kOctet, (__ffs(stop) - 1 - lane) * S::kOctet, bar);
-        }
-        token += S::kTile;
-        return left == 0;
+        if (lane / kOctets == at && bytes > 0) bulk_load(smem_addr(place) + lane % kOctets * S::kOctet, from, bytes, bar);
+        return ++fed == f.units;
     }
 };
 
@@ -635,7 +643,7 @@ attend_kernel(const __grid_constant__ AttendArgs A)
     // unit `next` of the share
     auto feed = [&](int next) {
         const int place = next % kStages;
-        const bool end = feeder.bring(s_item[warp], A, ring + place * S::kStage, full + place, held + place, lane);
+        const bool end = feeder.bring(s_item[warp], ring + place * S::kStage, full + place, held + place, lane);
         if (next + 1 == total) return;
         if (end) {
             Walk w = s_feed[warp];
@@ -643,7 +651,7 @@ attend_kernel(const __grid_constant__ AttendArgs A)
             walk_next<kTile>(w, A);
             if (lane == 0) s_feed[warp] = w;
             feeder.begin(s_item[warp], A, w, total - next - 1, kRows ? 0 : kBite * warp, lane);
-        } else feeder.look(s_item[warp], A, lane);
+        } else if ((feeder.fed & (Feeder<J, NT, kRows>::kUnits - 1)) == 0) feeder.look(s_item[warp], A, lane);
     };
     if (feeds) {
         feeder.begin(s_item[warp], A, s_feed[warp], total, kRows ? 0 : kBite * warp, lane);
