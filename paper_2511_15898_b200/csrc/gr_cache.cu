@@ -8,8 +8,8 @@
 // one whose window its first token is in, so that a prompt's octets are written whole.
 //
 // Measured (bytes that it cannot do without, against the copy rate): 9000 tokens of 12 ragged prompts, 8 heads and 32 query heads of 128 dims,
-// fp16: 41 to 44 us, 77 to 82 %; the same keys and values from bf16 into 4 bits 40 us and out of them 17, where the bytes of both take 14: instructions bound
-// both, 270 for a row of 128 numbers of two tokens at less than half of the issue rate.  65536 tokens
+// fp16: 41 to 44 us, 77 to 82 %; the same keys and values from bf16 into 4 bits 36 us and out of them 16, where the bytes of both take 14: instructions bound
+// both, 250 for a row of 128 numbers of two tokens at half of the issue rate.  65536 tokens
 // out of 4 bits as bf16: 64 us, 82 %.  One token for each of 64 rows: 2.8 us, latency.
 #include <math.h>
 #include <algorithm>
@@ -381,10 +381,9 @@ __device__ __forceinline__ unsigned quantise(const unsigned long long (&x)[4], u
     // (a NaN stays the largest; magnitudes order as their bits, the sign goes below them)
     float hi = f_lo(x[0]), lo = hi;
 #pragma unroll
-    for (int i = 1; i < 8; i++) {
-        const float v = i & 1 ? f_hi(x[i / 2]) : f_lo(x[i / 2]);
-        asm("max.NaN.f32 %0, %0, %1;" : "+f"(hi) : "f"(v));
-        lo = fminf(lo, v);
+    for (int i = 0; i < 4; i++) {
+        asm("max.NaN.f32 %0, %0, %1, %2;" : "+f"(hi) : "f"(f_lo(x[i])), "f"(f_hi(x[i])));
+        asm("min.f32 %0, %0, %1, %2;" : "+f"(lo) : "f"(f_lo(x[i])), "f"(f_hi(x[i])));
     }
     const float peak = -lo > hi ? lo : hi;
     unsigned most = __funnelshift_l(~__float_as_uint(peak), __float_as_uint(peak), 1);
@@ -401,16 +400,17 @@ __device__ __forceinline__ unsigned quantise(const unsigned long long (&x)[4], u
     // exact in one fused operation, and where it is more than half of s, or half of it and w odd, its sign says which.
     const float magic = 12582912.f + 8.f, half = 0.5f * fabsf(s);
     const unsigned long long inverse2 = f_pack(inverse, inverse), magic2 = f_pack(magic, magic), s2 = f_pack(-s, -s), back2 = f_pack(-magic, -magic);
-    int code[8];
+    constexpr int kZero = 0x4b400000, kZeros = (int)(0x4b400000u * 0x11111111u);      // the bits of 12582912, in code and in eight of them
+    int code[8];                               // and kZero
     unsigned long long left[4];
     float most_left = 0.f;
 #pragma unroll
     for (int i = 0; i < 4; i++) {
         const unsigned long long y = fma2(x[i], inverse2, magic2);
         left[i] = fma2(add2(y, back2), s2, x[i]);
-        most_left = fmaxf(most_left, fmaxf(fabsf(f_lo(left[i])), fabsf(f_hi(left[i]))));
-        code[2 * i] = (int)(unsigned)y - (int)__float_as_uint(12582912.f);
-        code[2 * i + 1] = (int)(unsigned)(y >> 32) - (int)__float_as_uint(12582912.f);
+        asm("max.abs.f32 %0, %0, %1, %2;" : "+f"(most_left) : "f"(f_lo(left[i])), "f"(f_hi(left[i])));
+        code[2 * i] = (int)(unsigned)y;
+        code[2 * i + 1] = (int)(unsigned)(y >> 32);
     }
     // (fp16 scales below 2^-14 are so coarse that quotients below -8 come up)
     if (most_left >= half || (scale & 0x7c00u) == 0) {
@@ -418,13 +418,13 @@ __device__ __forceinline__ unsigned quantise(const unsigned long long (&x)[4], u
         for (int i = 0; i < 8; i++) {
             const float r = i & 1 ? f_hi(left[i / 2]) : f_lo(left[i / 2]);
             if (fabsf(r) > half || (fabsf(r) == half && (code[i] & 1))) code[i] += (r < 0.f) != (s < 0.f) ? -1 : 1;
-            code[i] = max(code[i], 0);
+            code[i] = max(code[i], kZero);
         }
     }
-    unsigned w = (unsigned)min(code[7], 15);
+    unsigned w = (unsigned)min(code[7], kZero + 15);
 #pragma unroll
-    for (int i = 6; i >= 0; i--) w = w * 16u + (unsigned)min(code[i], 15);
-    return w;
+    for (int i = 6; i >= 0; i--) w = w * 16u + (unsigned)min(code[i], kZero + 15);
+    return w - (unsigned)kZeros;
 }
 
 // x cos + y sin of eight elements next to one another and their partners (sin of the sign that the elements' side of the pairs has), products rounded
@@ -746,10 +746,11 @@ int check_cache(const void* keys, const void* values, const gr_cache_layout* lay
 }
 
 // How a call's tokens are dealt out: windows of one token where there are few, with the heads in several CTAs until an SM has two; of `most`
-// where that leaves every SM four, else of eight.
-static void deal(CacheArgs& A, int rows_of_token, int most)
+// where that leaves every SM `each`, else of eight.  (4 bits, 8 heads of 128 dims, 8 and 16 tokens, us: append 12000 38 and 41, 20000 67 and 69, 40000
+// 125 and 120, 65536 199 and 190: a CTA's time is its last wave's; read 9600 12.4 and 12.1, 65536 72 and 64.)
+static void deal(CacheArgs& A, int rows_of_token, int most, int each)
 {
-    A.window = A.tokens >= 4 * kSms * most ? most : A.tokens >= kCacheMany ? 8 : 1;
+    A.window = A.tokens >= each * kSms * most ? most : A.tokens >= kCacheMany ? 8 : 1;
     const int windows = (A.tokens + A.window - 1) / A.window;
     A.split = std::max(1, std::min((2 * kSms + windows - 1) / windows, (rows_of_token + kCacheWarps - 1) / kCacheWarps));
 }
@@ -900,7 +901,7 @@ int gr_cache_append(void* keys, void* values, const gr_cache_layout* layout, con
         const bool vec = kv.bits % 16 == 0 && (interleaved || (rot / 2) % 8 == 0);
         const int n = fits(4, q.bits, 0) ? 4 : 1;
         A.four = 1;
-        gr::deal(A, 8 * L.heads + (X.q_heads + 3) / 4, 16);
+        gr::deal(A, 8 * L.heads + (X.q_heads + 3) / 4, 16, 16);
         const int smem = (A.window + 7) * gr::angle_step(A.half) * (int)sizeof(float2);
         if (X.dtype == GR_F32) gr::launch_append4<float>(A, vec, n, smem, st);
         else if (X.dtype == GR_BF16) gr::launch_append4<__nv_bfloat16>(A, vec, n, smem, st);
@@ -908,7 +909,7 @@ int gr_cache_append(void* keys, void* values, const gr_cache_layout* layout, con
     } else {
         const unsigned long long own = kv.bits | q.bits;
         const int n = e == 2 && gr::type_size(L.format) == 2 && fits(8, own, c.bits) ? 8 : fits(4, own, c.bits) ? 4 : 1;
-        gr::deal(A, (2 * L.heads + X.q_heads + 3) / 4, 8);
+        gr::deal(A, (2 * L.heads + X.q_heads + 3) / 4, 8, 4);
         const int smem = A.window * gr::angle_step(A.half) * (int)sizeof(float2);
         if (X.dtype == GR_F32) gr::launch_append_to<float>(A, L.format, n, smem, st);
         else if (X.dtype == GR_BF16) gr::launch_append_to<__nv_bfloat16>(A, L.format, n, smem, st);
@@ -948,7 +949,7 @@ int gr_cache_read(const void* keys, const void* values, const gr_cache_layout* l
     gr::NvtxRange whole("gr_cache_read");
     if (L.format == GR_Q4) {
         A.four = 1;
-        gr::deal(A, L.heads, 16);
+        gr::deal(A, L.heads, 16, 4);
         const bool vec = out.bits % (unsigned long long)(8 * e) == 0;
         if (dtype == GR_F32) gr::launch_read4<float>(R, vec, st);
         else if (dtype == GR_BF16) gr::launch_read4<__nv_bfloat16>(R, vec, st);
@@ -958,7 +959,7 @@ int gr_cache_read(const void* keys, const void* values, const gr_cache_layout* l
         c.add(keys, ce, {L.block_stride, L.token_stride, L.head_stride}); c.add(values, ce, {L.block_stride, L.token_stride, L.head_stride});
         auto fits = [&](int n) { return out.bits % (unsigned long long)(n * e) == 0 && c.bits % (unsigned long long)(n * ce) == 0 && L.dim % n == 0; };
         const int n = e == 2 && ce == 2 && fits(8) ? 8 : fits(4) ? 4 : 1;
-        gr::deal(A, (2 * L.heads + 3) / 4, 8);
+        gr::deal(A, (2 * L.heads + 3) / 4, 8, 4);
         if (L.format == GR_F32) gr::launch_read_to<float>(R, dtype, n, st);
         else if (L.format == GR_BF16) gr::launch_read_to<__nv_bfloat16>(R, dtype, n, st);
         else gr::launch_read_to<__half>(R, dtype, n, st);

@@ -109,7 +109,7 @@ def test_append(T, H, Hq, D, rot, bs, dtype, cache, inter):
     (1, 1, 32, 32, 8, "bf16", False), (7, 2, 64, 64, 16, "f16", False), (50, 1, 96, 48, 24, "bf16", True),
     (64, 2, 128, 128, 64, "bf16", False), (30, 2, 128, 64, 16, "f32", False), (21, 1, 256, 256, 8, "bf16", True),
     (20, 1, 160, 0, 40, "f32", False), (23, 1, 224, 222, 16, "f32", False), (2400, 1, 64, 64, 16, "bf16", False),
-    (9601, 1, 64, 64, 24, "f16", False),
+    (9601, 1, 64, 64, 24, "f16", False), (37890, 1, 32, 32, 40, "bf16", False),
 ])
 def test_append_in_four_bits(T, H, D, rot, bs, dtype, inter):
     g, N, slots, positions, k, v = _case(T * 3 + D, T, H, D, bs, DT[dtype])
