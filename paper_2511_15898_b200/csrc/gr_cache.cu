@@ -427,11 +427,11 @@ __device__ __forceinline__ unsigned quantise(const unsigned long long (&x)[4], u
     return w - (unsigned)kZeros;
 }
 
-// x cos + y sin of eight elements next to one another and their partners (sin of the sign that the elements' side of the pairs has), products rounded
-// one by one
+// x cos + y sin of two elements next to one another and their partners (sin of the sign that the elements' side of the pairs has), each product and sum
+// rounded by itself.  (Not in packed arithmetic: the assembler joins mul.rn.f32x2 and add.rn.f32x2 to one operation that rounds once.)
 __device__ __forceinline__ unsigned long long turned2(unsigned long long x, unsigned long long y, float c0, float s0, float c1, float s1)
 {
-    return add2(mul2(x, f_pack(c0, c1)), mul2(y, f_pack(s0, s1)));
+    return f_pack(__fadd_rn(__fmul_rn(f_lo(x), c0), __fmul_rn(f_lo(y), s0)), __fadd_rn(__fmul_rn(f_hi(x), c1), __fmul_rn(f_hi(y), s1)));
 }
 
 template <typename T, bool kVec>
