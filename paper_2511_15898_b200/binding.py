@@ -149,7 +149,7 @@ def load_library():
     lib.gr_strerror.argtypes = [C.c_int]
     _entry.update({n: C.cast(getattr(lib, n), C.c_void_p).value
                    for n in ("gr_beam_select", "gr_reorder_states", "gr_block_plan", "gr_copy_blocks", "gr_cache_append", "gr_cache_read",
-                             "gr_cache_attend", "gr_token_logprobs")})
+                             "gr_cache_attend", "gr_attend_workspace_bytes", "gr_token_logprobs")})
     _lib = lib
     if "_tensors" not in globals():
         _tensors = _load_tensors()
@@ -1074,7 +1074,7 @@ def cache_attend(q: torch.Tensor, cache: KVCache, table: torch.Tensor, offsets: 
     tokens, itself the last.  `out`: a result of an earlier call of the same shape, written again; what lies behind the last row's tokens stays."""
     if (out is not None and out.shape[4] == cache.heads
             and _short("attend", "gr_cache_attend", q, cache.keys, cache.values, cache.block_size, cache.heads, cache.dim, table, offsets, positions,
-                       scale, window, out.workspace, out.out, out.status)):
+                       scale, window, out.workspace, out.out, out.status, _entry.get("gr_attend_workspace_bytes"))):
         return out
     a_cache, _, layout = _cache(cache)
     if layout.format != GR_Q4:
@@ -1092,15 +1092,18 @@ def cache_attend(q: torch.Tensor, cache: KVCache, table: torch.Tensor, offsets: 
     a_pos = _need(positions, "positions", torch.int32, (T,), dev)
     _fits("cache_attend", T, Hq, R, width, window)
     shape = (T, Hq, D, R, cache.heads, q.dtype)
+    wbytes = gr_attend_workspace_bytes(cache.heads, Hq, D, R, T)
+    if wbytes == 0:
+        raise GrError("invalid shape")
     if out is None or out.shape != shape or out.out.device != dev:
-        wbytes = gr_attend_workspace_bytes(cache.heads, Hq, D, R, T)
-        if wbytes == 0:
-            raise GrError("invalid shape")
         out = Attended(torch.zeros(T, Hq, D, dtype=q.dtype, device=dev), torch.empty(R, dtype=torch.int32, device=dev),
                        torch.empty(wbytes, dtype=torch.uint8, device=dev), shape)
     out_at = _rows(out.out, "out", q.shape, q.dtype, dev)
+    a_ws, a_status = _need(out.workspace, "out.workspace", torch.uint8, None, dev), _need(out.status, "out.status", torch.int32, (R,), dev)
+    if out.workspace.numel() < wbytes:
+        raise GrError(f"out.workspace: {wbytes} bytes are needed")
     _call(dev, "gr_cache_attend", gr_cache_attend, q_at[0], _CODES[q.dtype], Hq, *q_at[1:], a_cache, layout, a_table, width, R, a_off, a_pos,
-          T, D ** -0.5 if scale is None else scale, window, out.workspace.data_ptr(), *out_at, out.status.data_ptr())
+          T, D ** -0.5 if scale is None else scale, window, a_ws, *out_at, a_status)
     return out
 
 
@@ -1147,8 +1150,11 @@ def token_logprobs(logits: torch.Tensor, tokens: Optional[torch.Tensor] = None, 
         f32, i32 = dict(dtype=torch.float32, device=dev), dict(dtype=torch.int32, device=dev)
         out = Logprobs(torch.empty(R, given, **f32), torch.empty(R, **f32), torch.empty(R, top, **i32), torch.empty(R, top, **f32),
                        torch.empty(R, **i32), (R, given, top))
+    own = [_need(getattr(out, n), f"out.{n}", kind, size, dev)
+           for n, kind, size in (("logprob", torch.float32, (R, given)), ("entropy", torch.float32, (R,)), ("top_token", torch.int32, (R, top)),
+                                 ("top_logprob", torch.float32, (R, top)), ("status", torch.int32, (R,)))]
     if R > 0 and a_tokens and a_tokens == out.top_token.data_ptr() and top > 0:
         raise GrError("tokens is a tensor of `out`, which this call writes")
     _call(dev, "gr_token_logprobs", load_library().gr_token_logprobs, logits.data_ptr(), code, V, max(ld, V), R, temperature, a_tokens, given, top,
-          out.logprob.data_ptr(), out.entropy.data_ptr(), out.top_token.data_ptr(), out.top_logprob.data_ptr(), out.status.data_ptr())
+          *own)
     return out

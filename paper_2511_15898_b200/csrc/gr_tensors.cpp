@@ -315,17 +315,18 @@ PyObject* read(PyObject*, PyObject* const* a, Py_ssize_t n)
     GR_CATCH
 }
 
-// attend(function, q, keys, values, block_size, heads, dim, table, offsets, positions, scale, window, workspace, out, status) -> its answer or None.
-// (The last three are the binding's own, made for the shape.)
+// attend(function, q, keys, values, block_size, heads, dim, table, offsets, positions, scale, window, workspace, out, status, workspace's size) -> its answer
+// or None.
 PyObject* attend(PyObject*, PyObject* const* a, Py_ssize_t n)
 {
-    GR_OR_NONE(n == 15);
+    GR_OR_NONE(n == 16);
     GR_TRY
     auto* f = reinterpret_cast<decltype(&gr_cache_attend)>(PyLong_AsVoidPtr(a[0]));
+    auto* bytes = reinterpret_cast<decltype(&gr_attend_workspace_bytes)>(PyLong_AsVoidPtr(a[15]));
     gr_cache_layout L;
     void* values;
     const at::Tensor *q = tensor(a[1]), *keys = cache_of(a + 2, &L, &values), *table, *offsets, *positions;
-    GR_OR_NONE(f && q && keys && L.format == GR_Q4 && q->dim() == 3 && (q->scalar_type() == at::kBFloat16 || q->scalar_type() == at::kHalf));
+    GR_OR_NONE(f && bytes && q && keys && L.format == GR_Q4 && q->dim() == 3 && (q->scalar_type() == at::kBFloat16 || q->scalar_type() == at::kHalf));
     const c10::Device dev = keys->device();
     const long long T = q->size(0), heads = q->size(1);
     GR_OR_NONE(T < (1ll << 31) && heads <= GR_MAX_HEADS && rows_of(a[1], q->scalar_type(), dev, T, heads, L.dim));
@@ -333,7 +334,9 @@ PyObject* attend(PyObject*, PyObject* const* a, Py_ssize_t n)
     GR_OR_NONE(table->dim() == 2 && table->size(0) < (1ll << 31) - 1 && table->size(1) < (1ll << 31) && offsets->dim() == 1 && offsets->size(0) == table->size(0) + 1
                && positions->dim() == 1 && positions->size(0) == T);
     const at::Tensor *workspace = tensor(a[12]), *out = rows_of(a[13], q->scalar_type(), dev, T, heads, L.dim), *status = tensor(a[14]);
-    GR_OR_NONE(workspace && out && status && workspace->device() == dev && status->device() == dev && status->numel() == table->size(0));
+    GR_OR_NONE(workspace && out && workspace->device() == dev && workspace->scalar_type() == at::kByte && workspace->is_contiguous());
+    const size_t least = bytes(L.heads, (int)heads, L.dim, (int)table->size(0), (int)T);
+    GR_OR_NONE(least > 0 && (size_t)workspace->numel() >= least && is_plain(a[14], at::kInt, dev, false, &status) && status->numel() == table->size(0));
     const double scale = a[10] == Py_None ? pow((double)L.dim, -0.5) : PyFloat_AsDouble(a[10]);
     const long window = PyLong_AsLong(a[11]);
     GR_OR_NONE(!PyErr_Occurred() && window >= 0 && window < (1l << 31));
@@ -345,8 +348,7 @@ PyObject* attend(PyObject*, PyObject* const* a, Py_ssize_t n)
     GR_CATCH
 }
 
-// logprobs(function, logits, tokens, top, temperature, logprob, entropy, top_token, top_logprob, status) -> its answer or None.  (The last five are the
-// binding's own, made for the shape.)
+// logprobs(function, logits, tokens, top, temperature, logprob, entropy, top_token, top_logprob, status) -> its answer or None.
 PyObject* logprobs(PyObject*, PyObject* const* a, Py_ssize_t n)
 {
     GR_OR_NONE(n == 10);
@@ -363,7 +365,7 @@ PyObject* logprobs(PyObject*, PyObject* const* a, Py_ssize_t n)
     const long top = PyLong_AsLong(a[3]);
     const double temperature = PyFloat_AsDouble(a[4]);
     GR_OR_NONE(!PyErr_Occurred() && top >= 0 && top <= GR_MAX_SELECT && given <= GR_MAX_GIVEN);
-    for (int i = 0; i < 5; i++) GR_OR_NONE((own[i] = tensor(a[5 + i])) && own[i]->device() == dev);
+    for (int i = 0; i < 5; i++) GR_OR_NONE(is_plain(a[5 + i], i == 2 || i == 4 ? at::kInt : at::kFloat, dev, false, &own[i]));
     GR_OR_NONE(own[0]->numel() == R * given && own[1]->numel() == R && own[2]->numel() == R * top && own[3]->numel() == R * top && own[4]->numel() == R);
     GR_OR_NONE(!tokens || top == 0 || tokens->data_ptr() != own[2]->data_ptr());
     void* stream;

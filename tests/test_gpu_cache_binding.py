@@ -1,5 +1,7 @@
 """The two ways of the tensor front ends of caches and log probabilities (the compiled module's and the one in Python): the same results, and the same
 refusals, whichever a call takes; what is refused writes nothing."""
+import dataclasses
+
 import pytest
 import torch
 
@@ -124,6 +126,17 @@ def test_same_refusals(monkeypatch):
         lambda: G.token_logprobs(x.t(), t, 3, out=lp), lambda: G.token_logprobs(x.cpu(), t, 3, out=lp), lambda: G.token_logprobs(x[:1].expand(4, 50), t, 3, out=lp),
         lambda: G.token_logprobs(x, lp.top_token, 3, out=G.Logprobs(torch.zeros(4, 3, device="cuda"), lp.entropy, lp.top_token, lp.top_logprob, lp.status, (4, 3, 3))),
         lambda: G.token_logprobs(x, torch.zeros(4, 65, **I32)),
+        # results whose parts were replaced by ones that do not hold what the call writes
+        lambda: G.cache_attend(q, kv, table, offsets, positions, out=dataclasses.replace(r, workspace=r.workspace[:-1])),
+        lambda: G.cache_attend(q, kv, table, offsets, positions, out=dataclasses.replace(r, workspace=r.workspace[::2])),
+        lambda: G.cache_attend(q, kv, table, offsets, positions, out=dataclasses.replace(r, out=r.out[:9])),
+        lambda: G.cache_attend(q, kv, table, offsets, positions, out=dataclasses.replace(r, status=r.status[:2])),
+        lambda: G.cache_attend(q, kv, table, offsets, positions, out=dataclasses.replace(r, status=r.status.short())),
+        lambda: G.token_logprobs(x, t, 3, out=dataclasses.replace(lp, logprob=lp.logprob.half())),
+        lambda: G.token_logprobs(x, t, 3, out=dataclasses.replace(lp, entropy=lp.entropy[:3])),
+        lambda: G.token_logprobs(x, t, 3, out=dataclasses.replace(lp, top_token=lp.top_token.t())),
+        lambda: G.token_logprobs(x, t, 3, out=dataclasses.replace(lp, top_logprob=lp.top_logprob.cpu())),
+        lambda: G.token_logprobs(x, t, 3, out=dataclasses.replace(lp, status=lp.status.short())),
     ]
     kept = [z.clone() for z in (kv.keys, wide.keys, wide.values, q, r.out, lp.logprob, lp.top_token, *pair)]
     for i, call in enumerate(wrong):
