@@ -17,7 +17,7 @@
 // as (m, sum, product) in the workspace; a second kernel joins the pieces in the order of the tokens, so results do not depend on which CTA was first.
 //
 // What bounds it.  64 rows of 6000 tokens, 8 heads of 128 dims, 4 query heads each: 107 us, 64 % of the copy rate; 81 without the arithmetic.  16
-// tokens of a head take 300 warp instructions (80 of them the shifts and ANDs of their 256 words, 20 matrix instructions), which the
+// tokens of a head take 310 warp instructions (80 of them the shifts and ANDs of their 256 words, 20 matrix instructions), which the
 // SMs issue at half of their rate, 16 warps of 128 registers each; three CTAs of 168 registers are as fast, five of 96 spill (149 us).  36 query rows
 // (nine tokens of four heads): 126 us where the bytes take 18; matrix instructions of this kind at their full rate would take 30, and it has the same
 // half of the issue slots, barriers between making operands and using them among them (four warps that each made their own for 16 query rows: 163).
