@@ -412,8 +412,8 @@ __device__ __forceinline__ unsigned quantise(const unsigned long long (&x)[4], u
         code[2 * i] = (int)(unsigned)y;
         code[2 * i + 1] = (int)(unsigned)(y >> 32);
     }
-    // (fp16 scales below 2^-14 are so coarse that quotients below -8 come up)
-    if (most_left >= half || (scale & 0x7c00u) == 0) {
+    // (fp16 scales below 2^-14 are so coarse that quotients below -8 come up, and where the scale is clamped they are as small as elements are large)
+    if (most_left >= half || (scale & 0x7c00u) == 0 || (scale & 0x7fffu) == 0x7bffu) {
 #pragma unroll
         for (int i = 0; i < 8; i++) {
             const float r = i & 1 ? f_hi(left[i / 2]) : f_lo(left[i / 2]);
