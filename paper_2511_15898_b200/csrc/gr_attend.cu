@@ -14,7 +14,7 @@
 // a CTA, however ragged the rows are.  Up to 16 query rows: a CTA of four warps, each takes 32 of a unit's tokens for all of them and brings them
 // itself, the next ones while it works on these (cp.async.bulk into a ring of its own).  More: a CTA of up to eight warps, which
 // make the operands of 64 tokens together and each take all of them for eight query rows.  What a CTA does not finish it leaves
-// as (m, sum, product) in the workspace; a second kernel joins the pieces in the order of the tokens, so results do not depend on which CTA was first.
+// as (m, sum, f, product) in the workspace; a second kernel joins the pieces in the order of the tokens, so results do not depend on which CTA was first.
 //
 // What bounds it.  64 rows of 6000 tokens, 8 heads of 128 dims, 4 query heads each: 107 us, 64 % of the copy rate; 81 without the arithmetic.  16
 // tokens of a head take 310 warp instructions (80 of them the shifts and ANDs of their 256 words, 20 matrix instructions), which the
@@ -72,7 +72,7 @@ struct Shape {
     static int ctas(int warps) { return kRows ? std::max(1, std::min((J <= 4 ? 16 : 8) / warps, 227 * 1024 / (kSmem + 2560))) : kCtas; }
 };
 constexpr int kMaxStages = 4;
-__host__ __device__ inline size_t piece_floats(int tile_rows, int dim) { return (size_t)tile_rows * (dim + 2); }
+__host__ __device__ inline size_t piece_floats(int tile_rows, int dim) { return (size_t)tile_rows * (dim + 3); }      // m, l, f, product
 
 // ---------------------------------------------------------------- instructions
 
@@ -218,7 +218,7 @@ struct State {
     uint4 q[NT][J];                            // the queries as operands, scaled
     unsigned sum[NT][(J + 3) / 4];             // -8 2^-24 times the queries' sums by groups, in two fp16 parts, as operands (group t, t + 4)
     float f[NT][2];                            // from products to x, positive
-    float m[NT][2], ref[NT][2], l[NT][2];      // m: no product is above it; ref: its x, or 0 where there is none
+    float m[NT][2], ref[NT][2], l[NT][2];      // m: no product is above it; ref: the same, or 0 where there is none
     float o[NT][2 * J][4], off[NT][4];
 };
 
@@ -255,9 +255,12 @@ __device__ __forceinline__ void load_queries(State<J, NT>& s, const AttendArgs& 
         most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 1));
         most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 2));
         int up = 140 - (int)(__float_as_uint(most) >> 23) + 127;             // exponent field of 2^(13 - exponent of most)
-        up = most > 0.f && most < INFINITY ? min(max(up, 1), 254) : 127;
+        up = most > 0.f && most < INFINITY ? min(max(up, 1), 253) : 127;
         const float by = copysignf(__uint_as_float((unsigned)up << 23), A.scale);        // (a negative scale turns the queries around)
-        const float back = fmaxf(A.scale * 16777216.f / by, 1e-30f);
+        // (2^24 / by goes onto the scale from the side on which nothing overflows that is not beyond 2^100.  From there on, products that differ at all,
+        // which they do by 2^-72 at least, are so far apart that the largest alone has weight, as at 2^100; below 1e-30 no two are told apart)
+        const float size = fabsf(A.scale), inverse = __uint_as_float((unsigned)(254 - up) << 23);
+        const float back = fminf(fmaxf(up < 127 ? size * 16777216.f * inverse : size * (16777216.f * inverse), 1e-30f), 1.267650600e30f);
         s.f[x][0] = __shfl_sync(0xffffffffu, back, 8 * t); s.f[x][1] = __shfl_sync(0xffffffffu, back, 8 * t + 4);
 #pragma unroll
         for (int j = 0; j < J; j += 4) s.sum[x][j / 4] = 0u;
@@ -386,8 +389,8 @@ __device__ __forceinline__ void eat(State<J, NT>& s, const uint4* ready, const c
 #pragma unroll
                 for (int o = 4; o < 32; o *= 2) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
                 m = m > s.m[n][z] ? m + kHeadroom / s.f[n][z] : s.m[n][z];
-                const float ref = m == -INFINITY ? 0.f : m * s.f[n][z];
-                by[z] = s.m[n][z] == -INFINITY ? 1.f : exp2_of(s.ref[n][z] - ref);       // (nothing has been added up)
+                const float ref = m == -INFINITY ? 0.f : m;
+                by[z] = s.m[n][z] == -INFINITY ? 1.f : exp2_of((s.ref[n][z] - ref) * s.f[n][z]);       // (nothing has been added up)
                 s.m[n][z] = m;
                 s.ref[n][z] = ref;
                 s.l[n][z] *= by[z];
@@ -403,13 +406,16 @@ __device__ __forceinline__ void eat(State<J, NT>& s, const uint4* ready, const c
     unsigned p[NT][2][2];
 #pragma unroll
     for (int n = 0; n < NT; n++) {
+        const unsigned long long down = f_pack(-s.ref[n][0], -s.ref[n][1]), f = f_pack(s.f[n][0], s.f[n][1]);
 #pragma unroll
         for (int b = 0; b < 2; b++) {
             float e[4];
 #pragma unroll
-            for (int z = 0; z < 4; z++) {
-                e[z] = exp2_of(fmaf(x[n][b][z], s.f[n][z & 1], -s.ref[n][z & 1]));
-                s.l[n][z & 1] += e[z];
+            for (int z = 0; z < 4; z += 2) {
+                // (the difference first, which is exact where it tells: scores that 32 bits do not resolve keep their order, and equal ones their weight)
+                const unsigned long long y = mul2(add2(f_pack(x[n][b][z], x[n][b][z + 1]), down), f);
+                e[z] = exp2_of(f_lo(y)); e[z + 1] = exp2_of(f_hi(y));
+                s.l[n][0] += e[z]; s.l[n][1] += e[z + 1];
             }
             p[n][b][0] = transposed(pack_h2(e[0], e[1]));
             p[n][b][1] = transposed(pack_h2(e[2], e[3]));
@@ -715,7 +721,7 @@ attend_kernel(const __grid_constant__ AttendArgs A)
                 for (int x = 0; x < NT; x++)
 #pragma unroll
                     for (int z = 0; z < 2; z++) {
-                        s_m[warp][8 * x + 2 * t + z] = s.m[x][z] == -INFINITY ? -INFINITY : s.ref[x][z];
+                        s_m[warp][8 * x + 2 * t + z] = s.m[x][z];
                         s_l[warp][8 * x + 2 * t + z] = s.l[x][z];
                     }
             }
@@ -731,8 +737,8 @@ attend_kernel(const __grid_constant__ AttendArgs A)
 #pragma unroll
                     for (int k = 0; k < kEaters; k++) m = fmaxf(m, s_m[k][i]);
 #pragma unroll
-                    for (int k = 0; k < kEaters; k++) l += s_m[k][i] == -INFINITY ? s_l[k][i] : s_l[k][i] * exp2_of(s_m[k][i] - m);      // (0, or NaN)
-                    if (s.m[x][z] != -INFINITY) times(s, x, z, exp2_of(s.ref[x][z] - m));
+                    for (int k = 0; k < kEaters; k++) l += s_m[k][i] == -INFINITY ? s_l[k][i] : s_l[k][i] * exp2_of((s_m[k][i] - m) * s.f[x][z]);      // (0, or NaN)
+                    if (s.m[x][z] != -INFINITY) times(s, x, z, exp2_of((s.m[x][z] - m) * s.f[x][z]));
                     s.m[x][z] = m; s.l[x][z] = l;
                 }
 #pragma unroll
@@ -771,10 +777,10 @@ attend_kernel(const __grid_constant__ AttendArgs A)
                     const int i = (kRows ? warp * 8 * NT : 0) + 8 * x + 2 * t + z;
                     if (i >= item_rows) continue;
                     if (!complete) {
-                        if (g == 0) { piece[i] = kRows && s.m[x][z] != -INFINITY ? s.ref[x][z] : s.m[x][z]; piece[tile_rows + i] = s.l[x][z]; }
+                        if (g == 0) { piece[i] = s.m[x][z]; piece[tile_rows + i] = s.l[x][z]; piece[2 * tile_rows + i] = s.f[x][z]; }
 #pragma unroll
                         for (int j = 0; j < J; j++)
-                            *reinterpret_cast<float4*>(piece + 2 * tile_rows + i * D + 32 * j + 4 * g) =
+                            *reinterpret_cast<float4*>(piece + 3 * tile_rows + i * D + 32 * j + 4 * g) =
                                 make_float4(s.o[x][2 * j][z], s.o[x][2 * j][z + 2], s.o[x][2 * j + 1][z], s.o[x][2 * j + 1][z + 2]);
                         continue;
                     }
@@ -860,9 +866,10 @@ attend_join_kernel(const __grid_constant__ AttendArgs A, int tile_rows, int dim)
             for (int u = 0; u < kAhead; u++)
 #pragma unroll
                 for (int z = 0; z < V; z++)
-                    if (k0 + u < count) v[u][z] = *reinterpret_cast<const float4*>(piece(k0 + u) + 2 * tile_rows + i * dim + min(4 * (lane + 32 * z), dim - 4));
+                    if (k0 + u < count) v[u][z] = *reinterpret_cast<const float4*>(piece(k0 + u) + 3 * tile_rows + i * dim + min(4 * (lane + 32 * z), dim - 4));
         };
         load(0);
+        const float f = pieces[(2 * (size_t)first + 1) * size + 2 * tile_rows + i];
         float m = -INFINITY, l = 0.f;
         float4 sum[V];
 #pragma unroll
@@ -875,7 +882,7 @@ attend_join_kernel(const __grid_constant__ AttendArgs A, int tile_rows, int dim)
 #pragma unroll
             for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
             top = fmaxf(top, m);
-            const float down = m == -INFINITY ? 1.f : exp2_of(m - top), by = pm == -INFINITY ? 1.f : exp2_of(pm - top);      // (0 or NaN throughout where m is -infinity)
+            const float down = m == -INFINITY ? 1.f : exp2_of((m - top) * f), by = pm == -INFINITY ? 1.f : exp2_of((pm - top) * f);      // (0 or NaN throughout where m is -infinity)
             pl *= by;
 #pragma unroll
             for (int o = 16; o > 0; o >>= 1) pl += __shfl_xor_sync(0xffffffffu, pl, o);
@@ -912,7 +919,7 @@ attend_join_kernel(const __grid_constant__ AttendArgs A, int tile_rows, int dim)
 #pragma unroll
             for (int z = 0; z < V; z++) sum[z] = make_float4(0.f, 0.f, 0.f, 0.f);
             for (int k = 0; k < kJoinWarps; k++) {
-                const float by = s_m[k] == -INFINITY ? 1.f : exp2_of(s_m[k] - top);
+                const float by = s_m[k] == -INFINITY ? 1.f : exp2_of((s_m[k] - top) * f);
                 l = fmaf(s_l[k], by, l);
 #pragma unroll
                 for (int z = 0; z < V; z++) {
