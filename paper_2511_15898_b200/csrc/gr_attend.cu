@@ -7,8 +7,11 @@
 // (subnormal numbers, exact in the products), so a word of eight codes becomes operands by one shift and four ANDs; the 16 goes into
 // the queries, or into the result.  Queries are scaled by a power of two that brings a row's largest to 2^13 .. 2^14: exact.
 // Keys and values are the 16-row operand (tokens, and depth), query rows the 8 columns: a decode step of eight query heads or
-// tokens to a key head wastes nothing.  Rounded to fewer bits: p (11 bits) and p s (11 bits) before the second product; both are relative to
-// themselves, 2^-12 each, against an output of 8 or 11 bits.  x, m, sums of p and both products are fp32.
+// tokens to a key head wastes nothing.  Rounded to fewer bits: p and p s, to fp16 before the second product, as codes are there: 2^-12 of themselves each,
+// against an output of 8 or 11 bits, as long as they are normal fp16 numbers.  So p is held as 2^lift p (kLift), and what is not a normal number
+// then is off by 2^-35 of the largest weight: thousands of tokens that share a part of the weight keep it, whatever another token takes, with values
+// of 0.05 as with ones of 5 (a lift of 0 lost such parts).  x, m, sums of p and both products are fp32; weights come from x - m, so scores beyond
+// what fp32 resolves keep their order.
 //
 // Work.  A unit is 128 tokens of a (row, head, tile of query rows), or 64; the units of the call in that order are cut into equal shares, one to
 // a CTA, however ragged the rows are.  Up to 16 query rows: a CTA of four warps, each takes 32 of a unit's tokens for all of them and brings them
@@ -33,8 +36,12 @@ constexpr int kEaters = 4;                     // warps of a CTA that takes up t
 constexpr int kMostWarps = 8;                  // of one that takes more, 8 each
 constexpr int kBite = 32;                      // tokens that a warp takes at a time
 // How far above the largest x met the reference is put (p stays at or below 1): at 0 it has to follow every few tokens (36 query rows 141 -> 136 us, a
-// decode batch 115 -> 111).  Weights below 2^-10 of the largest, for 2^-14, are subnormal fp16 numbers, good to 2^-21 of it.
+// decode batch 115 -> 111).
 constexpr float kHeadroom = 4.f;
+// Weights are held as 2^lift p, lift 14 for scales of values up to 2 (values up to 16) and one less for each power of two that a query row's scales go beyond, so
+// that weights and their products with scales are at the upper end of fp16 numbers.  The largest weight is held as 2^10 at least; what is below 2^-14
+// is off by 2^-25, that is by 2^-35 of it.  (Looked at for all 32 tokens by one word or two to a lane: a decode batch 110 -> 111 us, drafts 126 -> 128.)
+constexpr float kLift = 14.f;
 constexpr int kJoinThreads = 256, kJoinWarps = kJoinThreads / 32;
 constexpr unsigned long long kWaitNs = 2000000000ull;      // longest wait for a copy
 
@@ -218,13 +225,40 @@ struct State {
     uint4 q[NT][J];                            // the queries as operands, scaled
     unsigned sum[NT][(J + 3) / 4];             // -8 2^-24 times the queries' sums by groups, in two fp16 parts, as operands (group t, t + 4)
     float f[NT][2];                            // from products to x, positive
-    float m[NT][2], ref[NT][2], l[NT][2];      // m: no product is above it; ref: the same, or 0 where there is none
+    float m[NT][2], ref[NT][2], l[NT][2];      // m: no product is above it; ref: `lift` below m, or 0 where there is none
     float o[NT][2 * J][4], off[NT][4];
 };
 
-// Query rows from flat row `row` on of the item's tokens.
+// Whether one of this lane's share of the scales of four octets' values, of those that are there, is 2 or more in magnitude (fp16 numbers that have
+// the highest bit of their exponent), or none.
+template <int J>
+__device__ __forceinline__ bool large_scales(const char* at, unsigned have, int lane)
+{
+    constexpr int D = 32 * J;
+    const char* from = at + (lane >> 3) * octet_bytes(D) + octet_vscale(D);
+    unsigned share = 0u;
+    if constexpr (J % 2 == 0) {
+        unsigned z[J / 2];
+        load_words<J / 2>(z, from + 2 * J * (lane & 7));
+#pragma unroll
+        for (int i = 0; i < J / 2; i++) share |= z[i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < (J + 1) / 2; i++)
+            if (8 * i + (lane & 7) < 4 * J) share |= *(const unsigned*)(from + 4 * (8 * i + (lane & 7)));
+    }
+    return (share & 0x40004000u) && have >> (lane >> 3) & 1;
+}
+// the lift for scales up to `top` (fp16, a number)
+__device__ __forceinline__ float lift_for(unsigned top)
+{
+    const unsigned bits = __float_as_uint(__half2float(__ushort_as_half((unsigned short)top)));
+    return fminf(kLift, kLift + 1.f + 127.f - (float)((bits + 0x7fffffu) >> 23));
+}
+
+// Query rows from flat row `row` on of the item's tokens.  lifts: their headroom and lift, in units of products, in shared memory.
 template <int J, int NT>
-__device__ __forceinline__ void load_queries(State<J, NT>& s, const AttendArgs& A, const Walk& w, int row, int lane)
+__device__ __forceinline__ void load_queries(State<J, NT>& s, float2* lifts, const AttendArgs& A, const Walk& w, int row, int lane)
 {
     const int g = lane >> 2, t = lane & 3;
 #pragma unroll
@@ -261,6 +295,7 @@ __device__ __forceinline__ void load_queries(State<J, NT>& s, const AttendArgs& 
         // which they do by 2^-72 at least, are so far apart that the largest alone has weight, as at 2^100; below 1e-30 no two are told apart)
         const float size = fabsf(A.scale), inverse = __uint_as_float((unsigned)(254 - up) << 23);
         const float back = fminf(fmaxf(up < 127 ? size * 16777216.f * inverse : size * (16777216.f * inverse), 1e-30f), 1.267650600e30f);
+        if (t == 0) lifts[8 * x + g] = make_float2(kHeadroom / back, kLift / back);
         s.f[x][0] = __shfl_sync(0xffffffffu, back, 8 * t); s.f[x][1] = __shfl_sync(0xffffffffu, back, 8 * t + 4);
 #pragma unroll
         for (int j = 0; j < J; j += 4) s.sum[x][j / 4] = 0u;
@@ -287,6 +322,7 @@ __device__ __forceinline__ void load_queries(State<J, NT>& s, const AttendArgs& 
             for (int j = 0; j < 2 * J; j++) s.o[x][j][z] = 0.f;
         }
     }
+    __syncwarp();                              // (lifts)
 }
 
 // Operands out of two octets' words: of keys rows are tokens, four dims of eight to a step; of values rows are dims.
@@ -313,7 +349,7 @@ __device__ __forceinline__ void make_operands(uint4* to, const char* at, bool va
 // are there, and each query row's own range which of the tokens it sees; what it does not see stays out whatever is held there.
 // kReady: `ready` holds the two halves' keys and values as operands (else they are made here).
 template <int J, int NT, bool kAll, bool kReady>
-__device__ __forceinline__ void eat(State<J, NT>& s, const uint4* ready, const char* at, int lane, const AttendArgs& A, const Walk& w, int row, int token, unsigned have)
+__device__ __forceinline__ void eat(State<J, NT>& s, float2* lifts, const uint4* ready, const char* at, int lane, const AttendArgs& A, const Walk& w, int row, int token, unsigned have)
 {
     constexpr int D = 32 * J, kOctet = octet_bytes(D);
     const int g = lane >> 2, t = lane & 3;
@@ -359,7 +395,9 @@ __device__ __forceinline__ void eat(State<J, NT>& s, const uint4* ready, const c
             }
         }
     }
-    bool more = false;
+    // (looked at here, where nothing waits for it)
+    const bool large = large_scales<J>(at, kAll ? 15u : have, lane);
+    bool more = large;
 #pragma unroll
     for (int n = 0; n < NT; n++) {
         if (!kAll) {
@@ -380,6 +418,34 @@ __device__ __forceinline__ void eat(State<J, NT>& s, const uint4* ready, const c
     }
     if (__any_sync(0xffffffffu, more)) {
         // a product is above the reference: that moves above it, by some more, and what has been added up moves along
+        // (a scale is 2 or more: the lift of the query rows that see it becomes what fits it)
+        const bool larger = __any_sync(0xffffffffu, large);
+        if (larger) {
+            // the largest scales of tokens g + 8 y, numbers only (a row sees those whose x is not -infinity)
+            unsigned most[4];
+#pragma unroll
+            for (int y = 0; y < 4; y++) {
+                const char* from = at + y * kOctet + octet_vscale(D) + 4 * J * (g >> 1) + 2 * (g & 1);
+                most[y] = 0u;
+#pragma unroll
+                for (int j = 0; j < J; j++) {
+                    const unsigned h = *(const unsigned short*)(from + 4 * j) & 0x7fffu;
+                    most[y] = max(most[y], h < 0x7c00u ? h : 0u);
+                }
+            }
+#pragma unroll
+            for (int n = 0; n < NT; n++)
+#pragma unroll
+                for (int z = 0; z < 2; z++) {
+                    unsigned top = 0u;
+#pragma unroll
+                    for (int y = 0; y < 4; y++) top = max(top, x[n][y >> 1][(y & 1) * 2 + z] == -INFINITY ? 0u : most[y]);
+#pragma unroll
+                    for (int o = 4; o < 32; o *= 2) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+                    if (g == 0) lifts[8 * n + 2 * t + z].y = fminf(lifts[8 * n + 2 * t + z].y, lift_for(top) / s.f[n][z]);
+                }
+            __syncwarp();
+        }
 #pragma unroll
         for (int n = 0; n < NT; n++) {
             float by[2];
@@ -388,8 +454,9 @@ __device__ __forceinline__ void eat(State<J, NT>& s, const uint4* ready, const c
                 float m = fmaxf(fmaxf(x[n][0][z], x[n][0][z + 2]), fmaxf(x[n][1][z], x[n][1][z + 2]));
 #pragma unroll
                 for (int o = 4; o < 32; o *= 2) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-                m = m > s.m[n][z] ? m + kHeadroom / s.f[n][z] : s.m[n][z];
-                const float ref = m == -INFINITY ? 0.f : m;
+                const float2 lift = lifts[8 * n + 2 * t + z];
+                m = m > s.m[n][z] ? m + lift.x : s.m[n][z];
+                const float ref = m == -INFINITY ? 0.f : __fsub_ru(m, lift.y);       // (up: no weight passes 2^lift)
                 by[z] = s.m[n][z] == -INFINITY ? 1.f : exp2_of((s.ref[n][z] - ref) * s.f[n][z]);       // (nothing has been added up)
                 s.m[n][z] = m;
                 s.ref[n][z] = ref;
@@ -577,6 +644,7 @@ attend_kernel(const __grid_constant__ AttendArgs A)
     __shared__ __align__(8) unsigned long long s_full[S::kRings][kMaxStages];
     __shared__ unsigned s_have[S::kRings][kMaxStages];
     __shared__ float s_m[kEaters][8 * NT], s_l[kEaters][8 * NT];
+    __shared__ float2 s_lift[kWarps][8 * NT];
     __shared__ long long s_scan[kWarps], s_from, s_to, s_total, s_ctas;
     __shared__ Walk s_eat[kWarps], s_feed[kWarps];         // each warp's own
     __shared__ FeedItem s_item[kWarps];
@@ -671,7 +739,7 @@ attend_kernel(const __grid_constant__ AttendArgs A)
     int done = 0;
     while (done < total) {
         const int row = w.y * tile_rows + (kRows ? warp * 8 * NT : 0);         // this warp's first query row
-        load_queries<J, NT>(s, A, w, row, lane);
+        load_queries<J, NT>(s, s_lift[warp], A, w, row, lane);
         const int item_rows = min(tile_rows, w.n * A.group - w.y * tile_rows), last_row = w.y * tile_rows + item_rows - 1;
         const bool idle = kRows && row > last_row;
         // tokens that all of the item's query rows see
@@ -696,15 +764,15 @@ attend_kernel(const __grid_constant__ AttendArgs A)
                         const unsigned four = have >> (4 * b) & 15;
                         const uint4* from = ready + b * J * 256;
                         if (four == 15 && token + kBite * b >= all_lo && token + kBite * (b + 1) <= all_hi)
-                            eat<J, NT, true, true>(s, from, octets + 4 * b * S::kOctet, lane, A, w, row, token + kBite * b, four);
-                        else if (four) eat<J, NT, false, true>(s, from, octets + 4 * b * S::kOctet, lane, A, w, row, token + kBite * b, four);
+                            eat<J, NT, true, true>(s, s_lift[warp], from, octets + 4 * b * S::kOctet, lane, A, w, row, token + kBite * b, four);
+                        else if (four) eat<J, NT, false, true>(s, s_lift[warp], from, octets + 4 * b * S::kOctet, lane, A, w, row, token + kBite * b, four);
                     }
                 }
                 __syncthreads();
                 if (feeds && ok && done + kStages < total) feed(done + kStages);
             } else {
-                if (have == 15 && token >= all_lo && token + kBite <= all_hi) eat<J, NT, true, false>(s, nullptr, octets, lane, A, w, row, token, have);
-                else if (have) eat<J, NT, false, false>(s, nullptr, octets, lane, A, w, row, token, have);
+                if (have == 15 && token >= all_lo && token + kBite <= all_hi) eat<J, NT, true, false>(s, s_lift[warp], nullptr, octets, lane, A, w, row, token, have);
+                else if (have) eat<J, NT, false, false>(s, s_lift[warp], nullptr, octets, lane, A, w, row, token, have);
                 __syncwarp();
                 if (ok && done + kStages < total) feed(done + kStages);
             }
@@ -721,7 +789,7 @@ attend_kernel(const __grid_constant__ AttendArgs A)
                 for (int x = 0; x < NT; x++)
 #pragma unroll
                     for (int z = 0; z < 2; z++) {
-                        s_m[warp][8 * x + 2 * t + z] = s.m[x][z];
+                        s_m[warp][8 * x + 2 * t + z] = s.m[x][z] == -INFINITY ? -INFINITY : s.ref[x][z];
                         s_l[warp][8 * x + 2 * t + z] = s.l[x][z];
                     }
             }
@@ -738,7 +806,7 @@ attend_kernel(const __grid_constant__ AttendArgs A)
                     for (int k = 0; k < kEaters; k++) m = fmaxf(m, s_m[k][i]);
 #pragma unroll
                     for (int k = 0; k < kEaters; k++) l += s_m[k][i] == -INFINITY ? s_l[k][i] : s_l[k][i] * exp2_of((s_m[k][i] - m) * s.f[x][z]);      // (0, or NaN)
-                    if (s.m[x][z] != -INFINITY) times(s, x, z, exp2_of((s.m[x][z] - m) * s.f[x][z]));
+                    if (s.m[x][z] != -INFINITY) times(s, x, z, exp2_of((s.ref[x][z] - m) * s.f[x][z]));
                     s.m[x][z] = m; s.l[x][z] = l;
                 }
 #pragma unroll
@@ -777,7 +845,7 @@ attend_kernel(const __grid_constant__ AttendArgs A)
                     const int i = (kRows ? warp * 8 * NT : 0) + 8 * x + 2 * t + z;
                     if (i >= item_rows) continue;
                     if (!complete) {
-                        if (g == 0) { piece[i] = s.m[x][z]; piece[tile_rows + i] = s.l[x][z]; piece[2 * tile_rows + i] = s.f[x][z]; }
+                        if (g == 0) { piece[i] = kRows && s.m[x][z] != -INFINITY ? s.ref[x][z] : s.m[x][z]; piece[tile_rows + i] = s.l[x][z]; piece[2 * tile_rows + i] = s.f[x][z]; }
 #pragma unroll
                         for (int j = 0; j < J; j++)
                             *reinterpret_cast<float4*>(piece + 3 * tile_rows + i * D + 32 * j + 4 * g) =
