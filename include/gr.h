@@ -465,7 +465,8 @@ typedef struct gr_cache_layout {
  * of the first `rot` dims of a key or query, pair c is turned by the angle p * frequencies[c],
  *   a' = a cos - b sin,  b' = b cos + a sin,
  * with (a, b) dims (c, c + rot / 2), or (2 c, 2 c + 1) if `interleaved`.  The angle is a 64-bit number, its cosine and sine are rounded to
- * 32 bits, products and sums are rounded to 32 bits one by one, the result once more, to what holds it.
+ * 32 bits, products and sums are rounded to 32 bits one by one, the result once more, to what holds it.  Cosine and sine of angles of 2^50 and
+ * more in magnitude, next to which 64-bit numbers are a fifth apart and more, are NaN, as they are where an angle is no number.
  *   k, v      [tokens, heads, dim] of type dtype (GR_F32, GR_BF16, GR_F16): (i, h) begins i * k_token + h * k_head elements after k.
  *   q, q_out  [tokens, q_heads, dim] likewise, of the same type; q_heads 0: there are none.  Queries of tokens with a negative position
  *             are left as they were in q_out.  q_out may be q, with equal strides; no other array that is written may share a byte with one that

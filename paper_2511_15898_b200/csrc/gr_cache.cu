@@ -39,11 +39,11 @@ struct CacheArgs {
 
 // ---------------------------------------------------------------- angles
 
-// sine and cosine of a, rounded to fp32
+// cosine and sine of a, rounded to fp32; NaN from 2^50 on
 __device__ __forceinline__ float2 cos_sin(double a)
 {
-    // (whole numbers by the sum with 1.5 2^52, whose low word they are: conversions have a fraction of the multiplications' rate; the
-    // quadrant counts up to 2^51 of them)
+    if ((__double2hiint(a) & 0x7fffffff) >= 0x43100000) a = NAN;
+    // (whole numbers by the sum with 1.5 2^52, whose low word they are, up to 2^51: conversions have a fraction of the multiplications' rate)
     const double magic = 6755399441055744.0, whole = fma(a, 0.63661977236758134308, magic), k = whole - magic;     // 2 / pi
     double r = fma(-k, 1.57079632679489655800e+00, a);                      // pi / 2 in two parts
     r = fma(-k, 6.12323399573676603587e-17, r);
