@@ -489,7 +489,8 @@ int gr_cache_append(void* keys, void* values, const gr_cache_layout* layout, con
 /*
  * gr_cache_read -- keys and values of listed slots, as numbers: k[i], v[i] become what slot slots[i] holds, rounded once to dtype (GR_F32,
  * GR_BF16, GR_F16); zeros for a slot outside the cache.  A slot may be listed any number of times.
- *   k, v   [tokens, heads, dim]: (i, h) begins i * k_token + h * k_head elements after k, and likewise for v.  No two places may share an element.
+ *   k, v   [tokens, heads, dim]: (i, h) begins i * k_token + h * k_head elements after k, and likewise for v.  No two places of them may share a
+ *          byte, nor one with the cache or the slots (k and v may lie between one another's places).
  */
 int gr_cache_read(const void* keys, const void* values, const gr_cache_layout* layout, const long long* slots, int tokens,
                   int dtype, void* k, long long k_token, long long k_head, void* v, long long v_token, long long v_head,

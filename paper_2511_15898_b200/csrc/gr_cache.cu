@@ -929,13 +929,17 @@ int gr_cache_read(const void* keys, const void* values, const gr_cache_layout* l
     const long long ks[2] = {k_token, k_head}, vs[2] = {v_token, v_head}, size[2] = {tokens, L.heads};
     if (!gr::apart(L.dim, ks, size, 2) || !gr::apart(L.dim, vs, size, 2)) return GR_E_INVALID;
     if (tokens == 0) return GR_OK;
-    if (!slots || !k || !v) return GR_E_NULL;
-    if (k == v) return GR_E_INVALID;
+    if (!k || !v) return GR_E_NULL;
     const int e = gr::type_size(dtype);
     if (((uintptr_t)k & (uintptr_t)(e - 1)) || ((uintptr_t)v & (uintptr_t)(e - 1))) return GR_E_ALIGN;
+    const gr::Places out_k = gr::rows_places(k, e, L.dim, k_token, k_head, tokens, L.heads), out_v = gr::rows_places(v, e, L.dim, v_token, v_head, tokens, L.heads);
+    if (gr::meet(out_k, out_v)) return GR_E_INVALID;
     const gr::Span written[2] = {gr::rows_span(k, e, L.dim, k_token, k_head, tokens, L.heads), gr::rows_span(v, e, L.dim, v_token, v_head, tokens, L.heads)};
     const gr::Span held[2] = {gr::cache_span(keys, L), L.format == GR_Q4 ? gr::Span{0, 0} : gr::cache_span(values, L)};
     for (const gr::Span& a : held) for (const gr::Span& b : written) if (gr::meet(a, b)) return GR_E_INVALID;
+    if (!slots) return GR_E_NULL;
+    const gr::Places read = gr::bytes_at(slots, 8ll * tokens);
+    if (gr::meet(out_k, read) || gr::meet(out_v, read)) return GR_E_INVALID;
     gr::ReadArgs R = {};
     gr::CacheArgs& A = R.c;
     A.keys = (char*)keys; A.values = (char*)values;

@@ -50,7 +50,7 @@ inline bool apart(long long unit, const long long* step, const long long* size, 
 // Whether strides of what is read are ones (31 bits; that of a single token or head is not looked at).
 inline bool counted(long long token, long long head, int tokens, int heads)
 {
-    return (tokens <= 1 || (token >= 0 && token < (1ll << 31))) && (heads <= 1 || (head >= 0 && head < (1ll << 31)));
+    return (tokens <= 1 || (token >= 0 && token < (1ll << 31) && token <= (1ll << 58) / tokens)) && (heads <= 1 || (head >= 0 && head < (1ll << 31)));
 }
 
 // First byte and the one behind the last of strided places.
@@ -61,6 +61,51 @@ inline Span span_of(const void* p, long long unit, const long long* step, const 
     return {(uintptr_t)p, (uintptr_t)p + (uintptr_t)unit};
 }
 inline bool meet(Span a, Span b) { return a.lo < b.hi && b.lo < a.hi; }
+
+// Where the pieces of a strided array lie, `unit` bytes each, the level of the largest step first; nowhere: unit 0.
+struct Places { uintptr_t at; long long unit; int levels; long long step[3], size[3]; };
+inline Places places_of(const void* p, long long unit, const long long* step, const long long* size, int count)
+{
+    Places a = {(uintptr_t)p, unit, 0, {}, {}};
+    for (int i = 0; i < count; i++) {
+        if (size[i] <= 0) a.unit = 0;
+        if (size[i] <= 1 || step[i] == 0) continue;
+        int at = a.levels++;
+        for (; at > 0 && a.step[at - 1] < step[i]; at--) { a.step[at] = a.step[at - 1]; a.size[at] = a.size[at - 1]; }
+        a.step[at] = step[i]; a.size[at] = size[i];
+    }
+    return a;
+}
+// Whether a piece of b meets one of a, by the levels from i and j on, b's beginning d bytes behind a's.  Levels of one step are looked at together (only differences
+// of about d / step leave the levels within anything to do), others piece by piece; `left`: how many more of these.
+inline bool pieces_meet(const Places& a, int i, const Places& b, int j, long long d, int& left)
+{
+    auto span = [](const Places& p, int from) { long long n = p.unit; for (int l = from; l < p.levels; l++) n += p.step[l] * (p.size[l] - 1); return n; };
+    if (d >= span(a, i) || -d >= span(b, j)) return false;
+    if (i == a.levels && j == b.levels) return true;
+    if (--left < 0) return true;
+    auto down = [](long long x, long long s) { return x >= 0 ? x / s : -((-x + s - 1) / s); };
+    const bool both = i < a.levels && j < b.levels && a.step[i] == b.step[j], of_a = both || j == b.levels || (i < a.levels && a.step[i] > b.step[j]);
+    const long long s = of_a ? a.step[i] : b.step[j];
+    // pieces c of a (less those of b): d - c s below what is left of a, above minus what is left of b
+    const long long in_a = span(a, of_a ? i + 1 : i), in_b = span(b, both || !of_a ? j + 1 : j);
+    long long from = down(d - in_a, s) + 1, to = down(d + in_b - 1, s);
+    from = std::max(from, both || !of_a ? 1 - b.size[j] : 0ll); to = std::min(to, of_a ? a.size[i] - 1 : 0ll);
+    for (long long c = from; c <= to; c++) if (pieces_meet(a, of_a ? i + 1 : i, b, both || !of_a ? j + 1 : j, d - c * s, left)) return true;
+    return false;
+}
+// (those within one another at different strides, of more than 2^20 pieces, are taken for it)
+inline bool meet(const Places& a, const Places& b)
+{
+    int left = 1 << 20;
+    return a.unit > 0 && b.unit > 0 && pieces_meet(a, 0, b, 0, (long long)(b.at - a.at), left);
+}
+inline Places bytes_at(const void* p, long long bytes) { return places_of(p, bytes, nullptr, nullptr, 0); }
+inline Places rows_places(const void* p, int e, int dim, long long token, long long head, int tokens, int heads)
+{
+    const long long step[2] = {token * e, head * e}, size[2] = {tokens, heads};
+    return places_of(p, (long long)dim * e, step, size, 2);
+}
 inline Span cache_span(const void* p, const gr_cache_layout& L)
 {
     if (L.format == GR_Q4) {
