@@ -866,7 +866,7 @@ int gr_cache_append(void* keys, void* values, const gr_cache_layout* layout, con
         if (X.q == X.q_out && ((tokens > 1 && X.q_token != X.out_token) || (X.q_heads > 1 && X.q_head != X.out_head))) return GR_E_INVALID;
     }
     if (tokens == 0) return GR_OK;
-    if (!X.k || !X.v || !slots || (rot > 0 && (!positions || !frequencies)) || (queries && (!X.q || !X.q_out))) return GR_E_NULL;
+    if (!X.k || !X.v || (queries && (!X.q || !X.q_out))) return GR_E_NULL;
     const uintptr_t unit = (uintptr_t)(e - 1);
     if (((uintptr_t)X.k & unit) || ((uintptr_t)X.v & unit) || (queries && (((uintptr_t)X.q & unit) || ((uintptr_t)X.q_out & unit)))) return GR_E_ALIGN;
     // (queries may lie among keys and values, as in one projection's output, and be rotated there; the cache lies apart from all of them)
@@ -874,7 +874,20 @@ int gr_cache_append(void* keys, void* values, const gr_cache_layout* layout, con
                               gr::rows_span(X.q, e, L.dim, X.q_token, X.q_head, tokens, X.q_heads), gr::rows_span(X.q_out, e, L.dim, X.out_token, X.out_head, tokens, X.q_heads)};
     const gr::Span held[2] = {gr::cache_span(keys, L), L.format == GR_Q4 ? gr::Span{0, 0} : gr::cache_span(values, L)};
     for (const gr::Span& a : held) for (const gr::Span& b : rows) if (gr::meet(a, b)) return GR_E_INVALID;
-    if (L.format != GR_Q4 && keys == values && L.num_blocks > 0) return GR_E_INVALID;
+    if (L.format != GR_Q4 && gr::meet(gr::cache_places(keys, L), gr::cache_places(values, L))) return GR_E_INVALID;
+    const gr::Places out = gr::rows_places(X.q_out, e, L.dim, X.out_token, X.out_head, tokens, X.q_heads);
+    if (queries) {
+        const gr::Places in[3] = {gr::rows_places(X.k, e, L.dim, X.k_token, X.k_head, tokens, L.heads), gr::rows_places(X.v, e, L.dim, X.v_token, X.v_head, tokens, L.heads),
+                                  gr::rows_places(X.q, e, L.dim, X.q_token, X.q_head, tokens, X.q_heads)};
+        for (int i = 0; i < (X.q == X.q_out ? 2 : 3); i++) if (gr::meet(in[i], out)) return GR_E_INVALID;
+    }
+    if (!slots || (rot > 0 && (!positions || !frequencies))) return GR_E_NULL;
+    const struct { const void* p; long long bytes; } lists[3] = {{slots, 8ll * tokens}, {positions, 4ll * tokens}, {rot > 0 ? frequencies : nullptr, 4ll * rot}};
+    for (const auto& l : lists) {
+        if (!l.p) continue;
+        const gr::Span span = {(uintptr_t)l.p, (uintptr_t)l.p + (uintptr_t)l.bytes};
+        if (gr::meet(held[0], span) || gr::meet(held[1], span) || (queries && gr::meet(out, gr::bytes_at(l.p, l.bytes)))) return GR_E_INVALID;
+    }
     gr::CacheArgs A = {};
     A.keys = (char*)keys; A.values = (char*)values;
     A.block_stride = L.block_stride; A.token_stride = L.token_stride; A.head_stride = L.head_stride;

@@ -100,6 +100,12 @@ inline bool meet(const Places& a, const Places& b)
     int left = 1 << 20;
     return a.unit > 0 && b.unit > 0 && pieces_meet(a, 0, b, 0, (long long)(b.at - a.at), left);
 }
+inline Places cache_places(const void* p, const gr_cache_layout& L)       // (not of 4 bits)
+{
+    const int e = type_size(L.format);
+    const long long step[3] = {L.block_stride * e, L.token_stride * e, L.head_stride * e}, size[3] = {L.num_blocks, L.block_size, L.heads};
+    return places_of(p, (long long)L.dim * e, step, size, 3);
+}
 inline Places bytes_at(const void* p, long long bytes) { return places_of(p, bytes, nullptr, nullptr, 0); }
 inline Places rows_places(const void* p, int e, int dim, long long token, long long head, int tokens, int heads)
 {

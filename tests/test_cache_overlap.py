@@ -60,3 +60,65 @@ def test_read():
     assert G.gr_cache_read(CACHE, CACHE + (1 << 30), big, 0, 1 << 20, G.GR_F16, A, 1024, 128, A + 2 * 64, 1024, 128, 0) == -2
     # slots among the outputs
     assert G.gr_cache_read(CACHE, CACHE + (1 << 30), big, A + 4096, 100, G.GR_F16, A, 1024, 64, A + (1 << 30), 1024, 64, 0) == -1
+
+
+def append(k, v, q, q_out, dim, heads, q_heads, tokens, ks, vs, qs, os, keys=CACHE, values=CACHE + (1 << 30), lay=None, slots=0, positions=0, freq=0, rot=0):
+    x = G.CacheTokens(k, v, q, q_out, G.GR_F16, q_heads, *ks, *vs, *qs, *os)
+    return G.gr_cache_append(keys, values, lay or layout(dim, heads), x, tokens, slots, positions, freq, rot, 0, 0)
+
+
+def test_append():
+    rng = random.Random(2)
+    met = {True: 0, False: 0}
+    for _ in range(4000):
+        dim, heads, q_heads, tokens = 2 * rng.randint(1, 3), rng.randint(1, 3), rng.randint(1, 4), rng.randint(1, 5)
+        os, span = strides(rng, dim, tokens, q_heads)
+        sizes = {"k": heads, "v": heads, "q": q_heads}
+        step = {n: os if rng.random() < 0.5 else strides(rng, dim, tokens, h)[0] for n, h in sizes.items()}
+        at = {n: A + 2 * rng.randint(-2 * span, 2 * span) for n in sizes}
+        if rng.random() < 0.3:
+            at["q"], step["q"] = A, os                      # in place
+        mine = places(A, 2 * dim, [2 * s for s in os], (tokens, q_heads))
+        want = any(places(at[n], 2 * dim, [2 * s for s in step[n]], (tokens, h)) & mine for n, h in sizes.items() if at[n] != A or n != "q")
+        if at["q"] == A and any(n > 1 and a != b for n, a, b in zip((tokens, q_heads), step["q"], os)):
+            want = True                                     # in place at other strides
+        rc = append(at["k"], at["v"], at["q"], A, dim, heads, q_heads, tokens, step["k"], step["v"], step["q"], os)
+        assert rc in (-1, -2) and (rc == -1) == want, (dim, heads, q_heads, tokens, os, step, at)
+        met[want] += 1
+    assert min(met.values()) > 300
+
+
+def test_append_within_a_projection():
+    # [tokens, q heads + 2 heads, dim], of many tokens, queries in place; one element further on
+    T, H, Hq, D = 1 << 19, 8, 32, 128
+    row = (Hq + 2 * H) * D
+    s = (row, D)
+    at = [A + 2 * Hq * D, A + 2 * (Hq + H) * D]
+    assert append(*at, A, A, D, H, Hq, T, s, s, s, s) == -2
+    assert append(at[0] - 2, at[1], A, A, D, H, Hq, T, s, s, s, s) == -1
+    assert append(at[0], at[1], A + (1 << 38), A + 2, D, H, Hq, T, s, s, s, s) == -1
+    assert append(at[0], at[1], A + 2, A, D, H, Hq, T, s, s, s, s) == -1
+
+
+def test_caches():
+    rng = random.Random(3)
+    met = {True: 0, False: 0}
+    for _ in range(2000):
+        dim, heads, block, blocks = 2 * rng.randint(1, 2), rng.randint(1, 3), rng.randint(1, 3), rng.randint(1, 3)
+        span, step = dim, [0, 0, 0]
+        for i in rng.sample(range(3), 3):
+            n = (blocks, block, heads)[i]
+            step[i] = span + rng.choice([0, 0, 1, rng.randint(0, 2 * span)])
+            span += step[i] * (n - 1)
+        lay = layout(dim, heads, block_size=block, num_blocks=blocks, block_stride=step[0], token_stride=step[1], head_stride=step[2])
+        values = CACHE + 2 * rng.randint(-span, span)
+        of = [places(p, 2 * dim, [2 * s for s in step], (blocks, block, heads)) for p in (CACHE, values)]
+        want = bool(of[0] & of[1])
+        rc = append(A, A, 0, 0, dim, heads, 0, 3, (dim, dim), (dim, dim), (0, 0), (0, 0), values=values, lay=lay)
+        assert rc in (-1, -2) and (rc == -1) == want, (dim, step, values - CACHE)
+        met[want] += 1
+    assert min(met.values()) > 200
+    # lists among what is written
+    s, far = (256, 64), A + (1 << 36)
+    for kw in (dict(slots=A + 8), dict(slots=far, positions=A + 512), dict(slots=far, positions=far + 4096, freq=A, rot=2), dict(slots=CACHE + 64), dict(slots=far, positions=CACHE + (1 << 30))):
+        assert append(far - (1 << 32), far - (1 << 32), far - (1 << 33), A, 64, 2, 4, 3, s, s, s, s, **kw) == -1, kw
