@@ -18,6 +18,7 @@
 #include <algorithm>
 #include "gr_host.h"
 #include "gr_list.cuh"
+#include "gr_cache.cuh"
 
 namespace gr {
 
@@ -400,8 +401,18 @@ int gr_token_logprobs(const void* logits, int dtype, int V, long long ld, int ro
     if (!(temperature > 0.f) || !isfinite(temperature) || ld < V || ld > (1ll << 32)) return GR_E_INVALID;
     if (given < 0 || given > GR_MAX_GIVEN || top < 0 || top > GR_MAX_SELECT) return GR_E_INVALID;
     if (rows == 0) return GR_OK;
-    if (!logits || !status || (given > 0 && (!tokens || !logprob)) || (top > 0 && (!top_token || !top_logprob))) return GR_E_NULL;
-    if ((uintptr_t)logits & (dtype == GR_F32 ? 3 : 1)) return GR_E_ALIGN;
+    if (!logits || (given > 0 && (!tokens || !logprob)) || (top > 0 && (!top_token || !top_logprob))) return GR_E_NULL;
+    const int e = gr::type_size(dtype);
+    if ((uintptr_t)logits & (uintptr_t)(e - 1)) return GR_E_ALIGN;
+    // (outputs lie apart from one another and from what is read; the status, looked at last, behind the others)
+    const long long step = ld * e, size = rows;
+    auto of = [&](const void* p, long long each) { return gr::bytes_at(p, p ? 4 * each * rows : 0); };
+    const gr::Places read[2] = {gr::places_of(logits, (long long)V * e, &step, &size, 1), of(tokens, given)};
+    const gr::Places written[5] = {of(logprob, given), of(entropy, 1), of(top_token, top), of(top_logprob, top), of(status, 1)};
+    for (int i = 0; i < 5; i++) {
+        if (i == 4 && !status) return GR_E_NULL;
+        for (int j = 0; j < i + 2; j++) if (gr::meet(written[i], j < 2 ? read[j] : written[j - 2])) return GR_E_INVALID;
+    }
     gr::ProbArgs A;
     A.logits = logits; A.ld = ld; A.V = V; A.rows = rows; A.given = given; A.top = top; A.keep = std::min(top, V);
     A.team = gr::prob_team(V, rows);

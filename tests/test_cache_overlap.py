@@ -122,3 +122,35 @@ def test_caches():
     s, far = (256, 64), A + (1 << 36)
     for kw in (dict(slots=A + 8), dict(slots=far, positions=A + 512), dict(slots=far, positions=far + 4096, freq=A, rot=2), dict(slots=CACHE + 64), dict(slots=far, positions=CACHE + (1 << 30))):
         assert append(far - (1 << 32), far - (1 << 32), far - (1 << 33), A, 64, 2, 4, 3, s, s, s, s, **kw) == -1, kw
+
+
+def test_token_logprobs():
+    rng = random.Random(4)
+    met = {True: 0, False: 0}
+    far = 1 << 36
+
+    def call(at, V, ld, rows, given, top, dtype=G.GR_BF16, status=0):
+        return G.gr_token_logprobs(at["logits"], dtype, V, ld, rows, 1.0, at["tokens"], given, top, at["logprob"], at["entropy"], at["top_token"], at["top_logprob"], status, 0)
+
+    for _ in range(4000):
+        V, rows, given, top = rng.randint(1, 12), rng.randint(1, 4), rng.randint(0, 3), rng.randint(0, 3)
+        ld = V + rng.choice([0, 0, 1, 14])
+        size = {"tokens": 4 * rows * given, "logprob": 4 * rows * given, "entropy": 4 * rows, "top_token": 4 * rows * top, "top_logprob": 4 * rows * top}
+        at = {n: A + (i + 1) * far for i, n in enumerate(size)}
+        at["logits"] = A
+        a, b = rng.sample(list(at), 2)
+        at[b] = at[a] + 4 * rng.randint(-20, 20)
+        bytes_of = {n: places(at[n], size[n], (), ()) for n in size}
+        bytes_of["logits"] = places(at["logits"], 2 * V, (2 * ld,), (rows,))
+        want = {a, b} != {"tokens", "logits"} and bool(bytes_of[a] & bytes_of[b])
+        rc = call(at, V, ld, rows, given, top)
+        assert rc in (-1, -2) and (rc == -1) == want, (V, ld, rows, given, top, a, b, at[b] - at[a])
+        met[want] += 1
+    assert min(met.values()) > 300
+    at = {n: A + (i + 1) * far for i, n in enumerate(("logits", "tokens", "logprob", "entropy", "top_token", "top_logprob"))}
+    for n in ("logits", "tokens", "logprob", "entropy", "top_token", "top_logprob"):
+        assert call(at, 1000, 1000, 4, 2, 5, status=at[n] + 4) == -1, n
+    assert call({**at, "entropy": 0}, 1000, 1000, 4, 2, 5) == -2
+    # an output in the gap between two rows of logits
+    assert call({**at, "logits": A, "entropy": A + 2 * 1000}, 1000, 1024, 4, 0, 0) == -2
+    assert call({**at, "logits": A, "entropy": A + 2 * 1024 - 12}, 1000, 1024, 4, 0, 0) == -1
