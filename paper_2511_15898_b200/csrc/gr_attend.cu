@@ -1093,6 +1093,7 @@ int gr_cache_attend(const void* q, int dtype, int q_heads, long long q_token, lo
     if (rows == 0) return GR_OK;
     if (!offsets || !status || !workspace || (tokens > 0 && (!q || !out || !positions)) || (width > 0 && !table)) return GR_E_NULL;
     if (((uintptr_t)q & 1) || ((uintptr_t)out & 1) || ((uintptr_t)workspace & 31)) return GR_E_ALIGN;
+    if (((uintptr_t)table | (uintptr_t)offsets | (uintptr_t)positions | (uintptr_t)status) & 3) return GR_E_ALIGN;
     const gr::Span written = gr::rows_span(out, 2, L.dim, out_token, out_head, tokens, q_heads);
     if (gr::meet(written, gr::cache_span(cache, L))) return GR_E_INVALID;
     if (gr::meet(written, gr::rows_span(q, 2, L.dim, q_token, q_head, tokens, q_heads))) return GR_E_INVALID;

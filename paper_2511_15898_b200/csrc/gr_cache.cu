@@ -882,6 +882,7 @@ int gr_cache_append(void* keys, void* values, const gr_cache_layout* layout, con
         for (int i = 0; i < (X.q == X.q_out ? 2 : 3); i++) if (gr::meet(in[i], out)) return GR_E_INVALID;
     }
     if (!slots || (rot > 0 && (!positions || !frequencies))) return GR_E_NULL;
+    if (((uintptr_t)slots & 7) || ((uintptr_t)positions & 3) || (rot > 0 && ((uintptr_t)frequencies & 7))) return GR_E_ALIGN;
     const struct { const void* p; long long bytes; } lists[3] = {{slots, 8ll * tokens}, {positions, 4ll * tokens}, {rot > 0 ? frequencies : nullptr, 4ll * rot}};
     for (const auto& l : lists) {
         if (!l.p) continue;
@@ -951,6 +952,7 @@ int gr_cache_read(const void* keys, const void* values, const gr_cache_layout* l
     const gr::Span held[2] = {gr::cache_span(keys, L), L.format == GR_Q4 ? gr::Span{0, 0} : gr::cache_span(values, L)};
     for (const gr::Span& a : held) for (const gr::Span& b : written) if (gr::meet(a, b)) return GR_E_INVALID;
     if (!slots) return GR_E_NULL;
+    if ((uintptr_t)slots & 7) return GR_E_ALIGN;
     const gr::Places read = gr::bytes_at(slots, 8ll * tokens);
     if (gr::meet(out_k, read) || gr::meet(out_v, read)) return GR_E_INVALID;
     gr::ReadArgs R = {};

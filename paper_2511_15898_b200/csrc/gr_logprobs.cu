@@ -404,6 +404,8 @@ int gr_token_logprobs(const void* logits, int dtype, int V, long long ld, int ro
     if (!logits || (given > 0 && (!tokens || !logprob)) || (top > 0 && (!top_token || !top_logprob))) return GR_E_NULL;
     const int e = gr::type_size(dtype);
     if ((uintptr_t)logits & (uintptr_t)(e - 1)) return GR_E_ALIGN;
+    const uintptr_t lists = (given > 0 ? (uintptr_t)tokens | (uintptr_t)logprob : 0) | (top > 0 ? (uintptr_t)top_token | (uintptr_t)top_logprob : 0);
+    if ((lists | (uintptr_t)entropy | (uintptr_t)status) & 3) return GR_E_ALIGN;
     // (outputs lie apart from one another and from what is read; the status, looked at last, behind the others)
     const long long step = ld * e, size = rows;
     auto of = [&](const void* p, long long each) { return gr::bytes_at(p, p ? 4 * each * rows : 0); };
