@@ -471,7 +471,7 @@ typedef struct gr_cache_layout {
  *   q, q_out  [tokens, q_heads, dim] likewise, of the same type; q_heads 0: there are none.  Queries of tokens with a negative position
  *             are left as they were in q_out.  q_out may be q, with equal strides; no other array that is written may share a byte with one that
  *             is read or another that is written, and no two places of q_out may share one.
- *   slots     [tokens], no slot twice.     positions [tokens]: not looked at (and may be NULL) without frequencies, that is rot 0.
+ *   slots     [tokens], no slot twice.     positions [tokens]; without frequencies, that is rot 0, they may be NULL, and all queries are then written.
  *   rot       even, 0 .. dim.              frequencies [rot / 2] double.
  *   Strides of k, v and q below 2^31.
  * Any alignment to the element works; pointers and strides that are multiples of 16 bytes are fastest.
@@ -504,7 +504,9 @@ int gr_cache_read(const void* keys, const void* values, const gr_cache_layout* l
  * prompt's.  The query of head i of a token at position p becomes
  *   out = sum_t w_t v_t / sum_t w_t,   w_t = exp(scale q . k_t),   over the row's tokens t with p - window < t <= p  (window 0: t <= p),
  * k_t, v_t those of key head i / (q_heads / heads) that slot table[r, t / block_size] * block_size + t % block_size holds.
- * What is held in other places does not tell, whatever it is.  A query that sees nothing gets zeros.
+ * What is held in other places does not tell, whatever it is.  A query that sees nothing gets zeros.  One that sees a NaN gets no number anywhere, be the
+ * NaN in one group of a value alone (a token whose weight is nothing beside the largest may be left out).
+ * Weights and their products with the values' scales are rounded to 11 bits each, those far below the largest to 2^-35 of that.
  *   q, out    [tokens, q_heads, dim], GR_BF16 or GR_F16: (i, h) begins i * q_token + h * q_head elements after q, i * out_token + h * out_head after out.
  *             out must not meet q or the cache in memory, and no two of its places may share an element.  What lies behind the last row's
  *             tokens is left as it was.

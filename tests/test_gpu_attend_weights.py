@@ -133,3 +133,23 @@ def test_large_values_that_are_not_seen_do_not_tell(news, group):
     got = G.cache_attend(q, kv, table, offsets, positions, window=20).out
     kv.keys.copy_(kept)
     assert torch.equal(got, G.cache_attend(q, kv, table, offsets, positions, window=20).out)
+
+
+def test_a_group_that_is_no_number():
+    """One group of one token's values: all that see the token are no numbers, all that do not are as before."""
+    n, D = 200, 96
+    kv, table = _sink(3.0, n, 1.0, D)
+    for group, news in ((2, 1), (2, 8), (8, 8)):
+        q = torch.ones(news, group, D, dtype=torch.float16, device="cuda")
+        call = (q, kv, table, torch.tensor([0, news], **I32), torch.arange(n - news, n, **I32))
+        words = kv.keys.view(torch.float16)
+        for token, windows in ((n - 1, (0,)), (50, (0, 100))):
+            want = [G.cache_attend(*call, window=w).out.clone() for w in windows]
+            words[token // 16, 0, token % 16 // 8][(8 * D + D // 2) // 2 + (token % 8 // 2 * (D // 32) + 1) * 2 + token % 2] = float("nan")
+            for w, before in zip(windows, want):
+                got = G.cache_attend(*call, window=w).out
+                sees = torch.tensor([(p >= token and (not w or p - w < token)) for p in range(n - news, n)], device="cuda")
+                assert torch.isnan(got[sees]).all() and torch.equal(got[~sees], before[~sees])
+            kv, table = _sink(3.0, n, 1.0, D)
+            call = (q, kv, *call[2:])
+            words = kv.keys.view(torch.float16)
