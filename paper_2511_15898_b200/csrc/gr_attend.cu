@@ -55,6 +55,7 @@ struct AttendArgs {
     int tile_rows;                             // query rows of an item
     float scale;                               // with log2(e)
     char* ws; int ctas;
+    GR_SPAN(in_q); GR_SPAN(out_q); GR_SPAN(held); GR_SPAN(blocks); GR_SPAN(starts); GR_SPAN(places); GR_SPAN(states); GR_SPAN(room);
 };
 
 // What a CTA says of the piece that it began and did not finish.
@@ -176,9 +177,10 @@ struct Walk {
 };
 __device__ __forceinline__ void walk_row(Walk& w, const AttendArgs& A)
 {
+    if (!GR_WITHIN(A.starts, A.offsets + w.r, 8)) { w.token = w.n = 0; w.p0 = -1; return; }
     w.token = min(max(A.offsets[w.r], 0), A.tokens);
     w.n = min(max(A.offsets[w.r + 1], w.token), A.tokens) - w.token;
-    w.p0 = w.n > 0 ? A.positions[w.token] : -1;
+    w.p0 = w.n > 0 && GR_WITHIN(A.places, A.positions + w.token, 4) ? A.positions[w.token] : -1;
 }
 template <int kTile>
 __device__ __forceinline__ void walk_item(Walk& w, const AttendArgs& A)
@@ -217,6 +219,8 @@ __device__ __forceinline__ long long share_of(long long total, int i, long long 
 {
     return total < (1 << 20) ? (long long)((unsigned)total * (unsigned)i / (unsigned)parts) : total * i / parts;
 }
+
+extern __shared__ __align__(128) char attend_rings[];
 
 // ---------------------------------------------------------------- a warp's share
 
@@ -272,7 +276,7 @@ __device__ __forceinline__ void load_queries(State<J, NT>& s, float2* lifts, con
 #pragma unroll
         for (int j = 0; j < J; j++) {
             unsigned d[4] = {0, 0, 0, 0};
-            if (in) {
+            if (in && GR_WITHIN(A.in_q, p + 32 * j, 16)) {
                 if (A.q_vec) { const uint4 z = *reinterpret_cast<const uint4*>(p + 32 * j); d[0] = z.x; d[1] = z.y; d[2] = z.z; d[3] = z.w; }
                 else {
 #pragma unroll
@@ -335,6 +339,7 @@ __device__ __forceinline__ void make_operands(uint4* to, const char* at, bool va
 {
     constexpr int D = 32 * J, kOctet = octet_bytes(D);
     unsigned w0[J], w1[J];
+    if (!GR_WITHIN(shared_span(attend_rings), at, 2 * kOctet) || !GR_WITHIN(shared_span(attend_rings), to, J * 1024)) return;
     at += (values ? octet_vcode(D) : 0) + 4 * J * lane;
     load_words<J>(w0, at);
     load_words<J>(w1, at + kOctet);
@@ -354,6 +359,7 @@ __device__ __forceinline__ void eat(State<J, NT>& s, float2* lifts, const uint4*
     constexpr int D = 32 * J, kOctet = octet_bytes(D);
     const int g = lane >> 2, t = lane & 3;
     float x[NT][2][4];
+    if (!GR_WITHIN(shared_span(attend_rings), at, 4 * kOctet) || (kReady && !GR_WITHIN(shared_span(attend_rings), ready, J * 4096))) return;
     {
         // what 8 is taken off for: group by group the scale times the queries' sum
 #pragma unroll
@@ -551,6 +557,7 @@ __device__ __forceinline__ void times(State<J, NT>& s, int x, int z, float by)
 __device__ __forceinline__ void store_out(const AttendArgs& A, long long at, const float (&v)[4])
 {
     unsigned short* p = (unsigned short*)A.out + at;
+    if (!GR_WITHIN(A.out_q, p, 8)) return;
     unsigned d[2];
     if (A.dtype == GR_BF16) {
 #pragma unroll
@@ -604,7 +611,7 @@ struct Feeder {
             // (blocks of a multiple of eight tokens; the quotient by a product with the reciprocal, rounded up)
             const unsigned octet = token >> 3, block = A.octets == 1 ? octet : __umulhi(octet, A.by_octets) >> A.shift;
             in = (int)(octet - block * (unsigned)A.octets);
-            if ((int)block < A.width) id = f.row[block];
+            if ((int)block < A.width && GR_WITHIN(A.blocks, f.row + block, 4)) id = f.row[block];
         }
         const bool want = id >= 0 && id < A.num_blocks;
         const unsigned mask = __ballot_sync(0xffffffffu, want);
@@ -618,7 +625,7 @@ struct Feeder {
         __syncwarp();
     }
     // The next unit into place `place` of the ring; `have`: which octets it will hold.  Whether that was the item's last.
-    __device__ __forceinline__ bool bring(const FeedItem& f, char* place, unsigned long long* full, unsigned* have, int lane)
+    __device__ __forceinline__ bool bring(const FeedItem& f, const AttendArgs& A, char* place, unsigned long long* full, unsigned* have, int lane)
     {
         const int at = fed & (kUnits - 1);
         const unsigned bar = smem_addr(full);
@@ -628,7 +635,7 @@ struct Feeder {
             bar_expect(bar, __popc(here) * S::kOctet);
         }
         __syncwarp();
-        if (lane / kOctets == at && bytes > 0) bulk_load(smem_addr(place) + lane % kOctets * S::kOctet, from, bytes, bar);
+        if (lane / kOctets == at && bytes > 0 && GR_WITHIN(A.held, from, bytes) && GR_WITHIN(shared_span(attend_rings), place + lane % kOctets * S::kOctet, bytes)) bulk_load(smem_addr(place) + lane % kOctets * S::kOctet, from, bytes, bar);
         return ++fed == f.units;
     }
 };
@@ -640,7 +647,7 @@ attend_kernel(const __grid_constant__ AttendArgs A)
     using S = Shape<J, NT, kRows>;
     constexpr int D = S::D, kStages = S::kStages, kTile = S::kTile, kWarps = S::kWarps;
     const int tile_rows = A.tile_rows, warps = kRows ? blockDim.x >> 5 : kEaters, threads = 32 * warps;
-    extern __shared__ __align__(128) char rings[];
+    char* rings = attend_rings;
     __shared__ __align__(8) unsigned long long s_full[S::kRings][kMaxStages];
     __shared__ unsigned s_have[S::kRings][kMaxStages];
     __shared__ float s_m[kEaters][8 * NT], s_l[kEaters][8 * NT];
@@ -704,6 +711,7 @@ attend_kernel(const __grid_constant__ AttendArgs A)
     const long long from = s_from;
     const int total = (int)(s_to - from);      // (a share of 2^31 units would take hours)
     AttendNote* note = reinterpret_cast<AttendNote*>(A.ws) + blockIdx.x;
+    if (!GR_WITHIN(A.room, note, sizeof(AttendNote))) return;
     if (total <= 0) {
         if (tid == 0) *note = AttendNote{0, 0, 0, 0, 0, 0, 0, 0};
         return;
@@ -717,7 +725,7 @@ attend_kernel(const __grid_constant__ AttendArgs A)
     // unit `next` of the share
     auto feed = [&](int next) {
         const int place = next % kStages;
-        const bool end = feeder.bring(s_item[warp], ring + place * S::kStage, full + place, held + place, lane);
+        const bool end = feeder.bring(s_item[warp], A, ring + place * S::kStage, full + place, held + place, lane);
         if (next + 1 == total) return;
         if (end) {
             Walk w = s_feed[warp];
@@ -819,8 +827,9 @@ attend_kernel(const __grid_constant__ AttendArgs A)
                         for (int z = 0; z < 2; z++)
 #pragma unroll
                             for (int j = 0; j < J; j++)
-                                *reinterpret_cast<float4*>(to + (8 * x + 2 * t + z) * S::kStep + 32 * j + 4 * g) =
-                                    make_float4(s.o[x][2 * j][z], s.o[x][2 * j][z + 2], s.o[x][2 * j + 1][z], s.o[x][2 * j + 1][z + 2]);
+                                if (GR_WITHIN(shared_span(attend_rings), to + (8 * x + 2 * t + z) * S::kStep + 32 * j + 4 * g, 16))
+                                    *reinterpret_cast<float4*>(to + (8 * x + 2 * t + z) * S::kStep + 32 * j + 4 * g) =
+                                        make_float4(s.o[x][2 * j][z], s.o[x][2 * j][z + 2], s.o[x][2 * j + 1][z], s.o[x][2 * j + 1][z + 2]);
                 }
                 __syncthreads();
                 if (warp < step) {
@@ -845,6 +854,7 @@ attend_kernel(const __grid_constant__ AttendArgs A)
                     const int i = (kRows ? warp * 8 * NT : 0) + 8 * x + 2 * t + z;
                     if (i >= item_rows) continue;
                     if (!complete) {
+                        if (!GR_WITHIN(A.room, piece, piece_floats(tile_rows, D) * sizeof(float))) continue;
                         if (g == 0) { piece[i] = kRows && s.m[x][z] != -INFINITY ? s.ref[x][z] : s.m[x][z]; piece[tile_rows + i] = s.l[x][z]; piece[2 * tile_rows + i] = s.f[x][z]; }
 #pragma unroll
                         for (int j = 0; j < J; j++)
@@ -934,7 +944,7 @@ attend_join_kernel(const __grid_constant__ AttendArgs A, int tile_rows, int dim)
             for (int u = 0; u < kAhead; u++)
 #pragma unroll
                 for (int z = 0; z < V; z++)
-                    if (k0 + u < count) v[u][z] = *reinterpret_cast<const float4*>(piece(k0 + u) + 3 * tile_rows + i * dim + min(4 * (lane + 32 * z), dim - 4));
+                    if (k0 + u < count && GR_WITHIN(A.room, piece(k0 + u), size * sizeof(float))) v[u][z] = *reinterpret_cast<const float4*>(piece(k0 + u) + 3 * tile_rows + i * dim + min(4 * (lane + 32 * z), dim - 4));
         };
         load(0);
         const float f = pieces[(2 * (size_t)first + 1) * size + 2 * tile_rows + i];
@@ -945,7 +955,7 @@ attend_join_kernel(const __grid_constant__ AttendArgs A, int tile_rows, int dim)
         // (the largest of up to 32 pieces at a time: what has been added up moves there)
         for (int k0 = 0; k0 < count; k0 += 32) {
             float pm = -INFINITY, pl = 0.f;
-            if (k0 + lane < count) { const float* p = piece(k0 + lane); pm = p[i]; pl = p[tile_rows + i]; }
+            if (k0 + lane < count && GR_WITHIN(A.room, piece(k0 + lane), size * sizeof(float))) { const float* p = piece(k0 + lane); pm = p[i]; pl = p[tile_rows + i]; }
             float top = pm;
 #pragma unroll
             for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
@@ -1022,12 +1032,13 @@ attend_join_kernel(const __grid_constant__ AttendArgs A, int tile_rows, int dim)
             const int last = (hi + size - 1) / size;
 #pragma unroll 4
             for (int b = lo / size + tid; b < last; b += kJoinThreads) {
+                if (!GR_WITHIN(A.blocks, A.table + (long long)r * A.width + b, 4)) continue;
                 const int id = A.table[(long long)r * A.width + b];
                 bad |= id < 0 || id >= A.num_blocks;
             }
         }
         bad = __syncthreads_or(bad);
-        if (tid == 0) A.status[r] = failed ? GR_CHECK_FAILED : bad ? GR_BAD_ROW : GR_OK;
+        if (tid == 0 && GR_WITHIN(A.states, A.status + r, 4)) A.status[r] = failed ? GR_CHECK_FAILED : bad ? GR_BAD_ROW : GR_OK;
     }
 }
 
@@ -1064,6 +1075,10 @@ static bool attend_shape_ok(int heads, int q_heads, int dim, int rows, int token
 }  // namespace gr
 
 extern "C" {
+
+#ifdef GR_CHECK
+int gr_attend_check(void) { return gr::span_check(); }
+#endif
 
 size_t gr_attend_workspace_bytes(int heads, int q_heads, int dim, int rows, int tokens)
 {
@@ -1108,6 +1123,10 @@ int gr_cache_attend(const void* q, int dtype, int q_heads, long long q_token, lo
     while (A.octets > 2 << A.shift) A.shift++;
     A.by_octets = A.octets > 1 ? (unsigned)(((1ull << (32 + A.shift)) + (unsigned)A.octets - 1) / (unsigned)A.octets) : 0u;
     A.scale = scale * 1.44269504088896340736f;
+    GR_SET_SPAN(A.in_q, gr::rows_span(q, 2, L.dim, q_token, q_head, tokens, q_heads)); GR_SET_SPAN(A.out_q, written); GR_SET_SPAN(A.held, gr::cache_span(cache, L));
+    GR_SET_SPAN(A.blocks, {(uintptr_t)table, (uintptr_t)(table + (size_t)rows * width)}); GR_SET_SPAN(A.starts, {(uintptr_t)offsets, (uintptr_t)(offsets + rows + 1)});
+    GR_SET_SPAN(A.places, {(uintptr_t)positions, (uintptr_t)(positions + tokens)}); GR_SET_SPAN(A.states, {(uintptr_t)status, (uintptr_t)(status + rows)});
+    GR_SET_SPAN(A.room, {(uintptr_t)workspace, (uintptr_t)workspace + gr_attend_workspace_bytes(L.heads, q_heads, L.dim, rows, tokens)});
     A.ws = (char*)workspace;
     gr::Align in, to;
     in.add(q, 2, {tokens > 1 ? q_token : 0, q_heads > 1 ? q_head : 0});

@@ -35,6 +35,7 @@ struct CacheArgs {
     // whole quotients that loops go on by, and 1 / n for first places (small numbers: exact with a half added)
     int by_half, by_heads, by_queries;
     float of_half, of_heads, of_queries;
+    GR_SPAN(in_k); GR_SPAN(in_v); GR_SPAN(in_q); GR_SPAN(out_q); GR_SPAN(held_k); GR_SPAN(held_v);
 };
 
 // ---------------------------------------------------------------- angles
@@ -102,7 +103,8 @@ __device__ __forceinline__ void window_angles(const CacheArgs& A, const Tokens& 
     int tok = (int)(((float)threadIdx.x + 0.5f) * A.of_half), f = threadIdx.x - tok * A.half;
     const int by_tok = A.by_half, by_f = kCacheThreads - by_tok * A.half;
     for (tok += from; tok < to;) {
-        cs[tok * step + angle_at(f)] = cos_sin(w.angle[tok] * A.freq[f]);
+        const float2 turn = cos_sin(w.angle[tok] * A.freq[f]);
+        if (GR_WITHIN(shared_span(cs), cs + tok * step + angle_at(f), sizeof(float2))) cs[tok * step + angle_at(f)] = turn;
         tok += by_tok; f += by_f;
         if (f >= A.half) { f -= A.half; tok++; }
     }
@@ -259,6 +261,8 @@ __device__ __forceinline__ void append_rows(const CacheArgs& A, const Tokens& w,
 #pragma unroll
             for (int u = 0; u < kTok; u++) {
                 some[u] = tok + u < n && e < chunks && (early || (queries ? w.position[tok + u] >= 0 : w.at[tok + u] >= 0));
+                some[u] = some[u] && GR_WITHIN(queries ? A.in_q : values ? A.in_v : A.in_k, src + u * src_step + p.c0, N * sizeof(T))
+                          && GR_WITHIN(queries ? A.in_q : values ? A.in_v : A.in_k, src + u * src_step + p.c1, N * sizeof(T));
                 if (some[u]) { a[u] = load_raw<T, N>(src + u * src_step + p.c0); b[u] = load_raw<T, N>(src + u * src_step + p.c1); }
             }
             if (early) {
@@ -271,13 +275,16 @@ __device__ __forceinline__ void append_rows(const CacheArgs& A, const Tokens& w,
                 if (!some[u]) continue;
                 float x[N], y[N];
                 unpack(x, a[u]); unpack(y, b[u]);
+                if (half > 0 && !GR_WITHIN(shared_span(cs), cs + (tok + u) * step, step * sizeof(float2))) continue;
                 turn_pieces<N>(x, y, p, cs + (tok + u) * step, half, interleaved);
                 if (queries) {
                     T* to = (T*)A.x.q_out + (long long)head * A.x.out_head + (i0 + tok + u) * A.x.out_token;
-                    store_n<T, N>(to + p.c0, x); store_n<T, N>(to + p.c1, y);
+                    if (GR_WITHIN(A.out_q, to + p.c0, N * sizeof(T)) && GR_WITHIN(A.out_q, to + p.c1, N * sizeof(T))) { store_n<T, N>(to + p.c0, x); store_n<T, N>(to + p.c1, y); }
                 } else {
                     C* to = (C*)(values ? A.values : A.keys) + (long long)head * A.head_stride + w.at[tok + u];
-                    store_n<C, N>(to + p.c0, x); store_n<C, N>(to + p.c1, y);
+                    if (GR_WITHIN(values ? A.held_v : A.held_k, to + p.c0, N * sizeof(C)) && GR_WITHIN(values ? A.held_v : A.held_k, to + p.c1, N * sizeof(C))) {
+                        store_n<C, N>(to + p.c0, x); store_n<C, N>(to + p.c1, y);
+                    }
                 }
             }
         }
@@ -314,6 +321,8 @@ __device__ __forceinline__ void append_kind(const CacheArgs& A, const Tokens& w,
                     at[u] = kCache ? w.at[tok + u] : (long long)(i0 + tok + u) * dst_token;
                     some[u] = kCache ? at[u] >= 0 : w.position[tok + u] >= 0;
                 }
+                some[u] = some[u] && GR_WITHIN(kCache ? (kTurn ? A.in_k : A.in_v) : A.in_q, from + u * src_token + p.c0, N * sizeof(T))
+                          && GR_WITHIN(kCache ? (kTurn ? A.in_k : A.in_v) : A.in_q, from + u * src_token + p.c1, N * sizeof(T));
                 if (some[u]) { a[u] = load_raw<T, N>(from + u * src_token + p.c0); b[u] = load_raw<T, N>(from + u * src_token + p.c1); }
             }
 #pragma unroll
@@ -321,8 +330,12 @@ __device__ __forceinline__ void append_kind(const CacheArgs& A, const Tokens& w,
                 if (!some[u]) continue;
                 float x[N], y[N];
                 unpack(x, a[u]); unpack(y, b[u]);
+                if (half > 0 && !GR_WITHIN(shared_span(cs), cs + (tok + u) * step, step * sizeof(float2))) continue;
                 if (kTurn) turn_pieces<N>(x, y, p, cs + (tok + u) * step, half, interleaved);
-                store_n<C, N>(to + at[u] + p.c0, x); store_n<C, N>(to + at[u] + p.c1, y);
+                if (GR_WITHIN(kCache ? (kTurn ? A.held_k : A.held_v) : A.out_q, to + at[u] + p.c0, N * sizeof(C))
+                    && GR_WITHIN(kCache ? (kTurn ? A.held_k : A.held_v) : A.out_q, to + at[u] + p.c1, N * sizeof(C))) {
+                    store_n<C, N>(to + at[u] + p.c0, x); store_n<C, N>(to + at[u] + p.c1, y);
+                }
             }
         }
     }
@@ -471,17 +484,17 @@ append4_kernel(const __grid_constant__ CacheArgs A)
                 const int other = two ? c - half : c + half;
                 const float sign = two ? 1.f : -1.f;
                 Raw<T, 8> x_next, y_next;
-                if (kVec && in && from < A.heads) { x_next = load_raw<T, 8>(row + c); if (pairs) y_next = load_raw<T, 8>(row + other); }
+                if (kVec && in && from < A.heads) { if (GR_WITHIN(A.in_k, row + c, 8 * sizeof(T))) x_next = load_raw<T, 8>(row + c); if (pairs && GR_WITHIN(A.in_k, row + other, 8 * sizeof(T))) y_next = load_raw<T, 8>(row + other); }
                 for (int head = from; head < A.heads; head += every) {
                     float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
                     unsigned long long x2[4];
                     const T* here = row;
                     row += (long long)every * A.x.k_head;
-                    if (in) {
+                    if (in && (kVec || GR_WITHIN(A.in_k, here, D * sizeof(T))) && (half == 0 || GR_WITHIN(shared_span(cs), angle, angle_step(half) * sizeof(float2)))) {
                         if (kVec) {
                             // (a head ahead)
                             const Raw<T, 8> x_raw = x_next, y_raw = y_next;
-                            if (head + every < A.heads) { x_next = load_raw<T, 8>(row + c); if (pairs) y_next = load_raw<T, 8>(row + other); }
+                            if (head + every < A.heads) { if (GR_WITHIN(A.in_k, row + c, 8 * sizeof(T))) x_next = load_raw<T, 8>(row + c); if (pairs && GR_WITHIN(A.in_k, row + other, 8 * sizeof(T))) y_next = load_raw<T, 8>(row + other); }
                             unpack(x, x_raw);
                             if (pairs) {
                                 // (the eight are on one side of their pairs: a difference is a sum with a number of the other sign)
@@ -519,7 +532,7 @@ append4_kernel(const __grid_constant__ CacheArgs A)
                     for (int i = 0; i < 4; i++) x2[i] = f_pack(x[2 * i], x[2 * i + 1]);
                     unsigned scale;
                     const unsigned code = quantise(x2, scale);
-                    if (in) {
+                    if (in && GR_WITHIN(A.held_k, octet, octet_bytes(D))) {
                         *(unsigned*)(octet + (o0 + mine) * (D / 2) + (t * J + j) * 4) = code;
                         if (t == 0) *(unsigned short*)(octet + octet_kscale(D) + ((o0 + mine) * J + j) * 2) = (unsigned short)scale;
                     }
@@ -531,15 +544,15 @@ append4_kernel(const __grid_constant__ CacheArgs A)
                 const T* row = (const T*)A.x.v + (long long)from * A.x.v_head + (long long)(w0 + at) * A.x.v_token;
                 char* octet = A.keys + w.at[tok] + from * head_bytes;
                 Raw<T, 8> x_next;
-                if (kVec && in && from < A.heads) x_next = load_raw<T, 8>(row + c);
+                if (kVec && in && from < A.heads && GR_WITHIN(A.in_v, row + c, 8 * sizeof(T))) x_next = load_raw<T, 8>(row + c);
                 for (int head = from; head < A.heads; head += every) {
                     float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
                     const T* here = row;
                     row += (long long)every * A.x.v_head;
-                    if (in) {
+                    if (in && (kVec || GR_WITHIN(A.in_v, here, D * sizeof(T)))) {
                         if (kVec) {
                             const Raw<T, 8> x_raw = x_next;
-                            if (head + every < A.heads) x_next = load_raw<T, 8>(row + c);
+                            if (head + every < A.heads && GR_WITHIN(A.in_v, row + c, 8 * sizeof(T))) x_next = load_raw<T, 8>(row + c);
                             unpack(x, x_raw);
                         } else {
 #pragma unroll
@@ -553,14 +566,15 @@ append4_kernel(const __grid_constant__ CacheArgs A)
                     const unsigned code = quantise(x2, scale), other = __shfl_xor_sync(0xffffffffu, code, 16);
                     // half words 2 t and 2 t + 1 of this token: the first token's lane writes the former of both, the second's the latter
                     char* to = octet + octet_vcode(D) + (((2 * t + mine) * 4 + (o0 >> 1)) * J + j) * 4;
+                    const bool writes = in && GR_WITHIN(A.held_k, octet, octet_bytes(D));
                     if (both) {
-                        if (in) *(unsigned*)to = mine ? __byte_perm(other, code, 0x7632) : __byte_perm(code, other, 0x5410);
-                    } else if (in) {
+                        if (writes) *(unsigned*)to = mine ? __byte_perm(other, code, 0x7632) : __byte_perm(code, other, 0x5410);
+                    } else if (writes) {
                         char* own = octet + octet_vcode(D) + ((2 * t * 4 + (o0 >> 1)) * J + j) * 4 + 2 * mine;
                         *(unsigned short*)own = (unsigned short)code;
                         *(unsigned short*)(own + 16 * J) = (unsigned short)(code >> 16);
                     }
-                    if (in && t == 0) *(unsigned short*)(octet + octet_vscale(D) + ((o0 >> 1) * J + j) * 4 + 2 * mine) = (unsigned short)scale;
+                    if (writes && t == 0) *(unsigned short*)(octet + octet_vscale(D) + ((o0 >> 1) * J + j) * 4 + 2 * mine) = (unsigned short)scale;
                     octet += every * head_bytes;
                 }
             }
@@ -595,22 +609,24 @@ read_kernel(const __grid_constant__ ReadArgs R)
     for (int r0 = blockIdx.y * teams + threadIdx.x / team; r0 < total; r0 += kRows * A.split * teams) {
         const C* src[kRows];
         T* dst[kRows];
+        bool second[kRows];
 #pragma unroll
         for (int u = 0; u < kRows; u++) {
             const int r = r0 + u * A.split * teams;
-            src[u] = nullptr; dst[u] = nullptr;
+            src[u] = nullptr; dst[u] = nullptr; second[u] = false;
             if (r >= total) continue;
             const int tok = (int)(((float)r + 0.5f) * by_per), row = r - tok * per;
-            const bool second = row >= A.heads;
-            const int head = second ? row - A.heads : row;
+            second[u] = row >= A.heads;
+            const int head = second[u] ? row - A.heads : row;
             const long long i = i0 + tok;
-            dst[u] = second ? (T*)R.v + i * R.v_token + head * R.v_head : (T*)R.k + i * R.k_token + head * R.k_head;
-            if (w.at[tok] >= 0) src[u] = (const C*)(second ? A.values : A.keys) + w.at[tok] + head * A.head_stride;
+            dst[u] = second[u] ? (T*)R.v + i * R.v_token + head * R.v_head : (T*)R.k + i * R.k_token + head * R.k_head;
+            if (w.at[tok] >= 0) src[u] = (const C*)(second[u] ? A.values : A.keys) + w.at[tok] + head * A.head_stride;
         }
         for (int e = in_team; e < chunks; e += team) {
             Raw<C, N> x[kRows];
 #pragma unroll
-            for (int u = 0; u < kRows; u++) if (src[u]) x[u] = load_raw<C, N>(src[u] + e * N);
+            for (int u = 0; u < kRows; u++)
+                if (src[u] && (GR_WITHIN(second[u] ? A.held_v : A.held_k, src[u] + e * N, N * sizeof(C)))) x[u] = load_raw<C, N>(src[u] + e * N);
 #pragma unroll
             for (int u = 0; u < kRows; u++) {
                 if (!dst[u]) continue;
@@ -618,7 +634,7 @@ read_kernel(const __grid_constant__ ReadArgs R)
                 unpack(y, x[u]);
 #pragma unroll
                 for (int i = 0; i < N; i++) y[i] = src[u] ? y[i] : 0.f;
-                store_n<T, N>(dst[u] + e * N, y);
+                if (GR_WITHIN(second[u] ? A.in_v : A.in_k, dst[u] + e * N, N * sizeof(T))) store_n<T, N>(dst[u] + e * N, y);
             }
         }
     }
@@ -704,6 +720,9 @@ read4_kernel(const __grid_constant__ ReadArgs R)
     for (int item = blockIdx.y * kCacheWarps + warp; item < w.runs * A.heads; item += A.split * kCacheWarps) {
         const int run = item / A.heads, head = item - run * A.heads, tok = w.first[run];
         const long long i = w0 + tok;
+        if (!GR_WITHIN(A.held_k, A.keys + w.at[tok] + head * head_bytes, octet_bytes(D))) continue;
+        if (!GR_WITHIN(A.in_k, (T*)R.k + i * R.k_token + head * R.k_head, ((w.size[run] - 1) * R.k_token + D) * sizeof(T))) continue;
+        if (!GR_WITHIN(A.in_v, (T*)R.v + i * R.v_token + head * R.v_head, ((w.size[run] - 1) * R.v_token + D) * sizeof(T))) continue;
         read_octet<T, J, kVec>(A.keys + w.at[tok] + head * head_bytes, (T*)R.k + i * R.k_token + head * R.k_head, (T*)R.v + i * R.v_token + head * R.v_head,
                                R.k_token, R.v_token, (int)(w.slot[tok] & 7), w.size[run], lane);
     }
@@ -714,6 +733,7 @@ read4_kernel(const __grid_constant__ ReadArgs R)
         const long long i = w0 + tok;
         for (int row = blockIdx.y * kCacheWarps + warp; row < 2 * A.heads; row += A.split * kCacheWarps) {
             T* to = row < A.heads ? (T*)R.k + i * R.k_token + row * R.k_head : (T*)R.v + i * R.v_token + (row - A.heads) * R.v_head;
+            if (!GR_WITHIN(row < A.heads ? A.in_k : A.in_v, to, D * sizeof(T))) continue;
             if (kVec) { if (8 * lane < D) store_n<T, 8>(to + 8 * lane, none); }
             else for (int d = lane; d < D; d += 32) to[d] = from_f32<T>(0.f);
         }
@@ -847,6 +867,10 @@ static void launch_read4(ReadArgs& R, bool vec, cudaStream_t st)
 
 extern "C" {
 
+#ifdef GR_CHECK
+int gr_cache_check(void) { return gr::span_check(); }
+#endif
+
 int gr_cache_append(void* keys, void* values, const gr_cache_layout* layout, const gr_cache_tokens* in, int tokens,
                     const long long* slots, const int* positions, const double* frequencies, int rot, int interleaved, void* stream)
 {
@@ -895,6 +919,7 @@ int gr_cache_append(void* keys, void* values, const gr_cache_layout* layout, con
     A.heads = L.heads; A.dim = L.dim; A.block = L.block_size; A.num_blocks = L.num_blocks;
     A.x = X; A.tokens = tokens; A.slots = slots; A.positions = positions; A.freq = frequencies;
     A.half = rot / 2; A.interleaved = interleaved != 0;
+    GR_SET_SPAN(A.in_k, rows[0]); GR_SET_SPAN(A.in_v, rows[1]); GR_SET_SPAN(A.in_q, rows[2]); GR_SET_SPAN(A.out_q, rows[3]); GR_SET_SPAN(A.held_k, held[0]); GR_SET_SPAN(A.held_v, held[1]);
     const bool four = L.format == GR_Q4;
     gr::Align kv, q, c;
     kv.add(X.k, e, {X.k_token, X.k_head}); kv.add(X.v, e, {X.v_token, X.v_head});
@@ -961,6 +986,7 @@ int gr_cache_read(const void* keys, const void* values, const gr_cache_layout* l
     A.block_stride = L.block_stride; A.token_stride = L.token_stride; A.head_stride = L.head_stride;
     A.heads = L.heads; A.dim = L.dim; A.block = L.block_size; A.num_blocks = L.num_blocks;
     A.tokens = tokens; A.slots = slots;
+    GR_SET_SPAN(A.in_k, written[0]); GR_SET_SPAN(A.in_v, written[1]); GR_SET_SPAN(A.held_k, held[0]); GR_SET_SPAN(A.held_v, held[1]);
     R.k = k; R.v = v; R.k_token = k_token; R.k_head = k_head; R.v_token = v_token; R.v_head = v_head;
     gr::Align out, c;
     out.add(k, e, {k_token, k_head}); out.add(v, e, {v_token, v_head});

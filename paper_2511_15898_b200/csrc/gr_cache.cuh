@@ -32,6 +32,41 @@ template <typename T, int N> struct __align__(sizeof(T) * N) Pack { T x[N]; };
 __host__ inline bool known_type(int t) { return t == GR_F32 || t == GR_BF16 || t == GR_F16; }
 __host__ inline int type_size(int t) { return t == GR_F32 ? 4 : 2; }
 
+// The bounds-checked build (gr_common.cuh) in the kernels of caches and attention: GR_WITHIN(span, p, n) says whether n bytes at p lie in a span that the
+// arguments carry there, GR_IN_SHARED(p, n) whether in the launch's shared memory; an access elsewhere is skipped, and met by the next call of gr_cache_check
+// or gr_attend_check.  In the regular build both are true.
+struct Span { uintptr_t lo, hi; };
+#ifdef GR_CHECK
+static __device__ int g_span_check;
+__device__ __noinline__ inline bool within(Span s, const void* p, long long n)
+{
+    const uintptr_t a = (uintptr_t)p;
+    if (a >= s.lo && a + (uintptr_t)n <= s.hi) return true;
+    g_span_check = 1;
+    return false;
+}
+__device__ inline Span shared_span(const void* p)
+{
+    unsigned n;
+    asm("mov.u32 %0, %dynamic_smem_size;" : "=r"(n));
+    return {(uintptr_t)p, (uintptr_t)p + n};
+}
+// whether an access was skipped since the last call of this (-1: it cannot be read)
+static int span_check()
+{
+    int met = -1, none = 0;
+    if (cudaMemcpyFromSymbol(&met, g_span_check, sizeof(int)) != cudaSuccess || cudaMemcpyToSymbol(g_span_check, &none, sizeof(int)) != cudaSuccess) return -1;
+    return met;
+}
+#define GR_SPAN(name) ::gr::Span name
+#define GR_SET_SPAN(name, ...) ((void)((name) = __VA_ARGS__))
+#define GR_WITHIN(span, p, n) ::gr::within(span, p, n)
+#else
+#define GR_SPAN(name) static_assert(true, "")
+#define GR_SET_SPAN(name, ...) ((void)0)
+#define GR_WITHIN(span, p, n) true
+#endif
+
 // Whether places of `count` strided dimensions lie apart, each `unit` elements long.
 inline bool apart(long long unit, const long long* step, const long long* size, int count)
 {
@@ -54,7 +89,6 @@ inline bool counted(long long token, long long head, int tokens, int heads)
 }
 
 // First byte and the one behind the last of strided places.
-struct Span { uintptr_t lo, hi; };
 inline Span span_of(const void* p, long long unit, const long long* step, const long long* size, int count)
 {
     for (int i = 0; i < count; i++) { if (size[i] <= 0) return {0, 0}; unit += step[i] * (size[i] - 1); }
