@@ -508,8 +508,8 @@ int gr_cache_read(const void* keys, const void* values, const gr_cache_layout* l
  * NaN in one group of a value alone (a token whose weight is nothing beside the largest may be left out).
  * Weights and their products with the values' scales are rounded to 11 bits each, those far below the largest to 2^-35 of that.
  *   q, out    [tokens, q_heads, dim], GR_BF16 or GR_F16: (i, h) begins i * q_token + h * q_head elements after q, i * out_token + h * out_head after out.
- *             out must not meet q or the cache in memory, and no two of its places may share an element.  What lies behind the last row's
- *             tokens is left as it was.
+ *             out must not meet q or the cache in memory, and no two of its places may share an element; out, workspace and status share no byte with one
+ *             another or with what is read.  What lies behind the last row's tokens is left as it was.
  *   cache     of format GR_Q4, as in gr_cache_append.
  *   table     [rows, width] int;  offsets [rows + 1] int, ascending, 0 .. tokens;  positions [tokens] int.
  *   heads divides q_heads.  Strides of q below 2^31.  window >= 0.  |scale| < 1.7e38.  rows <= 2^20, rows * width < 2^31, width * block_size < 2^31 - 256,

@@ -1106,12 +1106,24 @@ int gr_cache_attend(const void* q, int dtype, int q_heads, long long q_token, lo
     const long long step[2] = {out_token, out_head}, size[2] = {tokens, q_heads};
     if (!gr::apart(L.dim, step, size, 2)) return GR_E_INVALID;
     if (rows == 0) return GR_OK;
-    if (!offsets || !status || !workspace || (tokens > 0 && (!q || !out || !positions)) || (width > 0 && !table)) return GR_E_NULL;
+    if (!offsets || !workspace || (tokens > 0 && (!q || !out || !positions)) || (width > 0 && !table)) return GR_E_NULL;
     if (((uintptr_t)q & 1) || ((uintptr_t)out & 1) || ((uintptr_t)workspace & 31)) return GR_E_ALIGN;
     if (((uintptr_t)table | (uintptr_t)offsets | (uintptr_t)positions | (uintptr_t)status) & 3) return GR_E_ALIGN;
     const gr::Span written = gr::rows_span(out, 2, L.dim, out_token, out_head, tokens, q_heads);
     if (gr::meet(written, gr::cache_span(cache, L))) return GR_E_INVALID;
     if (gr::meet(written, gr::rows_span(q, 2, L.dim, q_token, q_head, tokens, q_heads))) return GR_E_INVALID;
+    // (workspace and status lie apart from all, the lists from what is written; the status is looked at last)
+    const gr::Places result = gr::rows_places(out, 2, L.dim, out_token, out_head, tokens, q_heads), in = gr::rows_places(q, 2, L.dim, q_token, q_head, tokens, q_heads);
+    const gr::Places lists[3] = {gr::bytes_at(table, 4ll * rows * width), gr::bytes_at(offsets, 4ll * rows + 4), gr::bytes_at(positions, 4ll * tokens)};
+    const gr::Places own[2] = {gr::bytes_at(workspace, (long long)gr_attend_workspace_bytes(L.heads, q_heads, L.dim, rows, tokens)), gr::bytes_at(status, 4ll * rows)};
+    const gr::Span held = gr::cache_span(cache, L);
+    for (const gr::Places& l : lists) if (gr::meet(result, l)) return GR_E_INVALID;
+    for (int i = 0; i < 2; i++) {
+        if (i == 1 && !status) return GR_E_NULL;
+        const gr::Places& o = own[i];
+        for (const gr::Places& l : lists) if (gr::meet(o, l)) return GR_E_INVALID;
+        if (gr::meet(o, result) || gr::meet(o, in) || gr::meet(held, {o.at, o.at + (uintptr_t)o.unit}) || (i == 1 && gr::meet(o, own[0]))) return GR_E_INVALID;
+    }
     gr::AttendArgs A = {};
     A.q = q; A.out = out; A.q_token = q_token; A.q_head = q_head; A.out_token = out_token; A.out_head = out_head;
     A.octets = L.block_size / 8; A.num_blocks = L.num_blocks; A.block_stride = L.block_stride;
@@ -1128,10 +1140,10 @@ int gr_cache_attend(const void* q, int dtype, int q_heads, long long q_token, lo
     GR_SET_SPAN(A.places, {(uintptr_t)positions, (uintptr_t)(positions + tokens)}); GR_SET_SPAN(A.states, {(uintptr_t)status, (uintptr_t)(status + rows)});
     GR_SET_SPAN(A.room, {(uintptr_t)workspace, (uintptr_t)workspace + gr_attend_workspace_bytes(L.heads, q_heads, L.dim, rows, tokens)});
     A.ws = (char*)workspace;
-    gr::Align in, to;
-    in.add(q, 2, {tokens > 1 ? q_token : 0, q_heads > 1 ? q_head : 0});
+    gr::Align from, to;
+    from.add(q, 2, {tokens > 1 ? q_token : 0, q_heads > 1 ? q_head : 0});
     to.add(out, 2, {tokens > 1 ? out_token : 0, q_heads > 1 ? out_head : 0});
-    A.q_vec = in.bits % 16 == 0; A.out_vec = to.bits % 8 == 0;
+    A.q_vec = from.bits % 16 == 0; A.out_vec = to.bits % 8 == 0;
     cudaStream_t st = (cudaStream_t)stream;
     gr::NvtxRange whole("gr_cache_attend");
     const gr::Choice c = gr::choose(L.dim, A.group, rows, tokens);

@@ -154,3 +154,30 @@ def test_token_logprobs():
     # an output in the gap between two rows of logits
     assert call({**at, "logits": A, "entropy": A + 2 * 1000}, 1000, 1024, 4, 0, 0) == -2
     assert call({**at, "logits": A, "entropy": A + 2 * 1024 - 12}, 1000, 1024, 4, 0, 0) == -1
+
+
+def test_attend():
+    T, R, width, H, Hq, D = 6, 3, 4, 2, 4, 32
+    lay = G.CacheLayout(G.GR_Q4, H, D, 16, 5, 2 * 2 * 9 * D, 0, 0)
+    far = 1 << 36
+    size = {"q": 2 * T * Hq * D, "out": 2 * T * Hq * D, "table": 4 * R * width, "offsets": 4 * R + 4, "positions": 4 * T, "ws": G.gr_attend_workspace_bytes(H, Hq, D, R, T),
+            "status": 4 * R, "cache": 5 * 2 * 2 * 9 * D}
+    at = {n: A + (i + 1) * far for i, n in enumerate(size)}
+
+    def call(at):
+        return G.gr_cache_attend(at["q"], G.GR_F16, Hq, Hq * D, D, at["cache"], lay, at["table"], width, R, at["offsets"], at["positions"], T, 0.1, 0, at["ws"], at["out"], Hq * D, D,
+                                 at["status"], 0)
+
+    written = ("out", "ws", "status")
+    for a in written:
+        for b in size:
+            if a == b:
+                continue
+            for where, meets in ((0, True), (size[a] - 32 if size[a] >= 32 else 0, True), (size[a] + 31 & ~31, False), (-(size[b] + 31 & ~31), False)):
+                # (without a status the call answers -2 where it has found nothing)
+                moved = {**at, b: at[a] + where}
+                if "status" not in (a, b):
+                    moved["status"] = 0
+                elif not meets:
+                    continue
+                assert call(moved) == (-1 if meets else -2), (a, b, where)
