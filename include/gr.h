@@ -514,6 +514,8 @@ int gr_cache_read(const void* keys, const void* values, const gr_cache_layout* l
  *   table     [rows, width] int;  offsets [rows + 1] int, ascending, 0 .. tokens;  positions [tokens] int.
  *   heads divides q_heads.  Strides of q below 2^31.  window >= 0.  |scale| < 1.7e38.  rows <= 2^20, rows * width < 2^31, width * block_size < 2^31 - 256,
  *             tokens * (q_heads / heads) < 2^31 - 256.
+ *             The kernel is chosen by tokens / rows, room behind the last row's tokens included: give it the tokens that there are, and prompts in a
+ *             call of their own, not among rows of one token.
  *   workspace gr_attend_workspace_bytes() bytes, aligned to 32.
  *   status    out [rows]: GR_OK; GR_BAD_ROW where offsets are none, a position is beyond the table, or a block id of a token that is looked at is outside the
  *             pool (such tokens are left out); GR_CHECK_FAILED in all rows when a copy did not arrive in two seconds (out is then not to be used).

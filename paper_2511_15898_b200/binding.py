@@ -1071,7 +1071,8 @@ def cache_attend(q: torch.Tensor, cache: KVCache, table: torch.Tensor, offsets: 
     """gr_cache_attend on torch CUDA tensors: queries q [tokens, heads, dim] bfloat16 or float16 (a multiple of the cache's heads), a cache in 4
     bits, the rows' block table [rows, width] int32, and, as block_plan returns them, offsets [rows + 1] (row r's queries are
     offsets[r] .. offsets[r + 1] - 1) and positions [tokens] int32.  `scale` defaults to dim ** -0.5; with a window a query sees that many
-    tokens, itself the last.  `out`: a result of an earlier call of the same shape, written again; what lies behind the last row's tokens stays."""
+    tokens, itself the last.  The kernel is chosen by tokens / rows: fastest without room behind the last row's tokens, and with prompts in a call of their own.
+    `out`: a result of an earlier call of the same shape, written again; what lies behind the last row's tokens stays."""
     if (out is not None and out.shape[4] == cache.heads
             and _short("attend", "gr_cache_attend", q, cache.keys, cache.values, cache.block_size, cache.heads, cache.dim, table, offsets, positions,
                        scale, window, out.workspace, out.out, out.status, _entry.get("gr_attend_workspace_bytes"))):

@@ -19,12 +19,12 @@
 // make the operands of 64 tokens together and each take all of them for eight query rows.  What a CTA does not finish it leaves
 // as (m, sum, f, product) in the workspace; a second kernel joins the pieces in the order of the tokens, so results do not depend on which CTA was first.
 //
-// What bounds it.  64 rows of 6000 tokens, 8 heads of 128 dims, 4 query heads each: 107 us, 64 % of the copy rate; 81 without the arithmetic.  16
-// tokens of a head take 310 warp instructions (80 of them the shifts and ANDs of their 256 words, 20 matrix instructions), which the
+// What bounds it.  64 rows of 6000 tokens, 8 heads of 128 dims, 4 query heads each: 108 us, 63 % of the copy rate; 81 without the arithmetic.  16
+// tokens of a head take 320 warp instructions (80 of them the shifts and ANDs of their 256 words, 20 matrix instructions), which the
 // SMs issue at half of their rate, 16 warps of 128 registers each; three CTAs of 168 registers are as fast, five of 96 spill (149 us).  36 query rows
-// (nine tokens of four heads): 126 us where the bytes take 18; matrix instructions of this kind at their full rate would take 30, and it has the same
+// (nine tokens of four heads): 127 us where the bytes take 18; matrix instructions of this kind at their full rate would take 30, and it has the same
 // half of the issue slots, barriers between making operands and using them among them (four warps that each made their own for 16 query rows: 163).
-// One request of 900 tokens: 11 us, two launches and the chains of loads (offsets, positions, table, octets) before the first product.
+// One request of 900 tokens: 12 us, two launches and the chains of loads (offsets, positions, table, octets) before the first product.
 #include <math.h>
 #include <algorithm>
 #include "gr_host.h"
@@ -1046,6 +1046,8 @@ attend_join_kernel(const __grid_constant__ AttendArgs A, int tile_rows, int dim)
 
 // The kernel for a call, by a key head's query rows (a row's tokens times its group, on average): up to 8 in one tile, up to 16 in two (with heads of more
 // than 128 dims there are no registers for two); beyond, a warp for each 8.  (17 to 64 by tiles of 8 that each read the row again: 136 us for 126 at 36.)
+// The average is all that the host knows, and `tokens` counts the room behind the last row's: 64 decode rows take 105 us, with room for 64 tokens behind them
+// too, with room for 1024 383; 63 of them and a prompt of 1000 tokens in one call 670, in two 103 and 113.
 struct Choice { int nt; bool rows; int warps; };
 static Choice choose(int dim, int group, int rows, int tokens)
 {

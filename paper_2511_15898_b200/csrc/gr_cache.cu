@@ -8,9 +8,10 @@
 // one whose window its first token is in, so that a prompt's octets are written whole.
 //
 // Measured (bytes that it cannot do without, against the copy rate): 9000 tokens of 12 ragged prompts, 8 heads and 32 query heads of 128 dims,
-// fp16: 41 to 44 us, 77 to 82 %; the same keys and values from bf16 into 4 bits 36 us and out of them 16, where the bytes of both take 14: instructions bound
-// both, 250 for a row of 128 numbers of two tokens at half of the issue rate.  65536 tokens
-// out of 4 bits as bf16: 64 us, 82 %.  One token for each of 64 rows: 2.8 us, latency.
+// fp16: 38 to 41 us, 82 to 89 %; the same keys and values from bf16 into 4 bits and out of them 49 to 52, where the bytes of both take 14 (9000 tokens without
+// ragged ends 29 and 12): instructions bound both, 250 for a row of 128 numbers of two tokens at half of the issue rate.  65536 tokens
+// out of 4 bits as bf16: 64 us, 83 %; out of 16 bits 99 and out of 32 171 us, 83 and 96 %.  One token for each of 64 rows: 2.5 us into 16 bits, with
+// 32 query heads; 6.4 into 4: latency.
 #include <math.h>
 #include <algorithm>
 #include "gr_host.h"
@@ -766,8 +767,8 @@ int check_cache(const void* keys, const void* values, const gr_cache_layout* lay
 }
 
 // How a call's tokens are dealt out: windows of one token where there are few, with the heads in several CTAs until an SM has two; of `most`
-// where that leaves every SM `each`, else of eight.  (4 bits, 8 heads of 128 dims, 8 and 16 tokens, us: append 12000 38 and 41, 20000 67 and 69, 40000
-// 125 and 120, 65536 199 and 190: a CTA's time is its last wave's; read 9600 12.4 and 12.1, 65536 72 and 64.)
+// where that leaves every SM `each`, else of eight.  (4 bits, 8 heads of 128 dims, 8 and 16 tokens, us: append 12000 39 and 41, 20000 66 and 69, 40000
+// 125 and 120, 65536 201 and 189: a CTA's time is its last wave's; read 9600 12.5 and 12.7, 20000 26.5 and 24.6, 65536 72 and 66.)
 static void deal(CacheArgs& A, int rows_of_token, int most, int each)
 {
     A.window = A.tokens >= each * kSms * most ? most : A.tokens >= kCacheMany ? 8 : 1;
