@@ -153,3 +153,13 @@ def test_a_group_that_is_no_number():
             kv, table = _sink(3.0, n, 1.0, D)
             call = (q, kv, *call[2:])
             words = kv.keys.view(torch.float16)
+
+
+@pytest.mark.parametrize("D", [32, 96, 160, 192, 224])
+@pytest.mark.parametrize("group,news", [(3, 1), (4, 3), (8, 4)])
+def test_heads_of_other_sizes(D, group, news):
+    for v_size, n, gap in ((0.02, 3000, 9.5), (50.0, 1500, 6.0), (2e4, 700, 2.0)):
+        kv, table = _sink(gap, n, v_size, D, seed=D)
+        q = torch.ones(news, group, D, dtype=torch.bfloat16, device="cuda")
+        for window in (0, 333):
+            _check(q, kv, table, [0, news], list(range(n - news, n)), 1.0, window)
